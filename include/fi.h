@@ -357,6 +357,217 @@ fi_status_t fi_gemm_plan_describe(int32_t count, int64_t n_entries, int32_t num_
                                   int32_t max_batch, int32_t cta, int32_t *plan_out, int32_t *items_out,
                                   int32_t *n_items);
 
+/*
+ * ---- Attention layers behind the caches ----
+ *
+ * When the layers of the network are attention layers, the requests that a layer's cache does not freeze run the next
+ * layer (Pseudocode 1; Sec. 5 rebuilds the batch from them), and that layer needs the keys and values of their
+ * earlier tokens.  The calls below serve one such layer for the surviving requests: the page tables of the layer's
+ * key/value store are brought forward on the device (fi_pages_*), queries and keys are normed and rotated
+ * (fi_head_norm_rope), keys and values are stored in 4 bits (fi_kv_append), and the queries attend to what is stored
+ * (fi_kv_attend).  The paper has no counterpart: its networks are convolutional.  As in a cascade step the survivors come
+ * as a list of rows with a device-resident count (miss_idx and miss_count of fi_cascade_state_t), so that a step needs
+ * no host round trip.  A request that was frozen before a layer leaves no token in that layer, so every layer has its own
+ * lengths and tables.
+ *
+ * Rows: a request owns one row of `lens` and of `block_table` as long as it lives.  lens[row] = tokens of the request in
+ * this layer's store; token t lies in page block_table[row][t / page_size] at place t % page_size; its slot is
+ * page * page_size + place.  Free pages are a stack: free_pages[0 .. *free_count).
+ */
+
+typedef struct fi_pages fi_pages_t; /* opaque: geometry and commit counters of the page tables of one layer */
+
+typedef struct {
+    int32_t page_size;  /* tokens per page: a power of two, 16..1024 */
+    int32_t max_blocks; /* columns of the block table (pages a request may own), >= 1; max_blocks * page_size < 2^31 */
+    int32_t max_batch;  /* most requests of one call, 1..8192 */
+    int32_t device;
+} fi_pages_config_t;
+
+/* One step of the tables.  Pointers are device pointers; "nullable" where it says so. */
+typedef struct {
+    const int32_t *lens;        /* [rows] tokens stored before the step */
+    const int32_t *free_pages;  /* [num_pages] stack of free pages */
+    const int32_t *free_count;  /* [1] */
+    int32_t *block_table;       /* [rows x table_ld], first max_blocks columns used; entries of new pages are written in place */
+    const int32_t *row_idx;     /* [batch_max] row of each request of the step, no row twice; nullable: request i is row i */
+    const int32_t *batch_count; /* [1] requests of the step (<= batch_max); nullable: batch_max */
+    const int32_t *new_lens;    /* [batch_max] new tokens of each request; nullable: one each */
+    int64_t *slot_map;          /* out [max_tokens] slot of each new token, -1 where there is none */
+    int32_t *positions;         /* out [max_tokens] its index in this layer's store, -1 past the last token */
+    int32_t *cu_tokens;         /* out [batch_max + 1] first token of each request; constant past the actual batch */
+    int32_t *granted;           /* out [batch_max] tokens that got their place: new_lens or, when refused, 0 */
+    int32_t *lens_out;          /* out [rows] lengths after the step; may be `lens` itself */
+    int32_t *free_count_out;    /* out [1]; may be `free_count` itself */
+    int64_t table_ld;           /* leading dimension of block_table in elements, >= max_blocks */
+    int32_t rows;
+    int32_t num_pages;
+    int32_t batch_max;          /* 0..max_batch of the handle */
+    int32_t max_tokens;         /* entries of slot_map and positions */
+} fi_pages_extend_t;
+
+/*
+ * fi_pages_extend: place new_lens[i] new tokens behind the lens[row] stored ones of every request of the step, and
+ * lay the new tokens of all requests end to end (request order): token cu_tokens[i] + j is the j-th new one of request i.
+ * Missing pages are popped from the end of the free stack, in request order.  A request is refused, and keeps its length,
+ * when its tokens would need more than max_blocks pages, when they would end past max_tokens, or when it needs pages and
+ * the pages wanted by it and by the requests before it exceed the free ones; refused requests keep their places in
+ * cu_tokens and positions, with slot -1.  Nothing of a refused request is written to the tables.
+ * Rows outside [0, rows) and negative lengths are treated as requests without tokens.  Calls of one handle share its
+ * counters and must be ordered on one stream.  Asynchronous; no wait on the device, no atomics on results: the same
+ * inputs give the same tables.
+ * Errors: INVALID_ARG (null pointers, sizes, a batch above max_batch), CUDA.
+ */
+fi_status_t fi_pages_create(const fi_pages_config_t *cfg, fi_pages_t **out);
+fi_status_t fi_pages_destroy(fi_pages_t *pages);
+fi_status_t fi_pages_extend(fi_pages_t *pages, const fi_pages_extend_t *step, void *cuda_stream);
+
+/*
+ * fi_pages_release: give the pages of the listed rows (requests that ended) back to the free stack, in list order, and
+ * set their length to 0.  row_idx [batch_max], batch_count nullable, lens_out / free_count_out as in fi_pages_extend.
+ * free_pages is written behind *free_count; the block table is only read (its entries past a row's length mean
+ * nothing).  A row must not be listed twice.  Errors as fi_pages_extend.
+ */
+fi_status_t fi_pages_release(fi_pages_t *pages, const int32_t *row_idx, int32_t batch_max, const int32_t *batch_count,
+                             const int32_t *lens, int32_t rows, const int32_t *block_table, int64_t table_ld,
+                             int32_t *free_pages, int32_t num_pages, const int32_t *free_count, int32_t *lens_out,
+                             int32_t *free_count_out, void *cuda_stream);
+
+/*
+ * Norm and rotation of queries and keys, each head by itself, in one pass:
+ *   n = x / sqrt(mean(x^2) + eps);  z = n * weight;  y = R(position) z
+ * R turns the pairs of the first rot_dim values of a head by the angles of the row `position` of the table `rope`
+ * [max_pos x rot_dim] float: rot_dim / 2 cosines, then rot_dim / 2 sines; pair i is (z[i], z[i + rot_dim / 2]), or
+ * (z[2i], z[2i + 1]) with interleaved != 0.  The other values pass unturned.  Arithmetic in fp32, rounded once.
+ *   q [tokens x q_heads x head_dim], k [tokens x k_heads x head_dim]: dtype float32 or bfloat16, strides in elements
+ *   between tokens and between heads (heads may be slices of one projection's output); q_out / k_out likewise, and
+ *   they may be q / k themselves.  q_weight, k_weight [head_dim] float, nullable (ones).  positions [tokens] int32; a
+ *   position outside [0, max_pos) gives NaN (the table is not read there).
+ *   tokens_dev [1] device int32, nullable: actual number of tokens (<= tokens); later rows are left untouched.
+ * Pointers and strides are multiples of 16 bytes; head_dim and rot_dim multiples of 16, 16 <= head_dim <= 256,
+ * 0 <= rot_dim <= head_dim; q_heads >= 1, k_heads >= 0.  Asynchronous, on the current device.
+ *
+ * fi_head_norm_rope_backward: gradients for dy = (dq_out, dk_out), from the same x (nothing of the forward is kept):
+ *   g = R^T dy;  dx = (g * weight - n * mean(g * weight * n)) / sqrt(mean(x^2) + eps);  dweight = sum over tokens and heads of g * n
+ * dq / dk may be dq_out / dk_out themselves.  dq_weight, dk_weight [head_dim] float, overwritten, nullable; the sums run
+ * in a fixed order.  `workspace`: fi_head_norm_rope_workspace(head_dim) bytes of device memory, contents free, not
+ * shared by calls that overlap; may be null when both weight gradients are.
+ */
+typedef struct {
+    const void *q, *k;          /* inputs of the forward pass; k nullable when k_heads = 0 */
+    void *q_out, *k_out;        /* forward: results.  backward: dq, dk */
+    const void *dq_out, *dk_out;/* backward only: gradients of the results */
+    const float *q_weight, *k_weight;
+    const float *rope;          /* nullable when rot_dim = 0 */
+    const int32_t *positions;   /* nullable when rot_dim = 0 */
+    const int32_t *tokens_dev;  /* nullable */
+    float *dq_weight, *dk_weight; /* backward only */
+    void *workspace;            /* backward only */
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+    int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+    int64_t dq_out_token_stride, dq_out_head_stride, dk_out_token_stride, dk_out_head_stride; /* backward only */
+    int64_t tokens;
+    int32_t q_heads, k_heads, head_dim, rot_dim;
+    int32_t max_pos;
+    int32_t interleaved;
+    int32_t dtype;              /* fi_dtype_t */
+    float eps;
+} fi_head_norm_rope_t;
+fi_status_t fi_head_norm_rope(const fi_head_norm_rope_t *args, void *cuda_stream);
+fi_status_t fi_head_norm_rope_backward(const fi_head_norm_rope_t *args, void *cuda_stream);
+int64_t fi_head_norm_rope_workspace(int32_t head_dim);
+
+/*
+ * Keys and values of one layer in 4 bits.  A vector (one token, one head) is stored as head_dim / 2 bytes of codes, byte j
+ * holding value 2j in its low and value 2j + 1 in its high half, and a pair of bfloat16 (scale, offset); the value is
+ * code * scale + offset.  fi_kv_append chooses, from the vector's least and largest value,
+ *   offset = min rounded down to bf16,  scale = max((max - offset) / 15 rounded up to bf16, 2^-40),
+ *   code = round((x - offset) / scale), ties to even
+ * in fp32, so every value lies in the range and is off by half a scale at most.  A vector with a NaN or an infinity is stored with
+ * offset NaN (it reads as NaN).
+ * The pools are the caller's: codes [num_pages][kv_heads][page_size][head_dim / 2] bytes and meta
+ * [num_pages][kv_heads][page_size] bf16 pairs, with free strides between pages, heads and tokens, the same for keys
+ * and values (bytes for codes, multiples of 16; pairs for meta).
+ * fi_kv_create keeps geometry and pointers and owns the scratch of fi_kv_attend (partial results of requests whose keys
+ * are cut over several CTAs: 32 KiB to 256 KiB per CTA slot, at most 8 CTAs per SM) and a status word.
+ */
+typedef struct fi_kv fi_kv_t;
+
+typedef struct {
+    void *k_codes, *v_codes;   /* device, 16-byte aligned */
+    void *k_meta, *v_meta;     /* device, 4-byte aligned */
+    int64_t page_stride, head_stride, token_stride;                /* codes, bytes */
+    int64_t meta_page_stride, meta_head_stride, meta_token_stride; /* meta, pairs */
+    int32_t num_pages;
+    int32_t page_size;         /* a power of two, 16..1024 */
+    int32_t q_heads;           /* a multiple of kv_heads */
+    int32_t kv_heads;
+    int32_t head_dim;          /* 64, 128, 192 or 256 */
+    int32_t device;
+} fi_kv_config_t;
+
+fi_status_t fi_kv_create(const fi_kv_config_t *cfg, fi_kv_t **out);
+fi_status_t fi_kv_destroy(fi_kv_t *kv);
+
+/*
+ * Store the keys and values of `tokens` new tokens at their slots (slot_map of fi_pages_extend; a negative slot is
+ * skipped, one past the pool is skipped and reported by fi_kv_poll_status).  k, v [tokens x kv_heads x head_dim], float32 or
+ * bfloat16 (`dtype`), strides in elements, pointers and strides multiples of 16 bytes.  tokens_dev as in
+ * fi_head_norm_rope.  k_stored, v_stored [tokens x kv_heads x head_dim] contiguous, same dtype, nullable: what the codes
+ * stand for, rounded to the dtype (also for skipped slots).  A slot must not be listed twice.  Asynchronous.
+ */
+typedef struct {
+    const void *k, *v;
+    const int64_t *slot_map;
+    const int32_t *tokens_dev;  /* nullable */
+    void *k_stored, *v_stored;  /* nullable */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    int64_t tokens;
+    int32_t dtype;
+} fi_kv_append_t;
+fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *args, void *cuda_stream);
+
+/*
+ * Attention of new tokens over the stored keys and values.  Request i (row row_idx[i]) has n = cu_tokens[i + 1] -
+ * cu_tokens[i] queries, the last n of its lens[row] tokens (which are stored already): query j stands at position
+ * lens[row] - n + j and sees the keys at positions up to its own, with window > 0 only the last `window` of them.
+ *   out = softmax(scale * q . k) v,  q_heads / kv_heads query heads share a key head
+ * A query that sees no key (a position below 0) gets zeros, and -inf as lse.
+ *   q, out [max_tokens x q_heads x head_dim], float32 or bfloat16, strides in elements, multiples of 16 bytes;
+ *   lse [max_tokens x q_heads] float, contiguous, nullable: natural logarithm of the softmax sum
+ *   cu_tokens nullable: one query per request, token i of request i; max_query: most queries of a request (a hint
+ *   that chooses the kernel: any number is computed correctly)
+ * Softmax statistics and sums in fp32; products on tensor cores with the codes exact and, for float32 queries, with
+ * queries and probabilities as pairs of half-precision numbers.  Tokens past cu_tokens' end are left untouched.  Page
+ * numbers outside the pool hide their tokens and are reported by fi_kv_poll_status.  Asynchronous; calls of one
+ * handle share its scratch and must be ordered on one stream.
+ */
+typedef struct {
+    const void *q;
+    void *out;
+    float *lse;                  /* nullable */
+    const int32_t *lens;         /* [rows] */
+    const int32_t *block_table;  /* [rows x table_ld] */
+    const int32_t *row_idx;      /* [batch_max] nullable */
+    const int32_t *batch_count;  /* [1] nullable */
+    const int32_t *cu_tokens;    /* [batch_max + 1] nullable */
+    int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+    int64_t table_ld;
+    int32_t rows;
+    int32_t max_blocks;          /* columns of the block table that may be read */
+    int32_t batch_max;
+    int32_t max_tokens;          /* tokens of q and out */
+    int32_t max_query;
+    int32_t window;              /* 0: all earlier keys */
+    int32_t dtype;
+    float scale;
+} fi_kv_attend_t;
+fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *args, void *cuda_stream);
+
+/* Synchronise the device; FI_ERR_INVALID_ARG when a kernel of this handle met a slot or a page outside the pool since the
+ * last poll (the word is cleared), FI_OK otherwise. */
+fi_status_t fi_kv_poll_status(fi_kv_t *kv);
+
 /* Number of kernels this library has launched in the calling process (all caches). */
 int64_t fi_launch_count(void);
 

@@ -28,7 +28,10 @@ EXPORTS = ["fi_cache_create", "fi_cache_destroy", "fi_cache_insert", "fi_cache_s
            "fi_projection_create", "fi_projection_destroy", "fi_projection_set_weights", "fi_projection_apply", "fi_projection_poll_status", "fi_projection_set_profiling",
            "fi_projection_read_profile",
            "fi_cascade_step_projected", "fi_cache_set_repair", "fi_cache_read_certificate",
-           "fi_cache_read_slot_certificates", "fi_cache_lookup_view", "fi_cache_set_sm_limit", "fi_gemm_plan_describe", "fi_launch_count", "fi_last_error", "fi_status_string"]
+           "fi_cache_read_slot_certificates", "fi_cache_lookup_view", "fi_cache_set_sm_limit", "fi_gemm_plan_describe",
+           "fi_pages_create", "fi_pages_destroy", "fi_pages_extend", "fi_pages_release", "fi_head_norm_rope",
+           "fi_head_norm_rope_backward", "fi_head_norm_rope_workspace", "fi_kv_create", "fi_kv_destroy", "fi_kv_append",
+           "fi_kv_attend", "fi_kv_poll_status", "fi_launch_count", "fi_last_error", "fi_status_string"]
 
 
 class fi_cache_config_t(ctypes.Structure):
@@ -47,6 +50,46 @@ class fi_cascade_state_t(ctypes.Structure):
     _fields_ = [("active_idx", ctypes.c_void_p), ("active_count", ctypes.c_void_p), ("miss_idx", ctypes.c_void_p),
                 ("miss_count", ctypes.c_void_p), ("final_label", ctypes.c_void_p), ("exit_stage", ctypes.c_void_p),
                 ("final_conf", ctypes.c_void_p), ("stage", ctypes.c_int32), ("batch0", ctypes.c_int32)]
+
+
+def _fields(kind, names: str):
+    return [(n, kind) for n in names.split()]
+
+
+class fi_pages_config_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_int32, "page_size max_blocks max_batch device")
+
+
+class fi_pages_extend_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "lens free_pages free_count block_table row_idx batch_count new_lens slot_map "
+                                        "positions cu_tokens granted lens_out free_count_out") \
+        + [("table_ld", ctypes.c_int64)] + _fields(ctypes.c_int32, "rows num_pages batch_max max_tokens")
+
+
+class fi_head_norm_rope_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "q k q_out k_out dq_out dk_out q_weight k_weight rope positions tokens_dev "
+                                        "dq_weight dk_weight workspace") \
+        + _fields(ctypes.c_int64, "q_token_stride q_head_stride k_token_stride k_head_stride q_out_token_stride "
+                                  "q_out_head_stride k_out_token_stride k_out_head_stride dq_out_token_stride "
+                                  "dq_out_head_stride dk_out_token_stride dk_out_head_stride tokens") \
+        + _fields(ctypes.c_int32, "q_heads k_heads head_dim rot_dim max_pos interleaved dtype") + [("eps", ctypes.c_float)]
+
+
+class fi_kv_config_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "k_codes v_codes k_meta v_meta") \
+        + _fields(ctypes.c_int64, "page_stride head_stride token_stride meta_page_stride meta_head_stride meta_token_stride") \
+        + _fields(ctypes.c_int32, "num_pages page_size q_heads kv_heads head_dim device")
+
+
+class fi_kv_append_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "k v slot_map tokens_dev k_stored v_stored") \
+        + _fields(ctypes.c_int64, "k_token_stride k_head_stride v_token_stride v_head_stride tokens") + [("dtype", ctypes.c_int32)]
+
+
+class fi_kv_attend_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "q out lse lens block_table row_idx batch_count cu_tokens") \
+        + _fields(ctypes.c_int64, "q_token_stride q_head_stride out_token_stride out_head_stride table_ld") \
+        + _fields(ctypes.c_int32, "rows max_blocks batch_max max_tokens max_query window dtype") + [("scale", ctypes.c_float)]
 
 
 class FiError(RuntimeError):
@@ -110,6 +153,20 @@ def load_library(path: Optional[str] = None):
     lib.fi_gemm_plan_describe.argtypes = [i32, i64, i32, i32, i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32),
                                           ctypes.POINTER(i32)]
     lib.fi_gemm_plan_describe.restype = i32
+    ptr = ctypes.POINTER
+    lib.fi_pages_create.argtypes = [ptr(fi_pages_config_t), ptr(vp)]
+    lib.fi_pages_destroy.argtypes = [vp]
+    lib.fi_pages_extend.argtypes = [vp, ptr(fi_pages_extend_t), vp]
+    lib.fi_pages_release.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, vp, i32, vp, vp, vp, vp]
+    lib.fi_head_norm_rope.argtypes = [ptr(fi_head_norm_rope_t), vp]
+    lib.fi_head_norm_rope_backward.argtypes = [ptr(fi_head_norm_rope_t), vp]
+    lib.fi_head_norm_rope_workspace.argtypes = [i32]
+    lib.fi_head_norm_rope_workspace.restype = i64
+    lib.fi_kv_create.argtypes = [ptr(fi_kv_config_t), ptr(vp)]
+    lib.fi_kv_destroy.argtypes = [vp]
+    lib.fi_kv_append.argtypes = [vp, ptr(fi_kv_append_t), vp]
+    lib.fi_kv_attend.argtypes = [vp, ptr(fi_kv_attend_t), vp]
+    lib.fi_kv_poll_status.argtypes = [vp]
     lib.fi_launch_count.argtypes = []
     lib.fi_launch_count.restype = i64
     lib.fi_last_error.argtypes = []
@@ -514,3 +571,291 @@ def cascade_run_host(caches: Sequence[FreezeCache], acts_host: Sequence[torch.Te
     ap = (ctypes.c_void_p * n)(*[a.data_ptr() for a in acts_host])
     _check(load_library().fi_cascade_run_host(hs, n, ap, batch0, _dp(final_label), _dp(exit_stage), _dp(final_conf),
                                               _dp(arrivals), _stream_ptr(caches[0].device)))
+
+
+# ---- attention layers behind the caches ----
+
+_FI_DTYPE = {torch.float32: FI_F32, torch.bfloat16: FI_BF16}
+
+
+def _check_int(t: Optional[torch.Tensor], name: str, device, dtype=torch.int32, at_least: int = 0) -> None:
+    if t is None:
+        return
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < at_least:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device} with at least {at_least} entries")
+
+
+def _check_heads(t: torch.Tensor, name: str, device, dtype, tokens: int, head_dim: int, heads: Optional[int] = None) -> None:
+    if t.dim() != 3 or t.dtype != dtype or t.device != device or t.shape[0] != tokens or t.shape[2] != head_dim \
+            or t.stride(2) != 1 or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [tokens, heads, head_dim] on {device} in {dtype}, values of a head side by side")
+
+
+class ExtendOut:
+    """What KvTables.extend gives (torch owns the memory): slot_map [max_tokens] int64, positions [max_tokens], cu_tokens
+    [batch + 1], granted [batch], lens [rows] and free_count [1] int32."""
+
+    def __init__(self, batch: int, max_tokens: int, rows: int, device):
+        self.slot_map = torch.empty(max_tokens, dtype=torch.int64, device=device)
+        # one block of memory for the small ones
+        words = torch.empty(max_tokens + 2 * batch + 1 + rows + 1, dtype=torch.int32, device=device)
+        self.positions, self.cu_tokens, self.granted, self.lens, self.free_count = words.split(
+            [max_tokens, batch + 1, batch, rows, 1])
+
+
+class KvTables:
+    """Page tables of one layer's key/value store: fi_pages_*."""
+
+    def __init__(self, *, page_size: int, max_blocks: int, max_batch: int = 1024, device: int = 0):
+        self._lib = load_library()
+        self._h = ctypes.c_void_p()
+        self.page_size, self.max_blocks, self.max_batch = page_size, max_blocks, max_batch
+        self.device = torch.device("cuda", device)
+        cfg = fi_pages_config_t(page_size, max_blocks, max_batch, device)
+        _check(self._lib.fi_pages_create(ctypes.byref(cfg), ctypes.byref(self._h)))
+
+    # -- fi_pages_destroy
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.fi_pages_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check_table(self, lens, free_pages, free_count, block_table) -> None:
+        _check_int(lens, "lens", self.device)
+        _check_int(free_pages, "free_pages", self.device)
+        _check_int(free_count, "free_count", self.device, at_least=1)
+        if block_table.dtype != torch.int32 or block_table.device != self.device or block_table.dim() != 2 \
+                or block_table.shape[0] < lens.numel() or block_table.shape[1] < self.max_blocks or block_table.stride(1) != 1:
+            raise ValueError("block_table must be int32 [rows, max_blocks] on the tables' device, a row for each entry of lens")
+
+    # -- fi_pages_extend
+    def extend(self, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor, *,
+               new_lens: Optional[torch.Tensor] = None, row_idx: Optional[torch.Tensor] = None,
+               batch_count: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None,
+               out: Optional[ExtendOut] = None) -> ExtendOut:
+        """Places the step's new tokens (new_lens, or one per request) behind the stored ones.  block_table is written in
+        place; lens and free_count stay as they are unless `out` holds them."""
+        self._check_table(lens, free_pages, free_count, block_table)
+        rows = lens.numel()
+        batch = row_idx.numel() if row_idx is not None else rows
+        _check_int(row_idx, "row_idx", self.device)
+        _check_int(batch_count, "batch_count", self.device, at_least=1)
+        _check_int(new_lens, "new_lens", self.device, at_least=batch)
+        if max_tokens is None:
+            if new_lens is not None:
+                raise ValueError("max_tokens is needed with new_lens")
+            max_tokens = batch
+        if out is None:
+            out = ExtendOut(batch, max_tokens, rows, self.device)
+        else:
+            _check_int(out.slot_map, "out.slot_map", self.device, torch.int64, max_tokens)
+            for name, n in (("positions", max_tokens), ("cu_tokens", batch + 1), ("granted", batch), ("lens", rows), ("free_count", 1)):
+                _check_int(getattr(out, name), "out." + name, self.device, at_least=n)
+        st = fi_pages_extend_t(_dp(lens), _dp(free_pages), _dp(free_count), _dp(block_table), _dp(row_idx), _dp(batch_count),
+                               _dp(new_lens), _dp(out.slot_map), _dp(out.positions), _dp(out.cu_tokens), _dp(out.granted),
+                               _dp(out.lens), _dp(out.free_count), block_table.stride(0), rows, free_pages.numel(), batch, max_tokens)
+        _check(self._lib.fi_pages_extend(self._h, ctypes.byref(st), _stream_ptr(self.device)))
+        return out
+
+    # -- fi_pages_release
+    def release(self, row_idx: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                block_table: torch.Tensor, *, batch_count: Optional[torch.Tensor] = None,
+                out: Optional[Sequence[torch.Tensor]] = None):
+        """Gives the pages of the listed rows back (free_pages is written in place); returns (lens, free_count) after it.  `out` may be
+        (lens, free_count) themselves."""
+        self._check_table(lens, free_pages, free_count, block_table)
+        _check_int(row_idx, "row_idx", self.device)
+        _check_int(batch_count, "batch_count", self.device, at_least=1)
+        lens_out, count_out = out if out is not None else (torch.empty_like(lens), torch.empty_like(free_count))
+        _check_int(lens_out, "out[0]", self.device, at_least=lens.numel())
+        _check_int(count_out, "out[1]", self.device, at_least=1)
+        _check(self._lib.fi_pages_release(self._h, _dp(row_idx), row_idx.numel(), _dp(batch_count), _dp(lens), lens.numel(),
+                                          _dp(block_table), block_table.stride(0), _dp(free_pages), free_pages.numel(),
+                                          _dp(free_count), _dp(lens_out), _dp(count_out), _stream_ptr(self.device)))
+        return lens_out, count_out
+
+
+def _norm_rope_struct(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count) -> fi_head_norm_rope_t:
+    dev, (tokens, q_heads, head_dim) = q.device, q.shape
+    if q.dtype not in _FI_DTYPE:
+        raise ValueError("q must be float32 or bfloat16")
+    _check_heads(q, "q", dev, q.dtype, tokens, head_dim)
+    if k is not None:
+        _check_heads(k, "k", dev, q.dtype, tokens, head_dim)
+    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _check_int(w, name, dev, torch.float32, head_dim)
+    rot = 0
+    if rope is not None:
+        if rope.dim() != 2 or rope.dtype != torch.float32 or rope.device != dev or not rope.is_contiguous():
+            raise ValueError("rope must be a contiguous float32 [max_pos, rot_dim] tensor on q's device")
+        if positions is None:
+            raise ValueError("rope needs positions")
+        rot = rope.shape[1]
+        _check_int(positions, "positions", dev, at_least=tokens)
+    _check_int(count, "count", dev, at_least=1)
+    st = fi_head_norm_rope_t()
+    st.q, st.k, st.q_weight, st.k_weight = _dp(q), _dp(k), _dp(q_weight), _dp(k_weight)
+    st.rope, st.positions, st.tokens_dev = _dp(rope), _dp(positions), _dp(count)
+    st.q_token_stride, st.q_head_stride = q.stride(0), q.stride(1)
+    if k is not None:
+        st.k_token_stride, st.k_head_stride, st.k_heads = k.stride(0), k.stride(1), k.shape[1]
+    st.tokens, st.q_heads, st.head_dim, st.rot_dim = tokens, q_heads, head_dim, rot
+    st.max_pos, st.interleaved = (rope.shape[0] if rot else 0), 1 if interleaved else 0
+    st.dtype, st.eps = _FI_DTYPE[q.dtype], float(eps)
+    return st
+
+
+def _set_results(st, q, k, q_out, k_out):
+    """Result tensors of the shapes of q and k (made here when not given), entered into the struct."""
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    _check_heads(q_out, "q result", q.device, q.dtype, q.shape[0], q.shape[2], q.shape[1])
+    st.q_out, st.q_out_token_stride, st.q_out_head_stride = _dp(q_out), q_out.stride(0), q_out.stride(1)
+    if k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        _check_heads(k_out, "k result", k.device, k.dtype, k.shape[0], k.shape[2], k.shape[1])
+        st.k_out, st.k_out_token_stride, st.k_out_head_stride = _dp(k_out), k_out.stride(0), k_out.stride(1)
+    return q_out, k_out
+
+
+def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
+                   k_weight: Optional[torch.Tensor], rope: Optional[torch.Tensor], positions: Optional[torch.Tensor], *,
+                   eps: float = 1e-6, interleaved: bool = False, count: Optional[torch.Tensor] = None,
+                   q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """fi_head_norm_rope: (q, k) normed head by head and turned to their positions.  q_out / k_out may be q / k."""
+    st = _norm_rope_struct(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count)
+    q_out, k_out = _set_results(st, q, k, q_out, k_out)
+    with torch.cuda.device(q.device):
+        _check(load_library().fi_head_norm_rope(ctypes.byref(st), _stream_ptr(q.device)))
+    return q_out, k_out
+
+
+def head_norm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
+                            k_weight: Optional[torch.Tensor], rope: Optional[torch.Tensor], positions: Optional[torch.Tensor],
+                            dq_out: torch.Tensor, dk_out: Optional[torch.Tensor], *, eps: float = 1e-6,
+                            interleaved: bool = False, count: Optional[torch.Tensor] = None,
+                            dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None):
+    """fi_head_norm_rope_backward: (dq, dk, dq_weight, dk_weight) from the forward pass's inputs and the gradients of its
+    results.  The gradient of a weight that is None is None."""
+    st = _norm_rope_struct(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count)
+    dev, head_dim = q.device, q.shape[2]
+    _check_heads(dq_out, "dq_out", dev, q.dtype, q.shape[0], head_dim, q.shape[1])
+    st.dq_out, st.dq_out_token_stride, st.dq_out_head_stride = _dp(dq_out), dq_out.stride(0), dq_out.stride(1)
+    if k is not None:
+        _check_heads(dk_out, "dk_out", dev, k.dtype, k.shape[0], head_dim, k.shape[1])
+        st.dk_out, st.dk_out_token_stride, st.dk_out_head_stride = _dp(dk_out), dk_out.stride(0), dk_out.stride(1)
+    dq, dk = _set_results(st, q, k, dq, dk)
+    dqw = torch.empty(head_dim, dtype=torch.float32, device=dev) if q_weight is not None else None
+    dkw = torch.empty(head_dim, dtype=torch.float32, device=dev) if k_weight is not None and k is not None else None
+    lib = load_library()
+    work = None
+    if dqw is not None or dkw is not None:
+        work = torch.empty(lib.fi_head_norm_rope_workspace(head_dim), dtype=torch.uint8, device=dev)
+    st.dq_weight, st.dk_weight, st.workspace = _dp(dqw), _dp(dkw), _dp(work)
+    with torch.cuda.device(dev):
+        _check(lib.fi_head_norm_rope_backward(ctypes.byref(st), _stream_ptr(dev)))
+    return dq, dk, dqw, dkw
+
+
+class KvCache:
+    """Keys and values of one layer in 4 bits (fi_kv_*) over pools the caller owns: codes uint8 [pages, kv_heads, page_size,
+    head_dim / 2], meta bfloat16 [pages, kv_heads, page_size, 2] (scale, offset)."""
+
+    def __init__(self, k_codes: torch.Tensor, k_meta: torch.Tensor, v_codes: torch.Tensor, v_meta: torch.Tensor, *, q_heads: int):
+        self._lib = load_library()
+        self._h = ctypes.c_void_p()
+        dev = k_codes.device
+        if k_codes.dim() != 4 or dev.type != "cuda":
+            raise ValueError("k_codes must be uint8 [pages, kv_heads, page_size, head_dim / 2] on a GPU")
+        pages, heads, page, half = k_codes.shape
+        for codes, meta in ((k_codes, k_meta), (v_codes, v_meta)):
+            if codes.dtype != torch.uint8 or codes.shape != k_codes.shape or codes.device != dev or codes.stride() != k_codes.stride() \
+                    or codes.stride(3) != 1:
+                raise ValueError("codes must be uint8 tensors of one shape and layout, bytes of a vector side by side")
+            if meta.dtype != torch.bfloat16 or tuple(meta.shape) != (pages, heads, page, 2) or meta.device != dev \
+                    or meta.stride() != k_meta.stride() or meta.stride(3) != 1 or any(s % 2 for s in meta.stride()[:3]):
+                raise ValueError("meta must be bfloat16 [pages, kv_heads, page_size, 2] tensors of one layout, pairs side by side")
+        self.k_codes, self.k_meta, self.v_codes, self.v_meta = k_codes, k_meta, v_codes, v_meta   # kept alive
+        self.device, self.pages, self.kv_heads, self.page_size, self.head_dim = dev, pages, heads, page, 2 * half
+        self.q_heads = q_heads
+        cs, ms = k_codes.stride(), k_meta.stride()
+        cfg = fi_kv_config_t(_dp(k_codes), _dp(v_codes), _dp(k_meta), _dp(v_meta), cs[0], cs[1], cs[2], ms[0] // 2, ms[1] // 2,
+                             ms[2] // 2, pages, page, q_heads, heads, 2 * half, dev.index or 0)
+        _check(self._lib.fi_kv_create(ctypes.byref(cfg), ctypes.byref(self._h)))
+
+    # -- fi_kv_destroy
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.fi_kv_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- fi_kv_poll_status
+    def poll_status(self) -> None:
+        _check(self._lib.fi_kv_poll_status(self._h))
+
+    # -- fi_kv_append
+    def append(self, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, *, count: Optional[torch.Tensor] = None,
+               with_stored: bool = False):
+        """Stores keys and values [tokens, kv_heads, head_dim] at their slots; with with_stored returns what the codes stand
+        for, in k's dtype."""
+        tokens = k.shape[0]
+        if k.dtype not in _FI_DTYPE:
+            raise ValueError("k must be float32 or bfloat16")
+        _check_heads(k, "k", self.device, k.dtype, tokens, self.head_dim, self.kv_heads)
+        _check_heads(v, "v", self.device, k.dtype, tokens, self.head_dim, self.kv_heads)
+        _check_int(slot_map, "slot_map", self.device, torch.int64, tokens)
+        _check_int(count, "count", self.device, at_least=1)
+        ks = vs = None
+        if with_stored:
+            ks, vs = (torch.empty(k.shape, dtype=k.dtype, device=self.device) for _ in range(2))
+        st = fi_kv_append_t(_dp(k), _dp(v), _dp(slot_map), _dp(count), _dp(ks), _dp(vs), k.stride(0), k.stride(1), v.stride(0),
+                            v.stride(1), tokens, _FI_DTYPE[k.dtype])
+        _check(self._lib.fi_kv_append(self._h, ctypes.byref(st), _stream_ptr(self.device)))
+        return (ks, vs) if with_stored else None
+
+    # -- fi_kv_attend
+    def attend(self, q: torch.Tensor, lens: torch.Tensor, block_table: torch.Tensor, *, cu_tokens: Optional[torch.Tensor] = None,
+               row_idx: Optional[torch.Tensor] = None, batch_count: Optional[torch.Tensor] = None, max_query: int = 1,
+               window: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False,
+               lse: Optional[torch.Tensor] = None):
+        """Attention of q [tokens, q_heads, head_dim] (the last tokens of each request, which are stored already) over the
+        stored keys and values; scale defaults to 1 / sqrt(head_dim).  Returns out, or (out, lse)."""
+        tokens = q.shape[0]
+        if q.dtype not in _FI_DTYPE:
+            raise ValueError("q must be float32 or bfloat16")
+        _check_heads(q, "q", self.device, q.dtype, tokens, self.head_dim, self.q_heads)
+        _check_int(lens, "lens", self.device)
+        rows = lens.numel()
+        if block_table.dtype != torch.int32 or block_table.device != self.device or block_table.dim() != 2 \
+                or block_table.shape[0] < rows or block_table.stride(1) != 1:
+            raise ValueError("block_table must be int32 [rows, blocks] on the cache's device, a row for each entry of lens")
+        _check_int(row_idx, "row_idx", self.device)
+        _check_int(batch_count, "batch_count", self.device, at_least=1)
+        batch = row_idx.numel() if row_idx is not None else rows
+        _check_int(cu_tokens, "cu_tokens", self.device, at_least=batch + 1)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        else:
+            _check_heads(out, "out", self.device, q.dtype, tokens, self.head_dim, self.q_heads)
+        if lse is None and with_lse:
+            lse = torch.empty(tokens, self.q_heads, dtype=torch.float32, device=self.device)
+        elif lse is not None:
+            _check_int(lse, "lse", self.device, torch.float32, tokens * self.q_heads)
+        st = fi_kv_attend_t(_dp(q), _dp(out), _dp(lse), _dp(lens), _dp(block_table), _dp(row_idx), _dp(batch_count), _dp(cu_tokens),
+                            q.stride(0), q.stride(1), out.stride(0), out.stride(1), block_table.stride(0), rows,
+                            block_table.shape[1], batch, tokens, int(max_query), int(window), _FI_DTYPE[q.dtype],
+                            self.head_dim ** -0.5 if scale is None else float(scale))
+        _check(self._lib.fi_kv_attend(self._h, ctypes.byref(st), _stream_ptr(self.device)))
+        return out if lse is None else (out, lse)

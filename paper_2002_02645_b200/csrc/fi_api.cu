@@ -14,25 +14,6 @@ namespace {
 thread_local char g_err[512] = "";
 std::atomic<long long> g_launches{0};
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
-
-fi_status_t cuda_fail(cudaError_t e, const char *what) {
-    set_error("%s: %s", what, cudaGetErrorString(e));
-    cudaGetLastError();
-    return e == cudaErrorMemoryAllocation ? FI_ERR_OOM : FI_ERR_CUDA;
-}
-
 __global__ void fill_f32_kernel(float *p, int64_t n, float v) {
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) p[i] = v;
 }
@@ -255,6 +236,12 @@ void set_error(const char *fmt, ...) {
 }
 
 void count_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
+
+fi_status_t cuda_fail(cudaError_t e, const char *what) {
+    set_error("%s: %s", what, cudaGetErrorString(e));
+    cudaGetLastError();
+    return e == cudaErrorMemoryAllocation ? FI_ERR_OOM : FI_ERR_CUDA;
+}
 
 fi_status_t check_launch(const char *what) {
     cudaError_t e = cudaGetLastError();

@@ -1,0 +1,890 @@
+// Attention over keys and values held in 4 bits.
+//
+// With k = n s_k + m_k and v = n' s_v + m_v (codes n, n' in 0..15; one scale and offset per token and key head)
+//   x_t = scale log2(e) (s_k (q . n) + m_k sum(q)),   out = sum_t p_t (s_v n' + m_v) / sum_t p_t,   p_t = 2^(x_t - max)
+// so scales and offsets never touch the codes: the products run on the codes themselves, and the offset of v is one
+// sum per query row.  The scale of v goes into the exponent: with y_t = x_t + log2(s_v) and M >= max y - 8, the weight
+// P_t = 2^(y_t - M) multiplies n' directly, sum p_t = sum P_t / s_v and the offset's part is sum P_t m_v / s_v.
+//
+// A code is a half-precision number without any conversion: a 16-bit word that holds only the four bits n is the
+// subnormal n 2^-24 (n 2^-20 when it sits in the next four bits), which the tensor cores multiply exactly.  Eight codes
+// cost one shift and four masks; the powers of two are taken back once per row.
+//
+// Codes are all positive, so the product part and the offset part are larger than what they add up to.  The offset part
+// therefore takes the weights as they were rounded for the product, and float32 queries, which must not lose what the parts have in
+// common, take the codes less 7.5 (one more instruction per two codes) and offsets moved by 7.5 scales.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "fi_internal.cuh"
+
+namespace fi {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kUnit = 128;                 // keys a CTA takes per step: 32 per warp
+constexpr float kMinScale = 0x1p-40f;      // smallest scale append stores
+constexpr float kNoMax = -1e30f;           // maximum of nothing
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttendParams {
+    const void *q;
+    void *out;
+    float *lse;
+    const int32_t *lens, *block_table, *row_idx, *batch_count, *cu_tokens;
+    const unsigned char *k_codes, *v_codes;
+    const uint32_t *k_meta, *v_meta;
+    float *partial;
+    uint32_t *tickets;
+    int32_t *status;
+    long long q_ts, q_hs, out_ts, out_hs;             // elements
+    long long ps, hs, ts, mps, mhs, mts;              // pools
+    long long table_ld;
+    int rows, max_blocks, batch_max, max_tokens, window;
+    int num_pages, page_shift, kv_heads, group;
+    int min_units;
+    float scale_log2;                                 // scale * log2(e)
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float lg2(float x) {
+    float y;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return reinterpret_cast<const uint32_t &>(h);
+}
+
+// what pack_half left over
+__device__ __forceinline__ uint32_t pack_rest(uint32_t packed, float lo, float hi) {
+    const float2 f = __half22float2(reinterpret_cast<const __half2 &>(packed));
+    return pack_half(lo - f.x, hi - f.y);
+}
+
+// Two codes as halves: n 2^-24 (ROW 0) or n 2^-20 (ROW 1) as they are, or 2^10 (n - 7.5) times that when CENTRED.
+template <bool CENTRED, int ROW>
+__device__ __forceinline__ uint32_t codes(uint32_t w) {
+    if constexpr (CENTRED) {
+        const uint32_t grow = 0x64006400u;                                  // 2^10
+        const uint32_t less = ROW ? 0x9f809f80u : 0x8f808f80u;              // -7.5 2^-10, -7.5 2^-14
+        const __half2 h = __hfma2(reinterpret_cast<const __half2 &>(w), reinterpret_cast<const __half2 &>(grow),
+                                  reinterpret_cast<const __half2 &>(less));
+        return reinterpret_cast<const uint32_t &>(h);
+    } else {
+        return w;
+    }
+}
+
+// N words from an address that is a multiple of 4 * (largest power of two in N) bytes
+template <int N>
+__device__ __forceinline__ void load_words(const unsigned char *p, uint32_t *w) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+    } else if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p) + i);
+            w[2 * i] = v.x; w[2 * i + 1] = v.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+    }
+}
+
+__device__ __forceinline__ float meta_scale(uint32_t m) { return __uint_as_float(m << 16); }
+__device__ __forceinline__ float meta_offset(uint32_t m) { return __uint_as_float(m & 0xffff0000u); }
+
+// One request as the kernel sees it.
+struct Request {
+    int row, len, queries, first_token;   // queries = 0: nothing to do
+    int unit0, units, row_tiles;          // key units it reads, tiles of query rows per key head
+};
+
+template <int ROWS>
+__device__ __forceinline__ Request request_of(const AttendParams &p, int i) {
+    Request r;
+    r.first_token = p.cu_tokens ? p.cu_tokens[i] : i;
+    r.queries = p.cu_tokens ? p.cu_tokens[i + 1] - r.first_token : 1;
+    r.row = p.row_idx ? p.row_idx[i] : i;
+    if (r.row < 0 || r.row >= p.rows || r.first_token < 0 || r.queries < 0 || r.queries > p.max_tokens - r.first_token) r.queries = 0;
+    r.len = r.queries > 0 ? p.lens[r.row] : 0;
+    const long long most = (long long)p.max_blocks << p.page_shift;
+    if (r.len > most) r.len = (int)most;
+    if (r.len < 0) r.len = 0;
+    long long lo = 0;
+    if (p.window > 0) {
+        lo = (long long)max(r.len - r.queries, 0) - p.window + 1;
+        if (lo < 0) lo = 0;
+    }
+    r.unit0 = (int)(lo / kUnit);
+    const int end = (r.len + kUnit - 1) / kUnit;
+    r.units = end > r.unit0 ? end - r.unit0 : 1;      // a request without keys still gets its zeros
+    r.row_tiles = (int)(((long long)r.queries * p.group + ROWS - 1) / ROWS);
+    return r;
+}
+
+// The codes of 32 keys as a warp holds them for q . k: block b holds 16 keys, lane (g, c) = (lane / 4, lane % 4) the c-th quarter
+// of keys g and g + 8.
+template <int D>
+struct KeyTile {
+    uint32_t w[2][2][D / 32];
+    uint32_t meta[2][2];
+};
+
+template <int D>
+__device__ __forceinline__ void load_keys(const AttendParams &p, KeyTile<D> &t, const int (&page)[2], int tok, int head, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+    const int mask = (1 << p.page_shift) - 1;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int place = ((tok + 16 * b) & mask) + g;
+        const unsigned char *base = p.k_codes + (long long)page[b] * p.ps + (long long)head * p.hs + (long long)place * p.ts + c * (D / 8);
+        const uint32_t *meta = p.k_meta + (long long)page[b] * p.mps + (long long)head * p.mhs + (long long)place * p.mts;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            load_words<D / 32>(base + 8 * e * p.ts, t.w[b][e]);
+            t.meta[b][e] = __ldg(meta + 8 * e * p.mts);
+        }
+    }
+}
+
+// Page of each 16-key block of the warp's 32 keys; -1 for keys past the end, -2 for a number outside the pool.
+__device__ __forceinline__ void load_pages(const AttendParams &p, const int32_t *table, int tok, int len, int (&page)[2]) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        page[b] = -1;
+        if (tok + 16 * b < len) {
+            page[b] = __ldg(table + ((tok + 16 * b) >> p.page_shift));
+            if (page[b] < 0 || page[b] >= p.num_pages) page[b] = -2;
+        }
+    }
+}
+
+// Result of a query row from its sums: weights' total, offsets' part, maximum.
+template <bool F32>
+__device__ __forceinline__ void store_out(void *out, long long at, const float *o, int n) {
+    if constexpr (F32) {
+        float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(out) + at);
+        for (int i = 0; i < n / 4; ++i) d[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    } else {
+        uint2 *d = reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(out) + at);
+        for (int i = 0; i < n / 4; ++i) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(o[4 * i], o[4 * i + 1]), b = __floats2bfloat162_rn(o[4 * i + 2], o[4 * i + 3]);
+            d[i] = make_uint2(reinterpret_cast<const uint32_t &>(a), reinterpret_cast<const uint32_t &>(b));
+        }
+    }
+}
+
+template <int D, int NT>
+__host__ __device__ constexpr int slot_floats() { return 8 * NT * (D + 4); }
+
+template <int D, int NT, bool F32>
+constexpr int attend_smem() {
+    return (kWarps * 8 * (D + 4) + kWarps * 8 * NT * 4) * 4 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1);
+}
+
+// A CTA takes an equal share of all (request, key head, tile of query rows, 128 keys) units, whatever requests they belong to;
+// each of its four warps works on 32 keys at a time against the tile's 8 NT rows, straight from global memory to registers
+// (no staging: every byte of a code row is used by one lane only).  Keys are the rows of the products (m16), query rows
+// their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
+//   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
+// The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
+template <int D, int NT, bool F32>
+__global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams p) {
+    constexpr int ROWS = 8 * NT;
+    constexpr int KS = D / 16;              // steps of 16 in the product over head_dim
+    constexpr int WV = D / 64;              // words of a value row per lane
+    constexpr int LD = D + 4;
+    constexpr float kBack = F32 ? 0x1p14f : 0x1p24f;   // takes back the powers of two of codes<F32, 0>()
+    extern __shared__ __align__(16) float smem[];
+    float *const s_o = smem;                                   // [warps][8][LD]
+    float *const s_stat = s_o + kWarps * 8 * LD;               // [warps][ROWS][4]: maximum, sum, offset sum
+    uint2 *const s_q = reinterpret_cast<uint2 *>(s_stat + kWarps * ROWS * 4);   // [1 or 2][NT][KS][32]
+    __shared__ long long s_sum[kThreads];
+    __shared__ long long s_start;
+    __shared__ int s_request;
+    __shared__ bool s_last;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+
+    // ---- this CTA's share ----
+    int n = p.batch_max;
+    if (p.batch_count) n = min(max(*p.batch_count, 0), p.batch_max);
+    const int per_thread = (n + kThreads - 1) / kThreads;
+    long long mine = 0;
+    for (int e = 0; e < per_thread; ++e) {
+        const int i = tid * per_thread + e;
+        if (i < n) {
+            const Request r = request_of<ROWS>(p, i);
+            if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
+        }
+    }
+    long long before = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, before, d);
+        if (lane >= d) before += o;
+    }
+    s_sum[tid] = before;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const long long s = s_sum[32 * w + 31];
+        if (w < warp) before += s;
+        total += s;
+    }
+    before -= mine;
+    if (total == 0) return;
+    long long ctas = total / p.min_units;
+    ctas = ctas < 1 ? 1 : ctas > gridDim.x ? gridDim.x : ctas;
+    if (blockIdx.x >= ctas) return;
+    long long u = total * blockIdx.x / ctas;
+    const long long u_end = total * (blockIdx.x + 1) / ctas;
+    if (before <= u && u < before + mine) {
+        int i = tid * per_thread;
+        long long at = before;
+        for (;; ++i) {
+            const Request r = request_of<ROWS>(p, i);
+            const long long here = r.queries > 0 ? (long long)r.units * r.row_tiles * p.kv_heads : 0;
+            if (u < at + here) break;
+            at += here;
+        }
+        s_request = i;
+        s_start = at;
+    }
+    __syncthreads();
+    int request = s_request;
+    long long request_start = s_start;
+    const long long u_first = u;
+
+    while (u < u_end) {
+        const Request r = request_of<ROWS>(p, request);
+        const long long here = r.queries > 0 ? (long long)r.units * r.row_tiles * p.kv_heads : 0;
+        if (u >= request_start + here) {
+            request_start += here;
+            ++request;
+            continue;
+        }
+        const long long in_request = (u - request_start) / r.units;
+        const int unit = (int)((u - request_start) - in_request * r.units);
+        const int tile = (int)(in_request / p.kv_heads), head = (int)(in_request - (long long)tile * p.kv_heads);
+        const long long item_begin = u - unit, item_end = item_begin + r.units;
+        const int steps = (int)((item_end < u_end ? item_end : u_end) - u);
+        const int total_rows = r.queries * p.group;
+        const int row0 = tile * ROWS;
+
+        // ---- the tile's queries, as halves, laid out as the products take them ----
+        float cq[NT][2], sq[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = row0 + nt * 8 + g;
+            const bool real = row < total_rows;
+            const int j = real ? row / p.group : 0, qh = real ? head * p.group + row - j * p.group : 0;
+            const long long at = (long long)(r.first_token + j) * p.q_ts + (long long)qh * p.q_hs + c * (D / 4);
+            float x[D / 4];
+            float top = 0.f, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                float *const v = x + 8 * i;
+                if (!real) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+                } else if constexpr (F32) {
+                    const float4 *s = reinterpret_cast<const float4 *>(static_cast<const float *>(p.q) + at + 8 * i);
+                    const float4 lo = __ldg(s), hi = __ldg(s + 1);
+                    v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+                } else {
+                    const uint4 s = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + at + 8 * i));
+                    const uint32_t w[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[2 * e] = __uint_as_float(w[e] << 16);
+                        v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    top = fmaxf(top, fabsf(v[e]));
+                    sum += v[e];
+                }
+            }
+#pragma unroll
+            for (int d = 1; d < 4; d <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            }
+            // the row's largest value goes to 2^14 .. 2^15: bf16 values stay exact as halves
+            int up = 0;
+            if (top > 0.f && top < INFINITY) {
+                up = 141 - (int)(__float_as_uint(top) >> 23);
+                up = up < -110 ? -110 : up > 110 ? 110 : up;
+            }
+            const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+            if (warp == nt % kWarps) {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const float *const v = x + 8 * i;
+                    // codes in the upper four bits of a byte count 16 times as much
+                    const float f16 = f * 0.0625f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float a0 = v[2 * h] * f, a1 = v[2 * h + 4] * f, b0 = v[2 * h + 1] * f16, b1 = v[2 * h + 5] * f16;
+                        const uint2 w = make_uint2(pack_half(a0, a1), pack_half(b0, b1));
+                        s_q[(nt * KS + 2 * i + h) * 32 + lane] = w;
+                        if constexpr (F32)
+                            s_q[((NT + nt) * KS + 2 * i + h) * 32 + lane] = make_uint2(pack_rest(w.x, a0, a1), pack_rest(w.y, b0, b1));
+                    }
+                }
+            }
+            const float back = p.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23) * kBack;
+            sum *= p.scale_log2;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {   // columns of the products: rows 2c, 2c + 1
+                cq[nt][h] = __shfl_sync(0xffffffffu, back, (2 * c + h) * 4);
+                sq[nt][h] = __shfl_sync(0xffffffffu, sum, (2 * c + h) * 4);
+            }
+        }
+        // keys a row sees: [low, high).  Rows past the last query see what the last one sees; they are never stored.
+        int high[NT][2], low[NT][2];
+        int all_high, any_high, all_low, any_low;   // keys every row, any row of the tile sees
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = min(row0 + nt * 8 + 2 * c + h, total_rows - 1);
+                const int pos = r.len - r.queries + row / p.group;
+                high[nt][h] = pos + 1;
+                low[nt][h] = p.window > 0 ? max(pos, 0) - p.window + 1 : 0;
+            }
+        {
+            const int first = r.len - r.queries + row0 / p.group, last = r.len - r.queries + (min(row0 + ROWS, total_rows) - 1) / p.group;
+            all_high = first + 1;
+            any_high = last + 1;
+            all_low = p.window > 0 ? max(last, 0) - p.window + 1 : 0;
+            any_low = p.window > 0 ? max(first, 0) - p.window + 1 : 0;
+        }
+        __syncthreads();
+
+        float o[KS][NT][4];
+        float top[NT][2], sum[NT][2], off[NT][2];
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                top[nt][h] = kNoMax;
+                sum[nt][h] = off[nt][h] = 0.f;
+            }
+
+        const int32_t *const table = p.block_table + (long long)r.row * p.table_ld;
+        int tok = (r.unit0 + unit) * kUnit + warp * 32;
+        int page[2], next_page[2];
+        KeyTile<D> keys;
+        load_pages(p, table, tok, r.len, page);
+        load_pages(p, table, steps > 1 ? tok + kUnit : 0x7fffff00, r.len, next_page);
+        {
+            const int safe[2] = {max(page[0], 0), max(page[1], 0)};
+            load_keys<D>(p, keys, safe, tok, head, lane);
+        }
+        for (int step = 0; step < steps; ++step, tok += kUnit) {
+            const int safe[2] = {max(page[0], 0), max(page[1], 0)};
+            if (page[0] == -2 || page[1] == -2) {
+                if (lane == 0) atomicOr(p.status, 2);
+            }
+            const bool work = tok < any_high && tok + 32 > any_low && tok < r.len;
+            // values: lane (g, c) holds the g-th eighth of keys 2c, 2c + 1, 2c + 8, 2c + 9 of each block
+            uint32_t v[2][4][WV];
+            uint32_t vmeta[2][2];
+            if (work) {
+                const int mask = (1 << p.page_shift) - 1;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int place = (tok + 16 * b) & mask;
+                    const unsigned char *base = p.v_codes + (long long)safe[b] * p.ps + (long long)head * p.hs + (long long)(place + 2 * c) * p.ts + g * (D / 16);
+                    const uint32_t *meta = p.v_meta + (long long)safe[b] * p.mps + (long long)head * p.mhs + (long long)(place + g) * p.mts;
+                    load_words<WV>(base, v[b][0]);
+                    load_words<WV>(base + p.ts, v[b][1]);
+                    load_words<WV>(base + 8 * p.ts, v[b][2]);
+                    load_words<WV>(base + 9 * p.ts, v[b][3]);
+                    vmeta[b][0] = __ldg(meta);
+                    vmeta[b][1] = __ldg(meta + 8 * p.mts);
+                }
+            }
+            KeyTile<D> cur = keys;
+            if (step + 1 < steps) {
+                const int next_safe[2] = {max(next_page[0], 0), max(next_page[1], 0)};
+                load_keys<D>(p, keys, next_safe, tok + kUnit, head, lane);
+            }
+            const int cur_page[2] = {page[0], page[1]};
+            page[0] = next_page[0];
+            page[1] = next_page[1];
+            if (step + 2 < steps) load_pages(p, table, tok + 2 * kUnit, r.len, next_page);
+            if (!work) continue;
+
+            // ---- S^T = K Q^T ----
+            float s[2][NT][4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][nt][e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                uint32_t a[2][4];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t w0 = cur.w[b][0][ks >> 1] >> ((ks & 1) * 8), w1 = cur.w[b][1][ks >> 1] >> ((ks & 1) * 8);
+                    a[b][0] = codes<F32, 0>(w0 & 0x000f000fu);
+                    a[b][1] = codes<F32, 0>(w1 & 0x000f000fu);
+                    a[b][2] = codes<F32, 1>(w0 & 0x00f000f0u);
+                    a[b][3] = codes<F32, 1>(w1 & 0x00f000f0u);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint2 q = s_q[(nt * KS + ks) * 32 + lane];
+                    mma(s[0][nt], a[0], q.x, q.y);
+                    mma(s[1][nt], a[1], q.x, q.y);
+                    if constexpr (F32) {
+                        const uint2 q2 = s_q[((NT + nt) * KS + ks) * 32 + lane];
+                        mma(s[0][nt], a[0], q2.x, q2.y);
+                        mma(s[1][nt], a[1], q2.x, q2.y);
+                    }
+                }
+            }
+
+            // ---- weights ----
+            const bool whole = tok + 32 <= all_high && tok >= all_low && cur_page[0] >= 0 && cur_page[1] >= 0;
+            float inv[2][2], offv[2][2];
+            bool grow = false;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {      // keys g and g + 8
+                    const float sk = meta_scale(cur.meta[b][e]), sv = fmaxf(meta_scale(vmeta[b][e]), kMinScale);
+                    float mk = meta_offset(cur.meta[b][e]), mv = meta_offset(vmeta[b][e]);
+                    const float lsv = lg2(sv);
+                    if constexpr (F32) {
+                        mk = fmaf(7.5f, sk, mk);
+                        mv = fmaf(7.5f, sv, mv);
+                        inv[b][e] = __frcp_rn(sv);
+                    } else {
+                        inv[b][e] = __fdividef(1.f, sv);
+                    }
+                    offv[b][e] = mv * inv[b][e];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float &x = s[b][nt][2 * e + h];
+                            x = fmaf(x * cq[nt][h], sk, fmaf(mk, sq[nt][h], lsv));
+                            if (!whole) {
+                                const int t = tok + 16 * b + 8 * e + g;
+                                if (t >= high[nt][h] || t < low[nt][h] || cur_page[b] < 0) x = -INFINITY;
+                            }
+                            grow = grow || x > top[nt][h] + 8.f;
+                        }
+                }
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float m = fmaxf(fmaxf(s[0][nt][h], s[0][nt][2 + h]), fmaxf(s[1][nt][h], s[1][nt][2 + h]));
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                        m = fmaxf(m, top[nt][h]);
+                        const float f = ex2(top[nt][h] - m);
+                        top[nt][h] = m;
+                        sum[nt][h] *= f;
+                        off[nt][h] *= f;
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) {
+                            o[i][nt][h] *= f;
+                            o[i][nt][2 + h] *= f;
+                        }
+                    }
+            }
+            uint32_t pb[2][NT][2], pb2[2][NT][2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float x0 = s[b][nt][2 * e], x1 = s[b][nt][2 * e + 1];
+                        const float w0 = ex2(x0 - top[nt][0]), w1 = ex2(x1 - top[nt][1]);
+                        const uint32_t packed = pack_half(w0, w1);
+                        float2 w = __half22float2(reinterpret_cast<const __half2 &>(packed));
+                        pb[b][nt][e] = transpose8x8(packed);
+                        if constexpr (F32) {
+                            const uint32_t rest = pack_half(w0 - w.x, w1 - w.y);
+                            pb2[b][nt][e] = transpose8x8(rest);
+                            const float2 w2 = __half22float2(reinterpret_cast<const __half2 &>(rest));
+                            w.x += w2.x;
+                            w.y += w2.y;
+                        }
+                        // a hidden key adds nothing, even when its scale or offset is no number
+                        if (whole || !(x0 == -INFINITY)) {
+                            sum[nt][0] = fmaf(w0, inv[b][e], sum[nt][0]);
+                            off[nt][0] = fmaf(w.x, offv[b][e], off[nt][0]);
+                        }
+                        if (whole || !(x1 == -INFINITY)) {
+                            sum[nt][1] = fmaf(w1, inv[b][e], sum[nt][1]);
+                            off[nt][1] = fmaf(w.y, offv[b][e], off[nt][1]);
+                        }
+                    }
+
+            // ---- O^T += V^T P^T ----
+#pragma unroll
+            for (int w = 0; w < WV; ++w) {
+                uint32_t x[2][4];   // block; (keys 2c, 2c + 1 | keys 2c + 8, 2c + 9) x (first | last four dims of the word)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    x[b][0] = __byte_perm(v[b][0][w], v[b][1][w], 0x5410);
+                    x[b][1] = __byte_perm(v[b][0][w], v[b][1][w], 0x7632);
+                    x[b][2] = __byte_perm(v[b][2][w], v[b][3][w], 0x5410);
+                    x[b][3] = __byte_perm(v[b][2][w], v[b][3][w], 0x7632);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float part[NT][4];
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) part[nt][e] = 0.f;
+                    }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t lo = x[b][i >> 1] >> ((i & 1) * 8), hi = x[b][2 + (i >> 1)] >> ((i & 1) * 8);
+                        const uint32_t a[4] = {codes<F32, 0>(lo & 0x000f000fu), codes<F32, 1>(lo & 0x00f000f0u),
+                                               codes<F32, 0>(hi & 0x000f000fu), codes<F32, 1>(hi & 0x00f000f0u)};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            if constexpr (F32) {
+                                mma(part[nt], a, pb[b][nt][0], pb[b][nt][1]);
+                                mma(part[nt], a, pb2[b][nt][0], pb2[b][nt][1]);
+                            } else {
+                                mma(o[4 * w + i][nt], a, pb[b][nt][0], pb[b][nt][1]);
+                            }
+                        }
+                    }
+                    if constexpr (F32) {   // tensor cores cut what they add: long sums are kept outside of them
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[4 * w + i][nt][e] += part[nt][e];
+                    }
+                }
+            }
+        }
+
+        // ---- the four warps' results together ----
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    sum[nt][h] += __shfl_xor_sync(0xffffffffu, sum[nt][h], d);
+                    off[nt][h] += __shfl_xor_sync(0xffffffffu, off[nt][h], d);
+                }
+                if (g == 0) {
+                    float *const st = s_stat + (warp * ROWS + nt * 8 + 2 * c + h) * 4;
+                    st[0] = top[nt][h];
+                    st[1] = sum[nt][h];
+                    st[2] = off[nt][h];
+                }
+            }
+        const bool complete = item_begin >= u_first && item_end <= u_end;
+        const long long slot = 2 * (long long)blockIdx.x + (u == u_first ? 0 : 1);
+        float *const part = p.partial + slot * slot_floats<D, NT>();
+        constexpr int PER = D / 16;      // dims per thread: 16 threads to a row
+        const int my_row = tid >> 4, my_dim = (tid & 15) * 4;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<float2 *>(s_o + (warp * 8 + 2 * c + h) * LD + g * (D / 8) + 2 * i) =
+                        make_float2(o[i][nt][h] * kBack, o[i][nt][2 + h] * (kBack / 16));
+            __syncthreads();
+            const int row = nt * 8 + my_row;
+            float m = kNoMax, f[kWarps], l = 0.f, b = 0.f, acc[PER];
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_stat[(w * ROWS + row) * 4]);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float *const st = s_stat + (w * ROWS + row) * 4;
+                f[w] = ex2(st[0] - m);
+                l = fmaf(st[1], f[w], l);
+                b = fmaf(st[2], f[w], b);
+#pragma unroll
+                for (int i = 0; i < PER / 4; ++i) {
+                    const float4 x = *reinterpret_cast<const float4 *>(s_o + (w * 8 + my_row) * LD + my_dim + 64 * i);
+                    acc[4 * i] = fmaf(x.x, f[w], acc[4 * i]);
+                    acc[4 * i + 1] = fmaf(x.y, f[w], acc[4 * i + 1]);
+                    acc[4 * i + 2] = fmaf(x.z, f[w], acc[4 * i + 2]);
+                    acc[4 * i + 3] = fmaf(x.w, f[w], acc[4 * i + 3]);
+                }
+            }
+            if (complete) {
+                const int abs_row = row0 + row;
+                if (abs_row < total_rows) {
+                    const int j = abs_row / p.group, qh = head * p.group + abs_row - j * p.group;
+                    const float scale = l != 0.f ? 1.f / l : 0.f;
+                    const long long token = r.first_token + j;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) acc[i] = l != 0.f ? (acc[i] + b) * scale : 0.f;
+#pragma unroll
+                    for (int i = 0; i < PER / 4; ++i)
+                        store_out<F32>(p.out, token * p.out_ts + (long long)qh * p.out_hs + my_dim + 64 * i, acc + 4 * i, 4);
+                    if (p.lse && (tid & 15) == 0)
+                        p.lse[token * (p.kv_heads * p.group) + qh] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                }
+            } else {
+                float *const d = part + row * LD;
+#pragma unroll
+                for (int i = 0; i < PER / 4; ++i)
+                    __stcg(reinterpret_cast<float4 *>(d + my_dim + 64 * i), make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]));
+                if ((tid & 15) == 0) __stcg(reinterpret_cast<float4 *>(d + D), make_float4(m, l, b, 0.f));
+            }
+        }
+        if (!complete) {
+            // the last of the CTAs that share this item adds up what they left, in the order of the keys
+            const int c0 = (int)(((item_begin + 1) * ctas - 1) / total), c1 = (int)((item_end * ctas - 1) / total);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                s_last = atomicAdd(p.tickets + c0, 1u) == (uint32_t)(c1 - c0);
+                if (s_last) p.tickets[c0] = 0;
+                __threadfence();
+            }
+            __syncthreads();
+            if (s_last) {
+#pragma unroll 1
+                for (int nt = 0; nt < NT; ++nt) {
+                    const int row = nt * 8 + my_row, abs_row = row0 + row;
+                    if (abs_row >= total_rows) continue;
+                    float m = kNoMax, l = 0.f, b = 0.f, acc[PER];
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+#pragma unroll 4
+                    for (int k = c0; k <= c1; ++k) {
+                        const bool leads = total * k / ctas >= item_begin;
+                        const float *const d = p.partial + (2 * (long long)k + (leads ? 0 : 1)) * slot_floats<D, NT>() + row * LD;
+                        const float4 st = __ldcg(reinterpret_cast<const float4 *>(d + D));
+                        float4 x[PER / 4];
+#pragma unroll
+                        for (int i = 0; i < PER / 4; ++i) x[i] = __ldcg(reinterpret_cast<const float4 *>(d + my_dim + 64 * i));
+                        const float m2 = fmaxf(m, st.x), f = ex2(m - m2), f2 = ex2(st.x - m2);
+                        m = m2;
+                        l = fmaf(l, f, st.y * f2);
+                        b = fmaf(b, f, st.z * f2);
+#pragma unroll
+                        for (int i = 0; i < PER / 4; ++i) {
+                            acc[4 * i] = fmaf(acc[4 * i], f, x[i].x * f2);
+                            acc[4 * i + 1] = fmaf(acc[4 * i + 1], f, x[i].y * f2);
+                            acc[4 * i + 2] = fmaf(acc[4 * i + 2], f, x[i].z * f2);
+                            acc[4 * i + 3] = fmaf(acc[4 * i + 3], f, x[i].w * f2);
+                        }
+                    }
+                    const int j = abs_row / p.group, qh = head * p.group + abs_row - j * p.group;
+                    const float scale = l != 0.f ? 1.f / l : 0.f;
+                    const long long token = r.first_token + j;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) acc[i] = l != 0.f ? (acc[i] + b) * scale : 0.f;
+#pragma unroll
+                    for (int i = 0; i < PER / 4; ++i)
+                        store_out<F32>(p.out, token * p.out_ts + (long long)qh * p.out_hs + my_dim + 64 * i, acc + 4 * i, 4);
+                    if (p.lse && (tid & 15) == 0)
+                        p.lse[token * (p.kv_heads * p.group) + qh] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                }
+            }
+        }
+        __syncthreads();
+        u += steps;
+    }
+}
+
+// One compiled variant: its kernel, shared memory and tile height.
+struct Variant {
+    const void *kernel;
+    int smem, rows, slot;
+};
+
+template <int D, int NT, bool F32>
+Variant variant() { return {reinterpret_cast<const void *>(&kv_attend_kernel<D, NT, F32>), attend_smem<D, NT, F32>(), 8 * NT, slot_floats<D, NT>()}; }
+
+// Rows of queries that share a key head decide the tile: as few columns of 8 as hold them, so that no product is wasted on
+// empty ones; more rows than the largest tile are walked tile by tile.
+template <bool F32>
+Variant pick(int head_dim, long long rows) {
+    const int nt = rows <= 8 ? 1 : rows <= 16 || head_dim > 128 ? 2 : 4;
+    switch (head_dim) {
+        case 64: return nt == 1 ? variant<64, 1, F32>() : nt == 2 ? variant<64, 2, F32>() : variant<64, 4, F32>();
+        case 128: return nt == 1 ? variant<128, 1, F32>() : nt == 2 ? variant<128, 2, F32>() : variant<128, 4, F32>();
+        case 192: return nt == 1 ? variant<192, 1, F32>() : variant<192, 2, F32>();
+        default: return nt == 1 ? variant<256, 1, F32>() : variant<256, 2, F32>();
+    }
+}
+
+constexpr int kTileRows[3] = {8, 16, 32};   // row counts that reach every variant of pick()
+
+}  // namespace
+
+fi_status_t prepare_attend(fi_kv *kv) {
+    size_t floats = 0;
+    int most_ctas = 0;
+    for (int f32 = 0; f32 < 2; ++f32)
+        for (int i = 0; i < 3; ++i) {
+            const Variant v = f32 ? pick<true>(kv->cfg.head_dim, kTileRows[i]) : pick<false>(kv->cfg.head_dim, kTileRows[i]);
+            int ctas = 0;
+            cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, v.smem);
+            if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, v.kernel, kThreads, v.smem);
+            if (e == cudaSuccess && ctas < 1) e = cudaErrorInvalidConfiguration;
+            if (e != cudaSuccess) return cuda_fail(e, "fi_kv_create: attention kernels");
+            kv->attend_ctas[f32][i] = ctas * kv->sm_count;
+            if (ctas * kv->sm_count > most_ctas) most_ctas = ctas * kv->sm_count;
+            const size_t need = (size_t)ctas * kv->sm_count * 2 * v.slot;
+            if (need > floats) floats = need;
+        }
+    most_ctas = (most_ctas + 3) / 4 * 4;   // the partial results behind the tickets stay 16-byte aligned
+    kv->tickets = most_ctas;
+    cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&kv->scratch), floats * 4 + (size_t)most_ctas * 4);
+    if (e == cudaSuccess) e = cudaMemset(kv->scratch, 0, (size_t)most_ctas * 4);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_kv_create: attention scratch");
+}
+
+}  // namespace fi
+
+using namespace fi;
+
+extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *cuda_stream) {
+    if (!kv || !a) {
+        set_error("fi_kv_attend: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->dtype != FI_F32 && a->dtype != FI_BF16) {
+        set_error("fi_kv_attend: dtype must be FI_F32 or FI_BF16");
+        return FI_ERR_INVALID_ARG;
+    }
+    const long long most_keys = (long long)a->max_blocks << kv->page_shift;
+    if (a->batch_max < 0 || a->max_tokens < 0 || a->rows < 0 || a->max_blocks < 0 || a->window < 0 || a->max_query < 0 ||
+        a->table_ld < a->max_blocks || most_keys > 2147483647ll - 1024 || (!a->row_idx && a->batch_max > a->rows) ||
+        (!a->cu_tokens && a->batch_max > a->max_tokens) ||
+        (long long)a->max_tokens * (kv->cfg.q_heads / kv->cfg.kv_heads) > 2147483647ll - 1024) {
+        set_error("fi_kv_attend: negative size, table_ld below max_blocks, more keys or query rows than 2^31 - 1,024, or fewer rows "
+                  "or tokens than requests");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->batch_max == 0 || a->max_tokens == 0) return FI_OK;
+    if (!a->q || !a->out || !a->lens || (a->max_blocks > 0 && !a->block_table)) {
+        set_error("fi_kv_attend: null pointer (only lse, row_idx, batch_count and cu_tokens may be)");
+        return FI_ERR_INVALID_ARG;
+    }
+    const int unit = a->dtype == FI_BF16 ? 8 : 4;
+    if ((reinterpret_cast<uintptr_t>(a->q) & 15) || (reinterpret_cast<uintptr_t>(a->out) & 15) || a->q_token_stride % unit ||
+        a->q_head_stride % unit || a->out_token_stride % unit || a->out_head_stride % unit || a->q_token_stride < 0 ||
+        a->q_head_stride < 0 || a->out_token_stride < 0 || a->out_head_stride < 0) {
+        set_error("fi_kv_attend: heads must start on 16-byte boundaries, strides must not be negative");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (!(a->scale > -3e38f && a->scale < 3e38f)) {
+        set_error("fi_kv_attend: scale must be finite");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(kv->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_kv_attend");
+    const fi_kv_config_t &c = kv->cfg;
+    AttendParams p;
+    p.q = a->q;
+    p.out = a->out;
+    p.lse = a->lse;
+    p.lens = a->lens;
+    p.block_table = a->block_table;
+    p.row_idx = a->row_idx;
+    p.batch_count = a->batch_count;
+    p.cu_tokens = a->cu_tokens;
+    p.k_codes = static_cast<const unsigned char *>(c.k_codes);
+    p.v_codes = static_cast<const unsigned char *>(c.v_codes);
+    p.k_meta = static_cast<const uint32_t *>(c.k_meta);
+    p.v_meta = static_cast<const uint32_t *>(c.v_meta);
+    p.tickets = reinterpret_cast<uint32_t *>(kv->scratch);
+    p.partial = reinterpret_cast<float *>(kv->scratch + (size_t)kv->tickets * 4);
+    p.status = kv->status_dev;
+    p.q_ts = a->q_token_stride;
+    p.q_hs = a->q_head_stride;
+    p.out_ts = a->out_token_stride;
+    p.out_hs = a->out_head_stride;
+    p.ps = c.page_stride;
+    p.hs = c.head_stride;
+    p.ts = c.token_stride;
+    p.mps = c.meta_page_stride;
+    p.mhs = c.meta_head_stride;
+    p.mts = c.meta_token_stride;
+    p.table_ld = a->table_ld;
+    p.rows = a->rows;
+    p.max_blocks = a->max_blocks;
+    p.batch_max = a->batch_max;
+    p.max_tokens = a->max_tokens;
+    p.window = a->window < most_keys ? a->window : 0;
+    p.num_pages = c.num_pages;
+    p.page_shift = kv->page_shift;
+    p.kv_heads = c.kv_heads;
+    p.group = c.q_heads / c.kv_heads;
+    p.min_units = 1;
+    p.scale_log2 = a->scale * kLog2e;
+    const bool f32 = a->dtype == FI_F32;
+    const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;
+    const long long rows = per_request * p.group;
+    const Variant v = f32 ? pick<true>(c.head_dim, rows) : pick<false>(c.head_dim, rows);
+    long long grid = kv->attend_ctas[f32 ? 1 : 0][rows <= 8 ? 0 : rows <= 16 ? 1 : 2];
+    const long long units = (most_keys + kUnit - 1) / kUnit;
+    const double most = (double)a->batch_max * c.kv_heads * (double)((rows + v.rows - 1) / v.rows) * (double)(units < 1 ? 1 : units);
+    if (most < (double)grid) grid = (long long)most;
+    void *args[] = {&p};
+    const cudaError_t e = cudaLaunchKernel(v.kernel, dim3((unsigned)grid), dim3(kThreads), args, (size_t)v.smem,
+                                           static_cast<cudaStream_t>(cuda_stream));
+    count_launch();
+    if (e != cudaSuccess) return cuda_fail(e, "fi_kv_attend");
+    return check_launch("fi_kv_attend");
+}

@@ -317,11 +317,40 @@ struct fi_cache {
     cudaEvent_t *prof_ev;    // 2 * kProfSlots events, created on first use
 };
 
+// The 4-bit key/value store of a layer behind its handle.
+struct fi_kv {
+    fi_kv_config_t cfg;
+    int page_shift;
+    int sm_count;
+    int32_t *status_dev;     // bit 0: a slot past the pool (append), bit 1: a page outside the pool (attend)
+    unsigned char *scratch;  // attention: a ticket per CTA, then two slots of partial results per CTA
+    int tickets;
+    int attend_ctas[2][3];   // CTAs that fill the device: bf16 / float32 queries x tiles of 8, 16, more rows
+};
+
 namespace fi {
 
 void set_error(const char *fmt, ...);
 void count_launch(int n = 1);
 fi_status_t check_launch(const char *what);
+fi_status_t cuda_fail(cudaError_t e, const char *what);
+
+// makes `dev` current for a scope
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = true;
+    explicit DeviceGuard(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~DeviceGuard() {
+        int cur = -1;
+        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
+    }
+};
+
+// attention over the 4-bit store: scratch and per-device set-up of a new handle
+fi_status_t prepare_attend(fi_kv *kv);
 
 // ---- launchers (each enqueues on `stream`, returns a status) ----
 // squared norms of n stored rows; norm_max_bits (nullable) is raised to the largest of them (float bit pattern)

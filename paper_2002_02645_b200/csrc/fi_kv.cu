@@ -1,0 +1,646 @@
+// Page tables of a layer's key/value store, and the store itself in 4 bits (the attention that reads it is in
+// fi_attend.cu).
+#include <cfloat>
+#include <cstring>
+#include <new>
+
+#include <cuda_bf16.h>
+
+#include "fi_internal.cuh"
+
+struct fi_pages {
+    fi_pages_config_t cfg;
+    int sm_count;
+    uint32_t *ticket;   // [1] CTAs of the running call that are done; the last one puts it back to 0
+};
+
+namespace fi {
+namespace {
+
+constexpr int kPageThreads = 1024;
+constexpr int kPageMaxBatch = 8192;
+constexpr int kRefused = -2147483647 - 1;
+constexpr int kPageItems = kPageMaxBatch / kPageThreads;   // requests per thread, at most
+
+// Exclusive sum over the block of one value per thread; *total receives the sum.  64 bits: lengths come from the device
+// unchecked, and their sum must not wrap.
+__device__ long long block_exclusive(long long v, long long *total) {
+    __shared__ long long warp_sum[kPageThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long inc = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+        long long w = warp_sum[lane];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, w, d);
+            if (lane >= d) w += o;
+        }
+        warp_sum[lane] = w;
+    }
+    __syncthreads();
+    const long long before = (warp ? warp_sum[warp - 1] : 0) + inc - v;
+    *total = warp_sum[kPageThreads / 32 - 1];
+    __syncthreads();   // the next call writes warp_sum again
+    return before;
+}
+
+__device__ __forceinline__ int clamp_int(long long v) { return v > 2147483647ll ? 2147483647 : (int)v; }
+
+// last i in [0, n) with first[i] <= x, for non-decreasing first[] with first[0] <= x
+__device__ __forceinline__ int find_last(const int *first, int n, int x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// True in the last CTA of the grid to get here; everything the grid read before is then free to be overwritten.
+__device__ bool last_cta(uint32_t *ticket) {
+    if (gridDim.x == 1) return true;
+    __shared__ bool last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+        if (last) *ticket = 0;
+    }
+    __syncthreads();
+    return last;
+}
+
+__device__ __forceinline__ int actual_count(const int32_t *count_dev, int most) {
+    if (!count_dev) return most;
+    const int c = *count_dev;
+    return c < 0 ? 0 : c > most ? most : c;
+}
+
+// The step of the tables.  Every CTA forms both sums (tokens, then wanted pages) over all requests for itself: up to
+// 8,192 lengths from L2 cost less than a second launch, and one CTA is all that a decode step needs.  The tokens are
+// then dealt out, one per thread; a token finds its request in the sums (binary search in shared memory) and a token
+// that opens a new page also writes the table entry.  Bound by the 12 bytes written per token for prompts, and by the
+// chain of loads and block sums (about 3 us) for a decode step.  Lengths and the free count are committed by the last CTA
+// to finish, so they may be updated in place.
+__global__ void __launch_bounds__(kPageThreads) pages_extend_kernel(fi_pages_extend_t a, int page_shift, int max_blocks,
+                                                                    uint32_t *ticket) {
+    extern __shared__ int smem[];
+    int *const s_cu = smem;                       // first token of each request
+    int *const s_first = s_cu + a.batch_max;      // place of its first page in the free stack, or kRefused
+    int *const s_have = s_first + a.batch_max;
+    int *const s_row = s_have + a.batch_max;
+    const int n = actual_count(a.batch_count, a.batch_max);
+    const int free_count = min(max(*a.free_count, 0), a.num_pages);
+    const int items = (a.batch_max + kPageThreads - 1) / kPageThreads;
+    const int i0 = threadIdx.x * items;
+    int have[kPageItems], fresh[kPageItems];
+    long long sum = 0;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        have[e] = 0;
+        fresh[e] = 0;
+        if (e < items && i < n) {
+            const int row = a.row_idx ? a.row_idx[i] : i;
+            const bool ok = row >= 0 && row < a.rows;
+            if (ok) {
+                have[e] = a.lens[row];
+                fresh[e] = max(a.new_lens ? a.new_lens[i] : 1, 0);
+                if (have[e] < 0) { have[e] = 0; fresh[e] = 0; }
+            }
+            s_row[i] = ok ? row : -1;
+            s_have[i] = have[e];
+            sum += fresh[e];
+        }
+    }
+    long long tokens;
+    long long cu = block_exclusive(sum, &tokens);
+    long long need_sum = 0;
+    int need[kPageItems];
+    const long long page_mask = (1ll << page_shift) - 1;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        need[e] = -1;
+        if (e < items && i < n) {
+            s_cu[i] = clamp_int(cu);
+            if (blockIdx.x == 0) a.cu_tokens[i] = clamp_int(cu);
+            cu += fresh[e];
+            const long long had = (have[e] + page_mask) >> page_shift, want = (have[e] + (long long)fresh[e] + page_mask) >> page_shift;
+            if (want <= max_blocks && cu <= a.max_tokens) {
+                need[e] = (int)(want - had);
+                need_sum += need[e];
+            }
+        }
+    }
+    long long pages;
+    long long before = block_exclusive(need_sum, &pages);
+    long long taken = 0;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        if (e < items && i < n) {
+            const bool given = need[e] >= 0 && (need[e] == 0 || before + need[e] <= free_count);
+            // a request that needs no page may stand behind any number of refused ones: its place is not used
+            s_first[i] = !given ? kRefused : need[e] == 0 ? 0 : free_count - 1 - (int)before;
+            if (need[e] > 0) before += need[e];
+            if (given) taken += need[e];
+            if (blockIdx.x == 0) a.granted[i] = given ? fresh[e] : 0;
+            fresh[e] = given ? fresh[e] : 0;
+        }
+    }
+    long long taken_all;
+    block_exclusive(taken, &taken_all);           // (also the barrier before the shared arrays are read)
+    if (blockIdx.x == 0) {
+        for (int i = n + threadIdx.x; i <= a.batch_max; i += kPageThreads) {
+            a.cu_tokens[i] = clamp_int(tokens);
+            if (i < a.batch_max) a.granted[i] = 0;
+        }
+    }
+    const long long step = (long long)gridDim.x * kPageThreads;
+    for (long long t = (long long)blockIdx.x * kPageThreads + threadIdx.x; t < a.max_tokens; t += step) {
+        long long slot = -1;
+        int pos = -1;
+        if (t < tokens) {
+            // requests without tokens share their first token with the next one: the last of them owns it
+            const int i = find_last(s_cu, n, (int)t);
+            const long long p = (long long)s_have[i] + ((int)t - s_cu[i]);
+            pos = clamp_int(p);
+            const int first = s_first[i];
+            if (first != kRefused) {
+                const int block = (int)(p >> page_shift), row = s_row[i];
+                const int had = (int)((s_have[i] + page_mask) >> page_shift);
+                int32_t *const entry = a.block_table + (long long)row * a.table_ld + block;
+                int page;
+                if (block >= had) {
+                    page = a.free_pages[first - (block - had)];
+                    if ((p & page_mask) == 0) *entry = page;
+                } else {
+                    page = *entry;
+                }
+                if (page >= 0) slot = ((long long)page << page_shift) + (p & page_mask);
+            }
+        }
+        a.slot_map[t] = slot;
+        a.positions[t] = pos;
+    }
+    if (!last_cta(ticket)) return;
+    if (a.lens_out != a.lens) {
+        for (int r = threadIdx.x; r < a.rows; r += kPageThreads) a.lens_out[r] = a.lens[r];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        if (e < items && i < n && s_row[i] >= 0 && fresh[e] > 0) a.lens_out[s_row[i]] = have[e] + fresh[e];
+    }
+    if (threadIdx.x == 0) *a.free_count_out = free_count - (int)taken_all;
+}
+
+struct ReleaseParams {
+    const int32_t *row_idx, *batch_count, *lens, *block_table, *free_count;
+    int32_t *free_pages, *lens_out, *free_count_out;
+    long long table_ld;
+    int batch_max, rows, num_pages, max_blocks, page_shift;
+};
+
+// The way back: the pages of the listed rows are copied behind the free stack, in list order.
+__global__ void __launch_bounds__(kPageThreads) pages_release_kernel(ReleaseParams a, uint32_t *ticket) {
+    extern __shared__ int smem[];
+    int *const s_cu = smem;
+    int *const s_row = s_cu + a.batch_max;
+    const int n = actual_count(a.batch_count, a.batch_max);
+    const int free_count = min(max(*a.free_count, 0), a.num_pages);
+    const int items = (a.batch_max + kPageThreads - 1) / kPageThreads;
+    const int i0 = threadIdx.x * items;
+    int used[kPageItems];
+    long long sum = 0;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        used[e] = 0;
+        if (e < items && i < n) {
+            const int row = a.row_idx[i];
+            const bool ok = row >= 0 && row < a.rows;
+            if (ok) {
+                const long long len = max(a.lens[row], 0);
+                used[e] = (int)min((len + (1ll << a.page_shift) - 1) >> a.page_shift, (long long)a.max_blocks);
+            }
+            s_row[i] = ok ? row : -1;
+            sum += used[e];
+        }
+    }
+    long long pages;
+    long long cu = block_exclusive(sum, &pages);
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        if (e < items && i < n) {
+            s_cu[i] = clamp_int(cu);
+            cu += used[e];
+        }
+    }
+    __syncthreads();
+    if (pages > a.num_pages - free_count) pages = a.num_pages - free_count;   // a row listed twice: nothing is written past the stack
+    const long long step = (long long)gridDim.x * kPageThreads;
+    for (long long p = (long long)blockIdx.x * kPageThreads + threadIdx.x; p < pages; p += step) {
+        const int i = find_last(s_cu, n, (int)p);
+        a.free_pages[free_count + p] = a.block_table[(long long)s_row[i] * a.table_ld + ((int)p - s_cu[i])];
+    }
+    if (!last_cta(ticket)) return;
+    if (a.lens_out != a.lens) {
+        for (int r = threadIdx.x; r < a.rows; r += kPageThreads) a.lens_out[r] = a.lens[r];
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += kPageThreads)
+        if (s_row[i] >= 0) a.lens_out[s_row[i]] = 0;
+    if (threadIdx.x == 0) *a.free_count_out = free_count + (int)pages;
+}
+
+// ------------------------------------------------------------------------------------------------------- 4-bit append
+
+struct AppendParams {
+    const void *k, *v;
+    const int64_t *slot_map;
+    const int32_t *tokens_dev;
+    void *k_stored, *v_stored;
+    long long k_ts, k_hs, v_ts, v_hs;          // elements
+    unsigned char *k_codes, *v_codes;
+    uint32_t *k_meta, *v_meta;
+    long long ps, hs, ts, mps, mhs, mts;
+    long long rows, slots;                     // tokens * heads; slots of the pool
+    int heads, page_shift;
+    int32_t *status;
+};
+
+// 16 consecutive values of a vector as fp32
+template <bool BF16>
+__device__ __forceinline__ void load16(const void *base, long long elem, float (&x)[16]) {
+    if constexpr (BF16) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + elem * 2);
+        const uint4 a = p[0], b = p[1];
+        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+        const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + elem);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 a = p[i];
+            x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
+        }
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store16(void *base, long long elem, const float (&x)[16]) {
+    if constexpr (BF16) {
+        uint4 *p = reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 2);
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = reinterpret_cast<const uint32_t &>(h);
+        }
+        p[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        p[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+        float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(base) + elem);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+    }
+}
+
+// largest bf16 value not above x (as fp32); the scale is rounded up by the same function on -x
+__device__ __forceinline__ float bf16_down(float x) {
+    const uint32_t bits = __float_as_uint(x), cut = bits & 0xffff0000u;
+    return __uint_as_float(x < 0.f && bits != cut ? cut + 0x10000u : cut);
+}
+
+// One vector held by LANES neighbouring lanes, 16 values each (lanes past D / 16 hold none).
+template <int D, int LANES, bool BF16>
+__device__ __forceinline__ void pack_vector(float (&x)[16], bool active, bool write, unsigned char *codes, uint32_t *meta,
+                                            void *stored, long long stored_at) {
+    float lo = FLT_MAX, hi = -FLT_MAX;
+    bool finite = true;
+    if (active) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            lo = fminf(lo, x[i]);
+            hi = fmaxf(hi, x[i]);
+            finite = finite && fabsf(x[i]) <= FLT_MAX;
+        }
+    }
+    const int lane = (threadIdx.x & 31) & (LANES - 1);
+    if (!finite) lo = -INFINITY;      // travels through the minimum below, and -inf marks the vector
+#pragma unroll
+    for (int d = 1; d < LANES; d <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+    }
+    float offset = bf16_down(lo);
+    float scale = fmaxf(-bf16_down(-__fdiv_rn(__fsub_rn(hi, offset), 15.f)), 0x1p-40f);
+    const bool good = lo >= -FLT_MAX && offset >= -FLT_MAX && scale <= FLT_MAX;
+    uint32_t packed[2] = {0u, 0u};
+    if (good) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            // a true division: a value half-way between two codes is then decided as in exact arithmetic
+            const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], offset), scale)), 0.f), 15.f);
+            packed[i >> 3] |= (uint32_t)(int)c << (4 * (i & 7));
+            x[i] = fmaf(c, scale, offset);
+        }
+    } else {
+        offset = __uint_as_float(0x7fc00000u);
+        scale = 1.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = offset;
+    }
+    if (!active) return;
+    if (write) {
+        *reinterpret_cast<uint2 *>(codes + lane * 8) = make_uint2(packed[0], packed[1]);
+        if (lane == 0) *meta = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
+    }
+    if (stored) store16<BF16>(stored, stored_at + lane * 16, x);
+}
+
+// A group of LANES lanes packs the key and the value of one token and head: two independent 32-byte (bf16) loads per lane in
+// flight, minimum and maximum by shuffles, 8 bytes of codes per lane.  One pass over the data; bound by its bytes.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) kv_append_kernel(AppendParams a) {
+    constexpr int LANES = D <= 64 ? 4 : D <= 128 ? 8 : 16;
+    const int lane = threadIdx.x & (LANES - 1);
+    const long long row = ((long long)blockIdx.x * 256 + threadIdx.x) / LANES;
+    const bool there = row < a.rows;
+    const unsigned token = there ? (unsigned)row / (unsigned)a.heads : 0u;
+    const int head = there ? (int)((unsigned)row - token * (unsigned)a.heads) : 0;
+    const bool real = there && (!a.tokens_dev || (int)token < *a.tokens_dev);
+    const bool active = real && lane < D / 16;
+    float k[16], v[16];
+    if (active) {
+        load16<BF16>(a.k, token * a.k_ts + head * a.k_hs + lane * 16, k);
+        load16<BF16>(a.v, token * a.v_ts + head * a.v_hs + lane * 16, v);
+    }
+    const long long slot = real ? a.slot_map[token] : -1;
+    if (slot >= a.slots && lane == 0 && head == 0) atomicOr(a.status, 1);
+    const bool write = slot >= 0 && slot < a.slots;
+    const long long page = write ? slot >> a.page_shift : 0, place = write ? slot & ((1ll << a.page_shift) - 1) : 0;
+    const long long at = page * a.ps + head * a.hs + place * a.ts, mat = page * a.mps + head * a.mhs + place * a.mts;
+    const long long stored_at = row * D;
+    pack_vector<D, LANES, BF16>(k, active, write, a.k_codes + at, a.k_meta + mat, a.k_stored, stored_at);
+    pack_vector<D, LANES, BF16>(v, active, write, a.v_codes + at, a.v_meta + mat, a.v_stored, stored_at);
+}
+
+template <int D>
+void append_dispatch(const AppendParams &p, bool bf16, cudaStream_t stream) {
+    constexpr int LANES = D <= 64 ? 4 : D <= 128 ? 8 : 16;
+    const unsigned grid = (unsigned)((p.rows * LANES + 255) / 256);
+    if (bf16) kv_append_kernel<D, true><<<grid, 256, 0, stream>>>(p);
+    else kv_append_kernel<D, false><<<grid, 256, 0, stream>>>(p);
+}
+
+int log2_of(int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+bool page_size_ok(int p) { return p >= 16 && p <= 1024 && (p & (p - 1)) == 0; }
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace
+}  // namespace fi
+
+using namespace fi;
+
+extern "C" {
+
+fi_status_t fi_pages_destroy(fi_pages_t *p) {
+    if (!p) return FI_OK;
+    DeviceGuard guard(p->cfg.device);
+    cudaDeviceSynchronize();
+    cudaFree(p->ticket);
+    delete p;
+    return FI_OK;
+}
+
+fi_status_t fi_pages_create(const fi_pages_config_t *cfg, fi_pages_t **out) {
+    if (out) *out = nullptr;
+    if (!cfg || !out) {
+        set_error("fi_pages_create: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (!page_size_ok(cfg->page_size) || cfg->max_blocks < 1 || (long long)cfg->max_blocks * cfg->page_size > 2147483647ll ||
+        cfg->max_batch < 1 || cfg->max_batch > kPageMaxBatch || cfg->device < 0) {
+        set_error("fi_pages_create: page_size a power of two in 16..1024, max_blocks >= 1 with max_blocks * page_size < 2^31, "
+                  "max_batch in 1..%d", kPageMaxBatch);
+        return FI_ERR_INVALID_ARG;
+    }
+    fi_pages *p = new (std::nothrow) fi_pages();
+    if (!p) {
+        set_error("fi_pages_create: out of host memory");
+        return FI_ERR_OOM;
+    }
+    p->cfg = *cfg;
+    DeviceGuard guard(cfg->device);
+    cudaError_t e = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 16);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_release_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 8);
+    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&p->ticket), sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaMemset(p->ticket, 0, sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) {
+        const fi_status_t st = cuda_fail(e, "fi_pages_create");
+        fi_pages_destroy(p);
+        return st;
+    }
+    *out = p;
+    return FI_OK;
+}
+
+fi_status_t fi_pages_extend(fi_pages_t *p, const fi_pages_extend_t *s, void *cuda_stream) {
+    if (!p || !s) {
+        set_error("fi_pages_extend: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (s->batch_max < 0 || s->batch_max > p->cfg.max_batch || s->max_tokens < 0 || s->rows < 0 || s->num_pages < 0 ||
+        s->table_ld < p->cfg.max_blocks || (!s->row_idx && s->batch_max > s->rows)) {
+        set_error("fi_pages_extend: batch %d outside 0..%d, a negative size, table_ld below max_blocks, or more requests than rows",
+                  s->batch_max, p->cfg.max_batch);
+        return FI_ERR_INVALID_ARG;
+    }
+    if ((s->rows > 0 && (!s->lens || !s->lens_out || !s->block_table)) || (s->num_pages > 0 && !s->free_pages) || !s->free_count ||
+        !s->free_count_out || !s->cu_tokens || (s->batch_max > 0 && !s->granted) ||
+        (s->max_tokens > 0 && (!s->slot_map || !s->positions))) {
+        set_error("fi_pages_extend: null pointer (only row_idx, batch_count and new_lens may be)");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(p->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_extend");
+    int grid = s->max_tokens / 4096;   // below that the sums cost more than the tokens
+    grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
+    pages_extend_kernel<<<grid, kPageThreads, (size_t)s->batch_max * 16, static_cast<cudaStream_t>(cuda_stream)>>>(
+        *s, log2_of(p->cfg.page_size), p->cfg.max_blocks, p->ticket);
+    count_launch();
+    return check_launch("fi_pages_extend");
+}
+
+fi_status_t fi_pages_release(fi_pages_t *p, const int32_t *row_idx, int32_t batch_max, const int32_t *batch_count,
+                             const int32_t *lens, int32_t rows, const int32_t *block_table, int64_t table_ld,
+                             int32_t *free_pages, int32_t num_pages, const int32_t *free_count, int32_t *lens_out,
+                             int32_t *free_count_out, void *cuda_stream) {
+    if (!p || (rows > 0 && (!lens || !block_table || !lens_out)) || (num_pages > 0 && !free_pages) || !free_count || !free_count_out ||
+        (batch_max > 0 && !row_idx)) {
+        set_error("fi_pages_release: null argument (only batch_count may be)");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (batch_max < 0 || batch_max > p->cfg.max_batch || rows < 0 || num_pages < 0 || table_ld < p->cfg.max_blocks) {
+        set_error("fi_pages_release: batch %d outside 0..%d, a negative size, or table_ld below max_blocks", batch_max, p->cfg.max_batch);
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(p->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_release");
+    ReleaseParams a = {row_idx, batch_count, lens, block_table, free_count, free_pages, lens_out, free_count_out, table_ld,
+                       batch_max, rows, num_pages, p->cfg.max_blocks, log2_of(p->cfg.page_size)};
+    long long grid = (long long)batch_max * p->cfg.max_blocks / 16384;   // an upper bound of the pages, rarely met
+    grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
+    pages_release_kernel<<<(int)grid, kPageThreads, (size_t)batch_max * 8, static_cast<cudaStream_t>(cuda_stream)>>>(a, p->ticket);
+    count_launch();
+    return check_launch("fi_pages_release");
+}
+
+fi_status_t fi_kv_destroy(fi_kv_t *kv) {
+    if (!kv) return FI_OK;
+    DeviceGuard guard(kv->cfg.device);
+    cudaDeviceSynchronize();
+    cudaFree(kv->status_dev);
+    cudaFree(kv->scratch);
+    delete kv;
+    return FI_OK;
+}
+
+fi_status_t fi_kv_create(const fi_kv_config_t *cfg, fi_kv_t **out) {
+    if (out) *out = nullptr;
+    if (!cfg || !out || !cfg->k_codes || !cfg->v_codes || !cfg->k_meta || !cfg->v_meta) {
+        set_error("fi_kv_create: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    const int d = cfg->head_dim;
+    if (!page_size_ok(cfg->page_size) || cfg->num_pages < 1 || (d != 64 && d != 128 && d != 192 && d != 256) ||
+        cfg->kv_heads < 1 || cfg->q_heads < cfg->kv_heads || cfg->q_heads % cfg->kv_heads != 0 || cfg->q_heads > 65535 ||
+        cfg->device < 0) {
+        set_error("fi_kv_create: page_size a power of two in 16..1024, num_pages >= 1, head_dim 64, 128, 192 or 256, q_heads a "
+                  "multiple of kv_heads");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (!aligned16(cfg->k_codes) || !aligned16(cfg->v_codes) || (reinterpret_cast<uintptr_t>(cfg->k_meta) & 3) != 0 ||
+        (reinterpret_cast<uintptr_t>(cfg->v_meta) & 3) != 0 || cfg->page_stride % 16 != 0 || cfg->head_stride % 16 != 0 ||
+        cfg->token_stride % 16 != 0 || cfg->page_stride < 0 || cfg->head_stride < 0 || cfg->token_stride < d / 2 ||
+        cfg->meta_page_stride < 0 || cfg->meta_head_stride < 0 || cfg->meta_token_stride < 1) {
+        set_error("fi_kv_create: codes and their strides must be multiples of 16 bytes, meta of 4, strides not negative and "
+                  "tokens not overlapping");
+        return FI_ERR_INVALID_ARG;
+    }
+    fi_kv *kv = new (std::nothrow) fi_kv();
+    if (!kv) {
+        set_error("fi_kv_create: out of host memory");
+        return FI_ERR_OOM;
+    }
+    kv->cfg = *cfg;
+    kv->page_shift = log2_of(cfg->page_size);
+    DeviceGuard guard(cfg->device);
+    cudaError_t e = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
+    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&kv->status_dev), sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMemset(kv->status_dev, 0, sizeof(int32_t));
+    fi_status_t st = e == cudaSuccess ? prepare_attend(kv) : cuda_fail(e, "fi_kv_create");
+    if (st == FI_OK) {
+        e = cudaDeviceSynchronize();
+        if (e != cudaSuccess) st = cuda_fail(e, "fi_kv_create");
+    }
+    if (st != FI_OK) {
+        fi_kv_destroy(kv);
+        return st;
+    }
+    *out = kv;
+    return FI_OK;
+}
+
+fi_status_t fi_kv_poll_status(fi_kv_t *kv) {
+    if (!kv) {
+        set_error("fi_kv_poll_status: null handle");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(kv->cfg.device);
+    int32_t word = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(&word, kv->status_dev, sizeof word, cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && word) e = cudaMemset(kv->status_dev, 0, sizeof word);
+    if (e != cudaSuccess) return cuda_fail(e, "fi_kv_poll_status");
+    if (word) {
+        set_error("fi_kv_poll_status:%s%s", word & 1 ? " a slot past the pool was skipped by fi_kv_append;" : "",
+                  word & 2 ? " a page number outside the pool was met by fi_kv_attend" : "");
+        return FI_ERR_INVALID_ARG;
+    }
+    return FI_OK;
+}
+
+fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *a, void *cuda_stream) {
+    if (!kv || !a) {
+        set_error("fi_kv_append: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->dtype != FI_F32 && a->dtype != FI_BF16) {
+        set_error("fi_kv_append: dtype must be FI_F32 or FI_BF16");
+        return FI_ERR_INVALID_ARG;
+    }
+    const long long rows = a->tokens * (long long)kv->cfg.kv_heads;
+    if (a->tokens < 0 || a->tokens > 2147483647ll || rows > 2147483647ll) {
+        set_error("fi_kv_append: tokens * kv_heads must lie in 0..2^31 - 1");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->tokens == 0) return FI_OK;
+    if (!a->k || !a->v || !a->slot_map) {
+        set_error("fi_kv_append: null pointer (only tokens_dev, k_stored and v_stored may be)");
+        return FI_ERR_INVALID_ARG;
+    }
+    const int unit = a->dtype == FI_BF16 ? 8 : 4;
+    if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->k_stored) || !aligned16(a->v_stored) || a->k_token_stride % unit ||
+        a->k_head_stride % unit || a->v_token_stride % unit || a->v_head_stride % unit || a->k_token_stride < 0 ||
+        a->k_head_stride < 0 || a->v_token_stride < 0 || a->v_head_stride < 0) {
+        set_error("fi_kv_append: vectors must start on 16-byte boundaries, strides must not be negative");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(kv->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_kv_append");
+    const fi_kv_config_t &c = kv->cfg;
+    AppendParams p = {a->k, a->v, a->slot_map, a->tokens_dev, a->k_stored, a->v_stored, a->k_token_stride, a->k_head_stride,
+                      a->v_token_stride, a->v_head_stride, static_cast<unsigned char *>(c.k_codes),
+                      static_cast<unsigned char *>(c.v_codes), static_cast<uint32_t *>(c.k_meta), static_cast<uint32_t *>(c.v_meta),
+                      c.page_stride, c.head_stride, c.token_stride, c.meta_page_stride, c.meta_head_stride, c.meta_token_stride,
+                      rows, (long long)c.num_pages << kv->page_shift, c.kv_heads, kv->page_shift, kv->status_dev};
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const bool bf16 = a->dtype == FI_BF16;
+    switch (c.head_dim) {
+        case 64: append_dispatch<64>(p, bf16, stream); break;
+        case 128: append_dispatch<128>(p, bf16, stream); break;
+        case 192: append_dispatch<192>(p, bf16, stream); break;
+        default: append_dispatch<256>(p, bf16, stream); break;
+    }
+    count_launch();
+    return check_launch("fi_kv_append");
+}
+
+}  // extern "C"

@@ -1,0 +1,434 @@
+// Norm of each query and key head with the position rotation in the same pass, and its gradients.
+//
+//   n = x r, r = 1 / sqrt(mean(x^2) + eps);  z = n w;  y = R z
+//   backward:  g = R^T dy;  dx = r (g w - n mean(g w n));  dw = sum over tokens and heads of g n
+//
+// One head of one token (a row) is held by a group of 1..16 neighbouring lanes, 16 values each, in two pieces of 8 that
+// lie half a rotation apart, so that both members of every pair are in one lane and the rotation needs no exchange.  The
+// sums over a row are shuffles inside the group.  Everything is read once and written once: the bound is the traffic.
+#include <cuda_bf16.h>
+
+#include "fi_internal.cuh"
+
+namespace fi {
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kMaxPartials = 1024;   // CTAs of a backward pass, at most
+
+// rows of one operand: (token, head) pairs
+struct NormSide {
+    const void *x;
+    const void *dy;
+    void *out;
+    const float *weight;
+    long long x_ts, x_hs, dy_ts, dy_hs, out_ts, out_hs;   // elements
+    int heads;
+};
+
+struct NormParams {
+    NormSide q, k;
+    const float *rope;
+    const int32_t *positions;
+    const int32_t *tokens_dev;
+    float *partial;        // backward: [CTAs][2][head_dim]
+    long long tokens;
+    int head_dim, rot, max_pos, interleaved;
+    float eps, inv_dim;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *base, long long elem, float *x) {
+    if constexpr (BF16) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + elem * 2);
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+        const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + elem);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 a = p[i];
+            x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
+        }
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store8(void *base, long long elem, const float *x) {
+    if constexpr (BF16) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = reinterpret_cast<const uint32_t &>(h);
+        }
+        *reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(base) + elem);
+        p[0] = make_float4(x[0], x[1], x[2], x[3]);
+        p[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+
+// Where a lane's two pieces start, and the first of the 8 angles it turns by (turned = false: its values pass unturned).
+struct LanePlace {
+    int a, b, angle;
+    bool there, turned;
+};
+
+__device__ __forceinline__ LanePlace lane_place(const NormParams &p, int lane) {
+    LanePlace l;
+    l.there = lane < p.head_dim / 16;
+    l.turned = lane < p.rot / 16;
+    l.angle = lane * 8;
+    if (p.interleaved) {
+        l.a = lane * 16;
+        l.b = l.a + 8;
+    } else if (l.turned) {
+        l.a = lane * 8;
+        l.b = p.rot / 2 + lane * 8;
+    } else {
+        l.a = lane * 16;   // the rest behind the rotated values starts at a multiple of 16 too
+        l.b = l.a + 8;
+    }
+    return l;
+}
+
+// turn v[0..7], v[8..15] by the lane's angles (dir = -1: back)
+__device__ __forceinline__ void turn(float (&v)[16], const float (&c)[8], const float (&s)[8], int interleaved, float dir) {
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = v[2 * i], b = v[2 * i + 1], t = s[i] * dir;
+            v[2 * i] = a * c[i] - b * t;
+            v[2 * i + 1] = b * c[i] + a * t;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = v[i], b = v[8 + i], t = s[i] * dir;
+            v[i] = a * c[i] - b * t;
+            v[8 + i] = b * c[i] + a * t;
+        }
+    }
+}
+
+__device__ __forceinline__ void load_angles(const NormParams &p, const LanePlace &l, int pos, float (&c)[8], float (&s)[8]) {
+    if (pos < 0 || pos >= p.max_pos) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
+        return;
+    }
+    const float *row = p.rope + (long long)pos * p.rot;
+    load8<false>(row, l.angle, c);
+    load8<false>(row, p.rot / 2 + l.angle, s);
+}
+
+template <int LANES>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int d = 1; d < LANES; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+__device__ __forceinline__ long long actual_tokens(const NormParams &p) {
+    if (!p.tokens_dev) return p.tokens;
+    const long long t = *p.tokens_dev;
+    return t < 0 ? 0 : t > p.tokens ? p.tokens : t;
+}
+
+template <int LANES, bool BF16>
+__global__ void __launch_bounds__(kNormThreads) head_norm_rope_kernel(NormParams p) {
+    const int lane = threadIdx.x & (LANES - 1);
+    const unsigned heads = p.q.heads + p.k.heads;
+    const unsigned row = blockIdx.x * (unsigned)(kNormThreads / LANES) + threadIdx.x / LANES;
+    const unsigned token = row / heads;
+    const bool real = (long long)token < actual_tokens(p);
+    const LanePlace l = lane_place(p, lane);
+    const bool active = real && l.there;
+    int head = (int)(row - token * heads);
+    const bool is_k = head >= p.q.heads;
+    const NormSide &side = is_k ? p.k : p.q;
+    if (is_k) head -= p.q.heads;
+    float v[16], c[8], s[8];
+    float sum = 0.f;
+    const bool turned = active && l.turned;
+    if (active) {
+        const long long at = (long long)token * side.x_ts + (long long)head * side.x_hs;
+        load8<BF16>(side.x, at + l.a, v);
+        load8<BF16>(side.x, at + l.b, v + 8);
+        if (turned) load_angles(p, l, p.positions[token], c, s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
+    }
+    sum = group_sum<LANES>(sum);
+    if (!active) return;
+    const float r = 1.f / sqrtf(fmaf(sum, p.inv_dim, p.eps));
+    if (side.weight) {
+        float w[16];
+        load8<false>(side.weight, l.a, w);
+        load8<false>(side.weight, l.b, w + 8);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = v[i] * r * w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= r;
+    }
+    if (turned) turn(v, c, s, p.interleaved, 1.f);
+    const long long to = (long long)token * side.out_ts + (long long)head * side.out_hs;
+    store8<BF16>(side.out, to + l.a, v);
+    store8<BF16>(side.out, to + l.b, v + 8);
+}
+
+// Gradients of the rows of one operand, dealt out to the groups of the grid in turn; `dw` gathers the lane's 16 columns of the
+// weight gradient over all its rows.
+template <int LANES, bool BF16>
+__device__ __forceinline__ void backward_rows(const NormParams &p, const NormSide &side, long long tokens, float (&dw)[16]) {
+    const int lane = threadIdx.x & (LANES - 1);
+    const LanePlace l = lane_place(p, lane);
+    const long long rows = tokens * side.heads;
+    const long long groups = (long long)gridDim.x * (kNormThreads / LANES);
+    const long long rounds = (rows + groups - 1) / groups;
+    float w[16];
+    if (l.there && side.weight) {
+        load8<false>(side.weight, l.a, w);
+        load8<false>(side.weight, l.b, w + 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = 1.f;
+    }
+    for (long long round = 0; round < rounds; ++round) {   // the whole warp stays: the sums below are its shuffles
+        const long long row = round * groups + (long long)blockIdx.x * (kNormThreads / LANES) + threadIdx.x / LANES;
+        const bool active = row < rows && l.there;
+        const unsigned token = active ? (unsigned)row / (unsigned)side.heads : 0u;
+        const int head = active ? (int)((unsigned)row - token * (unsigned)side.heads) : 0;
+        float x[16], g[16];
+        float sum = 0.f;
+        if (active) {
+            const long long at = (long long)token * side.x_ts + (long long)head * side.x_hs;
+            const long long dat = (long long)token * side.dy_ts + (long long)head * side.dy_hs;
+            load8<BF16>(side.x, at + l.a, x);
+            load8<BF16>(side.x, at + l.b, x + 8);
+            load8<BF16>(side.dy, dat + l.a, g);
+            load8<BF16>(side.dy, dat + l.b, g + 8);
+            if (l.turned) {
+                float c[8], s[8];
+                load_angles(p, l, p.positions[token], c, s);
+                turn(g, c, s, p.interleaved, -1.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
+        }
+        sum = group_sum<LANES>(sum);
+        const float r = 1.f / sqrtf(fmaf(sum, p.inv_dim, p.eps));
+        float dot = 0.f;
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] *= r;                       // n
+                dw[i] = fmaf(g[i], x[i], dw[i]);
+                g[i] *= w[i];
+                dot = fmaf(g[i], x[i], dot);
+            }
+        }
+        dot = group_sum<LANES>(dot) * p.inv_dim;
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g[i] = r * (g[i] - x[i] * dot);
+            const long long to = (long long)token * side.out_ts + (long long)head * side.out_hs;
+            store8<BF16>(side.out, to + l.a, g);
+            store8<BF16>(side.out, to + l.b, g + 8);
+        }
+    }
+}
+
+// Each CTA leaves its sums of the weight gradients in `partial`; the groups of the CTA are added in a fixed order.
+template <int LANES, bool BF16>
+__global__ void __launch_bounds__(kNormThreads) head_norm_rope_backward_kernel(NormParams p) {
+    constexpr int GROUPS = kNormThreads / LANES;
+    __shared__ float s_dw[GROUPS][LANES * 16 + 1];
+    const long long tokens = actual_tokens(p);
+    const LanePlace l = lane_place(p, threadIdx.x & (LANES - 1));
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const NormSide &side = which ? p.k : p.q;
+        float dw[16] = {};
+        if (side.heads > 0) backward_rows<LANES, BF16>(p, side, tokens, dw);
+        if (!p.partial) continue;
+        __syncthreads();
+        if (l.there) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s_dw[threadIdx.x / LANES][l.a + i] = dw[i];
+                s_dw[threadIdx.x / LANES][l.b + i] = dw[8 + i];
+            }
+        }
+        __syncthreads();
+        for (int d = threadIdx.x; d < p.head_dim; d += kNormThreads) {
+            float sum = 0.f;
+#pragma unroll 8
+            for (int g = 0; g < GROUPS; ++g) sum += s_dw[g][d];
+            p.partial[((long long)blockIdx.x * 2 + which) * p.head_dim + d] = sum;
+        }
+    }
+}
+
+// dw[which][d] = sum of the CTAs' partial sums, 32 columns per CTA, always in the same order
+__global__ void __launch_bounds__(1024) norm_weight_sum_kernel(const float *partial, int ctas, int head_dim, float *dq_weight,
+                                                               float *dk_weight) {
+    __shared__ float s[32][33];
+    const int col = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    float sum = 0.f;
+    if (col < 2 * head_dim)
+        for (int b = part; b < ctas; b += 32) sum += partial[(long long)b * 2 * head_dim + col];
+    s[part][threadIdx.x & 31] = sum;
+    __syncthreads();
+    if (part == 0 && col < 2 * head_dim) {
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) total += s[i][threadIdx.x];
+        float *const out = col < head_dim ? dq_weight : dk_weight;
+        if (out) out[col < head_dim ? col : col - head_dim] = total;
+    }
+}
+
+bool norm_aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int lanes_for(int head_dim) { return head_dim <= 16 ? 1 : head_dim <= 32 ? 2 : head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
+
+template <int LANES>
+void launch_norm(const NormParams &p, bool bf16, unsigned grid, bool backward, cudaStream_t stream) {
+    if (backward) {
+        if (bf16) head_norm_rope_backward_kernel<LANES, true><<<grid, kNormThreads, 0, stream>>>(p);
+        else head_norm_rope_backward_kernel<LANES, false><<<grid, kNormThreads, 0, stream>>>(p);
+    } else {
+        if (bf16) head_norm_rope_kernel<LANES, true><<<grid, kNormThreads, 0, stream>>>(p);
+        else head_norm_rope_kernel<LANES, false><<<grid, kNormThreads, 0, stream>>>(p);
+    }
+}
+
+void launch_norm_lanes(int lanes, const NormParams &p, bool bf16, unsigned grid, bool backward, cudaStream_t stream) {
+    switch (lanes) {
+        case 1: launch_norm<1>(p, bf16, grid, backward, stream); break;
+        case 2: launch_norm<2>(p, bf16, grid, backward, stream); break;
+        case 4: launch_norm<4>(p, bf16, grid, backward, stream); break;
+        case 8: launch_norm<8>(p, bf16, grid, backward, stream); break;
+        default: launch_norm<16>(p, bf16, grid, backward, stream); break;
+    }
+}
+
+fi_status_t check_norm_args(const fi_head_norm_rope_t *a, bool backward, const char *name) {
+    if (!a) {
+        set_error("%s: null argument", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->dtype != FI_F32 && a->dtype != FI_BF16) {
+        set_error("%s: dtype must be FI_F32 or FI_BF16", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->head_dim < 16 || a->head_dim > 256 || a->head_dim % 16 || a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16 ||
+        a->q_heads < 1 || a->k_heads < 0 || a->tokens < 0 || a->max_pos < 0 ||
+        a->tokens * ((long long)a->q_heads + a->k_heads) > 2147483647ll || a->tokens > 2147483647ll) {
+        set_error("%s: head_dim and rot_dim multiples of 16 with rot_dim <= head_dim <= 256, q_heads >= 1, k_heads >= 0, and "
+                  "tokens * heads below 2^31 (got head_dim %d, rot_dim %d, heads %d + %d)", name, a->head_dim, a->rot_dim, a->q_heads,
+                  a->k_heads);
+        return FI_ERR_INVALID_ARG;
+    }
+    const bool k = a->k_heads > 0;
+    if (a->tokens > 0 && (!a->q || !a->q_out || (k && (!a->k || !a->k_out)) || (a->rot_dim > 0 && (!a->rope || !a->positions)) ||
+                          (backward && (!a->dq_out || (k && !a->dk_out))))) {
+        set_error("%s: null pointer", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (backward && (a->dq_weight || a->dk_weight) && !a->workspace) {
+        set_error("%s: weight gradients need a workspace", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    const int unit = a->dtype == FI_BF16 ? 8 : 4;
+    const int64_t strides[12] = {a->q_token_stride, a->q_head_stride, k ? a->k_token_stride : 0, k ? a->k_head_stride : 0,
+                                 a->q_out_token_stride, a->q_out_head_stride, k ? a->k_out_token_stride : 0, k ? a->k_out_head_stride : 0,
+                                 backward ? a->dq_out_token_stride : 0, backward ? a->dq_out_head_stride : 0,
+                                 backward && k ? a->dk_out_token_stride : 0, backward && k ? a->dk_out_head_stride : 0};
+    bool ok = norm_aligned(a->q) && norm_aligned(a->q_out) && (!k || (norm_aligned(a->k) && norm_aligned(a->k_out))) &&
+              norm_aligned(a->q_weight) && norm_aligned(a->k_weight) && norm_aligned(a->rope) &&
+              (!backward || (norm_aligned(a->dq_out) && (!k || norm_aligned(a->dk_out)) && norm_aligned(a->workspace)));
+    for (int64_t s : strides) ok = ok && s >= 0 && s % unit == 0;
+    if (!ok) {
+        set_error("%s: heads, weights and the rope table must start on 16-byte boundaries, strides must not be negative", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    return FI_OK;
+}
+
+NormParams norm_params(const fi_head_norm_rope_t *a, bool backward) {
+    NormParams p = {};
+    p.q = {a->q, a->dq_out, a->q_out, a->q_weight, a->q_token_stride, a->q_head_stride, a->dq_out_token_stride,
+           a->dq_out_head_stride, a->q_out_token_stride, a->q_out_head_stride, a->q_heads};
+    p.k = {a->k, a->dk_out, a->k_out, a->k_weight, a->k_token_stride, a->k_head_stride, a->dk_out_token_stride,
+           a->dk_out_head_stride, a->k_out_token_stride, a->k_out_head_stride, a->k_heads};
+    p.rope = a->rope;
+    p.positions = a->positions;
+    p.tokens_dev = a->tokens_dev;
+    p.partial = backward && (a->dq_weight || a->dk_weight) ? static_cast<float *>(a->workspace) : nullptr;
+    p.tokens = a->tokens;
+    p.head_dim = a->head_dim;
+    p.rot = a->rot_dim;
+    p.max_pos = a->max_pos;
+    p.interleaved = a->interleaved != 0;
+    p.eps = a->eps;
+    p.inv_dim = 1.f / (float)a->head_dim;
+    return p;
+}
+
+}  // namespace
+}  // namespace fi
+
+using namespace fi;
+
+extern "C" {
+
+int64_t fi_head_norm_rope_workspace(int32_t head_dim) {
+    return head_dim < 16 || head_dim > 256 ? 0 : (int64_t)kMaxPartials * 2 * head_dim * sizeof(float);
+}
+
+fi_status_t fi_head_norm_rope(const fi_head_norm_rope_t *a, void *cuda_stream) {
+    fi_status_t st = check_norm_args(a, false, "fi_head_norm_rope");
+    if (st != FI_OK || a->tokens == 0) return st;
+    const NormParams p = norm_params(a, false);
+    const int lanes = lanes_for(a->head_dim), per_cta = kNormThreads / lanes;
+    const long long rows = a->tokens * ((long long)a->q_heads + a->k_heads);
+    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, (unsigned)((rows + per_cta - 1) / per_cta), false,
+                      static_cast<cudaStream_t>(cuda_stream));
+    count_launch();
+    return check_launch("fi_head_norm_rope");
+}
+
+fi_status_t fi_head_norm_rope_backward(const fi_head_norm_rope_t *a, void *cuda_stream) {
+    fi_status_t st = check_norm_args(a, true, "fi_head_norm_rope_backward");
+    if (st != FI_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const NormParams p = norm_params(a, true);
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_fail(e, "fi_head_norm_rope_backward");
+    const int lanes = lanes_for(a->head_dim), per_cta = kNormThreads / lanes;
+    const long long rows = a->tokens * (long long)(a->q_heads > a->k_heads ? a->q_heads : a->k_heads);
+    long long grid = (rows + per_cta - 1) / per_cta;
+    const long long most = sms * 4 < kMaxPartials ? sms * 4 : kMaxPartials;
+    grid = grid < 1 ? 1 : grid > most ? most : grid;
+    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, (unsigned)grid, true, stream);   // no tokens: the sums are zero
+    count_launch();
+    if (p.partial) {
+        norm_weight_sum_kernel<<<(2 * a->head_dim + 31) / 32, 1024, 0, stream>>>(p.partial, (int)grid, a->head_dim, a->dq_weight,
+                                                                               a->dk_weight);
+        count_launch();
+    }
+    return check_launch("fi_head_norm_rope_backward");
+}
+
+}  // extern "C"
