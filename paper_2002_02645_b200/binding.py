@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import torch
@@ -156,16 +157,16 @@ def load_library(path: Optional[str] = None):
     ptr = ctypes.POINTER
     lib.fi_pages_create.argtypes = [ptr(fi_pages_config_t), ptr(vp)]
     lib.fi_pages_destroy.argtypes = [vp]
-    lib.fi_pages_extend.argtypes = [vp, ptr(fi_pages_extend_t), vp]
+    lib.fi_pages_extend.argtypes = [vp, ctypes.c_char_p, vp]           # a packed fi_pages_extend_t
     lib.fi_pages_release.argtypes = [vp, vp, i32, vp, vp, i32, vp, i64, vp, i32, vp, vp, vp, vp]
-    lib.fi_head_norm_rope.argtypes = [ptr(fi_head_norm_rope_t), vp]
-    lib.fi_head_norm_rope_backward.argtypes = [ptr(fi_head_norm_rope_t), vp]
+    lib.fi_head_norm_rope.argtypes = [ctypes.c_char_p, vp]             # a packed fi_head_norm_rope_t
+    lib.fi_head_norm_rope_backward.argtypes = [ctypes.c_char_p, vp]
     lib.fi_head_norm_rope_workspace.argtypes = [i32]
     lib.fi_head_norm_rope_workspace.restype = i64
     lib.fi_kv_create.argtypes = [ptr(fi_kv_config_t), ptr(vp)]
     lib.fi_kv_destroy.argtypes = [vp]
-    lib.fi_kv_append.argtypes = [vp, ptr(fi_kv_append_t), vp]
-    lib.fi_kv_attend.argtypes = [vp, ptr(fi_kv_attend_t), vp]
+    lib.fi_kv_append.argtypes = [vp, ctypes.c_char_p, vp]           # a packed fi_kv_append_t
+    lib.fi_kv_attend.argtypes = [vp, ctypes.c_char_p, vp]           # a packed fi_kv_attend_t
     lib.fi_kv_poll_status.argtypes = [vp]
     lib.fi_launch_count.argtypes = []
     lib.fi_launch_count.restype = i64
@@ -211,6 +212,10 @@ def launch_count() -> int:
 
 def _stream_ptr(device: torch.device) -> int:
     return torch.cuda.current_stream(device).cuda_stream
+
+
+# the same for an ordinal, without making a Stream object: a decode step makes three of these calls per layer
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _dp(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -574,21 +579,49 @@ def cascade_run_host(caches: Sequence[FreezeCache], acts_host: Sequence[torch.Te
 
 
 # ---- attention layers behind the caches ----
+#
+# These calls are made several times per layer and decode step, where the host's time is the step's time: their argument
+# blocks are packed in one go, and the checks ask the cheapest question that decides.
 
 _FI_DTYPE = {torch.float32: FI_F32, torch.bfloat16: FI_BF16}
 
 
-def _check_int(t: Optional[torch.Tensor], name: str, device, dtype=torch.int32, at_least: int = 0) -> None:
-    if t is None:
-        return
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < at_least:
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device} with at least {at_least} entries")
+def _packer(kind) -> struct.Struct:
+    """Packs the fields of a ctypes structure in order (native layout; null pointers are 0)."""
+    code = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
+    p = struct.Struct("@" + "".join(code[t] for _, t in kind._fields_) + "0q")
+    assert p.size == ctypes.sizeof(kind)
+    return p
 
 
-def _check_heads(t: torch.Tensor, name: str, device, dtype, tokens: int, head_dim: int, heads: Optional[int] = None) -> None:
-    if t.dim() != 3 or t.dtype != dtype or t.device != device or t.shape[0] != tokens or t.shape[2] != head_dim \
-            or t.stride(2) != 1 or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be [tokens, heads, head_dim] on {device} in {dtype}, values of a head side by side")
+_pack_extend, _pack_norm, _pack_append, _pack_attend = (
+    _packer(k).pack for k in (fi_pages_extend_t, fi_head_norm_rope_t, fi_kv_append_t, fi_kv_attend_t))
+
+
+def _at(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def _check_flat(t: Optional[torch.Tensor], name: str, index: int, at_least: int = 0, dtype=torch.int32) -> None:
+    if t is not None and (t.dtype is not dtype or t.get_device() != index or t.numel() < at_least or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on cuda:{index} with at least {at_least} entries")
+
+
+def _check_heads(t: torch.Tensor, name: str, index: int, dtype, tokens: int, heads: int, head_dim: int):
+    """Strides between tokens and heads of a [tokens, heads, head_dim] tensor."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (tokens, heads, head_dim):
+        raise ValueError(f"{name} must be {dtype} [{tokens}, {heads}, {head_dim}] on cuda:{index}")
+    token, head, value = t.stride()
+    if value != 1 and head_dim > 1:
+        raise ValueError(f"{name}: the values of a head must lie side by side")
+    return token, head
+
+
+def _check_table(block_table: torch.Tensor, rows: int, blocks: int, index: int) -> None:
+    if block_table.dtype is not torch.int32 or block_table.get_device() != index or block_table.dim() != 2 \
+            or block_table.size(0) < rows or block_table.size(1) < blocks or block_table.stride(1) != 1:
+        raise ValueError(f"block_table must be int32 [rows, blocks] on cuda:{index}, a row for each entry of lens (at least "
+                         f"{rows} x {blocks})")
 
 
 class ExtendOut:
@@ -598,8 +631,8 @@ class ExtendOut:
     def __init__(self, batch: int, max_tokens: int, rows: int, device):
         self.slot_map = torch.empty(max_tokens, dtype=torch.int64, device=device)
         # one block of memory for the small ones
-        words = torch.empty(max_tokens + 2 * batch + 1 + rows + 1, dtype=torch.int32, device=device)
-        self.positions, self.cu_tokens, self.granted, self.lens, self.free_count = words.split(
+        words = torch.empty(max_tokens + 2 * batch + rows + 2, dtype=torch.int32, device=device)
+        self.positions, self.cu_tokens, self.granted, self.lens, self.free_count = words.split_with_sizes(
             [max_tokens, batch + 1, batch, rows, 1])
 
 
@@ -610,7 +643,7 @@ class KvTables:
         self._lib = load_library()
         self._h = ctypes.c_void_p()
         self.page_size, self.max_blocks, self.max_batch = page_size, max_blocks, max_batch
-        self.device = torch.device("cuda", device)
+        self.device, self._index = torch.device("cuda", device), device
         cfg = fi_pages_config_t(page_size, max_blocks, max_batch, device)
         _check(self._lib.fi_pages_create(ctypes.byref(cfg), ctypes.byref(self._h)))
 
@@ -626,13 +659,14 @@ class KvTables:
         except Exception:
             pass
 
-    def _check_table(self, lens, free_pages, free_count, block_table) -> None:
-        _check_int(lens, "lens", self.device)
-        _check_int(free_pages, "free_pages", self.device)
-        _check_int(free_count, "free_count", self.device, at_least=1)
-        if block_table.dtype != torch.int32 or block_table.device != self.device or block_table.dim() != 2 \
-                or block_table.shape[0] < lens.numel() or block_table.shape[1] < self.max_blocks or block_table.stride(1) != 1:
-            raise ValueError("block_table must be int32 [rows, max_blocks] on the tables' device, a row for each entry of lens")
+    def _check_state(self, lens, free_pages, free_count, block_table) -> int:
+        index = self._index
+        _check_flat(lens, "lens", index)
+        _check_flat(free_pages, "free_pages", index)
+        _check_flat(free_count, "free_count", index, 1)
+        rows = lens.numel()
+        _check_table(block_table, rows, self.max_blocks, index)
+        return rows
 
     # -- fi_pages_extend
     def extend(self, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor, *,
@@ -641,12 +675,11 @@ class KvTables:
                out: Optional[ExtendOut] = None) -> ExtendOut:
         """Places the step's new tokens (new_lens, or one per request) behind the stored ones.  block_table is written in
         place; lens and free_count stay as they are unless `out` holds them."""
-        self._check_table(lens, free_pages, free_count, block_table)
-        rows = lens.numel()
+        rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
         batch = row_idx.numel() if row_idx is not None else rows
-        _check_int(row_idx, "row_idx", self.device)
-        _check_int(batch_count, "batch_count", self.device, at_least=1)
-        _check_int(new_lens, "new_lens", self.device, at_least=batch)
+        _check_flat(row_idx, "row_idx", index)
+        _check_flat(batch_count, "batch_count", index, 1)
+        _check_flat(new_lens, "new_lens", index, batch)
         if max_tokens is None:
             if new_lens is not None:
                 raise ValueError("max_tokens is needed with new_lens")
@@ -654,13 +687,19 @@ class KvTables:
         if out is None:
             out = ExtendOut(batch, max_tokens, rows, self.device)
         else:
-            _check_int(out.slot_map, "out.slot_map", self.device, torch.int64, max_tokens)
-            for name, n in (("positions", max_tokens), ("cu_tokens", batch + 1), ("granted", batch), ("lens", rows), ("free_count", 1)):
-                _check_int(getattr(out, name), "out." + name, self.device, at_least=n)
-        st = fi_pages_extend_t(_dp(lens), _dp(free_pages), _dp(free_count), _dp(block_table), _dp(row_idx), _dp(batch_count),
-                               _dp(new_lens), _dp(out.slot_map), _dp(out.positions), _dp(out.cu_tokens), _dp(out.granted),
-                               _dp(out.lens), _dp(out.free_count), block_table.stride(0), rows, free_pages.numel(), batch, max_tokens)
-        _check(self._lib.fi_pages_extend(self._h, ctypes.byref(st), _stream_ptr(self.device)))
+            _check_flat(out.slot_map, "out.slot_map", index, max_tokens, torch.int64)
+            _check_flat(out.positions, "out.positions", index, max_tokens)
+            _check_flat(out.cu_tokens, "out.cu_tokens", index, batch + 1)
+            _check_flat(out.granted, "out.granted", index, batch)
+            _check_flat(out.lens, "out.lens", index, rows)
+            _check_flat(out.free_count, "out.free_count", index, 1)
+        args = _pack_extend(lens.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), block_table.data_ptr(), _at(row_idx),
+                            _at(batch_count), _at(new_lens), out.slot_map.data_ptr(), out.positions.data_ptr(),
+                            out.cu_tokens.data_ptr(), out.granted.data_ptr(), out.lens.data_ptr(), out.free_count.data_ptr(),
+                            block_table.stride(0), rows, free_pages.numel(), batch, max_tokens)
+        st = self._lib.fi_pages_extend(self._h, args, _raw_stream(index))
+        if st:
+            _check(st)
         return out
 
     # -- fi_pages_release
@@ -669,59 +708,69 @@ class KvTables:
                 out: Optional[Sequence[torch.Tensor]] = None):
         """Gives the pages of the listed rows back (free_pages is written in place); returns (lens, free_count) after it.  `out` may be
         (lens, free_count) themselves."""
-        self._check_table(lens, free_pages, free_count, block_table)
-        _check_int(row_idx, "row_idx", self.device)
-        _check_int(batch_count, "batch_count", self.device, at_least=1)
-        lens_out, count_out = out if out is not None else (torch.empty_like(lens), torch.empty_like(free_count))
-        _check_int(lens_out, "out[0]", self.device, at_least=lens.numel())
-        _check_int(count_out, "out[1]", self.device, at_least=1)
-        _check(self._lib.fi_pages_release(self._h, _dp(row_idx), row_idx.numel(), _dp(batch_count), _dp(lens), lens.numel(),
-                                          _dp(block_table), block_table.stride(0), _dp(free_pages), free_pages.numel(),
-                                          _dp(free_count), _dp(lens_out), _dp(count_out), _stream_ptr(self.device)))
+        rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
+        _check_flat(row_idx, "row_idx", index)
+        _check_flat(batch_count, "batch_count", index, 1)
+        if out is None:
+            out = torch.empty(rows + 1, dtype=torch.int32, device=self.device).split_with_sizes([rows, 1])
+        lens_out, count_out = out
+        _check_flat(lens_out, "out[0]", index, rows)
+        _check_flat(count_out, "out[1]", index, 1)
+        st = self._lib.fi_pages_release(self._h, row_idx.data_ptr(), row_idx.numel(), _at(batch_count), lens.data_ptr(), rows,
+                                        block_table.data_ptr(), block_table.stride(0), free_pages.data_ptr(), free_pages.numel(),
+                                        free_count.data_ptr(), lens_out.data_ptr(), count_out.data_ptr(), _raw_stream(index))
+        if st:
+            _check(st)
         return lens_out, count_out
 
 
-def _norm_rope_struct(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count) -> fi_head_norm_rope_t:
-    dev, (tokens, q_heads, head_dim) = q.device, q.shape
-    if q.dtype not in _FI_DTYPE:
-        raise ValueError("q must be float32 or bfloat16")
-    _check_heads(q, "q", dev, q.dtype, tokens, head_dim)
+def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count, q_res, k_res, dq_out=None,
+                    dk_out=None, dq_weight=None, dk_weight=None, workspace=None):
+    """Checks and packs the arguments of both directions; makes the results (q_res, k_res) that are not given."""
+    dtype, index = q.dtype, q.get_device()
+    if dtype not in _FI_DTYPE or q.dim() != 3 or index < 0:
+        raise ValueError("q must be a float32 or bfloat16 [tokens, heads, head_dim] tensor on a GPU")
+    tokens, q_heads, dim = q.shape
+    if q_res is None:
+        q_res = q.new_empty((tokens, q_heads, dim))
+    strides = _check_heads(q, "q", index, dtype, tokens, q_heads, dim)
+    k_heads, k_strides, k_res_strides, dk_strides = 0, (0, 0), (0, 0), (0, 0)
     if k is not None:
-        _check_heads(k, "k", dev, q.dtype, tokens, head_dim)
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _check_int(w, name, dev, torch.float32, head_dim)
-    rot = 0
+        k_heads = k.size(1) if k.dim() == 3 else 0
+        k_strides = _check_heads(k, "k", index, dtype, tokens, k_heads, dim)
+        if k_res is None:
+            k_res = k.new_empty((tokens, k_heads, dim))
+        k_res_strides = _check_heads(k_res, "result for k", index, dtype, tokens, k_heads, dim)
+    else:
+        k_res = None
+    res_strides = _check_heads(q_res, "result for q", index, dtype, tokens, q_heads, dim)
+    dq_strides = (0, 0)
+    if dq_out is not None:
+        dq_strides = _check_heads(dq_out, "dq_out", index, dtype, tokens, q_heads, dim)
+        if k is not None:
+            dk_strides = _check_heads(dk_out, "dk_out", index, dtype, tokens, k_heads, dim)
+    _check_flat(q_weight, "q_weight", index, dim, torch.float32)
+    _check_flat(k_weight, "k_weight", index, dim, torch.float32)
+    max_pos = rot = 0
     if rope is not None:
-        if rope.dim() != 2 or rope.dtype != torch.float32 or rope.device != dev or not rope.is_contiguous():
-            raise ValueError("rope must be a contiguous float32 [max_pos, rot_dim] tensor on q's device")
-        if positions is None:
-            raise ValueError("rope needs positions")
-        rot = rope.shape[1]
-        _check_int(positions, "positions", dev, at_least=tokens)
-    _check_int(count, "count", dev, at_least=1)
-    st = fi_head_norm_rope_t()
-    st.q, st.k, st.q_weight, st.k_weight = _dp(q), _dp(k), _dp(q_weight), _dp(k_weight)
-    st.rope, st.positions, st.tokens_dev = _dp(rope), _dp(positions), _dp(count)
-    st.q_token_stride, st.q_head_stride = q.stride(0), q.stride(1)
-    if k is not None:
-        st.k_token_stride, st.k_head_stride, st.k_heads = k.stride(0), k.stride(1), k.shape[1]
-    st.tokens, st.q_heads, st.head_dim, st.rot_dim = tokens, q_heads, head_dim, rot
-    st.max_pos, st.interleaved = (rope.shape[0] if rot else 0), 1 if interleaved else 0
-    st.dtype, st.eps = _FI_DTYPE[q.dtype], float(eps)
-    return st
-
-
-def _set_results(st, q, k, q_out, k_out):
-    """Result tensors of the shapes of q and k (made here when not given), entered into the struct."""
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    _check_heads(q_out, "q result", q.device, q.dtype, q.shape[0], q.shape[2], q.shape[1])
-    st.q_out, st.q_out_token_stride, st.q_out_head_stride = _dp(q_out), q_out.stride(0), q_out.stride(1)
-    if k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        _check_heads(k_out, "k result", k.device, k.dtype, k.shape[0], k.shape[2], k.shape[1])
-        st.k_out, st.k_out_token_stride, st.k_out_head_stride = _dp(k_out), k_out.stride(0), k_out.stride(1)
-    return q_out, k_out
+        if positions is None or rope.dim() != 2:
+            raise ValueError("rope must be [max_pos, rot_dim], and needs positions")
+        _check_flat(rope, "rope", index, 0, torch.float32)
+        _check_flat(positions, "positions", index, tokens)
+        max_pos, rot = rope.shape
+    _check_flat(count, "count", index, 1)
+    args = _pack_norm(q.data_ptr(), _at(k), q_res.data_ptr(), _at(k_res), _at(dq_out), _at(dk_out), _at(q_weight), _at(k_weight),
+                      _at(rope), _at(positions), _at(count), _at(dq_weight), _at(dk_weight), _at(workspace), *strides, *k_strides,
+                      *res_strides, *k_res_strides, *dq_strides, *dk_strides, tokens, q_heads, k_heads, dim, rot, max_pos,
+                      1 if interleaved else 0, _FI_DTYPE[dtype], eps)
+    if torch._C._cuda_getDevice() == index:
+        st = fn(args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            st = fn(args, _raw_stream(index))
+    if st:
+        _check(st)
+    return q_res, k_res
 
 
 def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
@@ -729,11 +778,8 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optiona
                    eps: float = 1e-6, interleaved: bool = False, count: Optional[torch.Tensor] = None,
                    q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """fi_head_norm_rope: (q, k) normed head by head and turned to their positions.  q_out / k_out may be q / k."""
-    st = _norm_rope_struct(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count)
-    q_out, k_out = _set_results(st, q, k, q_out, k_out)
-    with torch.cuda.device(q.device):
-        _check(load_library().fi_head_norm_rope(ctypes.byref(st), _stream_ptr(q.device)))
-    return q_out, k_out
+    return _norm_rope_call(load_library().fi_head_norm_rope, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
+                           q_out, k_out)
 
 
 def head_norm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
@@ -743,23 +789,17 @@ def head_norm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], q_weight
                             dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None):
     """fi_head_norm_rope_backward: (dq, dk, dq_weight, dk_weight) from the forward pass's inputs and the gradients of its
     results.  The gradient of a weight that is None is None."""
-    st = _norm_rope_struct(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count)
-    dev, head_dim = q.device, q.shape[2]
-    _check_heads(dq_out, "dq_out", dev, q.dtype, q.shape[0], head_dim, q.shape[1])
-    st.dq_out, st.dq_out_token_stride, st.dq_out_head_stride = _dp(dq_out), dq_out.stride(0), dq_out.stride(1)
-    if k is not None:
-        _check_heads(dk_out, "dk_out", dev, k.dtype, k.shape[0], head_dim, k.shape[1])
-        st.dk_out, st.dk_out_token_stride, st.dk_out_head_stride = _dp(dk_out), dk_out.stride(0), dk_out.stride(1)
-    dq, dk = _set_results(st, q, k, dq, dk)
-    dqw = torch.empty(head_dim, dtype=torch.float32, device=dev) if q_weight is not None else None
-    dkw = torch.empty(head_dim, dtype=torch.float32, device=dev) if k_weight is not None and k is not None else None
     lib = load_library()
+    dim = q.shape[-1]
+    dqw = q_weight.new_empty(dim) if q_weight is not None else None
+    dkw = k_weight.new_empty(dim) if k_weight is not None and k is not None else None
     work = None
     if dqw is not None or dkw is not None:
-        work = torch.empty(lib.fi_head_norm_rope_workspace(head_dim), dtype=torch.uint8, device=dev)
-    st.dq_weight, st.dk_weight, st.workspace = _dp(dqw), _dp(dkw), _dp(work)
-    with torch.cuda.device(dev):
-        _check(lib.fi_head_norm_rope_backward(ctypes.byref(st), _stream_ptr(dev)))
+        work = torch.empty(lib.fi_head_norm_rope_workspace(dim), dtype=torch.uint8, device=q.device)
+    if dq_out is None or (k is not None and dk_out is None):
+        raise ValueError("the gradients of the results are needed")
+    dq, dk = _norm_rope_call(lib.fi_head_norm_rope_backward, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
+                             dq, dk, dq_out, dk_out, dqw, dkw, work)
     return dq, dk, dqw, dkw
 
 
@@ -782,11 +822,12 @@ class KvCache:
                     or meta.stride() != k_meta.stride() or meta.stride(3) != 1 or any(s % 2 for s in meta.stride()[:3]):
                 raise ValueError("meta must be bfloat16 [pages, kv_heads, page_size, 2] tensors of one layout, pairs side by side")
         self.k_codes, self.k_meta, self.v_codes, self.v_meta = k_codes, k_meta, v_codes, v_meta   # kept alive
-        self.device, self.pages, self.kv_heads, self.page_size, self.head_dim = dev, pages, heads, page, 2 * half
+        self.device, self._index = dev, k_codes.get_device()
+        self.pages, self.kv_heads, self.page_size, self.head_dim = pages, heads, page, 2 * half
         self.q_heads = q_heads
         cs, ms = k_codes.stride(), k_meta.stride()
         cfg = fi_kv_config_t(_dp(k_codes), _dp(v_codes), _dp(k_meta), _dp(v_meta), cs[0], cs[1], cs[2], ms[0] // 2, ms[1] // 2,
-                             ms[2] // 2, pages, page, q_heads, heads, 2 * half, dev.index or 0)
+                             ms[2] // 2, pages, page, q_heads, heads, 2 * half, self._index)
         _check(self._lib.fi_kv_create(ctypes.byref(cfg), ctypes.byref(self._h)))
 
     # -- fi_kv_destroy
@@ -810,19 +851,22 @@ class KvCache:
                with_stored: bool = False):
         """Stores keys and values [tokens, kv_heads, head_dim] at their slots; with with_stored returns what the codes stand
         for, in k's dtype."""
-        tokens = k.shape[0]
-        if k.dtype not in _FI_DTYPE:
+        tokens, index, dtype = k.size(0), self._index, k.dtype
+        kind = _FI_DTYPE.get(dtype)
+        if kind is None:
             raise ValueError("k must be float32 or bfloat16")
-        _check_heads(k, "k", self.device, k.dtype, tokens, self.head_dim, self.kv_heads)
-        _check_heads(v, "v", self.device, k.dtype, tokens, self.head_dim, self.kv_heads)
-        _check_int(slot_map, "slot_map", self.device, torch.int64, tokens)
-        _check_int(count, "count", self.device, at_least=1)
+        k_token, k_head = _check_heads(k, "k", index, dtype, tokens, self.kv_heads, self.head_dim)
+        v_token, v_head = _check_heads(v, "v", index, dtype, tokens, self.kv_heads, self.head_dim)
+        _check_flat(slot_map, "slot_map", index, tokens, torch.int64)
+        _check_flat(count, "count", index, 1)
         ks = vs = None
         if with_stored:
-            ks, vs = (torch.empty(k.shape, dtype=k.dtype, device=self.device) for _ in range(2))
-        st = fi_kv_append_t(_dp(k), _dp(v), _dp(slot_map), _dp(count), _dp(ks), _dp(vs), k.stride(0), k.stride(1), v.stride(0),
-                            v.stride(1), tokens, _FI_DTYPE[k.dtype])
-        _check(self._lib.fi_kv_append(self._h, ctypes.byref(st), _stream_ptr(self.device)))
+            ks, vs = k.new_empty((2, tokens, self.kv_heads, self.head_dim)).unbind(0)
+        st = self._lib.fi_kv_append(self._h, _pack_append(k.data_ptr(), v.data_ptr(), slot_map.data_ptr(), _at(count), _at(ks),
+                                                          _at(vs), k_token, k_head, v_token, v_head, tokens, kind),
+                                    _raw_stream(index))
+        if st:
+            _check(st)
         return (ks, vs) if with_stored else None
 
     # -- fi_kv_attend
@@ -832,30 +876,31 @@ class KvCache:
                lse: Optional[torch.Tensor] = None):
         """Attention of q [tokens, q_heads, head_dim] (the last tokens of each request, which are stored already) over the
         stored keys and values; scale defaults to 1 / sqrt(head_dim).  Returns out, or (out, lse)."""
-        tokens = q.shape[0]
-        if q.dtype not in _FI_DTYPE:
+        tokens, index, dtype, heads, dim = q.size(0), self._index, q.dtype, self.q_heads, self.head_dim
+        kind = _FI_DTYPE.get(dtype)
+        if kind is None:
             raise ValueError("q must be float32 or bfloat16")
-        _check_heads(q, "q", self.device, q.dtype, tokens, self.head_dim, self.q_heads)
-        _check_int(lens, "lens", self.device)
+        q_token, q_head = _check_heads(q, "q", index, dtype, tokens, heads, dim)
+        _check_flat(lens, "lens", index)
         rows = lens.numel()
-        if block_table.dtype != torch.int32 or block_table.device != self.device or block_table.dim() != 2 \
-                or block_table.shape[0] < rows or block_table.stride(1) != 1:
-            raise ValueError("block_table must be int32 [rows, blocks] on the cache's device, a row for each entry of lens")
-        _check_int(row_idx, "row_idx", self.device)
-        _check_int(batch_count, "batch_count", self.device, at_least=1)
-        batch = row_idx.numel() if row_idx is not None else rows
-        _check_int(cu_tokens, "cu_tokens", self.device, at_least=batch + 1)
+        _check_table(block_table, rows, 0, index)
+        batch = rows
+        if row_idx is not None:
+            _check_flat(row_idx, "row_idx", index)
+            batch = row_idx.numel()
+        _check_flat(batch_count, "batch_count", index, 1)
+        _check_flat(cu_tokens, "cu_tokens", index, batch + 1)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        else:
-            _check_heads(out, "out", self.device, q.dtype, tokens, self.head_dim, self.q_heads)
-        if lse is None and with_lse:
-            lse = torch.empty(tokens, self.q_heads, dtype=torch.float32, device=self.device)
-        elif lse is not None:
-            _check_int(lse, "lse", self.device, torch.float32, tokens * self.q_heads)
-        st = fi_kv_attend_t(_dp(q), _dp(out), _dp(lse), _dp(lens), _dp(block_table), _dp(row_idx), _dp(batch_count), _dp(cu_tokens),
-                            q.stride(0), q.stride(1), out.stride(0), out.stride(1), block_table.stride(0), rows,
-                            block_table.shape[1], batch, tokens, int(max_query), int(window), _FI_DTYPE[q.dtype],
-                            self.head_dim ** -0.5 if scale is None else float(scale))
-        _check(self._lib.fi_kv_attend(self._h, ctypes.byref(st), _stream_ptr(self.device)))
+            out = q.new_empty((tokens, heads, dim))
+        out_token, out_head = _check_heads(out, "out", index, dtype, tokens, heads, dim)
+        if lse is not None:
+            _check_flat(lse, "lse", index, tokens * heads, torch.float32)
+        elif with_lse:
+            lse = q.new_empty((tokens, heads), dtype=torch.float32)
+        st = self._lib.fi_kv_attend(self._h, _pack_attend(
+            q.data_ptr(), out.data_ptr(), _at(lse), lens.data_ptr(), block_table.data_ptr(), _at(row_idx), _at(batch_count),
+            _at(cu_tokens), q_token, q_head, out_token, out_head, block_table.stride(0), rows, block_table.size(1), batch, tokens,
+            max_query, window, kind, dim ** -0.5 if scale is None else scale), _raw_stream(index))
+        if st:
+            _check(st)
         return out if lse is None else (out, lse)
