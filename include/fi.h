@@ -487,7 +487,7 @@ int64_t fi_head_norm_rope_workspace(int32_t head_dim);
  * offset NaN (it reads as NaN).
  * The pools are the caller's: codes [num_pages][kv_heads][page_size][head_dim / 2] bytes and meta
  * [num_pages][kv_heads][page_size] bf16 pairs, with free strides between pages, heads and tokens, the same for keys
- * and values (bytes for codes, multiples of 16; pairs for meta).
+ * and values (bytes for codes, multiples of 16; pairs for meta; the strides of a page and of page_size tokens below 2^31).
  * fi_kv_create keeps geometry and pointers and owns the scratch of fi_kv_attend (partial results of requests whose keys
  * are cut over several CTAs: 32 KiB to 256 KiB per CTA slot, at most 8 CTAs per SM) and a status word.
  */
@@ -565,7 +565,7 @@ typedef struct {
 fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *args, void *cuda_stream);
 
 /* Synchronise the device; FI_ERR_INVALID_ARG when a kernel of this handle met a slot or a page outside the pool since the
- * last poll (the word is cleared), FI_OK otherwise. */
+ * last poll (the word is cleared), FI_ERR_TIMEOUT when a bounded wait inside one ran out, FI_OK otherwise. */
 fi_status_t fi_kv_poll_status(fi_kv_t *kv);
 
 /* Number of kernels this library has launched in the calling process (all caches). */

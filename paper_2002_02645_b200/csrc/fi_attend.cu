@@ -21,9 +21,12 @@
 namespace fi {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
+constexpr int kWarps = 4;                  // warps that compute; one more brings the codes
+constexpr int kComputeThreads = kWarps * 32;
+constexpr int kThreads = kComputeThreads + 32;
 constexpr int kUnit = 128;                 // keys a CTA takes per step: 32 per warp
+constexpr int kBlocks = kUnit / 16;        // blocks of 16 keys, each in one page
+constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s) after which a wait gives up
 constexpr float kMinScale = 0x1p-40f;      // smallest scale append stores
 constexpr float kNoMax = -1e30f;           // maximum of nothing
 constexpr float kLog2e = 1.4426950408889634f;
@@ -40,11 +43,13 @@ struct AttendParams {
     uint32_t *tickets;
     int32_t *status;
     long long q_ts, q_hs, out_ts, out_hs;             // elements
-    long long ps, hs, ts, mps, mhs, mts;              // pools
+    long long hs, mhs;                                // pools: strides of heads,
+    uint32_t ps, ts, mps, mts;                        // of pages and of tokens (bytes of codes, pairs of meta)
     long long table_ld;
     int rows, max_blocks, batch_max, max_tokens, window;
     int num_pages, page_shift, kv_heads, group;
     int min_units;
+    int dense;                                        // blocks of 16 keys are contiguous and 16-byte aligned, codes and meta
     float scale_log2;                                 // scale * log2(e)
 };
 
@@ -56,9 +61,20 @@ __device__ __forceinline__ float ex2(float x) {
 
 __device__ __forceinline__ float lg2(float x) {
     float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <bool B>
+struct Bool {
+    static constexpr bool value = B;
+};
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -97,26 +113,91 @@ __device__ __forceinline__ uint32_t codes(uint32_t w) {
     }
 }
 
-// N words from an address that is a multiple of 4 * (largest power of two in N) bytes
+// N words of shared memory from an address that is a multiple of 4 * (largest power of two in N) bytes
 template <int N>
 __device__ __forceinline__ void load_words(const unsigned char *p, uint32_t *w) {
     if constexpr (N % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+            const uint4 v = *(reinterpret_cast<const uint4 *>(p) + i);
             w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
         }
     } else if constexpr (N % 2 == 0) {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
-            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p) + i);
+            const uint2 v = *(reinterpret_cast<const uint2 *>(p) + i);
             w[2 * i] = v.x; w[2 * i + 1] = v.y;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+        for (int i = 0; i < N; ++i) w[i] = *(reinterpret_cast<const uint32_t *>(p) + i);
     }
 }
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(bar)), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void bar_arrive(uint64_t *bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(bar)) : "memory");
+}
+
+__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(bar)), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(smem_at(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
+// Bounded wait.  When it gives up, every later wait of the CTA does so at once: the kernel runs to its end with whatever
+// the stages hold, and the status word says that the results are not valid.
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile int *gave_up, int32_t *status) {
+    if (bar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (uint32_t spins = 1;; ++spins) {
+        if (bar_try(bar, parity)) return true;
+        if ((spins & 255) == 0) {
+            if (*gave_up) return false;
+            if (clock64() - t0 > kWaitLimit) {
+                *gave_up = 1;
+                atomicOr(status, 4);
+                return false;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void bulk_copy(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(dst)), "l"(src),
+                 "r"(bytes), "r"(smem_at(bar))
+                 : "memory");
+}
+
+template <int BYTES>
+__device__ __forceinline__ void async_copy(void *dst, const void *src) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(dst)), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_at(dst)), "l"(src) : "memory");
+}
+
+// arrives when the thread's copies so far have landed
+__device__ __forceinline__ void async_arrive(uint64_t *bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_at(bar)) : "memory");
+}
+
+__device__ __forceinline__ void sync_compute() { asm volatile("bar.sync 1, %0;" ::"n"(kComputeThreads) : "memory"); }
 
 __device__ __forceinline__ float meta_scale(uint32_t m) { return __uint_as_float(m << 16); }
 __device__ __forceinline__ float meta_offset(uint32_t m) { return __uint_as_float(m & 0xffff0000u); }
@@ -150,41 +231,46 @@ __device__ __forceinline__ Request request_of(const AttendParams &p, int i) {
     return r;
 }
 
-// The codes of 32 keys as a warp holds them for q . k: block b holds 16 keys, lane (g, c) = (lane / 4, lane % 4) the c-th quarter
-// of keys g and g + 8.
+// One stage of the ring: the codes and the meta of 128 keys.
 template <int D>
-struct KeyTile {
-    uint32_t w[2][2][D / 32];
-    uint32_t meta[2][2];
+struct Stage {
+    unsigned char k[kUnit * D / 2], v[kUnit * D / 2];
+    uint32_t k_meta[kUnit], v_meta[kUnit];
 };
 
-template <int D>
-__device__ __forceinline__ void load_keys(const AttendParams &p, KeyTile<D> &t, const int (&page)[2], int tok, int head, int lane) {
-    const int g = lane >> 2, c = lane & 3;
-    const int mask = (1 << p.page_shift) - 1;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const int place = ((tok + 16 * b) & mask) + g;
-        const unsigned char *base = p.k_codes + (long long)page[b] * p.ps + (long long)head * p.hs + (long long)place * p.ts + c * (D / 8);
-        const uint32_t *meta = p.k_meta + (long long)page[b] * p.mps + (long long)head * p.mhs + (long long)place * p.mts;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            load_words<D / 32>(base + 8 * e * p.ts, t.w[b][e]);
-            t.meta[b][e] = __ldg(meta + 8 * e * p.mts);
-        }
-    }
-}
+// The walk over a CTA's share of the (request, tile of query rows, key head, 128 keys) units, in that order.
+struct Walk {
+    long long u, u_end, request_start;
+    int request;
+};
 
-// Page of each 16-key block of the warp's 32 keys; -1 for keys past the end, -2 for a number outside the pool.
-__device__ __forceinline__ void load_pages(const AttendParams &p, const int32_t *table, int tok, int len, int (&page)[2]) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        page[b] = -1;
-        if (tok + 16 * b < len) {
-            page[b] = __ldg(table + ((tok + 16 * b) >> p.page_shift));
-            if (page[b] < 0 || page[b] >= p.num_pages) page[b] = -2;
+// A piece of the walk: consecutive units of one request, tile and head.
+struct Piece {
+    Request r;
+    int head, tile, unit, steps;
+    long long item_begin, item_end;   // all units of that request, tile and head
+};
+
+template <int ROWS>
+__device__ __forceinline__ bool next_piece(const AttendParams &p, Walk &w, Piece &x) {
+    while (w.u < w.u_end) {
+        x.r = request_of<ROWS>(p, w.request);
+        const long long here = x.r.queries > 0 ? (long long)x.r.units * x.r.row_tiles * p.kv_heads : 0;
+        if (w.u >= w.request_start + here) {
+            w.request_start += here;
+            ++w.request;
+            continue;
         }
+        const long long in_request = (w.u - w.request_start) / x.r.units;
+        x.unit = (int)((w.u - w.request_start) - in_request * x.r.units);
+        x.tile = (int)(in_request / p.kv_heads);
+        x.head = (int)(in_request - (long long)x.tile * p.kv_heads);
+        x.item_begin = w.u - x.unit;
+        x.item_end = x.item_begin + x.r.units;
+        x.steps = (int)((x.item_end < w.u_end ? x.item_end : w.u_end) - w.u);
+        return true;
     }
+    return false;
 }
 
 // Result of a query row from its sums: weights' total, offsets' part, maximum.
@@ -205,59 +291,83 @@ __device__ __forceinline__ void store_out(void *out, long long at, const float *
 template <int D, int NT>
 __host__ __device__ constexpr int slot_floats() { return 8 * NT * (D + 4); }
 
+// Stages of the ring: what the CTAs of an SM can hold together, at least two.
+template <int D, int NT>
+__host__ __device__ constexpr int stages() { return D == 64 ? 5 : D == 128 ? (NT == 1 ? 3 : 4) : D == 192 ? 3 : 2; }
+
+// CTAs per SM the registers are cut to
+template <int D, int NT>
+__host__ __device__ constexpr int min_ctas() { return D * NT <= 128 ? 3 : 2; }
+
 template <int D, int NT, bool F32>
 constexpr int attend_smem() {
-    return (kWarps * 8 * (D + 4) + kWarps * 8 * NT * 4) * 4 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1);
+    return stages<D, NT>() * (int)sizeof(Stage<D>) + (kWarps * 8 * (D + 4) + kWarps * 8 * NT * 4) * 4 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1);
 }
 
-// A CTA takes an equal share of all (request, key head, tile of query rows, 128 keys) units, whatever requests they belong to;
-// each of its four warps works on 32 keys at a time against the tile's 8 NT rows, straight from global memory to registers
-// (no staging: every byte of a code row is used by one lane only).  Keys are the rows of the products (m16), query rows
-// their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
+// A CTA takes an equal share of all (request, tile of query rows, key head, 128 keys) units, whatever requests they belong
+// to.  One warp brings the codes into a ring of stages: a block of 16 keys of a head is one kilobyte in one page (head_dim
+// 128), so a lane fetches a block's keys, values or meta with one bulk copy, and it runs ahead over the ends of requests.
+// Pools of another layout are gathered with 16-byte copies.  Each of the four other warps works on 32 of the 128 keys
+// against the tile's 8 NT rows.  Keys are the rows of the products (m16), query rows their columns (n8), so that the usual
+// 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
 template <int D, int NT, bool F32>
-__global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kernel(const AttendParams p) {
     constexpr int ROWS = 8 * NT;
     constexpr int KS = D / 16;              // steps of 16 in the product over head_dim
     constexpr int WV = D / 64;              // words of a value row per lane
     constexpr int LD = D + 4;
+    constexpr int STAGES = stages<D, NT>();
     constexpr float kBack = F32 ? 0x1p14f : 0x1p24f;   // takes back the powers of two of codes<F32, 0>()
-    extern __shared__ __align__(16) float smem[];
-    float *const s_o = smem;                                   // [warps][8][LD]
+    extern __shared__ __align__(128) unsigned char smem[];
+    Stage<D> *const s_stage = reinterpret_cast<Stage<D> *>(smem);
+    float *const s_o = reinterpret_cast<float *>(smem + STAGES * sizeof(Stage<D>));   // [warps][8][LD]
     float *const s_stat = s_o + kWarps * 8 * LD;               // [warps][ROWS][4]: maximum, sum, offset sum
     uint2 *const s_q = reinterpret_cast<uint2 *>(s_stat + kWarps * ROWS * 4);   // [1 or 2][NT][KS][32]
-    __shared__ long long s_sum[kThreads];
+    __shared__ uint64_t s_full[STAGES], s_empty[STAGES];
+    __shared__ uint32_t s_valid[STAGES];    // blocks that were brought, a bit each
+    __shared__ long long s_sum[kWarps];
     __shared__ long long s_start;
     __shared__ int s_request;
     __shared__ bool s_last;
+    __shared__ volatile int s_gave_up;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    if (tid == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            bar_init(&s_full[i], p.dense ? 1 : 33);   // lane 0, or lane 0 and the lanes' copies
+            bar_init(&s_empty[i], kWarps);
+        }
+        s_gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
 
     // ---- this CTA's share ----
     int n = p.batch_max;
     if (p.batch_count) n = min(max(*p.batch_count, 0), p.batch_max);
-    const int per_thread = (n + kThreads - 1) / kThreads;
+    const int per_thread = (n + kComputeThreads - 1) / kComputeThreads;
     long long mine = 0;
-    for (int e = 0; e < per_thread; ++e) {
-        const int i = tid * per_thread + e;
-        if (i < n) {
-            const Request r = request_of<ROWS>(p, i);
-            if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
+    if (warp < kWarps)
+        for (int e = 0; e < per_thread; ++e) {
+            const int i = tid * per_thread + e;
+            if (i < n) {
+                const Request r = request_of<ROWS>(p, i);
+                if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
+            }
         }
-    }
     long long before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const long long o = __shfl_up_sync(0xffffffffu, before, d);
         if (lane >= d) before += o;
     }
-    s_sum[tid] = before;
+    if (lane == 31 && warp < kWarps) s_sum[warp] = before;
     __syncthreads();
     long long total = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-        const long long s = s_sum[32 * w + 31];
+        const long long s = s_sum[w];
         if (w < warp) before += s;
         total += s;
     }
@@ -266,38 +376,113 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
     long long ctas = total / p.min_units;
     ctas = ctas < 1 ? 1 : ctas > gridDim.x ? gridDim.x : ctas;
     if (blockIdx.x >= ctas) return;
-    long long u = total * blockIdx.x / ctas;
-    const long long u_end = total * (blockIdx.x + 1) / ctas;
-    if (before <= u && u < before + mine) {
+    Walk walk;
+    walk.u = total * blockIdx.x / ctas;
+    walk.u_end = total * (blockIdx.x + 1) / ctas;
+    if (before <= walk.u && walk.u < before + mine) {
         int i = tid * per_thread;
         long long at = before;
         for (;; ++i) {
             const Request r = request_of<ROWS>(p, i);
             const long long here = r.queries > 0 ? (long long)r.units * r.row_tiles * p.kv_heads : 0;
-            if (u < at + here) break;
+            if (walk.u < at + here) break;
             at += here;
         }
         s_request = i;
         s_start = at;
     }
     __syncthreads();
-    int request = s_request;
-    long long request_start = s_start;
-    const long long u_first = u;
+    walk.request = s_request;
+    walk.request_start = s_start;
 
-    while (u < u_end) {
-        const Request r = request_of<ROWS>(p, request);
-        const long long here = r.queries > 0 ? (long long)r.units * r.row_tiles * p.kv_heads : 0;
-        if (u >= request_start + here) {
-            request_start += here;
-            ++request;
-            continue;
+    if (warp == kWarps) {
+        // ---- the warp that brings the codes ----
+        int stage = 0;
+        uint32_t phase = 1;      // the first round finds every stage empty
+        Piece x;
+        const int block = lane >> 2, kind = lane & 3;     // dense pools: a lane per block and kind of data
+        const int mask = (1 << p.page_shift) - 1;
+        while (next_piece<ROWS>(p, walk, x)) {
+            const int32_t *const table = p.block_table + (long long)x.r.row * p.table_ld;
+            int first_key = 0;                            // that any query sees
+            if (p.window > 0) first_key = max(max(x.r.len - x.r.queries, 0) - p.window + 1, 0);
+            int tok = (x.r.unit0 + x.unit) * kUnit + 16 * block;
+            const auto page_at = [&](int t) { return t < x.r.len ? __ldg(table + (t >> p.page_shift)) : -1; };
+            int page = page_at(tok);
+            for (int step = 0; step < x.steps; ++step, tok += kUnit) {
+                const int next = step + 1 < x.steps ? page_at(tok + kUnit) : -1;
+                const bool there = tok < x.r.len && tok + 16 > first_key;
+                const bool good = there && page >= 0 && page < p.num_pages;
+                if (there && !good && kind == 0) atomicOr(p.status, 2);
+                bar_wait(&s_empty[stage], phase, &s_gave_up, p.status);
+                const uint32_t lanes = __ballot_sync(0xffffffffu, good && !s_gave_up);
+                Stage<D> &st = s_stage[stage];
+                const bool bring = (lanes >> lane) & 1;
+                if (lane == 0) {
+                    uint32_t valid = 0;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) valid |= ((lanes >> (4 * b)) & 1u) << b;
+                    s_valid[stage] = valid;
+                    if (p.dense) bar_expect(&s_full[stage], __popc(valid) * (16 * D + 128));
+                    else bar_arrive(&s_full[stage]);
+                }
+                __syncwarp();
+                const long long at = (long long)page * p.ps + x.head * p.hs + (long long)(tok & mask) * p.ts;
+                const long long meta_at = (long long)page * p.mps + x.head * p.mhs + (long long)(tok & mask) * p.mts;
+                if (p.dense) {
+                    if (bring) {
+                        if (kind == 0) bulk_copy(st.k + 8 * D * block, p.k_codes + at, 8 * D, &s_full[stage]);
+                        else if (kind == 1) bulk_copy(st.v + 8 * D * block, p.v_codes + at, 8 * D, &s_full[stage]);
+                        else if (kind == 2) bulk_copy(st.k_meta + 16 * block, p.k_meta + meta_at, 64, &s_full[stage]);
+                        else bulk_copy(st.v_meta + 16 * block, p.v_meta + meta_at, 64, &s_full[stage]);
+                    }
+                } else {
+                    if (bring) {                          // the four lanes of a block take four keys each
+#pragma unroll 1
+                        for (int e = 0; e < 4; ++e) {
+                            const int key = 4 * kind + e;
+                            const unsigned char *const k = p.k_codes + at + (long long)key * p.ts, *const v = p.v_codes + at + (long long)key * p.ts;
+#pragma unroll
+                            for (int i = 0; i < D / 32; ++i) {
+                                async_copy<16>(st.k + (16 * block + key) * (D / 2) + 16 * i, k + 16 * i);
+                                async_copy<16>(st.v + (16 * block + key) * (D / 2) + 16 * i, v + 16 * i);
+                            }
+                            async_copy<4>(st.k_meta + 16 * block + key, p.k_meta + meta_at + (long long)key * p.mts);
+                            async_copy<4>(st.v_meta + 16 * block + key, p.v_meta + meta_at + (long long)key * p.mts);
+                        }
+                    }
+                    async_arrive(&s_full[stage]);
+                }
+                page = next;
+                if (++stage == STAGES) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            walk.u += x.steps;
         }
-        const long long in_request = (u - request_start) / r.units;
-        const int unit = (int)((u - request_start) - in_request * r.units);
-        const int tile = (int)(in_request / p.kv_heads), head = (int)(in_request - (long long)tile * p.kv_heads);
-        const long long item_begin = u - unit, item_end = item_begin + r.units;
-        const int steps = (int)((item_end < u_end ? item_end : u_end) - u);
+        // the compute warps have waited for every stage, unless they gave up: then the copies are waited for here
+        if (s_gave_up)
+            for (int i = 0; i < STAGES; ++i) {
+                const long long t0 = clock64();
+                while (!bar_try(&s_full[stage], phase) && clock64() - t0 < 200000000ll) {}
+                if (++stage == STAGES) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+        return;
+    }
+
+    // ---- the warps that compute ----
+    const long long u_first = walk.u;
+    int stage = 0;
+    uint32_t phase = 0;
+    Piece x;
+    while (next_piece<ROWS>(p, walk, x)) {
+        const Request &r = x.r;
+        const int head = x.head, tile = x.tile, steps = x.steps;
+        const long long item_begin = x.item_begin, item_end = x.item_end;
         const int total_rows = r.queries * p.group;
         const int row0 = tile * ROWS;
 
@@ -391,7 +576,7 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
             all_low = p.window > 0 ? max(last, 0) - p.window + 1 : 0;
             any_low = p.window > 0 ? max(first, 0) - p.window + 1 : 0;
         }
-        __syncthreads();
+        sync_compute();
 
         float o[KS][NT][4];
         float top[NT][2], sum[NT][2], off[NT][2];
@@ -409,164 +594,160 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
                 sum[nt][h] = off[nt][h] = 0.f;
             }
 
-        const int32_t *const table = p.block_table + (long long)r.row * p.table_ld;
-        int tok = (r.unit0 + unit) * kUnit + warp * 32;
-        int page[2], next_page[2];
-        KeyTile<D> keys;
-        load_pages(p, table, tok, r.len, page);
-        load_pages(p, table, steps > 1 ? tok + kUnit : 0x7fffff00, r.len, next_page);
-        {
-            const int safe[2] = {max(page[0], 0), max(page[1], 0)};
-            load_keys<D>(p, keys, safe, tok, head, lane);
-        }
+        int tok = (r.unit0 + x.unit) * kUnit + warp * 32;
         for (int step = 0; step < steps; ++step, tok += kUnit) {
-            const int safe[2] = {max(page[0], 0), max(page[1], 0)};
-            if (page[0] == -2 || page[1] == -2) {
-                if (lane == 0) atomicOr(p.status, 2);
-            }
+            bar_wait(&s_full[stage], phase, &s_gave_up, p.status);
+            const Stage<D> &st = s_stage[stage];
+            const uint32_t valid = s_valid[stage] >> (2 * warp);
             const bool work = tok < any_high && tok + 32 > any_low && tok < r.len;
-            // values: lane (g, c) holds the g-th eighth of keys 2c, 2c + 1, 2c + 8, 2c + 9 of each block
-            uint32_t v[2][4][WV];
-            uint32_t vmeta[2][2];
+            const bool whole = tok + 32 <= all_high && tok >= all_low && (valid & 3) == 3;
+
             if (work) {
-                const int mask = (1 << p.page_shift) - 1;
+                // ---- S^T = K Q^T: lane (g, c) holds the c-th quarter of keys g and g + 8 of each block of 16 ----
+                float s[2][NT][4];
+                uint32_t kw[2][2][D / 32];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int place = (tok + 16 * b) & mask;
-                    const unsigned char *base = p.v_codes + (long long)safe[b] * p.ps + (long long)head * p.hs + (long long)(place + 2 * c) * p.ts + g * (D / 16);
-                    const uint32_t *meta = p.v_meta + (long long)safe[b] * p.mps + (long long)head * p.mhs + (long long)(place + g) * p.mts;
-                    load_words<WV>(base, v[b][0]);
-                    load_words<WV>(base + p.ts, v[b][1]);
-                    load_words<WV>(base + 8 * p.ts, v[b][2]);
-                    load_words<WV>(base + 9 * p.ts, v[b][3]);
-                    vmeta[b][0] = __ldg(meta);
-                    vmeta[b][1] = __ldg(meta + 8 * p.mts);
-                }
-            }
-            KeyTile<D> cur = keys;
-            if (step + 1 < steps) {
-                const int next_safe[2] = {max(next_page[0], 0), max(next_page[1], 0)};
-                load_keys<D>(p, keys, next_safe, tok + kUnit, head, lane);
-            }
-            const int cur_page[2] = {page[0], page[1]};
-            page[0] = next_page[0];
-            page[1] = next_page[1];
-            if (step + 2 < steps) load_pages(p, table, tok + 2 * kUnit, r.len, next_page);
-            if (!work) continue;
-
-            // ---- S^T = K Q^T ----
-            float s[2][NT][4];
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                    for (int e = 0; e < 2; ++e)
+                        load_words<D / 32>(st.k + (warp * 32 + 16 * b + 8 * e + g) * (D / 2) + c * (D / 8), kw[b][e]);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][nt][e] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                uint32_t a[2][4];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const uint32_t w0 = cur.w[b][0][ks >> 1] >> ((ks & 1) * 8), w1 = cur.w[b][1][ks >> 1] >> ((ks & 1) * 8);
-                    a[b][0] = codes<F32, 0>(w0 & 0x000f000fu);
-                    a[b][1] = codes<F32, 0>(w1 & 0x000f000fu);
-                    a[b][2] = codes<F32, 1>(w0 & 0x00f000f0u);
-                    a[b][3] = codes<F32, 1>(w1 & 0x00f000f0u);
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const uint2 q = s_q[(nt * KS + ks) * 32 + lane];
-                    mma(s[0][nt], a[0], q.x, q.y);
-                    mma(s[1][nt], a[1], q.x, q.y);
-                    if constexpr (F32) {
-                        const uint2 q2 = s_q[((NT + nt) * KS + ks) * 32 + lane];
-                        mma(s[0][nt], a[0], q2.x, q2.y);
-                        mma(s[1][nt], a[1], q2.x, q2.y);
-                    }
-                }
-            }
-
-            // ---- weights ----
-            const bool whole = tok + 32 <= all_high && tok >= all_low && cur_page[0] >= 0 && cur_page[1] >= 0;
-            float inv[2][2], offv[2][2];
-            bool grow = false;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {      // keys g and g + 8
-                    const float sk = meta_scale(cur.meta[b][e]), sv = fmaxf(meta_scale(vmeta[b][e]), kMinScale);
-                    float mk = meta_offset(cur.meta[b][e]), mv = meta_offset(vmeta[b][e]);
-                    const float lsv = lg2(sv);
-                    if constexpr (F32) {
-                        mk = fmaf(7.5f, sk, mk);
-                        mv = fmaf(7.5f, sv, mv);
-                        inv[b][e] = __frcp_rn(sv);
-                    } else {
-                        inv[b][e] = __fdividef(1.f, sv);
-                    }
-                    offv[b][e] = mv * inv[b][e];
+                for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            float &x = s[b][nt][2 * e + h];
-                            x = fmaf(x * cq[nt][h], sk, fmaf(mk, sq[nt][h], lsv));
-                            if (!whole) {
-                                const int t = tok + 16 * b + 8 * e + g;
-                                if (t >= high[nt][h] || t < low[nt][h] || cur_page[b] < 0) x = -INFINITY;
-                            }
-                            grow = grow || x > top[nt][h] + 8.f;
+                        for (int e = 0; e < 4; ++e) s[b][nt][e] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    uint32_t a[2][4];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const uint32_t w0 = kw[b][0][ks >> 1] >> ((ks & 1) * 8), w1 = kw[b][1][ks >> 1] >> ((ks & 1) * 8);
+                        a[b][0] = codes<F32, 0>(w0 & 0x000f000fu);
+                        a[b][1] = codes<F32, 0>(w1 & 0x000f000fu);
+                        a[b][2] = codes<F32, 1>(w0 & 0x00f000f0u);
+                        a[b][3] = codes<F32, 1>(w1 & 0x00f000f0u);
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint2 q = s_q[(nt * KS + ks) * 32 + lane];
+                        mma(s[0][nt], a[0], q.x, q.y);
+                        mma(s[1][nt], a[1], q.x, q.y);
+                        if constexpr (F32) {
+                            const uint2 q2 = s_q[((NT + nt) * KS + ks) * 32 + lane];
+                            mma(s[0][nt], a[0], q2.x, q2.y);
+                            mma(s[1][nt], a[1], q2.x, q2.y);
                         }
+                    }
                 }
-            if (__any_sync(0xffffffffu, grow)) {
+                uint32_t km[2][2], vmeta[2][2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        km[b][e] = st.k_meta[warp * 32 + 16 * b + 8 * e + g];
+                        vmeta[b][e] = st.v_meta[warp * 32 + 16 * b + 8 * e + g];
+                    }
+                uint32_t pb[2][NT][2], pb2[2][NT][2];
+            // whole: every row of the tile sees all 32 keys
+            auto weights = [&](auto whole_) {
+                constexpr bool WHOLE = decltype(whole_)::value;
+                float inv[2][2], offv[2][2];
+                bool grow = false;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {      // keys g and g + 8
+                        const float sk = meta_scale(km[b][e]), sv = fmaxf(meta_scale(vmeta[b][e]), kMinScale);
+                        float mk = meta_offset(km[b][e]), mv = meta_offset(vmeta[b][e]);
+                        const float lsv = lg2(sv);
+                        if constexpr (F32) {
+                            mk = fmaf(7.5f, sk, mk);
+                            mv = fmaf(7.5f, sv, mv);
+                            inv[b][e] = __frcp_rn(sv);
+                        } else {
+                            inv[b][e] = rcp(sv);
+                        }
+                        offv[b][e] = mv * inv[b][e];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float &x = s[b][nt][2 * e + h];
+                                x = fmaf(x * cq[nt][h], sk, fmaf(mk, sq[nt][h], lsv));
+                                if constexpr (!WHOLE) {
+                                    const int t = tok + 16 * b + 8 * e + g;
+                                    if (t >= high[nt][h] || t < low[nt][h] || !((valid >> b) & 1)) x = -INFINITY;
+                                }
+                            }
+                    }
+                float most[NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float m = fmaxf(fmaxf(s[0][nt][h], s[0][nt][2 + h]), fmaxf(s[1][nt][h], s[1][nt][2 + h]));
-#pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                        m = fmaxf(m, top[nt][h]);
-                        const float f = ex2(top[nt][h] - m);
-                        top[nt][h] = m;
-                        sum[nt][h] *= f;
-                        off[nt][h] *= f;
-#pragma unroll
-                        for (int i = 0; i < KS; ++i) {
-                            o[i][nt][h] *= f;
-                            o[i][nt][2 + h] *= f;
-                        }
+                        most[nt][h] = fmaxf(fmaxf(s[0][nt][h], s[0][nt][2 + h]), fmaxf(s[1][nt][h], s[1][nt][2 + h]));
+                        grow = grow || most[nt][h] > top[nt][h] + 8.f;
                     }
-            }
-            uint32_t pb[2][NT][2], pb2[2][NT][2];
+                if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                        for (int h = 0; h < 2; ++h) {
+                            float m = most[nt][h];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float x0 = s[b][nt][2 * e], x1 = s[b][nt][2 * e + 1];
-                        const float w0 = ex2(x0 - top[nt][0]), w1 = ex2(x1 - top[nt][1]);
-                        const uint32_t packed = pack_half(w0, w1);
-                        float2 w = __half22float2(reinterpret_cast<const __half2 &>(packed));
-                        pb[b][nt][e] = transpose8x8(packed);
-                        if constexpr (F32) {
-                            const uint32_t rest = pack_half(w0 - w.x, w1 - w.y);
-                            pb2[b][nt][e] = transpose8x8(rest);
-                            const float2 w2 = __half22float2(reinterpret_cast<const __half2 &>(rest));
-                            w.x += w2.x;
-                            w.y += w2.y;
+                            for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                            m = fmaxf(m, top[nt][h]);
+                            const float f = ex2(top[nt][h] - m);
+                            top[nt][h] = m;
+                            sum[nt][h] *= f;
+                            off[nt][h] *= f;
+#pragma unroll
+                            for (int i = 0; i < KS; ++i) {
+                                o[i][nt][h] *= f;
+                                o[i][nt][2 + h] *= f;
+                            }
                         }
-                        // a hidden key adds nothing, even when its scale or offset is no number
-                        if (whole || !(x0 == -INFINITY)) {
-                            sum[nt][0] = fmaf(w0, inv[b][e], sum[nt][0]);
-                            off[nt][0] = fmaf(w.x, offv[b][e], off[nt][0]);
+                }
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float x0 = s[b][nt][2 * e], x1 = s[b][nt][2 * e + 1];
+                            const float w0 = ex2(x0 - top[nt][0]), w1 = ex2(x1 - top[nt][1]);
+                            const uint32_t packed = pack_half(w0, w1);
+                            float2 w = __half22float2(reinterpret_cast<const __half2 &>(packed));
+                            pb[b][nt][e] = transpose8x8(packed);
+                            if constexpr (F32) {
+                                const uint32_t rest = pack_half(w0 - w.x, w1 - w.y);
+                                pb2[b][nt][e] = transpose8x8(rest);
+                                const float2 w2 = __half22float2(reinterpret_cast<const __half2 &>(rest));
+                                w.x += w2.x;
+                                w.y += w2.y;
+                            }
+                            // a hidden key adds nothing, even when its scale or offset is no number
+                            if (WHOLE || !(x0 == -INFINITY)) {
+                                sum[nt][0] = fmaf(w0, inv[b][e], sum[nt][0]);
+                                off[nt][0] = fmaf(w.x, offv[b][e], off[nt][0]);
+                            }
+                            if (WHOLE || !(x1 == -INFINITY)) {
+                                sum[nt][1] = fmaf(w1, inv[b][e], sum[nt][1]);
+                                off[nt][1] = fmaf(w.y, offv[b][e], off[nt][1]);
+                            }
                         }
-                        if (whole || !(x1 == -INFINITY)) {
-                            sum[nt][1] = fmaf(w1, inv[b][e], sum[nt][1]);
-                            off[nt][1] = fmaf(w.y, offv[b][e], off[nt][1]);
-                        }
-                    }
+            };
+                if (whole) weights(Bool<true>{});
+                else weights(Bool<false>{});
+
+                // lane (g, c) holds the g-th eighth of keys 2c, 2c + 1, 2c + 8, 2c + 9 of each block
+                uint32_t vw[2][4][WV];
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        load_words<WV>(st.v + (warp * 32 + 16 * b + 2 * c + (e & 1) + 8 * (e >> 1)) * (D / 2) + g * (D / 16), vw[b][e]);
 
             // ---- O^T += V^T P^T ----
 #pragma unroll
@@ -574,10 +755,10 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
                 uint32_t x[2][4];   // block; (keys 2c, 2c + 1 | keys 2c + 8, 2c + 9) x (first | last four dims of the word)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    x[b][0] = __byte_perm(v[b][0][w], v[b][1][w], 0x5410);
-                    x[b][1] = __byte_perm(v[b][0][w], v[b][1][w], 0x7632);
-                    x[b][2] = __byte_perm(v[b][2][w], v[b][3][w], 0x5410);
-                    x[b][3] = __byte_perm(v[b][2][w], v[b][3][w], 0x7632);
+                    x[b][0] = __byte_perm(vw[b][0][w], vw[b][1][w], 0x5410);
+                    x[b][1] = __byte_perm(vw[b][0][w], vw[b][1][w], 0x7632);
+                    x[b][2] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x5410);
+                    x[b][3] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x7632);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -611,6 +792,13 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
                     }
                 }
             }
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(&s_empty[stage]);
+            if (++stage == STAGES) {
+                stage = 0;
+                phase ^= 1;
+            }
         }
 
         // ---- the four warps' results together ----
@@ -630,21 +818,21 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
                     st[2] = off[nt][h];
                 }
             }
-        const bool complete = item_begin >= u_first && item_end <= u_end;
-        const long long slot = 2 * (long long)blockIdx.x + (u == u_first ? 0 : 1);
+        const bool complete = item_begin >= u_first && item_end <= walk.u_end;
+        const long long slot = 2 * (long long)blockIdx.x + (walk.u == u_first ? 0 : 1);
         float *const part = p.partial + slot * slot_floats<D, NT>();
         constexpr int PER = D / 16;      // dims per thread: 16 threads to a row
         const int my_row = tid >> 4, my_dim = (tid & 15) * 4;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            if (nt > 0) __syncthreads();
+            if (nt > 0) sync_compute();
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     *reinterpret_cast<float2 *>(s_o + (warp * 8 + 2 * c + h) * LD + g * (D / 8) + 2 * i) =
                         make_float2(o[i][nt][h] * kBack, o[i][nt][2 + h] * (kBack / 16));
-            __syncthreads();
+            sync_compute();
             const int row = nt * 8 + my_row;
             float m = kNoMax, f[kWarps], l = 0.f, b = 0.f, acc[PER];
 #pragma unroll
@@ -692,13 +880,13 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
             // the last of the CTAs that share this item adds up what they left, in the order of the keys
             const int c0 = (int)(((item_begin + 1) * ctas - 1) / total), c1 = (int)((item_end * ctas - 1) / total);
             __threadfence();
-            __syncthreads();
+            sync_compute();
             if (tid == 0) {
                 s_last = atomicAdd(p.tickets + c0, 1u) == (uint32_t)(c1 - c0);
                 if (s_last) p.tickets[c0] = 0;
                 __threadfence();
             }
-            __syncthreads();
+            sync_compute();
             if (s_last) {
 #pragma unroll 1
                 for (int nt = 0; nt < NT; ++nt) {
@@ -740,8 +928,8 @@ __global__ void __launch_bounds__(kThreads) kv_attend_kernel(const AttendParams 
                 }
             }
         }
-        __syncthreads();
-        u += steps;
+        sync_compute();
+        walk.u += steps;
     }
 }
 
@@ -755,19 +943,21 @@ template <int D, int NT, bool F32>
 Variant variant() { return {reinterpret_cast<const void *>(&kv_attend_kernel<D, NT, F32>), attend_smem<D, NT, F32>(), 8 * NT, slot_floats<D, NT>()}; }
 
 // Rows of queries that share a key head decide the tile: as few columns of 8 as hold them, so that no product is wasted on
-// empty ones; more rows than the largest tile are walked tile by tile.
-template <bool F32>
-Variant pick(int head_dim, long long rows) {
-    const int nt = rows <= 8 ? 1 : rows <= 16 || head_dim > 128 ? 2 : 4;
-    switch (head_dim) {
-        case 64: return nt == 1 ? variant<64, 1, F32>() : nt == 2 ? variant<64, 2, F32>() : variant<64, 4, F32>();
-        case 128: return nt == 1 ? variant<128, 1, F32>() : nt == 2 ? variant<128, 2, F32>() : variant<128, 4, F32>();
-        case 192: return nt == 1 ? variant<192, 1, F32>() : variant<192, 2, F32>();
-        default: return nt == 1 ? variant<256, 1, F32>() : variant<256, 2, F32>();
-    }
+// empty ones, up to what the registers of a thread hold (head_dim / 16 x 4 accumulators per 8 rows); more rows than the
+// largest tile are walked tile by tile.
+__host__ constexpr int tile_columns(int head_dim, long long rows) {
+    return rows <= 8 || head_dim > 128 ? 1 : rows <= 16 || head_dim > 64 ? 2 : 4;
 }
 
-constexpr int kTileRows[3] = {8, 16, 32};   // row counts that reach every variant of pick()
+template <bool F32>
+Variant pick(int head_dim, int nt) {
+    switch (head_dim) {
+        case 64: return nt == 1 ? variant<64, 1, F32>() : nt == 2 ? variant<64, 2, F32>() : variant<64, 4, F32>();
+        case 128: return nt == 1 ? variant<128, 1, F32>() : variant<128, 2, F32>();
+        case 192: return variant<192, 1, F32>();
+        default: return variant<256, 1, F32>();
+    }
+}
 
 }  // namespace
 
@@ -776,7 +966,9 @@ fi_status_t prepare_attend(fi_kv *kv) {
     int most_ctas = 0;
     for (int f32 = 0; f32 < 2; ++f32)
         for (int i = 0; i < 3; ++i) {
-            const Variant v = f32 ? pick<true>(kv->cfg.head_dim, kTileRows[i]) : pick<false>(kv->cfg.head_dim, kTileRows[i]);
+            const int nt = 1 << i;
+            if (nt > tile_columns(kv->cfg.head_dim, 1 << 30)) continue;
+            const Variant v = f32 ? pick<true>(kv->cfg.head_dim, nt) : pick<false>(kv->cfg.head_dim, nt);
             int ctas = 0;
             cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, v.smem);
             if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, v.kernel, kThreads, v.smem);
@@ -855,12 +1047,12 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.q_hs = a->q_head_stride;
     p.out_ts = a->out_token_stride;
     p.out_hs = a->out_head_stride;
-    p.ps = c.page_stride;
+    p.ps = (uint32_t)c.page_stride;
     p.hs = c.head_stride;
-    p.ts = c.token_stride;
-    p.mps = c.meta_page_stride;
+    p.ts = (uint32_t)c.token_stride;
+    p.mps = (uint32_t)c.meta_page_stride;
     p.mhs = c.meta_head_stride;
-    p.mts = c.meta_token_stride;
+    p.mts = (uint32_t)c.meta_token_stride;
     p.table_ld = a->table_ld;
     p.rows = a->rows;
     p.max_blocks = a->max_blocks;
@@ -872,12 +1064,15 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.kv_heads = c.kv_heads;
     p.group = c.q_heads / c.kv_heads;
     p.min_units = 1;
+    p.dense = c.token_stride == c.head_dim / 2 && c.meta_token_stride == 1 && c.meta_page_stride % 4 == 0 && c.meta_head_stride % 4 == 0 &&
+              ((reinterpret_cast<uintptr_t>(c.k_meta) | reinterpret_cast<uintptr_t>(c.v_meta)) & 15) == 0;
     p.scale_log2 = a->scale * kLog2e;
     const bool f32 = a->dtype == FI_F32;
     const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;
     const long long rows = per_request * p.group;
-    const Variant v = f32 ? pick<true>(c.head_dim, rows) : pick<false>(c.head_dim, rows);
-    long long grid = kv->attend_ctas[f32 ? 1 : 0][rows <= 8 ? 0 : rows <= 16 ? 1 : 2];
+    const int nt = tile_columns(c.head_dim, rows);
+    const Variant v = f32 ? pick<true>(c.head_dim, nt) : pick<false>(c.head_dim, nt);
+    long long grid = kv->attend_ctas[f32 ? 1 : 0][nt >> 1];
     const long long units = (most_keys + kUnit - 1) / kUnit;
     const double most = (double)a->batch_max * c.kv_heads * (double)((rows + v.rows - 1) / v.rows) * (double)(units < 1 ? 1 : units);
     if (most < (double)grid) grid = (long long)most;

@@ -325,7 +325,7 @@ struct fi_kv {
     int32_t *status_dev;     // bit 0: a slot past the pool (append), bit 1: a page outside the pool (attend)
     unsigned char *scratch;  // attention: a ticket per CTA, then two slots of partial results per CTA
     int tickets;
-    int attend_ctas[2][3];   // CTAs that fill the device: bf16 / float32 queries x tiles of 8, 16, more rows
+    int attend_ctas[2][3];   // CTAs that fill the device: bf16 / float32 queries x tiles of 8, 16, 32 rows
 };
 
 namespace fi {

@@ -548,9 +548,11 @@ fi_status_t fi_kv_create(const fi_kv_config_t *cfg, fi_kv_t **out) {
     if (!aligned16(cfg->k_codes) || !aligned16(cfg->v_codes) || (reinterpret_cast<uintptr_t>(cfg->k_meta) & 3) != 0 ||
         (reinterpret_cast<uintptr_t>(cfg->v_meta) & 3) != 0 || cfg->page_stride % 16 != 0 || cfg->head_stride % 16 != 0 ||
         cfg->token_stride % 16 != 0 || cfg->page_stride < 0 || cfg->head_stride < 0 || cfg->token_stride < d / 2 ||
-        cfg->meta_page_stride < 0 || cfg->meta_head_stride < 0 || cfg->meta_token_stride < 1) {
-        set_error("fi_kv_create: codes and their strides must be multiples of 16 bytes, meta of 4, strides not negative and "
-                  "tokens not overlapping");
+        cfg->meta_page_stride < 0 || cfg->meta_head_stride < 0 || cfg->meta_token_stride < 1 || cfg->page_stride > 2147483647ll ||
+        cfg->token_stride > 2147483647ll / cfg->page_size || cfg->meta_page_stride > 2147483647ll ||
+        cfg->meta_token_stride > 2147483647ll / cfg->page_size) {
+        set_error("fi_kv_create: codes and their strides must be multiples of 16 bytes, meta of 4, strides not negative, tokens "
+                  "not overlapping, and strides of pages and of page_size tokens below 2^31");
         return FI_ERR_INVALID_ARG;
     }
     fi_kv *kv = new (std::nothrow) fi_kv();
@@ -589,6 +591,10 @@ fi_status_t fi_kv_poll_status(fi_kv_t *kv) {
     if (e == cudaSuccess) e = cudaMemcpy(&word, kv->status_dev, sizeof word, cudaMemcpyDeviceToHost);
     if (e == cudaSuccess && word) e = cudaMemset(kv->status_dev, 0, sizeof word);
     if (e != cudaSuccess) return cuda_fail(e, "fi_kv_poll_status");
+    if (word & 4) {
+        set_error("fi_kv_poll_status: a bounded wait inside the attention kernel ran out");
+        return FI_ERR_TIMEOUT;
+    }
     if (word) {
         set_error("fi_kv_poll_status:%s%s", word & 1 ? " a slot past the pool was skipped by fi_kv_append;" : "",
                   word & 2 ? " a page number outside the pool was met by fi_kv_attend" : "");
