@@ -21,12 +21,10 @@
 namespace fi {
 namespace {
 
-constexpr int kWarps = 4;                  // warps that compute; one more brings the codes
-constexpr int kComputeThreads = kWarps * 32;
-constexpr int kThreads = kComputeThreads + 32;
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
 constexpr int kUnit = 128;                 // keys a CTA takes per step: 32 per warp
-constexpr int kBlocks = kUnit / 16;        // blocks of 16 keys, each in one page
-constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s) after which a wait gives up
+constexpr int kStages = 3;                 // steps a warp has on the way
 constexpr float kMinScale = 0x1p-40f;      // smallest scale append stores
 constexpr float kNoMax = -1e30f;           // maximum of nothing
 constexpr float kLog2e = 1.4426950408889634f;
@@ -49,7 +47,6 @@ struct AttendParams {
     int rows, max_blocks, batch_max, max_tokens, window;
     int num_pages, page_shift, kv_heads, group;
     int min_units;
-    int dense;                                        // blocks of 16 keys are contiguous and 16-byte aligned, codes and meta
     float scale_log2;                                 // scale * log2(e)
 };
 
@@ -136,68 +133,18 @@ __device__ __forceinline__ void load_words(const unsigned char *p, uint32_t *w) 
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
-__device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(bar)), "r"(count) : "memory");
-}
-
-__device__ __forceinline__ void bar_arrive(uint64_t *bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(bar)) : "memory");
-}
-
-__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(bar)), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n"
-        ".reg .pred p;\n"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        "selp.u32 %0, 1, 0, p;\n"
-        "}\n"
-        : "=r"(ok)
-        : "r"(smem_at(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
-// Bounded wait.  When it gives up, every later wait of the CTA does so at once: the kernel runs to its end with whatever
-// the stages hold, and the status word says that the results are not valid.
-__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile int *gave_up, int32_t *status) {
-    if (bar_try(bar, parity)) return true;
-    const long long t0 = clock64();
-    for (uint32_t spins = 1;; ++spins) {
-        if (bar_try(bar, parity)) return true;
-        if ((spins & 255) == 0) {
-            if (*gave_up) return false;
-            if (clock64() - t0 > kWaitLimit) {
-                *gave_up = 1;
-                atomicOr(status, 4);
-                return false;
-            }
-        }
-    }
-}
-
-__device__ __forceinline__ void bulk_copy(void *dst, const void *src, uint32_t bytes, uint64_t *bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(dst)), "l"(src),
-                 "r"(bytes), "r"(smem_at(bar))
-                 : "memory");
-}
-
 template <int BYTES>
-__device__ __forceinline__ void async_copy(void *dst, const void *src) {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(dst)), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_at(dst)), "l"(src) : "memory");
+__device__ __forceinline__ void async_copy(uint32_t dst, const void *src) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// arrives when the thread's copies so far have landed
-__device__ __forceinline__ void async_arrive(uint64_t *bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_at(bar)) : "memory");
-}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
-__device__ __forceinline__ void sync_compute() { asm volatile("bar.sync 1, %0;" ::"n"(kComputeThreads) : "memory"); }
+template <int N>
+__device__ __forceinline__ void async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 __device__ __forceinline__ float meta_scale(uint32_t m) { return __uint_as_float(m << 16); }
 __device__ __forceinline__ float meta_offset(uint32_t m) { return __uint_as_float(m & 0xffff0000u); }
@@ -231,12 +178,24 @@ __device__ __forceinline__ Request request_of(const AttendParams &p, int i) {
     return r;
 }
 
-// One stage of the ring: the codes and the meta of 128 keys.
+// One step of a warp: the codes and the meta of 32 keys.
 template <int D>
 struct Stage {
-    unsigned char k[kUnit * D / 2], v[kUnit * D / 2];
-    uint32_t k_meta[kUnit], v_meta[kUnit];
+    unsigned char k[32 * D / 2], v[32 * D / 2];
+    uint32_t meta[2][2][16];          // block of 16 keys; keys, values
 };
+
+// Page of each 16-key block of the warp's 32 keys; -1 for keys past the end, -2 for a number outside the pool.
+__device__ __forceinline__ void load_pages(const AttendParams &p, const int32_t *table, int tok, int len, int (&page)[2]) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        page[b] = -1;
+        if (tok + 16 * b < len) {
+            page[b] = __ldg(table + ((tok + 16 * b) >> p.page_shift));
+            if (page[b] < 0 || page[b] >= p.num_pages) page[b] = -2;
+        }
+    }
+}
 
 // The walk over a CTA's share of the (request, tile of query rows, key head, 128 keys) units, in that order.
 struct Walk {
@@ -291,25 +250,24 @@ __device__ __forceinline__ void store_out(void *out, long long at, const float *
 template <int D, int NT>
 __host__ __device__ constexpr int slot_floats() { return 8 * NT * (D + 4); }
 
-// Stages of the ring: what the CTAs of an SM can hold together, at least two.
-template <int D, int NT>
-__host__ __device__ constexpr int stages() { return D == 64 ? 5 : D == 128 ? (NT == 1 ? 3 : 4) : D == 192 ? 3 : 2; }
-
 // CTAs per SM the registers are cut to
 template <int D, int NT>
-__host__ __device__ constexpr int min_ctas() { return D * NT <= 128 ? 3 : 2; }
+__host__ __device__ constexpr int min_ctas() { return D * NT <= 128 ? 4 : D * NT <= 192 ? 3 : 2; }
 
-template <int D, int NT, bool F32>
-constexpr int attend_smem() {
-    return stages<D, NT>() * (int)sizeof(Stage<D>) + (kWarps * 8 * (D + 4) + kWarps * 8 * NT * 4) * 4 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1);
+// shared memory: the warps' rings, later the warps' results; then the statistics and the queries
+template <int D>
+__host__ __device__ constexpr int ring_bytes() {
+    return kWarps * kStages * (int)sizeof(Stage<D>) > kWarps * 8 * (D + 4) * 4 ? kWarps * kStages * (int)sizeof(Stage<D>) : kWarps * 8 * (D + 4) * 4;
 }
 
+template <int D, int NT, bool F32>
+constexpr int attend_smem() { return ring_bytes<D>() + kWarps * 8 * NT * 16 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1); }
+
 // A CTA takes an equal share of all (request, tile of query rows, key head, 128 keys) units, whatever requests they belong
-// to.  One warp brings the codes into a ring of stages: a block of 16 keys of a head is one kilobyte in one page (head_dim
-// 128), so a lane fetches a block's keys, values or meta with one bulk copy, and it runs ahead over the ends of requests.
-// Pools of another layout are gathered with 16-byte copies.  Each of the four other warps works on 32 of the 128 keys
-// against the tile's 8 NT rows.  Keys are the rows of the products (m16), query rows their columns (n8), so that the usual
-// 4 to 8 query heads of a key head fill a tile:
+// to; each of its four warps works on 32 keys at a time against the tile's 8 NT rows.  A warp fetches its own codes, two
+// steps ahead, with 16-byte asynchronous copies into its own ring (every byte of a code row is used by one lane only, so
+// warps have nothing to share, and they never wait for each other until a request is done).  Keys are the rows of the products
+// (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
 template <int D, int NT, bool F32>
@@ -317,52 +275,49 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     constexpr int ROWS = 8 * NT;
     constexpr int KS = D / 16;              // steps of 16 in the product over head_dim
     constexpr int WV = D / 64;              // words of a value row per lane
+    constexpr int CH = D / 32;              // 16-byte pieces of a code row
     constexpr int LD = D + 4;
-    constexpr int STAGES = stages<D, NT>();
     constexpr float kBack = F32 ? 0x1p14f : 0x1p24f;   // takes back the powers of two of codes<F32, 0>()
     extern __shared__ __align__(128) unsigned char smem[];
-    Stage<D> *const s_stage = reinterpret_cast<Stage<D> *>(smem);
-    float *const s_o = reinterpret_cast<float *>(smem + STAGES * sizeof(Stage<D>));   // [warps][8][LD]
-    float *const s_stat = s_o + kWarps * 8 * LD;               // [warps][ROWS][4]: maximum, sum, offset sum
+    float *const s_o = reinterpret_cast<float *>(smem);        // [warps][8][LD]
+    float *const s_stat = reinterpret_cast<float *>(smem + ring_bytes<D>());    // [warps][ROWS][4]: maximum, sum, offset sum
     uint2 *const s_q = reinterpret_cast<uint2 *>(s_stat + kWarps * ROWS * 4);   // [1 or 2][NT][KS][32]
-    __shared__ uint64_t s_full[STAGES], s_empty[STAGES];
-    __shared__ uint32_t s_valid[STAGES];    // blocks that were brought, a bit each
     __shared__ long long s_sum[kWarps];
     __shared__ long long s_start;
     __shared__ int s_request;
     __shared__ bool s_last;
-    __shared__ volatile int s_gave_up;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-    if (tid == 0) {
-        for (int i = 0; i < STAGES; ++i) {
-            bar_init(&s_full[i], p.dense ? 1 : 33);   // lane 0, or lane 0 and the lanes' copies
-            bar_init(&s_empty[i], kWarps);
-        }
-        s_gave_up = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    const Stage<D> *const ring = reinterpret_cast<const Stage<D> *>(smem) + warp * kStages;
+    const uint32_t ring_at = smem_at(ring);
+    // a 16-key block of codes is CH / 2 pieces per lane: where they come from and go to
+    uint32_t piece_from[CH / 2], piece_to[CH / 2];
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+        const int piece = lane + 32 * i, key = piece / CH, part = piece - key * CH;
+        piece_from[i] = key * p.ts + part * 16;
+        piece_to[i] = key * (D / 2) + part * 16;
     }
 
     // ---- this CTA's share ----
     int n = p.batch_max;
     if (p.batch_count) n = min(max(*p.batch_count, 0), p.batch_max);
-    const int per_thread = (n + kComputeThreads - 1) / kComputeThreads;
+    const int per_thread = (n + kThreads - 1) / kThreads;
     long long mine = 0;
-    if (warp < kWarps)
-        for (int e = 0; e < per_thread; ++e) {
-            const int i = tid * per_thread + e;
-            if (i < n) {
-                const Request r = request_of<ROWS>(p, i);
-                if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
-            }
+    for (int e = 0; e < per_thread; ++e) {
+        const int i = tid * per_thread + e;
+        if (i < n) {
+            const Request r = request_of<ROWS>(p, i);
+            if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
         }
+    }
     long long before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const long long o = __shfl_up_sync(0xffffffffu, before, d);
         if (lane >= d) before += o;
     }
-    if (lane == 31 && warp < kWarps) s_sum[warp] = before;
+    if (lane == 31) s_sum[warp] = before;
     __syncthreads();
     long long total = 0;
 #pragma unroll
@@ -395,89 +350,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     walk.request = s_request;
     walk.request_start = s_start;
 
-    if (warp == kWarps) {
-        // ---- the warp that brings the codes ----
-        int stage = 0;
-        uint32_t phase = 1;      // the first round finds every stage empty
-        Piece x;
-        const int block = lane >> 2, kind = lane & 3;     // dense pools: a lane per block and kind of data
-        const int mask = (1 << p.page_shift) - 1;
-        while (next_piece<ROWS>(p, walk, x)) {
-            const int32_t *const table = p.block_table + (long long)x.r.row * p.table_ld;
-            int first_key = 0;                            // that any query sees
-            if (p.window > 0) first_key = max(max(x.r.len - x.r.queries, 0) - p.window + 1, 0);
-            int tok = (x.r.unit0 + x.unit) * kUnit + 16 * block;
-            const auto page_at = [&](int t) { return t < x.r.len ? __ldg(table + (t >> p.page_shift)) : -1; };
-            int page = page_at(tok);
-            for (int step = 0; step < x.steps; ++step, tok += kUnit) {
-                const int next = step + 1 < x.steps ? page_at(tok + kUnit) : -1;
-                const bool there = tok < x.r.len && tok + 16 > first_key;
-                const bool good = there && page >= 0 && page < p.num_pages;
-                if (there && !good && kind == 0) atomicOr(p.status, 2);
-                bar_wait(&s_empty[stage], phase, &s_gave_up, p.status);
-                const uint32_t lanes = __ballot_sync(0xffffffffu, good && !s_gave_up);
-                Stage<D> &st = s_stage[stage];
-                const bool bring = (lanes >> lane) & 1;
-                if (lane == 0) {
-                    uint32_t valid = 0;
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) valid |= ((lanes >> (4 * b)) & 1u) << b;
-                    s_valid[stage] = valid;
-                    if (p.dense) bar_expect(&s_full[stage], __popc(valid) * (16 * D + 128));
-                    else bar_arrive(&s_full[stage]);
-                }
-                __syncwarp();
-                const long long at = (long long)page * p.ps + x.head * p.hs + (long long)(tok & mask) * p.ts;
-                const long long meta_at = (long long)page * p.mps + x.head * p.mhs + (long long)(tok & mask) * p.mts;
-                if (p.dense) {
-                    if (bring) {
-                        if (kind == 0) bulk_copy(st.k + 8 * D * block, p.k_codes + at, 8 * D, &s_full[stage]);
-                        else if (kind == 1) bulk_copy(st.v + 8 * D * block, p.v_codes + at, 8 * D, &s_full[stage]);
-                        else if (kind == 2) bulk_copy(st.k_meta + 16 * block, p.k_meta + meta_at, 64, &s_full[stage]);
-                        else bulk_copy(st.v_meta + 16 * block, p.v_meta + meta_at, 64, &s_full[stage]);
-                    }
-                } else {
-                    if (bring) {                          // the four lanes of a block take four keys each
-#pragma unroll 1
-                        for (int e = 0; e < 4; ++e) {
-                            const int key = 4 * kind + e;
-                            const unsigned char *const k = p.k_codes + at + (long long)key * p.ts, *const v = p.v_codes + at + (long long)key * p.ts;
-#pragma unroll
-                            for (int i = 0; i < D / 32; ++i) {
-                                async_copy<16>(st.k + (16 * block + key) * (D / 2) + 16 * i, k + 16 * i);
-                                async_copy<16>(st.v + (16 * block + key) * (D / 2) + 16 * i, v + 16 * i);
-                            }
-                            async_copy<4>(st.k_meta + 16 * block + key, p.k_meta + meta_at + (long long)key * p.mts);
-                            async_copy<4>(st.v_meta + 16 * block + key, p.v_meta + meta_at + (long long)key * p.mts);
-                        }
-                    }
-                    async_arrive(&s_full[stage]);
-                }
-                page = next;
-                if (++stage == STAGES) {
-                    stage = 0;
-                    phase ^= 1;
-                }
-            }
-            walk.u += x.steps;
-        }
-        // the compute warps have waited for every stage, unless they gave up: then the copies are waited for here
-        if (s_gave_up)
-            for (int i = 0; i < STAGES; ++i) {
-                const long long t0 = clock64();
-                while (!bar_try(&s_full[stage], phase) && clock64() - t0 < 200000000ll) {}
-                if (++stage == STAGES) {
-                    stage = 0;
-                    phase ^= 1;
-                }
-            }
-        return;
-    }
-
-    // ---- the warps that compute ----
     const long long u_first = walk.u;
-    int stage = 0;
-    uint32_t phase = 0;
     Piece x;
     while (next_piece<ROWS>(p, walk, x)) {
         const Request &r = x.r;
@@ -485,6 +358,48 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         const long long item_begin = x.item_begin, item_end = x.item_end;
         const int total_rows = r.queries * p.group;
         const int row0 = tile * ROWS;
+
+        // ---- the first keys and values on their way ----
+        const int32_t *const table = p.block_table + (long long)r.row * p.table_ld;
+        int first_key = 0;                                // that any query sees
+        if (p.window > 0) first_key = max(max(r.len - r.queries, 0) - p.window + 1, 0);
+        const unsigned char *const k_head = p.k_codes + head * p.hs, *const v_head = p.v_codes + head * p.hs;
+        const uint32_t *const meta_head = (lane < 16 ? p.k_meta : p.v_meta) + head * p.mhs + (lane & 15) * p.mts;
+        int tok = (r.unit0 + x.unit) * kUnit + warp * 32;
+        int page[2];
+        uint32_t brought = 0;                             // two bits per step on the way, the latest lowest: its blocks
+        uint32_t fill = ring_at;
+        // fetches the 32 keys at t, whose pages are in `page`
+        const auto fetch = [&](int t) {
+            brought <<= 2;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int at = t + 16 * b;
+                if (page[b] >= 0 && at + 16 > first_key) {
+                    brought |= 1u << b;
+                    const int place = at & ((1 << p.page_shift) - 1);
+                    const unsigned long long off = (unsigned long long)(uint32_t)page[b] * p.ps + (uint32_t)place * p.ts;
+                    const unsigned long long moff = (unsigned long long)(uint32_t)page[b] * p.mps + (uint32_t)place * p.mts;
+                    const uint32_t to = fill + b * 8 * D;
+#pragma unroll
+                    for (int i = 0; i < CH / 2; ++i) {
+                        async_copy<16>(to + piece_to[i], k_head + off + piece_from[i]);
+                        async_copy<16>(to + 16 * D + piece_to[i], v_head + off + piece_from[i]);
+                    }
+                    async_copy<4>(fill + 32 * D + b * 128 + lane * 4, meta_head + moff);
+                } else if (page[b] == -2 && at + 16 > first_key && lane == 0) {
+                    atomicOr(p.status, 2);
+                }
+            }
+            async_commit();
+            fill = fill == ring_at + (kStages - 1) * sizeof(Stage<D>) ? ring_at : fill + (uint32_t)sizeof(Stage<D>);
+        };
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            load_pages(p, table, i < steps ? tok + i * kUnit : 0x7fffff00, r.len, page);
+            fetch(tok + i * kUnit);
+        }
+        load_pages(p, table, kStages - 1 < steps ? tok + (kStages - 1) * kUnit : 0x7fffff00, r.len, page);
 
         // ---- the tile's queries, as halves, laid out as the products take them ----
         float cq[NT][2], sq[NT][2];
@@ -576,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
             all_low = p.window > 0 ? max(last, 0) - p.window + 1 : 0;
             any_low = p.window > 0 ? max(first, 0) - p.window + 1 : 0;
         }
-        sync_compute();
+        __syncthreads();
 
         float o[KS][NT][4];
         float top[NT][2], sum[NT][2], off[NT][2];
@@ -594,11 +509,14 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 sum[nt][h] = off[nt][h] = 0.f;
             }
 
-        int tok = (r.unit0 + x.unit) * kUnit + warp * 32;
+        const Stage<D> *drain = ring;
         for (int step = 0; step < steps; ++step, tok += kUnit) {
-            bar_wait(&s_full[stage], phase, &s_gave_up, p.status);
-            const Stage<D> &st = s_stage[stage];
-            const uint32_t valid = s_valid[stage] >> (2 * warp);
+            fetch(tok + (kStages - 1) * kUnit);
+            load_pages(p, table, step + kStages < steps ? tok + kStages * kUnit : 0x7fffff00, r.len, page);
+            async_wait<kStages - 1>();
+            __syncwarp();
+            const Stage<D> &st = *drain;
+            const uint32_t valid = brought >> (2 * (kStages - 1));
             const bool work = tok < any_high && tok + 32 > any_low && tok < r.len;
             const bool whole = tok + 32 <= all_high && tok >= all_low && (valid & 3) == 3;
 
@@ -610,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        load_words<D / 32>(st.k + (warp * 32 + 16 * b + 8 * e + g) * (D / 2) + c * (D / 8), kw[b][e]);
+                        load_words<D / 32>(st.k + (16 * b + 8 * e + g) * (D / 2) + c * (D / 8), kw[b][e]);
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -645,8 +563,8 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        km[b][e] = st.k_meta[warp * 32 + 16 * b + 8 * e + g];
-                        vmeta[b][e] = st.v_meta[warp * 32 + 16 * b + 8 * e + g];
+                        km[b][e] = st.meta[b][0][8 * e + g];
+                        vmeta[b][e] = st.meta[b][1][8 * e + g];
                     }
                 uint32_t pb[2][NT][2], pb2[2][NT][2];
             // whole: every row of the tile sees all 32 keys
@@ -747,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        load_words<WV>(st.v + (warp * 32 + 16 * b + 2 * c + (e & 1) + 8 * (e >> 1)) * (D / 2) + g * (D / 16), vw[b][e]);
+                        load_words<WV>(st.v + (16 * b + 2 * c + (e & 1) + 8 * (e >> 1)) * (D / 2) + g * (D / 16), vw[b][e]);
 
             // ---- O^T += V^T P^T ----
 #pragma unroll
@@ -793,13 +711,11 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 }
             }
             }
-            __syncwarp();
-            if (lane == 0) bar_arrive(&s_empty[stage]);
-            if (++stage == STAGES) {
-                stage = 0;
-                phase ^= 1;
-            }
+            __syncwarp();     // the next fetch fills what was read here
+            drain = drain == ring + kStages - 1 ? ring : drain + 1;
         }
+        async_wait<0>();
+        __syncthreads();      // the rings become the place of the results
 
         // ---- the four warps' results together ----
 #pragma unroll
@@ -825,14 +741,14 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         const int my_row = tid >> 4, my_dim = (tid & 15) * 4;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            if (nt > 0) sync_compute();
+            if (nt > 0) __syncthreads();
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
                     *reinterpret_cast<float2 *>(s_o + (warp * 8 + 2 * c + h) * LD + g * (D / 8) + 2 * i) =
                         make_float2(o[i][nt][h] * kBack, o[i][nt][2 + h] * (kBack / 16));
-            sync_compute();
+            __syncthreads();
             const int row = nt * 8 + my_row;
             float m = kNoMax, f[kWarps], l = 0.f, b = 0.f, acc[PER];
 #pragma unroll
@@ -880,14 +796,16 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
             // the last of the CTAs that share this item adds up what they left, in the order of the keys
             const int c0 = (int)(((item_begin + 1) * ctas - 1) / total), c1 = (int)((item_end * ctas - 1) / total);
             __threadfence();
-            sync_compute();
+            __syncthreads();
             if (tid == 0) {
                 s_last = atomicAdd(p.tickets + c0, 1u) == (uint32_t)(c1 - c0);
                 if (s_last) p.tickets[c0] = 0;
                 __threadfence();
             }
-            sync_compute();
+            __syncthreads();
             if (s_last) {
+                // the item opens the share of every CTA but the first, and of that one when the share begins with it
+                const int first_slot = total * c0 / ctas == item_begin ? 0 : 1;
 #pragma unroll 1
                 for (int nt = 0; nt < NT; ++nt) {
                     const int row = nt * 8 + my_row, abs_row = row0 + row;
@@ -895,10 +813,9 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                     float m = kNoMax, l = 0.f, b = 0.f, acc[PER];
 #pragma unroll
                     for (int i = 0; i < PER; ++i) acc[i] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
                     for (int k = c0; k <= c1; ++k) {
-                        const bool leads = total * k / ctas >= item_begin;
-                        const float *const d = p.partial + (2 * (long long)k + (leads ? 0 : 1)) * slot_floats<D, NT>() + row * LD;
+                        const float *const d = p.partial + (2 * (long long)k + (k == c0 ? first_slot : 0)) * slot_floats<D, NT>() + row * LD;
                         const float4 st = __ldcg(reinterpret_cast<const float4 *>(d + D));
                         float4 x[PER / 4];
 #pragma unroll
@@ -928,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 }
             }
         }
-        sync_compute();
+        __syncthreads();
         walk.u += steps;
     }
 }
@@ -1064,8 +981,6 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.kv_heads = c.kv_heads;
     p.group = c.q_heads / c.kv_heads;
     p.min_units = 1;
-    p.dense = c.token_stride == c.head_dim / 2 && c.meta_token_stride == 1 && c.meta_page_stride % 4 == 0 && c.meta_head_stride % 4 == 0 &&
-              ((reinterpret_cast<uintptr_t>(c.k_meta) | reinterpret_cast<uintptr_t>(c.v_meta)) & 15) == 0;
     p.scale_log2 = a->scale * kLog2e;
     const bool f32 = a->dtype == FI_F32;
     const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;
