@@ -487,7 +487,8 @@ int64_t fi_head_norm_rope_workspace(int32_t head_dim);
  * offset NaN (it reads as NaN).
  * The pools are the caller's: codes [num_pages][kv_heads][page_size][head_dim / 2] bytes and meta
  * [num_pages][kv_heads][page_size] bf16 pairs, with free strides between pages, heads and tokens, the same for keys
- * and values (bytes for codes, multiples of 16; pairs for meta; the strides of a page and of page_size tokens below 2^31).
+ * and values (bytes for codes, multiples of 16; pairs for meta; the strides of a page and of page_size tokens below 2^31, and the pages
+ * of a pool within 64 GiB of codes and 16 GiB of meta).
  * fi_kv_create keeps geometry and pointers and owns the scratch of fi_kv_attend (partial results of requests whose keys
  * are cut over several CTAs: 32 KiB to 256 KiB per CTA slot, at most 8 CTAs per SM) and a status word.
  */

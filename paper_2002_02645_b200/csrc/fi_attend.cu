@@ -42,7 +42,7 @@ struct AttendParams {
     int32_t *status;
     long long q_ts, q_hs, out_ts, out_hs;             // elements
     long long hs, mhs;                                // pools: strides of heads,
-    uint32_t ps, ts, mps, mts;                        // of pages and of tokens (bytes of codes, pairs of meta)
+    uint32_t ps, ts, mps, mts;                        // of pages and of tokens (codes: 16 bytes, meta: pairs)
     long long table_ld;
     int rows, max_blocks, batch_max, max_tokens, window;
     int num_pages, page_shift, kv_heads, group;
@@ -185,16 +185,12 @@ struct Stage {
     uint32_t meta[2][2][16];          // block of 16 keys; keys, values
 };
 
-// Page of each 16-key block of the warp's 32 keys; -1 for keys past the end, -2 for a number outside the pool.
-__device__ __forceinline__ void load_pages(const AttendParams &p, const int32_t *table, int tok, int len, int (&page)[2]) {
+constexpr uint32_t kNoPage = 0xffffffffu;
+
+// Page of each 16-key block of the warp's 32 keys, kNoPage for keys past the end.
+__device__ __forceinline__ void load_pages(const AttendParams &p, const int32_t *table, int tok, int len, uint32_t (&page)[2]) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        page[b] = -1;
-        if (tok + 16 * b < len) {
-            page[b] = __ldg(table + ((tok + 16 * b) >> p.page_shift));
-            if (page[b] < 0 || page[b] >= p.num_pages) page[b] = -2;
-        }
-    }
+    for (int b = 0; b < 2; ++b) page[b] = tok + 16 * b < len ? min((uint32_t)__ldg(table + ((tok + 16 * b) >> p.page_shift)), kNoPage - 1) : kNoPage;
 }
 
 // The walk over a CTA's share of the (request, tile of query rows, key head, 128 keys) units, in that order.
@@ -290,15 +286,6 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     const Stage<D> *const ring = reinterpret_cast<const Stage<D> *>(smem) + warp * kStages;
     const uint32_t ring_at = smem_at(ring);
-    // a 16-key block of codes is CH / 2 pieces per lane: where they come from and go to
-    uint32_t piece_from[CH / 2], piece_to[CH / 2];
-#pragma unroll
-    for (int i = 0; i < CH / 2; ++i) {
-        const int piece = lane + 32 * i, key = piece / CH, part = piece - key * CH;
-        piece_from[i] = key * p.ts + part * 16;
-        piece_to[i] = key * (D / 2) + part * 16;
-    }
-
     // ---- this CTA's share ----
     int n = p.batch_max;
     if (p.batch_count) n = min(max(*p.batch_count, 0), p.batch_max);
@@ -363,36 +350,44 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         const int32_t *const table = p.block_table + (long long)r.row * p.table_ld;
         int first_key = 0;                                // that any query sees
         if (p.window > 0) first_key = max(max(r.len - r.queries, 0) - p.window + 1, 0);
-        const unsigned char *const k_head = p.k_codes + head * p.hs, *const v_head = p.v_codes + head * p.hs;
-        const uint32_t *const meta_head = (lane < 16 ? p.k_meta : p.v_meta) + head * p.mhs + (lane & 15) * p.mts;
+        // a 16-key block of codes is CH / 2 pieces of 16 bytes per lane; where they are in a page's first block:
+        const unsigned char *k_from[CH / 2], *v_from[CH / 2];
+#pragma unroll
+        for (int i = 0; i < CH / 2; ++i) {
+            const int piece = lane + 32 * i, key = piece / CH, part = piece - key * CH;
+            const long long at = head * p.hs + ((long long)key * p.ts + part) * 16;
+            k_from[i] = p.k_codes + at;
+            v_from[i] = p.v_codes + at;
+        }
+        const uint32_t *const meta_from = (lane < 16 ? p.k_meta : p.v_meta) + head * p.mhs + (lane & 15) * p.mts;
+        const int place_mask = (1 << p.page_shift) - 1;
         int tok = (r.unit0 + x.unit) * kUnit + warp * 32;
-        int page[2];
+        uint32_t page[2];
         uint32_t brought = 0;                             // two bits per step on the way, the latest lowest: its blocks
-        uint32_t fill = ring_at;
+        uint32_t fill = ring_at + lane * 16;
         // fetches the 32 keys at t, whose pages are in `page`
         const auto fetch = [&](int t) {
             brought <<= 2;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int at = t + 16 * b;
-                if (page[b] >= 0 && at + 16 > first_key) {
-                    brought |= 1u << b;
-                    const int place = at & ((1 << p.page_shift) - 1);
-                    const unsigned long long off = (unsigned long long)(uint32_t)page[b] * p.ps + (uint32_t)place * p.ts;
-                    const unsigned long long moff = (unsigned long long)(uint32_t)page[b] * p.mps + (uint32_t)place * p.mts;
-                    const uint32_t to = fill + b * 8 * D;
+                if (page[b] < (uint32_t)p.num_pages) {
+                    if (at + 16 > first_key) {
+                        brought |= 1u << b;
+                        const uint32_t place = at & place_mask, off = page[b] * p.ps + place * p.ts, moff = page[b] * p.mps + place * p.mts;
 #pragma unroll
-                    for (int i = 0; i < CH / 2; ++i) {
-                        async_copy<16>(to + piece_to[i], k_head + off + piece_from[i]);
-                        async_copy<16>(to + 16 * D + piece_to[i], v_head + off + piece_from[i]);
+                        for (int i = 0; i < CH / 2; ++i) {
+                            async_copy<16>(fill + b * 8 * D + i * 512, k_from[i] + off * 16ull);
+                            async_copy<16>(fill + 16 * D + b * 8 * D + i * 512, v_from[i] + off * 16ull);
+                        }
+                        async_copy<4>(fill - lane * 12 + 32 * D + b * 128, meta_from + moff);
                     }
-                    async_copy<4>(fill + 32 * D + b * 128 + lane * 4, meta_head + moff);
-                } else if (page[b] == -2 && at + 16 > first_key && lane == 0) {
+                } else if (page[b] != kNoPage && at + 16 > first_key && lane == 0) {
                     atomicOr(p.status, 2);
                 }
             }
             async_commit();
-            fill = fill == ring_at + (kStages - 1) * sizeof(Stage<D>) ? ring_at : fill + (uint32_t)sizeof(Stage<D>);
+            fill = fill >= ring_at + (kStages - 1) * (uint32_t)sizeof(Stage<D>) ? ring_at + lane * 16 : fill + (uint32_t)sizeof(Stage<D>);
         };
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) {
@@ -517,7 +512,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
             __syncwarp();
             const Stage<D> &st = *drain;
             const uint32_t valid = brought >> (2 * (kStages - 1));
-            const bool work = tok < any_high && tok + 32 > any_low && tok < r.len;
+            const bool work = tok < any_high && tok + 32 > any_low;
             const bool whole = tok + 32 <= all_high && tok >= all_low && (valid & 3) == 3;
 
             if (work) {
@@ -964,9 +959,9 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.q_hs = a->q_head_stride;
     p.out_ts = a->out_token_stride;
     p.out_hs = a->out_head_stride;
-    p.ps = (uint32_t)c.page_stride;
+    p.ps = (uint32_t)(c.page_stride / 16);
     p.hs = c.head_stride;
-    p.ts = (uint32_t)c.token_stride;
+    p.ts = (uint32_t)(c.token_stride / 16);
     p.mps = (uint32_t)c.meta_page_stride;
     p.mhs = c.meta_head_stride;
     p.mts = (uint32_t)c.meta_token_stride;

@@ -550,9 +550,12 @@ fi_status_t fi_kv_create(const fi_kv_config_t *cfg, fi_kv_t **out) {
         cfg->token_stride % 16 != 0 || cfg->page_stride < 0 || cfg->head_stride < 0 || cfg->token_stride < d / 2 ||
         cfg->meta_page_stride < 0 || cfg->meta_head_stride < 0 || cfg->meta_token_stride < 1 || cfg->page_stride > 2147483647ll ||
         cfg->token_stride > 2147483647ll / cfg->page_size || cfg->meta_page_stride > 2147483647ll ||
-        cfg->meta_token_stride > 2147483647ll / cfg->page_size) {
+        cfg->meta_token_stride > 2147483647ll / cfg->page_size ||
+        (double)cfg->num_pages * (double)cfg->page_stride + (double)cfg->page_size * (double)cfg->token_stride >= 16.0 * 4294967296.0 ||
+        (double)cfg->num_pages * (double)cfg->meta_page_stride + (double)cfg->page_size * (double)cfg->meta_token_stride >= 4294967296.0) {
         set_error("fi_kv_create: codes and their strides must be multiples of 16 bytes, meta of 4, strides not negative, tokens "
-                  "not overlapping, and strides of pages and of page_size tokens below 2^31");
+                  "not overlapping, strides of pages and of page_size tokens below 2^31, pools of at most 64 GiB of codes and "
+                  "16 GiB of meta");
         return FI_ERR_INVALID_ARG;
     }
     fi_kv *kv = new (std::nothrow) fi_kv();
