@@ -23,8 +23,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kUnit = 128;                 // keys a CTA takes per step: 32 per warp
-constexpr int kStages = 3;                 // steps a warp has on the way
+constexpr int kStages = 2;                 // steps of a warp in its ring: the one it works on and the next
 constexpr float kMinScale = 0x1p-40f;      // smallest scale append stores
 constexpr float kNoMax = -1e30f;           // maximum of nothing
 constexpr float kLog2e = 1.4426950408889634f;
@@ -155,7 +154,15 @@ struct Request {
     int unit0, units, row_tiles;          // key units it reads, tiles of query rows per key head
 };
 
-template <int ROWS>
+// blocks of 16 keys a warp takes per step, and keys a CTA does (a unit): with 8 rows there are registers for four blocks,
+// whose products, exponentials and copies overlap; two blocks took 10 % longer on 64 requests of 100 to 8,192 keys
+template <int D, int NT>
+__host__ __device__ constexpr int blocks() { return D <= 128 && NT == 1 ? 4 : 2; }
+
+template <int D, int NT>
+__host__ __device__ constexpr int unit_keys() { return kWarps * 16 * blocks<D, NT>(); }
+
+template <int ROWS, int UNIT>
 __device__ __forceinline__ Request request_of(const AttendParams &p, int i) {
     Request r;
     r.first_token = p.cu_tokens ? p.cu_tokens[i] : i;
@@ -171,29 +178,30 @@ __device__ __forceinline__ Request request_of(const AttendParams &p, int i) {
         lo = (long long)max(r.len - r.queries, 0) - p.window + 1;
         if (lo < 0) lo = 0;
     }
-    r.unit0 = (int)(lo / kUnit);
-    const int end = (r.len + kUnit - 1) / kUnit;
+    r.unit0 = (int)(lo / UNIT);
+    const int end = (r.len + UNIT - 1) / UNIT;
     r.units = end > r.unit0 ? end - r.unit0 : 1;      // a request without keys still gets its zeros
     r.row_tiles = (int)(((long long)r.queries * p.group + ROWS - 1) / ROWS);
     return r;
 }
 
-// One step of a warp: the codes and the meta of 32 keys.
-template <int D>
+// One step of a warp: the codes and the meta of 16 NB keys.
+template <int D, int NB>
 struct Stage {
-    unsigned char k[32 * D / 2], v[32 * D / 2];
-    uint32_t meta[2][2][16];          // block of 16 keys; keys, values
+    unsigned char k[NB * 8 * D], v[NB * 8 * D];
+    uint32_t meta[NB][2][16];         // block of 16 keys; keys, values
+};
+
+// What the weights need of a key, worked out once per key.
+template <int NB>
+struct KeyFactors {
+    float4 f[16 * NB];                // scale and offset of the key, log2 of the value's scale and its reciprocal
+    float off[16 * NB];               // the value's offset over its scale
 };
 
 constexpr uint32_t kNoPage = 0xffffffffu;
 
-// Page of each 16-key block of the warp's 32 keys, kNoPage for keys past the end.
-__device__ __forceinline__ void load_pages(const AttendParams &p, const int32_t *table, int tok, int len, uint32_t (&page)[2]) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) page[b] = tok + 16 * b < len ? min((uint32_t)__ldg(table + ((tok + 16 * b) >> p.page_shift)), kNoPage - 1) : kNoPage;
-}
-
-// The walk over a CTA's share of the (request, tile of query rows, key head, 128 keys) units, in that order.
+// The walk over a CTA's share of the (request, tile of query rows, key head, unit of keys) units, in that order.
 struct Walk {
     long long u, u_end, request_start;
     int request;
@@ -206,19 +214,31 @@ struct Piece {
     long long item_begin, item_end;   // all units of that request, tile and head
 };
 
-template <int ROWS>
+// a * b / c without a 64-bit division where 32 bits hold the product
+__device__ __forceinline__ long long mul_div(long long a, long long b, long long c) {
+    const unsigned long long m = (unsigned long long)a * (unsigned long long)b;
+    return m >> 32 ? (long long)(m / (unsigned long long)c) : (long long)((uint32_t)m / (uint32_t)c);
+}
+
+// the CTA whose share [total i / ctas, total (i + 1) / ctas) holds unit u
+__device__ __forceinline__ long long owner_of(long long u, long long ctas, long long total) {
+    const unsigned long long m = (unsigned long long)(u + 1) * (unsigned long long)ctas - 1;
+    return m >> 32 || total >> 32 ? (long long)(m / (unsigned long long)total) : (long long)((uint32_t)m / (uint32_t)total);
+}
+
+template <int ROWS, int UNIT>
 __device__ __forceinline__ bool next_piece(const AttendParams &p, Walk &w, Piece &x) {
     while (w.u < w.u_end) {
-        x.r = request_of<ROWS>(p, w.request);
+        x.r = request_of<ROWS, UNIT>(p, w.request);
         const long long here = x.r.queries > 0 ? (long long)x.r.units * x.r.row_tiles * p.kv_heads : 0;
         if (w.u >= w.request_start + here) {
             w.request_start += here;
             ++w.request;
             continue;
         }
-        const long long in_request = (w.u - w.request_start) / x.r.units;
+        const long long in_request = mul_div(w.u - w.request_start, 1, x.r.units);
         x.unit = (int)((w.u - w.request_start) - in_request * x.r.units);
-        x.tile = (int)(in_request / p.kv_heads);
+        x.tile = (int)mul_div(in_request, 1, p.kv_heads);
         x.head = (int)(in_request - (long long)x.tile * p.kv_heads);
         x.item_begin = w.u - x.unit;
         x.item_end = x.item_begin + x.r.units;
@@ -248,21 +268,24 @@ __host__ __device__ constexpr int slot_floats() { return 8 * NT * (D + 4); }
 
 // CTAs per SM the registers are cut to
 template <int D, int NT>
-__host__ __device__ constexpr int min_ctas() { return D * NT <= 128 ? 4 : D * NT <= 192 ? 3 : 2; }
+__host__ __device__ constexpr int min_ctas() { return D * NT <= 192 ? 3 : 2; }
 
 // shared memory: the warps' rings, later the warps' results; then the statistics and the queries
-template <int D>
+template <int D, int NT>
 __host__ __device__ constexpr int ring_bytes() {
-    return kWarps * kStages * (int)sizeof(Stage<D>) > kWarps * 8 * (D + 4) * 4 ? kWarps * kStages * (int)sizeof(Stage<D>) : kWarps * 8 * (D + 4) * 4;
+    return kWarps * kStages * (int)sizeof(Stage<D, blocks<D, NT>()>) > kWarps * 8 * (D + 4) * 4
+               ? kWarps * kStages * (int)sizeof(Stage<D, blocks<D, NT>()>) : kWarps * 8 * (D + 4) * 4;
 }
 
 template <int D, int NT, bool F32>
-constexpr int attend_smem() { return ring_bytes<D>() + kWarps * 8 * NT * 16 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1); }
+constexpr int attend_smem() {
+    return ring_bytes<D, NT>() + kWarps * 8 * NT * 16 + NT * (D / 16) * 32 * 8 * (F32 ? 2 : 1);
+}
 
-// A CTA takes an equal share of all (request, tile of query rows, key head, 128 keys) units, whatever requests they belong
-// to; each of its four warps works on 32 keys at a time against the tile's 8 NT rows.  A warp fetches its own codes, two
-// steps ahead, with 16-byte asynchronous copies into its own ring (every byte of a code row is used by one lane only, so
-// warps have nothing to share, and they never wait for each other until a request is done).  Keys are the rows of the products
+// A CTA takes an equal share of all (request, tile of query rows, key head, unit of keys) units, whatever requests they
+// belong to; each of its four warps works on a quarter of a unit at a time against the tile's 8 NT rows.  A warp fetches its
+// own codes, a step ahead, with 16-byte asynchronous copies into its own ring (every byte of a code row is used by one lane
+// only, so warps have nothing to share, and they never wait for each other until a request is done).  Keys are the rows of the products
 // (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
@@ -273,10 +296,11 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     constexpr int WV = D / 64;              // words of a value row per lane
     constexpr int CH = D / 32;              // 16-byte pieces of a code row
     constexpr int LD = D + 4;
+    constexpr int NB = blocks<D, NT>(), UNIT = unit_keys<D, NT>(), WARP_KEYS = 16 * NB;
     constexpr float kBack = F32 ? 0x1p14f : 0x1p24f;   // takes back the powers of two of codes<F32, 0>()
     extern __shared__ __align__(128) unsigned char smem[];
     float *const s_o = reinterpret_cast<float *>(smem);        // [warps][8][LD]
-    float *const s_stat = reinterpret_cast<float *>(smem + ring_bytes<D>());    // [warps][ROWS][4]: maximum, sum, offset sum
+    float *const s_stat = reinterpret_cast<float *>(smem + ring_bytes<D, NT>());    // [warps][ROWS][4]: maximum, sum, offset sum
     uint2 *const s_q = reinterpret_cast<uint2 *>(s_stat + kWarps * ROWS * 4);   // [1 or 2][NT][KS][32]
     __shared__ long long s_sum[kWarps];
     __shared__ long long s_start;
@@ -284,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     __shared__ bool s_last;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
-    const Stage<D> *const ring = reinterpret_cast<const Stage<D> *>(smem) + warp * kStages;
+    Stage<D, NB> *const ring = reinterpret_cast<Stage<D, NB> *>(smem) + warp * kStages;
     const uint32_t ring_at = smem_at(ring);
     // ---- this CTA's share ----
     int n = p.batch_max;
@@ -294,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     for (int e = 0; e < per_thread; ++e) {
         const int i = tid * per_thread + e;
         if (i < n) {
-            const Request r = request_of<ROWS>(p, i);
+            const Request r = request_of<ROWS, UNIT>(p, i);
             if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
         }
     }
@@ -315,17 +339,17 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     }
     before -= mine;
     if (total == 0) return;
-    long long ctas = total / p.min_units;
+    long long ctas = mul_div(total, 1, p.min_units);
     ctas = ctas < 1 ? 1 : ctas > gridDim.x ? gridDim.x : ctas;
     if (blockIdx.x >= ctas) return;
     Walk walk;
-    walk.u = total * blockIdx.x / ctas;
-    walk.u_end = total * (blockIdx.x + 1) / ctas;
+    walk.u = mul_div(total, blockIdx.x, ctas);
+    walk.u_end = mul_div(total, blockIdx.x + 1, ctas);
     if (before <= walk.u && walk.u < before + mine) {
         int i = tid * per_thread;
         long long at = before;
         for (;; ++i) {
-            const Request r = request_of<ROWS>(p, i);
+            const Request r = request_of<ROWS, UNIT>(p, i);
             const long long here = r.queries > 0 ? (long long)r.units * r.row_tiles * p.kv_heads : 0;
             if (walk.u < at + here) break;
             at += here;
@@ -339,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
 
     const long long u_first = walk.u;
     Piece x;
-    while (next_piece<ROWS>(p, walk, x)) {
+    while (next_piece<ROWS, UNIT>(p, walk, x)) {
         const Request &r = x.r;
         const int head = x.head, tile = x.tile, steps = x.steps;
         const long long item_begin = x.item_begin, item_end = x.item_end;
@@ -361,40 +385,41 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         }
         const uint32_t *const meta_from = (lane < 16 ? p.k_meta : p.v_meta) + head * p.mhs + (lane & 15) * p.mts;
         const int place_mask = (1 << p.page_shift) - 1;
-        int tok = (r.unit0 + x.unit) * kUnit + warp * 32;
-        uint32_t page[2];
-        uint32_t brought = 0;                             // two bits per step on the way, the latest lowest: its blocks
+        int tok = (r.unit0 + x.unit) * UNIT + warp * WARP_KEYS;
+        // lane l looks up the page of block l mod NB, kNoPage past the end
+        const auto page_at = [&](int t) {
+            t += 16 * (lane & (NB - 1));
+            return t < r.len ? min((uint32_t)__ldg(table + (t >> p.page_shift)), kNoPage - 1) : kNoPage;
+        };
+        uint32_t brought = 0;                             // NB bits per step on the way, the latest lowest: its blocks
         uint32_t fill = ring_at + lane * 16;
-        // fetches the 32 keys at t, whose pages are in `page`
-        const auto fetch = [&](int t) {
-            brought <<= 2;
+        // fetches the warp's keys at t, whose pages the lanes hold
+        const auto fetch = [&](int t, uint32_t page_l) {
+            brought <<= NB;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t page = __shfl_sync(0xffffffffu, page_l, b);
                 const int at = t + 16 * b;
-                if (page[b] < (uint32_t)p.num_pages) {
+                if (page < (uint32_t)p.num_pages) {
                     if (at + 16 > first_key) {
                         brought |= 1u << b;
-                        const uint32_t place = at & place_mask, off = page[b] * p.ps + place * p.ts, moff = page[b] * p.mps + place * p.mts;
+                        const uint32_t place = at & place_mask, off = page * p.ps + place * p.ts, moff = page * p.mps + place * p.mts;
 #pragma unroll
                         for (int i = 0; i < CH / 2; ++i) {
                             async_copy<16>(fill + b * 8 * D + i * 512, k_from[i] + off * 16ull);
-                            async_copy<16>(fill + 16 * D + b * 8 * D + i * 512, v_from[i] + off * 16ull);
+                            async_copy<16>(fill + (NB + b) * 8 * D + i * 512, v_from[i] + off * 16ull);
                         }
-                        async_copy<4>(fill - lane * 12 + 32 * D + b * 128, meta_from + moff);
+                        async_copy<4>(fill - lane * 12 + NB * 16 * D + b * 128, meta_from + moff);
                     }
-                } else if (page[b] != kNoPage && at + 16 > first_key && lane == 0) {
+                } else if (page != kNoPage && at + 16 > first_key && lane == 0) {
                     atomicOr(p.status, 2);
                 }
             }
             async_commit();
-            fill = fill >= ring_at + (kStages - 1) * (uint32_t)sizeof(Stage<D>) ? ring_at + lane * 16 : fill + (uint32_t)sizeof(Stage<D>);
+            fill = fill >= ring_at + (uint32_t)sizeof(Stage<D, NB>) ? ring_at + lane * 16 : fill + (uint32_t)sizeof(Stage<D, NB>);
         };
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) {
-            load_pages(p, table, i < steps ? tok + i * kUnit : 0x7fffff00, r.len, page);
-            fetch(tok + i * kUnit);
-        }
-        load_pages(p, table, kStages - 1 < steps ? tok + (kStages - 1) * kUnit : 0x7fffff00, r.len, page);
+        fetch(tok, page_at(tok));
+        uint32_t next_page = steps > 1 ? page_at(tok + UNIT) : kNoPage;
 
         // ---- the tile's queries, as halves, laid out as the products take them ----
         float cq[NT][2], sq[NT][2];
@@ -504,102 +529,104 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 sum[nt][h] = off[nt][h] = 0.f;
             }
 
-        const Stage<D> *drain = ring;
-        for (int step = 0; step < steps; ++step, tok += kUnit) {
-            fetch(tok + (kStages - 1) * kUnit);
-            load_pages(p, table, step + kStages < steps ? tok + kStages * kUnit : 0x7fffff00, r.len, page);
-            async_wait<kStages - 1>();
+        Stage<D, NB> *drain = ring;
+        for (int step = 0; step < steps; ++step, tok += UNIT) {
+            fetch(tok + UNIT, next_page);
+            next_page = step + 2 < steps ? page_at(tok + 2 * UNIT) : kNoPage;
+            async_wait<1>();
             __syncwarp();
-            const Stage<D> &st = *drain;
-            const uint32_t valid = brought >> (2 * (kStages - 1));
-            const bool work = tok < any_high && tok + 32 > any_low;
-            const bool whole = tok + 32 <= all_high && tok >= all_low && (valid & 3) == 3;
+            Stage<D, NB> &st = *drain;
+            const uint32_t valid = (brought >> NB) & ((1u << NB) - 1);
+            const bool work = tok < any_high && tok + WARP_KEYS > any_low;
+            const bool whole = tok + WARP_KEYS <= all_high && tok >= all_low && valid == (1u << NB) - 1;
 
             if (work) {
                 // ---- S^T = K Q^T: lane (g, c) holds the c-th quarter of keys g and g + 8 of each block of 16 ----
-                float s[2][NT][4];
-                uint32_t kw[2][2][D / 32];
+                float s[NB][NT][4];
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        load_words<D / 32>(st.k + (16 * b + 8 * e + g) * (D / 2) + c * (D / 8), kw[b][e]);
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[b][nt][e] = 0.f;
+                uint32_t kw[NB][2][D / 32];
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        load_words<D / 32>(st.k + (16 * b + 8 * e + g) * (D / 2) + c * (D / 8), kw[b][e]);
+                // the codes of the keys are in registers: their place takes the keys' factors
+                KeyFactors<NB> &my_key = *reinterpret_cast<KeyFactors<NB> *>(st.k);
+                static_assert(sizeof(KeyFactors<NB>) <= sizeof(st.k), "factors must fit");
+                __syncwarp();
+#pragma unroll
+                for (int k = lane; k < WARP_KEYS; k += 32) {
+                    const uint32_t km = st.meta[k >> 4][0][k & 15], vm = st.meta[k >> 4][1][k & 15];
+                    const float sk = meta_scale(km), sv = fmaxf(meta_scale(vm), kMinScale);
+                    float mk = meta_offset(km), mv = meta_offset(vm), inv;
+                    if constexpr (F32) {
+                        mk = fmaf(7.5f, sk, mk);
+                        mv = fmaf(7.5f, sv, mv);
+                        inv = __frcp_rn(sv);
+                    } else {
+                        inv = rcp(sv);
+                    }
+                    my_key.f[k] = make_float4(sk, mk, lg2(sv), inv);
+                    my_key.off[k] = mv * inv;
+                }
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    uint32_t a[2][4];
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const uint32_t w0 = kw[b][0][ks >> 1] >> ((ks & 1) * 8), w1 = kw[b][1][ks >> 1] >> ((ks & 1) * 8);
-                        a[b][0] = codes<F32, 0>(w0 & 0x000f000fu);
-                        a[b][1] = codes<F32, 0>(w1 & 0x000f000fu);
-                        a[b][2] = codes<F32, 1>(w0 & 0x00f000f0u);
-                        a[b][3] = codes<F32, 1>(w1 & 0x00f000f0u);
-                    }
+                    uint2 q[NT], q2[NT];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        const uint2 q = s_q[(nt * KS + ks) * 32 + lane];
-                        mma(s[0][nt], a[0], q.x, q.y);
-                        mma(s[1][nt], a[1], q.x, q.y);
-                        if constexpr (F32) {
-                            const uint2 q2 = s_q[((NT + nt) * KS + ks) * 32 + lane];
-                            mma(s[0][nt], a[0], q2.x, q2.y);
-                            mma(s[1][nt], a[1], q2.x, q2.y);
+                        q[nt] = s_q[(nt * KS + ks) * 32 + lane];
+                        if constexpr (F32) q2[nt] = s_q[((NT + nt) * KS + ks) * 32 + lane];
+                    }
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const uint32_t w0 = kw[b][0][ks >> 1] >> ((ks & 1) * 8), w1 = kw[b][1][ks >> 1] >> ((ks & 1) * 8);
+                        const uint32_t a[4] = {codes<F32, 0>(w0 & 0x000f000fu), codes<F32, 0>(w1 & 0x000f000fu),
+                                               codes<F32, 1>(w0 & 0x00f000f0u), codes<F32, 1>(w1 & 0x00f000f0u)};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma(s[b][nt], a, q[nt].x, q[nt].y);
+                            if constexpr (F32) mma(s[b][nt], a, q2[nt].x, q2[nt].y);
                         }
                     }
                 }
-                uint32_t km[2][2], vmeta[2][2];
+                __syncwarp();     // the keys' factors are there
+                uint32_t pb[NB][NT][2], pb2[NB][NT][2];
+                // whole: every row of the tile sees all keys of the step
+                auto weights = [&](auto whole_) {
+                    constexpr bool WHOLE = decltype(whole_)::value;
+                    float inv[NB][2];
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                    for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        km[b][e] = st.meta[b][0][8 * e + g];
-                        vmeta[b][e] = st.meta[b][1][8 * e + g];
-                    }
-                uint32_t pb[2][NT][2], pb2[2][NT][2];
-            // whole: every row of the tile sees all 32 keys
-            auto weights = [&](auto whole_) {
-                constexpr bool WHOLE = decltype(whole_)::value;
-                float inv[2][2], offv[2][2];
-                bool grow = false;
+                        for (int e = 0; e < 2; ++e) {      // keys g and g + 8
+                            const float4 f = my_key.f[16 * b + 8 * e + g];
+                            inv[b][e] = f.w;
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {      // keys g and g + 8
-                        const float sk = meta_scale(km[b][e]), sv = fmaxf(meta_scale(vmeta[b][e]), kMinScale);
-                        float mk = meta_offset(km[b][e]), mv = meta_offset(vmeta[b][e]);
-                        const float lsv = lg2(sv);
-                        if constexpr (F32) {
-                            mk = fmaf(7.5f, sk, mk);
-                            mv = fmaf(7.5f, sv, mv);
-                            inv[b][e] = __frcp_rn(sv);
-                        } else {
-                            inv[b][e] = rcp(sv);
-                        }
-                        offv[b][e] = mv * inv[b][e];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                float &x = s[b][nt][2 * e + h];
-                                x = fmaf(x * cq[nt][h], sk, fmaf(mk, sq[nt][h], lsv));
-                                if constexpr (!WHOLE) {
-                                    const int t = tok + 16 * b + 8 * e + g;
-                                    if (t >= high[nt][h] || t < low[nt][h] || !((valid >> b) & 1)) x = -INFINITY;
+                                for (int h = 0; h < 2; ++h) {
+                                    float &x = s[b][nt][2 * e + h];
+                                    x = fmaf(x * cq[nt][h], f.x, fmaf(f.y, sq[nt][h], f.z));
+                                    if constexpr (!WHOLE) {
+                                        const int t = tok + 16 * b + 8 * e + g;
+                                        if (t >= high[nt][h] || t < low[nt][h] || !((valid >> b) & 1)) x = -INFINITY;
+                                    }
                                 }
-                            }
-                    }
+                        }
+                    bool grow = false;
                 float most[NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        most[nt][h] = fmaxf(fmaxf(s[0][nt][h], s[0][nt][2 + h]), fmaxf(s[1][nt][h], s[1][nt][2 + h]));
+                        most[nt][h] = s[0][nt][h];
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) most[nt][h] = fmaxf(fmaxf(most[nt][h], s[b][nt][h]), s[b][nt][2 + h]);
                         grow = grow || most[nt][h] > top[nt][h] + 8.f;
                     }
                 if (__any_sync(0xffffffffu, grow)) {
@@ -623,11 +650,12 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                         }
                 }
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
+                            const float offv = my_key.off[16 * b + 8 * e + g];
                             const float x0 = s[b][nt][2 * e], x1 = s[b][nt][2 * e + 1];
                             const float w0 = ex2(x0 - top[nt][0]), w1 = ex2(x1 - top[nt][1]);
                             const uint32_t packed = pack_half(w0, w1);
@@ -643,68 +671,69 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                             // a hidden key adds nothing, even when its scale or offset is no number
                             if (WHOLE || !(x0 == -INFINITY)) {
                                 sum[nt][0] = fmaf(w0, inv[b][e], sum[nt][0]);
-                                off[nt][0] = fmaf(w.x, offv[b][e], off[nt][0]);
+                                off[nt][0] = fmaf(w.x, offv, off[nt][0]);
                             }
                             if (WHOLE || !(x1 == -INFINITY)) {
                                 sum[nt][1] = fmaf(w1, inv[b][e], sum[nt][1]);
-                                off[nt][1] = fmaf(w.y, offv[b][e], off[nt][1]);
+                                off[nt][1] = fmaf(w.y, offv, off[nt][1]);
                             }
                         }
             };
                 if (whole) weights(Bool<true>{});
                 else weights(Bool<false>{});
 
-                // lane (g, c) holds the g-th eighth of keys 2c, 2c + 1, 2c + 8, 2c + 9 of each block
-                uint32_t vw[2][4][WV];
+                // ---- O^T += V^T P^T, two blocks at a time: lane (g, c) holds the g-th eighth of keys 2c, 2c + 1, 2c + 8, 2c + 9 of each ----
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int b0 = 0; b0 < NB; b0 += 2) {
+                    uint32_t vw[2][4][WV];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        load_words<WV>(st.v + (16 * b + 2 * c + (e & 1) + 8 * (e >> 1)) * (D / 2) + g * (D / 16), vw[b][e]);
-
-            // ---- O^T += V^T P^T ----
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int w = 0; w < WV; ++w) {
-                uint32_t x[2][4];   // block; (keys 2c, 2c + 1 | keys 2c + 8, 2c + 9) x (first | last four dims of the word)
+                        for (int e = 0; e < 4; ++e)
+                            load_words<WV>(st.v + (16 * (b0 + b) + 2 * c + (e & 1) + 8 * (e >> 1)) * (D / 2) + g * (D / 16), vw[b][e]);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    x[b][0] = __byte_perm(vw[b][0][w], vw[b][1][w], 0x5410);
-                    x[b][1] = __byte_perm(vw[b][0][w], vw[b][1][w], 0x7632);
-                    x[b][2] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x5410);
-                    x[b][3] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x7632);
-                }
+                    for (int w = 0; w < WV; ++w) {
+                        uint32_t x[2][4];   // block; (keys 2c, 2c + 1 | keys 2c + 8, 2c + 9) x (first | last four dims of the word)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float part[NT][4];
-                    if constexpr (F32) {
+                        for (int b = 0; b < 2; ++b) {
+                            x[b][0] = __byte_perm(vw[b][0][w], vw[b][1][w], 0x5410);
+                            x[b][1] = __byte_perm(vw[b][0][w], vw[b][1][w], 0x7632);
+                            x[b][2] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x5410);
+                            x[b][3] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x7632);
+                        }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) part[nt][e] = 0.f;
-                    }
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const uint32_t lo = x[b][i >> 1] >> ((i & 1) * 8), hi = x[b][2 + (i >> 1)] >> ((i & 1) * 8);
-                        const uint32_t a[4] = {codes<F32, 0>(lo & 0x000f000fu), codes<F32, 1>(lo & 0x00f000f0u),
-                                               codes<F32, 0>(hi & 0x000f000fu), codes<F32, 1>(hi & 0x00f000f0u)};
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
+                        for (int i = 0; i < 4; ++i) {
+                            float part[NT][4];
                             if constexpr (F32) {
-                                mma(part[nt], a, pb[b][nt][0], pb[b][nt][1]);
-                                mma(part[nt], a, pb2[b][nt][0], pb2[b][nt][1]);
-                            } else {
-                                mma(o[4 * w + i][nt], a, pb[b][nt][0], pb[b][nt][1]);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) part[nt][e] = 0.f;
+                            }
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                const uint32_t lo = x[b][i >> 1] >> ((i & 1) * 8), hi = x[b][2 + (i >> 1)] >> ((i & 1) * 8);
+                                const uint32_t a[4] = {codes<F32, 0>(lo & 0x000f000fu), codes<F32, 1>(lo & 0x00f000f0u),
+                                                       codes<F32, 0>(hi & 0x000f000fu), codes<F32, 1>(hi & 0x00f000f0u)};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    if constexpr (F32) {
+                                        mma(part[nt], a, pb[b0 + b][nt][0], pb[b0 + b][nt][1]);
+                                        mma(part[nt], a, pb2[b0 + b][nt][0], pb2[b0 + b][nt][1]);
+                                    } else {
+                                        mma(o[4 * w + i][nt], a, pb[b0 + b][nt][0], pb[b0 + b][nt][1]);
+                                    }
+                                }
+                            }
+                            if constexpr (F32) {   // tensor cores cut what they add: long sums are kept outside of them
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) o[4 * w + i][nt][e] += part[nt][e];
                             }
                         }
                     }
-                    if constexpr (F32) {   // tensor cores cut what they add: long sums are kept outside of them
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[4 * w + i][nt][e] += part[nt][e];
-                    }
                 }
-            }
             }
             __syncwarp();     // the next fetch fills what was read here
             drain = drain == ring + kStages - 1 ? ring : drain + 1;
@@ -789,7 +818,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         }
         if (!complete) {
             // the last of the CTAs that share this item adds up what they left, in the order of the keys
-            const int c0 = (int)(((item_begin + 1) * ctas - 1) / total), c1 = (int)((item_end * ctas - 1) / total);
+            const int c0 = (int)owner_of(item_begin, ctas, total), c1 = (int)owner_of(item_end - 1, ctas, total);
             __threadfence();
             __syncthreads();
             if (tid == 0) {
@@ -800,7 +829,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
             __syncthreads();
             if (s_last) {
                 // the item opens the share of every CTA but the first, and of that one when the share begins with it
-                const int first_slot = total * c0 / ctas == item_begin ? 0 : 1;
+                const int first_slot = mul_div(total, c0, ctas) == item_begin ? 0 : 1;
 #pragma unroll 1
                 for (int nt = 0; nt < NT; ++nt) {
                     const int row = nt * 8 + my_row, abs_row = row0 + row;
@@ -848,11 +877,12 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
 // One compiled variant: its kernel, shared memory and tile height.
 struct Variant {
     const void *kernel;
-    int smem, rows, slot;
+    int smem, rows, slot, unit;
 };
 
 template <int D, int NT, bool F32>
-Variant variant() { return {reinterpret_cast<const void *>(&kv_attend_kernel<D, NT, F32>), attend_smem<D, NT, F32>(), 8 * NT, slot_floats<D, NT>()}; }
+Variant variant() { return {reinterpret_cast<const void *>(&kv_attend_kernel<D, NT, F32>), attend_smem<D, NT, F32>(), 8 * NT, slot_floats<D, NT>(),
+            unit_keys<D, NT>()}; }
 
 // Rows of queries that share a key head decide the tile: as few columns of 8 as hold them, so that no product is wasted on
 // empty ones, up to what the registers of a thread hold (head_dim / 16 x 4 accumulators per 8 rows); more rows than the
@@ -983,7 +1013,7 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     const int nt = tile_columns(c.head_dim, rows);
     const Variant v = f32 ? pick<true>(c.head_dim, nt) : pick<false>(c.head_dim, nt);
     long long grid = kv->attend_ctas[f32 ? 1 : 0][nt >> 1];
-    const long long units = (most_keys + kUnit - 1) / kUnit;
+    const long long units = (most_keys + v.unit - 1) / v.unit;
     const double most = (double)a->batch_max * c.kv_heads * (double)((rows + v.rows - 1) / v.rows) * (double)(units < 1 ? 1 : units);
     if (most < (double)grid) grid = (long long)most;
     void *args[] = {&p};
