@@ -327,22 +327,35 @@ __device__ __forceinline__ float bf16_down(float x) {
     return __uint_as_float(x < 0.f && bits != cut ? cut + 0x10000u : cut);
 }
 
+// Code of a value: round(a / scale), ties to even, as the correctly rounded quotient decides it, for 0 <= a / scale <= 15.
+// The product with the reciprocal is off by less than 15 x 2^-22, so the division itself is only needed where the product lies
+// that close to the middle between two codes (about one bf16 value in 300).  Adding 1.5 x 2^23 rounds to a whole number, which
+// then sits in the low bits.
+constexpr float kRound = 12582912.f;
+constexpr uint32_t kRoundBits = 0x4b400000u;
+
+__device__ __forceinline__ float rounded_code(float a, float scale, float inv) {
+    const float t = __fmul_rn(a, inv);
+    float r = __fadd_rn(t, kRound);
+    if (fabsf(__fsub_rn(t, __fsub_rn(r, kRound))) > 0.49999f) r = __fadd_rn(__fdiv_rn(a, scale), kRound);
+    return r;
+}
+
 // One vector held by LANES neighbouring lanes, 16 values each (lanes past D / 16 hold none).
 template <int D, int LANES, bool BF16>
 __device__ __forceinline__ void pack_vector(float (&x)[16], bool active, bool write, unsigned char *codes, uint32_t *meta,
                                             void *stored, long long stored_at) {
-    float lo = FLT_MAX, hi = -FLT_MAX;
-    bool finite = true;
+    float lo = FLT_MAX, hi = -FLT_MAX, none = 0.f;
     if (active) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             lo = fminf(lo, x[i]);
             hi = fmaxf(hi, x[i]);
-            finite = finite && fabsf(x[i]) <= FLT_MAX;
+            none = fmaf(x[i], 0.f, none);      // NaN as soon as a value is one or is infinite
         }
     }
     const int lane = (threadIdx.x & 31) & (LANES - 1);
-    if (!finite) lo = -INFINITY;      // travels through the minimum below, and -inf marks the vector
+    if (none != 0.f) lo = -INFINITY;           // travels through the minimum below, and -inf marks the vector
 #pragma unroll
     for (int d = 1; d < LANES; d <<= 1) {
         lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
@@ -353,12 +366,12 @@ __device__ __forceinline__ void pack_vector(float (&x)[16], bool active, bool wr
     const bool good = lo >= -FLT_MAX && offset >= -FLT_MAX && scale <= FLT_MAX;
     uint32_t packed[2] = {0u, 0u};
     if (good) {
+        const float inv = __frcp_rn(scale);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            // a true division: a value half-way between two codes is then decided as in exact arithmetic
-            const float c = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], offset), scale)), 0.f), 15.f);
-            packed[i >> 3] |= (uint32_t)(int)c << (4 * (i & 7));
-            x[i] = fmaf(c, scale, offset);
+            const float r = rounded_code(__fsub_rn(x[i], offset), scale, inv);
+            packed[i >> 3] += (__float_as_uint(r) - kRoundBits) << (4 * (i & 7));
+            x[i] = fmaf(__fsub_rn(r, kRound), scale, offset);
         }
     } else {
         offset = __uint_as_float(0x7fc00000u);

@@ -37,24 +37,42 @@ struct NormParams {
     float eps, inv_dim;
 };
 
+// 8 values as they are in memory, and as fp32
 template <bool BF16>
-__device__ __forceinline__ void load8(const void *base, long long elem, float *x) {
+struct Raw8 {
+    uint4 w[BF16 ? 1 : 2];
+};
+
+template <bool BF16>
+__device__ __forceinline__ Raw8<BF16> fetch8(const void *base, long long elem) {
+    Raw8<BF16> r;
+    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + elem * (BF16 ? 2 : 4));
+    r.w[0] = p[0];
+    if constexpr (!BF16) r.w[1] = p[1];
+    return r;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void widen8(const Raw8<BF16> &r, float *x) {
     if constexpr (BF16) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + elem * 2);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+        const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] = __uint_as_float(w[i] << 16);
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     } else {
-        const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + elem);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float4 a = p[i];
-            x[4 * i] = a.x; x[4 * i + 1] = a.y; x[4 * i + 2] = a.z; x[4 * i + 3] = a.w;
+            x[4 * i] = __uint_as_float(r.w[i].x); x[4 * i + 1] = __uint_as_float(r.w[i].y);
+            x[4 * i + 2] = __uint_as_float(r.w[i].z); x[4 * i + 3] = __uint_as_float(r.w[i].w);
         }
     }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *base, long long elem, float *x) {
+    widen8<BF16>(fetch8<BF16>(base, elem), x);
 }
 
 template <bool BF16>
@@ -141,47 +159,63 @@ __device__ __forceinline__ long long actual_tokens(const NormParams &p) {
     return t < 0 ? 0 : t > p.tokens ? p.tokens : t;
 }
 
-template <int LANES, bool BF16>
+// A group takes R heads of one token, of the queries or of the keys: their loads are all on the way at once, and the angles
+// and the weight are loaded once for them.  R = 4 keeps 64 bytes per thread in flight and reads the table a quarter as
+// often: 16,384 tokens of 32 + 8 heads of 128 took 103 us with one head per group.  Small calls take R = 1, which has the
+// shorter chain (launch_norm).
+template <int LANES, bool BF16, int R>
 __global__ void __launch_bounds__(kNormThreads) head_norm_rope_kernel(NormParams p) {
     const int lane = threadIdx.x & (LANES - 1);
-    const unsigned heads = p.q.heads + p.k.heads;
-    const unsigned row = blockIdx.x * (unsigned)(kNormThreads / LANES) + threadIdx.x / LANES;
-    const unsigned token = row / heads;
-    const bool real = (long long)token < actual_tokens(p);
+    const unsigned q_parts = (p.q.heads + R - 1) / R, parts = q_parts + (p.k.heads + R - 1) / R;
+    const unsigned item = blockIdx.x * (unsigned)(kNormThreads / LANES) + threadIdx.x / LANES;
+    const unsigned token = item / parts, part = item - token * parts;
     const LanePlace l = lane_place(p, lane);
-    const bool active = real && l.there;
-    int head = (int)(row - token * heads);
-    const bool is_k = head >= p.q.heads;
+    const bool active = (long long)token < actual_tokens(p) && l.there;
+    const bool is_k = part >= q_parts;
     const NormSide &side = is_k ? p.k : p.q;
-    if (is_k) head -= p.q.heads;
-    float v[16], c[8], s[8];
-    float sum = 0.f;
+    const int head0 = (int)(is_k ? part - q_parts : part) * R, heads = min(side.heads - head0, R);
+    Raw8<BF16> raw[R][2];
+    float c[8], s[8], w[16];
     const bool turned = active && l.turned;
     if (active) {
-        const long long at = (long long)token * side.x_ts + (long long)head * side.x_hs;
-        load8<BF16>(side.x, at + l.a, v);
-        load8<BF16>(side.x, at + l.b, v + 8);
+        const long long at = (long long)token * side.x_ts + (long long)head0 * side.x_hs;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < heads) {
+                raw[i][0] = fetch8<BF16>(side.x, at + i * side.x_hs + l.a);
+                raw[i][1] = fetch8<BF16>(side.x, at + i * side.x_hs + l.b);
+            }
         if (turned) load_angles(p, l, p.positions[token], c, s);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
+        if (side.weight) {
+            load8<false>(side.weight, l.a, w);
+            load8<false>(side.weight, l.b, w + 8);
+        }
     }
-    sum = group_sum<LANES>(sum);
-    if (!active) return;
-    const float r = 1.f / sqrtf(fmaf(sum, p.inv_dim, p.eps));
-    if (side.weight) {
-        float w[16];
-        load8<false>(side.weight, l.a, w);
-        load8<false>(side.weight, l.b, w + 8);
+    const long long to = (long long)token * side.out_ts + (long long)head0 * side.out_hs;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = v[i] * r * w[i];
-    } else {
+    for (int i = 0; i < R; ++i) {
+        float v[16], sum = 0.f;
+        if (active && i < heads) {
+            widen8<BF16>(raw[i][0], v);
+            widen8<BF16>(raw[i][1], v + 8);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] *= r;
+            for (int e = 0; e < 16; ++e) sum = fmaf(v[e], v[e], sum);
+        }
+        sum = group_sum<LANES>(sum);
+        if (active && i < heads) {
+            const float r = 1.f / sqrtf(fmaf(sum, p.inv_dim, p.eps));
+            if (side.weight) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = v[e] * r * w[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] *= r;
+            }
+            if (turned) turn(v, c, s, p.interleaved, 1.f);
+            store8<BF16>(side.out, to + i * side.out_hs + l.a, v);
+            store8<BF16>(side.out, to + i * side.out_hs + l.b, v + 8);
+        }
     }
-    if (turned) turn(v, c, s, p.interleaved, 1.f);
-    const long long to = (long long)token * side.out_ts + (long long)head * side.out_hs;
-    store8<BF16>(side.out, to + l.a, v);
-    store8<BF16>(side.out, to + l.b, v + 8);
 }
 
 // Gradients of the rows of one operand, dealt out to the groups of the grid in turn; `dw` gathers the lane's 16 columns of the
@@ -201,25 +235,52 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
 #pragma unroll
         for (int i = 0; i < 16; ++i) w[i] = 1.f;
     }
-    for (long long round = 0; round < rounds; ++round) {   // the whole warp stays: the sums below are its shuffles
+    // row of a round, its token and head
+    struct Row {
+        bool active;
+        unsigned token;
+        int head;
+    };
+    const auto row_of = [&](long long round) {
         const long long row = round * groups + (long long)blockIdx.x * (kNormThreads / LANES) + threadIdx.x / LANES;
-        const bool active = row < rows && l.there;
-        const unsigned token = active ? (unsigned)row / (unsigned)side.heads : 0u;
-        const int head = active ? (int)((unsigned)row - token * (unsigned)side.heads) : 0;
-        float x[16], g[16];
+        Row o;
+        o.active = row < rows && l.there;
+        o.token = o.active ? (unsigned)row / (unsigned)side.heads : 0u;
+        o.head = o.active ? (int)((unsigned)row - o.token * (unsigned)side.heads) : 0;
+        return o;
+    };
+    Raw8<BF16> rx[2], rg[2];
+    int pos = 0;
+    const auto fetch = [&](const Row &o) {
+        if (!o.active) return;
+        const long long at = (long long)o.token * side.x_ts + (long long)o.head * side.x_hs;
+        const long long dat = (long long)o.token * side.dy_ts + (long long)o.head * side.dy_hs;
+        rx[0] = fetch8<BF16>(side.x, at + l.a);
+        rx[1] = fetch8<BF16>(side.x, at + l.b);
+        rg[0] = fetch8<BF16>(side.dy, dat + l.a);
+        rg[1] = fetch8<BF16>(side.dy, dat + l.b);
+        if (l.turned) pos = p.positions[o.token];
+    };
+    Row now = row_of(0);
+    fetch(now);
+    for (long long round = 0; round < rounds; ++round) {   // the whole warp stays: the sums below are its shuffles
+        const bool active = now.active;
+        const unsigned token = now.token;
+        const int head = now.head;
+        float x[16], g[16], c[8], s[8];
         float sum = 0.f;
         if (active) {
-            const long long at = (long long)token * side.x_ts + (long long)head * side.x_hs;
-            const long long dat = (long long)token * side.dy_ts + (long long)head * side.dy_hs;
-            load8<BF16>(side.x, at + l.a, x);
-            load8<BF16>(side.x, at + l.b, x + 8);
-            load8<BF16>(side.dy, dat + l.a, g);
-            load8<BF16>(side.dy, dat + l.b, g + 8);
-            if (l.turned) {
-                float c[8], s[8];
-                load_angles(p, l, p.positions[token], c, s);
-                turn(g, c, s, p.interleaved, -1.f);
-            }
+            widen8<BF16>(rx[0], x);
+            widen8<BF16>(rx[1], x + 8);
+            widen8<BF16>(rg[0], g);
+            widen8<BF16>(rg[1], g + 8);
+            if (l.turned) load_angles(p, l, pos, c, s);
+        }
+        // the next row is on its way while this one is worked on
+        now = row_of(round + 1);
+        fetch(now);
+        if (active) {
+            if (l.turned) turn(g, c, s, p.interleaved, -1.f);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
         }
@@ -248,7 +309,7 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
 
 // Each CTA leaves its sums of the weight gradients in `partial`; the groups of the CTA are added in a fixed order.
 template <int LANES, bool BF16>
-__global__ void __launch_bounds__(kNormThreads) head_norm_rope_backward_kernel(NormParams p) {
+__global__ void __launch_bounds__(kNormThreads, 2) head_norm_rope_backward_kernel(NormParams p) {
     constexpr int GROUPS = kNormThreads / LANES;
     __shared__ float s_dw[GROUPS][LANES * 16 + 1];
     const long long tokens = actual_tokens(p);
@@ -301,24 +362,41 @@ bool norm_aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) 
 int lanes_for(int head_dim) { return head_dim <= 16 ? 1 : head_dim <= 32 ? 2 : head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
 
 template <int LANES>
-void launch_norm(const NormParams &p, bool bf16, unsigned grid, bool backward, cudaStream_t stream) {
+void launch_norm(const NormParams &p, bool bf16, bool backward, unsigned grid, int sms, cudaStream_t stream) {
     if (backward) {
         if (bf16) head_norm_rope_backward_kernel<LANES, true><<<grid, kNormThreads, 0, stream>>>(p);
         else head_norm_rope_backward_kernel<LANES, false><<<grid, kNormThreads, 0, stream>>>(p);
+        return;
+    }
+    const int per_cta = kNormThreads / LANES;
+    const auto ctas = [&](int r) {
+        const long long parts = (p.q.heads + r - 1) / r + (p.k.heads + r - 1) / r;
+        return (unsigned)((p.tokens * parts + per_cta - 1) / per_cta);
+    };
+    if (ctas(1) <= (unsigned)sms * 4) {     // all groups are resident at once even with a head each
+        if (bf16) head_norm_rope_kernel<LANES, true, 1><<<ctas(1), kNormThreads, 0, stream>>>(p);
+        else head_norm_rope_kernel<LANES, false, 1><<<ctas(1), kNormThreads, 0, stream>>>(p);
     } else {
-        if (bf16) head_norm_rope_kernel<LANES, true><<<grid, kNormThreads, 0, stream>>>(p);
-        else head_norm_rope_kernel<LANES, false><<<grid, kNormThreads, 0, stream>>>(p);
+        if (bf16) head_norm_rope_kernel<LANES, true, 4><<<ctas(4), kNormThreads, 0, stream>>>(p);
+        else head_norm_rope_kernel<LANES, false, 2><<<ctas(2), kNormThreads, 0, stream>>>(p);
     }
 }
 
-void launch_norm_lanes(int lanes, const NormParams &p, bool bf16, unsigned grid, bool backward, cudaStream_t stream) {
+void launch_norm_lanes(int lanes, const NormParams &p, bool bf16, bool backward, unsigned grid, int sms, cudaStream_t stream) {
     switch (lanes) {
-        case 1: launch_norm<1>(p, bf16, grid, backward, stream); break;
-        case 2: launch_norm<2>(p, bf16, grid, backward, stream); break;
-        case 4: launch_norm<4>(p, bf16, grid, backward, stream); break;
-        case 8: launch_norm<8>(p, bf16, grid, backward, stream); break;
-        default: launch_norm<16>(p, bf16, grid, backward, stream); break;
+        case 1: launch_norm<1>(p, bf16, backward, grid, sms, stream); break;
+        case 2: launch_norm<2>(p, bf16, backward, grid, sms, stream); break;
+        case 4: launch_norm<4>(p, bf16, backward, grid, sms, stream); break;
+        case 8: launch_norm<8>(p, bf16, backward, grid, sms, stream); break;
+        default: launch_norm<16>(p, bf16, backward, grid, sms, stream); break;
     }
+}
+
+fi_status_t current_sms(int *sms, const char *name) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, name);
 }
 
 fi_status_t check_norm_args(const fi_head_norm_rope_t *a, bool backward, const char *name) {
@@ -398,11 +476,10 @@ int64_t fi_head_norm_rope_workspace(int32_t head_dim) {
 fi_status_t fi_head_norm_rope(const fi_head_norm_rope_t *a, void *cuda_stream) {
     fi_status_t st = check_norm_args(a, false, "fi_head_norm_rope");
     if (st != FI_OK || a->tokens == 0) return st;
-    const NormParams p = norm_params(a, false);
-    const int lanes = lanes_for(a->head_dim), per_cta = kNormThreads / lanes;
-    const long long rows = a->tokens * ((long long)a->q_heads + a->k_heads);
-    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, (unsigned)((rows + per_cta - 1) / per_cta), false,
-                      static_cast<cudaStream_t>(cuda_stream));
+    int sms = 0;
+    st = current_sms(&sms, "fi_head_norm_rope");
+    if (st != FI_OK) return st;
+    launch_norm_lanes(lanes_for(a->head_dim), norm_params(a, false), a->dtype == FI_BF16, false, 0, sms, static_cast<cudaStream_t>(cuda_stream));
     count_launch();
     return check_launch("fi_head_norm_rope");
 }
@@ -412,16 +489,15 @@ fi_status_t fi_head_norm_rope_backward(const fi_head_norm_rope_t *a, void *cuda_
     if (st != FI_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const NormParams p = norm_params(a, true);
-    int device = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e != cudaSuccess) return cuda_fail(e, "fi_head_norm_rope_backward");
+    int sms = 0;
+    st = current_sms(&sms, "fi_head_norm_rope_backward");
+    if (st != FI_OK) return st;
     const int lanes = lanes_for(a->head_dim), per_cta = kNormThreads / lanes;
     const long long rows = a->tokens * (long long)(a->q_heads > a->k_heads ? a->q_heads : a->k_heads);
     long long grid = (rows + per_cta - 1) / per_cta;
-    const long long most = sms * 4 < kMaxPartials ? sms * 4 : kMaxPartials;
+    const long long most = sms * 2 < kMaxPartials ? sms * 2 : kMaxPartials;   // what is resident at once
     grid = grid < 1 ? 1 : grid > most ? most : grid;
-    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, (unsigned)grid, true, stream);   // no tokens: the sums are zero
+    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, true, (unsigned)grid, sms, stream);   // no tokens: the sums are zero
     count_launch();
     if (p.partial) {
         norm_weight_sum_kernel<<<(2 * a->head_dim + 31) / 32, 1024, 0, stream>>>(p.partial, (int)grid, a->head_dim, a->dq_weight,
