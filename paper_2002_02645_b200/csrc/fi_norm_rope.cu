@@ -75,6 +75,15 @@ __device__ __forceinline__ void load8(const void *base, long long elem, float *x
     widen8<BF16>(fetch8<BF16>(base, elem), x);
 }
 
+// 8 floats that stay in L1: loaded where they are used, so that they do not hold registers in between
+__device__ __forceinline__ void load8_again(const float *p, float *x) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(x[4 * i]), "=f"(x[4 * i + 1]), "=f"(x[4 * i + 2]), "=f"(x[4 * i + 3])
+                     : "l"(p + 4 * i));
+}
+
 template <bool BF16>
 __device__ __forceinline__ void store8(void *base, long long elem, const float *x) {
     if constexpr (BF16) {
@@ -164,7 +173,7 @@ __device__ __forceinline__ long long actual_tokens(const NormParams &p) {
 // often: 16,384 tokens of 32 + 8 heads of 128 took 103 us with one head per group.  Small calls take R = 1, which has the
 // shorter chain (launch_norm).
 template <int LANES, bool BF16, int R>
-__global__ void __launch_bounds__(kNormThreads) head_norm_rope_kernel(NormParams p) {
+__global__ void __launch_bounds__(kNormThreads, R == 1 ? 4 : 3) head_norm_rope_kernel(NormParams p) {
     const int lane = threadIdx.x & (LANES - 1);
     const unsigned q_parts = (p.q.heads + R - 1) / R, parts = q_parts + (p.k.heads + R - 1) / R;
     const unsigned item = blockIdx.x * (unsigned)(kNormThreads / LANES) + threadIdx.x / LANES;
@@ -175,7 +184,7 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_rope_kernel(NormParams
     const NormSide &side = is_k ? p.k : p.q;
     const int head0 = (int)(is_k ? part - q_parts : part) * R, heads = min(side.heads - head0, R);
     Raw8<BF16> raw[R][2];
-    float c[8], s[8], w[16];
+    float c[8], s[8];
     const bool turned = active && l.turned;
     if (active) {
         const long long at = (long long)token * side.x_ts + (long long)head0 * side.x_hs;
@@ -186,10 +195,6 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_rope_kernel(NormParams
                 raw[i][1] = fetch8<BF16>(side.x, at + i * side.x_hs + l.b);
             }
         if (turned) load_angles(p, l, p.positions[token], c, s);
-        if (side.weight) {
-            load8<false>(side.weight, l.a, w);
-            load8<false>(side.weight, l.b, w + 8);
-        }
     }
     const long long to = (long long)token * side.out_ts + (long long)head0 * side.out_hs;
 #pragma unroll
@@ -203,8 +208,11 @@ __global__ void __launch_bounds__(kNormThreads) head_norm_rope_kernel(NormParams
         }
         sum = group_sum<LANES>(sum);
         if (active && i < heads) {
-            const float r = 1.f / sqrtf(fmaf(sum, p.inv_dim, p.eps));
+            const float r = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
             if (side.weight) {
+                float w[16];
+                load8_again(side.weight + l.a, w);
+                load8_again(side.weight + l.b, w + 8);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) v[e] = v[e] * r * w[e];
             } else {
@@ -227,14 +235,6 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
     const long long rows = tokens * side.heads;
     const long long groups = (long long)gridDim.x * (kNormThreads / LANES);
     const long long rounds = (rows + groups - 1) / groups;
-    float w[16];
-    if (l.there && side.weight) {
-        load8<false>(side.weight, l.a, w);
-        load8<false>(side.weight, l.b, w + 8);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = 1.f;
-    }
     // row of a round, its token and head
     struct Row {
         bool active;
@@ -250,8 +250,8 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
         return o;
     };
     Raw8<BF16> rx[2], rg[2];
-    int pos = 0;
-    const auto fetch = [&](const Row &o) {
+    float nc[8], ns[8];
+    const auto fetch = [&](const Row &o, int pos) {
         if (!o.active) return;
         const long long at = (long long)o.token * side.x_ts + (long long)o.head * side.x_hs;
         const long long dat = (long long)o.token * side.dy_ts + (long long)o.head * side.dy_hs;
@@ -259,10 +259,12 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
         rx[1] = fetch8<BF16>(side.x, at + l.b);
         rg[0] = fetch8<BF16>(side.dy, dat + l.a);
         rg[1] = fetch8<BF16>(side.dy, dat + l.b);
-        if (l.turned) pos = p.positions[o.token];
+        if (l.turned) load_angles(p, l, pos, nc, ns);
     };
-    Row now = row_of(0);
-    fetch(now);
+    const auto position_of = [&](const Row &o) { return o.active && l.turned ? p.positions[o.token] : 0; };
+    Row now = row_of(0), next = row_of(1);
+    fetch(now, position_of(now));
+    int next_pos = position_of(next);
     for (long long round = 0; round < rounds; ++round) {   // the whole warp stays: the sums below are its shuffles
         const bool active = now.active;
         const unsigned token = now.token;
@@ -274,20 +276,34 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
             widen8<BF16>(rx[1], x + 8);
             widen8<BF16>(rg[0], g);
             widen8<BF16>(rg[1], g + 8);
-            if (l.turned) load_angles(p, l, pos, c, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                c[i] = nc[i];
+                s[i] = ns[i];
+            }
         }
-        // the next row is on its way while this one is worked on
-        now = row_of(round + 1);
-        fetch(now);
+        // the next row and its angles are on their way while this one is worked on
+        now = next;
+        fetch(now, next_pos);
+        next = row_of(round + 2);
+        next_pos = position_of(next);
         if (active) {
             if (l.turned) turn(g, c, s, p.interleaved, -1.f);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum = fmaf(x[i], x[i], sum);
         }
         sum = group_sum<LANES>(sum);
-        const float r = 1.f / sqrtf(fmaf(sum, p.inv_dim, p.eps));
+        const float r = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
         float dot = 0.f;
         if (active) {
+            float w[16];
+            if (side.weight) {
+                load8_again(side.weight + l.a, w);
+                load8_again(side.weight + l.b, w + 8);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = 1.f;
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 x[i] *= r;                       // n
