@@ -26,7 +26,7 @@ constexpr int kPageItems = kPageMaxBatch / kPageThreads;   // requests per threa
 // unchecked, and their sum must not wrap.
 __device__ long long block_exclusive(long long v, long long *total) {
     __shared__ long long warp_sum[kPageThreads / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     long long inc = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -35,20 +35,17 @@ __device__ long long block_exclusive(long long v, long long *total) {
     }
     if (lane == 31) warp_sum[warp] = inc;
     __syncthreads();
-    if (warp == 0) {
-        long long w = warp_sum[lane];
+    // every warp adds up the warps' sums for itself: one barrier less than handing them back
+    long long w = lane < warps ? warp_sum[lane] : 0;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long o = __shfl_up_sync(0xffffffffu, w, d);
-            if (lane >= d) w += o;
-        }
-        warp_sum[lane] = w;
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long o = __shfl_up_sync(0xffffffffu, w, d);
+        if (lane >= d) w += o;
     }
-    __syncthreads();
-    const long long before = (warp ? warp_sum[warp - 1] : 0) + inc - v;
-    *total = warp_sum[kPageThreads / 32 - 1];
+    const long long before = warp ? __shfl_sync(0xffffffffu, w, warp - 1) : 0;
+    *total = __shfl_sync(0xffffffffu, w, 31);
     __syncthreads();   // the next call writes warp_sum again
-    return before;
+    return before + inc - v;
 }
 
 __device__ __forceinline__ int clamp_int(long long v) { return v > 2147483647ll ? 2147483647 : (int)v; }
@@ -65,17 +62,44 @@ __device__ __forceinline__ int find_last(const int *first, int n, int x) {
 
 // True in the last CTA of the grid to get here; everything the grid read before is then free to be overwritten.
 __device__ bool last_cta(uint32_t *ticket) {
-    if (gridDim.x == 1) return true;
+    if (gridDim.x == 1) {
+        __syncthreads();
+        return true;
+    }
     __shared__ bool last;
+    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
-        __threadfence();
         last = atomicAdd(ticket, 1u) == gridDim.x - 1;
         if (last) *ticket = 0;
+        __threadfence();
     }
     __syncthreads();
     return last;
 }
+
+// lens_out = lens, unless they are one array: each CTA copies its share before the last one enters the new lengths.  The loads
+// are issued at the start of the kernel and stored (put) when their values are there anyway.
+struct LensCopy {
+    int v[4];
+    int first, threads, rows;
+
+    __device__ __forceinline__ void get(const int32_t *lens, const int32_t *lens_out, int rows_) {
+        threads = gridDim.x * blockDim.x;
+        first = blockIdx.x * blockDim.x + threadIdx.x;
+        rows = lens_out == lens ? 0 : rows_;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + e * (long long)threads < rows) v[e] = lens[first + e * threads];
+    }
+
+    __device__ __forceinline__ void put(const int32_t *lens, int32_t *lens_out) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (first + e * (long long)threads < rows) lens_out[first + e * threads] = v[e];
+        for (long long r = first + 4ll * threads; r < rows; r += threads) lens_out[r] = lens[r];
+    }
+};
 
 __device__ __forceinline__ int actual_count(const int32_t *count_dev, int most) {
     if (!count_dev) return most;
@@ -85,37 +109,49 @@ __device__ __forceinline__ int actual_count(const int32_t *count_dev, int most) 
 
 // The step of the tables.  Every CTA forms both sums (tokens, then wanted pages) over all requests for itself: up to
 // 8,192 lengths from L2 cost less than a second launch, and one CTA is all that a decode step needs.  The tokens are
-// then dealt out, one per thread; a token finds its request in the sums (binary search in shared memory) and a token
-// that opens a new page also writes the table entry.  Bound by the 12 bytes written per token for prompts, and by the
-// chain of loads and block sums (about 3 us) for a decode step.  Lengths and the free count are committed by the last CTA
-// to finish, so they may be updated in place.
+// then dealt out, four neighbours per thread, which mostly share their request (found in the sums by binary search in
+// shared memory) and their page; a token that opens a new page also writes the table entry.  Bound by the 12 bytes
+// written per token for prompts, and by the chain of loads and block sums for a decode step.  Lengths and the free count
+// are committed by the last CTA to finish, so they may be updated in place.
+// ITEMS: most requests per thread (1 keeps the code short: a decode step also waits for its instructions).
+template <int ITEMS>
 __global__ void __launch_bounds__(kPageThreads) pages_extend_kernel(fi_pages_extend_t a, int page_shift, int max_blocks,
-                                                                    uint32_t *ticket) {
+                                                                    bool wide, uint32_t *ticket) {
     extern __shared__ int smem[];
     int *const s_cu = smem;                       // first token of each request
     int *const s_first = s_cu + a.batch_max;      // place of its first page in the free stack, or kRefused
     int *const s_have = s_first + a.batch_max;
     int *const s_row = s_have + a.batch_max;
+    __shared__ int s_taken;
+    if (threadIdx.x == 0) s_taken = 0;
+    const int items = ITEMS == 1 ? 1 : (a.batch_max + blockDim.x - 1) / blockDim.x;
+    const int i0 = threadIdx.x * items;
+    int have[ITEMS], fresh[ITEMS], rows[ITEMS];
+    // rows and lengths are loaded for the largest batch, beside the actual one
+#pragma unroll
+    for (int e = 0; e < ITEMS; ++e) {
+        const int i = i0 + e;
+        rows[e] = -1;
+        if (e < items && i < a.batch_max) {
+            rows[e] = a.row_idx ? a.row_idx[i] : i;
+            fresh[e] = a.new_lens ? a.new_lens[i] : 1;
+        }
+    }
+    LensCopy copy;
+    copy.get(a.lens, a.lens_out, a.rows);
     const int n = actual_count(a.batch_count, a.batch_max);
     const int free_count = min(max(*a.free_count, 0), a.num_pages);
-    const int items = (a.batch_max + kPageThreads - 1) / kPageThreads;
-    const int i0 = threadIdx.x * items;
-    int have[kPageItems], fresh[kPageItems];
     long long sum = 0;
 #pragma unroll
-    for (int e = 0; e < kPageItems; ++e) {
+    for (int e = 0; e < ITEMS; ++e) {
         const int i = i0 + e;
-        have[e] = 0;
-        fresh[e] = 0;
+        const bool ok = rows[e] >= 0 && rows[e] < a.rows;
+        have[e] = ok ? a.lens[rows[e]] : 0;
+        if (!ok || have[e] < 0 || fresh[e] < 0 || i >= n) fresh[e] = 0;
+        if (have[e] < 0) have[e] = 0;
+        if (!ok) rows[e] = -1;
         if (e < items && i < n) {
-            const int row = a.row_idx ? a.row_idx[i] : i;
-            const bool ok = row >= 0 && row < a.rows;
-            if (ok) {
-                have[e] = a.lens[row];
-                fresh[e] = max(a.new_lens ? a.new_lens[i] : 1, 0);
-                if (have[e] < 0) { have[e] = 0; fresh[e] = 0; }
-            }
-            s_row[i] = ok ? row : -1;
+            s_row[i] = rows[e];
             s_have[i] = have[e];
             sum += fresh[e];
         }
@@ -123,10 +159,10 @@ __global__ void __launch_bounds__(kPageThreads) pages_extend_kernel(fi_pages_ext
     long long tokens;
     long long cu = block_exclusive(sum, &tokens);
     long long need_sum = 0;
-    int need[kPageItems];
+    int need[ITEMS];
     const long long page_mask = (1ll << page_shift) - 1;
 #pragma unroll
-    for (int e = 0; e < kPageItems; ++e) {
+    for (int e = 0; e < ITEMS; ++e) {
         const int i = i0 + e;
         need[e] = -1;
         if (e < items && i < n) {
@@ -142,9 +178,9 @@ __global__ void __launch_bounds__(kPageThreads) pages_extend_kernel(fi_pages_ext
     }
     long long pages;
     long long before = block_exclusive(need_sum, &pages);
-    long long taken = 0;
+    int taken = 0;
 #pragma unroll
-    for (int e = 0; e < kPageItems; ++e) {
+    for (int e = 0; e < ITEMS; ++e) {
         const int i = i0 + e;
         if (e < items && i < n) {
             const bool given = need[e] >= 0 && (need[e] == 0 || before + need[e] <= free_count);
@@ -156,52 +192,84 @@ __global__ void __launch_bounds__(kPageThreads) pages_extend_kernel(fi_pages_ext
             fresh[e] = given ? fresh[e] : 0;
         }
     }
-    long long taken_all;
-    block_exclusive(taken, &taken_all);           // (also the barrier before the shared arrays are read)
+    if (taken > 0) atomicAdd(&s_taken, taken);
+    copy.put(a.lens, a.lens_out);
+    __syncthreads();
     if (blockIdx.x == 0) {
-        for (int i = n + threadIdx.x; i <= a.batch_max; i += kPageThreads) {
+        for (int i = n + threadIdx.x; i <= a.batch_max; i += blockDim.x) {
             a.cu_tokens[i] = clamp_int(tokens);
             if (i < a.batch_max) a.granted[i] = 0;
         }
     }
-    const long long step = (long long)gridDim.x * kPageThreads;
-    for (long long t = (long long)blockIdx.x * kPageThreads + threadIdx.x; t < a.max_tokens; t += step) {
-        long long slot = -1;
-        int pos = -1;
-        if (t < tokens) {
+    const long long step = (long long)gridDim.x * blockDim.x * 4;
+    for (long long t0 = ((long long)blockIdx.x * blockDim.x + threadIdx.x) * 4; t0 < a.max_tokens; t0 += step) {
+        long long slot[4] = {-1, -1, -1, -1};
+        int pos[4] = {-1, -1, -1, -1};
+        if (t0 < tokens) {
             // requests without tokens share their first token with the next one: the last of them owns it
-            const int i = find_last(s_cu, n, (int)t);
-            const long long p = (long long)s_have[i] + ((int)t - s_cu[i]);
-            pos = clamp_int(p);
-            const int first = s_first[i];
-            if (first != kRefused) {
-                const int block = (int)(p >> page_shift), row = s_row[i];
-                const int had = (int)((s_have[i] + page_mask) >> page_shift);
-                int32_t *const entry = a.block_table + (long long)row * a.table_ld + block;
-                int page;
-                if (block >= had) {
-                    page = a.free_pages[first - (block - had)];
-                    if ((p & page_mask) == 0) *entry = page;
-                } else {
-                    page = *entry;
+            int i = find_last(s_cu, n, (int)t0);
+            int end = i + 1 < n ? s_cu[i + 1] : clamp_int(tokens);
+            const int first0 = s_first[i], p0 = s_have[i] + ((int)t0 - s_cu[i]), place0 = p0 & (int)page_mask;
+            if (t0 + 4 <= end && first0 != kRefused && place0 + 4 <= page_mask + 1) {
+                // the usual four: one request, one page
+                const int block = p0 >> page_shift, had = (int)((s_have[i] + page_mask) >> page_shift);
+                int32_t *const entry = a.block_table + (long long)s_row[i] * a.table_ld + block;
+                const int page = block >= had ? a.free_pages[first0 - (block - had)] : *entry;
+                if (block >= had && place0 == 0) *entry = page;
+                const long long slot0 = ((long long)page << page_shift) + place0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    pos[e] = p0 + e;
+                    slot[e] = page >= 0 ? slot0 + e : -1;
                 }
-                if (page >= 0) slot = ((long long)page << page_shift) + (p & page_mask);
+            } else {
+#pragma unroll 1
+                for (int e = 0; e < 4 && t0 + e < tokens; ++e) {
+                    const int t = (int)t0 + e;
+                    while (t >= end) {
+                        ++i;
+                        end = i + 1 < n ? s_cu[i + 1] : clamp_int(tokens);
+                    }
+                    const long long p = (long long)s_have[i] + (t - s_cu[i]);
+                    long long sl = -1;
+                    const int first = s_first[i];
+                    if (first != kRefused) {
+                        const int block = (int)(p >> page_shift), had = (int)((s_have[i] + page_mask) >> page_shift);
+                        int32_t *const entry = a.block_table + (long long)s_row[i] * a.table_ld + block;
+                        const int page = block >= had ? a.free_pages[first - (block - had)] : *entry;
+                        if (block >= had && (p & page_mask) == 0) *entry = page;
+                        if (page >= 0) sl = ((long long)page << page_shift) + (p & page_mask);
+                    }
+                    const int ps = clamp_int(p);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (x == e) {
+                            slot[x] = sl;
+                            pos[x] = ps;
+                        }
+                }
             }
         }
-        a.slot_map[t] = slot;
-        a.positions[t] = pos;
+        if (wide && t0 + 4 <= a.max_tokens) {
+            reinterpret_cast<longlong2 *>(a.slot_map + t0)[0] = make_longlong2(slot[0], slot[1]);
+            reinterpret_cast<longlong2 *>(a.slot_map + t0)[1] = make_longlong2(slot[2], slot[3]);
+            *reinterpret_cast<int4 *>(a.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (t0 + e < a.max_tokens) {
+                    a.slot_map[t0 + e] = slot[e];
+                    a.positions[t0 + e] = pos[e];
+                }
+        }
     }
     if (!last_cta(ticket)) return;
-    if (a.lens_out != a.lens) {
-        for (int r = threadIdx.x; r < a.rows; r += kPageThreads) a.lens_out[r] = a.lens[r];
-        __syncthreads();
-    }
 #pragma unroll
-    for (int e = 0; e < kPageItems; ++e) {
+    for (int e = 0; e < ITEMS; ++e) {
         const int i = i0 + e;
         if (e < items && i < n && s_row[i] >= 0 && fresh[e] > 0) a.lens_out[s_row[i]] = have[e] + fresh[e];
     }
-    if (threadIdx.x == 0) *a.free_count_out = free_count - (int)taken_all;
+    if (threadIdx.x == 0) *a.free_count_out = free_count - s_taken;
 }
 
 struct ReleaseParams {
@@ -212,18 +280,21 @@ struct ReleaseParams {
 };
 
 // The way back: the pages of the listed rows are copied behind the free stack, in list order.
+template <int ITEMS>
 __global__ void __launch_bounds__(kPageThreads) pages_release_kernel(ReleaseParams a, uint32_t *ticket) {
     extern __shared__ int smem[];
     int *const s_cu = smem;
     int *const s_row = s_cu + a.batch_max;
+    LensCopy copy;
+    copy.get(a.lens, a.lens_out, a.rows);
     const int n = actual_count(a.batch_count, a.batch_max);
     const int free_count = min(max(*a.free_count, 0), a.num_pages);
-    const int items = (a.batch_max + kPageThreads - 1) / kPageThreads;
+    const int items = ITEMS == 1 ? 1 : (a.batch_max + blockDim.x - 1) / blockDim.x;
     const int i0 = threadIdx.x * items;
-    int used[kPageItems];
+    int used[ITEMS];
     long long sum = 0;
 #pragma unroll
-    for (int e = 0; e < kPageItems; ++e) {
+    for (int e = 0; e < ITEMS; ++e) {
         const int i = i0 + e;
         used[e] = 0;
         if (e < items && i < n) {
@@ -240,7 +311,7 @@ __global__ void __launch_bounds__(kPageThreads) pages_release_kernel(ReleasePara
     long long pages;
     long long cu = block_exclusive(sum, &pages);
 #pragma unroll
-    for (int e = 0; e < kPageItems; ++e) {
+    for (int e = 0; e < ITEMS; ++e) {
         const int i = i0 + e;
         if (e < items && i < n) {
             s_cu[i] = clamp_int(cu);
@@ -248,18 +319,15 @@ __global__ void __launch_bounds__(kPageThreads) pages_release_kernel(ReleasePara
         }
     }
     __syncthreads();
+    copy.put(a.lens, a.lens_out);
     if (pages > a.num_pages - free_count) pages = a.num_pages - free_count;   // a row listed twice: nothing is written past the stack
-    const long long step = (long long)gridDim.x * kPageThreads;
-    for (long long p = (long long)blockIdx.x * kPageThreads + threadIdx.x; p < pages; p += step) {
+    const long long step = (long long)gridDim.x * blockDim.x;
+    for (long long p = (long long)blockIdx.x * blockDim.x + threadIdx.x; p < pages; p += step) {
         const int i = find_last(s_cu, n, (int)p);
         a.free_pages[free_count + p] = a.block_table[(long long)s_row[i] * a.table_ld + ((int)p - s_cu[i])];
     }
     if (!last_cta(ticket)) return;
-    if (a.lens_out != a.lens) {
-        for (int r = threadIdx.x; r < a.rows; r += kPageThreads) a.lens_out[r] = a.lens[r];
-        __syncthreads();
-    }
-    for (int i = threadIdx.x; i < n; i += kPageThreads)
+    for (int i = threadIdx.x; i < n; i += blockDim.x)
         if (s_row[i] >= 0) a.lens_out[s_row[i]] = 0;
     if (threadIdx.x == 0) *a.free_count_out = free_count + (int)pages;
 }
@@ -469,8 +537,8 @@ fi_status_t fi_pages_create(const fi_pages_config_t *cfg, fi_pages_t **out) {
     DeviceGuard guard(cfg->device);
     cudaError_t e = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 16);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_release_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 8);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_extend_kernel<kPageItems>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 16);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_release_kernel<kPageItems>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 8);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&p->ticket), sizeof(uint32_t));
     if (e == cudaSuccess) e = cudaMemset(p->ticket, 0, sizeof(uint32_t));
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
@@ -504,8 +572,15 @@ fi_status_t fi_pages_extend(fi_pages_t *p, const fi_pages_extend_t *s, void *cud
     if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_extend");
     int grid = s->max_tokens / 4096;   // below that the sums cost more than the tokens
     grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
-    pages_extend_kernel<<<grid, kPageThreads, (size_t)s->batch_max * 16, static_cast<cudaStream_t>(cuda_stream)>>>(
-        *s, log2_of(p->cfg.page_size), p->cfg.max_blocks, p->ticket);
+    // a decode step of up to 256 requests: eight warps form the sums faster than 32
+    const int threads = s->batch_max <= 256 && s->max_tokens <= 1024 && s->rows <= 1024 ? 256 : kPageThreads;
+    const bool wide = aligned16(s->slot_map) && aligned16(s->positions);
+    if (s->batch_max <= threads)
+        pages_extend_kernel<1><<<grid, threads, (size_t)s->batch_max * 16, static_cast<cudaStream_t>(cuda_stream)>>>(
+            *s, log2_of(p->cfg.page_size), p->cfg.max_blocks, wide, p->ticket);
+    else
+        pages_extend_kernel<kPageItems><<<grid, threads, (size_t)s->batch_max * 16, static_cast<cudaStream_t>(cuda_stream)>>>(
+            *s, log2_of(p->cfg.page_size), p->cfg.max_blocks, wide, p->ticket);
     count_launch();
     return check_launch("fi_pages_extend");
 }
@@ -529,7 +604,11 @@ fi_status_t fi_pages_release(fi_pages_t *p, const int32_t *row_idx, int32_t batc
                        batch_max, rows, num_pages, p->cfg.max_blocks, log2_of(p->cfg.page_size)};
     long long grid = (long long)batch_max * p->cfg.max_blocks / 16384;   // an upper bound of the pages, rarely met
     grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
-    pages_release_kernel<<<(int)grid, kPageThreads, (size_t)batch_max * 8, static_cast<cudaStream_t>(cuda_stream)>>>(a, p->ticket);
+    const int threads = batch_max <= 256 && rows <= 1024 ? 256 : kPageThreads;
+    if (batch_max <= threads)
+        pages_release_kernel<1><<<(int)grid, threads, (size_t)batch_max * 8, static_cast<cudaStream_t>(cuda_stream)>>>(a, p->ticket);
+    else
+        pages_release_kernel<kPageItems><<<(int)grid, threads, (size_t)batch_max * 8, static_cast<cudaStream_t>(cuda_stream)>>>(a, p->ticket);
     count_launch();
     return check_launch("fi_pages_release");
 }

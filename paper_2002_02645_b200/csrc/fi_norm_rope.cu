@@ -31,7 +31,8 @@ struct NormParams {
     const float *rope;
     const int32_t *positions;
     const int32_t *tokens_dev;
-    float *partial;        // backward: [CTAs][2][head_dim]
+    float *partial;        // backward: [CTAs][head_dim]
+    int q_ctas;            // backward: CTAs that work on the queries, the others on the keys
     long long tokens;
     int head_dim, rot, max_pos, interleaved;
     float eps, inv_dim;
@@ -229,11 +230,12 @@ __global__ void __launch_bounds__(kNormThreads, R == 1 ? 4 : 3) head_norm_rope_k
 // Gradients of the rows of one operand, dealt out to the groups of the grid in turn; `dw` gathers the lane's 16 columns of the
 // weight gradient over all its rows.
 template <int LANES, bool BF16>
-__device__ __forceinline__ void backward_rows(const NormParams &p, const NormSide &side, long long tokens, float (&dw)[16]) {
+__device__ __forceinline__ void backward_rows(const NormParams &p, const NormSide &side, long long tokens, unsigned cta, unsigned ctas,
+                                              float (&dw)[16]) {
     const int lane = threadIdx.x & (LANES - 1);
     const LanePlace l = lane_place(p, lane);
     const long long rows = tokens * side.heads;
-    const long long groups = (long long)gridDim.x * (kNormThreads / LANES);
+    const long long groups = (long long)ctas * (kNormThreads / LANES);
     const long long rounds = (rows + groups - 1) / groups;
     // row of a round, its token and head
     struct Row {
@@ -242,7 +244,7 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
         int head;
     };
     const auto row_of = [&](long long round) {
-        const long long row = round * groups + (long long)blockIdx.x * (kNormThreads / LANES) + threadIdx.x / LANES;
+        const long long row = round * groups + (long long)cta * (kNormThreads / LANES) + threadIdx.x / LANES;
         Row o;
         o.active = row < rows && l.there;
         o.token = o.active ? (unsigned)row / (unsigned)side.heads : 0u;
@@ -330,46 +332,46 @@ __global__ void __launch_bounds__(kNormThreads, 2) head_norm_rope_backward_kerne
     __shared__ float s_dw[GROUPS][LANES * 16 + 1];
     const long long tokens = actual_tokens(p);
     const LanePlace l = lane_place(p, threadIdx.x & (LANES - 1));
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-        const NormSide &side = which ? p.k : p.q;
-        float dw[16] = {};
-        if (side.heads > 0) backward_rows<LANES, BF16>(p, side, tokens, dw);
-        if (!p.partial) continue;
-        __syncthreads();
-        if (l.there) {
+    const bool is_k = blockIdx.x >= (unsigned)p.q_ctas;
+    float dw[16] = {};
+    if (is_k) backward_rows<LANES, BF16>(p, p.k, tokens, blockIdx.x - p.q_ctas, gridDim.x - p.q_ctas, dw);
+    else backward_rows<LANES, BF16>(p, p.q, tokens, blockIdx.x, p.q_ctas, dw);
+    if (!p.partial) return;
+    if (l.there) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                s_dw[threadIdx.x / LANES][l.a + i] = dw[i];
-                s_dw[threadIdx.x / LANES][l.b + i] = dw[8 + i];
-            }
+        for (int i = 0; i < 8; ++i) {
+            s_dw[threadIdx.x / LANES][l.a + i] = dw[i];
+            s_dw[threadIdx.x / LANES][l.b + i] = dw[8 + i];
         }
-        __syncthreads();
-        for (int d = threadIdx.x; d < p.head_dim; d += kNormThreads) {
-            float sum = 0.f;
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < p.head_dim; d += kNormThreads) {
+        float sum = 0.f;
 #pragma unroll 8
-            for (int g = 0; g < GROUPS; ++g) sum += s_dw[g][d];
-            p.partial[((long long)blockIdx.x * 2 + which) * p.head_dim + d] = sum;
-        }
+        for (int g = 0; g < GROUPS; ++g) sum += s_dw[g][d];
+        p.partial[(long long)blockIdx.x * p.head_dim + d] = sum;
     }
 }
 
-// dw[which][d] = sum of the CTAs' partial sums, 32 columns per CTA, always in the same order
-__global__ void __launch_bounds__(1024) norm_weight_sum_kernel(const float *partial, int ctas, int head_dim, float *dq_weight,
+// Weight gradients from the CTAs' sums, 32 columns per CTA (of the queries' gradient, then of the keys'), always in the same order.
+__global__ void __launch_bounds__(1024) norm_weight_sum_kernel(const float *partial, int q_ctas, int ctas, int head_dim, float *dq_weight,
                                                                float *dk_weight) {
     __shared__ float s[32][33];
-    const int col = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    const int half = gridDim.x / 2;
+    const bool is_k = (int)blockIdx.x >= half;
+    const int col = ((int)blockIdx.x - (is_k ? half : 0)) * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+    float *const out = is_k ? dk_weight : dq_weight;
+    if (!out) return;
     float sum = 0.f;
-    if (col < 2 * head_dim)
-        for (int b = part; b < ctas; b += 32) sum += partial[(long long)b * 2 * head_dim + col];
+    if (col < head_dim)
+        for (int b = (is_k ? q_ctas : 0) + part; b < (is_k ? ctas : q_ctas); b += 32) sum += partial[(long long)b * head_dim + col];
     s[part][threadIdx.x & 31] = sum;
     __syncthreads();
-    if (part == 0 && col < 2 * head_dim) {
+    if (part == 0 && col < head_dim) {
         float total = 0.f;
 #pragma unroll
         for (int i = 0; i < 32; ++i) total += s[i][threadIdx.x];
-        float *const out = col < head_dim ? dq_weight : dk_weight;
-        if (out) out[col < head_dim ? col : col - head_dim] = total;
+        out[col] = total;
     }
 }
 
@@ -486,7 +488,7 @@ using namespace fi;
 extern "C" {
 
 int64_t fi_head_norm_rope_workspace(int32_t head_dim) {
-    return head_dim < 16 || head_dim > 256 ? 0 : (int64_t)kMaxPartials * 2 * head_dim * sizeof(float);
+    return head_dim < 16 || head_dim > 256 ? 0 : (int64_t)kMaxPartials * head_dim * sizeof(float);
 }
 
 fi_status_t fi_head_norm_rope(const fi_head_norm_rope_t *a, void *cuda_stream) {
@@ -504,20 +506,29 @@ fi_status_t fi_head_norm_rope_backward(const fi_head_norm_rope_t *a, void *cuda_
     fi_status_t st = check_norm_args(a, true, "fi_head_norm_rope_backward");
     if (st != FI_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const NormParams p = norm_params(a, true);
+    NormParams p = norm_params(a, true);
     int sms = 0;
     st = current_sms(&sms, "fi_head_norm_rope_backward");
     if (st != FI_OK) return st;
+    // as many CTAs as are resident at once, dealt out to queries and keys by their numbers of rows
     const int lanes = lanes_for(a->head_dim), per_cta = kNormThreads / lanes;
-    const long long rows = a->tokens * (long long)(a->q_heads > a->k_heads ? a->q_heads : a->k_heads);
-    long long grid = (rows + per_cta - 1) / per_cta;
-    const long long most = sms * 2 < kMaxPartials ? sms * 2 : kMaxPartials;   // what is resident at once
-    grid = grid < 1 ? 1 : grid > most ? most : grid;
-    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, true, (unsigned)grid, sms, stream);   // no tokens: the sums are zero
+    const long long most = sms * 2 < kMaxPartials ? sms * 2 : kMaxPartials;
+    const long long q_rows = a->tokens * (long long)a->q_heads, k_rows = a->tokens * (long long)a->k_heads;
+    long long q_ctas = (q_rows + per_cta - 1) / per_cta, k_ctas = (k_rows + per_cta - 1) / per_cta;
+    if (q_ctas + k_ctas > most) {
+        k_ctas = k_rows ? (most * k_rows + (q_rows + k_rows) / 2) / (q_rows + k_rows) : 0;
+        if (k_rows && k_ctas < 1) k_ctas = 1;
+        q_ctas = most - k_ctas;
+    }
+    if (q_ctas < 1) q_ctas = 1;                       // no tokens: the sums are zero
+    if (a->k_heads > 0 && k_ctas < 1) k_ctas = 1;
+    const int grid = (int)(q_ctas + k_ctas);
+    p.q_ctas = (int)q_ctas;
+    launch_norm_lanes(lanes, p, a->dtype == FI_BF16, true, (unsigned)grid, sms, stream);
     count_launch();
     if (p.partial) {
-        norm_weight_sum_kernel<<<(2 * a->head_dim + 31) / 32, 1024, 0, stream>>>(p.partial, (int)grid, a->head_dim, a->dq_weight,
-                                                                               a->dk_weight);
+        norm_weight_sum_kernel<<<2 * ((a->head_dim + 31) / 32), 1024, 0, stream>>>(p.partial, p.q_ctas, grid, a->head_dim, a->dq_weight,
+                                                                                 a->k_heads > 0 ? a->dk_weight : nullptr);
         count_launch();
     }
     return check_launch("fi_head_norm_rope_backward");
