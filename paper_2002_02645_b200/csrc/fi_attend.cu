@@ -837,23 +837,40 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                     float m = kNoMax, l = 0.f, b = 0.f, acc[PER];
 #pragma unroll
                     for (int i = 0; i < PER; ++i) acc[i] = 0.f;
-#pragma unroll 8
-                    for (int k = c0; k <= c1; ++k) {
-                        const float *const d = p.partial + (2 * (long long)k + (k == c0 ? first_slot : 0)) * slot_floats<D, NT>() + row * LD;
-                        const float4 st = __ldcg(reinterpret_cast<const float4 *>(d + D));
-                        float4 x[PER / 4];
+                    constexpr int BATCH = D <= 128 ? 8 : 4;      // parts whose loads are on the way together
+#pragma unroll 1
+                    for (int k0 = c0; k0 <= c1; k0 += BATCH) {
+                        float4 st[BATCH], v[BATCH][PER / 4];
 #pragma unroll
-                        for (int i = 0; i < PER / 4; ++i) x[i] = __ldcg(reinterpret_cast<const float4 *>(d + my_dim + 64 * i));
-                        const float m2 = fmaxf(m, st.x), f = ex2(m - m2), f2 = ex2(st.x - m2);
+                        for (int e = 0; e < BATCH; ++e) {
+                            const int k = min(k0 + e, c1);
+                            const float *const d = p.partial + (2 * (long long)k + (k == c0 ? first_slot : 0)) * slot_floats<D, NT>() + row * LD;
+                            st[e] = __ldcg(reinterpret_cast<const float4 *>(d + D));
+#pragma unroll
+                            for (int i = 0; i < PER / 4; ++i) v[e][i] = __ldcg(reinterpret_cast<const float4 *>(d + my_dim + 64 * i));
+                        }
+                        float m2 = m;
+#pragma unroll
+                        for (int e = 0; e < BATCH; ++e)
+                            m2 = fmaxf(m2, st[e].x);
+                        const float f = ex2(m - m2);
                         m = m2;
-                        l = fmaf(l, f, st.y * f2);
-                        b = fmaf(b, f, st.z * f2);
+                        l *= f;
+                        b *= f;
 #pragma unroll
-                        for (int i = 0; i < PER / 4; ++i) {
-                            acc[4 * i] = fmaf(acc[4 * i], f, x[i].x * f2);
-                            acc[4 * i + 1] = fmaf(acc[4 * i + 1], f, x[i].y * f2);
-                            acc[4 * i + 2] = fmaf(acc[4 * i + 2], f, x[i].z * f2);
-                            acc[4 * i + 3] = fmaf(acc[4 * i + 3], f, x[i].w * f2);
+                        for (int i = 0; i < PER; ++i) acc[i] *= f;
+#pragma unroll
+                        for (int e = 0; e < BATCH; ++e) {
+                            const float w = k0 + e <= c1 ? ex2(st[e].x - m) : 0.f;   // (the last part stands in past the end)
+                            l = fmaf(st[e].y, w, l);
+                            b = fmaf(st[e].z, w, b);
+#pragma unroll
+                            for (int i = 0; i < PER / 4; ++i) {
+                                acc[4 * i] = fmaf(v[e][i].x, w, acc[4 * i]);
+                                acc[4 * i + 1] = fmaf(v[e][i].y, w, acc[4 * i + 1]);
+                                acc[4 * i + 2] = fmaf(v[e][i].z, w, acc[4 * i + 2]);
+                                acc[4 * i + 3] = fmaf(v[e][i].w, w, acc[4 * i + 3]);
+                            }
                         }
                     }
                     const int j = abs_row / p.group, qh = head * p.group + abs_row - j * p.group;
