@@ -566,7 +566,7 @@ typedef struct {
 fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *args, void *cuda_stream);
 
 /* Synchronise the device; FI_ERR_INVALID_ARG when a kernel of this handle met a slot or a page outside the pool since the
- * last poll (the word is cleared), FI_OK otherwise. */
+ * last poll (the word is cleared), FI_ERR_TIMEOUT when a bounded wait inside one ran out, FI_OK otherwise. */
 fi_status_t fi_kv_poll_status(fi_kv_t *kv);
 
 /* Number of kernels this library has launched in the calling process (all caches). */

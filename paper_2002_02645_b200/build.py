@@ -10,8 +10,8 @@ CSRC = os.path.join(PKG, "csrc")
 # FICACHE_LIB names another build of the library to load instead of the in-tree one (it is then never rebuilt here)
 LIB = os.environ.get("FICACHE_LIB") or os.path.join(PKG, "libficache.so")
 SOURCES = ["fi_api.cu", "fi_stream.cu", "fi_finalize.cu", "fi_gemm.cu", "fi_noalloc.cu", "fi_kmeans.cu",
-           "fi_kv.cu", "fi_attend.cu", "fi_norm_rope.cu"]
-HEADERS = [os.path.join(CSRC, "fi_internal.cuh"), os.path.join(os.path.dirname(PKG), "include", "fi.h")]
+           "fi_kv.cu", "fi_attend.cu", "fi_attend_prompt.cu", "fi_norm_rope.cu"]
+HEADERS = [os.path.join(CSRC, "fi_internal.cuh"), os.path.join(CSRC, "fi_attend.cuh"), os.path.join(os.path.dirname(PKG), "include", "fi.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 OBJ_DIR = os.path.join(PKG, "_build")

@@ -13,10 +13,7 @@
 // Codes are all positive, so the product part and the offset part are larger than what they add up to.  The offset part
 // therefore takes the weights as they were rounded for the product, and float32 queries, which must not lose what the parts have in
 // common, take the codes less 7.5 (one more instruction per two codes) and offsets moved by 7.5 scales.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "fi_internal.cuh"
+#include "fi_attend.cuh"
 
 namespace fi {
 namespace {
@@ -24,37 +21,6 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kStages = 2;                 // steps of a warp in its ring: the one it works on and the next
-constexpr float kMinScale = 0x1p-40f;      // smallest scale append stores
-constexpr float kNoMax = -1e30f;           // maximum of nothing
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-
-struct AttendParams {
-    const void *q;
-    void *out;
-    float *lse;
-    const int32_t *lens, *block_table, *row_idx, *batch_count, *cu_tokens;
-    const unsigned char *k_codes, *v_codes;
-    const uint32_t *k_meta, *v_meta;
-    float *partial;
-    uint32_t *tickets;
-    int32_t *status;
-    long long q_ts, q_hs, out_ts, out_hs;             // elements
-    long long hs, mhs;                                // pools: strides of heads,
-    uint32_t ps, ts, mps, mts;                        // of pages and of tokens (codes: 16 bytes, meta: pairs)
-    long long table_ld;
-    int rows, max_blocks, batch_max, max_tokens, window;
-    int num_pages, page_shift, kv_heads, group;
-    int min_units;
-    float scale_log2;                                 // scale * log2(e)
-};
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 __device__ __forceinline__ float lg2(float x) {
     float y;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -130,8 +96,6 @@ __device__ __forceinline__ void load_words(const unsigned char *p, uint32_t *w) 
     }
 }
 
-__device__ __forceinline__ uint32_t smem_at(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
 template <int BYTES>
 __device__ __forceinline__ void async_copy(uint32_t dst, const void *src) {
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -144,9 +108,6 @@ template <int N>
 __device__ __forceinline__ void async_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-
-__device__ __forceinline__ float meta_scale(uint32_t m) { return __uint_as_float(m << 16); }
-__device__ __forceinline__ float meta_offset(uint32_t m) { return __uint_as_float(m & 0xffff0000u); }
 
 // One request as the kernel sees it.
 struct Request {
@@ -940,6 +901,8 @@ fi_status_t prepare_attend(fi_kv *kv) {
         }
     most_ctas = (most_ctas + 3) / 4 * 4;   // the partial results behind the tickets stay 16-byte aligned
     kv->tickets = most_ctas;
+    const fi_status_t st = prepare_attend_prompt(kv);
+    if (st != FI_OK) return st;
     cudaError_t e = cudaMalloc(reinterpret_cast<void **>(&kv->scratch), floats * 4 + (size_t)most_ctas * 4);
     if (e == cudaSuccess) e = cudaMemset(kv->scratch, 0, (size_t)most_ctas * 4);
     return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_kv_create: attention scratch");
@@ -1027,6 +990,7 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     const bool f32 = a->dtype == FI_F32;
     const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;
     const long long rows = per_request * p.group;
+    if (prompt_kernel_serves(kv, p, a->dtype, rows)) return launch_attend_prompt(kv, p, rows, static_cast<cudaStream_t>(cuda_stream));
     const int nt = tile_columns(c.head_dim, rows);
     const Variant v = f32 ? pick<true>(c.head_dim, nt) : pick<false>(c.head_dim, nt);
     long long grid = kv->attend_ctas[f32 ? 1 : 0][nt >> 1];

@@ -1,0 +1,613 @@
+// Attention over the 4-bit store for many queries per request (prompts): tensor-bound, so it runs on tcgen05.
+//
+// A CTA takes a tile of 128 query rows of one request and key head (row = query x heads of the group) and walks the keys in
+// tiles of 128.  Four warps unpack a tile of keys and values to halves in shared memory, one thread issues the products
+//   S = Q K^T  (128 x 128, fp32 in TMEM, two buffers)      O += P V  (128 x head_dim, fp32 in TMEM)
+// and four warps, a thread per row, turn S into the weights P.  The three meet at mbarriers: keys and values are unpacked
+// up to two tiles ahead, S of the next tile is multiplied while the weights of this one are formed.
+//
+// Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
+// rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
+// so no size of keys runs over; the power goes into the factor of the scores.  Values likewise, and their power F into the
+// exponent: P = 2^(x + F - M) with M >= max(x + F) - 8, and the sum takes P 2^-F.  A key whose scale or offset (or whose value's) is no
+// number becomes NaN in K and zero in V: the rows that see it get NaN, the others lose nothing.
+#include "fi_attend.cuh"
+
+namespace fi {
+namespace {
+
+constexpr int kTile = 128;                 // query rows and keys of a tile
+constexpr int kSoftmaxWarps = 4;           // warp w owns TMEM lanes 32 w ..
+constexpr int kUnpackWarps = 4;
+constexpr int kPromptThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
+constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
+constexpr int kTmemCols = 512;             // S, S, O
+
+struct PromptCtl {
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_free[2], p_full, pv_done, q_full;
+    float k_power[2], v_power[2];          // 2^E of a tile's keys; F of its values
+    uint32_t hidden[2][kUnpackWarps];      // keys of a tile whose page is not in the pool, a bit each
+    uint32_t red[2][2][kUnpackWarps];      // largest key and value of a tile, by warp
+    uint32_t tmem;
+    volatile int gave_up;
+};
+
+template <int D>
+struct PromptSmem {
+    static constexpr int kQ = kTile * D * 2, kK = kTile * D * 2, kV = kTile * D * 2, kP = kTile * kTile * 2;
+    static constexpr int q = 0, k = kQ, v = k + 2 * kK, p = v + 2 * kV, ctl = p + kP;
+    static constexpr int bytes = 1024 /* alignment */ + ctl + (int)sizeof(PromptCtl);
+};
+
+__device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(bar)), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void bar_arrive(uint64_t *bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(bar)) : "memory");
+}
+
+__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(smem_at(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
+// Bounded wait.  When it gives up, every later wait of the CTA does so at once: the kernel runs to its end with whatever is
+// in its buffers, and the status word says that the results are not valid.
+__device__ __forceinline__ void bar_wait(uint64_t *bar, uint32_t parity, PromptCtl *ctl, int32_t *status) {
+    if (bar_try(bar, parity)) return;
+    const long long t0 = clock64();
+    for (uint32_t spins = 1;; ++spins) {
+        if (bar_try(bar, parity)) return;
+        if ((spins & 255) == 0) {
+            if (ctl->gave_up) return;
+            if (clock64() - t0 > kWaitLimit) {
+                ctl->gave_up = 1;
+                atomicOr(status, 4);
+                return;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(bar)) : "memory");
+}
+
+// operand in shared memory: rows of 128 bytes, 128-byte swizzle, groups of eight rows 1,024 bytes apart
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// half x half -> fp32, M = 128
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, int n, uint32_t accumulate) {
+    const uint32_t idesc = (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// 16 columns of the thread's TMEM lane
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// the 16 registers may only be used behind the wait above it
+__device__ __forceinline__ void settle(uint32_t *v) {
+    asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                      "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+}
+
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return reinterpret_cast<const uint32_t &>(h);
+}
+
+// value of two codes: (n 2^-24) is made n exactly, then n scale + offset rounds once
+template <int ROW>
+__device__ __forceinline__ uint32_t value2(uint32_t codes, __half2 scale, __half2 offset) {
+    // 1024 + n, or 1024 + 16 n
+    const uint32_t big = codes | 0x64006400u;
+    const __half2 n = ROW ? __hfma2(reinterpret_cast<const __half2 &>(big), __float2half2_rn(0.0625f), __float2half2_rn(-64.f))
+                          : __hadd2(reinterpret_cast<const __half2 &>(big), __float2half2_rn(-1024.f));
+    const __half2 v = __hfma2(n, scale, offset);
+    return reinterpret_cast<const uint32_t &>(v);
+}
+
+// One tile of query rows as every role walks them: request by request, heads, row tiles from the last (most keys) to the first.
+struct Item {
+    int row, len, queries, first_token, head, row0, rows;   // rows: of the request and head
+    int first_key, tiles;                                   // tiles of 128 keys from first_key on
+};
+
+struct ItemWalk {
+    long long item, start;
+    int request, n;
+};
+
+__device__ __forceinline__ bool next_item(const AttendParams &p, ItemWalk &w, Item &x) {
+    for (; w.request < w.n; ++w.request) {
+        const int i = w.request;
+        x.first_token = p.cu_tokens ? p.cu_tokens[i] : i;
+        x.queries = p.cu_tokens ? p.cu_tokens[i + 1] - x.first_token : 1;
+        x.row = p.row_idx ? p.row_idx[i] : i;
+        if (x.row < 0 || x.row >= p.rows || x.first_token < 0 || x.queries < 0 || x.queries > p.max_tokens - x.first_token) x.queries = 0;
+        x.rows = x.queries * p.group;
+        const int row_tiles = (int)(((long long)x.rows + kTile - 1) / kTile);
+        const long long here = (long long)row_tiles * p.kv_heads;
+        if (w.item >= w.start + here) {
+            w.start += here;
+            continue;
+        }
+        const int in_request = (int)(w.item - w.start);
+        x.head = in_request / row_tiles;
+        x.row0 = (row_tiles - 1 - (in_request - x.head * row_tiles)) * kTile;
+        const long long most = (long long)p.max_blocks << p.page_shift;
+        x.len = p.lens[x.row];
+        if (x.len > most) x.len = (int)most;
+        if (x.len < 0) x.len = 0;
+        const int first = x.len - x.queries + x.row0 / p.group, last = x.len - x.queries + (min(x.row0 + kTile, x.rows) - 1) / p.group;
+        x.first_key = p.window > 0 ? max(max(first, 0) - p.window + 1, 0) / kTile * kTile : 0;
+        x.tiles = last < 0 ? 0 : (last + 1 - x.first_key + kTile - 1) / kTile;
+        w.item += gridDim.x;
+        return true;
+    }
+    return false;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(const __grid_constant__ AttendParams p) {
+    using S = PromptSmem<D>;
+    constexpr int PANEL = kTile * 128;     // 128 rows of 128 bytes
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
+    PromptCtl *const ctl = reinterpret_cast<PromptCtl *>(smem + S::ctl);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&ctl->k_full[i], kUnpackWarps * 32);
+            bar_init(&ctl->k_empty[i], 1);
+            bar_init(&ctl->v_full[i], kUnpackWarps * 32);
+            bar_init(&ctl->v_empty[i], 1);
+            bar_init(&ctl->s_full[i], 1);
+            bar_init(&ctl->s_free[i], kSoftmaxWarps * 32);
+        }
+        bar_init(&ctl->p_full, kSoftmaxWarps * 32);
+        bar_init(&ctl->pv_done, 1);
+        bar_init(&ctl->q_full, kSoftmaxWarps * 32);
+        ctl->gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async();
+    }
+    if (warp == kSoftmaxWarps + kUnpackWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = ctl->tmem;
+    ItemWalk walk = {(long long)blockIdx.x, 0, 0, p.batch_max};
+    if (p.batch_count) walk.n = min(max(*p.batch_count, 0), p.batch_max);
+    Item x;
+    uint32_t tiles_before = 0;             // of the items before: stages, buffers and parities follow from it
+
+    if (warp < kSoftmaxWarps) {
+        // ---- a thread per query row ----
+        uint32_t items_before = 0;
+        while (next_item(p, walk, x)) {
+            const int row = x.row0 + tid;
+            const bool real = row < x.rows;
+            const int shown = real ? row : x.rows - 1;        // rows past the last see what it sees; they are never stored
+            const int j = shown / p.group, qh = x.head * p.group + shown - j * p.group;
+            const int pos = x.len - x.queries + j;
+            const int high = pos + 1, low = p.window > 0 ? max(pos, 0) - p.window + 1 : 0;
+            const int first = x.len - x.queries + x.row0 / p.group, last = x.len - x.queries + (min(x.row0 + kTile, x.rows) - 1) / p.group;
+            const int all_high = first + 1, all_low = p.window > 0 ? max(last, 0) - p.window + 1 : 0;
+            float c = 0.f;
+            if (x.tiles > 0) {
+                // ---- the row's query as halves, its largest value at 2^14 .. 2^15 (exact for bf16), in the order of the codes ----
+                const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
+                                                                 (long long)(x.first_token + j) * p.q_ts + (long long)qh * p.q_hs);
+                uint4 w[D / 8];
+                float top = 0.f;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    w[i] = real ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+                    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        top = fmaxf(top, fmaxf(fabsf(__uint_as_float(u[e] << 16)), fabsf(__uint_as_float(u[e] & 0xffff0000u))));
+                }
+                int up = 0;
+                if (top > 0.f && top < INFINITY) {
+                    up = 141 - (int)(__float_as_uint(top) >> 23);
+                    up = up < -110 ? -110 : up > 110 ? 110 : up;
+                }
+                // the factor of the scores is kept positive: its sign goes into the query (and a factor of zero makes it zero)
+                float f = __uint_as_float((uint32_t)(127 + up) << 23);
+                c = fabsf(p.scale_log2) * __uint_as_float((uint32_t)(127 - up) << 23);
+                if (p.scale_log2 < 0.f) f = -f;
+                if (!(c > 0.f)) {
+                    f = 0.f;
+                    c = 1.f;
+                }
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[2 * e] = __uint_as_float(u[e] << 16) * f;
+                        v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u) * f;
+                    }
+                    *reinterpret_cast<uint4 *>(smem + S::q + (i >> 3) * PANEL + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
+                        make_uint4(half2_bits(v[0], v[4]), half2_bits(v[1], v[5]), half2_bits(v[2], v[6]), half2_bits(v[3], v[7]));
+                }
+                fence_async();
+                bar_arrive(&ctl->q_full);
+            }
+            float top = kNoMax, sum = 0.f;
+            for (int t = 0; t < x.tiles; ++t) {
+                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
+                const int key0 = x.first_key + t * kTile;
+                bar_wait(&ctl->v_full[b], ph, ctl, p.status);      // the tile's powers
+                const float ck = c * ctl->k_power[b], fv = ctl->v_power[b];
+                bar_wait(&ctl->s_full[b], ph, ctl, p.status);
+                tc_after();
+                uint32_t s[kTile];
+                const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16) + b * kTile;
+#pragma unroll
+                for (int i = 0; i < kTile / 16; ++i) tmem_load(at + 16 * i, s + 16 * i);
+                tmem_load_wait();
+#pragma unroll
+                for (int i = 0; i < kTile / 16; ++i) settle(s + 16 * i);
+                tc_before();
+                bar_arrive(&ctl->s_free[b]);
+                if (key0 + kTile > all_high || key0 < all_low) {
+#pragma unroll
+                    for (int i = 0; i < kTile; ++i)
+                        if (key0 + i >= high || key0 + i < low) s[i] = 0xff800000u;
+                }
+                if (ctl->hidden[b][0] | ctl->hidden[b][1] | ctl->hidden[b][2] | ctl->hidden[b][3]) {
+#pragma unroll
+                    for (int w = 0; w < kUnpackWarps; ++w) {
+                        const uint32_t lost = ctl->hidden[b][w];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if ((lost >> i) & 1) s[32 * w + i] = 0xff800000u;
+                    }
+                }
+                float most = __uint_as_float(s[0]);
+#pragma unroll
+                for (int i = 1; i + 1 < kTile; i += 2) most = fmaxf(fmaxf(most, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
+                most = fmaf(fmaxf(most, __uint_as_float(s[kTile - 1])), ck, fv);
+                bool waited = t == 0;
+                if (__any_sync(0xffffffffu, most > top + 8.f)) {
+                    const float m = fmaxf(most, top), shrink = ex2(top - m);
+                    top = m;
+                    sum *= shrink;
+                    if (t > 0) {
+                        bar_wait(&ctl->pv_done, (n - 1) & 1, ctl, p.status);
+                        waited = true;
+                        tc_after();
+                        const uint32_t o_at = tmem + ((uint32_t)(warp * 32) << 16) + 2 * kTile;
+#pragma unroll 1
+                        for (int i = 0; i < D / 16; ++i) {
+                            uint32_t o[16];
+                            tmem_load(o_at + 16 * i, o);
+                            tmem_load_wait();
+                            settle(o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+                            tmem_store(o_at + 16 * i, o);
+                        }
+                        tmem_store_wait();
+                        tc_before();
+                    }
+                }
+                const float shift = fv - top;
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < kTile; i += 2) {
+                    const float w0 = ex2(fmaf(__uint_as_float(s[i]), ck, shift)), w1 = ex2(fmaf(__uint_as_float(s[i + 1]), ck, shift));
+                    part[i & 2] += w0;
+                    part[(i & 2) + 1] += w1;
+                    s[i >> 1] = half2_bits(w0, w1);
+                }
+                sum = fmaf((part[0] + part[1]) + (part[2] + part[3]), ex2(-fv), sum);
+                if (!waited) bar_wait(&ctl->pv_done, (n - 1) & 1, ctl, p.status);   // the products have read the weights before
+#pragma unroll
+                for (int i = 0; i < kTile / 8; ++i)
+                    *reinterpret_cast<uint4 *>(smem + S::p + (i >> 3) * PANEL + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
+                        make_uint4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+                fence_async();
+                tc_before();
+                bar_arrive(&ctl->p_full);
+            }
+            tiles_before += x.tiles;
+            if (x.tiles > 0) {
+                bar_wait(&ctl->pv_done, (tiles_before - 1) & 1, ctl, p.status);
+                tc_after();
+                ++items_before;
+            }
+            const float scale = sum != 0.f ? 1.f / sum : 0.f;
+            __nv_bfloat16 *const out = static_cast<__nv_bfloat16 *>(p.out) + (long long)(x.first_token + j) * p.out_ts + (long long)qh * p.out_hs;
+            const uint32_t o_at = tmem + ((uint32_t)(warp * 32) << 16) + 2 * kTile;
+#pragma unroll 1
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t o[16];
+                if (x.tiles > 0) {
+                    tmem_load(o_at + 16 * i, o);
+                    tmem_load_wait();
+                    settle(o);
+                }
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v0 = sum != 0.f ? __uint_as_float(o[2 * e]) * scale : 0.f, v1 = sum != 0.f ? __uint_as_float(o[2 * e + 1]) * scale : 0.f;
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(v0, v1);
+                    w[e] = reinterpret_cast<const uint32_t &>(h);
+                }
+                if (real) {
+                    reinterpret_cast<uint4 *>(out)[2 * i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    reinterpret_cast<uint4 *>(out)[2 * i + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+                }
+            }
+            if (real && p.lse)
+                p.lse[(long long)(x.first_token + j) * (p.kv_heads * p.group) + qh] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+            tc_before();
+        }
+    } else if (warp < kSoftmaxWarps + kUnpackWarps) {
+        // ---- codes to values ----
+        const int u = tid - kSoftmaxWarps * 32, uw = u >> 5;
+        const int mask = (1 << p.page_shift) - 1;
+        uint32_t set = 0;
+        while (next_item(p, walk, x)) {
+            const int32_t *const table = p.block_table + (long long)x.row * p.table_ld;
+            const unsigned char *const k_head = p.k_codes + x.head * p.hs, *const v_head = p.v_codes + x.head * p.hs;
+            for (int t = 0; t < x.tiles; ++t) {
+                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
+                const int key0 = x.first_key + t * kTile;
+                // this thread's key
+                const int key = key0 + u;
+                uint32_t page = 0xffffffffu;
+                if (key < x.len) {
+                    page = (uint32_t)__ldg(table + (key >> p.page_shift));
+                    if (page >= (uint32_t)p.num_pages) {
+                        page = 0xffffffffu;
+                        atomicOr(p.status, 2);
+                    }
+                }
+                const bool there = page != 0xffffffffu;
+                uint32_t kw[D / 8], km = 0, vm = 0;
+                if (there) {
+                    const uint32_t place = key & mask, off = page * p.ps + place * p.ts, moff = page * p.mps + place * p.mts;
+                    const uint4 *from = reinterpret_cast<const uint4 *>(k_head + off * 16ull);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const uint4 a = __ldg(from + i);
+                        kw[4 * i] = a.x; kw[4 * i + 1] = a.y; kw[4 * i + 2] = a.z; kw[4 * i + 3] = a.w;
+                    }
+                    km = __ldg(p.k_meta + x.head * p.mhs + moff);
+                    vm = __ldg(p.v_meta + x.head * p.mhs + moff);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) kw[i] = 0;
+                }
+                // the values: words of eight dims of eight neighbouring keys, D / 64 of them per thread
+                uint32_t vw[D / 64][8];
+                const int group_lo = lane & 7, word_lo = lane >> 3;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const int part = uw + 4 * i, group = group_lo + 8 * (part & 1), word = word_lo + 4 * (part >> 1);
+                    const int first = key0 + 8 * group;
+                    uint32_t pg = 0xffffffffu;
+                    if (first < x.len) pg = (uint32_t)__ldg(table + (first >> p.page_shift));
+                    if (pg < (uint32_t)p.num_pages) {
+                        const uint32_t place = first & mask;
+                        const unsigned char *const from = v_head + (pg * p.ps + place * p.ts) * 16ull + word * 4;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) vw[i][e] = __ldg(reinterpret_cast<const uint32_t *>(from + (unsigned long long)(e * p.ts) * 16));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) vw[i][e] = 0;
+                    }
+                }
+                float ks = meta_scale(km), ko = meta_offset(km), vs = meta_scale(vm), vo = meta_offset(vm);
+                const float kmost = fmaxf(fabsf(ko), fabsf(fmaf(15.f, ks, ko))), vmost = fmaxf(fabsf(vo), fabsf(fmaf(15.f, vs, vo)));
+                // no number in scale or offset: x - x is no number for infinities too
+                const bool bad = (ks - ks) + (ko - ko) + (vs - vs) + (vo - vo) != 0.f;
+                if (bad) {
+                    ks = 0.f;
+                    ko = __uint_as_float(0x7fc00000u);
+                    vs = vo = 0.f;
+                }
+                const uint32_t k_top = __reduce_max_sync(0xffffffffu, bad ? 0u : __float_as_uint(kmost)), v_top = __reduce_max_sync(0xffffffffu, bad ? 0u : __float_as_uint(vmost));
+                if (lane == 0) {
+                    ctl->red[set][0][uw] = k_top;
+                    ctl->red[set][1][uw] = v_top;
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                uint32_t kt = 0, vt = 0;
+#pragma unroll
+                for (int i = 0; i < kUnpackWarps; ++i) {
+                    kt = max(kt, ctl->red[set][0][i]);
+                    vt = max(vt, ctl->red[set][1][i]);
+                }
+                set ^= 1;
+                // powers of two that put the largest at 2^14 .. 2^15
+                int ke = kt ? (int)(kt >> 23) - 141 : 0, ve = vt ? (int)(vt >> 23) - 141 : 0;
+                ke = ke < -100 ? -100 : ke > 100 ? 100 : ke;
+                ve = ve < -100 ? -100 : ve > 100 ? 100 : ve;
+                const float kf = __uint_as_float((uint32_t)(127 - ke) << 23), vf = __uint_as_float((uint32_t)(127 - ve) << 23);
+
+                // ---- keys: a row each ----
+                bar_wait(&ctl->k_empty[b], ph ^ 1, ctl, p.status);
+                {
+                    const __half2 s2 = __float2half2_rn(ks * kf), o2 = __float2half2_rn(ko * kf);
+                    unsigned char *const to = smem + S::k + b * S::kK + u * 128;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint32_t w = kw[i], w8 = w >> 8;
+                        *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) =
+                            make_uint4(value2<0>(w & 0x000f000fu, s2, o2), value2<1>(w & 0x00f000f0u, s2, o2),
+                                       value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
+                    }
+                }
+                fence_async();
+                bar_arrive(&ctl->k_full[b]);
+
+                // ---- values: transposed, a row per dim; eight keys are 16 bytes of it ----
+                bar_wait(&ctl->v_empty[b], ph ^ 1, ctl, p.status);
+                const uint32_t lost = __ballot_sync(0xffffffffu, key < x.len && !there);
+                if (lane == 0) ctl->hidden[b][uw] = lost;
+                if (u == 0) {
+                    ctl->k_power[b] = __uint_as_float((uint32_t)(127 + ke) << 23);
+                    ctl->v_power[b] = (float)ve;
+                }
+                const uint32_t my_meta = half2_bits(vs * vf, vo * vf);   // scale, offset of this thread's key
+                uint32_t *const s_meta = reinterpret_cast<uint32_t *>(smem + S::ctl + sizeof(PromptCtl)) + b * kTile;
+                s_meta[u] = my_meta;
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const int part = uw + 4 * i, group = group_lo + 8 * (part & 1), word = word_lo + 4 * (part >> 1);
+                    uint32_t v[4][8];                                    // pairs of keys; dims
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint2 m = *reinterpret_cast<const uint2 *>(s_meta + 8 * group + 2 * q);
+                        const uint32_t sc = __byte_perm(m.x, m.y, 0x5410), of = __byte_perm(m.x, m.y, 0x7632);
+                        const __half2 s2 = reinterpret_cast<const __half2 &>(sc), o2 = reinterpret_cast<const __half2 &>(of);
+                        const uint32_t lo = __byte_perm(vw[i][2 * q], vw[i][2 * q + 1], 0x5410), hi = __byte_perm(vw[i][2 * q], vw[i][2 * q + 1], 0x7632);
+                        const uint32_t lo8 = lo >> 8, hi8 = hi >> 8;
+                        v[q][0] = value2<0>(lo & 0x000f000fu, s2, o2);
+                        v[q][1] = value2<1>(lo & 0x00f000f0u, s2, o2);
+                        v[q][2] = value2<0>(lo8 & 0x000f000fu, s2, o2);
+                        v[q][3] = value2<1>(lo8 & 0x00f000f0u, s2, o2);
+                        v[q][4] = value2<0>(hi & 0x000f000fu, s2, o2);
+                        v[q][5] = value2<1>(hi & 0x00f000f0u, s2, o2);
+                        v[q][6] = value2<0>(hi8 & 0x000f000fu, s2, o2);
+                        v[q][7] = value2<1>(hi8 & 0x00f000f0u, s2, o2);
+                    }
+                    unsigned char *const to = smem + S::v + b * S::kV + (group >> 3) * (D * 128) + word * 8 * 128;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        *reinterpret_cast<uint4 *>(to + e * 128 + (((group & 7) ^ e) << 4)) = make_uint4(v[0][e], v[1][e], v[2][e], v[3][e]);
+                }
+                fence_async();
+                bar_arrive(&ctl->v_full[b]);
+            }
+            tiles_before += x.tiles;
+        }
+    } else if (lane == 0) {
+        // ---- the products ----
+        const uint32_t q_at = smem_at(smem + S::q), k_at = smem_at(smem + S::k), v_at = smem_at(smem + S::v), p_at = smem_at(smem + S::p);
+        uint32_t items_before = 0;
+        const auto scores = [&](uint32_t n) {
+            const uint32_t b = n & 1, ph = (n >> 1) & 1;
+            bar_wait(&ctl->k_full[b], ph, ctl, p.status);
+            bar_wait(&ctl->s_free[b], ph ^ 1, ctl, p.status);
+            tc_after();
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                mma_f16(tmem + b * kTile, operand(q_at + (i >> 2) * PANEL) + 2 * (i & 3), operand(k_at + b * S::kK + (i >> 2) * PANEL) + 2 * (i & 3),
+                        kTile, i != 0);
+            tc_commit(&ctl->s_full[b]);
+            tc_commit(&ctl->k_empty[b]);
+        };
+        while (next_item(p, walk, x)) {
+            if (x.tiles == 0) continue;
+            bar_wait(&ctl->q_full, items_before & 1, ctl, p.status);
+            ++items_before;
+            scores(tiles_before);
+            for (int t = 0; t < x.tiles; ++t) {
+                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
+                if (t + 1 < x.tiles) scores(n + 1);
+                bar_wait(&ctl->v_full[b], ph, ctl, p.status);
+                bar_wait(&ctl->p_full, n & 1, ctl, p.status);
+                tc_after();
+#pragma unroll
+                for (int i = 0; i < kTile / 16; ++i)
+                    mma_f16(tmem + 2 * kTile, operand(p_at + (i >> 2) * PANEL) + 2 * (i & 3),
+                            operand(v_at + b * S::kV + (i >> 2) * (D * 128)) + 2 * (i & 3), D, (t | i) != 0);
+                tc_commit(&ctl->pv_done);
+                tc_commit(&ctl->v_empty[b]);
+            }
+            tiles_before += x.tiles;
+        }
+        // every product has been waited for by the rows, unless a wait was given up: then here
+        if (ctl->gave_up && tiles_before > 0) {
+            const long long t0 = clock64();
+            while (!bar_try(&ctl->pv_done, (tiles_before - 1) & 1) && clock64() - t0 < 200000000ll) {}
+        }
+    }
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    if (warp == kSoftmaxWarps + kUnpackWarps) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+template <int D>
+constexpr int prompt_smem() { return PromptSmem<D>::bytes + 2 * kTile * 4; }
+
+}  // namespace
+
+// Tiles of 128 rows pay from half a tile on, and when there are enough of them for half the SMs: the kernel for few rows cuts long
+// keys over CTAs, this one does not.
+bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long rows) {
+    if (dtype != FI_BF16 || (kv->cfg.head_dim != 64 && kv->cfg.head_dim != 128) || rows < kTile / 2) return false;
+    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kTile - 1) / kTile);
+    return items >= kv->sm_count / 2;
+}
+
+fi_status_t prepare_attend_prompt(const fi_kv *kv) {
+    cudaError_t e = cudaSuccess;
+    if (kv->cfg.head_dim == 64) e = cudaFuncSetAttribute(kv_attend_prompt_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, prompt_smem<64>());
+    if (kv->cfg.head_dim == 128) e = cudaFuncSetAttribute(kv_attend_prompt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, prompt_smem<128>());
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_kv_create: attention kernels");
+}
+
+fi_status_t launch_attend_prompt(const fi_kv *kv, const AttendParams &p, long long rows, cudaStream_t stream) {
+    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kTile - 1) / kTile);
+    const int grid = items < kv->sm_count ? (int)items : kv->sm_count;
+    if (kv->cfg.head_dim == 64) kv_attend_prompt_kernel<64><<<grid, kPromptThreads, prompt_smem<64>(), stream>>>(p);
+    else kv_attend_prompt_kernel<128><<<grid, kPromptThreads, prompt_smem<128>(), stream>>>(p);
+    count_launch();
+    return check_launch("fi_kv_attend");
+}
+
+}  // namespace fi

@@ -686,6 +686,10 @@ fi_status_t fi_kv_poll_status(fi_kv_t *kv) {
     if (e == cudaSuccess) e = cudaMemcpy(&word, kv->status_dev, sizeof word, cudaMemcpyDeviceToHost);
     if (e == cudaSuccess && word) e = cudaMemset(kv->status_dev, 0, sizeof word);
     if (e != cudaSuccess) return cuda_fail(e, "fi_kv_poll_status");
+    if (word & 4) {
+        set_error("fi_kv_poll_status: a bounded wait inside an attention kernel ran out");
+        return FI_ERR_TIMEOUT;
+    }
     if (word) {
         set_error("fi_kv_poll_status:%s%s", word & 1 ? " a slot past the pool was skipped by fi_kv_append;" : "",
                   word & 2 ? " a page number outside the pool was met by fi_kv_attend" : "");

@@ -431,10 +431,14 @@ class Attention:
         codes, meta = c[p][:, h].reshape(-1, self.dim // 2)[:x], m[p][:, h].reshape(-1, 2)[:x].double()
         return unpack(codes).double() * meta[:, :1] + meta[:, 1:]
 
-    def check(self, out, lse, scale=None, q=None):
+    def check(self, out, lse, scale=None, q=None, halves=False):
+        """`halves`: keys and values were rounded to half precision (relative 2^-11 each) before the products.  A score is then off by
+        a sum of head_dim independent roundings: six times the root of the sum of their squares (Hoeffding: exceeded once in 3e7)."""
         q = self.q if q is None else q
         scale = self.dim ** -0.5 if scale is None else scale
         half_weights = 2.0 ** -11 if q.dtype == torch.bfloat16 else 2.0 ** -21
+        if halves:
+            half_weights *= 2
         for i, (length, n) in enumerate(zip(self.lens, self.queries)):
             if n == 0:
                 continue
@@ -456,6 +460,8 @@ class Attention:
                     want = p @ v
                     # exponents: the scores' float32 sums, a few u of the largest parts of a score
                     exponent = 2.0 ** -20 * (1 + reach[:, None])
+                    if halves and length:
+                        exponent = exponent + 6 * 2.0 ** -11 * abs(scale) * (q[a:b, g].double().square() @ k.T.square()).sqrt().amax(-1, keepdim=True)
                     bound = (half_weights + 2 * exponent + 2.0 ** -18) * (p @ parts[:, None]) + rounding(q.dtype) * want.abs() * 1.01
                     got = out[a:b, g].double()
                     assert got.isfinite().all()
@@ -509,6 +515,57 @@ def test_attend_matches_formula(name, dtype):
     tokens = a.cu[-1]
     assert torch.equal(out[:tokens], again[:tokens])              # cuts and sums in a fixed order
     a.kv.poll_status()
+
+
+PROMPT_CASES = {name: c for name, c in ATTEND_CASES.items() if c["dim"] <= 128 and name not in ("long", "many")}
+PROMPT_CASES.update({
+    "tiles": dict(lens=[128, 129, 384, 700], queries=[128, 127, 300, 1], q_heads=8, kv_heads=2, dim=128, page=32),
+    "one-head": dict(lens=[600], queries=[260], q_heads=1, kv_heads=1, dim=64, page=16),
+    "behind-a-context": dict(lens=[1000, 131], queries=[70, 3], q_heads=14, kv_heads=2, dim=128, order="token"),
+    "narrow-window": dict(lens=[700, 300], queries=[400, 300], q_heads=4, kv_heads=2, dim=64, window=33),
+    "wide-window": dict(lens=[900], queries=[150], q_heads=4, kv_heads=1, dim=128, window=500, page=64),
+    "many-requests": dict(lens=[int(x) for x in np.random.default_rng(2).integers(1, 200, 90)],
+                          queries=[int(x) for x in np.random.default_rng(3).integers(0, 40, 90)], q_heads=8, kv_heads=2, dim=64),
+})
+MANY = 20000        # a hint of this many queries takes the kernel for prompts, whatever there are
+
+
+@pytest.mark.parametrize("name", PROMPT_CASES)
+def test_attend_prompt_kernel_matches_formula(name):
+    a = Attention(**PROMPT_CASES[name])
+    out, lse = a.run(max_query=MANY)
+    a.check(out, lse, halves=True)
+    again, _ = a.run(max_query=MANY)
+    assert torch.equal(out[:a.cu[-1]], again[:a.cu[-1]])
+    a.kv.poll_status()
+
+
+@pytest.mark.parametrize("size,scale", [(1e-3, 1.0), (30.0, 1.0), (1e4, -1.0), (1.0, 0.0)])
+def test_attend_prompt_kernel_sizes_of_values(size, scale):
+    a = Attention(lens=[130, 700], queries=[100, 2], q_heads=4, kv_heads=2, dim=128, size=size)
+    scale = scale / (size * size * 128)
+    out, lse = a.run(scale=scale, max_query=MANY)
+    a.check(out, lse, scale=scale, halves=True)
+
+
+def test_attend_prompt_kernel_hidden_nan_and_bad_pages():
+    a = Attention(lens=[300], queries=[40], q_heads=4, kv_heads=2, dim=128)
+    whole, _ = a.run(max_query=MANY)
+    page = a.table[0, 280 // a.page].long()
+    a.vm[page, 0, 280 % a.page, 1] = math.nan                    # queries 0 .. 19 stand before it
+    out, lse = a.run(max_query=MANY)
+    assert torch.equal(out[:20], whole[:20]) and out[20:40, :2].isnan().all() and torch.equal(out[20:40, 2:], whole[20:40, 2:])
+    a.kv.poll_status()
+    b = Attention(lens=[300], queries=[40], q_heads=4, kv_heads=2, dim=128)
+    b.table[0, 3] = -1                                           # 16 keys hidden
+    hidden = b.run(max_query=MANY)
+    with pytest.raises(fb.FiError):
+        b.kv.poll_status()
+    few = b.run(max_query=1)
+    with pytest.raises(fb.FiError):
+        b.kv.poll_status()
+    assert ((hidden[0][:40].double() - few[0][:40].double()).abs() <= 2.0 ** -6 * (1 + few[0][:40].double().abs())).all()
+    assert ((hidden[1][:40] - few[1][:40]).abs() <= 2.0 ** -7).all()
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
