@@ -1,10 +1,13 @@
 // Attention over the 4-bit store for many queries per request (prompts): tensor-bound, so it runs on tcgen05.
 //
 // A CTA takes a tile of 128 query rows of one request and key head (row = query x heads of the group) and walks the keys in
-// tiles of 128.  Four warps unpack a tile of keys and values to halves in shared memory, one thread issues the products
+// tiles of 128.  Four warps unpack the keys of a tile to halves in shared memory and four its values, one thread issues the
+// products
 //   S = Q K^T  (128 x 128, fp32 in TMEM, two buffers)      O += P V  (128 x head_dim, fp32 in TMEM)
-// and four warps, a thread per row, turn S into the weights P.  The three meet at mbarriers: keys and values are unpacked
-// up to two tiles ahead, S of the next tile is multiplied while the weights of this one are formed.
+// and four warps, a thread per row, turn S into the weights P.  They meet at mbarriers: keys and values are unpacked up to
+// two tiles ahead, S of the next tile is multiplied while the weights of this one are formed.  Every role's loop is kept
+// short (S is read from TMEM twice, 64 columns at a time, rather than held): with all of it unrolled a third of the
+// warps' time went into waiting for instructions.
 //
 // Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
 // rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
@@ -18,8 +21,9 @@ namespace {
 
 constexpr int kTile = 128;                 // query rows and keys of a tile
 constexpr int kSoftmaxWarps = 4;           // warp w owns TMEM lanes 32 w ..
-constexpr int kUnpackWarps = 4;
-constexpr int kPromptThreads = (kSoftmaxWarps + kUnpackWarps + 1) * 32;
+constexpr int kUnpackWarps = 4;            // for the keys, and as many for the values
+constexpr int kProductWarp = kSoftmaxWarps + 2 * kUnpackWarps;
+constexpr int kPromptThreads = (kProductWarp + 1) * 32;
 constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
 constexpr int kTmemCols = 512;             // S, S, O
 
@@ -144,6 +148,31 @@ __device__ __forceinline__ uint32_t value2(uint32_t codes, __half2 scale, __half
     return reinterpret_cast<const uint32_t &>(v);
 }
 
+constexpr uint32_t kNone = 0xffffffffu;
+
+// Scale and offset of a key and of its value; bad: one of the four is no finite number (y - y is not 0 then).
+struct KeyMeta {
+    uint32_t k, v;
+    bool bad;
+    __device__ __forceinline__ KeyMeta(uint32_t k_, uint32_t v_) : k(k_), v(v_) {
+        const float ks = meta_scale(k), ko = meta_offset(k), vs = meta_scale(v), vo = meta_offset(v);
+        bad = (ks - ks) + (ko - ko) + (vs - vs) + (vo - vo) != 0.f;
+    }
+};
+
+// E of a tile, which puts the largest of its 128 values (one per thread of four warps) at 2^14 .. 2^15 when it is taken out; `red` is
+// used again two tiles later.
+__device__ __forceinline__ int tile_power(float most, uint32_t *red, int uw, int lane, int barrier) {
+    const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
+    if (lane == 0) red[uw] = top;
+    asm volatile("bar.sync %0, 128;" ::"r"(barrier) : "memory");
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < kUnpackWarps; ++i) all = max(all, *reinterpret_cast<volatile uint32_t *>(red + i));
+    const int e = all ? (int)(all >> 23) - 141 : 0;
+    return e < -100 ? -100 : e > 100 ? 100 : e;
+}
+
 // One tile of query rows as every role walks them: request by request, heads, row tiles from the last (most keys) to the first.
 struct Item {
     int row, len, queries, first_token, head, row0, rows;   // rows: of the request and head
@@ -209,7 +238,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
     }
-    if (warp == kSoftmaxWarps + kUnpackWarps) {
+    if (warp == kProductWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -281,37 +310,38 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             for (int t = 0; t < x.tiles; ++t) {
                 const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
                 const int key0 = x.first_key + t * kTile;
-                bar_wait(&ctl->v_full[b], ph, ctl, p.status);      // the tile's powers
+                bar_wait(&ctl->k_full[b], ph, ctl, p.status);      // the tile's powers
+                bar_wait(&ctl->v_full[b], ph, ctl, p.status);
                 const float ck = c * ctl->k_power[b], fv = ctl->v_power[b];
                 bar_wait(&ctl->s_full[b], ph, ctl, p.status);
                 tc_after();
-                uint32_t s[kTile];
                 const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16) + b * kTile;
+                const uint32_t lost = ctl->hidden[b][0] | ctl->hidden[b][1] | ctl->hidden[b][2] | ctl->hidden[b][3];
+                const bool edge = key0 + kTile > all_high || key0 < all_low || lost != 0;
+                // 64 scores from column c0 on, hidden ones at -infinity
+                uint32_t s[64];
+                const auto read = [&](int c0) {
 #pragma unroll
-                for (int i = 0; i < kTile / 16; ++i) tmem_load(at + 16 * i, s + 16 * i);
-                tmem_load_wait();
+                    for (int i = 0; i < 4; ++i) tmem_load(at + c0 + 16 * i, s + 16 * i);
+                    tmem_load_wait();
 #pragma unroll
-                for (int i = 0; i < kTile / 16; ++i) settle(s + 16 * i);
-                tc_before();
-                bar_arrive(&ctl->s_free[b]);
-                if (key0 + kTile > all_high || key0 < all_low) {
+                    for (int i = 0; i < 4; ++i) settle(s + 16 * i);
+                    if (edge) {
+                        const int hi = high - key0 - c0, lo = low - key0 - c0;
+                        const unsigned long long gone = lost ? (unsigned long long)ctl->hidden[b][c0 / 32 + 1] << 32 | ctl->hidden[b][c0 / 32] : 0;
 #pragma unroll
-                    for (int i = 0; i < kTile; ++i)
-                        if (key0 + i >= high || key0 + i < low) s[i] = 0xff800000u;
-                }
-                if (ctl->hidden[b][0] | ctl->hidden[b][1] | ctl->hidden[b][2] | ctl->hidden[b][3]) {
-#pragma unroll
-                    for (int w = 0; w < kUnpackWarps; ++w) {
-                        const uint32_t lost = ctl->hidden[b][w];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if ((lost >> i) & 1) s[32 * w + i] = 0xff800000u;
+                        for (int i = 0; i < 64; ++i)
+                            if (i >= hi || i < lo || ((gone >> i) & 1)) s[i] = 0xff800000u;
                     }
-                }
-                float most = __uint_as_float(s[0]);
+                };
+                float most = -INFINITY;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                    read(c0);
 #pragma unroll
-                for (int i = 1; i + 1 < kTile; i += 2) most = fmaxf(fmaxf(most, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
-                most = fmaf(fmaxf(most, __uint_as_float(s[kTile - 1])), ck, fv);
+                    for (int i = 0; i < 64; i += 2) most = fmaxf(fmaxf(most, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
+                }
+                most = fmaf(most, ck, fv);
                 bool waited = t == 0;
                 if (__any_sync(0xffffffffu, most > top + 8.f)) {
                     const float m = fmaxf(most, top), shrink = ex2(top - m);
@@ -336,21 +366,29 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                         tc_before();
                     }
                 }
+                if (!waited) bar_wait(&ctl->pv_done, (n - 1) & 1, ctl, p.status);   // the products have read the weights before
                 const float shift = fv - top;
                 float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                    read(c0);
 #pragma unroll
-                for (int i = 0; i < kTile; i += 2) {
-                    const float w0 = ex2(fmaf(__uint_as_float(s[i]), ck, shift)), w1 = ex2(fmaf(__uint_as_float(s[i + 1]), ck, shift));
-                    part[i & 2] += w0;
-                    part[(i & 2) + 1] += w1;
-                    s[i >> 1] = half2_bits(w0, w1);
+                    for (int i = 0; i < 64; i += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float w0 = ex2(fmaf(__uint_as_float(s[i + 2 * e]), ck, shift)), w1 = ex2(fmaf(__uint_as_float(s[i + 2 * e + 1]), ck, shift));
+                            part[(2 * e) & 3] += w0;
+                            part[(2 * e + 1) & 3] += w1;
+                            w[e] = half2_bits(w0, w1);
+                        }
+                        *reinterpret_cast<uint4 *>(smem + S::p + (c0 >> 6) * PANEL + tid * 128 + (((i >> 3) ^ (tid & 7)) << 4)) =
+                            make_uint4(w[0], w[1], w[2], w[3]);
+                    }
                 }
+                tc_before();
+                bar_arrive(&ctl->s_free[b]);
                 sum = fmaf((part[0] + part[1]) + (part[2] + part[3]), ex2(-fv), sum);
-                if (!waited) bar_wait(&ctl->pv_done, (n - 1) & 1, ctl, p.status);   // the products have read the weights before
-#pragma unroll
-                for (int i = 0; i < kTile / 8; ++i)
-                    *reinterpret_cast<uint4 *>(smem + S::p + (i >> 3) * PANEL + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
-                        make_uint4(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
                 fence_async();
                 tc_before();
                 bar_arrive(&ctl->p_full);
@@ -389,141 +427,150 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             tc_before();
         }
     } else if (warp < kSoftmaxWarps + kUnpackWarps) {
-        // ---- codes to values ----
+        // ---- keys: a thread per key; pages are looked up two tiles ahead, codes fetched one tile ahead ----
         const int u = tid - kSoftmaxWarps * 32, uw = u >> 5;
         const int mask = (1 << p.page_shift) - 1;
-        uint32_t set = 0;
         while (next_item(p, walk, x)) {
             const int32_t *const table = p.block_table + (long long)x.row * p.table_ld;
-            const unsigned char *const k_head = p.k_codes + x.head * p.hs, *const v_head = p.v_codes + x.head * p.hs;
+            const unsigned char *const k_head = p.k_codes + x.head * p.hs;
+            const uint32_t *const km_head = p.k_meta + x.head * p.mhs, *const vm_head = p.v_meta + x.head * p.mhs;
+            uint32_t page = kNone, next[D / 8], next_km = 0, next_vm = 0;
+            bool next_lost = false;
+            const auto look_up = [&](int t) {
+                const int key = x.first_key + t * kTile + u;
+                page = t < x.tiles && key < x.len ? min((uint32_t)__ldg(table + (key >> p.page_shift)), kNone - 1) : kNone;
+            };
+            const auto fetch = [&](int t) {
+                const int key = x.first_key + t * kTile + u;
+                const bool there = page < (uint32_t)p.num_pages;
+                next_lost = !there && page != kNone;
+                next_km = next_vm = 0;
+                const uint32_t place = key & mask, off = page * p.ps + place * p.ts, moff = page * p.mps + place * p.mts;
+                const uint4 *from = reinterpret_cast<const uint4 *>(k_head + off * 16ull);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const uint4 a = there ? __ldg(from + i) : make_uint4(0, 0, 0, 0);
+                    next[4 * i] = a.x; next[4 * i + 1] = a.y; next[4 * i + 2] = a.z; next[4 * i + 3] = a.w;
+                }
+                if (there) {
+                    next_km = __ldg(km_head + moff);
+                    next_vm = __ldg(vm_head + moff);
+                }
+            };
+            look_up(0);
+            fetch(0);
+            look_up(1);
             for (int t = 0; t < x.tiles; ++t) {
                 const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
-                const int key0 = x.first_key + t * kTile;
-                // this thread's key
-                const int key = key0 + u;
-                uint32_t page = 0xffffffffu;
-                if (key < x.len) {
-                    page = (uint32_t)__ldg(table + (key >> p.page_shift));
-                    if (page >= (uint32_t)p.num_pages) {
-                        page = 0xffffffffu;
-                        atomicOr(p.status, 2);
-                    }
-                }
-                const bool there = page != 0xffffffffu;
-                uint32_t kw[D / 8], km = 0, vm = 0;
-                if (there) {
-                    const uint32_t place = key & mask, off = page * p.ps + place * p.ts, moff = page * p.mps + place * p.mts;
-                    const uint4 *from = reinterpret_cast<const uint4 *>(k_head + off * 16ull);
+                uint32_t w[D / 8];
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) {
-                        const uint4 a = __ldg(from + i);
-                        kw[4 * i] = a.x; kw[4 * i + 1] = a.y; kw[4 * i + 2] = a.z; kw[4 * i + 3] = a.w;
-                    }
-                    km = __ldg(p.k_meta + x.head * p.mhs + moff);
-                    vm = __ldg(p.v_meta + x.head * p.mhs + moff);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) kw[i] = 0;
-                }
-                // the values: words of eight dims of eight neighbouring keys, D / 64 of them per thread
-                uint32_t vw[D / 64][8];
-                const int group_lo = lane & 7, word_lo = lane >> 3;
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const int part = uw + 4 * i, group = group_lo + 8 * (part & 1), word = word_lo + 4 * (part >> 1);
-                    const int first = key0 + 8 * group;
-                    uint32_t pg = 0xffffffffu;
-                    if (first < x.len) pg = (uint32_t)__ldg(table + (first >> p.page_shift));
-                    if (pg < (uint32_t)p.num_pages) {
-                        const uint32_t place = first & mask;
-                        const unsigned char *const from = v_head + (pg * p.ps + place * p.ts) * 16ull + word * 4;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) vw[i][e] = __ldg(reinterpret_cast<const uint32_t *>(from + (unsigned long long)(e * p.ts) * 16));
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) vw[i][e] = 0;
-                    }
-                }
-                float ks = meta_scale(km), ko = meta_offset(km), vs = meta_scale(vm), vo = meta_offset(vm);
-                const float kmost = fmaxf(fabsf(ko), fabsf(fmaf(15.f, ks, ko))), vmost = fmaxf(fabsf(vo), fabsf(fmaf(15.f, vs, vo)));
-                // no number in scale or offset: x - x is no number for infinities too
-                const bool bad = (ks - ks) + (ko - ko) + (vs - vs) + (vo - vo) != 0.f;
-                if (bad) {
-                    ks = 0.f;
-                    ko = __uint_as_float(0x7fc00000u);
-                    vs = vo = 0.f;
-                }
-                const uint32_t k_top = __reduce_max_sync(0xffffffffu, bad ? 0u : __float_as_uint(kmost)), v_top = __reduce_max_sync(0xffffffffu, bad ? 0u : __float_as_uint(vmost));
-                if (lane == 0) {
-                    ctl->red[set][0][uw] = k_top;
-                    ctl->red[set][1][uw] = v_top;
-                }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                uint32_t kt = 0, vt = 0;
-#pragma unroll
-                for (int i = 0; i < kUnpackWarps; ++i) {
-                    kt = max(kt, ctl->red[set][0][i]);
-                    vt = max(vt, ctl->red[set][1][i]);
-                }
-                set ^= 1;
-                // powers of two that put the largest at 2^14 .. 2^15
-                int ke = kt ? (int)(kt >> 23) - 141 : 0, ve = vt ? (int)(vt >> 23) - 141 : 0;
-                ke = ke < -100 ? -100 : ke > 100 ? 100 : ke;
-                ve = ve < -100 ? -100 : ve > 100 ? 100 : ve;
-                const float kf = __uint_as_float((uint32_t)(127 - ke) << 23), vf = __uint_as_float((uint32_t)(127 - ve) << 23);
-
-                // ---- keys: a row each ----
+                for (int i = 0; i < D / 8; ++i) w[i] = next[i];
+                const KeyMeta meta(next_km, next_vm);
+                const bool lost = next_lost;
+                if (lost) atomicOr(p.status, 2);
+                fetch(t + 1);
+                look_up(t + 2);
+                const float scale = meta.bad ? 0.f : meta_scale(meta.k), offset = meta.bad ? __uint_as_float(0x7fc00000u) : meta_offset(meta.k);
+                const int e = tile_power(meta.bad ? 0.f : fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][0], uw, lane, 1);
+                const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+                const __half2 s2 = __float2half2_rn(scale * f), o2 = __float2half2_rn(offset * f);
                 bar_wait(&ctl->k_empty[b], ph ^ 1, ctl, p.status);
-                {
-                    const __half2 s2 = __float2half2_rn(ks * kf), o2 = __float2half2_rn(ko * kf);
-                    unsigned char *const to = smem + S::k + b * S::kK + u * 128;
+                unsigned char *const to = smem + S::k + b * S::kK + u * 128;
 #pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const uint32_t w = kw[i], w8 = w >> 8;
-                        *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) =
-                            make_uint4(value2<0>(w & 0x000f000fu, s2, o2), value2<1>(w & 0x00f000f0u, s2, o2),
-                                       value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
-                    }
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint32_t w8 = w[i] >> 8;
+                    *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) =
+                        make_uint4(value2<0>(w[i] & 0x000f000fu, s2, o2), value2<1>(w[i] & 0x00f000f0u, s2, o2),
+                                   value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
                 }
+                // the rows are done with tile n - 2, whose powers these replace: its S was needed for this stage to be empty, its
+                // weights for v_empty, which the product of tile n - 2 comes before
+                bar_wait(&ctl->v_empty[b], ph ^ 1, ctl, p.status);
+                const uint32_t gone = __ballot_sync(0xffffffffu, lost);
+                if (lane == 0) ctl->hidden[b][uw] = gone;
+                if (u == 0) ctl->k_power[b] = __uint_as_float((uint32_t)(127 + e) << 23);
                 fence_async();
                 bar_arrive(&ctl->k_full[b]);
-
-                // ---- values: transposed, a row per dim; eight keys are 16 bytes of it ----
-                bar_wait(&ctl->v_empty[b], ph ^ 1, ctl, p.status);
-                const uint32_t lost = __ballot_sync(0xffffffffu, key < x.len && !there);
-                if (lane == 0) ctl->hidden[b][uw] = lost;
-                if (u == 0) {
-                    ctl->k_power[b] = __uint_as_float((uint32_t)(127 + ke) << 23);
-                    ctl->v_power[b] = (float)ve;
+            }
+            tiles_before += x.tiles;
+        }
+    } else if (warp < kProductWarp) {
+        // ---- values, transposed: a row per dim, eight neighbouring keys are 16 bytes of it.  A thread takes D / 64 times a word
+        // of eight dims of eight keys; pages are looked up two tiles ahead, codes fetched one tile ahead ----
+        constexpr int NV = D / 64;
+        const int u = tid - (kSoftmaxWarps + kUnpackWarps) * 32, uw = u >> 5;
+        const int mask = (1 << p.page_shift) - 1;
+        // eight lanes hold the groups of eight keys of half a tile, so that their 16-byte pieces of a row hit different banks
+        const int group = (lane & 7) + 8 * (uw & 1), word0 = (lane >> 3) + 4 * (uw >> 1);
+        uint32_t *const s_meta = reinterpret_cast<uint32_t *>(smem + S::ctl + sizeof(PromptCtl));
+        while (next_item(p, walk, x)) {
+            const int32_t *const table = p.block_table + (long long)x.row * p.table_ld;
+            const unsigned char *const v_head = p.v_codes + x.head * p.hs + word0 * 4;
+            const uint32_t *const km_head = p.k_meta + x.head * p.mhs, *const vm_head = p.v_meta + x.head * p.mhs;
+            uint32_t page = kNone, group_page = kNone, next[NV][8], next_km = 0, next_vm = 0;   // of the thread's key, of its group
+            const auto look_up = [&](int t) {
+                const int key = x.first_key + t * kTile + u, first = x.first_key + t * kTile + 8 * group;
+                page = t < x.tiles && key < x.len ? (uint32_t)__ldg(table + (key >> p.page_shift)) : kNone;
+                group_page = t < x.tiles && first < x.len ? (uint32_t)__ldg(table + (first >> p.page_shift)) : kNone;
+            };
+            const auto fetch = [&](int t) {
+                const int key = x.first_key + t * kTile + u, first = x.first_key + t * kTile + 8 * group;
+                next_km = next_vm = 0;
+                if (page < (uint32_t)p.num_pages) {
+                    const uint32_t moff = page * p.mps + (uint32_t)(key & mask) * p.mts;
+                    next_km = __ldg(km_head + moff);
+                    next_vm = __ldg(vm_head + moff);
                 }
-                const uint32_t my_meta = half2_bits(vs * vf, vo * vf);   // scale, offset of this thread's key
-                uint32_t *const s_meta = reinterpret_cast<uint32_t *>(smem + S::ctl + sizeof(PromptCtl)) + b * kTile;
-                s_meta[u] = my_meta;
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                const bool there = group_page < (uint32_t)p.num_pages;
+                const unsigned char *const from = v_head + (group_page * p.ps + (uint32_t)(first & mask) * p.ts) * 16ull;
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const int part = uw + 4 * i, group = group_lo + 8 * (part & 1), word = word_lo + 4 * (part >> 1);
-                    uint32_t v[4][8];                                    // pairs of keys; dims
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint2 m = *reinterpret_cast<const uint2 *>(s_meta + 8 * group + 2 * q);
-                        const uint32_t sc = __byte_perm(m.x, m.y, 0x5410), of = __byte_perm(m.x, m.y, 0x7632);
-                        const __half2 s2 = reinterpret_cast<const __half2 &>(sc), o2 = reinterpret_cast<const __half2 &>(of);
-                        const uint32_t lo = __byte_perm(vw[i][2 * q], vw[i][2 * q + 1], 0x5410), hi = __byte_perm(vw[i][2 * q], vw[i][2 * q + 1], 0x7632);
-                        const uint32_t lo8 = lo >> 8, hi8 = hi >> 8;
-                        v[q][0] = value2<0>(lo & 0x000f000fu, s2, o2);
-                        v[q][1] = value2<1>(lo & 0x00f000f0u, s2, o2);
-                        v[q][2] = value2<0>(lo8 & 0x000f000fu, s2, o2);
-                        v[q][3] = value2<1>(lo8 & 0x00f000f0u, s2, o2);
-                        v[q][4] = value2<0>(hi & 0x000f000fu, s2, o2);
-                        v[q][5] = value2<1>(hi & 0x00f000f0u, s2, o2);
-                        v[q][6] = value2<0>(hi8 & 0x000f000fu, s2, o2);
-                        v[q][7] = value2<1>(hi8 & 0x00f000f0u, s2, o2);
-                    }
-                    unsigned char *const to = smem + S::v + b * S::kV + (group >> 3) * (D * 128) + word * 8 * 128;
+                for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        *reinterpret_cast<uint4 *>(to + e * 128 + (((group & 7) ^ e) << 4)) = make_uint4(v[0][e], v[1][e], v[2][e], v[3][e]);
+                        next[i][e] = there ? __ldg(reinterpret_cast<const uint32_t *>(from + i * 32 + (unsigned long long)(e * p.ts) * 16)) : 0u;
+            };
+            look_up(0);
+            fetch(0);
+            look_up(1);
+            for (int t = 0; t < x.tiles; ++t) {
+                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
+                uint32_t w[NV][8];
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[i][e] = next[i][e];
+                const KeyMeta meta(next_km, next_vm);
+                fetch(t + 1);
+                look_up(t + 2);
+                const float scale = meta.bad ? 0.f : meta_scale(meta.v), offset = meta.bad ? 0.f : meta_offset(meta.v);
+                const int e = tile_power(fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][1], uw, lane, 2);
+                const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+                bar_wait(&ctl->v_empty[b], ph ^ 1, ctl, p.status);
+                s_meta[b * kTile + u] = half2_bits(scale * f, offset * f);
+                if (u == 0) ctl->v_power[b] = (float)e;
+                asm volatile("bar.sync 2, 128;" ::: "memory");
+                unsigned char *const to = smem + S::v + b * S::kV + (group >> 3) * (D * 128) + word0 * 1024;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {                        // four dims at a time: the registers hold no more
+                        uint32_t v[4][4];                                // pairs of keys; dims
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint2 m = *reinterpret_cast<const uint2 *>(s_meta + b * kTile + 8 * group + 2 * q);
+                            const uint32_t sc = __byte_perm(m.x, m.y, 0x5410), of = __byte_perm(m.x, m.y, 0x7632);
+                            const __half2 s2 = reinterpret_cast<const __half2 &>(sc), o2 = reinterpret_cast<const __half2 &>(of);
+                            const uint32_t c = __byte_perm(w[i][2 * q], w[i][2 * q + 1], h ? 0x7632 : 0x5410), c8 = c >> 8;
+                            v[q][0] = value2<0>(c & 0x000f000fu, s2, o2);
+                            v[q][1] = value2<1>(c & 0x00f000f0u, s2, o2);
+                            v[q][2] = value2<0>(c8 & 0x000f000fu, s2, o2);
+                            v[q][3] = value2<1>(c8 & 0x00f000f0u, s2, o2);
+                        }
+#pragma unroll
+                        for (int d = 0; d < 4; ++d)
+                            *reinterpret_cast<uint4 *>(to + i * 8192 + (4 * h + d) * 128 + (((group & 7) ^ (4 * h + d)) << 4)) =
+                                make_uint4(v[0][d], v[1][d], v[2][d], v[3][d]);
+                    }
                 }
                 fence_async();
                 bar_arrive(&ctl->v_full[b]);
@@ -575,7 +622,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
     __syncwarp();
     tc_before();
     __syncthreads();
-    if (warp == kSoftmaxWarps + kUnpackWarps) {
+    if (warp == kProductWarp) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
