@@ -268,15 +268,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 // ---- the row's query as halves, its largest value at 2^14 .. 2^15 (exact for bf16), in the order of the codes ----
                 const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
                                                                  (long long)(x.first_token + j) * p.q_ts + (long long)qh * p.q_hs);
-                uint4 w[D / 8];
                 float top = 0.f;
+                const auto words = [&](int i, float (&v)[8]) {
+                    const uint4 w = real ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[2 * e] = __uint_as_float(u[e] << 16);
+                        v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                    }
+                };
+#pragma unroll 4
                 for (int i = 0; i < D / 8; ++i) {
-                    w[i] = real ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
-                    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    float v[8];
+                    words(i, v);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        top = fmaxf(top, fmaxf(fabsf(__uint_as_float(u[e] << 16)), fabsf(__uint_as_float(u[e] & 0xffff0000u))));
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
                 }
                 int up = 0;
                 if (top > 0.f && top < INFINITY) {
@@ -291,17 +298,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     f = 0.f;
                     c = 1.f;
                 }
-#pragma unroll
+#pragma unroll 4
                 for (int i = 0; i < D / 8; ++i) {
-                    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
                     float v[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[2 * e] = __uint_as_float(u[e] << 16) * f;
-                        v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u) * f;
-                    }
+                    words(i, v);
                     *reinterpret_cast<uint4 *>(smem + S::q + (i >> 3) * PANEL + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
-                        make_uint4(half2_bits(v[0], v[4]), half2_bits(v[1], v[5]), half2_bits(v[2], v[6]), half2_bits(v[3], v[7]));
+                        make_uint4(half2_bits(v[0] * f, v[4] * f), half2_bits(v[1] * f, v[5] * f), half2_bits(v[2] * f, v[6] * f),
+                                   half2_bits(v[3] * f, v[7] * f));
                 }
                 fence_async();
                 bar_arrive(&ctl->q_full);
