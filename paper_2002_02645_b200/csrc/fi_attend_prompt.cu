@@ -1,13 +1,13 @@
 // Attention over the 4-bit store for many queries per request (prompts): tensor-bound, so it runs on tcgen05.
 //
-// A CTA takes a tile of 128 query rows of one request and key head (row = query x heads of the group) and walks the keys in
-// tiles of 128.  Four warps unpack the keys of a tile to halves in shared memory and four its values, one thread issues the
-// products
-//   S = Q K^T  (128 x 128, fp32 in TMEM, two buffers)      O += P V  (128 x head_dim, fp32 in TMEM)
-// and four warps, a thread per row, turn S into the weights P.  They meet at mbarriers: keys and values are unpacked up to
-// two tiles ahead, S of the next tile is multiplied while the weights of this one are formed.  Every role's loop is kept
-// short (S is read from TMEM twice, 64 columns at a time, rather than held): with all of it unrolled a third of the
-// warps' time went into waiting for instructions.
+// A CTA takes 256 query rows of one request and key head (row = query x heads of the group), as two halves of 128, and walks
+// the keys in tiles of 128.  Four warps unpack the keys of a tile to halves in shared memory and four its values; four warps
+// per half, a thread per row, turn S into the weights P; and one thread of a warp of its own issues the products
+//   S = Q K^T  (128 x 128, fp32 in TMEM)      O += P V  (128 x head_dim, fp32 in TMEM)
+// for each half.  The halves take turns: while one forms weights the other's products run.  All meet at mbarriers.
+//   Every role's loop is short (S is read from TMEM twice, 32 columns at a time, rather than held).  One half alone with all of
+// it unrolled spent a third of its warps' time waiting for instructions and took PLAIN us on two chunks of 1,024 queries of 32
+// heads behind 8,192 keys; products issued by a thread that forms weights hold it up by 2,000 cycles per tile.
 //
 // Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
 // rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
@@ -19,27 +19,30 @@
 namespace fi {
 namespace {
 
-constexpr int kTile = 128;                 // query rows and keys of a tile
-constexpr int kSoftmaxWarps = 4;           // warp w owns TMEM lanes 32 w ..
+constexpr int kTile = 128;                 // keys of a tile, query rows of a half
+constexpr int kRows = 2 * kTile;           // query rows of a CTA
+constexpr int kSoftmaxWarps = 8;           // warp w reads TMEM lanes 32 (w mod 4) .. of half w / 4
 constexpr int kUnpackWarps = 4;            // for the keys, and as many for the values
 constexpr int kProductWarp = kSoftmaxWarps + 2 * kUnpackWarps;
 constexpr int kPromptThreads = (kProductWarp + 1) * 32;
 constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
-constexpr int kTmemCols = 512;             // S, S, O
+constexpr int kTmemCols = 512;             // S of both halves, O of both
 
 struct PromptCtl {
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], s_free[2], p_full, pv_done, q_full;
-    float k_power[2], v_power[2];          // 2^E of a tile's keys; F of its values
-    uint32_t hidden[2][kUnpackWarps];      // keys of a tile whose page is not in the pool, a bit each
+    uint64_t k_full, k_empty, v_full, v_empty, k_info[4], q_full;   // (k_info runs ahead of the rows with the keys)
+    uint64_t s_full[2], p_full[2], pv_done[2];                      // of the halves
+    float k_power[4], v_power;             // 2^E of a tile's keys; F of its values
+    uint32_t hidden[4][kUnpackWarps];      // keys of a tile whose page is not in the pool, a bit each
     uint32_t red[2][2][kUnpackWarps];      // largest key and value of a tile, by warp
+    alignas(16) uint32_t meta[kTile];      // scale and offset of a tile's values, as halves
     uint32_t tmem;
     volatile int gave_up;
 };
 
 template <int D>
 struct PromptSmem {
-    static constexpr int kQ = kTile * D * 2, kK = kTile * D * 2, kV = kTile * D * 2, kP = kTile * kTile * 2;
-    static constexpr int q = 0, k = kQ, v = k + 2 * kK, p = v + 2 * kV, ctl = p + kP;
+    static constexpr int kQ = kTile * D * 2, kP = kTile * kTile * 2;   // of a half
+    static constexpr int q = 0, k = 2 * kQ, v = k + kTile * D * 2, p = v + kTile * D * 2, ctl = p + 2 * kP;
     static constexpr int bytes = 1024 /* alignment */ + ctl + (int)sizeof(PromptCtl);
 };
 
@@ -132,6 +135,24 @@ __device__ __forceinline__ void settle(uint32_t *v) {
                       "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
 }
 
+// two floats in one register pair, and the operations that take both at once
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return reinterpret_cast<const uint32_t &>(h);
@@ -176,7 +197,7 @@ __device__ __forceinline__ int tile_power(float most, uint32_t *red, int uw, int
 // One tile of query rows as every role walks them: request by request, heads, row tiles from the last (most keys) to the first.
 struct Item {
     int row, len, queries, first_token, head, row0, rows;   // rows: of the request and head
-    int first_key, tiles;                                   // tiles of 128 keys from first_key on
+    int first_key, tiles[2];                                // tiles of 128 keys from first_key on that a half sees; the second sees more
 };
 
 struct ItemWalk {
@@ -192,7 +213,7 @@ __device__ __forceinline__ bool next_item(const AttendParams &p, ItemWalk &w, It
         x.row = p.row_idx ? p.row_idx[i] : i;
         if (x.row < 0 || x.row >= p.rows || x.first_token < 0 || x.queries < 0 || x.queries > p.max_tokens - x.first_token) x.queries = 0;
         x.rows = x.queries * p.group;
-        const int row_tiles = (int)(((long long)x.rows + kTile - 1) / kTile);
+        const int row_tiles = (int)(((long long)x.rows + kRows - 1) / kRows);
         const long long here = (long long)row_tiles * p.kv_heads;
         if (w.item >= w.start + here) {
             w.start += here;
@@ -200,19 +221,26 @@ __device__ __forceinline__ bool next_item(const AttendParams &p, ItemWalk &w, It
         }
         const int in_request = (int)(w.item - w.start);
         x.head = in_request / row_tiles;
-        x.row0 = (row_tiles - 1 - (in_request - x.head * row_tiles)) * kTile;
+        x.row0 = (row_tiles - 1 - (in_request - x.head * row_tiles)) * kRows;
         const long long most = (long long)p.max_blocks << p.page_shift;
         x.len = p.lens[x.row];
         if (x.len > most) x.len = (int)most;
         if (x.len < 0) x.len = 0;
-        const int first = x.len - x.queries + x.row0 / p.group, last = x.len - x.queries + (min(x.row0 + kTile, x.rows) - 1) / p.group;
+        const int before = x.len - x.queries, first = before + x.row0 / p.group;
         x.first_key = p.window > 0 ? max(max(first, 0) - p.window + 1, 0) / kTile * kTile : 0;
-        x.tiles = last < 0 ? 0 : (last + 1 - x.first_key + kTile - 1) / kTile;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row0 = x.row0 + h * kTile, last = before + (min(row0 + kTile, x.rows) - 1) / p.group;
+            x.tiles[h] = row0 >= x.rows || last < 0 ? 0 : (last + 1 - x.first_key + kTile - 1) / kTile;
+        }
         w.item += gridDim.x;
         return true;
     }
     return false;
 }
+
+// tiles that are unpacked for an item
+__device__ __forceinline__ int tiles_of(const Item &x) { return max(x.tiles[0], x.tiles[1]); }
 
 template <int D>
 __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(const __grid_constant__ AttendParams p) {
@@ -223,22 +251,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
     PromptCtl *const ctl = reinterpret_cast<PromptCtl *>(smem + S::ctl);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
-            bar_init(&ctl->k_full[i], kUnpackWarps * 32);
-            bar_init(&ctl->k_empty[i], 1);
-            bar_init(&ctl->v_full[i], kUnpackWarps * 32);
-            bar_init(&ctl->v_empty[i], 1);
-            bar_init(&ctl->s_full[i], 1);
-            bar_init(&ctl->s_free[i], kSoftmaxWarps * 32);
-        }
-        bar_init(&ctl->p_full, kSoftmaxWarps * 32);
-        bar_init(&ctl->pv_done, 1);
+        bar_init(&ctl->k_full, kUnpackWarps * 32);
+        bar_init(&ctl->k_empty, 1);
+        bar_init(&ctl->v_full, kUnpackWarps * 32);
+        bar_init(&ctl->v_empty, 1);
+        for (int i = 0; i < 4; ++i) bar_init(&ctl->k_info[i], kUnpackWarps);
         bar_init(&ctl->q_full, kSoftmaxWarps * 32);
+        for (int h = 0; h < 2; ++h) {
+            bar_init(&ctl->s_full[h], 1);
+            bar_init(&ctl->p_full[h], kSoftmaxWarps * 16);
+            bar_init(&ctl->pv_done[h], 1);
+        }
         ctl->gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
     }
-    if (warp == kProductWarp) {
+    if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -249,22 +277,26 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
     ItemWalk walk = {(long long)blockIdx.x, 0, 0, p.batch_max};
     if (p.batch_count) walk.n = min(max(*p.batch_count, 0), p.batch_max);
     Item x;
-    uint32_t tiles_before = 0;             // of the items before: stages, buffers and parities follow from it
+    uint32_t tiles_before = 0;             // of the items before: parities follow from it
 
     if (warp < kSoftmaxWarps) {
         // ---- a thread per query row ----
-        uint32_t items_before = 0;
+        const int my_row = tid & (kTile - 1), half = tid >> 7;
+        const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t s_at = lanes_at + half * kTile, o_at = lanes_at + 2 * kTile + half * kTile;
+        uint32_t steps = 0;                                   // tiles of this half so far
         while (next_item(p, walk, x)) {
-            const int row = x.row0 + tid;
+            const int all = tiles_of(x), mine = x.tiles[half], row0 = x.row0 + half * kTile;
+            const int row = row0 + my_row;
             const bool real = row < x.rows;
             const int shown = real ? row : x.rows - 1;        // rows past the last see what it sees; they are never stored
             const int j = shown / p.group, qh = x.head * p.group + shown - j * p.group;
             const int pos = x.len - x.queries + j;
             const int high = pos + 1, low = p.window > 0 ? max(pos, 0) - p.window + 1 : 0;
-            const int first = x.len - x.queries + x.row0 / p.group, last = x.len - x.queries + (min(x.row0 + kTile, x.rows) - 1) / p.group;
+            const int first = x.len - x.queries + row0 / p.group, last = x.len - x.queries + (min(row0 + kTile, x.rows) - 1) / p.group;
             const int all_high = first + 1, all_low = p.window > 0 ? max(last, 0) - p.window + 1 : 0;
             float c = 0.f;
-            if (x.tiles > 0) {
+            if (all > 0) {
                 // ---- the row's query as halves, its largest value at 2^14 .. 2^15 (exact for bf16), in the order of the codes ----
                 const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
                                                                  (long long)(x.first_token + j) * p.q_ts + (long long)qh * p.q_hs);
@@ -302,7 +334,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 for (int i = 0; i < D / 8; ++i) {
                     float v[8];
                     words(i, v);
-                    *reinterpret_cast<uint4 *>(smem + S::q + (i >> 3) * PANEL + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
+                    *reinterpret_cast<uint4 *>(smem + S::q + half * S::kQ + (i >> 3) * PANEL + my_row * 128 + (((i & 7) ^ (my_row & 7)) << 4)) =
                         make_uint4(half2_bits(v[0] * f, v[4] * f), half2_bits(v[1] * f, v[5] * f), half2_bits(v[2] * f, v[6] * f),
                                    half2_bits(v[3] * f, v[7] * f));
                 }
@@ -310,105 +342,104 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 bar_arrive(&ctl->q_full);
             }
             float top = kNoMax, sum = 0.f;
-            for (int t = 0; t < x.tiles; ++t) {
-                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
+            for (int t = 0; t < all; ++t) {
+                const uint32_t n = tiles_before + t;
+                bar_wait(&ctl->k_info[n & 3], (n >> 2) & 1, ctl, p.status);   // the tile's powers
+                bar_wait(&ctl->v_full, n & 1, ctl, p.status);
+                if (t >= mine) {               // a tile for the other half: nobody may run ahead of this one all the same
+                    bar_arrive(&ctl->p_full[half]);
+                    continue;
+                }
                 const int key0 = x.first_key + t * kTile;
-                bar_wait(&ctl->k_full[b], ph, ctl, p.status);      // the tile's powers
-                bar_wait(&ctl->v_full[b], ph, ctl, p.status);
-                const float ck = c * ctl->k_power[b], fv = ctl->v_power[b];
-                bar_wait(&ctl->s_full[b], ph, ctl, p.status);
-                tc_after();
-                const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16) + b * kTile;
-                const uint32_t lost = ctl->hidden[b][0] | ctl->hidden[b][1] | ctl->hidden[b][2] | ctl->hidden[b][3];
+                const float ck = c * ctl->k_power[n & 3], fv = ctl->v_power;
+                const uint32_t lost = ctl->hidden[n & 3][0] | ctl->hidden[n & 3][1] | ctl->hidden[n & 3][2] | ctl->hidden[n & 3][3];
                 const bool edge = key0 + kTile > all_high || key0 < all_low || lost != 0;
-                // 64 scores from column c0 on, hidden ones at -infinity
-                uint32_t s[64];
+                bar_wait(&ctl->s_full[half], steps & 1, ctl, p.status);
+                tc_after();
+                // 32 scores from column c0 on, hidden ones at -infinity
+                uint32_t s[32];
                 const auto read = [&](int c0) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_load(at + c0 + 16 * i, s + 16 * i);
+                    tmem_load(s_at + c0, s);
+                    tmem_load(s_at + c0 + 16, s + 16);
                     tmem_load_wait();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) settle(s + 16 * i);
+                    settle(s);
+                    settle(s + 16);
                     if (edge) {
                         const int hi = high - key0 - c0, lo = low - key0 - c0;
-                        const unsigned long long gone = lost ? (unsigned long long)ctl->hidden[b][c0 / 32 + 1] << 32 | ctl->hidden[b][c0 / 32] : 0;
+                        const uint32_t gone = ctl->hidden[n & 3][c0 >> 5];
 #pragma unroll
-                        for (int i = 0; i < 64; ++i)
+                        for (int i = 0; i < 32; ++i)
                             if (i >= hi || i < lo || ((gone >> i) & 1)) s[i] = 0xff800000u;
                     }
                 };
                 float most = -INFINITY;
 #pragma unroll 1
-                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                for (int c0 = 0; c0 < kTile; c0 += 32) {
                     read(c0);
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) most = fmaxf(fmaxf(most, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
+                    for (int i = 0; i < 32; i += 2) most = fmaxf(fmaxf(most, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
                 }
                 most = fmaf(most, ck, fv);
-                bool waited = t == 0;
+                // the products have read the weights before and added them up
+                if (t > 0) bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p.status);
                 if (__any_sync(0xffffffffu, most > top + 8.f)) {
                     const float m = fmaxf(most, top), shrink = ex2(top - m);
                     top = m;
                     sum *= shrink;
                     if (t > 0) {
-                        bar_wait(&ctl->pv_done, (n - 1) & 1, ctl, p.status);
-                        waited = true;
                         tc_after();
-                        const uint32_t o_at = tmem + ((uint32_t)(warp * 32) << 16) + 2 * kTile;
 #pragma unroll 1
                         for (int i = 0; i < D / 16; ++i) {
-                            uint32_t o[16];
-                            tmem_load(o_at + 16 * i, o);
+                            tmem_load(o_at + 16 * i, s);
                             tmem_load_wait();
-                            settle(o);
+                            settle(s);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
-                            tmem_store(o_at + 16 * i, o);
+                            for (int e = 0; e < 16; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * shrink);
+                            tmem_store(o_at + 16 * i, s);
                         }
                         tmem_store_wait();
-                        tc_before();
                     }
                 }
-                if (!waited) bar_wait(&ctl->pv_done, (n - 1) & 1, ctl, p.status);   // the products have read the weights before
-                const float shift = fv - top;
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t ck2 = pair(ck, ck), shift2 = pair(fv - top, fv - top);
+                uint64_t part[2] = {0, 0};
 #pragma unroll 1
-                for (int c0 = 0; c0 < kTile; c0 += 64) {
+                for (int c0 = 0; c0 < kTile; c0 += 32) {
                     read(c0);
+                    unsigned char *const to = smem + S::p + half * S::kP + (c0 >> 6) * PANEL + my_row * 128;
 #pragma unroll
-                    for (int i = 0; i < 64; i += 8) {
+                    for (int i = 0; i < 32; i += 8) {
                         uint32_t w[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float w0 = ex2(fmaf(__uint_as_float(s[i + 2 * e]), ck, shift)), w1 = ex2(fmaf(__uint_as_float(s[i + 2 * e + 1]), ck, shift));
-                            part[(2 * e) & 3] += w0;
-                            part[(2 * e + 1) & 3] += w1;
+                            float w0, w1;
+                            unpair(fma2(pair(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1])), ck2, shift2), w0, w1);
+                            w0 = ex2(w0);
+                            w1 = ex2(w1);
+                            part[e & 1] = add2(part[e & 1], pair(w0, w1));
                             w[e] = half2_bits(w0, w1);
                         }
-                        *reinterpret_cast<uint4 *>(smem + S::p + (c0 >> 6) * PANEL + tid * 128 + (((i >> 3) ^ (tid & 7)) << 4)) =
-                            make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(to + ((((c0 & 32) + i) >> 3 ^ (my_row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
-                tc_before();
-                bar_arrive(&ctl->s_free[b]);
-                sum = fmaf((part[0] + part[1]) + (part[2] + part[3]), ex2(-fv), sum);
                 fence_async();
                 tc_before();
-                bar_arrive(&ctl->p_full);
+                bar_arrive(&ctl->p_full[half]);
+                ++steps;
+                float a0, a1;
+                unpair(add2(part[0], part[1]), a0, a1);
+                sum = fmaf(a0 + a1, ex2(-fv), sum);
             }
-            tiles_before += x.tiles;
-            if (x.tiles > 0) {
-                bar_wait(&ctl->pv_done, (tiles_before - 1) & 1, ctl, p.status);
+            tiles_before += all;
+            if (mine > 0) {
+                bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p.status);
                 tc_after();
-                ++items_before;
             }
             const float scale = sum != 0.f ? 1.f / sum : 0.f;
             __nv_bfloat16 *const out = static_cast<__nv_bfloat16 *>(p.out) + (long long)(x.first_token + j) * p.out_ts + (long long)qh * p.out_hs;
-            const uint32_t o_at = tmem + ((uint32_t)(warp * 32) << 16) + 2 * kTile;
 #pragma unroll 1
             for (int i = 0; i < D / 16; ++i) {
                 uint32_t o[16];
-                if (x.tiles > 0) {
+                if (mine > 0) {
                     tmem_load(o_at + 16 * i, o);
                     tmem_load_wait();
                     settle(o);
@@ -434,6 +465,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
         const int u = tid - kSoftmaxWarps * 32, uw = u >> 5;
         const int mask = (1 << p.page_shift) - 1;
         while (next_item(p, walk, x)) {
+            const int all = tiles_of(x);
             const int32_t *const table = p.block_table + (long long)x.row * p.table_ld;
             const unsigned char *const k_head = p.k_codes + x.head * p.hs;
             const uint32_t *const km_head = p.k_meta + x.head * p.mhs, *const vm_head = p.v_meta + x.head * p.mhs;
@@ -441,7 +473,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             bool next_lost = false;
             const auto look_up = [&](int t) {
                 const int key = x.first_key + t * kTile + u;
-                page = t < x.tiles && key < x.len ? min((uint32_t)__ldg(table + (key >> p.page_shift)), kNone - 1) : kNone;
+                page = t < all && key < x.len ? min((uint32_t)__ldg(table + (key >> p.page_shift)), kNone - 1) : kNone;
             };
             const auto fetch = [&](int t) {
                 const int key = x.first_key + t * kTile + u;
@@ -463,39 +495,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             look_up(0);
             fetch(0);
             look_up(1);
-            for (int t = 0; t < x.tiles; ++t) {
-                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
-                uint32_t w[D / 8];
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) w[i] = next[i];
+            for (int t = 0; t < all; ++t) {
+                const uint32_t n = tiles_before + t;
                 const KeyMeta meta(next_km, next_vm);
                 const bool lost = next_lost;
                 if (lost) atomicOr(p.status, 2);
-                fetch(t + 1);
-                look_up(t + 2);
                 const float scale = meta.bad ? 0.f : meta_scale(meta.k), offset = meta.bad ? __uint_as_float(0x7fc00000u) : meta_offset(meta.k);
                 const int e = tile_power(meta.bad ? 0.f : fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][0], uw, lane, 1);
                 const float f = __uint_as_float((uint32_t)(127 - e) << 23);
                 const __half2 s2 = __float2half2_rn(scale * f), o2 = __float2half2_rn(offset * f);
-                bar_wait(&ctl->k_empty[b], ph ^ 1, ctl, p.status);
-                unsigned char *const to = smem + S::k + b * S::kK + u * 128;
+                bar_wait(&ctl->k_empty, (n & 1) ^ 1, ctl, p.status);
+                unsigned char *const to = smem + S::k + u * 128;
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) {
-                    const uint32_t w8 = w[i] >> 8;
+                    const uint32_t w = next[i], w8 = w >> 8;
                     *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) =
-                        make_uint4(value2<0>(w[i] & 0x000f000fu, s2, o2), value2<1>(w[i] & 0x00f000f0u, s2, o2),
+                        make_uint4(value2<0>(w & 0x000f000fu, s2, o2), value2<1>(w & 0x00f000f0u, s2, o2),
                                    value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
                 }
-                // the rows are done with tile n - 2, whose powers these replace: its S was needed for this stage to be empty, its
-                // weights for v_empty, which the product of tile n - 2 comes before
-                bar_wait(&ctl->v_empty[b], ph ^ 1, ctl, p.status);
+                // S of tile n - 1 is there for both halves, so both have formed the weights of n - 2: the powers of n - 4 are free
                 const uint32_t gone = __ballot_sync(0xffffffffu, lost);
-                if (lane == 0) ctl->hidden[b][uw] = gone;
-                if (u == 0) ctl->k_power[b] = __uint_as_float((uint32_t)(127 + e) << 23);
+                if (lane == 0) {
+                    ctl->hidden[n & 3][uw] = gone;
+                    if (u == 0) ctl->k_power[n & 3] = __uint_as_float((uint32_t)(127 + e) << 23);
+                    bar_arrive(&ctl->k_info[n & 3]);
+                }
                 fence_async();
-                bar_arrive(&ctl->k_full[b]);
+                bar_arrive(&ctl->k_full);
+                fetch(t + 1);          // on their way while this thread waits for a free stage
+                look_up(t + 2);
             }
-            tiles_before += x.tiles;
+            tiles_before += all;
         }
     } else if (warp < kProductWarp) {
         // ---- values, transposed: a row per dim, eight neighbouring keys are 16 bytes of it.  A thread takes D / 64 times a word
@@ -505,16 +535,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
         const int mask = (1 << p.page_shift) - 1;
         // eight lanes hold the groups of eight keys of half a tile, so that their 16-byte pieces of a row hit different banks
         const int group = (lane & 7) + 8 * (uw & 1), word0 = (lane >> 3) + 4 * (uw >> 1);
-        uint32_t *const s_meta = reinterpret_cast<uint32_t *>(smem + S::ctl + sizeof(PromptCtl));
         while (next_item(p, walk, x)) {
+            const int all = tiles_of(x);
             const int32_t *const table = p.block_table + (long long)x.row * p.table_ld;
             const unsigned char *const v_head = p.v_codes + x.head * p.hs + word0 * 4;
             const uint32_t *const km_head = p.k_meta + x.head * p.mhs, *const vm_head = p.v_meta + x.head * p.mhs;
             uint32_t page = kNone, group_page = kNone, next[NV][8], next_km = 0, next_vm = 0;   // of the thread's key, of its group
             const auto look_up = [&](int t) {
                 const int key = x.first_key + t * kTile + u, first = x.first_key + t * kTile + 8 * group;
-                page = t < x.tiles && key < x.len ? (uint32_t)__ldg(table + (key >> p.page_shift)) : kNone;
-                group_page = t < x.tiles && first < x.len ? (uint32_t)__ldg(table + (first >> p.page_shift)) : kNone;
+                page = t < all && key < x.len ? (uint32_t)__ldg(table + (key >> p.page_shift)) : kNone;
+                group_page = t < all && first < x.len ? (uint32_t)__ldg(table + (first >> p.page_shift)) : kNone;
             };
             const auto fetch = [&](int t) {
                 const int key = x.first_key + t * kTile + u, first = x.first_key + t * kTile + 8 * group;
@@ -535,24 +565,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             look_up(0);
             fetch(0);
             look_up(1);
-            for (int t = 0; t < x.tiles; ++t) {
-                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
-                uint32_t w[NV][8];
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) w[i][e] = next[i][e];
+            for (int t = 0; t < all; ++t) {
+                const uint32_t n = tiles_before + t;
                 const KeyMeta meta(next_km, next_vm);
-                fetch(t + 1);
-                look_up(t + 2);
                 const float scale = meta.bad ? 0.f : meta_scale(meta.v), offset = meta.bad ? 0.f : meta_offset(meta.v);
                 const int e = tile_power(fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][1], uw, lane, 2);
                 const float f = __uint_as_float((uint32_t)(127 - e) << 23);
-                bar_wait(&ctl->v_empty[b], ph ^ 1, ctl, p.status);
-                s_meta[b * kTile + u] = half2_bits(scale * f, offset * f);
-                if (u == 0) ctl->v_power[b] = (float)e;
+                bar_wait(&ctl->v_empty, (n & 1) ^ 1, ctl, p.status);
+                ctl->meta[u] = half2_bits(scale * f, offset * f);
+                if (u == 0) ctl->v_power = (float)e;
                 asm volatile("bar.sync 2, 128;" ::: "memory");
-                unsigned char *const to = smem + S::v + b * S::kV + (group >> 3) * (D * 128) + word0 * 1024;
+                unsigned char *const to = smem + S::v + (group >> 3) * (D * 128) + word0 * 1024;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
 #pragma unroll
@@ -560,10 +583,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                         uint32_t v[4][4];                                // pairs of keys; dims
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const uint2 m = *reinterpret_cast<const uint2 *>(s_meta + b * kTile + 8 * group + 2 * q);
+                            const uint2 m = *reinterpret_cast<const uint2 *>(ctl->meta + 8 * group + 2 * q);
                             const uint32_t sc = __byte_perm(m.x, m.y, 0x5410), of = __byte_perm(m.x, m.y, 0x7632);
                             const __half2 s2 = reinterpret_cast<const __half2 &>(sc), o2 = reinterpret_cast<const __half2 &>(of);
-                            const uint32_t c = __byte_perm(w[i][2 * q], w[i][2 * q + 1], h ? 0x7632 : 0x5410), c8 = c >> 8;
+                            const uint32_t c = __byte_perm(next[i][2 * q], next[i][2 * q + 1], h ? 0x7632 : 0x5410), c8 = c >> 8;
                             v[q][0] = value2<0>(c & 0x000f000fu, s2, o2);
                             v[q][1] = value2<1>(c & 0x00f000f0u, s2, o2);
                             v[q][2] = value2<0>(c8 & 0x000f000fu, s2, o2);
@@ -576,63 +599,86 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     }
                 }
                 fence_async();
-                bar_arrive(&ctl->v_full[b]);
+                bar_arrive(&ctl->v_full);
+                fetch(t + 1);
+                look_up(t + 2);
             }
-            tiles_before += x.tiles;
+            tiles_before += all;
         }
     } else if (lane == 0) {
         // ---- the products ----
         const uint32_t q_at = smem_at(smem + S::q), k_at = smem_at(smem + S::k), v_at = smem_at(smem + S::v), p_at = smem_at(smem + S::p);
-        uint32_t items_before = 0;
-        const auto scores = [&](uint32_t n) {
-            const uint32_t b = n & 1, ph = (n >> 1) & 1;
-            bar_wait(&ctl->k_full[b], ph, ctl, p.status);
-            bar_wait(&ctl->s_free[b], ph ^ 1, ctl, p.status);
+        uint32_t items_before = 0, steps[2] = {0, 0};         // steps: P V products of each half so far
+        // S of tile n for half h
+        const auto scores = [&](int h) {
             tc_after();
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
-                mma_f16(tmem + b * kTile, operand(q_at + (i >> 2) * PANEL) + 2 * (i & 3), operand(k_at + b * S::kK + (i >> 2) * PANEL) + 2 * (i & 3),
+                mma_f16(tmem + h * kTile, operand(q_at + h * S::kQ + (i >> 2) * PANEL) + 2 * (i & 3), operand(k_at + (i >> 2) * PANEL) + 2 * (i & 3),
                         kTile, i != 0);
-            tc_commit(&ctl->s_full[b]);
-            tc_commit(&ctl->k_empty[b]);
+            tc_commit(&ctl->s_full[h]);
         };
         while (next_item(p, walk, x)) {
-            if (x.tiles == 0) continue;
+            const int all = tiles_of(x);
+            if (all == 0) continue;
             bar_wait(&ctl->q_full, items_before & 1, ctl, p.status);
             ++items_before;
-            scores(tiles_before);
-            for (int t = 0; t < x.tiles; ++t) {
-                const uint32_t n = tiles_before + t, b = n & 1, ph = (n >> 1) & 1;
-                if (t + 1 < x.tiles) scores(n + 1);
-                bar_wait(&ctl->v_full[b], ph, ctl, p.status);
-                bar_wait(&ctl->p_full, n & 1, ctl, p.status);
-                tc_after();
+            bar_wait(&ctl->k_full, tiles_before & 1, ctl, p.status);
+            if (x.tiles[0] > 0) scores(0);
+            if (x.tiles[1] > 0) scores(1);
+            tc_commit(&ctl->k_empty);
+            for (int t = 0; t < all; ++t) {
+                const uint32_t n = tiles_before + t;
+                const bool more = t + 1 < all;
+                bar_wait(&ctl->v_full, n & 1, ctl, p.status);
+                if (more) bar_wait(&ctl->k_full, (n + 1) & 1, ctl, p.status);
+                // whichever half has its weights: its next S first, so that it goes on, then what the weights give
+                bool open[2] = {true, true};
+                for (uint32_t spins = 0; open[0] || open[1]; ++spins) {
 #pragma unroll
-                for (int i = 0; i < kTile / 16; ++i)
-                    mma_f16(tmem + 2 * kTile, operand(p_at + (i >> 2) * PANEL) + 2 * (i & 3),
-                            operand(v_at + b * S::kV + (i >> 2) * (D * 128)) + 2 * (i & 3), D, (t | i) != 0);
-                tc_commit(&ctl->pv_done);
-                tc_commit(&ctl->v_empty[b]);
+                    for (int h = 0; h < 2; ++h) {
+                        if (!open[h]) continue;
+                        // the last one open is waited for, with the limit; of two each is tried in turn, for a while
+                        if (open[h ^ 1] && spins < (1u << 24)) {
+                            if (!bar_try(&ctl->p_full[h], n & 1) && !ctl->gave_up) continue;
+                        } else {
+                            bar_wait(&ctl->p_full[h], n & 1, ctl, p.status);
+                        }
+                        open[h] = false;
+                        if (t >= x.tiles[h]) continue;
+                        if (t + 1 < x.tiles[h]) scores(h);
+                        tc_after();
+#pragma unroll
+                        for (int i = 0; i < kTile / 16; ++i)
+                            mma_f16(tmem + 2 * kTile + h * kTile, operand(p_at + h * S::kP + (i >> 2) * PANEL) + 2 * (i & 3),
+                                    operand(v_at + (i >> 2) * (D * 128)) + 2 * (i & 3), D, (t | i) != 0);
+                        tc_commit(&ctl->pv_done[h]);
+                        ++steps[h];
+                    }
+                }
+                if (more) tc_commit(&ctl->k_empty);
+                tc_commit(&ctl->v_empty);
             }
-            tiles_before += x.tiles;
+            tiles_before += all;
         }
-        // every product has been waited for by the rows, unless a wait was given up: then here
-        if (ctl->gave_up && tiles_before > 0) {
-            const long long t0 = clock64();
-            while (!bar_try(&ctl->pv_done, (tiles_before - 1) & 1) && clock64() - t0 < 200000000ll) {}
-        }
+        // every product has been waited for by the rows, unless a wait was given up: then here, before TMEM is freed
+        if (ctl->gave_up)
+            for (int h = 0; h < 2; ++h) {
+                const long long t0 = clock64();
+                while (steps[h] > 0 && !bar_try(&ctl->pv_done[h], (steps[h] - 1) & 1) && clock64() - t0 < 200000000ll) {}
+            }
     }
     __syncwarp();
     tc_before();
     __syncthreads();
-    if (warp == kProductWarp) {
+    if (warp == 0) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
 }
 
 template <int D>
-constexpr int prompt_smem() { return PromptSmem<D>::bytes + 2 * kTile * 4; }
+constexpr int prompt_smem() { return PromptSmem<D>::bytes; }
 
 }  // namespace
 
@@ -640,7 +686,7 @@ constexpr int prompt_smem() { return PromptSmem<D>::bytes + 2 * kTile * 4; }
 // keys over CTAs, this one does not.
 bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long rows) {
     if (dtype != FI_BF16 || (kv->cfg.head_dim != 64 && kv->cfg.head_dim != 128) || rows < kTile / 2) return false;
-    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kTile - 1) / kTile);
+    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kRows - 1) / kRows);
     return items >= kv->sm_count / 2;
 }
 
@@ -652,7 +698,7 @@ fi_status_t prepare_attend_prompt(const fi_kv *kv) {
 }
 
 fi_status_t launch_attend_prompt(const fi_kv *kv, const AttendParams &p, long long rows, cudaStream_t stream) {
-    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kTile - 1) / kTile);
+    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kRows - 1) / kRows);
     const int grid = items < kv->sm_count ? (int)items : kv->sm_count;
     if (kv->cfg.head_dim == 64) kv_attend_prompt_kernel<64><<<grid, kPromptThreads, prompt_smem<64>(), stream>>>(p);
     else kv_attend_prompt_kernel<128><<<grid, kPromptThreads, prompt_smem<128>(), stream>>>(p);
