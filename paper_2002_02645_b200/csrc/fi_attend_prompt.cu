@@ -29,9 +29,10 @@ constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
 constexpr int kTmemCols = 512;             // S of both halves, O of both
 
 struct PromptCtl {
-    uint64_t k_full, k_empty, v_full, v_empty, k_info[4], q_full;   // (k_info runs ahead of the rows with the keys)
+    uint64_t k_full, k_empty, v_full, v_empty, q_full;
+    uint64_t k_info[4], v_info[4];         // a tile's powers: known before its keys and values have a place
     uint64_t s_full[2], p_full[2], pv_done[2];                      // of the halves
-    float k_power[4], v_power;             // 2^E of a tile's keys; F of its values
+    float k_power[4], v_power[4];          // 2^E of a tile's keys; F of its values
     uint32_t hidden[4][kUnpackWarps];      // keys of a tile whose page is not in the pool, a bit each
     uint32_t red[2][2][kUnpackWarps];      // largest key and value of a tile, by warp
     alignas(16) uint32_t meta[kTile];      // scale and offset of a tile's values, as halves
@@ -255,7 +256,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
         bar_init(&ctl->k_empty, 1);
         bar_init(&ctl->v_full, kUnpackWarps * 32);
         bar_init(&ctl->v_empty, 1);
-        for (int i = 0; i < 4; ++i) bar_init(&ctl->k_info[i], kUnpackWarps);
+        for (int i = 0; i < 4; ++i) {
+            bar_init(&ctl->k_info[i], kUnpackWarps);
+            bar_init(&ctl->v_info[i], 1);
+        }
         bar_init(&ctl->q_full, kSoftmaxWarps * 32);
         for (int h = 0; h < 2; ++h) {
             bar_init(&ctl->s_full[h], 1);
@@ -345,13 +349,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             for (int t = 0; t < all; ++t) {
                 const uint32_t n = tiles_before + t;
                 bar_wait(&ctl->k_info[n & 3], (n >> 2) & 1, ctl, p.status);   // the tile's powers
-                bar_wait(&ctl->v_full, n & 1, ctl, p.status);
-                if (t >= mine) {               // a tile for the other half: nobody may run ahead of this one all the same
+                bar_wait(&ctl->v_info[n & 3], (n >> 2) & 1, ctl, p.status);
+                if (t >= mine) {
+                    // A tile for the other half.  It is counted through here too, and not before its values are there: two phases of
+                    // p_full completed ahead of the thread that waits for them would look like none.
+                    bar_wait(&ctl->v_full, n & 1, ctl, p.status);
                     bar_arrive(&ctl->p_full[half]);
                     continue;
                 }
                 const int key0 = x.first_key + t * kTile;
-                const float ck = c * ctl->k_power[n & 3], fv = ctl->v_power;
+                const float ck = c * ctl->k_power[n & 3], fv = ctl->v_power[n & 3];
                 const uint32_t lost = ctl->hidden[n & 3][0] | ctl->hidden[n & 3][1] | ctl->hidden[n & 3][2] | ctl->hidden[n & 3][3];
                 const bool edge = key0 + kTile > all_high || key0 < all_low || lost != 0;
                 bar_wait(&ctl->s_full[half], steps & 1, ctl, p.status);
@@ -504,6 +511,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 const int e = tile_power(meta.bad ? 0.f : fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][0], uw, lane, 1);
                 const float f = __uint_as_float((uint32_t)(127 - e) << 23);
                 const __half2 s2 = __float2half2_rn(scale * f), o2 = __float2half2_rn(offset * f);
+                // (S of tile n - 2 is there for both halves, so both have formed the weights of n - 3: the powers of n - 4 are free)
+                const uint32_t gone = __ballot_sync(0xffffffffu, lost);
+                if (lane == 0) {
+                    ctl->hidden[n & 3][uw] = gone;
+                    if (u == 0) ctl->k_power[n & 3] = __uint_as_float((uint32_t)(127 + e) << 23);
+                    bar_arrive(&ctl->k_info[n & 3]);
+                }
                 bar_wait(&ctl->k_empty, (n & 1) ^ 1, ctl, p.status);
                 unsigned char *const to = smem + S::k + u * 128;
 #pragma unroll
@@ -512,13 +526,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) =
                         make_uint4(value2<0>(w & 0x000f000fu, s2, o2), value2<1>(w & 0x00f000f0u, s2, o2),
                                    value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
-                }
-                // S of tile n - 1 is there for both halves, so both have formed the weights of n - 2: the powers of n - 4 are free
-                const uint32_t gone = __ballot_sync(0xffffffffu, lost);
-                if (lane == 0) {
-                    ctl->hidden[n & 3][uw] = gone;
-                    if (u == 0) ctl->k_power[n & 3] = __uint_as_float((uint32_t)(127 + e) << 23);
-                    bar_arrive(&ctl->k_info[n & 3]);
                 }
                 fence_async();
                 bar_arrive(&ctl->k_full);
@@ -571,9 +578,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 const float scale = meta.bad ? 0.f : meta_scale(meta.v), offset = meta.bad ? 0.f : meta_offset(meta.v);
                 const int e = tile_power(fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][1], uw, lane, 2);
                 const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+                if (u == 0) {          // (the product of tile n - 2 is done: both halves have taken the power of n - 4)
+                    ctl->v_power[n & 3] = (float)e;
+                    bar_arrive(&ctl->v_info[n & 3]);
+                }
                 bar_wait(&ctl->v_empty, (n & 1) ^ 1, ctl, p.status);
                 ctl->meta[u] = half2_bits(scale * f, offset * f);
-                if (u == 0) ctl->v_power = (float)e;
                 asm volatile("bar.sync 2, 128;" ::: "memory");
                 unsigned char *const to = smem + S::v + (group >> 3) * (D * 128) + word0 * 1024;
 #pragma unroll
