@@ -5,9 +5,12 @@
 // per half, a thread per row, turn S into the weights P; and one thread of a warp of its own issues the products
 //   S = Q K^T  (128 x 128, fp32 in TMEM)      O += P V  (128 x head_dim, fp32 in TMEM)
 // for each half.  The halves take turns: while one forms weights the other's products run.  All meet at mbarriers.
-//   Every role's loop is short (S is read from TMEM twice, 32 columns at a time, rather than held).  One half alone with all of
-// it unrolled spent a third of its warps' time waiting for instructions and took PLAIN us on two chunks of 1,024 queries of 32
-// heads behind 8,192 keys; products issued by a thread that forms weights hold it up by 2,000 cycles per tile.
+//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 384 us, 635 TFLOP/s.  With one half only and everything
+// unrolled it was 680 us, a third of the warps' time spent waiting for instructions; so every role's loop is short, and S is
+// read from TMEM twice, 32 columns at a time, rather than held.  Products issued by a thread that forms weights hold it up by
+// 2,000 cycles per tile.  Waiting for a tile's values, rather than only for their power, before forming its weights cost
+// another 170 us.  What bounds it now: the exponentials (16 per cycle and SM: 2,048 cycles of about 5,700 per 256 x 128 tile),
+// the operands in shared memory (3,072 cycles of reads and writes), and 256 such items on 148 SMs.
 //
 // Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
 // rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
@@ -692,12 +695,22 @@ constexpr int prompt_smem() { return PromptSmem<D>::bytes; }
 
 }  // namespace
 
-// Tiles of 128 rows pay from half a tile on, and when there are enough of them for half the SMs: the kernel for few rows cuts long
-// keys over CTAs, this one does not.
+// Which kernel.  The one for few rows takes its time by tiles of 16 rows, however they are spread: it cuts long keys over CTAs.  This
+// one takes its time by rounds of CTAs, whose keys are not cut.  Both grow with the keys, so the choice does not need their number:
+// measured (bf16, head_dim 128, 4 heads to a key head, 8,192 keys) a tile of 16 rows costs as much as 1/500 to 1/600 of a round of
+// 148 CTAs.  16 requests x 8 key heads x 64 rows: 185 us there, 167 us here; 32 rows: 79 and 167; one request of 2,048 rows: 333 and
+// 204; 512 rows: 94 and 200.  Short keys leave the other kernel waiting for its starts and joins: at 512 keys and 256 rows of
+// one request it takes 37 us, this one 28; at 128 rows 20 and 21.
 bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long rows) {
-    if (dtype != FI_BF16 || (kv->cfg.head_dim != 64 && kv->cfg.head_dim != 128) || rows < kTile / 2) return false;
-    const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kRows - 1) / kRows);
-    return items >= kv->sm_count / 2;
+    if (dtype != FI_BF16 || (kv->cfg.head_dim != 64 && kv->cfg.head_dim != 128)) return false;
+    // Keys rounded to halves put a score off by about 2^-12 of its parts; among many keys that averages out of the softmax sum, among
+    // a few it would be seen in the logarithm of it, so that is left to the other kernel.
+    const long long most_keys = (long long)p.max_blocks << p.page_shift;
+    if (p.lse && most_keys < 1024) return false;
+    const double heads = (double)p.batch_max * kv->cfg.kv_heads;
+    const double tiles = heads * (double)((rows + 15) / 16), items = heads * (double)((rows + kRows - 1) / kRows);
+    if (tiles > 3.5 * kv->sm_count * (double)(long long)((items + kv->sm_count - 1) / kv->sm_count)) return true;
+    return rows >= 256 && most_keys <= 1024;
 }
 
 fi_status_t prepare_attend_prompt(const fi_kv *kv) {

@@ -387,13 +387,13 @@ class Attention:
     """A filled store, queries and the formula in 64 bits."""
 
     def __init__(self, *, lens, queries, q_heads, kv_heads, dim, page=16, dtype=torch.bfloat16, order="head", window=0, size=1.0,
-                 rows=None, seed=0, tail=None):
+                 rows=None, seed=0, room=0):
         rng = np.random.default_rng(seed)
         gen = torch.Generator(device=DEV).manual_seed(seed)
         self.lens, self.queries, self.window, self.dim, self.group = lens, queries, window, dim, q_heads // kv_heads
         n = len(lens)
         self.rows = list(range(n)) if rows is None else rows
-        blocks = max(1, max(-(-x // page) for x in lens))
+        blocks = max(1, max(-(-x // page) for x in lens), room // page)      # room: keys the table has columns for
         pages = sum(-(-x // page) for x in lens) + 3
         self.kc, self.km = pools(pages, kv_heads, page, dim, order)
         self.vc, self.vm = pools(pages, kv_heads, page, dim, order)
@@ -532,7 +532,7 @@ MANY = 20000        # a hint of this many queries takes the kernel for prompts, 
 
 @pytest.mark.parametrize("name", PROMPT_CASES)
 def test_attend_prompt_kernel_matches_formula(name):
-    a = Attention(**PROMPT_CASES[name])
+    a = Attention(room=1024, **PROMPT_CASES[name])
     out, lse = a.run(max_query=MANY)
     a.check(out, lse, halves=True)
     again, _ = a.run(max_query=MANY)
@@ -542,21 +542,21 @@ def test_attend_prompt_kernel_matches_formula(name):
 
 @pytest.mark.parametrize("size,scale", [(1e-3, 1.0), (30.0, 1.0), (1e4, -1.0), (1.0, 0.0)])
 def test_attend_prompt_kernel_sizes_of_values(size, scale):
-    a = Attention(lens=[130, 700], queries=[100, 2], q_heads=4, kv_heads=2, dim=128, size=size)
+    a = Attention(lens=[130, 700], queries=[100, 2], q_heads=4, kv_heads=2, dim=128, size=size, room=1024)
     scale = scale / (size * size * 128)
     out, lse = a.run(scale=scale, max_query=MANY)
     a.check(out, lse, scale=scale, halves=True)
 
 
 def test_attend_prompt_kernel_hidden_nan_and_bad_pages():
-    a = Attention(lens=[300], queries=[40], q_heads=4, kv_heads=2, dim=128)
+    a = Attention(lens=[300], queries=[40], q_heads=4, kv_heads=2, dim=128, room=1024)
     whole, _ = a.run(max_query=MANY)
     page = a.table[0, 280 // a.page].long()
     a.vm[page, 0, 280 % a.page, 1] = math.nan                    # queries 0 .. 19 stand before it
     out, lse = a.run(max_query=MANY)
     assert torch.equal(out[:20], whole[:20]) and out[20:40, :2].isnan().all() and torch.equal(out[20:40, 2:], whole[20:40, 2:])
     a.kv.poll_status()
-    b = Attention(lens=[300], queries=[40], q_heads=4, kv_heads=2, dim=128)
+    b = Attention(lens=[300], queries=[40], q_heads=4, kv_heads=2, dim=128, room=1024)
     b.table[0, 3] = -1                                           # 16 keys hidden
     hidden = b.run(max_query=MANY)
     with pytest.raises(fb.FiError):
