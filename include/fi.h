@@ -490,7 +490,7 @@ int64_t fi_head_norm_rope_workspace(int32_t head_dim);
  * and values (bytes for codes, multiples of 16; pairs for meta; the strides of a page and of page_size tokens below 2^31, and the pages
  * of a pool within 64 GiB of codes and 16 GiB of meta).
  * fi_kv_create keeps geometry and pointers and owns the scratch of fi_kv_attend (partial results of requests whose keys
- * are cut over several CTAs: 32 KiB to 256 KiB per CTA slot, at most 8 CTAs per SM) and a status word.
+ * are cut over several CTAs) and a status word.
  */
 typedef struct fi_kv fi_kv_t;
 

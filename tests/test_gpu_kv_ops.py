@@ -351,6 +351,33 @@ def test_append_stores_the_defined_codes(tokens, heads, dim, page, order, dtype)
         assert (codes.transpose(1, 2)[~touched] == 0xA5).all() and (meta.transpose(1, 2)[~touched] == 0).all()
 
 
+def test_append_decides_ties_and_extreme_scales_as_division_does():
+    """Values half-way between two codes (k + 1/2 scales above the least), one float32 to either side of it, and scales from
+    2^-40 to 2^120: the code is round-to-even of the correctly rounded quotient."""
+    rng = np.random.default_rng(8)
+    rows = []
+    for e in (-45, -38, -20, -3, 0, 7, 60, 105, 120):
+        for _ in range(40):
+            scale = np.float32((128 + rng.integers(0, 128)) * 2.0 ** (e - 7))
+            x = (rng.integers(0, 15, 64) + 0.5) * np.float64(scale)
+            x = x.astype(np.float32)
+            x = np.where(rng.random(64) < 0.3, np.nextafter(x, np.float32(np.inf)), x)
+            x = np.where(rng.random(64) < 0.2, np.nextafter(x, np.float32(-np.inf)), x)
+            x[0], x[1] = 0.0, np.float32(15.0 * np.float64(scale))
+            rows.append(x)
+    x = np.stack(rows).astype(np.float32)[:, None]
+    n = len(rows)
+    kc, km = pools(-(-n // 16), 1, 16, 64)
+    vc, vm = pools(-(-n // 16), 1, 16, 64)
+    kv = fb.KvCache(kc, km, vc, vm, q_heads=1)
+    t = torch.tensor(x, device=DEV)
+    kv.append(t, -t, torch.arange(n, device=DEV))
+    for codes, meta, given in ((kc, km, x), (vc, vm, -x)):
+        code, scale, offset, _ = plain_pack(given)
+        assert np.array_equal(unpack(codes.view(-1, 32)[:n]).cpu().numpy(), code[:, 0])
+        assert np.array_equal(meta.view(-1, 2)[:n].float().cpu().numpy(), np.concatenate([scale, offset], -1)[:, 0])
+
+
 def test_append_vectors_without_a_range_read_as_nan_and_harm_no_other():
     kc, km = pools(2, 2, 16, 64)
     vc, vm = pools(2, 2, 16, 64)
