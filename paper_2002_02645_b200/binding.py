@@ -612,9 +612,9 @@ def _check_heads(t: torch.Tensor, name: str, index: int, dtype, tokens: int, hea
     if t.dtype is not dtype or t.get_device() != index or t.shape != (tokens, heads, head_dim):
         raise ValueError(f"{name} must be {dtype} [{tokens}, {heads}, {head_dim}] on cuda:{index}")
     token, head, value = t.stride()
-    if value != 1 and head_dim > 1:
+    if value != 1:
         raise ValueError(f"{name}: the values of a head must lie side by side")
-    return token, head
+    return token if tokens > 1 else 0, head if heads > 1 else 0     # (the stride of a single token or head may be anything)
 
 
 def _check_table(block_table: torch.Tensor, rows: int, blocks: int, index: int) -> None:
@@ -630,7 +630,7 @@ class ExtendOut:
 
     def __init__(self, batch: int, max_tokens: int, rows: int, device):
         self.slot_map = torch.empty(max_tokens, dtype=torch.int64, device=device)
-        # one block of memory for the small ones
+        # one block of memory for the small ones; positions first, which the kernel writes 16 bytes at a time
         words = torch.empty(max_tokens + 2 * batch + rows + 2, dtype=torch.int32, device=device)
         self.positions, self.cu_tokens, self.granted, self.lens, self.free_count = words.split_with_sizes(
             [max_tokens, batch + 1, batch, rows, 1])
@@ -731,19 +731,23 @@ def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interlea
     if dtype not in _FI_DTYPE or q.dim() != 3 or index < 0:
         raise ValueError("q must be a float32 or bfloat16 [tokens, heads, head_dim] tensor on a GPU")
     tokens, q_heads, dim = q.shape
-    if q_res is None:
-        q_res = q.new_empty((tokens, q_heads, dim))
     strides = _check_heads(q, "q", index, dtype, tokens, q_heads, dim)
+    if q_res is None:
+        q_res = torch.empty_like(q)
+        res_strides = q_res.stride()[:2]
+    else:
+        res_strides = _check_heads(q_res, "result for q", index, dtype, tokens, q_heads, dim)
     k_heads, k_strides, k_res_strides, dk_strides = 0, (0, 0), (0, 0), (0, 0)
     if k is not None:
         k_heads = k.size(1) if k.dim() == 3 else 0
         k_strides = _check_heads(k, "k", index, dtype, tokens, k_heads, dim)
         if k_res is None:
-            k_res = k.new_empty((tokens, k_heads, dim))
-        k_res_strides = _check_heads(k_res, "result for k", index, dtype, tokens, k_heads, dim)
+            k_res = torch.empty_like(k)
+            k_res_strides = k_res.stride()[:2]
+        else:
+            k_res_strides = _check_heads(k_res, "result for k", index, dtype, tokens, k_heads, dim)
     else:
         k_res = None
-    res_strides = _check_heads(q_res, "result for q", index, dtype, tokens, q_heads, dim)
     dq_strides = (0, 0)
     if dq_out is not None:
         dq_strides = _check_heads(dq_out, "dq_out", index, dtype, tokens, q_heads, dim)
@@ -891,8 +895,10 @@ class KvCache:
         _check_flat(batch_count, "batch_count", index, 1)
         _check_flat(cu_tokens, "cu_tokens", index, batch + 1)
         if out is None:
-            out = q.new_empty((tokens, heads, dim))
-        out_token, out_head = _check_heads(out, "out", index, dtype, tokens, heads, dim)
+            out = torch.empty_like(q)
+            out_token, out_head, _ = out.stride()
+        else:
+            out_token, out_head = _check_heads(out, "out", index, dtype, tokens, heads, dim)
         if lse is not None:
             _check_flat(lse, "lse", index, tokens * heads, torch.float32)
         elif with_lse:
