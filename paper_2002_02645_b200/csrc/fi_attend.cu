@@ -250,6 +250,10 @@ constexpr int attend_smem() {
 // (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
+// With 8 heads of 128 over 262,143 keys of one request: 73 us, 3.9 TB/s of codes; 64 requests of 100 to 8,192 keys: 86 us.
+// What bounds it: the loop itself would take 7 TB/s (its integer and special-function instructions about as long as its bytes);
+// the start of a CTA (lengths, pages, queries, first codes: four trips to memory, 6 us) and of each further piece of a request come
+// on top of it, and overlap with the other CTAs of the SM only in part.
 template <int D, int NT, bool F32>
 __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kernel(const AttendParams p) {
     constexpr int ROWS = 8 * NT;
@@ -274,13 +278,13 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     // ---- this CTA's share ----
     int n = p.batch_max;
     if (p.batch_count) n = min(max(*p.batch_count, 0), p.batch_max);
-    const int per_thread = (n + kThreads - 1) / kThreads;
+    const int per_thread = (p.batch_max + kThreads - 1) / kThreads;
     long long mine = 0;
     for (int e = 0; e < per_thread; ++e) {
         const int i = tid * per_thread + e;
-        if (i < n) {
+        if (i < p.batch_max) {      // all entries are read, so that their loads need not wait for the count
             const Request r = request_of<ROWS, UNIT>(p, i);
-            if (r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
+            if (i < n && r.queries > 0) mine += (long long)r.units * r.row_tiles * p.kv_heads;
         }
     }
     long long before = mine;
@@ -300,8 +304,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
     }
     before -= mine;
     if (total == 0) return;
-    long long ctas = mul_div(total, 1, p.min_units);
-    ctas = ctas < 1 ? 1 : ctas > gridDim.x ? gridDim.x : ctas;
+    const long long ctas = total < gridDim.x ? total : gridDim.x;
     if (blockIdx.x >= ctas) return;
     Walk walk;
     walk.u = mul_div(total, blockIdx.x, ctas);
@@ -724,6 +727,20 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         float *const part = p.partial + slot * slot_floats<D, NT>();
         constexpr int PER = D / 16;      // dims per thread: 16 threads to a row
         const int my_row = tid >> 4, my_dim = (tid & 15) * 4;
+        const auto store_row = [&](int row, float m, float l, float b, float (&acc)[PER]) {
+            const int abs_row = row0 + row;
+            if (abs_row >= total_rows) return;
+            const int j = abs_row / p.group, qh = head * p.group + abs_row - j * p.group;
+            const float scale = l != 0.f ? 1.f / l : 0.f;
+            const long long token = r.first_token + j;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) acc[i] = l != 0.f ? (acc[i] + b) * scale : 0.f;
+#pragma unroll
+            for (int i = 0; i < PER / 4; ++i)
+                store_out<F32>(p.out, token * p.out_ts + (long long)qh * p.out_hs + my_dim + 64 * i, acc + 4 * i, 4);
+            if (p.lse && (tid & 15) == 0)
+                p.lse[token * (p.kv_heads * p.group) + qh] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+        };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (nt > 0) __syncthreads();
@@ -756,19 +773,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 }
             }
             if (complete) {
-                const int abs_row = row0 + row;
-                if (abs_row < total_rows) {
-                    const int j = abs_row / p.group, qh = head * p.group + abs_row - j * p.group;
-                    const float scale = l != 0.f ? 1.f / l : 0.f;
-                    const long long token = r.first_token + j;
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) acc[i] = l != 0.f ? (acc[i] + b) * scale : 0.f;
-#pragma unroll
-                    for (int i = 0; i < PER / 4; ++i)
-                        store_out<F32>(p.out, token * p.out_ts + (long long)qh * p.out_hs + my_dim + 64 * i, acc + 4 * i, 4);
-                    if (p.lse && (tid & 15) == 0)
-                        p.lse[token * (p.kv_heads * p.group) + qh] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-                }
+                store_row(row, m, l, b, acc);
             } else {
                 float *const d = part + row * LD;
 #pragma unroll
@@ -784,45 +789,42 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
             __syncthreads();
             if (tid == 0) {
                 s_last = atomicAdd(p.tickets + c0, 1u) == (uint32_t)(c1 - c0);
-                if (s_last) p.tickets[c0] = 0;
                 __threadfence();
+                if (s_last) p.tickets[c0] = 0;
             }
             __syncthreads();
             if (s_last) {
                 // the item opens the share of every CTA but the first, and of that one when the share begins with it
                 const int first_slot = mul_div(total, c0, ctas) == item_begin ? 0 : 1;
+                constexpr long long APART = 2 * slot_floats<D, NT>();
+                const int parts = c1 - c0 + 1;
+                const float *const at = p.partial + c0 * APART + my_row * LD, *const at0 = at + first_slot * slot_floats<D, NT>();
+                // rows 2 warp, 2 warp + 1 of how many tiles of 8 are there at all
+                const int tiles = min(NT, (total_rows - row0 - 2 * warp + 7) >> 3);
+                constexpr int FEW = D <= 128 ? 8 : 4;
+                // Few parts of several tiles are all loaded at once and added up by every thread for itself, which saves the
+                // exchange of weights for each tile.  (16 requests of 5 queries, 25 rows a head, up to 6 parts: the call takes 25.3 us
+                // so and 26.9 in the other way; 64 requests of 4 rows a head, mostly 2 or 3 parts: 86.2 and 84.7.)
+                if (NT > 1 && parts <= FEW) {
 #pragma unroll 1
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int row = nt * 8 + my_row, abs_row = row0 + row;
-                    if (abs_row >= total_rows) continue;
-                    float m = kNoMax, l = 0.f, b = 0.f, acc[PER];
+                    for (int nt = 0; nt < tiles; ++nt) {
+                        float4 st[FEW], v[FEW][PER / 4];
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) acc[i] = 0.f;
-                    constexpr int BATCH = D <= 128 ? 8 : 4;      // parts whose loads are on the way together
-#pragma unroll 1
-                    for (int k0 = c0; k0 <= c1; k0 += BATCH) {
-                        float4 st[BATCH], v[BATCH][PER / 4];
-#pragma unroll
-                        for (int e = 0; e < BATCH; ++e) {
-                            const int k = min(k0 + e, c1);
-                            const float *const d = p.partial + (2 * (long long)k + (k == c0 ? first_slot : 0)) * slot_floats<D, NT>() + row * LD;
+                        for (int e = 0; e < FEW; ++e) {
+                            const int k = min(e, parts - 1);
+                            const float *const d = (k ? at + k * APART : at0) + nt * 8 * LD;
                             st[e] = __ldcg(reinterpret_cast<const float4 *>(d + D));
 #pragma unroll
                             for (int i = 0; i < PER / 4; ++i) v[e][i] = __ldcg(reinterpret_cast<const float4 *>(d + my_dim + 64 * i));
                         }
-                        float m2 = m;
+                        float m = kNoMax, l = 0.f, b = 0.f, acc[PER];
 #pragma unroll
-                        for (int e = 0; e < BATCH; ++e)
-                            m2 = fmaxf(m2, st[e].x);
-                        const float f = ex2(m - m2);
-                        m = m2;
-                        l *= f;
-                        b *= f;
+                        for (int i = 0; i < PER; ++i) acc[i] = 0.f;
 #pragma unroll
-                        for (int i = 0; i < PER; ++i) acc[i] *= f;
+                        for (int e = 0; e < FEW; ++e) m = fmaxf(m, st[e].x);
 #pragma unroll
-                        for (int e = 0; e < BATCH; ++e) {
-                            const float w = k0 + e <= c1 ? ex2(st[e].x - m) : 0.f;   // (the last part stands in past the end)
+                        for (int e = 0; e < FEW; ++e) {
+                            const float w = e < parts ? ex2(st[e].x - m) : 0.f;   // (the last part stands in past the end)
                             l = fmaf(st[e].y, w, l);
                             b = fmaf(st[e].z, w, b);
 #pragma unroll
@@ -833,17 +835,108 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                                 acc[4 * i + 3] = fmaf(v[e][i].w, w, acc[4 * i + 3]);
                             }
                         }
+                        store_row(nt * 8 + my_row, m, l, b, acc);
                     }
-                    const int j = abs_row / p.group, qh = head * p.group + abs_row - j * p.group;
-                    const float scale = l != 0.f ? 1.f / l : 0.f;
-                    const long long token = r.first_token + j;
+                } else {
+                    // One warp per scheduler is all that works here, so what counts is the number of instructions in a row.  The
+                    // 16 threads of a row work out the weights of 32 parts at a time, two each; the parts themselves come through
+                    // the rings, each thread fetching what it adds up, FLIGHT groups of 4 on their way.  (All 56 parts of 262,143 keys
+                    // took 14,000 cycles with 8 at a time through registers, and take 9,500.)
+                    constexpr int GROUP = 4, CHUNK = 32, ROOM = ring_bytes<D, NT>() / (GROUP * kThreads * PER * 4);
+                    constexpr int FLIGHT = ROOM < 4 ? ROOM : 4;
+                    static_assert(FLIGHT >= 1 && NT * KS * 32 * 8 >= 8 * CHUNK * 4, "");
+                    const int t = tid & 15;
+                    float *const s_w = reinterpret_cast<float *>(s_q) + my_row * CHUNK;     // the queries have been used
+                    const uint32_t ring_first = smem_at(smem) + tid * 16;
+                    float4 st[2];
+                    const auto look = [&](int nt, int base) {
 #pragma unroll
-                    for (int i = 0; i < PER; ++i) acc[i] = l != 0.f ? (acc[i] + b) * scale : 0.f;
+                        for (int i = 0; i < 2; ++i) {
+                            const int k = base + t + 16 * i;
+                            st[i] = make_float4(kNoMax, 0.f, 0.f, 0.f);
+                            if (k < parts && nt < tiles)
+                                st[i] = __ldcg(reinterpret_cast<const float4 *>((k ? at + k * APART : at0) + nt * 8 * LD + D));
+                        }
+                    };
+                    look(0, 0);
+                    int sent = 0, sent_nt = 0;
+                    uint32_t to = ring_first;
+                    const float *src = at0 + my_dim, *next = at + my_dim;
+                    const auto bring = [&] {
+                        if (sent_nt < tiles) {
 #pragma unroll
-                    for (int i = 0; i < PER / 4; ++i)
-                        store_out<F32>(p.out, token * p.out_ts + (long long)qh * p.out_hs + my_dim + 64 * i, acc + 4 * i, 4);
-                    if (p.lse && (tid & 15) == 0)
-                        p.lse[token * (p.kv_heads * p.group) + qh] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                            for (int e = 0; e < GROUP; ++e) {
+#pragma unroll
+                                for (int i = 0; i < PER / 4; ++i)
+                                    async_copy<16>(to + (e * (PER / 4) + i) * kThreads * 16, src + 64 * i);
+                                if (++sent < parts) src = next += APART;    // (the last part again, past the end)
+                            }
+                            if (sent >= parts) {
+                                ++sent_nt;
+                                sent = 0;
+                                next = at + my_dim + sent_nt * 8 * LD;
+                                src = at0 + my_dim + sent_nt * 8 * LD;
+                            }
+                        }
+                        async_commit();
+                        to = to == ring_first + (FLIGHT - 1) * GROUP * kThreads * PER * 4 ? ring_first : to + GROUP * kThreads * PER * 4;
+                    };
+#pragma unroll 1
+                    for (int i = 0; i < FLIGHT; ++i) bring();
+                    int from = 0;
+#pragma unroll 1
+                    for (int nt = 0; nt < tiles; ++nt) {
+                        const int row = nt * 8 + my_row;
+                        float m = kNoMax, l = 0.f, b = 0.f, acc[PER];
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+#pragma unroll 1
+                        for (int base = 0; base < parts; base += CHUNK) {
+                            float m2 = fmaxf(m, fmaxf(st[0].x, st[1].x));
+#pragma unroll
+                            for (int d = 1; d < 16; d <<= 1) m2 = fmaxf(m2, __shfl_xor_sync(0xffffffffu, m2, d));
+                            const float w0 = ex2(st[0].x - m2), w1 = ex2(st[1].x - m2), f = ex2(m - m2);
+                            float l2 = st[0].y * w0 + st[1].y * w1, b2 = st[0].z * w0 + st[1].z * w1;
+#pragma unroll
+                            for (int d = 1; d < 16; d <<= 1) {
+                                l2 += __shfl_xor_sync(0xffffffffu, l2, d);
+                                b2 += __shfl_xor_sync(0xffffffffu, b2, d);
+                            }
+                            m = m2;
+                            l = fmaf(l, f, l2);
+                            b = fmaf(b, f, b2);
+#pragma unroll
+                            for (int i = 0; i < PER; ++i) acc[i] *= f;
+                            __syncwarp();
+                            s_w[t] = base + t < parts ? w0 : 0.f;
+                            s_w[t + 16] = base + t + 16 < parts ? w1 : 0.f;
+                            __syncwarp();
+                            if (base + CHUNK < parts) look(nt, base + CHUNK);
+                            else look(nt + 1, 0);
+                            const int here = min(CHUNK, parts - base);
+#pragma unroll 1
+                            for (int k = 0; k < here; k += GROUP) {
+                                async_wait<FLIGHT - 1>();
+                                const float4 *const v = reinterpret_cast<const float4 *>(smem) + from * (GROUP * kThreads * PER / 4) + tid;
+                                const float4 w4 = *reinterpret_cast<const float4 *>(s_w + k);
+                                const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+                                for (int e = 0; e < GROUP; ++e)
+#pragma unroll
+                                    for (int i = 0; i < PER / 4; ++i) {
+                                        const float4 x = v[(e * (PER / 4) + i) * kThreads];
+                                        acc[4 * i] = fmaf(x.x, w[e], acc[4 * i]);
+                                        acc[4 * i + 1] = fmaf(x.y, w[e], acc[4 * i + 1]);
+                                        acc[4 * i + 2] = fmaf(x.z, w[e], acc[4 * i + 2]);
+                                        acc[4 * i + 3] = fmaf(x.w, w[e], acc[4 * i + 3]);
+                                    }
+                                bring();
+                                from = from == FLIGHT - 1 ? 0 : from + 1;
+                            }
+                        }
+                        store_row(row, m, l, b, acc);
+                    }
+                    async_wait<0>();
                 }
             }
         }
@@ -985,7 +1078,6 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.page_shift = kv->page_shift;
     p.kv_heads = c.kv_heads;
     p.group = c.q_heads / c.kv_heads;
-    p.min_units = 1;
     p.scale_log2 = a->scale * kLog2e;
     const bool f32 = a->dtype == FI_F32;
     const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;

@@ -29,7 +29,6 @@ struct AttendParams {
     long long table_ld;
     int rows, max_blocks, batch_max, max_tokens, window;
     int num_pages, page_shift, kv_heads, group;
-    int min_units;
     float scale_log2;                                 // scale * log2(e)
 };
 
