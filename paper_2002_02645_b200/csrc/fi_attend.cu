@@ -250,10 +250,10 @@ constexpr int attend_smem() {
 // (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
-// With 8 heads of 128 over 262,143 keys of one request: 73 us, 3.9 TB/s of codes; 64 requests of 100 to 8,192 keys: 86 us.
-// What bounds it: the loop itself would take 7 TB/s (its integer and special-function instructions about as long as its bytes);
-// the start of a CTA (lengths, pages, queries, first codes: four trips to memory, 6 us) and of each further piece of a request come
-// on top of it, and overlap with the other CTAs of the SM only in part.
+// 8 key heads of 128 over 262,143 keys of one request take 69 us, 4.1 TB/s; 64 requests of 800 to 8,192 keys 85.5 us.
+// What bounds it: the loop itself runs at 7 TB/s (5.5 cycles per key and SM, as long for its instructions as for its bytes); the
+// start of a CTA (2 us to the first request for codes), the SMs' unequal speeds on equal shares, the partial results and their join
+// come on top, and so does the start of each further piece, which overlaps with the other CTAs of the SM only in part.
 template <int D, int NT, bool F32>
 __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kernel(const AttendParams p) {
     constexpr int ROWS = 8 * NT;

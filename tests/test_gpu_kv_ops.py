@@ -608,6 +608,18 @@ def test_attend_strides_scale_count_and_untouched_rows(dtype):
     a.check(out, lse, scale=-0.05, q=q)
 
 
+@pytest.mark.parametrize("dim,queries,q_heads", [(64, 1, 1), (64, 3, 5), (64, 9, 3), (128, 1, 7), (128, 2, 5), (192, 3, 3), (256, 1, 8)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attend_joins_many_parts(dim, queries, q_heads, dtype):
+    """One key head over 20,001 keys: a row's result is added up from 79 or 157 parts, of tiles that rows do not fill."""
+    a = Attention(lens=[20001], queries=[queries], q_heads=q_heads, kv_heads=1, dim=dim, page=64, dtype=dtype)
+    out, lse = a.run()
+    a.check(out, lse)
+    again, _ = a.run()
+    assert torch.equal(out[:queries], again[:queries])
+    a.kv.poll_status()
+
+
 @pytest.mark.parametrize("size", [1e-3, 30.0, 1e4])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_attend_sizes_of_values(size, dtype):
