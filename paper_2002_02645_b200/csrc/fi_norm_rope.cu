@@ -13,7 +13,8 @@
 namespace fi {
 namespace {
 
-constexpr int kNormThreads = 256;
+constexpr int kNormThreads = 64;      // of the forward pass: groups share nothing, and small CTAs leave no hole when they end
+constexpr int kBackwardThreads = 256;
 constexpr int kMaxPartials = 1024;   // CTAs of a backward pass, at most
 
 // rows of one operand: (token, head) pairs
@@ -85,7 +86,8 @@ __device__ __forceinline__ void load8_again(const float *p, float *x) {
                      : "l"(p + 4 * i));
 }
 
-template <bool BF16>
+// ONCE: not to be kept in L2 in the place of what is still to be read
+template <bool BF16, bool ONCE = false>
 __device__ __forceinline__ void store8(void *base, long long elem, const float *x) {
     if constexpr (BF16) {
         uint32_t w[4];
@@ -94,7 +96,10 @@ __device__ __forceinline__ void store8(void *base, long long elem, const float *
             const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
             w[i] = reinterpret_cast<const uint32_t &>(h);
         }
-        *reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+        uint4 *p = reinterpret_cast<uint4 *>(static_cast<char *>(base) + elem * 2);
+        const uint4 v = make_uint4(w[0], w[1], w[2], w[3]);
+        if constexpr (ONCE) __stcs(p, v);
+        else *p = v;
     } else {
         float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(base) + elem);
         p[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -171,10 +176,11 @@ __device__ __forceinline__ long long actual_tokens(const NormParams &p) {
 
 // A group takes R heads of one token, of the queries or of the keys: their loads are all on the way at once, and the angles
 // and the weight are loaded once for them.  R = 4 keeps 64 bytes per thread in flight and reads the table a quarter as
-// often: 16,384 tokens of 32 + 8 heads of 128 (bf16) took 103 us with one head per group and take 68, 5.0 TB/s.  Small calls take R = 1, which has the
+// often: 16,384 tokens of 32 + 8 heads of 128 (bf16) took 103 us with one head per group and take 65.5, 5.3 TB/s (68.3 in
+// CTAs of 256 threads, where the last group to end keeps the place of the others).  Small calls take R = 1, which has the
 // shorter chain (launch_norm).
 template <int LANES, bool BF16, int R>
-__global__ void __launch_bounds__(kNormThreads, R == 1 ? 4 : 3) head_norm_rope_kernel(NormParams p) {
+__global__ void __launch_bounds__(kNormThreads, R == 1 ? 16 : 12) head_norm_rope_kernel(NormParams p) {
     const int lane = threadIdx.x & (LANES - 1);
     const unsigned q_parts = (p.q.heads + R - 1) / R, parts = q_parts + (p.k.heads + R - 1) / R;
     const unsigned item = blockIdx.x * (unsigned)(kNormThreads / LANES) + threadIdx.x / LANES;
@@ -235,7 +241,7 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
     const int lane = threadIdx.x & (LANES - 1);
     const LanePlace l = lane_place(p, lane);
     const long long rows = tokens * side.heads;
-    const long long groups = (long long)ctas * (kNormThreads / LANES);
+    const long long groups = (long long)ctas * (kBackwardThreads / LANES);
     const long long rounds = (rows + groups - 1) / groups;
     // row of a round, its token and head
     struct Row {
@@ -244,7 +250,7 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
         int head;
     };
     const auto row_of = [&](long long round) {
-        const long long row = round * groups + (long long)cta * (kNormThreads / LANES) + threadIdx.x / LANES;
+        const long long row = round * groups + (long long)cta * (kBackwardThreads / LANES) + threadIdx.x / LANES;
         Row o;
         o.active = row < rows && l.there;
         o.token = o.active ? (unsigned)row / (unsigned)side.heads : 0u;
@@ -319,16 +325,18 @@ __device__ __forceinline__ void backward_rows(const NormParams &p, const NormSid
 #pragma unroll
             for (int i = 0; i < 16; ++i) g[i] = r * (g[i] - x[i] * dot);
             const long long to = (long long)token * side.out_ts + (long long)head * side.out_hs;
-            store8<BF16>(side.out, to + l.a, g);
-            store8<BF16>(side.out, to + l.b, g + 8);
+            store8<BF16, true>(side.out, to + l.a, g);
+            store8<BF16, true>(side.out, to + l.b, g + 8);
         }
     }
 }
 
 // Each CTA leaves its sums of the weight gradients in `partial`; the groups of the CTA are added in a fixed order.
+// 8,191 tokens of 16 + 4 heads of 128 (bf16, 64 values turned) take 33 us with the sums' kernel, 3.9 TB/s.  What bounds it: 128
+// registers leave two CTAs per SM, so 32 KB of loads in flight; with three the registers spill (57 us).
 template <int LANES, bool BF16>
-__global__ void __launch_bounds__(kNormThreads, 2) head_norm_rope_backward_kernel(NormParams p) {
-    constexpr int GROUPS = kNormThreads / LANES;
+__global__ void __launch_bounds__(kBackwardThreads, 2) head_norm_rope_backward_kernel(NormParams p) {
+    constexpr int GROUPS = kBackwardThreads / LANES;
     __shared__ float s_dw[GROUPS][LANES * 16 + 1];
     const long long tokens = actual_tokens(p);
     const LanePlace l = lane_place(p, threadIdx.x & (LANES - 1));
@@ -345,7 +353,7 @@ __global__ void __launch_bounds__(kNormThreads, 2) head_norm_rope_backward_kerne
         }
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < p.head_dim; d += kNormThreads) {
+    for (int d = threadIdx.x; d < p.head_dim; d += kBackwardThreads) {
         float sum = 0.f;
 #pragma unroll 8
         for (int g = 0; g < GROUPS; ++g) sum += s_dw[g][d];
@@ -382,8 +390,8 @@ int lanes_for(int head_dim) { return head_dim <= 16 ? 1 : head_dim <= 32 ? 2 : h
 template <int LANES>
 void launch_norm(const NormParams &p, bool bf16, bool backward, unsigned grid, int sms, cudaStream_t stream) {
     if (backward) {
-        if (bf16) head_norm_rope_backward_kernel<LANES, true><<<grid, kNormThreads, 0, stream>>>(p);
-        else head_norm_rope_backward_kernel<LANES, false><<<grid, kNormThreads, 0, stream>>>(p);
+        if (bf16) head_norm_rope_backward_kernel<LANES, true><<<grid, kBackwardThreads, 0, stream>>>(p);
+        else head_norm_rope_backward_kernel<LANES, false><<<grid, kBackwardThreads, 0, stream>>>(p);
         return;
     }
     const int per_cta = kNormThreads / LANES;
@@ -391,7 +399,7 @@ void launch_norm(const NormParams &p, bool bf16, bool backward, unsigned grid, i
         const long long parts = (p.q.heads + r - 1) / r + (p.k.heads + r - 1) / r;
         return (unsigned)((p.tokens * parts + per_cta - 1) / per_cta);
     };
-    if (ctas(1) <= (unsigned)sms * 4) {     // all groups are resident at once even with a head each
+    if (ctas(1) <= (unsigned)sms * 16) {     // all groups are resident at once even with a head each
         if (bf16) head_norm_rope_kernel<LANES, true, 1><<<ctas(1), kNormThreads, 0, stream>>>(p);
         else head_norm_rope_kernel<LANES, false, 1><<<ctas(1), kNormThreads, 0, stream>>>(p);
     } else {
@@ -511,7 +519,7 @@ fi_status_t fi_head_norm_rope_backward(const fi_head_norm_rope_t *a, void *cuda_
     st = current_sms(&sms, "fi_head_norm_rope_backward");
     if (st != FI_OK) return st;
     // as many CTAs as are resident at once, dealt out to queries and keys by their numbers of rows
-    const int lanes = lanes_for(a->head_dim), per_cta = kNormThreads / lanes;
+    const int lanes = lanes_for(a->head_dim), per_cta = kBackwardThreads / lanes;
     const long long most = sms * 2 < kMaxPartials ? sms * 2 : kMaxPartials;
     const long long q_rows = a->tokens * (long long)a->q_heads, k_rows = a->tokens * (long long)a->k_heads;
     long long q_ctas = (q_rows + per_cta - 1) / per_cta, k_ctas = (k_rows + per_cta - 1) / per_cta;
