@@ -460,7 +460,7 @@ struct Values16 {
 // System/6000 processor", 1990): two operations more than the product, and no division, as long as r is a normal number.  The
 // scale has 8 significant bits, so a - q scale is exact, and no quotient lies within 2^-9 of a last place of a tie.
 // What bounds it: 16,384 tokens of 8 heads of 128 (bf16, k and v) took 58.8 us with a division per value, 37.4 with one only
-// near a tie, and take 30.2 us, 5.0 TB/s; the extremes are found on the bf16 values, two at a time, and sums and products on pairs.
+// near a tie, and take 28.7 us, 5.3 TB/s; the extremes are found on the bf16 values, two at a time, and sums and products on pairs.
 template <int D, int LANES, bool BF16>
 __device__ __forceinline__ void pack_vector(const Values16<BF16> &v, bool active, bool write, unsigned char *codes, uint32_t *meta,
                                             void *stored, long long stored_at) {
@@ -519,12 +519,15 @@ __device__ __forceinline__ void pack_vector(const Values16<BF16> &v, bool active
 }
 
 // A group of LANES lanes packs the key and the value of one token and head: two independent 32-byte (bf16) loads per lane in
-// flight, minimum and maximum by shuffles, 8 bytes of codes per lane.  One pass over the data; bound by its bytes.
+// flight, minimum and maximum by shuffles, 8 bytes of codes per lane.  One pass over the data; bound by its bytes.  Groups share
+// nothing, so CTAs are small: with 256 threads the last group to end kept the place of the others (30.2 us, not 28.7).
+constexpr int kAppendThreads = 64;
+
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256) kv_append_kernel(AppendParams a) {
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendParams a) {
     constexpr int LANES = D <= 64 ? 4 : D <= 128 ? 8 : 16;
     const int lane = threadIdx.x & (LANES - 1);
-    const long long row = ((long long)blockIdx.x * 256 + threadIdx.x) / LANES;
+    const long long row = ((long long)blockIdx.x * kAppendThreads + threadIdx.x) / LANES;
     const bool there = row < a.rows;
     const unsigned token = there ? (unsigned)row / (unsigned)a.heads : 0u;
     const int head = there ? (int)((unsigned)row - token * (unsigned)a.heads) : 0;
@@ -548,9 +551,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(AppendParams a) {
 template <int D>
 void append_dispatch(const AppendParams &p, bool bf16, cudaStream_t stream) {
     constexpr int LANES = D <= 64 ? 4 : D <= 128 ? 8 : 16;
-    const unsigned grid = (unsigned)((p.rows * LANES + 255) / 256);
-    if (bf16) kv_append_kernel<D, true><<<grid, 256, 0, stream>>>(p);
-    else kv_append_kernel<D, false><<<grid, 256, 0, stream>>>(p);
+    const unsigned grid = (unsigned)((p.rows * LANES + kAppendThreads - 1) / kAppendThreads);
+    if (bf16) kv_append_kernel<D, true><<<grid, kAppendThreads, 0, stream>>>(p);
+    else kv_append_kernel<D, false><<<grid, kAppendThreads, 0, stream>>>(p);
 }
 
 int log2_of(int v) {
