@@ -10,7 +10,7 @@
 // read from TMEM twice, 32 columns at a time, rather than held.  Products issued by a thread that forms weights hold it up by
 // 2,000 cycles per tile.  Waiting for a tile's values, rather than only for their power, before forming its weights cost
 // another 170 us.  What bounds it now: the exponentials (16 per cycle and SM: 2,048 cycles of about 5,700 per 256 x 128 tile),
-// the operands in shared memory (3,072 cycles of reads and writes), and 256 such items on 148 SMs.
+// the operands in shared memory (about 3,000 cycles of reads and writes), and 256 such items on 148 SMs.
 //
 // Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
 // rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
