@@ -13,6 +13,10 @@
 // Codes are all positive, so the product part and the offset part are larger than what they add up to.  The offset part
 // therefore takes the weights as they were rounded for the product, and float32 queries, which must not lose what the parts have in
 // common, take the codes less 7.5 (one more instruction per two codes) and offsets moved by 7.5 scales.
+// A value vector of hardly any spread (a constant one has the smallest scale there is) is all offset: its P_t is far below the
+// others' and may round to nothing, although its p_t is like theirs.  Where the offset is more than kMostlyOffset scales, the
+// offset part takes the weight as it was before the rounding: what the two parts then differ in, 2^-12 of 15 scales, is below
+// 2^-13 of the value.  Up to there a weight that rounds to nothing (2^-25) loses 2^-18 of the largest product at most.
 #include "fi_attend.cuh"
 
 namespace fi {
@@ -21,6 +25,8 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kStages = 2;                 // steps of a warp in its ring: the one it works on and the next
+constexpr float kMostlyOffset = 64.f;      // offset over scale of a value vector that is its offset more than its codes
+
 __device__ __forceinline__ float lg2(float x) {
     float y;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -523,6 +529,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 KeyFactors<NB> &my_key = *reinterpret_cast<KeyFactors<NB> *>(st.k);
                 static_assert(sizeof(KeyFactors<NB>) <= sizeof(st.k), "factors must fit");
                 __syncwarp();
+                bool flat = false;     // a value vector of the step is mostly offset
 #pragma unroll
                 for (int k = lane; k < WARP_KEYS; k += 32) {
                     const uint32_t km = st.meta[k >> 4][0][k & 15], vm = st.meta[k >> 4][1][k & 15];
@@ -537,7 +544,9 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                     }
                     my_key.f[k] = make_float4(sk, mk, lg2(sv), inv);
                     my_key.off[k] = mv * inv;
+                    flat = flat || fabsf(mv * inv) > kMostlyOffset;
                 }
+                const bool ordinary = whole && !__any_sync(0xffffffffu, flat);
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
                     uint2 q[NT], q2[NT];
@@ -560,9 +569,9 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 }
                 __syncwarp();     // the keys' factors are there
                 uint32_t pb[NB][NT][2], pb2[NB][NT][2];
-                // whole: every row of the tile sees all keys of the step
-                auto weights = [&](auto whole_) {
-                    constexpr bool WHOLE = decltype(whole_)::value;
+                // ordinary: every row of the tile sees all keys of the step, and no value vector is mostly offset
+                auto weights = [&](auto ordinary_) {
+                    constexpr bool ORDINARY = decltype(ordinary_)::value;
                     float inv[NB][2];
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
@@ -576,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                                 for (int h = 0; h < 2; ++h) {
                                     float &x = s[b][nt][2 * e + h];
                                     x = fmaf(x * cq[nt][h], f.x, fmaf(f.y, sq[nt][h], f.z));
-                                    if constexpr (!WHOLE) {
+                                    if constexpr (!ORDINARY) {
                                         const int t = tok + 16 * b + 8 * e + g;
                                         if (t >= high[nt][h] || t < low[nt][h] || !((valid >> b) & 1)) x = -INFINITY;
                                     }
@@ -632,18 +641,21 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                                 w.x += w2.x;
                                 w.y += w2.y;
                             }
+                            if constexpr (!ORDINARY) {
+                                if (fabsf(offv) > kMostlyOffset) w = make_float2(w0, w1);
+                            }
                             // a hidden key adds nothing, even when its scale or offset is no number
-                            if (WHOLE || !(x0 == -INFINITY)) {
+                            if (ORDINARY || !(x0 == -INFINITY)) {
                                 sum[nt][0] = fmaf(w0, inv[b][e], sum[nt][0]);
                                 off[nt][0] = fmaf(w.x, offv, off[nt][0]);
                             }
-                            if (WHOLE || !(x1 == -INFINITY)) {
+                            if (ORDINARY || !(x1 == -INFINITY)) {
                                 sum[nt][1] = fmaf(w1, inv[b][e], sum[nt][1]);
                                 off[nt][1] = fmaf(w.y, offv, off[nt][1]);
                             }
                         }
             };
-                if (whole) weights(Bool<true>{});
+                if (ordinary) weights(Bool<true>{});
                 else weights(Bool<false>{});
 
                 // ---- O^T += V^T P^T, two blocks at a time: lane (g, c) holds the g-th eighth of keys 2c, 2c + 1, 2c + 8, 2c + 9 of each ----
