@@ -3,8 +3,11 @@
 // With k = n s_k + m_k and v = n' s_v + m_v (codes n, n' in 0..15; one scale and offset per token and key head)
 //   x_t = scale log2(e) (s_k (q . n) + m_k sum(q)),   out = sum_t p_t (s_v n' + m_v) / sum_t p_t,   p_t = 2^(x_t - max)
 // so scales and offsets never touch the codes: the products run on the codes themselves, and the offset of v is one
-// sum per query row.  The scale of v goes into the exponent: with y_t = x_t + log2(s_v) and M >= max y - 8, the weight
-// P_t = 2^(y_t - M) multiplies n' directly, sum p_t = sum P_t / s_v and the offset's part is sum P_t m_v / s_v.
+// sum per query row.  The scale of v goes into the exponent: with y_t = x_t + log2(s_v) and M = max y - 7 as it was when a y last
+// went over M + 15, the weight P_t = 2^(y_t - M) multiplies n' directly, sum p_t = sum P_t / s_v and the offset's part is
+// sum P_t m_v / s_v.  So the largest weight is between 2^7 and 2^15 as a half, whose last place is 2^-24 for all weights below
+// 2^-14: a weight is off by 2^-12 of itself or 2^-32 of the largest (float32 queries, with two halves: 2^-22 or 2^-32).  With weights up
+// to 1 instead, 32,763 float32 weights 8 nats below the largest were off by 2^-12 of themselves.
 //
 // A code is a half-precision number without any conversion: a 16-bit word that holds only the four bits n is the
 // subnormal n 2^-24 (n 2^-20 when it sits in the next four bits), which the tensor cores multiply exactly.  Eight codes
@@ -16,7 +19,7 @@
 // A value vector of hardly any spread (a constant one has the smallest scale there is) is all offset: its P_t is far below the
 // others' and may round to nothing, although its p_t is like theirs.  Where the offset is more than kMostlyOffset scales, the
 // offset part takes the weight as it was before the rounding: what the two parts then differ in, 2^-12 of 15 scales, is below
-// 2^-13 of the value.  Up to there a weight that rounds to nothing (2^-25) loses 2^-18 of the largest product at most.
+// 2^-13 of the value.  Up to there a weight that rounds to nothing loses 2^-25 of the largest product at most.
 #include "fi_attend.cuh"
 
 namespace fi {
@@ -484,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         __syncthreads();
 
         float o[KS][NT][4];
-        float top[NT][2], sum[NT][2], off[NT][2];
+        float top[NT][2], sum[NT][2], lost[NT][2], off[NT][2];
 #pragma unroll
         for (int i = 0; i < KS; ++i)
 #pragma unroll
@@ -496,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 top[nt][h] = kNoMax;
-                sum[nt][h] = off[nt][h] = 0.f;
+                sum[nt][h] = lost[nt][h] = off[nt][h] = 0.f;
             }
 
         Stage<D, NB> *drain = ring;
@@ -600,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                         most[nt][h] = s[0][nt][h];
 #pragma unroll
                         for (int b = 0; b < NB; ++b) most[nt][h] = fmaxf(fmaxf(most[nt][h], s[b][nt][h]), s[b][nt][2 + h]);
-                        grow = grow || most[nt][h] > top[nt][h] + 8.f;
+                        grow = grow || most[nt][h] > top[nt][h] + kMost;
                     }
                 if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
@@ -610,10 +613,11 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                             float m = most[nt][h];
 #pragma unroll
                             for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                            m = fmaxf(m, top[nt][h]);
+                            m = fmaxf(m - kStart, top[nt][h]);
                             const float f = ex2(top[nt][h] - m);
                             top[nt][h] = m;
                             sum[nt][h] *= f;
+                            lost[nt][h] *= f;
                             off[nt][h] *= f;
 #pragma unroll
                             for (int i = 0; i < KS; ++i) {
@@ -622,6 +626,10 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                             }
                         }
                 }
+                // a step's weights are added up by themselves first: long sums are rounded once a step and lane, and what the
+                // softmax sum loses there is kept (32,768 keys of one CTA, nearly all alike: the logarithm of the sum was off by
+                // 2e-5, and by 9e-6 with steps alone)
+                float part_sum[NT][2] = {}, part_off[NT][2] = {};
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -646,14 +654,23 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                             }
                             // a hidden key adds nothing, even when its scale or offset is no number
                             if (ORDINARY || !(x0 == -INFINITY)) {
-                                sum[nt][0] = fmaf(w0, inv[b][e], sum[nt][0]);
-                                off[nt][0] = fmaf(w.x, offv, off[nt][0]);
+                                part_sum[nt][0] = fmaf(w0, inv[b][e], part_sum[nt][0]);
+                                part_off[nt][0] = fmaf(w.x, offv, part_off[nt][0]);
                             }
                             if (ORDINARY || !(x1 == -INFINITY)) {
-                                sum[nt][1] = fmaf(w1, inv[b][e], sum[nt][1]);
-                                off[nt][1] = fmaf(w.y, offv, off[nt][1]);
+                                part_sum[nt][1] = fmaf(w1, inv[b][e], part_sum[nt][1]);
+                                part_off[nt][1] = fmaf(w.y, offv, part_off[nt][1]);
                             }
                         }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float both = sum[nt][h] + part_sum[nt][h];
+                        lost[nt][h] += part_sum[nt][h] - (both - sum[nt][h]);
+                        sum[nt][h] = both;
+                        off[nt][h] += part_off[nt][h];
+                    }
             };
                 if (ordinary) weights(Bool<true>{});
                 else weights(Bool<false>{});
@@ -722,6 +739,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                sum[nt][h] += lost[nt][h];
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
                     sum[nt][h] += __shfl_xor_sync(0xffffffffu, sum[nt][h], d);

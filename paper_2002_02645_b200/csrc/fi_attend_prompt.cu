@@ -15,7 +15,8 @@
 // Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
 // rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
 // so no size of keys runs over; the power goes into the factor of the scores.  Values likewise, and their power F into the
-// exponent: P = 2^(x + F - M) with M >= max(x + F) - 8, and the sum takes P 2^-F.  A key whose scale or offset (or whose value's) is no
+// exponent: P = 2^(x + F - M) with M = max(x + F) - 7 as it was when one last went over M + 15 (so halves start at 2^7 and lose what is
+// below 2^-32 of the largest, not 2^-25), and the sum takes P 2^-F.  A key whose scale or offset (or whose value's) is no
 // number becomes NaN in K and zero in V: the rows that see it get NaN, the others lose nothing.
 #include "fi_attend.cuh"
 
@@ -392,8 +393,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 most = fmaf(most, ck, fv);
                 // the products have read the weights before and added them up
                 if (t > 0) bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p.status);
-                if (__any_sync(0xffffffffu, most > top + 8.f)) {
-                    const float m = fmaxf(most, top), shrink = ex2(top - m);
+                if (__any_sync(0xffffffffu, most > top + kMost)) {
+                    const float m = fmaxf(most - kStart, top), shrink = ex2(top - m);
                     top = m;
                     sum *= shrink;
                     if (t > 0) {

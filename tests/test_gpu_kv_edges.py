@@ -29,6 +29,20 @@ def put(a, which, i, x):
     codes[pages], meta[pages] = kc[pages], km[pages]
 
 
+def formula(a, i, g, q, scale):
+    """Of head g of request i: weights [queries, keys], scores, values, in 64 bits."""
+    n, length = a.queries[i], a.lens[i]
+    h = g // a.group
+    x = q[a.cu[i]:a.cu[i + 1], g].double() @ a.values("k", i, h).T * scale
+    pos = torch.arange(length - n, length, device=DEV)[:, None]
+    t = torch.arange(length, device=DEV)
+    seen = t <= pos
+    if a.window:
+        seen = seen & (t > pos - a.window)
+    x = x.masked_fill(~seen, -math.inf)
+    return torch.softmax(x, -1), x, a.values("v", i, h)
+
+
 # ------------------------------------------------------------------------------ value vectors without a spread of their own
 
 SPREADS = {   # requests' lengths and queries; which keys' values are constant
@@ -64,3 +78,88 @@ def test_values_of_hardly_any_spread_count_beside_ordinary_ones(name, spread, di
     a.check(out, lse)
     again, _ = a.run()
     assert torch.equal(out[:a.cu[-1]], again[:a.cu[-1]])
+
+
+# --------------------------------------------------------------------------------------------------- peaked and long softmaxes
+
+def one_number_keys(a, i, codes0):
+    """Keys of request i: code codes0 (per key) in the first dimension, 0 in the others, scale 1 and offset 0, so that a query
+    (t, 0, 0, ...) scores t * code * scale exactly."""
+    pages = a.table[a.rows[i], :-(-a.lens[i] // a.page)].long()
+    t = torch.arange(a.lens[i], device=DEV)
+    where, off = pages[t // a.page], t % a.page
+    a.kc[where, :, off] = 0
+    a.kc[where, :, off, 0] = codes0.to(torch.uint8)[:, None]
+    a.km[where, :, off] = torch.tensor([1.0, 0.0], device=DEV, dtype=torch.bfloat16)
+
+
+def equal_spread_values(a, i, offset, gen):
+    """Values of request i: random codes, the same scale (2^-5) and offset everywhere."""
+    pages = a.table[a.rows[i], :-(-a.lens[i] // a.page)].long()
+    a.vc[pages] = torch.randint(0, 256, a.vc[pages].shape, generator=gen, device=DEV, dtype=torch.uint8)
+    a.vm[pages] = torch.tensor([2.0 ** -5, offset], device=DEV, dtype=torch.bfloat16)
+
+
+def everywhere(a, q, **kw):
+    """Attention of request 0 alone, as often as fills the device, so that a CTA takes a whole request."""
+    n = 6 * torch.cuda.get_device_properties(0).multi_processor_count
+    table = a.table[a.rows[0]:a.rows[0] + 1].expand(n, -1).contiguous()
+    out, lse = a.kv.attend(q.expand(n, -1, -1).contiguous(), ints([a.lens[0]] * n), table, with_lse=True, **kw)
+    return out[n // 2], lse[n // 2]
+
+
+SINKS = [5, 70, 140, 200]       # one in the share of each of a CTA's four warps
+
+
+@pytest.mark.parametrize("keys", [2048, 32768])
+@pytest.mark.parametrize("gap", [8.0, 9.0, 10.0])
+def test_float32_weights_far_below_the_largest_keep_their_bits(keys, gap):
+    """Four keys some nats above all others, which are equal.  Every weight may be off by 2^-21 of itself (a pair of halves and
+    the exponential, 2^-22 each) and by what float32 does to its exponent: four roundings of numbers up to the score's parts.
+    (The parts of a value are at most 15/2 scales and the offset moved by as much.)"""
+    heads = 16
+    a = Attention(lens=[keys], queries=[1], q_heads=heads, kv_heads=1, dim=128, page=64, dtype=torch.float32, seed=5)
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    codes0 = torch.zeros(keys, device=DEV)
+    codes0[SINKS] = 15
+    one_number_keys(a, 0, codes0)
+    equal_spread_values(a, 0, 1.0, gen)
+    gaps = gap + torch.linspace(0.0, 1.0, heads, device=DEV)
+    q = torch.zeros(1, heads, 128, device=DEV)
+    q[0, :, 0] = gaps / 15
+    a.q = q
+    out, lse = everywhere(a, q, scale=1.0)
+    for g in range(heads):
+        p, x, v = formula(a, 0, g, q, 1.0)
+        want = (p @ v)[0]
+        gap = gaps[g].item()
+        each = 2.0 ** -21 + 4 * 2.0 ** -24 * (1 + 2 * gap)
+        size = (v.abs().amax(-1) + 7.5 * 2.0 ** -5 + 1.25).max()
+        assert ((out[g].double() - want).abs() <= each * size).all(), ((out[g].double() - want).abs() / (each * size)).max()
+        assert (lse[g].double() - torch.logsumexp(x, -1)[0]).abs() <= each + 2.0 ** -22 * gap
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+def test_bf16_weights_far_below_the_largest_are_not_lost_together(prompt):
+    """Four keys 14 nats above 16,380 equal others; in half of the dimensions their value is zero, so that there the others' mean is
+    all there is.  Each of the others' weights may be off by 2^-11 (a half; for prompts the value too), exponents by a few u of
+    14, the result by its rounding."""
+    keys = 16384
+    a = Attention(lens=[keys], queries=[1], q_heads=4, kv_heads=1, dim=128, page=64, seed=6)
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    codes0 = torch.zeros(keys, device=DEV)
+    codes0[SINKS] = 14
+    one_number_keys(a, 0, codes0)
+    x = torch.randint(0, 16, (keys, 1, 128), generator=gen, device=DEV) * 0.125         # 0 .. 15/8: offset 0, scale 1/8
+    x[:, :, 0], x[:, :, 1] = 0.0, 15 * 0.125
+    x[SINKS, 0, 2:65] = 0.0
+    put(a, "v", 0, x)
+    q = torch.zeros(1, 4, 128, device=DEV, dtype=torch.bfloat16)
+    q[0, :, 0] = torch.tensor([1.0, 0.9375, 0.875, 0.75], device=DEV)
+    a.q = q
+    out = a.run(q=q, scale=1.0, max_query=MANY)[0][0] if prompt else everywhere(a, q, scale=1.0)[0]
+    for g in range(4):
+        p, _, v = formula(a, 0, g, q, 1.0)
+        want = (p @ v)[0]
+        each = 2.0 ** -11 * (2 if prompt else 1) + 2.0 ** -18
+        assert ((out[g].double() - want).abs() <= (each + 2.0 ** -8) * want.abs()).all()
