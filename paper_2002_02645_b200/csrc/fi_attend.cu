@@ -16,6 +16,10 @@
 // Codes are all positive, so the product part and the offset part are larger than what they add up to.  The offset part
 // therefore takes the weights as they were rounded for the product, and float32 queries, which must not lose what the parts have in
 // common, take the codes less 7.5 (one more instruction per two codes) and offsets moved by 7.5 scales.
+// Tensor cores cut what they add, so a sum kept there shrinks with every product (bf16 queries over 100,000 keys of a warp: by more
+// than the result's rounding).  So they add up 32 keys, and long sums are kept outside of them, which takes 5 % longer (64 requests of
+// 800 to 8,192 keys: 86.7 -> 91.5 us).  Taking them out every 16 steps only, into scratch of 16 KB per CTA, took 89.4 us; into tensor
+// memory 169 us, because fewer CTAs of a kernel that has some run per SM.
 // A value vector of hardly any spread (a constant one has the smallest scale there is) is all offset: its P_t is far below the
 // others' and may round to nothing, although its p_t is like theirs.  Where the offset is more than kMostlyOffset scales, the
 // offset part takes the weight as it was before the rounding: what the two parts then differ in, 2^-12 of 15 scales, is below
@@ -694,37 +698,27 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                             x[b][2] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x5410);
                             x[b][3] = __byte_perm(vw[b][2][w], vw[b][3][w], 0x7632);
                         }
+                        float part[4][NT][4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float part[NT][4];
-                            if constexpr (F32) {
+                        for (int b = 0; b < 2; ++b)
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) part[nt][e] = 0.f;
-                            }
-#pragma unroll
-                            for (int b = 0; b < 2; ++b) {
+                            for (int i = 0; i < 4; ++i) {
                                 const uint32_t lo = x[b][i >> 1] >> ((i & 1) * 8), hi = x[b][2 + (i >> 1)] >> ((i & 1) * 8);
                                 const uint32_t a[4] = {codes<F32, 0>(lo & 0x000f000fu), codes<F32, 1>(lo & 0x00f000f0u),
                                                        codes<F32, 0>(hi & 0x000f000fu), codes<F32, 1>(hi & 0x00f000f0u)};
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
-                                    if constexpr (F32) {
-                                        mma(part[nt], a, pb[b0 + b][nt][0], pb[b0 + b][nt][1]);
-                                        mma(part[nt], a, pb2[b0 + b][nt][0], pb2[b0 + b][nt][1]);
-                                    } else {
-                                        mma(o[4 * w + i][nt], a, pb[b0 + b][nt][0], pb[b0 + b][nt][1]);
-                                    }
+                                    if (b == 0) part[i][nt][0] = part[i][nt][1] = part[i][nt][2] = part[i][nt][3] = 0.f;
+                                    mma(part[i][nt], a, pb[b0 + b][nt][0], pb[b0 + b][nt][1]);
+                                    if constexpr (F32) mma(part[i][nt], a, pb2[b0 + b][nt][0], pb2[b0 + b][nt][1]);
                                 }
                             }
-                            if constexpr (F32) {   // tensor cores cut what they add: long sums are kept outside of them
 #pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) o[4 * w + i][nt][e] += part[nt][e];
-                            }
-                        }
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[4 * w + i][nt][e] += part[i][nt][e];
                     }
                 }
             }

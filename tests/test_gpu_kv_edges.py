@@ -163,3 +163,33 @@ def test_bf16_weights_far_below_the_largest_are_not_lost_together(prompt):
         want = (p @ v)[0]
         each = 2.0 ** -11 * (2 if prompt else 1) + 2.0 ** -18
         assert ((out[g].double() - want).abs() <= (each + 2.0 ** -8) * want.abs()).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_bf16_sums_over_many_keys_do_not_drift(dim):
+    """Requests that fill the device, each 400,000 keys long (all of them read the same pages), with weights that hardly differ: the
+    result is the mean of the values, a few hundred times smaller than they are.  Roundings of the weights (2^-12 at most, each for
+    itself) add up like independent errors: six times the root of the sum of their squares.  Sums in float32 may be off by 2^-19 of
+    the sum of the parts' sizes (codes less 7.5, offsets moved by as much), whatever the number of keys; the rounding to bf16 is 2^-8."""
+    keys, heads, page = 400000, 8, 256
+    blocks = -(-keys // page)
+    gen = torch.Generator(device=DEV).manual_seed(dim)
+    kc, km = pools(blocks, 1, page, dim)
+    vc, vm = pools(blocks, 1, page, dim)
+    kv = fb.KvCache(kc, km, vc, vm, q_heads=heads)
+    x = torch.randn(2, keys, 1, dim, generator=gen, device=DEV)
+    kv.append(x[0], x[1], torch.arange(keys, device=DEV))
+    requests = 3 * torch.cuda.get_device_properties(0).multi_processor_count
+    table = torch.arange(blocks, dtype=torch.int32, device=DEV).expand(requests, blocks).contiguous()
+    q = (0.1 * torch.randn(requests, heads, dim, generator=gen, device=DEV)).to(torch.bfloat16)
+    out = kv.attend(q, ints([keys] * requests), table)
+    value = lambda c, m: unpack(c.view(-1, dim // 2)[:keys]).double() * m.view(-1, 2)[:keys, :1].double() + m.view(-1, 2)[:keys, 1:].double()
+    k, v = value(kc, km), value(vc, vm)
+    scale, offset = (vm.view(-1, 2)[:keys, j:j + 1].double() for j in (0, 1))
+    parts = 7.5 * scale + (offset + 7.5 * scale).abs()
+    for r in (0, 1, requests // 2, requests - 1):
+        p = torch.softmax(q[r].double() @ k.T * dim ** -0.5, -1)
+        want = p @ v
+        bound = 6 * 2.0 ** -12 * (p.square() @ v.square()).sqrt() + 2.0 ** -19 * (p @ parts) + 2.0 ** -8 * want.abs()
+        off = (out[r].double() - want).abs() / bound
+        assert (off <= 1).all(), off.max().item()
