@@ -1,6 +1,8 @@
 // Shared by the two kernels of attention over the 4-bit store (fi_attend.cu, fi_attend_prompt.cu).
 #pragma once
 
+#include <cfloat>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -9,7 +11,7 @@
 namespace fi {
 
 constexpr float kMinScale = 0x1p-40f;      // smallest scale append stores
-constexpr float kNoMax = -1e30f;           // maximum of nothing
+constexpr float kNoMax = -FLT_MAX;         // maximum of nothing
 constexpr float kStart = 7.f, kMost = 15.f;   // log2 of the largest weight: as it is set, and as it may become
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;

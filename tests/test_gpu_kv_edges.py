@@ -193,3 +193,26 @@ def test_bf16_sums_over_many_keys_do_not_drift(dim):
         bound = 6 * 2.0 ** -12 * (p.square() @ v.square()).sqrt() + 2.0 ** -19 * (p @ parts) + 2.0 ** -8 * want.abs()
         off = (out[r].double() - want).abs() / bound
         assert (off <= 1).all(), off.max().item()
+
+
+# ------------------------------------------------------------------------------------------------- the ends of the types
+
+@BOTH
+@pytest.mark.parametrize("prompt", [False, True])
+def test_scores_below_minus_1e30_are_scores(prompt, dtype):
+    """All scores are about -2.5e30: the result is a mean of the values, not that of a query without keys.  (Exponents are off by some u
+    of the scores' size, so that at this size any weights are as good.)"""
+    if prompt and dtype is torch.float32:
+        pytest.skip("prompts of float32 take the same kernel")
+    a = Attention(lens=[37], queries=[2], q_heads=2, kv_heads=1, dim=64, dtype=dtype, seed=8)
+    put(a, "k", 0, torch.full((37, 1, 64), 2.0 ** 50, device=DEV))
+    a.q[:] = -(2.0 ** 48)
+    out, lse = a.run(max_query=MANY if prompt else 2)
+    for g in range(2):
+        _, x, v = formula(a, 0, g, a.q, 64 ** -0.5)
+        parts = (v.abs().amax(-1) + 15 * a.vm_scale(0, 0)).max()
+        slack = 2 * 2.0 ** -11 * parts + 2.0 ** -8 * v.abs().max()
+        got = out[:2, g].double()
+        assert (got >= v.min(0).values - slack).all() and (got <= v.max(0).values + slack).all()
+        ref = torch.logsumexp(x, -1)
+        assert ((lse[:2, g].double() - ref).abs() <= 2.0 ** -20 * ref.abs()).all()
