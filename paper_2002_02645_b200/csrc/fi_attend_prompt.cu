@@ -362,7 +362,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     continue;
                 }
                 const int key0 = x.first_key + t * kTile;
-                const float ck = c * ctl->k_power[n & 3], fv = ctl->v_power[n & 3];
+                // (never 0: a hidden score is -infinity and has to stay so)
+                const float ck = fminf(fmaxf(c * ctl->k_power[n & 3], FLT_MIN), FLT_MAX), fv = ctl->v_power[n & 3];
                 const uint32_t lost = ctl->hidden[n & 3][0] | ctl->hidden[n & 3][1] | ctl->hidden[n & 3][2] | ctl->hidden[n & 3][3];
                 const bool edge = key0 + kTile > all_high || key0 < all_low || lost != 0;
                 bar_wait(&ctl->s_full[half], steps & 1, ctl, p.status);

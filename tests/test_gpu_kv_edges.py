@@ -216,3 +216,16 @@ def test_scores_below_minus_1e30_are_scores(prompt, dtype):
         assert (got >= v.min(0).values - slack).all() and (got <= v.max(0).values + slack).all()
         ref = torch.logsumexp(x, -1)
         assert ((lse[:2, g].double() - ref).abs() <= 2.0 ** -20 * ref.abs()).all()
+
+
+@pytest.mark.parametrize("key,query,scale", [(0.0, 2.0 ** -90, None), (0.0, 2.0 ** -100, None), (0.0, 1.0, 2.0 ** -100),
+                                             (0.0, 2.0 ** -60, -2.0 ** -60), (2.0 ** -70, 2.0 ** -70, None)])
+def test_prompts_of_tiny_scores_average_the_values(key, query, scale):
+    """Scores of (almost) nothing: all visible keys weigh the same, and hidden ones stay hidden."""
+    a = Attention(lens=[300, 40], queries=[200, 3], q_heads=4, kv_heads=2, dim=128, seed=9, room=1024)
+    for i, n in enumerate(a.lens):
+        put(a, "k", i, torch.full((n, 2, 128), key, device=DEV))
+    a.q[:] = (a.q.sign() * query).to(a.q.dtype)
+    out, lse = a.run(max_query=MANY, scale=scale)
+    a.check(out, lse, scale=scale, halves=True)
+    a.check(a.run(max_query=MANY, scale=scale, with_lse=False), None, scale=scale, halves=True)
