@@ -196,7 +196,7 @@ __device__ __forceinline__ int tile_power(float most, uint32_t *red, int uw, int
 #pragma unroll
     for (int i = 0; i < kUnpackWarps; ++i) all = max(all, *reinterpret_cast<volatile uint32_t *>(red + i));
     const int e = all ? (int)(all >> 23) - 141 : 0;
-    return e < -100 ? -100 : e > 100 ? 100 : e;
+    return e < -100 ? -100 : e;            // (114 at most)
 }
 
 // One tile of query rows as every role walks them: request by request, heads, row tiles from the last (most keys) to the first.
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 int up = 0;
                 if (top > 0.f && top < INFINITY) {
                     up = 141 - (int)(__float_as_uint(top) >> 23);
-                    up = up < -110 ? -110 : up > 110 ? 110 : up;
+                    up = up > 110 ? 110 : up;            // (-113 at least)
                 }
                 // the factor of the scores is kept positive: its sign goes into the query (and a factor of zero makes it zero)
                 float f = __uint_as_float((uint32_t)(127 + up) << 23);

@@ -229,3 +229,27 @@ def test_prompts_of_tiny_scores_average_the_values(key, query, scale):
     out, lse = a.run(max_query=MANY, scale=scale)
     a.check(out, lse, scale=scale, halves=True)
     a.check(a.run(max_query=MANY, scale=scale, with_lse=False), None, scale=scale, halves=True)
+
+
+@pytest.mark.parametrize("key,query", [(2.0 ** 112, 2.0 ** -112), (2.0 ** 120, 2.0 ** -110), (2.0 ** 123, 2.0 ** -115), (2.0 ** -60, 2.0 ** 116)])
+def test_prompts_whose_keys_or_queries_reach_the_end_of_the_type(key, query):
+    a = Attention(lens=[300, 40], queries=[200, 3], q_heads=4, kv_heads=2, dim=128, seed=10, room=1024)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for i, n in enumerate(a.lens):
+        put(a, "k", i, torch.randn(n, 2, 128, generator=gen, device=DEV) * key)
+    a.q[:] = (torch.randn(a.q.shape, generator=gen, device=DEV) * query).to(a.q.dtype)
+    scale = 0.05 / (key * query)
+    if not 2.0 ** -120 < abs(scale) < 2.0 ** 120:
+        pytest.skip("no float32 scale")
+    out, lse = a.run(max_query=MANY, scale=scale)
+    a.check(out, lse, scale=scale, halves=True)
+    a.check(a.run(max_query=MANY, scale=scale, with_lse=False), None, scale=scale, halves=True)
+
+
+def test_prompt_values_reach_the_end_of_the_type():
+    a = Attention(lens=[200], queries=[70], q_heads=2, kv_heads=1, dim=64, seed=10, room=1024)
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    put(a, "v", 0, torch.randn(200, 1, 64, generator=gen, device=DEV) * 2.0 ** 121)
+    out, lse = a.run(max_query=MANY)
+    a.check(out, lse, halves=True)
+    a.check(a.run(max_query=MANY, with_lse=False), None, halves=True)
