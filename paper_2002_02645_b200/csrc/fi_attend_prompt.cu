@@ -18,6 +18,13 @@
 // exponent: P = 2^(x + F - M) with M = max(x + F) - 7 as it was when one last went over M + 15 (so halves start at 2^7 and lose what is
 // below 2^-32 of the largest, not 2^-25), and the sum takes P 2^-F.  A key whose scale or offset (or whose value's) is no
 // number becomes NaN in K and zero in V: the rows that see it get NaN, the others lose nothing.
+//
+// Keys rounded to halves put a score off by up to 2^-11 of its parts.  The result, whose weights are halves anyway, may have that; the
+// softmax sum's logarithm is a float32 number, which was off by up to 8e-4 where few keys count.  So when it is wanted, the
+// codes go into the product as they are, less 7.5 (exact), and the scores take each key's scale and offset behind it:
+//   y = (S c) s + (m + 7.5 s) (scale log2(e) sum(q)) + F
+// The case above takes 471 us then.  (One pass over S instead of two, with the maximum checked afterwards: 489 us, as it has to wait for the
+// product before.  Keys as two halves, in two products: 535 us.)
 #include "fi_attend.cuh"
 
 namespace fi {
@@ -34,11 +41,12 @@ constexpr int kTmemCols = 512;             // S of both halves, O of both
 
 struct PromptCtl {
     uint64_t k_full, k_empty, v_full, v_empty, q_full;
-    uint64_t k_info[4], v_info[4];         // a tile's powers: known before its keys and values have a place
+    uint64_t k_info[4], v_info[4];         // a tile's powers (EXACT: scales and offsets): known before its keys and values have a place
     uint64_t s_full[2], p_full[2], pv_done[2];                      // of the halves
     float k_power[4], v_power[4];          // 2^E of a tile's keys; F of its values
     uint32_t hidden[4][kUnpackWarps];      // keys of a tile whose page is not in the pool, a bit each
     uint32_t red[2][2][kUnpackWarps];      // largest key and value of a tile, by warp
+    alignas(16) float k_scale[4][kTile], k_offset[4][kTile];   // EXACT: of a tile's keys, offsets moved by 7.5 scales
     alignas(16) uint32_t meta[kTile];      // scale and offset of a tile's values, as halves
     uint32_t tmem;
     volatile int gave_up;
@@ -152,6 +160,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -171,6 +184,15 @@ __device__ __forceinline__ uint32_t value2(uint32_t codes, __half2 scale, __half
     const __half2 n = ROW ? __hfma2(reinterpret_cast<const __half2 &>(big), __float2half2_rn(0.0625f), __float2half2_rn(-64.f))
                           : __hadd2(reinterpret_cast<const __half2 &>(big), __float2half2_rn(-1024.f));
     const __half2 v = __hfma2(n, scale, offset);
+    return reinterpret_cast<const uint32_t &>(v);
+}
+
+// two codes n as (n - 7.5) 2^-9, exactly
+constexpr float kCode = 0x1p-9f;
+template <int ROW>
+__device__ __forceinline__ uint32_t centred2(uint32_t codes) {
+    const __half2 v = __hfma2(reinterpret_cast<const __half2 &>(codes), __float2half2_rn(kCode * (ROW ? 0x1p20f : 0x1p24f)),
+                              __float2half2_rn(-7.5f * kCode));
     return reinterpret_cast<const uint32_t &>(v);
 }
 
@@ -247,7 +269,7 @@ __device__ __forceinline__ bool next_item(const AttendParams &p, ItemWalk &w, It
 // tiles that are unpacked for an item
 __device__ __forceinline__ int tiles_of(const Item &x) { return max(x.tiles[0], x.tiles[1]); }
 
-template <int D>
+template <int D, bool EXACT>
 __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(const __grid_constant__ AttendParams p) {
     using S = PromptSmem<D>;
     constexpr int PANEL = kTile * 128;     // 128 rows of 128 bytes
@@ -303,7 +325,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             const int high = pos + 1, low = p.window > 0 ? max(pos, 0) - p.window + 1 : 0;
             const int first = x.len - x.queries + row0 / p.group, last = x.len - x.queries + (min(row0 + kTile, x.rows) - 1) / p.group;
             const int all_high = first + 1, all_low = p.window > 0 ? max(last, 0) - p.window + 1 : 0;
-            float c = 0.f;
+            float c = 0.f, q_sum = 0.f;                       // what S is worth; EXACT: the row's scale sum(q)
             if (all > 0) {
                 // ---- the row's query as halves, its largest value at 2^14 .. 2^15 (exact for bf16), in the order of the codes ----
                 const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
@@ -330,21 +352,33 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     up = 141 - (int)(__float_as_uint(top) >> 23);
                     up = up > 110 ? 110 : up;            // (-113 at least)
                 }
-                // the factor of the scores is kept positive: its sign goes into the query (and a factor of zero makes it zero)
                 float f = __uint_as_float((uint32_t)(127 + up) << 23);
-                c = fabsf(p.scale_log2) * __uint_as_float((uint32_t)(127 - up) << 23);
-                if (p.scale_log2 < 0.f) f = -f;
-                if (!(c > 0.f)) {
-                    f = 0.f;
-                    c = 1.f;
+                const float back = p.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+                if constexpr (!EXACT) {
+                    // the factor of the scores is kept positive: its sign goes into the query (and a factor of zero makes it zero)
+                    c = fabsf(back);
+                    if (back < 0.f) f = -f;
+                    if (!(c > 0.f)) {
+                        f = 0.f;
+                        c = 1.f;
+                    }
                 }
+                float total[EXACT ? 8 : 1] = {};
 #pragma unroll 4
                 for (int i = 0; i < D / 8; ++i) {
                     float v[8];
                     words(i, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] *= f;
+                        if constexpr (EXACT) total[e] += v[e];
+                    }
                     *reinterpret_cast<uint4 *>(smem + S::q + half * S::kQ + (i >> 3) * PANEL + my_row * 128 + (((i & 7) ^ (my_row & 7)) << 4)) =
-                        make_uint4(half2_bits(v[0] * f, v[4] * f), half2_bits(v[1] * f, v[5] * f), half2_bits(v[2] * f, v[6] * f),
-                                   half2_bits(v[3] * f, v[7] * f));
+                        make_uint4(half2_bits(v[0], v[4]), half2_bits(v[1], v[5]), half2_bits(v[2], v[6]), half2_bits(v[3], v[7]));
+                }
+                if constexpr (EXACT) {
+                    c = back / kCode;
+                    q_sum = back * (((total[0] + total[4]) + (total[1] + total[5])) + ((total[2] + total[6]) + (total[3] + total[7])));
                 }
                 fence_async();
                 bar_arrive(&ctl->q_full);
@@ -363,7 +397,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 }
                 const int key0 = x.first_key + t * kTile;
                 // (never 0: a hidden score is -infinity and has to stay so)
-                const float ck = fminf(fmaxf(c * ctl->k_power[n & 3], FLT_MIN), FLT_MAX), fv = ctl->v_power[n & 3];
+                const float ck = EXACT ? 1.f : fminf(fmaxf(c * ctl->k_power[n & 3], FLT_MIN), FLT_MAX), fv = ctl->v_power[n & 3];
                 const uint32_t lost = ctl->hidden[n & 3][0] | ctl->hidden[n & 3][1] | ctl->hidden[n & 3][2] | ctl->hidden[n & 3][3];
                 const bool edge = key0 + kTile > all_high || key0 < all_low || lost != 0;
                 bar_wait(&ctl->s_full[half], steps & 1, ctl, p.status);
@@ -376,6 +410,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     tmem_load_wait();
                     settle(s);
                     settle(s + 16);
+                };
+                const auto hide = [&](int c0) {
                     if (edge) {
                         const int hi = high - key0 - c0, lo = low - key0 - c0;
                         const uint32_t gone = ctl->hidden[n & 3][c0 >> 5];
@@ -388,10 +424,31 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
 #pragma unroll 1
                 for (int c0 = 0; c0 < kTile; c0 += 32) {
                     read(c0);
+                    if constexpr (EXACT) {
+                        const uint64_t c2 = pair(c, c), sq2 = pair(q_sum, q_sum), fv2 = pair(fv, fv);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 ks = *reinterpret_cast<const float4 *>(&ctl->k_scale[n & 3][c0 + i]),
+                                         ko = *reinterpret_cast<const float4 *>(&ctl->k_offset[n & 3][c0 + i]);
+                            float y[4];
+                            unpair(fma2(mul2(pair(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2), pair(ks.x, ks.y),
+                                        fma2(pair(ko.x, ko.y), sq2, fv2)), y[0], y[1]);
+                            unpair(fma2(mul2(pair(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), c2), pair(ks.z, ks.w),
+                                        fma2(pair(ko.z, ko.w), sq2, fv2)), y[2], y[3]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[i + e] = __float_as_uint(y[e]);
+                        }
+                    }
+                    hide(c0);
+                    if constexpr (EXACT) {      // y takes the place of S
+                        tmem_store(s_at + c0, s);
+                        tmem_store(s_at + c0 + 16, s + 16);
+                    }
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) most = fmaxf(fmaxf(most, __uint_as_float(s[i])), __uint_as_float(s[i + 1]));
                 }
-                most = fmaf(most, ck, fv);
+                if constexpr (EXACT) tmem_store_wait();
+                else most = fmaf(most, ck, fv);
                 // the products have read the weights before and added them up
                 if (t > 0) bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p.status);
                 if (__any_sync(0xffffffffu, most > top + kMost)) {
@@ -412,11 +469,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                         tmem_store_wait();
                     }
                 }
-                const uint64_t ck2 = pair(ck, ck), shift2 = pair(fv - top, fv - top);
+                const uint64_t ck2 = pair(ck, ck), shift2 = EXACT ? pair(-top, -top) : pair(fv - top, fv - top);
                 uint64_t part[2] = {0, 0};
 #pragma unroll 1
                 for (int c0 = 0; c0 < kTile; c0 += 32) {
                     read(c0);
+                    if constexpr (!EXACT) hide(c0);
                     unsigned char *const to = smem + S::p + half * S::kP + (c0 >> 6) * PANEL + my_row * 128;
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
@@ -424,7 +482,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             float w0, w1;
-                            unpair(fma2(pair(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1])), ck2, shift2), w0, w1);
+                            const uint64_t s2 = pair(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1]));
+                            unpair(EXACT ? add2(s2, shift2) : fma2(s2, ck2, shift2), w0, w1);
                             w0 = ex2(w0);
                             w1 = ex2(w1);
                             part[e & 1] = add2(part[e & 1], pair(w0, w1));
@@ -513,24 +572,35 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 const bool lost = next_lost;
                 if (lost) atomicOr(p.status, 2);
                 const float scale = meta.bad ? 0.f : meta_scale(meta.k), offset = meta.bad ? __uint_as_float(0x7fc00000u) : meta_offset(meta.k);
-                const int e = tile_power(meta.bad ? 0.f : fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][0], uw, lane, 1);
-                const float f = __uint_as_float((uint32_t)(127 - e) << 23);
-                const __half2 s2 = __float2half2_rn(scale * f), o2 = __float2half2_rn(offset * f);
-                // (S of tile n - 2 is there for both halves, so both have formed the weights of n - 3: the powers of n - 4 are free)
-                const uint32_t gone = __ballot_sync(0xffffffffu, lost);
-                if (lane == 0) {
-                    ctl->hidden[n & 3][uw] = gone;
+                // (S of tile n - 2 is there for both halves, so both have formed the weights of n - 3: the place of n - 4 is free)
+                __half2 s2, o2;
+                if constexpr (EXACT) {
+                    ctl->k_scale[n & 3][u] = scale;
+                    ctl->k_offset[n & 3][u] = fmaf(7.5f, scale, offset);
+                } else {
+                    const int e = tile_power(meta.bad ? 0.f : fmaxf(fabsf(offset), fabsf(fmaf(15.f, scale, offset))), ctl->red[n & 1][0], uw, lane, 1);
+                    const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+                    s2 = __float2half2_rn(scale * f);
+                    o2 = __float2half2_rn(offset * f);
                     if (u == 0) ctl->k_power[n & 3] = __uint_as_float((uint32_t)(127 + e) << 23);
-                    bar_arrive(&ctl->k_info[n & 3]);
                 }
+                const uint32_t gone = __ballot_sync(0xffffffffu, lost);
+                if (lane == 0) ctl->hidden[n & 3][uw] = gone;
+                __syncwarp();
+                if (lane == 0) bar_arrive(&ctl->k_info[n & 3]);
                 bar_wait(&ctl->k_empty, (n & 1) ^ 1, ctl, p.status);
                 unsigned char *const to = smem + S::k + u * 128;
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) {
                     const uint32_t w = next[i], w8 = w >> 8;
-                    *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) =
-                        make_uint4(value2<0>(w & 0x000f000fu, s2, o2), value2<1>(w & 0x00f000f0u, s2, o2),
-                                   value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
+                    uint4 v;
+                    if constexpr (EXACT)
+                        v = make_uint4(centred2<0>(w & 0x000f000fu), centred2<1>(w & 0x00f000f0u), centred2<0>(w8 & 0x000f000fu),
+                                       centred2<1>(w8 & 0x00f000f0u));
+                    else
+                        v = make_uint4(value2<0>(w & 0x000f000fu, s2, o2), value2<1>(w & 0x00f000f0u, s2, o2),
+                                       value2<0>(w8 & 0x000f000fu, s2, o2), value2<1>(w8 & 0x00f000f0u, s2, o2));
+                    *reinterpret_cast<uint4 *>(to + (i >> 3) * PANEL + (((i & 7) ^ (u & 7)) << 4)) = v;
                 }
                 fence_async();
                 bar_arrive(&ctl->k_full);
@@ -695,6 +765,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
 template <int D>
 constexpr int prompt_smem() { return PromptSmem<D>::bytes; }
 
+const void *prompt_kernel(bool wide, bool exact) {
+    if (wide) return exact ? reinterpret_cast<const void *>(&kv_attend_prompt_kernel<128, true>) : reinterpret_cast<const void *>(&kv_attend_prompt_kernel<128, false>);
+    return exact ? reinterpret_cast<const void *>(&kv_attend_prompt_kernel<64, true>) : reinterpret_cast<const void *>(&kv_attend_prompt_kernel<64, false>);
+}
+
 }  // namespace
 
 // Which kernel.  The one for few rows takes its time by tiles of 16 rows, however they are spread: it cuts long keys over CTAs.  This
@@ -705,10 +780,7 @@ constexpr int prompt_smem() { return PromptSmem<D>::bytes; }
 // one request it takes 37 us, this one 28; at 128 rows 20 and 21.
 bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long rows) {
     if (dtype != FI_BF16 || (kv->cfg.head_dim != 64 && kv->cfg.head_dim != 128)) return false;
-    // Keys rounded to halves put a score off by about 2^-12 of its parts; among many keys that averages out of the softmax sum, among
-    // a few it would be seen in the logarithm of it, so that is left to the other kernel.
     const long long most_keys = (long long)p.max_blocks << p.page_shift;
-    if (p.lse && most_keys < 1024) return false;
     const double heads = (double)p.batch_max * kv->cfg.kv_heads;
     const double tiles = heads * (double)((rows + 15) / 16), items = heads * (double)((rows + kRows - 1) / kRows);
     if (tiles > 3.5 * kv->sm_count * (double)(long long)((items + kv->sm_count - 1) / kv->sm_count)) return true;
@@ -716,18 +788,24 @@ bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, lon
 }
 
 fi_status_t prepare_attend_prompt(const fi_kv *kv) {
+    const bool wide = kv->cfg.head_dim == 128;
+    if (!wide && kv->cfg.head_dim != 64) return FI_OK;
     cudaError_t e = cudaSuccess;
-    if (kv->cfg.head_dim == 64) e = cudaFuncSetAttribute(kv_attend_prompt_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, prompt_smem<64>());
-    if (kv->cfg.head_dim == 128) e = cudaFuncSetAttribute(kv_attend_prompt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, prompt_smem<128>());
+    for (int exact = 0; exact < 2 && e == cudaSuccess; ++exact)
+        e = cudaFuncSetAttribute(prompt_kernel(wide, exact != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, wide ? prompt_smem<128>() : prompt_smem<64>());
     return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_kv_create: attention kernels");
 }
 
 fi_status_t launch_attend_prompt(const fi_kv *kv, const AttendParams &p, long long rows, cudaStream_t stream) {
     const double items = (double)p.batch_max * kv->cfg.kv_heads * (double)((rows + kRows - 1) / kRows);
     const int grid = items < kv->sm_count ? (int)items : kv->sm_count;
-    if (kv->cfg.head_dim == 64) kv_attend_prompt_kernel<64><<<grid, kPromptThreads, prompt_smem<64>(), stream>>>(p);
-    else kv_attend_prompt_kernel<128><<<grid, kPromptThreads, prompt_smem<128>(), stream>>>(p);
+    const bool wide = kv->cfg.head_dim == 128;
+    AttendParams args = p;
+    void *list[] = {&args};
+    const cudaError_t e = cudaLaunchKernel(prompt_kernel(wide, p.lse != nullptr), dim3((unsigned)grid), dim3(kPromptThreads), list,
+                                           (size_t)(wide ? prompt_smem<128>() : prompt_smem<64>()), stream);
     count_launch();
+    if (e != cudaSuccess) return cuda_fail(e, "fi_kv_attend");
     return check_launch("fi_kv_attend");
 }
 

@@ -253,3 +253,50 @@ def test_prompt_values_reach_the_end_of_the_type():
     out, lse = a.run(max_query=MANY)
     a.check(out, lse, halves=True)
     a.check(a.run(max_query=MANY, with_lse=False), None, halves=True)
+
+
+# --------------------------------------------------------------------------------- prompts: queries that see few keys
+
+def check_logarithms(a, lse):
+    """The softmax sum's logarithm is a float32 output: off by float32's roundings of a score's parts (2^-20 of their sum, as in the
+    tests of the kernel for few rows), however few keys a query sees and however many columns the block table has."""
+    scale = a.dim ** -0.5
+    for i, n in enumerate(a.queries):
+        for g in range(a.group * a.kv_heads):
+            _, x, _ = formula(a, i, g, a.q, scale)
+            ref = torch.logsumexp(x, -1)
+            reach = (a.q[a.cu[i]:a.cu[i + 1], g].double().abs().sum(-1, keepdim=True) * a.k_reach(i, g // a.group) * scale).amax(-1)
+            off = (lse[a.cu[i]:a.cu[i + 1], g].double() - ref).abs() / (2.0 ** -20 * (1 + reach) + 2.0 ** -20 * ref.abs())
+            assert (off <= 1).all(), off.max().item()
+
+
+FEW_KEYS = {
+    "prompt-from-nothing": dict(lens=[300, 7], queries=[300, 7], room=8192),
+    "short-requests": dict(lens=[1, 2, 9, 50], queries=[1, 1, 2, 30], room=4096),
+    "narrow-window": dict(lens=[900], queries=[200], window=3, room=2048),
+    "narrow-table": dict(lens=[300, 7], queries=[300, 7]),
+}
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("name", FEW_KEYS)
+def test_prompt_kernel_logarithms_of_few_keys(name, dim):
+    a = Attention(q_heads=8, kv_heads=2, dim=dim, seed=13, **FEW_KEYS[name])
+    for i, n in enumerate(a.lens):
+        put(a, "k", i, torch.randn(n, 2, dim, device=DEV) + 2.0)
+    out, lse = a.run(max_query=MANY)
+    a.check(out, None, halves=True)
+    check_logarithms(a, lse)
+
+
+def test_wider_block_table_keeps_the_results_as_exact():
+    """The same requests behind a table with room for 48 times the keys, which may choose another kernel."""
+    a = Attention(q_heads=32, kv_heads=4, dim=128, lens=[600, 900], queries=[600, 400], seed=14)
+    for room in (0, 48):
+        if room:
+            wide = torch.full((a.table.shape[0], 48 * a.table.shape[1]), -1, dtype=torch.int32, device=DEV)
+            wide[:, :a.table.shape[1]] = a.table
+            a.table = wide
+        out, lse = a.run()
+        a.check(out, None, halves=True)
+        check_logarithms(a, lse)
