@@ -537,7 +537,7 @@ fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *args, void *cuda_str
  *   q, out [max_tokens x q_heads x head_dim], float32 or bfloat16, strides in elements, multiples of 16 bytes;
  *   lse [max_tokens x q_heads] float, contiguous, nullable: natural logarithm of the softmax sum
  *   cu_tokens nullable: one query per request, token i of request i; max_query: most queries of a request (a hint
- *   that chooses the kernel: any number is computed correctly)
+ *   that chooses the kernel: any number is computed correctly; one above max_tokens asks for the kernel for prompts)
  * Softmax statistics and sums in fp32; products on tensor cores with the codes exact and, for float32 queries, with
  * queries and probabilities as pairs of half-precision numbers; a probability is off by 2^-12 of itself or 2^-32 of the row's
  * largest (float32 queries: 2^-22), exponents by some 2^-24 of the size of the scores.  Many bfloat16 queries per request (head_dim

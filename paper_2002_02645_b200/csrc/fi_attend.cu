@@ -1106,7 +1106,7 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     const bool f32 = a->dtype == FI_F32;
     const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;
     const long long rows = per_request * p.group;
-    if (prompt_kernel_serves(kv, p, a->dtype, rows)) return launch_attend_prompt(kv, p, rows, static_cast<cudaStream_t>(cuda_stream));
+    if (prompt_kernel_serves(kv, p, a->dtype, per_request)) return launch_attend_prompt(kv, p, rows, static_cast<cudaStream_t>(cuda_stream));
     const int nt = tile_columns(c.head_dim, rows);
     const Variant v = f32 ? pick<true>(c.head_dim, nt) : pick<false>(c.head_dim, nt);
     long long grid = kv->attend_ctas[f32 ? 1 : 0][nt >> 1];

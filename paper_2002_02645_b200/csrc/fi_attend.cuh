@@ -47,7 +47,7 @@ __device__ __forceinline__ float meta_offset(uint32_t m) { return __uint_as_floa
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
 // few rows per key head: any type, any head size (fi_attend.cu); many rows of bf16 queries (fi_attend_prompt.cu)
-bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long rows);
+bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long queries);
 fi_status_t prepare_attend_prompt(const fi_kv *kv);
 fi_status_t launch_attend_prompt(const fi_kv *kv, const AttendParams &p, long long rows, cudaStream_t stream);
 

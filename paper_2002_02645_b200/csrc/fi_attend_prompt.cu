@@ -774,17 +774,26 @@ const void *prompt_kernel(bool wide, bool exact) {
 
 // Which kernel.  The one for few rows takes its time by tiles of 16 rows, however they are spread: it cuts long keys over CTAs.  This
 // one takes its time by rounds of CTAs, whose keys are not cut.  Both grow with the keys, so the choice does not need their number:
-// measured (bf16, head_dim 128, 4 heads to a key head, 8,192 keys) a tile of 16 rows costs as much as 1/500 to 1/600 of a round of
-// 148 CTAs.  16 requests x 8 key heads x 64 rows: 185 us there, 167 us here; 32 rows: 79 and 167; one request of 2,048 rows: 333 and
-// 204; 512 rows: 94 and 200.  Short keys leave the other kernel waiting for its starts and joins: at 512 keys and 256 rows of
-// one request it takes 37 us, this one 28; at 128 rows 20 and 21.
-bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long rows) {
+// measured (bf16, head_dim 128, 4 heads to a key head, 8,192 keys) a tile of 16 rows takes 0.39 us, a round of 148 CTAs 167 to 204,
+// with the logarithm 223 to 254: as long as 3.2 or 4.2 tiles per CTA (head_dim 64: 0.23 us, 143 to 171, 186 to 219: 4.2 or 5.4).  16 requests x 8 key heads x 64 rows: 199 us there, 167 (223) us
+// here; 32 rows: 108 and 167 (223); one request of 2,048 rows: 368 and 204 (254); 512 rows: 104 and 200 (253).  Not every request has
+// as many rows as the largest: all of them have no more than max_tokens tokens, and no more than one tile or item each that is
+// not full.  One prompt of 1,024 tokens beside 255 single tokens, 2,000 keys each: 413 us there, 755 (964) here; four of 512
+// beside 60, 4,000 keys: 838 and 482 (619).  Short keys leave the other kernel waiting for its starts and joins: at 512 keys and 256
+// rows of one request it takes 37 us, this one 28 (31); at 128 rows 20 and 22.  (The table's columns stand for the keys, which are on the
+// device.)  A hint of more queries than there are tokens asks for this kernel.
+bool prompt_kernel_serves(const fi_kv *kv, const AttendParams &p, int dtype, long long queries) {
     if (dtype != FI_BF16 || (kv->cfg.head_dim != 64 && kv->cfg.head_dim != 128)) return false;
-    const long long most_keys = (long long)p.max_blocks << p.page_shift;
-    const double heads = (double)p.batch_max * kv->cfg.kv_heads;
-    const double tiles = heads * (double)((rows + 15) / 16), items = heads * (double)((rows + kRows - 1) / kRows);
-    if (tiles > 3.5 * kv->sm_count * (double)(long long)((items + kv->sm_count - 1) / kv->sm_count)) return true;
-    return rows >= 256 && most_keys <= 1024;
+    if (queries > p.max_tokens) return true;
+    const double rows = (double)queries * p.group, all_rows = (double)p.max_tokens * p.group, batch = p.batch_max;
+    const auto blocks = [&](int size) {
+        const double whole = batch * (double)(long long)((rows + size - 1) / size), packed = all_rows / size + batch;
+        return kv->cfg.kv_heads * (whole < packed ? whole : packed);
+    };
+    const double rounds = (double)(long long)((blocks(kRows) + kv->sm_count - 1) / kv->sm_count);
+    const double tiles_a_round = kv->cfg.head_dim == 64 ? (p.lse ? 5.4 : 4.2) : (p.lse ? 4.2 : 3.2);
+    if (blocks(16) > tiles_a_round * kv->sm_count * rounds) return true;
+    return rows >= 256 && all_rows >= 256 * batch && (long long)p.max_blocks << p.page_shift <= 1024;
 }
 
 fi_status_t prepare_attend_prompt(const fi_kv *kv) {

@@ -300,3 +300,25 @@ def test_wider_block_table_keeps_the_results_as_exact():
         out, lse = a.run()
         a.check(out, None, halves=True)
         check_logarithms(a, lse)
+
+
+# --------------------------------------------------------------------------------------------- mixed batches
+
+def test_one_prompt_among_many_single_tokens():
+    """A chunk of a prompt beside requests of one token: the choice of the kernel goes by the tokens there are."""
+    rng = np.random.default_rng(5)
+    lens = [int(x) for x in rng.integers(1, 900, 100)]
+    queries = [1] * 100
+    lens[40], queries[40] = 700, 500
+    a = Attention(lens=lens, queries=queries, q_heads=16, kv_heads=4, dim=128, seed=15, room=2048)
+    out, lse = a.run()
+    a.check(out, lse)
+
+
+def test_prompts_the_rule_gives_to_the_prompt_kernel():
+    """Many rows of many heads, no hint but the true number of queries."""
+    a = Attention(lens=[1500, 1400], queries=[1200, 1100], q_heads=32, kv_heads=4, dim=64, page=64, seed=16)
+    out, lse = a.run()
+    a.check(out, lse, halves=True)
+    again = a.run()
+    assert torch.equal(out[:2300], again[0][:2300]) and torch.equal(lse[:2300], again[1][:2300])
