@@ -55,7 +55,9 @@ class FreezeDecoderLayer:
         q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], 1)
         q, k = fb.head_norm_rope(q, k, self.q_weight, self.k_weight, rope, step.positions, count=count)
         self.kv.append(k, v, step.slot_map)
-        a = self.kv.attend(q, step.lens, self.block_table, cu_tokens=step.cu_tokens, row_idx=rows, batch_count=count)
+        # (a request that found no place, because it is longer than the table or pages are out, sees nothing here)
+        a = self.kv.attend(q, step.lens, self.block_table, cu_tokens=step.cu_tokens, row_idx=rows, batch_count=count,
+                           granted=step.granted)
         return a.reshape(n, -1) @ self.w_out, (q, k, v, a)
 
     def release(self, rows):

@@ -412,7 +412,8 @@ typedef struct {
  * Missing pages are popped from the end of the free stack, in request order.  A request is refused, and keeps its length,
  * when its tokens would need more than max_blocks pages, when they would end past max_tokens, or when it needs pages and
  * the pages wanted by it and by the requests before it exceed the free ones; refused requests keep their places in
- * cu_tokens and positions, with slot -1.  Nothing of a refused request is written to the tables.
+ * cu_tokens and positions, with slot -1.  Nothing of a refused request is written to the tables; its queries mean nothing to
+ * fi_kv_attend, which has to be told (`granted` there).
  * Rows outside [0, rows) and negative lengths are treated as requests without tokens.  Calls of one handle share its
  * counters and must be ordered on one stream.  Asynchronous; no wait on the device, no atomics on results: the same
  * inputs give the same tables.
@@ -533,7 +534,8 @@ fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *args, void *cuda_str
  * cu_tokens[i] queries, the last n of its lens[row] tokens (which are stored already): query j stands at position
  * lens[row] - n + j and sees the keys at positions up to its own, with window > 0 only the last `window` of them.
  *   out = softmax(scale * q . k) v,  q_heads / kv_heads query heads share a key head
- * A query that sees no key (a position below 0) gets zeros, and -inf as lse.
+ * A query that sees no key (a position below 0) gets zeros, and -inf as lse.  So do the queries of a request that fi_pages_extend
+ * refused, when `granted` says so; without it they stand at the request's last stored tokens, which are not theirs.
  *   q, out [max_tokens x q_heads x head_dim], float32 or bfloat16, strides in elements, multiples of 16 bytes;
  *   lse [max_tokens x q_heads] float, contiguous, nullable: natural logarithm of the softmax sum
  *   cu_tokens nullable: one query per request, token i of request i; max_query: most queries of a request (a hint
@@ -555,6 +557,7 @@ typedef struct {
     const int32_t *row_idx;      /* [batch_max] nullable */
     const int32_t *batch_count;  /* [1] nullable */
     const int32_t *cu_tokens;    /* [batch_max + 1] nullable */
+    const int32_t *granted;      /* [batch_max] of fi_pages_extend, nullable */
     int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
     int64_t table_ld;
     int32_t rows;

@@ -88,7 +88,7 @@ class fi_kv_append_t(ctypes.Structure):
 
 
 class fi_kv_attend_t(ctypes.Structure):
-    _fields_ = _fields(ctypes.c_void_p, "q out lse lens block_table row_idx batch_count cu_tokens") \
+    _fields_ = _fields(ctypes.c_void_p, "q out lse lens block_table row_idx batch_count cu_tokens granted") \
         + _fields(ctypes.c_int64, "q_token_stride q_head_stride out_token_stride out_head_stride table_ld") \
         + _fields(ctypes.c_int32, "rows max_blocks batch_max max_tokens max_query window dtype") + [("scale", ctypes.c_float)]
 
@@ -877,9 +877,10 @@ class KvCache:
     def attend(self, q: torch.Tensor, lens: torch.Tensor, block_table: torch.Tensor, *, cu_tokens: Optional[torch.Tensor] = None,
                row_idx: Optional[torch.Tensor] = None, batch_count: Optional[torch.Tensor] = None, max_query: int = 1,
                window: int = 0, scale: Optional[float] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False,
-               lse: Optional[torch.Tensor] = None):
+               lse: Optional[torch.Tensor] = None, granted: Optional[torch.Tensor] = None):
         """Attention of q [tokens, q_heads, head_dim] (the last tokens of each request, which are stored already) over the
-        stored keys and values; scale defaults to 1 / sqrt(head_dim).  Returns out, or (out, lse)."""
+        stored keys and values; scale defaults to 1 / sqrt(head_dim).  Requests that KvTables.extend refused get zeros when its
+        `granted` is given.  Returns out, or (out, lse)."""
         tokens, index, dtype, heads, dim = q.size(0), self._index, q.dtype, self.q_heads, self.head_dim
         kind = _FI_DTYPE.get(dtype)
         if kind is None:
@@ -894,6 +895,7 @@ class KvCache:
             batch = row_idx.numel()
         _check_flat(batch_count, "batch_count", index, 1)
         _check_flat(cu_tokens, "cu_tokens", index, batch + 1)
+        _check_flat(granted, "granted", index, batch)
         if out is None:
             out = torch.empty_like(q)
             out_token, out_head, _ = out.stride()
@@ -905,7 +907,7 @@ class KvCache:
             lse = q.new_empty((tokens, heads), dtype=torch.float32)
         st = self._lib.fi_kv_attend(self._h, _pack_attend(
             q.data_ptr(), out.data_ptr(), _at(lse), lens.data_ptr(), block_table.data_ptr(), _at(row_idx), _at(batch_count),
-            _at(cu_tokens), q_token, q_head, out_token, out_head, block_table.stride(0), rows, block_table.size(1), batch, tokens,
+            _at(cu_tokens), _at(granted), q_token, q_head, out_token, out_head, block_table.stride(0), rows, block_table.size(1), batch, tokens,
             max_query, window, kind, dim ** -0.5 if scale is None else scale), _raw_stream(index))
         if st:
             _check(st)

@@ -146,7 +146,7 @@ __device__ __forceinline__ Request request_of(const AttendParams &p, int i) {
     r.len = r.queries > 0 ? p.lens[r.row] : 0;
     const long long most = (long long)p.max_blocks << p.page_shift;
     if (r.len > most) r.len = (int)most;
-    if (r.len < 0) r.len = 0;
+    if (r.len < 0 || (p.granted && p.granted[i] < r.queries)) r.len = 0;     // (a refused request sees nothing)
     long long lo = 0;
     if (p.window > 0) {
         lo = (long long)max(r.len - r.queries, 0) - p.window + 1;
@@ -1049,7 +1049,7 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     }
     if (a->batch_max == 0 || a->max_tokens == 0) return FI_OK;
     if (!a->q || !a->out || !a->lens || (a->max_blocks > 0 && !a->block_table)) {
-        set_error("fi_kv_attend: null pointer (only lse, row_idx, batch_count and cu_tokens may be)");
+        set_error("fi_kv_attend: null pointer (only lse, row_idx, batch_count, cu_tokens and granted may be)");
         return FI_ERR_INVALID_ARG;
     }
     const int unit = a->dtype == FI_BF16 ? 8 : 4;
@@ -1075,6 +1075,7 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.row_idx = a->row_idx;
     p.batch_count = a->batch_count;
     p.cu_tokens = a->cu_tokens;
+    p.granted = a->granted;
     p.k_codes = static_cast<const unsigned char *>(c.k_codes);
     p.v_codes = static_cast<const unsigned char *>(c.v_codes);
     p.k_meta = static_cast<const uint32_t *>(c.k_meta);

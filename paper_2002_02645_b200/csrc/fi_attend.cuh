@@ -20,7 +20,7 @@ struct AttendParams {
     const void *q;
     void *out;
     float *lse;
-    const int32_t *lens, *block_table, *row_idx, *batch_count, *cu_tokens;
+    const int32_t *lens, *block_table, *row_idx, *batch_count, *cu_tokens, *granted;
     const unsigned char *k_codes, *v_codes;
     const uint32_t *k_meta, *v_meta;
     float *partial;

@@ -252,7 +252,7 @@ __device__ __forceinline__ bool next_item(const AttendParams &p, ItemWalk &w, It
         const long long most = (long long)p.max_blocks << p.page_shift;
         x.len = p.lens[x.row];
         if (x.len > most) x.len = (int)most;
-        if (x.len < 0) x.len = 0;
+        if (x.len < 0 || (p.granted && p.granted[i] < x.queries)) x.len = 0;     // (a refused request sees nothing)
         const int before = x.len - x.queries, first = before + x.row0 / p.group;
         x.first_key = p.window > 0 ? max(max(first, 0) - p.window + 1, 0) / kTile * kTile : 0;
 #pragma unroll

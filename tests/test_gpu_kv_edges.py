@@ -302,6 +302,54 @@ def test_wider_block_table_keeps_the_results_as_exact():
         check_logarithms(a, lse)
 
 
+# ------------------------------------------------------------------------------------------------- refused requests
+
+@BOTH
+@pytest.mark.parametrize("prompt", [False, True])
+def test_refused_requests_get_zeros_through_the_whole_layer(prompt, dtype):
+    """Too few pages: some requests are refused, between granted ones.  Their queries see nothing, as the attention call is told by
+    `granted`; the others are as without them."""
+    page, blocks, batch, heads, dim = 16, 8, 7, 2, 64
+    gen = torch.Generator(device=DEV).manual_seed(21)
+    kv = fb.KvCache(*pools(9, heads, page, dim), *pools(9, heads, page, dim), q_heads=4)
+    tables = fb.KvTables(page_size=page, max_blocks=blocks, max_batch=batch)
+    table = torch.full((batch, blocks), -1, dtype=torch.int32, device=DEV)
+    free, count, lens = ints(list(range(9))), ints([9]), ints([0] * batch)
+    news = [[20, 3, 40, 1, 16, 0, 5], [30, 2, 9, 1, 60, 1, 1]]
+    stored = [[] for _ in range(batch)]
+    for new in news:
+        total = sum(new)
+        step = tables.extend(lens, free, count, table, new_lens=ints(new), max_tokens=total)
+        k, v = torch.randn(2, total, heads, dim, generator=gen, device=DEV).to(dtype)
+        q = torch.randn(total, 4, dim, generator=gen, device=DEV).to(dtype)
+        granted = step.granted.tolist()
+        for i, n in enumerate(new):
+            if n and not granted[i]:
+                q[step.cu_tokens[i]:step.cu_tokens[i + 1]] = math.nan          # a position past the rope table gives this
+        ks, vs = kv.append(k, v, step.slot_map, with_stored=True)
+        out, lse = kv.attend(q, step.lens, table, cu_tokens=step.cu_tokens, granted=step.granted, with_lse=True,
+                             max_query=MANY if prompt else max(new))
+        cu = step.cu_tokens.tolist()
+        for i, n in enumerate(new):
+            at = slice(cu[i], cu[i + 1])
+            if granted[i] < n:
+                assert (out[at] == 0).all() and (lse[at] == -math.inf).all()
+                continue
+            stored[i] += [(ks[t].double(), vs[t].double()) for t in range(cu[i], cu[i + 1])]
+            for j in range(n):
+                see = stored[i][:len(stored[i]) - n + j + 1]
+                kk, vv = torch.stack([s[0] for s in see]), torch.stack([s[1] for s in see])
+                x = torch.einsum("hgd,thd->hgt", q[cu[i] + j].double().view(heads, 2, dim), kk) / 8
+                want = torch.einsum("hgt,thd->hgd", torch.softmax(x, -1), vv).reshape(4, dim)
+                # `stored` is rounded to bf16 (2^-8 of numbers up to 4): scores move by 2^-8 of their parts, values by 2^-8 of theirs
+                assert (out[cu[i] + j].double() - want).abs().max() <= 2.0 ** -8 * (4 + 2 * 8 * 4)
+        lens, count = step.lens, step.free_count
+    assert 0 in granted and max(granted) > 0
+    kv.poll_status()
+    with pytest.raises(ValueError):
+        kv.attend(q, lens, table, cu_tokens=step.cu_tokens, granted=step.granted[:3])
+
+
 # --------------------------------------------------------------------------------------------- mixed batches
 
 def test_one_prompt_among_many_single_tokens():
