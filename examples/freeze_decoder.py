@@ -3,8 +3,9 @@
 Every layer first looks its input up in its freeze cache; the requests that it freezes skip the layer and all later ones,
 the others (known on the device only) run it: their query, key and value heads are normed and rotated, a place is found in the
 layer's paged key/value store, keys and values are stored there in 4 bits, and the queries attend to what is stored.  A
-request that was frozen before a layer leaves no token there, so every layer has its own lengths and page tables.  No call
-waits for the host: a step could be captured in a CUDA graph.
+request that was frozen before a layer leaves no token there, so every layer has its own lengths and page tables; a
+token's angle goes by its place in the request, not in a layer's store, which has holes where the request was frozen.  No
+call waits for the host.
 
     python examples/freeze_decoder.py [steps]
 """
@@ -44,16 +45,16 @@ class FreezeDecoderLayer:
         self.out.lens.zero_()
         self.out.free_count.fill_(pages)
 
-    def run(self, x, rope, rows, count):
-        """x [requests, hidden]: the survivors' activations, in the order of `rows` ([requests], `count` of them real).
-        Returns what the layer adds to them (rows past the count hold anything) and what its attention saw."""
+    def run(self, x, rope, positions, rows, count):
+        """x [requests, hidden]: the survivors' activations, in the order of `rows` ([requests], `count` of them real), at
+        `positions` in their requests.  Returns what the layer adds to them (rows past the count hold anything) and what its attention saw."""
         n = x.shape[0]
         step = self.tables.extend(self.out.lens, self.free_pages, self.out.free_count, self.block_table, row_idx=rows,
                                   batch_count=count, out=self.out)             # lengths and free count are updated in place
         normed = torch.nn.functional.rms_norm(x.float(), x.shape[1:]).to(x.dtype)
         qkv = (normed @ self.w_qkv).view(n, self.heads + 2 * self.kv_heads, self.head_dim)
         q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], 1)
-        q, k = fb.head_norm_rope(q, k, self.q_weight, self.k_weight, rope, step.positions, count=count)
+        q, k = fb.head_norm_rope(q, k, self.q_weight, self.k_weight, rope, positions, count=count)
         self.kv.append(k, v, step.slot_map)
         # (a request that found no place, because it is longer than the table or pages are out, sees nothing here)
         a = self.kv.attend(q, step.lens, self.block_table, cu_tokens=step.cu_tokens, row_idx=rows, batch_count=count,
@@ -76,6 +77,8 @@ class FreezeDecoder:
         self.rope = torch.cat([angles.cos(), angles.sin()], 1).contiguous()
         self.requests, self.hidden, self.device = requests, hidden, torch.device(device)
         self.slots = torch.arange(requests, device=device)
+        self.max_keys, self.steps = max_keys, 0
+        self.positions = torch.zeros(requests + 1, dtype=torch.int32, device=device)    # of each request's next token
 
     def calibrate(self, h, share):
         """Sets every layer's threshold so that it would freeze `share` of the requests at the activations that reach it."""
@@ -83,13 +86,15 @@ class FreezeDecoder:
         count = torch.full((1,), self.requests, dtype=torch.int32, device=self.device)
         for layer in self.layers:
             layer.cache.set_threshold(float(layer.cache.lookup_batch(h).conf.quantile(1 - share)))
-            h = h + layer.run(h, self.rope, rows, count)[0]
+            h = h + layer.run(h, self.rope, self.positions, rows, count)[0]
         for layer in self.layers:
             layer.release(rows)
 
     def step(self, h, observe=None):
         """One token of every request: h [requests, hidden] bf16 -> (h behind the layers, CascadeState with labels, exit stages and
         confidences).  A frozen request's h stays what the layer that froze it was given."""
+        if self.steps == self.max_keys:
+            raise RuntimeError(f"a request has room for {self.max_keys} tokens")
         state = fb.CascadeState(self.requests, self.device)
         fb.cascade_init(state, len(self.layers))
         work = torch.cat([h, h[:1]])                                            # one row more, for slots without a request
@@ -98,17 +103,19 @@ class FreezeDecoder:
             rows, count = state.survivors(i)
             here = torch.where(self.slots < count, rows, self.requests).long()
             x = work[here]
-            y, seen = layer.run(x, self.rope, rows, count)
+            y, seen = layer.run(x, self.rope, self.positions[here], rows, count)
             if observe:
                 observe(i, rows, count, *seen)
             work[here] = x + y
+        self.positions += 1
+        self.steps += 1
         return work[:-1], state
 
 
 def main():
     steps = int(sys.argv[1]) if len(sys.argv) > 1 else 64
     torch.manual_seed(0)
-    model = FreezeDecoder()
+    model = FreezeDecoder(max_keys=max(256, steps))
     h = torch.randn(model.requests, model.hidden, device=model.device).to(torch.bfloat16)
     model.calibrate(h, 0.1)
     frozen = torch.zeros(len(model.layers) + 1, dtype=torch.int64)

@@ -394,7 +394,8 @@ typedef struct {
     const int32_t *batch_count; /* [1] requests of the step (<= batch_max); nullable: batch_max */
     const int32_t *new_lens;    /* [batch_max] new tokens of each request; nullable: one each */
     int64_t *slot_map;          /* out [max_tokens] slot of each new token, -1 where there is none */
-    int32_t *positions;         /* out [max_tokens] its index in this layer's store, -1 past the last token */
+    int32_t *positions;         /* out [max_tokens] its index in this layer's store, -1 past the last token.  Where requests may be
+                                   frozen the store has holes, and this is not the token's place in the request: a rotation goes by that */
     int32_t *cu_tokens;         /* out [batch_max + 1] first token of each request; constant past the actual batch */
     int32_t *granted;           /* out [batch_max] tokens that got their place: new_lens or, when refused, 0 */
     int32_t *lens_out;          /* out [rows] lengths after the step; may be `lens` itself */
@@ -532,7 +533,8 @@ fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *args, void *cuda_str
 /*
  * Attention of new tokens over the stored keys and values.  Request i (row row_idx[i]) has n = cu_tokens[i + 1] -
  * cu_tokens[i] queries, the last n of its lens[row] tokens (which are stored already): query j stands at position
- * lens[row] - n + j and sees the keys at positions up to its own, with window > 0 only the last `window` of them.
+ * lens[row] - n + j and sees the keys at positions up to its own, with window > 0 only the last `window` of them (stored keys are
+ * counted: tokens that were frozen before this layer are none).
  *   out = softmax(scale * q . k) v,  q_heads / kv_heads query heads share a key head
  * A query that sees no key (a position below 0) gets zeros, and -inf as lse.  So do the queries of a request that fi_pages_extend
  * refused, when `granted` says so; without it they stand at the request's last stored tokens, which are not theirs.
