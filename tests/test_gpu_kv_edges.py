@@ -370,3 +370,25 @@ def test_prompts_the_rule_gives_to_the_prompt_kernel():
     a.check(out, lse, halves=True)
     again = a.run()
     assert torch.equal(out[:2300], again[0][:2300]) and torch.equal(lse[:2300], again[1][:2300])
+
+
+# ---------------------------------------------------------------------------------------------- a single token's strides
+
+@BOTH
+def test_single_tokens_may_have_any_token_stride(dtype):
+    """The distance to a next token that is not there does not matter, whatever number the tensor has for it."""
+    flat = torch.randn(4 * 64, device=DEV).to(dtype)
+    odd = flat.as_strided((1, 4, 64), (4 * 64 + 3, 64, 1))
+    plain = flat.view(1, 4, 64)
+    w = torch.ones(64, device=DEV)
+    for args in ((odd, None), (odd, odd), (plain, odd)):
+        q, k = fb.head_norm_rope(*args, w, w, None, None)
+        want, _ = fb.head_norm_rope(plain, None, w, None, None, None)
+        assert torch.equal(q, want) and (k is None or torch.equal(k, want))
+    got = fb.head_norm_rope_backward(odd, odd, w, w, None, None, odd, odd)
+    ref = fb.head_norm_rope_backward(plain, plain, w, w, None, None, plain, plain)
+    assert all(torch.equal(x, y) for x, y in zip(got, ref))
+    kv = fb.KvCache(*pools(2, 4, 16, 64), *pools(2, 4, 16, 64), q_heads=4)
+    kv.append(odd, odd, ints([0], torch.int64))
+    table = ints([[0, 1]])
+    assert torch.equal(kv.attend(odd, ints([1]), table), kv.attend(plain, ints([1]), table))
