@@ -786,7 +786,13 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optiona
                    k_weight: Optional[torch.Tensor], rope: Optional[torch.Tensor], positions: Optional[torch.Tensor], *,
                    eps: float = 1e-6, interleaved: bool = False, count: Optional[torch.Tensor] = None,
                    q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
-    """fi_head_norm_rope: (q, k) normed head by head and turned to their positions.  q_out / k_out may be q / k."""
+    """fi_head_norm_rope: (q, k) normed head by head and turned to their positions.  q_out / k_out may be q / k.  Gradients flow to
+    q, k and the weights; results that are given have none, so they are refused where one is asked for."""
+    if (q.requires_grad or k is not None and k.requires_grad or q_weight is not None and q_weight.requires_grad
+            or k_weight is not None and k_weight.requires_grad) and torch.is_grad_enabled():
+        if q_out is not None or k_out is not None:
+            raise ValueError("q_out and k_out are given, but a gradient is asked for")
+        return _HeadNormRope.apply(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count)
     return _norm_rope_call(load_library().fi_head_norm_rope, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
                            q_out, k_out)
 
@@ -812,8 +818,36 @@ def head_norm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], q_weight
     return dq, dk, dqw, dkw
 
 
+def _as_heads(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy that the kernels read: values of a head side by side, heads on 16-byte boundaries."""
+    unit = 16 // t.element_size()
+    ok = t.stride(2) == 1 and t.data_ptr() % 16 == 0 and t.stride(0) % unit == 0 and t.stride(1) % unit == 0
+    return t if ok else t.clone(memory_format=torch.contiguous_format)
+
+
+class _HeadNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count):
+        ctx.save_for_backward(q, k, q_weight, k_weight, rope, positions, count)
+        ctx.eps, ctx.interleaved = eps, interleaved
+        return _norm_rope_call(load_library().fi_head_norm_rope, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
+                               None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight, rope, positions, count = ctx.saved_tensors
+        # tokens past the count have no gradient, and the kernel leaves them alone
+        dq, dk = (None if t is None or count is None else torch.zeros_like(t) for t in (q, k))
+        dq, dk, dqw, dkw = head_norm_rope_backward(q, k, q_weight, k_weight, rope, positions, _as_heads(dq_out),
+                                                   None if k is None else _as_heads(dk_out), eps=ctx.eps,
+                                                   interleaved=ctx.interleaved, count=count, dq=dq, dk=dk)
+        dqw, dkw = (None if d is None else d.view_as(w) for d, w in ((dqw, q_weight), (dkw, k_weight)))
+        return dq, dk, dqw, dkw, None, None, None, None, None
+
+
 class KvCache:
-    """Keys and values of one layer in 4 bits (fi_kv_*) over pools the caller owns: codes uint8 [pages, kv_heads, page_size,
+    """Keys and values of one layer in 4 bits (fi_kv_*; for inference: the calls give no gradients) over pools the caller owns: codes uint8 [pages, kv_heads, page_size,
     head_dim / 2], meta bfloat16 [pages, kv_heads, page_size, 2] (scale, offset)."""
 
     def __init__(self, k_codes: torch.Tensor, k_meta: torch.Tensor, v_codes: torch.Tensor, v_meta: torch.Tensor, *, q_heads: int):

@@ -392,3 +392,39 @@ def test_single_tokens_may_have_any_token_stride(dtype):
     kv.append(odd, odd, ints([0], torch.int64))
     table = ints([[0, 1]])
     assert torch.equal(kv.attend(odd, ints([1]), table), kv.attend(plain, ints([1]), table))
+
+
+# ---------------------------------------------------------------------------------------------------------- gradients
+
+@BOTH
+def test_head_norm_rope_takes_part_in_backpropagation(dtype):
+    gen = torch.Generator(device=DEV).manual_seed(31)
+    qkv = torch.randn(9, 8, 64, generator=gen, device=DEV).to(dtype).requires_grad_()
+    wq, wk = ((1 + 0.1 * torch.randn(64, generator=gen, device=DEV)).requires_grad_() for _ in range(2))
+    angle = torch.rand(50, 16, generator=gen, device=DEV)
+    rope = torch.cat([angle.cos(), angle.sin()], 1)
+    pos = torch.randint(0, 50, (9,), generator=gen, device=DEV, dtype=torch.int32)
+    q, k, _ = qkv.split([5, 2, 1], 1)
+    yq, yk = fb.head_norm_rope(q, k, wq, wk, rope, pos, eps=1e-5, interleaved=True)
+    aq, ak = (torch.randn(t.shape, generator=gen, device=DEV).to(dtype) for t in (yq, yk))
+    ((yq * aq).sum() + (yk * ak).sum()).backward()
+    with torch.no_grad():
+        dq, dk, dwq, dwk = fb.head_norm_rope_backward(q, k, wq, wk, rope, pos, aq, ak, eps=1e-5, interleaved=True)
+        same = fb.head_norm_rope(q, k, wq, wk, rope, pos, eps=1e-5, interleaved=True)
+    assert torch.equal(same[0], yq) and torch.equal(same[1], yk) and not same[0].requires_grad
+    assert torch.equal(qkv.grad[:, :5], dq) and torch.equal(qkv.grad[:, 5:7], dk) and (qkv.grad[:, 7] == 0).all()
+    assert torch.equal(wq.grad, dwq) and torch.equal(wk.grad, dwk)
+    # only one result is used, only the weights learn, no keys
+    wq.grad = wk.grad = None
+    fb.head_norm_rope(q.detach(), k.detach(), wq, wk, rope, pos)[0].float().sum().backward()
+    assert wq.grad is not None and (wk.grad is None or (wk.grad == 0).all())
+    x = torch.randn(3, 2, 64, generator=gen, device=DEV).to(dtype).requires_grad_()
+    fb.head_norm_rope(x, None, None, None, None, None)[0].float().square().sum().backward()
+    assert x.grad.isfinite().all()
+    # tokens past the count: no gradient, whatever is in theirs
+    x.grad = None
+    y = fb.head_norm_rope(x, None, None, None, None, None, count=ints([2]))[0]
+    y.backward(torch.full_like(y, math.nan).index_fill_(0, ints([0, 1], torch.int64), 1.0))
+    assert x.grad[:2].isfinite().all() and (x.grad[2] == 0).all()
+    with pytest.raises(ValueError):             # results written in place keep no way back
+        fb.head_norm_rope(q, None, wq, None, None, None, q_out=torch.empty_like(q))
