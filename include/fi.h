@@ -446,7 +446,7 @@ fi_status_t fi_pages_release(fi_pages_t *pages, const int32_t *row_idx, int32_t 
  *   they may be q / k themselves.  q_weight, k_weight [head_dim] float, nullable (ones).  positions [tokens] int32; a
  *   position outside [0, max_pos) gives NaN (the table is not read there).
  *   tokens_dev [1] device int32, nullable: actual number of tokens (<= tokens); later rows are left untouched.
- * Pointers and strides are multiples of 16 bytes; head_dim and rot_dim multiples of 16, 16 <= head_dim <= 256,
+ * Pointers and strides (between two or more) are multiples of 16 bytes; head_dim and rot_dim multiples of 16, 16 <= head_dim <= 256,
  * 0 <= rot_dim <= head_dim; q_heads >= 1, k_heads >= 0.  Asynchronous, on the current device.
  *
  * fi_head_norm_rope_backward: gradients for dy = (dq_out, dk_out), from the same x (nothing of the forward is kept):

@@ -614,14 +614,7 @@ def _check_heads(t: torch.Tensor, name: str, index: int, dtype, tokens: int, hea
     token, head, value = t.stride()
     if value != 1:
         raise ValueError(f"{name}: the values of a head must lie side by side")
-    return token if tokens > 1 else 0, head if heads > 1 else 0     # (the stride of a single token or head may be anything)
-
-
-def _new_like(t: torch.Tensor):
-    """A result as t is laid out, and its strides between tokens and between heads."""
-    r = torch.empty_like(t)
-    token, head, _ = r.stride()
-    return r, token if t.size(0) > 1 else 0, head if t.size(1) > 1 else 0
+    return token, head
 
 
 def _check_table(block_table: torch.Tensor, rows: int, blocks: int, index: int) -> None:
@@ -740,7 +733,8 @@ def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interlea
     tokens, q_heads, dim = q.shape
     strides = _check_heads(q, "q", index, dtype, tokens, q_heads, dim)
     if q_res is None:
-        q_res, *res_strides = _new_like(q)
+        q_res = torch.empty_like(q)
+        res_strides = q_res.stride()[:2]
     else:
         res_strides = _check_heads(q_res, "result for q", index, dtype, tokens, q_heads, dim)
     k_heads, k_strides, k_res_strides, dk_strides = 0, (0, 0), (0, 0), (0, 0)
@@ -748,7 +742,8 @@ def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interlea
         k_heads = k.size(1) if k.dim() == 3 else 0
         k_strides = _check_heads(k, "k", index, dtype, tokens, k_heads, dim)
         if k_res is None:
-            k_res, *k_res_strides = _new_like(k)
+            k_res = torch.empty_like(k)
+            k_res_strides = k_res.stride()[:2]
         else:
             k_res_strides = _check_heads(k_res, "result for k", index, dtype, tokens, k_heads, dim)
     else:
@@ -936,7 +931,8 @@ class KvCache:
         _check_flat(cu_tokens, "cu_tokens", index, batch + 1)
         _check_flat(granted, "granted", index, batch)
         if out is None:
-            out, out_token, out_head = _new_like(q)
+            out = torch.empty_like(q)
+            out_token, out_head, _ = out.stride()
         else:
             out_token, out_head = _check_heads(out, "out", index, dtype, tokens, heads, dim)
         if lse is not None:

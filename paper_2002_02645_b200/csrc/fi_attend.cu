@@ -1053,9 +1053,9 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
         return FI_ERR_INVALID_ARG;
     }
     const int unit = a->dtype == FI_BF16 ? 8 : 4;
-    if ((reinterpret_cast<uintptr_t>(a->q) & 15) || (reinterpret_cast<uintptr_t>(a->out) & 15) || a->q_token_stride % unit ||
-        a->q_head_stride % unit || a->out_token_stride % unit || a->out_head_stride % unit || a->q_token_stride < 0 ||
-        a->q_head_stride < 0 || a->out_token_stride < 0 || a->out_head_stride < 0) {
+    const auto bad = [&](int64_t stride, int count) { return count > 1 && (stride < 0 || stride % unit != 0); };
+    if ((reinterpret_cast<uintptr_t>(a->q) & 15) || (reinterpret_cast<uintptr_t>(a->out) & 15) || bad(a->q_token_stride, a->max_tokens) ||
+        bad(a->out_token_stride, a->max_tokens) || bad(a->q_head_stride, kv->cfg.q_heads) || bad(a->out_head_stride, kv->cfg.q_heads)) {
         set_error("fi_kv_attend: heads must start on 16-byte boundaries, strides must not be negative");
         return FI_ERR_INVALID_ARG;
     }

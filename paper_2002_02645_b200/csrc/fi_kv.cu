@@ -784,9 +784,9 @@ fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *a, void *cuda_stream
         return FI_ERR_INVALID_ARG;
     }
     const int unit = a->dtype == FI_BF16 ? 8 : 4;
-    if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->k_stored) || !aligned16(a->v_stored) || a->k_token_stride % unit ||
-        a->k_head_stride % unit || a->v_token_stride % unit || a->v_head_stride % unit || a->k_token_stride < 0 ||
-        a->k_head_stride < 0 || a->v_token_stride < 0 || a->v_head_stride < 0) {
+    const auto bad = [&](int64_t stride, int64_t count) { return count > 1 && (stride < 0 || stride % unit != 0); };
+    if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->k_stored) || !aligned16(a->v_stored) || bad(a->k_token_stride, a->tokens) ||
+        bad(a->v_token_stride, a->tokens) || bad(a->k_head_stride, kv->cfg.kv_heads) || bad(a->v_head_stride, kv->cfg.kv_heads)) {
         set_error("fi_kv_append: vectors must start on 16-byte boundaries, strides must not be negative");
         return FI_ERR_INVALID_ARG;
     }

@@ -461,7 +461,10 @@ fi_status_t check_norm_args(const fi_head_norm_rope_t *a, bool backward, const c
     bool ok = norm_aligned(a->q) && norm_aligned(a->q_out) && (!k || (norm_aligned(a->k) && norm_aligned(a->k_out))) &&
               norm_aligned(a->q_weight) && norm_aligned(a->k_weight) && norm_aligned(a->rope) &&
               (!backward || (norm_aligned(a->dq_out) && (!k || norm_aligned(a->dk_out)) && norm_aligned(a->workspace)));
-    for (int64_t s : strides) ok = ok && s >= 0 && s % unit == 0;
+    for (int i = 0; i < 12; ++i) {     // (strides between tokens and between heads in turn; of a single one it may be anything)
+        const int64_t count = i % 2 == 0 ? a->tokens : i % 4 == 1 ? a->q_heads : a->k_heads;
+        ok = ok && (count <= 1 || (strides[i] >= 0 && strides[i] % unit == 0));
+    }
     if (!ok) {
         set_error("%s: heads, weights and the rope table must start on 16-byte boundaries, strides must not be negative", name);
         return FI_ERR_INVALID_ARG;
