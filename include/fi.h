@@ -573,6 +573,11 @@ typedef struct {
 } fi_kv_attend_t;
 fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *args, void *cuda_stream);
 
+/* Limit in SM cycles of the waits inside the attention kernels of this handle, for calls made from now on; 0 puts the default
+ * back (8e9, about 4 s, also the most).  A wait that runs out ends the kernel with results that mean nothing, and
+ * fi_kv_poll_status says so; nothing faults, traps or hangs.  For tests: no wait runs out by itself. */
+fi_status_t fi_kv_set_wait_limit(fi_kv_t *kv, int64_t limit_cycles);
+
 /* Synchronise the device; FI_ERR_INVALID_ARG when a kernel of this handle met a slot or a page outside the pool since the
  * last poll (the word is cleared), FI_ERR_TIMEOUT when a bounded wait inside one ran out, FI_OK otherwise. */
 fi_status_t fi_kv_poll_status(fi_kv_t *kv);

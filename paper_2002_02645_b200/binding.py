@@ -32,7 +32,7 @@ EXPORTS = ["fi_cache_create", "fi_cache_destroy", "fi_cache_insert", "fi_cache_s
            "fi_cache_read_slot_certificates", "fi_cache_lookup_view", "fi_cache_set_sm_limit", "fi_gemm_plan_describe",
            "fi_pages_create", "fi_pages_destroy", "fi_pages_extend", "fi_pages_release", "fi_head_norm_rope",
            "fi_head_norm_rope_backward", "fi_head_norm_rope_workspace", "fi_kv_create", "fi_kv_destroy", "fi_kv_append",
-           "fi_kv_attend", "fi_kv_poll_status", "fi_launch_count", "fi_last_error", "fi_status_string"]
+           "fi_kv_attend", "fi_kv_set_wait_limit", "fi_kv_poll_status", "fi_launch_count", "fi_last_error", "fi_status_string"]
 
 
 class fi_cache_config_t(ctypes.Structure):
@@ -167,6 +167,7 @@ def load_library(path: Optional[str] = None):
     lib.fi_kv_destroy.argtypes = [vp]
     lib.fi_kv_append.argtypes = [vp, ctypes.c_char_p, vp]           # a packed fi_kv_append_t
     lib.fi_kv_attend.argtypes = [vp, ctypes.c_char_p, vp]           # a packed fi_kv_attend_t
+    lib.fi_kv_set_wait_limit.argtypes = [vp, i64]
     lib.fi_kv_poll_status.argtypes = [vp]
     lib.fi_launch_count.argtypes = []
     lib.fi_launch_count.restype = i64
@@ -879,6 +880,12 @@ class KvCache:
             self.close()
         except Exception:
             pass
+
+    # -- fi_kv_set_wait_limit
+    def set_wait_limit(self, limit_cycles: int = 0) -> None:
+        """Limit of the waits inside attend's kernels in SM cycles (0: the default); past it the next poll_status() raises
+        FI_ERR_TIMEOUT."""
+        _check(self._lib.fi_kv_set_wait_limit(self._h, int(limit_cycles)))
 
     # -- fi_kv_poll_status
     def poll_status(self) -> None:

@@ -1104,6 +1104,7 @@ extern "C" fi_status_t fi_kv_attend(fi_kv_t *kv, const fi_kv_attend_t *a, void *
     p.kv_heads = c.kv_heads;
     p.group = c.q_heads / c.kv_heads;
     p.scale_log2 = a->scale * kLog2e;
+    p.wait_limit = kv->wait_limit;
     const bool f32 = a->dtype == FI_F32;
     const long long per_request = a->cu_tokens ? (a->max_query < 1 ? 1 : a->max_query) : 1;
     const long long rows = per_request * p.group;

@@ -33,6 +33,7 @@ struct AttendParams {
     int rows, max_blocks, batch_max, max_tokens, window;
     int num_pages, page_shift, kv_heads, group;
     float scale_log2;                                 // scale * log2(e)
+    long long wait_limit;                             // SM cycles
 };
 
 __device__ __forceinline__ float ex2(float x) {

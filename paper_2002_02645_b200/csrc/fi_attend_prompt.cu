@@ -23,7 +23,7 @@
 // softmax sum's logarithm is a float32 number, which was off by up to 8e-4 where few keys count.  So when it is wanted, the
 // codes go into the product as they are, less 7.5 (exact), and the scores take each key's scale and offset behind it:
 //   y = (S c) s + (m + 7.5 s) (scale log2(e) sum(q)) + F
-// The case above takes 471 us then.  (One pass over S instead of two, with the maximum checked afterwards: 489 us, as it has to wait for the
+// The case above takes 462 us then.  (One pass over S instead of two, with the maximum checked afterwards: 489 us, as it has to wait for the
 // product before.  Keys as two halves, in two products: 535 us.)
 #include "fi_attend.cuh"
 
@@ -36,13 +36,15 @@ constexpr int kSoftmaxWarps = 8;           // warp w reads TMEM lanes 32 (w mod 
 constexpr int kUnpackWarps = 4;            // for the keys, and as many for the values
 constexpr int kProductWarp = kSoftmaxWarps + 2 * kUnpackWarps;
 constexpr int kPromptThreads = (kProductWarp + 1) * 32;
-constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
+constexpr long long kShortLimit = 1 << 20;       // SM cycles (about 0.5 ms): limits below it are a test's
+constexpr long long kDrainLimit = 200000000ll;   // (about 0.1 s)
 constexpr int kTmemCols = 512;             // S of both halves, O of both
 
 struct PromptCtl {
     uint64_t k_full, k_empty, v_full, v_empty, q_full;
     uint64_t k_info[4], v_info[4];         // a tile's powers (EXACT: scales and offsets): known before its keys and values have a place
     uint64_t s_full[2], p_full[2], pv_done[2];                      // of the halves
+    uint64_t drained;                      // every product that was issued is over
     float k_power[4], v_power[4];          // 2^E of a tile's keys; F of its values
     uint32_t hidden[4][kUnpackWarps];      // keys of a tile whose page is not in the pool, a bit each
     uint32_t red[2][2][kUnpackWarps];      // largest key and value of a tile, by warp
@@ -81,22 +83,26 @@ __device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
     return ok != 0;
 }
 
-// Bounded wait.  When it gives up, every later wait of the CTA does so at once: the kernel runs to its end with whatever is
-// in its buffers, and the status word says that the results are not valid.
-__device__ __forceinline__ void bar_wait(uint64_t *bar, uint32_t parity, PromptCtl *ctl, int32_t *status) {
-    if (bar_try(bar, parity)) return;
+// Bounded wait.  When it gives up, every later wait of the CTA does so at once: no more products are issued, the kernel runs to its
+// end with whatever is in its buffers, and the status word says that the results are not valid.  What a wait does when it is not over
+// at once is one copy of code: in line it took the registers of the loops (399 us, not 385).
+__device__ __noinline__ bool bar_wait_long(uint64_t *bar, uint32_t parity, PromptCtl *ctl, int32_t *status, long long limit) {
     const long long t0 = clock64();
     for (uint32_t spins = 1;; ++spins) {
-        if (bar_try(bar, parity)) return;
+        if (bar_try(bar, parity)) return true;
         if ((spins & 255) == 0) {
-            if (ctl->gave_up) return;
-            if (clock64() - t0 > kWaitLimit) {
+            if (ctl->gave_up) return false;
+            if (clock64() - t0 > limit) {
                 ctl->gave_up = 1;
                 atomicOr(status, 4);
-                return;
+                return false;
             }
         }
     }
+}
+
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, PromptCtl *ctl, const AttendParams &p) {
+    return bar_try(bar, parity) || bar_wait_long(bar, parity, ctl, p.status, p.wait_limit);
 }
 
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -287,6 +293,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             bar_init(&ctl->v_info[i], 1);
         }
         bar_init(&ctl->q_full, kSoftmaxWarps * 32);
+        bar_init(&ctl->drained, 1);
         for (int h = 0; h < 2; ++h) {
             bar_init(&ctl->s_full[h], 1);
             bar_init(&ctl->p_full[h], kSoftmaxWarps * 16);
@@ -308,6 +315,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
     if (p.batch_count) walk.n = min(max(*p.batch_count, 0), p.batch_max);
     Item x;
     uint32_t tiles_before = 0;             // of the items before: parities follow from it
+
+    // so that a wait runs out for certain: nothing completes this barrier yet, and the products wait for this thread
+    if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->drained, 0, ctl, p);
 
     if (warp < kSoftmaxWarps) {
         // ---- a thread per query row ----
@@ -386,12 +396,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             float top = kNoMax, sum = 0.f;
             for (int t = 0; t < all; ++t) {
                 const uint32_t n = tiles_before + t;
-                bar_wait(&ctl->k_info[n & 3], (n >> 2) & 1, ctl, p.status);   // the tile's powers
-                bar_wait(&ctl->v_info[n & 3], (n >> 2) & 1, ctl, p.status);
+                bar_wait(&ctl->k_info[n & 3], (n >> 2) & 1, ctl, p);   // the tile's powers
+                bar_wait(&ctl->v_info[n & 3], (n >> 2) & 1, ctl, p);
                 if (t >= mine) {
                     // A tile for the other half.  It is counted through here too, and not before its values are there: two phases of
                     // p_full completed ahead of the thread that waits for them would look like none.
-                    bar_wait(&ctl->v_full, n & 1, ctl, p.status);
+                    bar_wait(&ctl->v_full, n & 1, ctl, p);
                     bar_arrive(&ctl->p_full[half]);
                     continue;
                 }
@@ -400,7 +410,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 const float ck = EXACT ? 1.f : fminf(fmaxf(c * ctl->k_power[n & 3], FLT_MIN), FLT_MAX), fv = ctl->v_power[n & 3];
                 const uint32_t lost = ctl->hidden[n & 3][0] | ctl->hidden[n & 3][1] | ctl->hidden[n & 3][2] | ctl->hidden[n & 3][3];
                 const bool edge = key0 + kTile > all_high || key0 < all_low || lost != 0;
-                bar_wait(&ctl->s_full[half], steps & 1, ctl, p.status);
+                bar_wait(&ctl->s_full[half], steps & 1, ctl, p);
                 tc_after();
                 // 32 scores from column c0 on, hidden ones at -infinity
                 uint32_t s[32];
@@ -450,7 +460,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 if constexpr (EXACT) tmem_store_wait();
                 else most = fmaf(most, ck, fv);
                 // the products have read the weights before and added them up
-                if (t > 0) bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p.status);
+                if (t > 0) bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p);
                 if (__any_sync(0xffffffffu, most > top + kMost)) {
                     const float m = fmaxf(most - kStart, top), shrink = ex2(top - m);
                     top = m;
@@ -502,7 +512,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             }
             tiles_before += all;
             if (mine > 0) {
-                bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p.status);
+                bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p);
                 tc_after();
             }
             const float scale = sum != 0.f ? 1.f / sum : 0.f;
@@ -588,7 +598,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 if (lane == 0) ctl->hidden[n & 3][uw] = gone;
                 __syncwarp();
                 if (lane == 0) bar_arrive(&ctl->k_info[n & 3]);
-                bar_wait(&ctl->k_empty, (n & 1) ^ 1, ctl, p.status);
+                bar_wait(&ctl->k_empty, (n & 1) ^ 1, ctl, p);
                 unsigned char *const to = smem + S::k + u * 128;
 #pragma unroll
                 for (int i = 0; i < D / 8; ++i) {
@@ -657,7 +667,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                     ctl->v_power[n & 3] = (float)e;
                     bar_arrive(&ctl->v_info[n & 3]);
                 }
-                bar_wait(&ctl->v_empty, (n & 1) ^ 1, ctl, p.status);
+                bar_wait(&ctl->v_empty, (n & 1) ^ 1, ctl, p);
                 ctl->meta[u] = half2_bits(scale * f, offset * f);
                 asm volatile("bar.sync 2, 128;" ::: "memory");
                 unsigned char *const to = smem + S::v + (group >> 3) * (D * 128) + word0 * 1024;
@@ -693,7 +703,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
     } else if (lane == 0) {
         // ---- the products ----
         const uint32_t q_at = smem_at(smem + S::q), k_at = smem_at(smem + S::k), v_at = smem_at(smem + S::v), p_at = smem_at(smem + S::p);
-        uint32_t items_before = 0, steps[2] = {0, 0};         // steps: P V products of each half so far
+        uint32_t items_before = 0;
+        bool go = true;                                       // no wait has been given up here
         // S of tile n for half h
         const auto scores = [&](int h) {
             tc_after();
@@ -703,20 +714,20 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                         kTile, i != 0);
             tc_commit(&ctl->s_full[h]);
         };
-        while (next_item(p, walk, x)) {
+        while (go && next_item(p, walk, x)) {
             const int all = tiles_of(x);
             if (all == 0) continue;
-            bar_wait(&ctl->q_full, items_before & 1, ctl, p.status);
+            go = bar_wait(&ctl->q_full, items_before & 1, ctl, p) && bar_wait(&ctl->k_full, tiles_before & 1, ctl, p);
             ++items_before;
-            bar_wait(&ctl->k_full, tiles_before & 1, ctl, p.status);
+            if (!go) break;
             if (x.tiles[0] > 0) scores(0);
             if (x.tiles[1] > 0) scores(1);
             tc_commit(&ctl->k_empty);
-            for (int t = 0; t < all; ++t) {
+            for (int t = 0; t < all && go; ++t) {
                 const uint32_t n = tiles_before + t;
                 const bool more = t + 1 < all;
-                bar_wait(&ctl->v_full, n & 1, ctl, p.status);
-                if (more) bar_wait(&ctl->k_full, (n + 1) & 1, ctl, p.status);
+                go = bar_wait(&ctl->v_full, n & 1, ctl, p);
+                if (more) go = bar_wait(&ctl->k_full, (n + 1) & 1, ctl, p) && go;
                 // whichever half has its weights: its next S first, so that it goes on, then what the weights give
                 bool open[2] = {true, true};
                 for (uint32_t spins = 0; open[0] || open[1]; ++spins) {
@@ -725,12 +736,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                         if (!open[h]) continue;
                         // the last one open is waited for, with the limit; of two each is tried in turn, for a while
                         if (open[h ^ 1] && spins < (1u << 24)) {
-                            if (!bar_try(&ctl->p_full[h], n & 1) && !ctl->gave_up) continue;
+                            if (!bar_try(&ctl->p_full[h], n & 1)) {
+                                if (!ctl->gave_up) continue;
+                                go = false;
+                            }
                         } else {
-                            bar_wait(&ctl->p_full[h], n & 1, ctl, p.status);
+                            go = bar_wait(&ctl->p_full[h], n & 1, ctl, p) && go;
                         }
                         open[h] = false;
-                        if (t >= x.tiles[h]) continue;
+                        if (t >= x.tiles[h] || !go) continue;
                         if (t + 1 < x.tiles[h]) scores(h);
                         tc_after();
 #pragma unroll
@@ -738,7 +752,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                             mma_f16(tmem + 2 * kTile + h * kTile, operand(p_at + h * S::kP + (i >> 2) * PANEL) + 2 * (i & 3),
                                     operand(v_at + (i >> 2) * (D * 128)) + 2 * (i & 3), D, (t | i) != 0);
                         tc_commit(&ctl->pv_done[h]);
-                        ++steps[h];
                     }
                 }
                 if (more) tc_commit(&ctl->k_empty);
@@ -746,12 +759,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
             }
             tiles_before += all;
         }
-        // every product has been waited for by the rows, unless a wait was given up: then here, before TMEM is freed
-        if (ctl->gave_up)
-            for (int h = 0; h < 2; ++h) {
-                const long long t0 = clock64();
-                while (steps[h] > 0 && !bar_try(&ctl->pv_done[h], (steps[h] - 1) & 1) && clock64() - t0 < 200000000ll) {}
-            }
+        // no product is on its way when TMEM is freed, after a wait that was given up either
+        tc_commit(&ctl->drained);
+        const long long t0 = clock64();
+        while (!bar_try(&ctl->drained, 0) && clock64() - t0 < kDrainLimit) {}
     }
     __syncwarp();
     tc_before();

@@ -322,7 +322,8 @@ struct fi_kv {
     fi_kv_config_t cfg;
     int page_shift;
     int sm_count;
-    int32_t *status_dev;     // bit 0: a slot past the pool (append), bit 1: a page outside the pool (attend)
+    int32_t *status_dev;     // bit 0: a slot past the pool (append), bit 1: a page outside the pool (attend), bit 2: a wait ran out (attend)
+    long long wait_limit;    // SM cycles of a wait inside an attention kernel
     unsigned char *scratch;  // attention: a ticket per CTA, then two slots of partial results per CTA
     int tickets;
     int attend_ctas[2][3];   // CTAs that fill the device: bf16 / float32 queries x tiles of 8, 16, 32 rows

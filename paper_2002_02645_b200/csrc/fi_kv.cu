@@ -562,6 +562,8 @@ int log2_of(int v) {
     return s;
 }
 
+constexpr long long kKvWaitLimit = 8000000000ll;   // about 4 s
+
 bool page_size_ok(int p) { return p >= 16 && p <= 1024 && (p & (p - 1)) == 0; }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -722,6 +724,7 @@ fi_status_t fi_kv_create(const fi_kv_config_t *cfg, fi_kv_t **out) {
         return FI_ERR_OOM;
     }
     kv->cfg = *cfg;
+    kv->wait_limit = kKvWaitLimit;
     kv->page_shift = log2_of(cfg->page_size);
     DeviceGuard guard(cfg->device);
     cudaError_t e = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
@@ -738,6 +741,15 @@ fi_status_t fi_kv_create(const fi_kv_config_t *cfg, fi_kv_t **out) {
         return st;
     }
     *out = kv;
+    return FI_OK;
+}
+
+fi_status_t fi_kv_set_wait_limit(fi_kv_t *kv, int64_t limit_cycles) {
+    if (!kv || limit_cycles < 0 || limit_cycles > kKvWaitLimit) {
+        set_error("fi_kv_set_wait_limit: null handle or limit outside 0..%lld cycles", kKvWaitLimit);
+        return FI_ERR_INVALID_ARG;
+    }
+    kv->wait_limit = limit_cycles ? limit_cycles : kKvWaitLimit;
     return FI_OK;
 }
 

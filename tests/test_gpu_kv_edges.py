@@ -372,6 +372,28 @@ def test_prompts_the_rule_gives_to_the_prompt_kernel():
     assert torch.equal(out[:2300], again[0][:2300]) and torch.equal(lse[:2300], again[1][:2300])
 
 
+def test_prompts_and_gradients_in_a_graph():
+    a = Attention(lens=[500, 33], queries=[300, 20], q_heads=8, kv_heads=2, dim=128, seed=17)
+    cu, rows, out = ints(a.cu), ints(a.rows), torch.empty_like(a.q)
+    x = torch.randn(200, 4, 64, device=DEV)
+    w, dy = torch.ones(64, device=DEV), torch.randn(200, 4, 64, device=DEV)
+
+    def call():
+        a.kv.attend(a.q, a.d_lens, a.table, cu_tokens=cu, row_idx=rows, max_query=MANY, out=out)
+        return fb.head_norm_rope_backward(x, None, w, None, None, None, dy, None)
+    want = [t.clone() for t in call() if t is not None] + [out.clone()]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = [t for t in call() if t is not None]
+    out.zero_()
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    for p, r in zip(got + [out[:320]], want[:-1] + [want[-1][:320]]):
+        assert torch.equal(p, r)
+
+
 # ---------------------------------------------------------------------------------------------- a single token's strides
 
 @BOTH
@@ -426,5 +448,33 @@ def test_head_norm_rope_takes_part_in_backpropagation(dtype):
     y = fb.head_norm_rope(x, None, None, None, None, None, count=ints([2]))[0]
     y.backward(torch.full_like(y, math.nan).index_fill_(0, ints([0, 1], torch.int64), 1.0))
     assert x.grad[:2].isfinite().all() and (x.grad[2] == 0).all()
+    # tokens past the count: no gradient, whatever is in theirs
+    x.grad = None
+    y = fb.head_norm_rope(x, None, None, None, None, None, count=ints([2]))[0]
+    y.backward(torch.full_like(y, math.nan).index_fill_(0, ints([0, 1], torch.int64), 1.0))
+    assert x.grad[:2].isfinite().all() and (x.grad[2] == 0).all()
     with pytest.raises(ValueError):             # results written in place keep no way back
         fb.head_norm_rope(q, None, wq, None, None, None, q_out=torch.empty_like(q))
+
+
+# ------------------------------------------------------------------------------------------------------- bounded waits
+
+def test_prompt_waits_that_run_out_are_reported_and_harm_nothing():
+    """With a limit of nothing the first wait that is not over at once is given up: the kernel ends, the next poll says so, and the next
+    call is right."""
+    a = Attention(lens=[900, 300], queries=[400, 260], q_heads=8, kv_heads=2, dim=128, seed=18, room=1024)
+    want = a.run(max_query=MANY)
+    a.kv.poll_status()
+    a.kv.set_wait_limit(1)
+    a.run(max_query=MANY)
+    with pytest.raises(fb.FiError) as e:
+        a.kv.poll_status()
+    assert e.value.status == fb.FI_ERR_TIMEOUT and "bounded wait" in str(e.value)
+    a.kv.set_wait_limit()
+    for _ in range(2):
+        got = a.run(max_query=MANY)
+        a.kv.poll_status()                       # reported once
+        assert torch.equal(got[0][:660], want[0][:660]) and torch.equal(got[1][:660], want[1][:660])
+    for bad in (1 << 40, -5):
+        with pytest.raises(fb.FiError):
+            a.kv.set_wait_limit(bad)
