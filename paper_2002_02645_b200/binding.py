@@ -215,8 +215,9 @@ def _stream_ptr(device: torch.device) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
 
-# the same for an ordinal, without making a Stream object: a decode step makes three of these calls per layer
+# the same for an ordinal, without making a Stream object, and the current ordinal: a decode step makes three of these calls per layer
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _dp(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -768,7 +769,7 @@ def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interlea
                       _at(rope), _at(positions), _at(count), _at(dq_weight), _at(dk_weight), _at(workspace), *strides, *k_strides,
                       *res_strides, *k_res_strides, *dq_strides, *dk_strides, tokens, q_heads, k_heads, dim, rot, max_pos,
                       1 if interleaved else 0, _FI_DTYPE[dtype], eps)
-    if torch._C._cuda_getDevice() == index:
+    if _current_device() == index:
         st = fn(args, _raw_stream(index))
     else:
         with torch.cuda.device(index):

@@ -762,7 +762,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
         // no product is on its way when TMEM is freed, after a wait that was given up either
         tc_commit(&ctl->drained);
         const long long t0 = clock64();
-        while (!bar_try(&ctl->drained, 0) && clock64() - t0 < kDrainLimit) {}
+        bool over = false;
+        while (!(over = bar_try(&ctl->drained, 0)) && clock64() - t0 < kDrainLimit) {}
+        if (!over) atomicOr(p.status, 4);
     }
     __syncwarp();
     tc_before();
