@@ -485,8 +485,8 @@ int64_t fi_head_norm_rope_workspace(int32_t head_dim);
  * code * scale + offset.  fi_kv_append chooses, from the vector's least and largest value,
  *   offset = min rounded down to bf16,  scale = max((max - offset) / 15 rounded up to bf16, 2^-40),
  *   code = round((x - offset) / scale), ties to even
- * in fp32, so every value lies in the range and is off by half a scale at most.  A vector with a NaN or an infinity is stored with
- * offset NaN (it reads as NaN).
+ * in fp32, so every value lies in the range and is off by half a scale at most.  A vector with a NaN or an infinity, or whose range
+ * float32 does not hold, is stored with offset NaN (it reads as NaN).
  * The pools are the caller's: codes [num_pages][kv_heads][page_size][head_dim / 2] bytes and meta
  * [num_pages][kv_heads][page_size] bf16 pairs, with free strides between pages, heads and tokens, the same for keys
  * and values (bytes for codes, multiples of 16; pairs for meta; the strides of a page and of page_size tokens below 2^31, and the pages
@@ -543,7 +543,8 @@ fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *args, void *cuda_str
  *   cu_tokens nullable: one query per request, token i of request i; max_query: most queries of a request (a hint
  *   that chooses the kernel: any number is computed correctly; one above max_tokens asks for the kernel for prompts)
  * Softmax statistics and sums in fp32; products on tensor cores with the codes exact and, for float32 queries, with
- * queries and probabilities as pairs of half-precision numbers; a probability is off by 2^-12 of itself or 2^-32 of the row's
+ * queries and probabilities as pairs of half-precision numbers (queries up to 2^115 in size; scales of the values of a request up to
+ * 2^120 apart); a probability is off by 2^-12 of itself or 2^-32 of the row's
  * largest (float32 queries: 2^-22), exponents by some 2^-24 of the size of the scores.  Many bfloat16 queries per request (head_dim
  * 64 or 128) go through a kernel that rounds values to half precision (relative 2^-11) after a power of two common to 128 keys, and
  * keys too unless lse is wanted, which is as exact as float32 then whatever kernel it comes from.  Tokens past cu_tokens' end are left untouched.  Page

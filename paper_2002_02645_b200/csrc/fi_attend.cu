@@ -129,7 +129,7 @@ struct Request {
 };
 
 // blocks of 16 keys a warp takes per step, and keys a CTA does (a unit): with 8 rows there are registers for four blocks,
-// whose products, exponentials and copies overlap; two blocks took 10 % longer on 64 requests of 100 to 8,192 keys
+// whose products, exponentials and copies overlap; two blocks take 7 % longer on 64 requests of 800 to 8,192 keys
 template <int D, int NT>
 __host__ __device__ constexpr int blocks() { return D <= 128 && NT == 1 ? 4 : 2; }
 
@@ -263,8 +263,8 @@ constexpr int attend_smem() {
 // (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
-// 8 key heads of 128 over 262,143 keys of one request take 69 us, 4.1 TB/s; 64 requests of 800 to 8,192 keys 85.5 us.
-// What bounds it: the loop itself runs at 7 TB/s (5.5 cycles per key and SM, as long for its instructions as for its bytes); the
+// 8 key heads of 128 over 262,143 keys of one request take 74 us, 3.9 TB/s; 64 requests of 800 to 8,192 keys 91 us.
+// What bounds it: the loop's instructions (a further 131,072 keys of 8 heads take 27 us, 5.3 TB/s: 7 cycles per key and SM); the
 // start of a CTA (2 us to the first request for codes), the SMs' unequal speeds on equal shares, the partial results and their join
 // come on top, and so does the start of each further piece, which overlaps with the other CTAs of the SM only in part.
 template <int D, int NT, bool F32>
@@ -827,8 +827,8 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                 const int tiles = min(NT, (total_rows - row0 - 2 * warp + 7) >> 3);
                 constexpr int FEW = D <= 128 ? 8 : 4;
                 // Few parts of several tiles are all loaded at once and added up by every thread for itself, which saves the
-                // exchange of weights for each tile.  (16 requests of 5 queries, 25 rows a head, up to 6 parts: the call takes 25.3 us
-                // so and 26.9 in the other way; 64 requests of 4 rows a head, mostly 2 or 3 parts: 86.2 and 84.7.)
+                // exchange of weights for each tile.  (16 requests of 5 queries, 25 rows a head, up to 6 parts: the call takes 25.5 us
+                // so and 26.8 in the other way; 64 requests of 4 rows a head, mostly 2 or 3 parts: 91.3 us in both.)
                 if (NT > 1 && parts <= FEW) {
 #pragma unroll 1
                     for (int nt = 0; nt < tiles; ++nt) {

@@ -5,7 +5,7 @@
 // per half, a thread per row, turn S into the weights P; and one thread of a warp of its own issues the products
 //   S = Q K^T  (128 x 128, fp32 in TMEM)      O += P V  (128 x head_dim, fp32 in TMEM)
 // for each half.  The halves take turns: while one forms weights the other's products run.  All meet at mbarriers.
-//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 384 us, 635 TFLOP/s.  With one half only and everything
+//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 380 us, 640 TFLOP/s, without the logarithm.  With one half only and everything
 // unrolled it was 680 us, a third of the warps' time spent waiting for instructions; so every role's loop is short, and S is
 // read from TMEM twice, 32 columns at a time, rather than held.  Products issued by a thread that forms weights hold it up by
 // 2,000 cycles per tile.  Waiting for a tile's values, rather than only for their power, before forming its weights cost
@@ -14,17 +14,18 @@
 //
 // Unlike in the kernel for few rows, codes are brought to their values here (128 rows share the work): k = n s + m as a half,
 // rounded once (2^-11), after a power of two common to the tile has put the largest value of its 128 keys at 2^14 .. 2^15,
-// so no size of keys runs over; the power goes into the factor of the scores.  Values likewise, and their power F into the
+// so no size of keys runs over (they may reach the end of bf16); the power goes into the factor of the scores.  Values likewise, and their power F into the
 // exponent: P = 2^(x + F - M) with M = max(x + F) - 7 as it was when one last went over M + 15 (so halves start at 2^7 and lose what is
 // below 2^-32 of the largest, not 2^-25), and the sum takes P 2^-F.  A key whose scale or offset (or whose value's) is no
-// number becomes NaN in K and zero in V: the rows that see it get NaN, the others lose nothing.
+// number becomes NaN in its scores and zero in V: the rows that see it get NaN, the others lose nothing.
 //
 // Keys rounded to halves put a score off by up to 2^-11 of its parts.  The result, whose weights are halves anyway, may have that; the
 // softmax sum's logarithm is a float32 number, which was off by up to 8e-4 where few keys count.  So when it is wanted, the
 // codes go into the product as they are, less 7.5 (exact), and the scores take each key's scale and offset behind it:
 //   y = (S c) s + (m + 7.5 s) (scale log2(e) sum(q)) + F
-// The case above takes 462 us then.  (One pass over S instead of two, with the maximum checked afterwards: 489 us, as it has to wait for the
-// product before.  Keys as two halves, in two products: 535 us.)
+// The case above takes 462 us then: a thread loads 64 times 16 bytes of factors per tile, two scores take three more packed operations,
+// and y is written back to TMEM.  (When it took 471: one pass over S instead of two, with the maximum checked afterwards, 489, as it has to
+// wait for the product before; keys as two halves, in two products, 535.)
 #include "fi_attend.cuh"
 
 namespace fi {
