@@ -540,7 +540,9 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
 #pragma unroll
                 for (int k = lane; k < WARP_KEYS; k += 32) {
                     const uint32_t km = st.meta[k >> 4][0][k & 15], vm = st.meta[k >> 4][1][k & 15];
-                    const float sk = meta_scale(km), sv = fmaxf(meta_scale(vm), kMinScale);
+                    // (a scale below 2^-30 of the offset counts as that: codes times it are nothing to the value, and the quotient of the
+                    // two stays finite)
+                    const float sk = meta_scale(km), sv = fmaxf(fmaxf(meta_scale(vm), kMinScale), fabsf(meta_offset(vm)) * 0x1p-30f);
                     float mk = meta_offset(km), mv = meta_offset(vm), inv;
                     if constexpr (F32) {
                         mk = fmaf(7.5f, sk, mk);

@@ -218,6 +218,18 @@ def test_scores_below_minus_1e30_are_scores(prompt, dtype):
         assert ((lse[:2, g].double() - ref).abs() <= 2.0 ** -20 * ref.abs()).all()
 
 
+@BOTH
+@pytest.mark.parametrize("value", [2.0 ** 90, -(2.0 ** 100), 1.75 * 2.0 ** 125])
+def test_constant_values_of_any_size(value, dtype):
+    """A constant vector's offset over its scale (2^-40) is no float32 number any more; the vector is.  Bound: the roundings of the
+    result, and of sums and quotients in float32."""
+    a = Attention(lens=[1, 2, 37, 700], queries=[1, 2, 5, 3], q_heads=4, kv_heads=2, dim=128, dtype=dtype, seed=20)
+    for i, n in enumerate(a.lens):
+        put(a, "v", i, torch.full((n, 2, 128), value, device=DEV))
+    out, _ = a.run()
+    assert ((out[:a.cu[-1]].double() - value).abs() <= (2.0 ** -8 if dtype is torch.bfloat16 else 2.0 ** -18) * abs(value)).all()
+
+
 @pytest.mark.parametrize("key,query,scale", [(0.0, 2.0 ** -90, None), (0.0, 2.0 ** -100, None), (0.0, 1.0, 2.0 ** -100),
                                              (0.0, 2.0 ** -60, -2.0 ** -60), (2.0 ** -70, 2.0 ** -70, None)])
 def test_prompts_of_tiny_scores_average_the_values(key, query, scale):
