@@ -40,6 +40,12 @@ __device__ __forceinline__ float lg2(float x) {
     return y;
 }
 
+// log2 of a scale, off by 2^-22 whatever its size (lg2 alone: of the result's size, and a scale of 2^-40 is a weight off by 4e-6)
+__device__ __forceinline__ float log2_scale(float x) {
+    const uint32_t bits = __float_as_uint(x);
+    return (float)((int)(bits >> 23) - 127) + lg2(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u));
+}
+
 __device__ __forceinline__ float rcp(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -551,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                     } else {
                         inv = rcp(sv);
                     }
-                    my_key.f[k] = make_float4(sk, mk, lg2(sv), inv);
+                    my_key.f[k] = make_float4(sk, mk, log2_scale(sv), inv);
                     my_key.off[k] = mv * inv;
                     flat = flat || fabsf(mv * inv) > kMostlyOffset;
                 }
@@ -765,7 +771,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
             for (int i = 0; i < PER / 4; ++i)
                 store_out<F32>(p.out, token * p.out_ts + (long long)qh * p.out_hs + my_dim + 64 * i, acc + 4 * i, 4);
             if (p.lse && (tid & 15) == 0)
-                p.lse[token * (p.kv_heads * p.group) + qh] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                p.lse[token * (p.kv_heads * p.group) + qh] = log_sum(m, l);
         };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {

@@ -42,6 +42,15 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// Natural logarithm of 2^top sum, a softmax sum.  Where values have small scales (or a tile a large power) top and the sum's exponent
+// are large and cancel, so they are added up before the logarithm of the rest comes to them.
+__device__ __forceinline__ float log_sum(float top, float sum) {
+    if (sum == 0.f) return -INFINITY;
+    if (!(sum >= FLT_MIN && sum < INFINITY)) return (top + log2f(sum)) * kLn2;
+    const uint32_t bits = __float_as_uint(sum);
+    return (top + (float)((int)(bits >> 23) - 127) + log2f(__uint_as_float((bits & 0x7fffffu) | 0x3f800000u))) * kLn2;
+}
+
 __device__ __forceinline__ float meta_scale(uint32_t m) { return __uint_as_float(m << 16); }
 __device__ __forceinline__ float meta_offset(uint32_t m) { return __uint_as_float(m & 0xffff0000u); }
 

@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 }
             }
             if (real && p.lse)
-                p.lse[(long long)(x.first_token + j) * (p.kv_heads * p.group) + qh] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+                p.lse[(long long)(x.first_token + j) * (p.kv_heads * p.group) + qh] = log_sum(top, sum);
             tc_before();
         }
     } else if (warp < kSoftmaxWarps + kUnpackWarps) {

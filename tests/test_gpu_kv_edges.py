@@ -282,6 +282,24 @@ def check_logarithms(a, lse):
             assert (off <= 1).all(), off.max().item()
 
 
+@BOTH
+@pytest.mark.parametrize("value", [0.0, 3.0, 2.0 ** 100])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_logarithms_do_not_depend_on_the_values(prompt, value, dtype):
+    """Scores of 0: the logarithm is that of the number of keys, whatever scale the values are stored with (a constant vector's is
+    2^-40).  Off by float32's roundings of itself."""
+    if prompt and dtype is torch.float32:
+        pytest.skip("prompts of float32 take the same kernel")
+    a = Attention(lens=[1, 2, 37, 700], queries=[1, 2, 5, 300], q_heads=4, kv_heads=2, dim=128, dtype=dtype, seed=20)
+    for i, n in enumerate(a.lens):
+        put(a, "v", i, torch.full((n, 2, 128), value, device=DEV))
+    out, lse = a.run(scale=0.0, max_query=MANY if prompt else 300)
+    for i, (n, length) in enumerate(zip(a.queries, a.lens)):
+        ref = torch.log(torch.arange(length - n + 1, length + 1, dtype=torch.float64, device=DEV))[:, None]
+        assert ((lse[a.cu[i]:a.cu[i + 1]].double() - ref).abs() <= 2.0 ** -21 * (1 + ref)).all()
+        assert ((out[a.cu[i]:a.cu[i + 1]].double() - value).abs() <= 2.0 ** -10 * value).all()
+
+
 FEW_KEYS = {
     "prompt-from-nothing": dict(lens=[300, 7], queries=[300, 7], room=8192),
     "short-requests": dict(lens=[1, 2, 9, 50], queries=[1, 1, 2, 30], room=4096),
