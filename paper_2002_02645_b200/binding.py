@@ -844,8 +844,9 @@ class _HeadNormRope(torch.autograd.Function):
 
 
 class KvCache:
-    """Keys and values of one layer in 4 bits (fi_kv_*; for inference: the calls give no gradients) over pools the caller owns: codes uint8 [pages, kv_heads, page_size,
-    head_dim / 2], meta bfloat16 [pages, kv_heads, page_size, 2] (scale, offset)."""
+    """Keys and values of one layer in 4 bits (fi_kv_*) over pools the caller owns: codes uint8 [pages, kv_heads, page_size,
+    head_dim / 2], meta bfloat16 [pages, kv_heads, page_size, 2] (scale, offset).  For inference: the calls give no gradients.
+    Attention calls of one object share its scratch: they belong on one stream."""
 
     def __init__(self, k_codes: torch.Tensor, k_meta: torch.Tensor, v_codes: torch.Tensor, v_meta: torch.Tensor, *, q_heads: int):
         self._lib = load_library()

@@ -269,7 +269,7 @@ constexpr int attend_smem() {
 // (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
-// 8 key heads of 128 over 262,143 keys of one request take 74 us, 3.9 TB/s; 64 requests of 800 to 8,192 keys 91 us.
+// 8 key heads of 128 over 262,143 keys of one request take 76 us, 3.8 TB/s; 64 requests of 800 to 8,192 keys 92 us.
 // What bounds it: the loop's instructions (a further 131,072 keys of 8 heads take 27 us, 5.3 TB/s: 7 cycles per key and SM); the
 // start of a CTA (2 us to the first request for codes), the SMs' unequal speeds on equal shares, the partial results and their join
 // come on top, and so does the start of each further piece, which overlaps with the other CTAs of the SM only in part.

@@ -5,7 +5,7 @@
 // per half, a thread per row, turn S into the weights P; and one thread of a warp of its own issues the products
 //   S = Q K^T  (128 x 128, fp32 in TMEM)      O += P V  (128 x head_dim, fp32 in TMEM)
 // for each half.  The halves take turns: while one forms weights the other's products run.  All meet at mbarriers.
-//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 380 us, 640 TFLOP/s, without the logarithm.  With one half only and everything
+//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 378 us, 645 TFLOP/s, without the logarithm.  With one half only and everything
 // unrolled it was 680 us, a third of the warps' time spent waiting for instructions; so every role's loop is short, and S is
 // read from TMEM twice, 32 columns at a time, rather than held.  Products issued by a thread that forms weights hold it up by
 // 2,000 cycles per tile.  Waiting for a tile's values, rather than only for their power, before forming its weights cost
@@ -23,7 +23,7 @@
 // softmax sum's logarithm is a float32 number, which was off by up to 8e-4 where few keys count.  So when it is wanted, the
 // codes go into the product as they are, less 7.5 (exact), and the scores take each key's scale and offset behind it:
 //   y = (S c) s + (m + 7.5 s) (scale log2(e) sum(q)) + F
-// The case above takes 462 us then: a thread loads 64 times 16 bytes of factors per tile, two scores take three more packed operations,
+// The case above takes 464 us then: a thread loads 64 times 16 bytes of factors per tile, two scores take three more packed operations,
 // and y is written back to TMEM.  (When it took 471: one pass over S instead of two, with the maximum checked afterwards, 489, as it has to
 // wait for the product before; keys as two halves, in two products, 535.)
 #include "fi_attend.cuh"
