@@ -52,11 +52,6 @@ __device__ __forceinline__ float rcp(float x) {
     return y;
 }
 
-template <bool B>
-struct Bool {
-    static constexpr bool value = B;
-};
-
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -269,7 +264,7 @@ constexpr int attend_smem() {
 // (m16), query rows their columns (n8), so that the usual 4 to 8 query heads of a key head fill a tile:
 //   S^T[key, row] = K Q^T,  O^T[dim, row] += V^T P^T
 // The product over head_dim runs in the order in which lanes hold the codes; q is laid out to match.
-// 8 key heads of 128 over 262,143 keys of one request take 76 us, 3.8 TB/s; 64 requests of 800 to 8,192 keys 92 us.
+// 8 key heads of 128 over 262,143 keys of one request take 76 us, 3.8 TB/s; 64 requests of 800 to 8,192 keys 93 us.
 // What bounds it: the loop's instructions (a further 131,072 keys of 8 heads take 27 us, 5.3 TB/s: 7 cycles per key and SM); the
 // start of a CTA (2 us to the first request for codes), the SMs' unequal speeds on equal shares, the partial results and their join
 // come on top, and so does the start of each further piece, which overlaps with the other CTAs of the SM only in part.
@@ -615,7 +610,7 @@ __global__ void __launch_bounds__(kThreads, (min_ctas<D, NT>())) kv_attend_kerne
                         most[nt][h] = s[0][nt][h];
 #pragma unroll
                         for (int b = 0; b < NB; ++b) most[nt][h] = fmaxf(fmaxf(most[nt][h], s[b][nt][h]), s[b][nt][2 + h]);
-                        grow = grow || most[nt][h] > top[nt][h] + kMost;
+                        grow = grow || most[nt][h] - top[nt][h] > kMost;     // (the difference is exact where it matters)
                     }
                 if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll

@@ -36,6 +36,11 @@ struct AttendParams {
     long long wait_limit;                             // SM cycles
 };
 
+template <bool B>
+struct Bool {
+    static constexpr bool value = B;
+};
+
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -5,7 +5,7 @@
 // per half, a thread per row, turn S into the weights P; and one thread of a warp of its own issues the products
 //   S = Q K^T  (128 x 128, fp32 in TMEM)      O += P V  (128 x head_dim, fp32 in TMEM)
 // for each half.  The halves take turns: while one forms weights the other's products run.  All meet at mbarriers.
-//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 378 us, 645 TFLOP/s, without the logarithm.  With one half only and everything
+//   Two chunks of 1,024 queries of 32 heads behind 8,192 keys take 382 us, 638 TFLOP/s, without the logarithm.  With one half only and everything
 // unrolled it was 680 us, a third of the warps' time spent waiting for instructions; so every role's loop is short, and S is
 // read from TMEM twice, 32 columns at a time, rather than held.  Products issued by a thread that forms weights hold it up by
 // 2,000 cycles per tile.  Waiting for a tile's values, rather than only for their power, before forming its weights cost
@@ -23,7 +23,7 @@
 // softmax sum's logarithm is a float32 number, which was off by up to 8e-4 where few keys count.  So when it is wanted, the
 // codes go into the product as they are, less 7.5 (exact), and the scores take each key's scale and offset behind it:
 //   y = (S c) s + (m + 7.5 s) (scale log2(e) sum(q)) + F
-// The case above takes 464 us then: a thread loads 64 times 16 bytes of factors per tile, two scores take three more packed operations,
+// The case above takes 467 us then: a thread loads 64 times 16 bytes of factors per tile, two scores take three more packed operations,
 // and y is written back to TMEM.  (When it took 471: one pass over S instead of two, with the maximum checked afterwards, 489, as it has to
 // wait for the product before; keys as two halves, in two products, 535.)
 #include "fi_attend.cuh"
@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                 else most = fmaf(most, ck, fv);
                 // the products have read the weights before and added them up
                 if (t > 0) bar_wait(&ctl->pv_done[half], (steps - 1) & 1, ctl, p);
-                if (__any_sync(0xffffffffu, most > top + kMost)) {
+                if (__any_sync(0xffffffffu, most - top > kMost)) {
                     const float m = fmaxf(most - kStart, top), shrink = ex2(top - m);
                     top = m;
                     sum *= shrink;
@@ -480,29 +480,36 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attend_prompt_kernel(con
                         tmem_store_wait();
                     }
                 }
-                const uint64_t ck2 = pair(ck, ck), shift2 = EXACT ? pair(-top, -top) : pair(fv - top, fv - top);
+                const uint64_t ck2 = pair(ck, ck), fv2 = pair(fv, fv), less2 = pair(-top, -top), shift2 = pair(fv - top, fv - top);
                 uint64_t part[2] = {0, 0};
+                // Beside large scores y is rounded before the maximum is taken off it, as it was for the maximum: then no weight is above
+                // 2^15 (in one step it might be, by the roundings of y).  ROUNDED costs one more operation for two scores.
+                const auto weights = [&](auto rounded_) {
+                    constexpr bool ROUNDED = decltype(rounded_)::value;
 #pragma unroll 1
-                for (int c0 = 0; c0 < kTile; c0 += 32) {
-                    read(c0);
-                    if constexpr (!EXACT) hide(c0);
-                    unsigned char *const to = smem + S::p + half * S::kP + (c0 >> 6) * PANEL + my_row * 128;
+                    for (int c0 = 0; c0 < kTile; c0 += 32) {
+                        read(c0);
+                        if constexpr (!EXACT) hide(c0);
+                        unsigned char *const to = smem + S::p + half * S::kP + (c0 >> 6) * PANEL + my_row * 128;
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        uint32_t w[4];
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float w0, w1;
-                            const uint64_t s2 = pair(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1]));
-                            unpair(EXACT ? add2(s2, shift2) : fma2(s2, ck2, shift2), w0, w1);
-                            w0 = ex2(w0);
-                            w1 = ex2(w1);
-                            part[e & 1] = add2(part[e & 1], pair(w0, w1));
-                            w[e] = half2_bits(w0, w1);
+                            for (int e = 0; e < 4; ++e) {
+                                float w0, w1;
+                                const uint64_t s2 = pair(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1]));
+                                unpair(EXACT ? add2(s2, less2) : ROUNDED ? add2(fma2(s2, ck2, fv2), less2) : fma2(s2, ck2, shift2), w0, w1);
+                                w0 = ex2(w0);
+                                w1 = ex2(w1);
+                                part[e & 1] = add2(part[e & 1], pair(w0, w1));
+                                w[e] = half2_bits(w0, w1);
+                            }
+                            *reinterpret_cast<uint4 *>(to + ((((c0 & 32) + i) >> 3 ^ (my_row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                        *reinterpret_cast<uint4 *>(to + ((((c0 & 32) + i) >> 3 ^ (my_row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                }
+                };
+                if (!EXACT && __any_sync(0xffffffffu, fabsf(top) > 0x1p20f && top != kNoMax)) weights(Bool<true>{});
+                else weights(Bool<false>{});
                 fence_async();
                 tc_before();
                 bar_arrive(&ctl->p_full[half]);

@@ -219,6 +219,35 @@ def test_scores_below_minus_1e30_are_scores(prompt, dtype):
 
 
 @BOTH
+@pytest.mark.parametrize("size", [2.0 ** e for e in (14, 20, 23, 24, 25, 26, 30, 60)])
+@pytest.mark.parametrize("prompt", [False, True])
+def test_scores_of_any_size_choose_the_largest(prompt, size, dtype):
+    """Where one score is above all others by more than float32's roundings of its parts, its value is the result."""
+    if prompt and dtype is torch.float32:
+        pytest.skip("prompts of float32 take the same kernel")
+    a = Attention(lens=[300, 700, 40], queries=[150, 2, 30], q_heads=8, kv_heads=2, dim=64, dtype=dtype, seed=22, room=1024)
+    a.q *= size
+    chosen = 0
+    for with_lse in (True, False):
+        got = a.run(max_query=MANY if prompt else 150, with_lse=with_lse)
+        out = got[0] if with_lse else got
+        assert out[:a.cu[-1]].isfinite().all()
+        for i, n in enumerate(a.queries):
+            for g in range(8):
+                _, x, v = formula(a, i, g, a.q, 64 ** -0.5)
+                reach = (a.q[a.cu[i]:a.cu[i + 1], g].double().abs().sum(-1, keepdim=True) * a.k_reach(i, g // a.group) / 8).amax(-1)
+                best = x.topk(2, -1).values if x.shape[1] > 1 else x.new_zeros(n, 2)
+                clear = best[:, 0] - best[:, 1] > 2.0 ** -18 * reach + 40
+                want = v[x.argmax(-1)][clear]
+                # a weight as a half, a value as another, the result as bf16 (float32: pairs of halves); codes and offset are summed apart
+                parts = v.abs().amax() + 15 * a.vm_scale(i, g // a.group).max()
+                bound = (2.0 ** -10 if dtype is torch.bfloat16 else 2.0 ** -19) * parts + (2.0 ** -8 if dtype is torch.bfloat16 else 0) * want.abs()
+                assert ((out[a.cu[i]:a.cu[i + 1], g][clear].double() - want).abs() <= bound).all()
+                chosen += int(clear.sum())
+    assert chosen > 300 or size < 2.0 ** 20
+
+
+@BOTH
 @pytest.mark.parametrize("value", [2.0 ** 90, -(2.0 ** 100), 1.75 * 2.0 ** 125])
 def test_constant_values_of_any_size(value, dtype):
     """A constant vector's offset over its scale (2^-40) is no float32 number any more; the vector is.  Bound: the roundings of the
