@@ -544,11 +544,11 @@ fi_status_t fi_kv_append(fi_kv_t *kv, const fi_kv_append_t *args, void *cuda_str
  *   that chooses the kernel: any number is computed correctly; one above max_tokens asks for the kernel for prompts)
  * Softmax statistics and sums in fp32; products on tensor cores with the codes exact and, for float32 queries, with
  * queries and probabilities as pairs of half-precision numbers (queries up to 2^115 in size; scales of the values of a request up to
- * 2^120 apart); a probability is off by 2^-12 of itself or 2^-32 of the row's
- * largest (float32 queries: 2^-22), exponents by some 2^-24 of the size of the scores.  Many bfloat16 queries per request (head_dim
- * 64 or 128) go through a kernel that rounds values to half precision (relative 2^-11) after a power of two common to 128 keys, and
- * keys too unless lse is wanted, which is as exact as float32 then whatever kernel it comes from.  Tokens past cu_tokens' end are left untouched.  Page
- * numbers outside the pool hide their tokens and are reported by fi_kv_poll_status.  Asynchronous; calls of one
+ * 2^120 apart); a probability is off by 2^-12 of itself or 2^-32 of the row's largest (float32 queries: 2^-22), exponents by some
+ * 2^-24 of the size of the scores and of log2 of the values' scales.  Many bfloat16 queries per request (head_dim 64 or 128) go
+ * through a kernel that rounds values to half precision (relative 2^-11) after a power of two common to 128 keys, and keys too
+ * unless lse is wanted, which is as exact as float32 then whatever kernel it comes from.  Tokens past cu_tokens' end are left
+ * untouched.  Page numbers outside the pool hide their tokens and are reported by fi_kv_poll_status.  Asynchronous; calls of one
  * handle share its scratch and must be ordered on one stream.
  */
 typedef struct {
