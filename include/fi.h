@@ -583,6 +583,65 @@ fi_status_t fi_kv_set_wait_limit(fi_kv_t *kv, int64_t limit_cycles);
  * last poll (the word is cleared), FI_ERR_TIMEOUT when a bounded wait inside one ran out, FI_OK otherwise. */
 fi_status_t fi_kv_poll_status(fi_kv_t *kv);
 
+/*
+ * The products of a layer, for all requests or for those that were not frozen:
+ *   y[i] = act(x[i] W^T + bias) + residual[rows[i]],  stored in row rows[i] of out
+ *   x [tokens x in_dim] bfloat16; weight [out_dim x in_dim] bfloat16; bias [out_dim] float, nullable
+ *   residual, out [out_rows x out_dim], float32 or bfloat16 (out_dtype); residual nullable; it may be out itself
+ *   rows [tokens] device int32, nullable: row of residual and out of each token (miss_idx of a cascade step), no row twice; a row
+ *   outside [0, out_rows) is not stored; null: token i is row i.  Rows that are not listed are left untouched.
+ *   tokens_dev [1] device int32, nullable: actual number of tokens (<= tokens); later ones are left out.
+ *   preact [tokens x out_dim] bfloat16, nullable: x W^T + bias before the activation, which the gradients need.
+ * Products on the tensor cores, sums in fp32; one rounding at the end.  A float32 out is summed up in pieces of about 512 values outside
+ * of the tensor cores, which cut what they add (an error of some 2^-25 of the sum for 16 values).
+ * in_dim and out_dim multiples of 8; rows of x and weight start on 16-byte boundaries; strides in elements.  Asynchronous, on the
+ * current device; no workspace, so calls may overlap.  x and weight must not be written by the call's own results.
+ *
+ * fi_linear_backward: gradients for dy [tokens x out_dim] bfloat16 (of the result without its residual, whose gradient is dy itself):
+ *   dz = dy act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over tokens of dz
+ * dx, dweight bfloat16, dbias float; each nullable.  dz is rounded to bfloat16 for the products (2^-9 of each value), not for dbias;
+ * without an activation it is dy and preact is not read.  dbias is summed in a fixed order.  `workspace`: fi_linear_backward_workspace
+ * bytes of device memory on a 16-byte boundary, contents free, not shared by calls that overlap; may be null without activation and dbias.
+ *
+ * fi_linear_poll_status: synchronises the current device; FI_ERR_TIMEOUT when a bounded wait inside a kernel of these calls ran out
+ * there since the last poll (the word is cleared).
+ */
+typedef enum { FI_ACT_NONE = 0, FI_ACT_RELU = 1, FI_ACT_GELU = 2 /* z Phi(z) */, FI_ACT_GELU_TANH = 3, FI_ACT_SILU = 4 } fi_act_t;
+
+typedef struct {
+    const void *x, *weight;
+    const float *bias;          /* nullable */
+    const void *residual;       /* nullable */
+    void *out;
+    void *preact;               /* nullable */
+    const int32_t *rows;        /* nullable */
+    const int32_t *tokens_dev;  /* nullable */
+    int64_t x_stride, weight_stride, residual_stride, out_stride, preact_stride;
+    int64_t tokens;
+    int64_t out_rows;           /* rows of residual and out; read with `rows` only */
+    int64_t wait_limit;         /* SM cycles a wait inside the kernel may take; 0: 8e9 (about 4 s), also the most.  For tests */
+    int32_t in_dim, out_dim;
+    int32_t activation;         /* fi_act_t */
+    int32_t out_dtype;          /* fi_dtype_t */
+} fi_linear_t;
+fi_status_t fi_linear(const fi_linear_t *args, void *cuda_stream);
+
+typedef struct {
+    const void *x, *weight;     /* x: for dweight; weight: for dx */
+    const void *dy;
+    const void *preact;         /* read when there is an activation */
+    void *dx, *dweight;         /* nullable */
+    float *dbias;               /* nullable */
+    void *workspace;
+    int64_t x_stride, weight_stride, dy_stride, preact_stride, dx_stride, dweight_stride;
+    int64_t tokens;
+    int32_t in_dim, out_dim;
+    int32_t activation;
+} fi_linear_backward_t;
+fi_status_t fi_linear_backward(const fi_linear_backward_t *args, void *cuda_stream);
+int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation);
+fi_status_t fi_linear_poll_status(void);
+
 /* Number of kernels this library has launched in the calling process (all caches). */
 int64_t fi_launch_count(void);
 

@@ -32,7 +32,8 @@ EXPORTS = ["fi_cache_create", "fi_cache_destroy", "fi_cache_insert", "fi_cache_s
            "fi_cache_read_slot_certificates", "fi_cache_lookup_view", "fi_cache_set_sm_limit", "fi_gemm_plan_describe",
            "fi_pages_create", "fi_pages_destroy", "fi_pages_extend", "fi_pages_release", "fi_head_norm_rope",
            "fi_head_norm_rope_backward", "fi_head_norm_rope_workspace", "fi_kv_create", "fi_kv_destroy", "fi_kv_append",
-           "fi_kv_attend", "fi_kv_set_wait_limit", "fi_kv_poll_status", "fi_launch_count", "fi_last_error", "fi_status_string"]
+           "fi_kv_attend", "fi_kv_set_wait_limit", "fi_kv_poll_status", "fi_linear", "fi_linear_backward",
+           "fi_linear_backward_workspace", "fi_linear_poll_status", "fi_launch_count", "fi_last_error", "fi_status_string"]
 
 
 class fi_cache_config_t(ctypes.Structure):
@@ -91,6 +92,18 @@ class fi_kv_attend_t(ctypes.Structure):
     _fields_ = _fields(ctypes.c_void_p, "q out lse lens block_table row_idx batch_count cu_tokens granted") \
         + _fields(ctypes.c_int64, "q_token_stride q_head_stride out_token_stride out_head_stride table_ld") \
         + _fields(ctypes.c_int32, "rows max_blocks batch_max max_tokens max_query window dtype") + [("scale", ctypes.c_float)]
+
+
+class fi_linear_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "x weight bias residual out preact rows tokens_dev") \
+        + _fields(ctypes.c_int64, "x_stride weight_stride residual_stride out_stride preact_stride tokens out_rows wait_limit") \
+        + _fields(ctypes.c_int32, "in_dim out_dim activation out_dtype")
+
+
+class fi_linear_backward_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "x weight dy preact dx dweight dbias workspace") \
+        + _fields(ctypes.c_int64, "x_stride weight_stride dy_stride preact_stride dx_stride dweight_stride tokens") \
+        + _fields(ctypes.c_int32, "in_dim out_dim activation")
 
 
 class FiError(RuntimeError):
@@ -169,6 +182,11 @@ def load_library(path: Optional[str] = None):
     lib.fi_kv_attend.argtypes = [vp, ctypes.c_char_p, vp]           # a packed fi_kv_attend_t
     lib.fi_kv_set_wait_limit.argtypes = [vp, i64]
     lib.fi_kv_poll_status.argtypes = [vp]
+    lib.fi_linear.argtypes = [ctypes.c_char_p, vp]                     # a packed fi_linear_t
+    lib.fi_linear_backward.argtypes = [ctypes.c_char_p, vp]
+    lib.fi_linear_backward_workspace.argtypes = [i64, i32, i32]
+    lib.fi_linear_backward_workspace.restype = i64
+    lib.fi_linear_poll_status.argtypes = []
     lib.fi_launch_count.argtypes = []
     lib.fi_launch_count.restype = i64
     lib.fi_last_error.argtypes = []
@@ -596,8 +614,8 @@ def _packer(kind) -> struct.Struct:
     return p
 
 
-_pack_extend, _pack_norm, _pack_append, _pack_attend = (
-    _packer(k).pack for k in (fi_pages_extend_t, fi_head_norm_rope_t, fi_kv_append_t, fi_kv_attend_t))
+_pack_extend, _pack_norm, _pack_append, _pack_attend, _pack_linear, _pack_linear_backward = (
+    _packer(k).pack for k in (fi_pages_extend_t, fi_head_norm_rope_t, fi_kv_append_t, fi_kv_attend_t, fi_linear_t, fi_linear_backward_t))
 
 
 def _at(t: Optional[torch.Tensor]) -> int:
@@ -841,6 +859,169 @@ class _HeadNormRope(torch.autograd.Function):
                                                    interleaved=ctx.interleaved, count=count, dq=dq, dk=dk)
         dqw, dkw = (None if d is None else d.view_as(w) for d, w in ((dqw, q_weight), (dkw, k_weight)))
         return dq, dk, dqw, dkw, None, None, None, None, None
+
+
+FI_ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _on_device(index: int, call, *args) -> None:
+    """Runs a call of the library that works on the current device."""
+    if _current_device() == index:
+        st = call(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            st = call(*args, _raw_stream(index))
+    if st:
+        _check(st)
+
+
+def _check_rows(t: torch.Tensor, name: str, index: int, dtype, rows: Optional[int], dim: int) -> int:
+    """Stride between rows of a [rows, dim] tensor."""
+    if t.dtype is not dtype or t.get_device() != index or t.dim() != 2 or t.size(1) != dim or (rows is not None and t.size(0) != rows):
+        raise ValueError(f"{name} must be {dtype} [{'rows' if rows is None else rows}, {dim}] on cuda:{index}")
+    row, value = t.stride()
+    if value != 1 and dim > 1:
+        raise ValueError(f"{name}: the values of a row must lie side by side")
+    return row
+
+
+def _activation(name: str) -> int:
+    kind = FI_ACTIVATIONS.get(name)
+    if kind is None:
+        raise ValueError(f"activation must be one of {', '.join(FI_ACTIVATIONS)}")
+    return kind
+
+
+def _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit=0):
+    index = x.get_device()
+    if x.dtype is not torch.bfloat16 or x.dim() != 2 or index < 0:
+        raise ValueError("x must be a bfloat16 [tokens, in_dim] tensor on a GPU")
+    tokens, in_dim = x.shape
+    x_stride = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
+    if weight.dim() != 2:
+        raise ValueError("weight must be [out_dim, in_dim]")
+    out_dim = weight.size(0)
+    weight_stride = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
+    _check_flat(bias, "bias", index, out_dim, torch.float32)
+    _check_flat(rows, "rows", index, tokens)
+    _check_flat(count, "count", index, 1)
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else residual.dtype if residual is not None else torch.bfloat16
+    if out_dtype not in _FI_DTYPE:
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    out_rows, residual_stride = tokens, 0
+    if rows is not None:
+        if out is None:
+            raise ValueError("rows are rows of `out`, which has to be given")
+        out_rows = out.size(0)
+    if out is None:
+        out = torch.empty((tokens, out_dim), dtype=out_dtype, device=x.device)
+        out_stride = out_dim
+    else:
+        out_stride = _check_rows(out, "out", index, out_dtype, out_rows, out_dim)
+    if residual is not None:
+        residual_stride = _check_rows(residual, "residual", index, out_dtype, out_rows, out_dim)
+    preact_stride = 0
+    if preact is not None:
+        preact_stride = _check_rows(preact, "preact", index, torch.bfloat16, tokens, out_dim)
+    args = _pack_linear(x.data_ptr(), weight.data_ptr(), _at(bias), _at(residual), out.data_ptr(), _at(preact), _at(rows), _at(count), x_stride,
+                        weight_stride, residual_stride, out_stride, preact_stride, tokens, out_rows, wait_limit, in_dim, out_dim,
+                        _activation(activation), _FI_DTYPE[out_dtype])
+    _on_device(index, load_library().fi_linear, args)
+    return out
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *, activation: str = "none",
+           residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
+           count: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None, preact: Optional[torch.Tensor] = None,
+           wait_limit: int = 0) -> torch.Tensor:
+    """fi_linear: act(x weight^T + bias) + residual, of x [tokens, in_dim] and weight [out_dim, in_dim] in bfloat16.  With `rows`, token i
+    belongs to row rows[i] of residual and out (out may be residual); with `count` only that many tokens are real.  preact takes the sums
+    before the activation.  Gradients flow to x, weight, bias and residual; not through rows, count, out or preact, which are refused
+    where one is asked for."""
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+                                    or residual is not None and residual.requires_grad):
+        if out is not None or rows is not None or count is not None or preact is not None:
+            raise ValueError("out, rows, count or preact is given, but a gradient is asked for")
+        return _Linear.apply(x, weight, bias, residual, activation, out_dtype, wait_limit)
+    return _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
+
+
+def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], dy: torch.Tensor, *, preact: Optional[torch.Tensor] = None,
+                    activation: str = "none", with_bias: bool = False, dx: Optional[torch.Tensor] = None,
+                    dweight: Optional[torch.Tensor] = None):
+    """fi_linear_backward: (dx, dweight, dbias) for dy, the bfloat16 gradient of the result.  Without weight there is no dx, without x no
+    dweight, and dbias only with with_bias."""
+    lib, kind, index = load_library(), _activation(activation), dy.get_device()
+    if dy.dtype is not torch.bfloat16 or dy.dim() != 2 or index < 0:
+        raise ValueError("dy must be a bfloat16 [tokens, out_dim] tensor on a GPU")
+    tokens, out_dim = dy.shape
+    if x is None and weight is None:
+        in_dim = 8                                         # nothing but dbias
+    else:
+        in_dim = (x if x is not None else weight).shape[-1]
+    strides = [0, 0, _check_rows(dy, "dy", index, torch.bfloat16, tokens, out_dim), 0, 0, 0]
+    if weight is not None:
+        strides[1] = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
+        if dx is None:
+            dx = torch.empty((tokens, in_dim), dtype=torch.bfloat16, device=dy.device)
+        strides[4] = _check_rows(dx, "dx", index, torch.bfloat16, tokens, in_dim)
+    elif dx is not None:
+        raise ValueError("dx needs weight")
+    if x is not None:
+        strides[0] = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
+        if dweight is None:
+            dweight = torch.empty((out_dim, in_dim), dtype=torch.bfloat16, device=dy.device)
+        strides[5] = _check_rows(dweight, "dweight", index, torch.bfloat16, out_dim, in_dim)
+    elif dweight is not None:
+        raise ValueError("dweight needs x")
+    if kind:
+        if preact is None:
+            raise ValueError("the gradient of an activation needs preact")
+        strides[3] = _check_rows(preact, "preact", index, torch.bfloat16, tokens, out_dim)
+    dbias = torch.empty(out_dim, dtype=torch.float32, device=dy.device) if with_bias else None
+    work = None
+    if kind or with_bias:
+        work = torch.empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind), dtype=torch.uint8, device=dy.device)
+    args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
+                                 *strides, tokens, in_dim, out_dim, kind)
+    _on_device(index, lib.fi_linear_backward, args)
+    return dx, dweight, dbias
+
+
+def linear_poll_status(device: int = 0) -> None:
+    """fi_linear_poll_status of a device: raises FI_ERR_TIMEOUT when a wait inside a product's kernel ran out there."""
+    with torch.cuda.device(device):
+        _check(load_library().fi_linear_poll_status())
+
+
+def _as_rows(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy that the kernels read: bfloat16 values of a row side by side, rows on 16-byte boundaries."""
+    t = t.to(torch.bfloat16)
+    return t if t.stride(1) == 1 and t.stride(0) % 8 == 0 and t.stride(0) >= t.size(1) and t.data_ptr() % 16 == 0 else t.contiguous()
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, activation, out_dtype, wait_limit):
+        preact = None
+        if _activation(activation):
+            preact = torch.empty((x.size(0), weight.size(0)), dtype=torch.bfloat16, device=x.device)
+        y = _linear_call(x, weight, bias, activation, residual, None, None, None, out_dtype, preact, wait_limit)
+        ctx.save_for_backward(x, weight, preact)
+        ctx.activation, ctx.with_bias = activation, bias is not None
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, preact = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if need[0] or need[1] or need[2]:
+            dx, dw, db = linear_backward(x if need[1] else None, weight if need[0] else None, _as_rows(dy), preact=preact,
+                                         activation=ctx.activation, with_bias=need[2])
+        return dx, dw, db, dy if need[3] else None, None, None, None
 
 
 class KvCache:

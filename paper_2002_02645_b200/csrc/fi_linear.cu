@@ -1,0 +1,728 @@
+// The products of a layer: y = act(x W^T + b) + r for a list of rows, and the gradients.
+//
+// All three products are one form, D[n][m] = sum_k A(m, k) B(n, k), with the output's contiguous dimension as the MMA's
+// rows, so that the 32 lanes of a warp hold neighbouring values of one output row and store them side by side:
+//   forward    D = y   [tokens][out]   A = W  (k contiguous)   B = x  (k contiguous)      k over in
+//   dx         D = dx  [tokens][in]    A = W  (m contiguous)   B = dz (k contiguous)      k over out
+//   dW         D = dW  [out][in]       A = x  (m contiguous)   B = dz (n contiguous)      k over tokens
+// Operands come by TMA in blocks of 64 along k, 128-byte swizzle, as they lie in memory: the tensor cores take either order.
+// Sums are fp32 in TMEM.
+#include <cuda_bf16.h>
+
+#include <atomic>
+
+#include "fi_internal.cuh"
+
+namespace fi {
+namespace {
+
+constexpr int kM = 128;                   // output columns of a CTA (MMA rows)
+constexpr int kKb = 64;                   // reduction values of a stage
+constexpr int kABytes = kM * kKb * 2;
+constexpr int kMaxN = 256;                // output rows of a tile, at most
+constexpr int kMaxStages = 12;
+constexpr int kEpiThreads = 256;          // warps 0..7: TMEM lanes 32 (w mod 4) ..; warp 8 loads, warp 9 issues the products
+constexpr int kThreads = kEpiThreads + 64;
+constexpr int kSmemMost = 227 * 1024;
+constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
+constexpr long long kShortLimit = 1 << 20;       // limits below it are a test's
+constexpr long long kDrainLimit = 200000000ll;   // (about 0.1 s)
+
+__device__ int32_t g_linear_status;       // 1: a bounded wait ran out
+
+struct LinearCtl {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t done, never;
+    uint32_t tmem;
+    volatile int gave_up;
+};
+
+struct LinearParams {
+    const float *bias;             // [m]
+    const void *residual;          // type of out
+    void *out;
+    __nv_bfloat16 *preact;
+    const int32_t *rows, *count;
+    long long ld_res, ld_out, ld_preact, out_rows, wait_limit;
+    int m, n, kb;                  // output columns, rows; blocks of 64 of the reduction
+    int m_tiles, tile_n;
+    int a_mn, b_mn;                // operand with the reduction strided (its own index contiguous)
+    int split;                     // CTAs of a cluster that share a tile's reduction
+    int bufs;                      // accumulators that a CTA's reduction is cut into
+    int tmem_cols, stages, b_bytes;
+    int act;
+};
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(smem_at(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// Bounded wait: when one gives up, every later wait of the CTA does so at once, the kernel runs to its end with whatever is in its
+// buffers, and the status word says that the results are not valid.
+template <typename Ctl>
+__device__ __noinline__ bool bar_wait_long(uint64_t *bar, uint32_t parity, Ctl *ctl, long long limit) {
+    const long long t0 = clock64();
+    for (uint32_t spins = 1;; ++spins) {
+        if (bar_try(bar, parity)) return true;
+        if ((spins & 255) == 0) {
+            if (ctl->gave_up) return false;
+            if (clock64() - t0 > limit) {
+                ctl->gave_up = 1;
+                atomicOr(&g_linear_status, 1);
+                return false;
+            }
+        }
+    }
+}
+template <typename Ctl>
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, Ctl *ctl, long long limit) {
+    return bar_try(bar, parity) || bar_wait_long(bar, parity, ctl, limit);
+}
+// for the end of a role that gave up: what it has started is over before the CTA leaves
+__device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!bar_try(bar, parity))
+        if (clock64() - t0 > kDrainLimit) {
+            atomicOr(&g_linear_status, 1);
+            return;
+        }
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(bar)) : "memory");
+}
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_at(bar)), "r"(x), "r"(y)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
+    uint32_t out;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(out) : "r"(addr), "r"(rank));
+    return out;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Operand in shared memory, 128-byte swizzle.  Reduction contiguous: rows of 128 bytes, groups of eight 1,024 bytes apart.  Else a
+// line of 128 bytes holds 64 rows at one k: 8 k's are 1,024 bytes, the next 64 rows 8,192 bytes further.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, int mn) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(mn ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+// between the k's of successive MMAs (16 of them), in units of 16 bytes
+__device__ __forceinline__ uint32_t operand_step(int mn) { return mn ? 2048 >> 4 : 32 >> 4; }
+// bf16 x bf16 -> fp32
+__device__ __forceinline__ uint32_t instruction(int m, int n, int a_mn, int b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// 16 columns of the thread's TMEM lane
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr)
+        : "memory");
+}
+// wait for the loads; the registers may only be used behind it
+__device__ __forceinline__ void tmem_wait(uint32_t *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                   "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+// result of a load that is not volatile to the compiler's order, from shared memory of a CTA of the cluster
+__device__ __forceinline__ float cluster_load(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+constexpr float kGeluTanh = 0.044715f, kGeluTwice = 1.5957691216057308f;   // 2 sqrt(2 / pi)
+
+__device__ __forceinline__ float logistic(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+
+__device__ __forceinline__ float activate(float z, int act) {
+    switch (act) {
+        case FI_ACT_RELU: return z < 0.f ? 0.f : z;                      // (NaN stays)
+        case FI_ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);     // (not 1 + erf, which loses the small values of z < 0)
+        case FI_ACT_GELU_TANH: return z * logistic(kGeluTwice * fmaf(kGeluTanh * z, z * z, z));
+        case FI_ACT_SILU: return z * logistic(z);
+        default: return z;
+    }
+}
+
+// slope of the activation; where it has reached 0 or 1 it is taken as that, so that no product of infinities comes up
+__device__ __forceinline__ float slope(float z, int act) {
+    switch (act) {
+        case FI_ACT_RELU: return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+        case FI_ACT_GELU: {
+            if (fabsf(z) > 20.f) return z > 0.f ? 1.f : 0.f;
+            return fmaf(z * 0.39894228f, __expf(-0.5f * z * z), 0.5f * erfcf(z * -0.70710678f));
+        }
+        case FI_ACT_GELU_TANH: {
+            if (fabsf(z) > 20.f) return z > 0.f ? 1.f : 0.f;
+            const float s = logistic(kGeluTwice * fmaf(kGeluTanh * z, z * z, z));
+            return fmaf(z * s * (1.f - s), kGeluTwice * fmaf(3.f * kGeluTanh * z, z, 1.f), s);
+        }
+        case FI_ACT_SILU: {
+            if (fabsf(z) > 100.f) return z > 0.f ? 1.f : 0.f;
+            const float s = logistic(z);
+            return s * fmaf(z, 1.f - s, 1.f);
+        }
+        default: return 1.f;
+    }
+}
+
+__device__ __forceinline__ int actual_rows(const LinearParams &p) {
+    if (!p.count) return p.n;
+    const int c = *p.count;
+    return c < 0 ? 0 : c > p.n ? p.n : c;
+}
+
+// What becomes of one sum: column m of row n of the product, `to` its row of out.
+template <bool F32>
+__device__ __forceinline__ void finish(const LinearParams &p, float v, float bias, int m, int n, long long to) {
+    const float z = v + bias;
+    if (p.preact) p.preact[(long long)n * p.ld_preact + m] = __float2bfloat16_rn(z);
+    float y = activate(z, p.act);
+    if (F32) {
+        if (p.residual) y += static_cast<const float *>(p.residual)[to * p.ld_res + m];
+        static_cast<float *>(p.out)[to * p.ld_out + m] = y;
+    } else {
+        if (p.residual) y += __bfloat162float(static_cast<const __nv_bfloat16 *>(p.residual)[to * p.ld_res + m]);
+        static_cast<__nv_bfloat16 *>(p.out)[to * p.ld_out + m] = __float2bfloat16_rn(y);
+    }
+}
+
+// Few tiles: a CTA takes 128 output columns and up to 256 output rows, `split` CTAs of a cluster share its reduction and add up
+// their sums through distributed shared memory, in the order of their ranks.
+template <bool F32>
+__global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                   const __grid_constant__ CUtensorMap map_b,
+                                                                   const __grid_constant__ LinearParams p) {
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ LinearCtl ctl_space;
+    LinearCtl *const ctl = &ctl_space;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tile = blockIdx.x / p.split, rank = blockIdx.x - tile * p.split;
+    const int m0 = (tile % p.m_tiles) * kM, n0 = (tile / p.m_tiles) * p.tile_n;
+    const int rows = actual_rows(p);
+    if (n0 >= rows) return;                                 // (all CTAs of the cluster)
+    unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
+    const int kb0 = (int)((long long)p.kb * rank / p.split), kb1 = (int)((long long)p.kb * (rank + 1) / p.split);
+    const int stage_bytes = kABytes + p.b_bytes;
+    if (tid == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            bar_init(&ctl->full[s], 1);
+            bar_init(&ctl->empty[s], 1);
+        }
+        bar_init(&ctl->done, 1);
+        bar_init(&ctl->never, 1);
+        ctl->gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(p.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = ctl->tmem;
+    // so that a wait runs out for certain
+    if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
+    if (warp == 8) {
+        if (lane == 0) {
+            int kb = kb0;
+            uint32_t stage = 0, phase = 0;
+            for (; kb < kb1; ++kb) {
+                if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) break;
+                const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
+                uint64_t *const bar = &ctl->full[stage];
+                bar_expect(bar, (uint32_t)stage_bytes);
+                if (p.a_mn) {
+                    load_box(a, &map_a, bar, m0, kb * kKb);
+                    load_box(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
+                } else {
+                    load_box(a, &map_a, bar, kb * kKb, m0);
+                }
+                if (p.b_mn)
+                    for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
+                else
+                    load_box(b, &map_b, bar, kb * kKb, n0);
+                if (++stage == (uint32_t)p.stages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            if (kb < kb1) {                                 // gave up: the copies that were started land first
+                int back = min(kb - kb0, p.stages);
+                for (; back > 0; --back) {
+                    if (stage == 0) {
+                        stage = p.stages;
+                        phase ^= 1;
+                    }
+                    bar_drain(&ctl->full[--stage], phase);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0) {
+            const uint32_t idesc = instruction(kM, p.tile_n, p.a_mn, p.b_mn);
+            const uint32_t a_step = operand_step(p.a_mn), b_step = operand_step(p.b_mn);
+            const int length = (kb1 - kb0 + p.bufs - 1) / p.bufs;
+            uint32_t stage = 0, phase = 0, d = tmem;
+            int in_buf = 0;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) break;
+                tc_after();
+                const uint32_t at = smem_at(smem + stage * stage_bytes);
+                const uint64_t a = operand(at, p.a_mn), b = operand(at + kABytes, p.b_mn);
+#pragma unroll
+                for (int i = 0; i < kKb / 16; ++i) mma(d, a + i * a_step, b + i * b_step, idesc, (in_buf | i) != 0);
+                tc_commit(&ctl->empty[stage]);
+                if (++in_buf == length) {
+                    in_buf = 0;
+                    d += p.tile_n;
+                }
+                if (++stage == (uint32_t)p.stages) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            tc_commit(&ctl->done);
+            bar_drain(&ctl->done, 0);
+        }
+    }
+    __syncwarp();
+    if (warp < 8) {
+        bar_wait(&ctl->done, 0, ctl, p.wait_limit);
+        tc_after();
+    }
+    __syncthreads();                                        // (the loader too has nothing on its way now)
+    // the CTA's sums into shared memory, [output row][128 columns]
+    float *const part = reinterpret_cast<float *>(smem);
+    const int cols = min(p.tile_n, rows - n0);
+    if (warp < 8) {
+        const int used = (kb1 - kb0 + p.bufs - 1) / p.bufs;                       // blocks of a buffer
+        const int bufs = (kb1 - kb0 + used - 1) / used;                           // buffers that hold something
+        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        for (int c = (warp >> 2) * 16; c < cols; c += 32) {
+            uint32_t v[16], w[16];
+            tmem_load(at + c, v);
+            tmem_wait(v);
+            for (int b = 1; b < bufs; ++b) {
+                tmem_load(at + b * p.tile_n + c, w);
+                tmem_wait(w);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[(c + i) * kM + (warp & 3) * 32 + lane] = __uint_as_float(v[i]);
+        }
+        tc_before();
+    }
+    if (p.split > 1) cluster_sync();
+    else __syncthreads();
+    if (warp < 8) {
+        const int m = m0 + (tid & (kM - 1));
+        const float bias = p.bias && m < p.m ? p.bias[m] : 0.f;
+        const uint32_t mine = smem_at(part) + (tid & (kM - 1)) * 4;
+        for (int c = rank * 2 + (tid >> 7); c < cols && m < p.m; c += 2 * p.split) {
+            float v = 0.f;
+            if (p.split > 1)
+                for (int s = 0; s < p.split; ++s) v += cluster_load(map_to_rank(mine + c * (kM * 4), s));
+            else
+                v = part[c * kM + (tid & (kM - 1))];
+            const long long to = p.rows ? p.rows[n0 + c] : n0 + c;
+            if (to >= 0 && to < p.out_rows) finish<F32>(p, v, bias, m, n0 + c, to);
+        }
+    }
+    if (p.split > 1) cluster_sync();                        // the others have read this CTA's sums
+    else __syncthreads();
+    if (warp == 0) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
+    }
+}
+
+// dz = dy act'(preact), and the CTA's sums of its columns (of dy itself without an activation: nothing is stored then).  A CTA takes 64
+// columns, eight per thread, and every gridDim.y-th group of 32 rows.
+constexpr int kSlopeThreads = 256, kSlopeCols = 64, kSlopeRows = kSlopeThreads * 8 / kSlopeCols;
+
+__global__ void __launch_bounds__(kSlopeThreads) linear_slope_kernel(const __nv_bfloat16 *dy, long long ld_dy, const __nv_bfloat16 *z, long long ld_z,
+                                                                     __nv_bfloat16 *dz, float *partial, long long rows, int cols, int act) {
+    __shared__ float s[kSlopeRows][kSlopeCols + 1];
+    const int part = threadIdx.x & (kSlopeCols / 8 - 1), group = threadIdx.x / (kSlopeCols / 8);
+    const int c = blockIdx.x * kSlopeCols + part * 8;
+    float sum[8] = {};
+    if (c < cols)
+        for (long long r = (long long)blockIdx.y * kSlopeRows + group; r < rows; r += (long long)gridDim.y * kSlopeRows) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(dy + r * ld_dy + c);
+            uint4 b = make_uint4(0, 0, 0, 0);
+            if (act != FI_ACT_NONE) b = *reinterpret_cast<const uint4 *>(z + r * ld_z + c);
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float lo = __uint_as_float(aw[i] << 16), hi = __uint_as_float(aw[i] & 0xffff0000u);
+                if (act != FI_ACT_NONE) {
+                    lo *= slope(__uint_as_float(bw[i] << 16), act);
+                    hi *= slope(__uint_as_float(bw[i] & 0xffff0000u), act);
+                }
+                sum[2 * i] += lo;
+                sum[2 * i + 1] += hi;
+                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+                o[i] = reinterpret_cast<const uint32_t &>(h);
+            }
+            if (act != FI_ACT_NONE) *reinterpret_cast<uint4 *>(dz + r * cols + c) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    if (!partial) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[group][part * 8 + i] = sum[i];
+    __syncthreads();
+    if (threadIdx.x < kSlopeCols && blockIdx.x * kSlopeCols + threadIdx.x < (unsigned)cols) {
+        float total = 0.f;
+#pragma unroll 8
+        for (int g = 0; g < kSlopeRows; ++g) total += s[g][threadIdx.x];
+        partial[(long long)blockIdx.y * cols + blockIdx.x * kSlopeCols + threadIdx.x] = total;
+    }
+}
+
+// dbias from the CTAs' sums, always in the same order
+__global__ void __launch_bounds__(256) linear_bias_sum_kernel(const float *partial, int parts, int cols, float *dbias) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    float sum = 0.f;
+    for (int i = 0; i < parts; ++i) sum += partial[(long long)i * cols + c];
+    dbias[c] = sum;
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+
+struct DeviceFacts {
+    std::atomic<int> sms{0};
+};
+DeviceFacts g_facts[kMaxDevices];
+
+fi_status_t device_facts(int *sms, const char *name) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_fail(e, name);
+    if (dev < 0 || dev >= kMaxDevices) {
+        set_error("%s: device ordinal %d", name, dev);
+        return FI_ERR_UNSUPPORTED;
+    }
+    *sms = g_facts[dev].sms.load(std::memory_order_acquire);
+    if (*sms) return FI_OK;
+    int n = 0;
+    e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
+    if (e != cudaSuccess) return cuda_fail(e, name);
+    g_facts[dev].sms.store(n, std::memory_order_release);
+    *sms = n;
+    return FI_OK;
+}
+
+// one operand: `rows` lines of `dim` contiguous values
+struct Matrix {
+    const void *base;
+    long long rows, dim, ld;
+};
+
+fi_status_t operand_map(CUtensorMap *map, const Matrix &x, int box_rows, const char *name) {
+    static std::atomic<void *> entry{nullptr};
+    void *fn = entry.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            set_error("%s: cuTensorMapEncodeTiled is not available from this driver", name);
+            return FI_ERR_UNSUPPORTED;
+        }
+        entry.store(fn, std::memory_order_release);
+    }
+    const cuuint64_t size[2] = {(cuuint64_t)x.dim, (cuuint64_t)x.rows}, stride[1] = {(cuuint64_t)(x.rows > 1 ? x.ld : (x.dim + 7) / 8 * 8) * 2};
+    const cuuint32_t box[2] = {kKb, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const CUresult r = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(fn)(
+        map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(x.base), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_error("%s: cuTensorMapEncodeTiled failed with code %d (%lld x %lld values, %lld apart)", name, (int)r, x.rows, x.dim, x.ld);
+        return FI_ERR_CUDA;
+    }
+    return FI_OK;
+}
+
+// D[n][m] = sum over k of A(m, k) B(n, k); `p` holds what becomes of the sums
+fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, LinearParams p, int sms,
+                           cudaStream_t stream, const char *name) {
+    p.m = (int)m;
+    p.n = (int)n;
+    p.kb = (int)((k + kKb - 1) / kKb);
+    p.a_mn = a_mn;
+    p.b_mn = b_mn;
+    p.m_tiles = (int)((m + kM - 1) / kM);
+    // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
+    int widest = kMaxN;
+    if (f32) {
+        const int pieces = (p.kb + 7) / 8;
+        widest = pieces >= 32 ? 16 : 512 / pieces / 16 * 16;
+        if (widest > 128) widest = 128;
+    }
+    p.tile_n = n >= widest ? widest : (int)((n + 15) / 16 * 16);
+    const long long n_tiles = (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
+    p.split = 1;
+    while (p.split < 8 && tiles * p.split * 2 <= sms && p.kb >= 4 * p.split) p.split *= 2;
+    const int most = 512 / p.tile_n, blocks = (p.kb + p.split - 1) / p.split;
+    p.bufs = 1;
+    if (f32) p.bufs = (blocks + 7) / 8 < most ? (blocks + 7) / 8 : most;
+    p.tmem_cols = 32;
+    while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
+    p.b_bytes = b_mn ? (p.tile_n + 63) / 64 * 8192 : p.tile_n * kKb * 2;
+    const int stage = kABytes + p.b_bytes, room = kSmemMost - 1024 /* static */ - 1024 /* alignment */;
+    p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
+    int smem = p.stages * stage;
+    if (smem < p.tile_n * kM * 4) smem = p.tile_n * kM * 4;
+    smem += 1024;
+    if (tiles * p.split > 2147483647ll) {
+        set_error("%s: too many tiles", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    CUtensorMap map_a, map_b;
+    fi_status_t st = operand_map(&map_a, a, a_mn ? kKb : kM, name);
+    if (st == FI_OK) st = operand_map(&map_b, b, b_mn ? kKb : p.tile_n, name);
+    if (st != FI_OK) return st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = p.split;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * p.split));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = f32 ? cudaLaunchKernelEx(&cfg, linear_split_kernel<true>, map_a, map_b, p) : cudaLaunchKernelEx(&cfg, linear_split_kernel<false>, map_a, map_b, p);
+    if (e != cudaSuccess) return cuda_fail(e, name);
+    count_launch();
+    return check_launch(name);
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+fi_status_t check_sizes(long long tokens, int in_dim, int out_dim, int act, const char *name) {
+    if (tokens < 0 || tokens > 2147483647ll || in_dim < 8 || in_dim % 8 || out_dim < 8 || out_dim % 8) {
+        set_error("%s: in_dim and out_dim must be multiples of 8, 0 <= tokens < 2^31 (got %lld tokens, %d -> %d)", name, tokens, in_dim, out_dim);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (act < FI_ACT_NONE || act > FI_ACT_SILU) {
+        set_error("%s: unknown activation %d", name, act);
+        return FI_ERR_INVALID_ARG;
+    }
+    return FI_OK;
+}
+
+// rows of `dim` values that TMA reads: on 16-byte boundaries, strides below 2^39
+bool tma_rows(const void *p, long long rows, long long dim, long long ld) {
+    return aligned16(p) && (rows <= 1 || (ld % 8 == 0 && ld >= dim && ld < (1ll << 38)));
+}
+
+long long round256(long long v) { return (v + 255) / 256 * 256; }
+
+int slope_parts(long long tokens, int out_dim) {
+    const long long columns = (out_dim + kSlopeCols - 1) / kSlopeCols, groups = (tokens + kSlopeRows - 1) / kSlopeRows;
+    long long parts = (8 * 148 + columns - 1) / columns;
+    if (parts > (groups + 3) / 4) parts = (groups + 3) / 4;
+    return parts < 1 ? 1 : parts > 256 ? 256 : (int)parts;
+}
+
+}  // namespace
+}  // namespace fi
+
+using namespace fi;
+
+extern "C" {
+
+fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
+    const char *const name = "fi_linear";
+    if (!a) {
+        set_error("%s: null argument", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    fi_status_t st = check_sizes(a->tokens, a->in_dim, a->out_dim, a->activation, name);
+    if (st != FI_OK) return st;
+    if (a->out_dtype != FI_F32 && a->out_dtype != FI_BF16) {
+        set_error("%s: out_dtype must be FI_F32 or FI_BF16", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->tokens == 0) return FI_OK;
+    if (!a->x || !a->weight || !a->out) {
+        set_error("%s: null pointer", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    const long long out_rows = a->rows ? a->out_rows : a->tokens;
+    const int size = a->out_dtype == FI_F32 ? 4 : 2;
+    if (!tma_rows(a->x, a->tokens, a->in_dim, a->x_stride) || !tma_rows(a->weight, a->out_dim, a->in_dim, a->weight_stride)) {
+        set_error("%s: rows of x and weight must start on 16-byte boundaries and not overlap", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (out_rows < 0 || (out_rows > 1 && (a->out_stride < a->out_dim || (a->residual && a->residual_stride < a->out_dim))) ||
+        (a->preact && a->tokens > 1 && a->preact_stride < a->out_dim) || (reinterpret_cast<uintptr_t>(a->out) & (size - 1)) ||
+        (reinterpret_cast<uintptr_t>(a->residual) & (size - 1)) || (reinterpret_cast<uintptr_t>(a->preact) & 1) ||
+        (reinterpret_cast<uintptr_t>(a->bias) & 3) || a->wait_limit < 0) {
+        set_error("%s: rows of out, residual and preact must not overlap; pointers must be aligned to their types", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    int sms = 0;
+    st = device_facts(&sms, name);
+    if (st != FI_OK) return st;
+    LinearParams p = {};
+    p.bias = a->bias;
+    p.residual = a->residual;
+    p.out = a->out;
+    p.preact = static_cast<__nv_bfloat16 *>(a->preact);
+    p.rows = a->rows;
+    p.count = a->tokens_dev;
+    p.ld_res = a->residual_stride;
+    p.ld_out = a->out_stride;
+    p.ld_preact = a->preact_stride;
+    p.out_rows = out_rows;
+    p.wait_limit = a->wait_limit > 0 && a->wait_limit < kWaitLimit ? a->wait_limit : kWaitLimit;
+    p.act = a->activation;
+    const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
+    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, p, sms, static_cast<cudaStream_t>(cuda_stream),
+                          name);
+}
+
+int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation) {
+    if (tokens < 0 || tokens > 2147483647ll || out_dim < 8) return 0;
+    return round256((int64_t)slope_parts(tokens, out_dim) * out_dim * 4) + (activation != FI_ACT_NONE ? round256(tokens * out_dim * 2) : 0);
+}
+
+fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream) {
+    const char *const name = "fi_linear_backward";
+    if (!a) {
+        set_error("%s: null argument", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    fi_status_t st = check_sizes(a->tokens, a->in_dim, a->out_dim, a->activation, name);
+    if (st != FI_OK) return st;
+    const bool slopes = a->activation != FI_ACT_NONE;
+    if ((a->tokens > 0 && (!a->dy || (slopes && !a->preact) || (a->dx && !a->weight) || (a->dweight && !a->x))) ||
+        ((slopes || a->dbias) && !a->workspace)) {
+        set_error("%s: null pointer", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (!tma_rows(a->dy, a->tokens, a->out_dim, a->dy_stride) || (slopes && !tma_rows(a->preact, a->tokens, a->out_dim, a->preact_stride)) ||
+        (a->dx && !tma_rows(a->weight, a->out_dim, a->in_dim, a->weight_stride)) ||
+        (a->dweight && !tma_rows(a->x, a->tokens, a->in_dim, a->x_stride)) || !aligned16(a->workspace)) {
+        set_error("%s: rows of x, weight, dy and preact must start on 16-byte boundaries and not overlap", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if ((a->dx && a->tokens > 1 && a->dx_stride < a->in_dim) || (a->dweight && a->dweight_stride < a->in_dim) ||
+        (reinterpret_cast<uintptr_t>(a->dx) & 1) || (reinterpret_cast<uintptr_t>(a->dweight) & 1) || (reinterpret_cast<uintptr_t>(a->dbias) & 3)) {
+        set_error("%s: rows of dx and dweight must not overlap; pointers must be aligned to their types", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    int sms = 0;
+    st = device_facts(&sms, name);
+    if (st != FI_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (a->tokens == 0) {                                   // sums over nothing
+        cudaError_t e = cudaSuccess;
+        if (a->dweight) e = cudaMemset2DAsync(a->dweight, (size_t)a->dweight_stride * 2, 0, (size_t)a->in_dim * 2, (size_t)a->out_dim, stream);
+        if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, (size_t)a->out_dim * 4, stream);
+        return e == cudaSuccess ? FI_OK : cuda_fail(e, name);
+    }
+    const int parts = slope_parts(a->tokens, a->out_dim);
+    float *const partial = a->dbias ? static_cast<float *>(a->workspace) : nullptr;
+    __nv_bfloat16 *const dz = slopes ? reinterpret_cast<__nv_bfloat16 *>(static_cast<char *>(a->workspace) + round256((long long)parts * a->out_dim * 4)) : nullptr;
+    if ((slopes && (a->dx || a->dweight)) || a->dbias) {
+        linear_slope_kernel<<<dim3((a->out_dim + kSlopeCols - 1) / kSlopeCols, parts), kSlopeThreads, 0, stream>>>(
+            static_cast<const __nv_bfloat16 *>(a->dy), a->dy_stride, static_cast<const __nv_bfloat16 *>(a->preact), a->preact_stride, dz, partial, a->tokens,
+            a->out_dim, a->activation);
+        count_launch();
+        st = check_launch(name);
+        if (st != FI_OK) return st;
+    }
+    const Matrix g = slopes ? Matrix{dz, a->tokens, a->out_dim, a->out_dim} : Matrix{a->dy, a->tokens, a->out_dim, a->dy_stride};
+    LinearParams p = {};
+    p.wait_limit = kWaitLimit;
+    if (a->dx) {
+        p.out = a->dx;
+        p.ld_out = a->dx_stride;
+        p.out_rows = a->tokens;
+        const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride};
+        st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, p, sms, stream, name);
+        if (st != FI_OK) return st;
+    }
+    if (a->dweight) {
+        p.out = a->dweight;
+        p.ld_out = a->dweight_stride;
+        p.out_rows = a->out_dim;
+        const Matrix x = {a->x, a->tokens, a->in_dim, a->x_stride};
+        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, p, sms, stream, name);
+        if (st != FI_OK) return st;
+    }
+    if (a->dbias) {
+        linear_bias_sum_kernel<<<(a->out_dim + 255) / 256, 256, 0, stream>>>(partial, parts, a->out_dim, a->dbias);
+        count_launch();
+        st = check_launch(name);
+    }
+    return st;
+}
+
+fi_status_t fi_linear_poll_status(void) {
+    int32_t word = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&word, g_linear_status, sizeof word);
+    if (e == cudaSuccess && word) {
+        const int32_t zero = 0;
+        e = cudaMemcpyToSymbol(g_linear_status, &zero, sizeof zero);
+    }
+    if (e != cudaSuccess) return cuda_fail(e, "fi_linear_poll_status");
+    if (word) {
+        set_error("fi_linear: a wait inside a kernel ran out; its results are not valid");
+        return FI_ERR_TIMEOUT;
+    }
+    return FI_OK;
+}
+
+}  // extern "C"
