@@ -642,6 +642,42 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *args, void *cuda_stre
 int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation);
 fi_status_t fi_linear_poll_status(void);
 
+/*
+ * Norm of whole rows in front of those products, by mean and variance or (rms != 0) by root mean square:
+ *   n = (x - mean) / sqrt(mean((x - mean)^2) + eps), with rms mean = 0;  out = n * weight + bias
+ *   x [x_rows x dim], out [tokens x dim]: float32 or bfloat16 each (x_dtype, y_dtype); weight, bias [dim] float, nullable (ones, zeros)
+ *   rows [tokens] device int32, nullable: row of x of each token (miss_idx of a cascade step); null: token i is row i.  A token whose row
+ *   is outside [0, x_rows) is left out.  tokens_dev as in fi_linear; rows of out that are left out are untouched.
+ * 1 <= dim <= 16384, strides between rows in elements, any alignment (16-byte boundaries and dim a multiple of 8 are faster).  out may
+ * be x itself when types and rows are the same.  Arithmetic in fp32 (a row whose squares float32 does not hold has no finite norm),
+ * rounded once.  Asynchronous, on the current device.
+ *
+ * fi_layer_norm_backward: gradients for dy [tokens x dim] (y_dtype), from the same x (nothing of the forward is kept):
+ *   g = dy * weight;  out = dx = (g - mean(g) - n * mean(g * n)) / sqrt(...), with rms without mean(g);  dweight = sum of dy * n, dbias = sum of dy
+ * dx (x_dtype) may be dy itself when their types are the same.  dweight, dbias [dim] float, overwritten, nullable; the sums run in a fixed
+ * order.  `workspace`: fi_layer_norm_workspace(dim) bytes of device memory, contents free, not shared by calls that overlap; may be null
+ * when both are.  rows and tokens_dev must be null.
+ */
+typedef struct {
+    const void *x, *dy;         /* dy: backward only */
+    void *out;                  /* result; backward: dx */
+    const float *weight, *bias; /* nullable */
+    const int32_t *rows;        /* nullable */
+    const int32_t *tokens_dev;  /* nullable */
+    float *dweight, *dbias;     /* backward only */
+    void *workspace;            /* backward only */
+    int64_t x_stride, dy_stride, out_stride;
+    int64_t tokens;
+    int64_t x_rows;             /* read with `rows` only */
+    int32_t dim;
+    int32_t rms;
+    int32_t x_dtype, y_dtype;   /* fi_dtype_t */
+    float eps;
+} fi_layer_norm_t;
+fi_status_t fi_layer_norm(const fi_layer_norm_t *args, void *cuda_stream);
+fi_status_t fi_layer_norm_backward(const fi_layer_norm_t *args, void *cuda_stream);
+int64_t fi_layer_norm_workspace(int32_t dim);
+
 /* Number of kernels this library has launched in the calling process (all caches). */
 int64_t fi_launch_count(void);
 

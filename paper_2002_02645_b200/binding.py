@@ -33,7 +33,8 @@ EXPORTS = ["fi_cache_create", "fi_cache_destroy", "fi_cache_insert", "fi_cache_s
            "fi_pages_create", "fi_pages_destroy", "fi_pages_extend", "fi_pages_release", "fi_head_norm_rope",
            "fi_head_norm_rope_backward", "fi_head_norm_rope_workspace", "fi_kv_create", "fi_kv_destroy", "fi_kv_append",
            "fi_kv_attend", "fi_kv_set_wait_limit", "fi_kv_poll_status", "fi_linear", "fi_linear_backward",
-           "fi_linear_backward_workspace", "fi_linear_poll_status", "fi_launch_count", "fi_last_error", "fi_status_string"]
+           "fi_linear_backward_workspace", "fi_linear_poll_status", "fi_layer_norm", "fi_layer_norm_backward", "fi_layer_norm_workspace",
+           "fi_launch_count", "fi_last_error", "fi_status_string"]
 
 
 class fi_cache_config_t(ctypes.Structure):
@@ -104,6 +105,12 @@ class fi_linear_backward_t(ctypes.Structure):
     _fields_ = _fields(ctypes.c_void_p, "x weight dy preact dx dweight dbias workspace") \
         + _fields(ctypes.c_int64, "x_stride weight_stride dy_stride preact_stride dx_stride dweight_stride tokens") \
         + _fields(ctypes.c_int32, "in_dim out_dim activation")
+
+
+class fi_layer_norm_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "x dy out weight bias rows tokens_dev dweight dbias workspace") \
+        + _fields(ctypes.c_int64, "x_stride dy_stride out_stride tokens x_rows") \
+        + _fields(ctypes.c_int32, "dim rms x_dtype y_dtype") + [("eps", ctypes.c_float)]
 
 
 class FiError(RuntimeError):
@@ -187,6 +194,10 @@ def load_library(path: Optional[str] = None):
     lib.fi_linear_backward_workspace.argtypes = [i64, i32, i32]
     lib.fi_linear_backward_workspace.restype = i64
     lib.fi_linear_poll_status.argtypes = []
+    lib.fi_layer_norm.argtypes = [ctypes.c_char_p, vp]                 # a packed fi_layer_norm_t
+    lib.fi_layer_norm_backward.argtypes = [ctypes.c_char_p, vp]
+    lib.fi_layer_norm_workspace.argtypes = [i32]
+    lib.fi_layer_norm_workspace.restype = i64
     lib.fi_launch_count.argtypes = []
     lib.fi_launch_count.restype = i64
     lib.fi_last_error.argtypes = []
@@ -614,8 +625,9 @@ def _packer(kind) -> struct.Struct:
     return p
 
 
-_pack_extend, _pack_norm, _pack_append, _pack_attend, _pack_linear, _pack_linear_backward = (
-    _packer(k).pack for k in (fi_pages_extend_t, fi_head_norm_rope_t, fi_kv_append_t, fi_kv_attend_t, fi_linear_t, fi_linear_backward_t))
+_pack_extend, _pack_norm, _pack_append, _pack_attend, _pack_linear, _pack_linear_backward, _pack_layer_norm = (
+    _packer(k).pack for k in (fi_pages_extend_t, fi_head_norm_rope_t, fi_kv_append_t, fi_kv_attend_t, fi_linear_t, fi_linear_backward_t,
+                               fi_layer_norm_t))
 
 
 def _at(t: Optional[torch.Tensor]) -> int:
@@ -1022,6 +1034,91 @@ class _Linear(torch.autograd.Function):
             dx, dw, db = linear_backward(x if need[1] else None, weight if need[0] else None, _as_rows(dy), preact=preact,
                                          activation=ctx.activation, with_bias=need[2])
         return dx, dw, db, dy if need[3] else None, None, None, None
+
+
+def _norm_types(x: torch.Tensor, y_dtype, weight, bias, index: int):
+    if x.dtype not in _FI_DTYPE or x.dim() != 2 or index < 0:
+        raise ValueError("x must be a float32 or bfloat16 [rows, dim] tensor on a GPU")
+    if y_dtype not in _FI_DTYPE:
+        raise ValueError("the result must be float32 or bfloat16")
+    for w, name in ((weight, "weight"), (bias, "bias")):
+        if w is not None and w.numel() != x.size(1):
+            raise ValueError(f"{name} must have {x.size(1)} values")
+        _check_flat(w, name, index, 0, torch.float32)
+    return _FI_DTYPE[x.dtype], _FI_DTYPE[y_dtype]
+
+
+def _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out):
+    index = x.get_device()
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    kinds = _norm_types(x, out_dtype, weight, bias, index)
+    x_rows, dim = x.shape
+    x_stride = _check_rows(x, "x", index, x.dtype, x_rows, dim)
+    _check_flat(rows, "rows", index)
+    _check_flat(count, "count", index, 1)
+    tokens = x_rows if rows is None else rows.numel()
+    if out is None:
+        out = torch.empty((tokens, dim), dtype=out_dtype, device=x.device)
+        out_stride = dim
+    else:
+        out_stride = _check_rows(out, "out", index, out_dtype, tokens, dim)
+    args = _pack_layer_norm(x.data_ptr(), 0, out.data_ptr(), _at(weight), _at(bias), _at(rows), _at(count), 0, 0, 0, x_stride, 0, out_stride, tokens,
+                            x_rows, dim, 1 if rms else 0, *kinds, eps)
+    _on_device(index, load_library().fi_layer_norm, args)
+    return out
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, eps: float = 1e-5, rms: bool = False,
+               out_dtype: Optional[torch.dtype] = None, rows: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """fi_layer_norm: the rows of x [rows, dim] normed by mean and variance, or by root mean square.  With `rows`, token i of the result is
+    row rows[i] of x; with `count` only that many tokens are real (the others are left as they are).  Gradients flow to x, weight and
+    bias; not through rows, count or out, which are refused where one is asked for."""
+    if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad):
+        if out is not None or rows is not None or count is not None:
+            raise ValueError("out, rows or count is given, but a gradient is asked for")
+        return _LayerNorm.apply(x, weight, bias, eps, rms, out_dtype)
+    return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out)
+
+
+def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: torch.Tensor, *, eps: float = 1e-5, rms: bool = False,
+                        with_bias: bool = False, dx: Optional[torch.Tensor] = None):
+    """fi_layer_norm_backward: (dx, dweight, dbias) from the forward pass's x and weight and the gradient of its result.  Without a weight
+    there is no dweight, and dbias only with with_bias.  dx may be dy."""
+    lib, index = load_library(), x.get_device()
+    kinds = _norm_types(x, dy.dtype, weight, None, index)
+    tokens, dim = x.shape
+    x_stride, dy_stride = _check_rows(x, "x", index, x.dtype, tokens, dim), _check_rows(dy, "dy", index, dy.dtype, tokens, dim)
+    if dx is None:
+        dx = torch.empty((tokens, dim), dtype=x.dtype, device=x.device)
+    dx_stride = _check_rows(dx, "dx", index, x.dtype, tokens, dim)
+    dw = torch.empty(dim, dtype=torch.float32, device=x.device) if weight is not None else None
+    db = torch.empty(dim, dtype=torch.float32, device=x.device) if with_bias else None
+    work = None
+    if dw is not None or db is not None:
+        work = torch.empty(lib.fi_layer_norm_workspace(dim), dtype=torch.uint8, device=x.device)
+    args = _pack_layer_norm(x.data_ptr(), dy.data_ptr(), dx.data_ptr(), _at(weight), 0, 0, 0, _at(dw), _at(db), _at(work), x_stride, dy_stride, dx_stride,
+                            tokens, 0, dim, 1 if rms else 0, *kinds, eps)
+    _on_device(index, lib.fi_layer_norm_backward, args)
+    return dx, dw, db
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, rms, out_dtype):
+        ctx.save_for_backward(x, weight)
+        ctx.eps, ctx.rms, ctx.bias = eps, rms, None if bias is None else bias.shape
+        return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, None, None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight = ctx.saved_tensors
+        if dy.stride(1) != 1 or dy.stride(0) < dy.size(1):
+            dy = dy.contiguous()
+        dx, dw, db = layer_norm_backward(x, weight, dy, eps=ctx.eps, rms=ctx.rms, with_bias=ctx.needs_input_grad[2])
+        return dx, None if dw is None else dw.view_as(weight), None if db is None else db.view(ctx.bias), None, None, None
 
 
 class KvCache:

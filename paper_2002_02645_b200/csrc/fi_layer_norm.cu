@@ -1,0 +1,457 @@
+// Norm of whole rows, by mean and variance or by root mean square, and its gradients.
+//
+//   n = (x - mean) r, r = 1 / sqrt(mean((x - mean)^2) + eps);  y = n w + b        (rms: mean taken as 0)
+//   backward:  g = dy w;  dx = r (g - mean(g) - n mean(g n));  dw = sum dy n, db = sum dy        (rms: without mean(g))
+//
+// A row is held in registers by a warp (up to 1,024 values) or a CTA, so that it is read once, its deviations are squared after the
+// mean is known, and it is written once: the bound is the traffic.  Nothing of the forward pass is kept for the gradients; mean
+// and r come again from x, which they read anyway.
+#include <cuda_bf16.h>
+
+#include <type_traits>
+
+#include "fi_internal.cuh"
+
+namespace fi {
+namespace {
+
+constexpr int kMaxDim = 16384;
+constexpr int kMaxPartials = 1024;     // CTAs of a backward pass, at most
+
+struct RowNormParams {
+    const void *x, *dy;
+    void *out;                         // y, or dx
+    const float *weight, *bias;
+    const int32_t *rows, *count;
+    float *partial;                    // backward: [CTAs][2][dim]; nullable
+    long long x_stride, dy_stride, out_stride, tokens, x_rows;
+    int dim, rms;
+    float eps, inv_dim;
+};
+
+// 8 values of a row (VEC), widened to fp32
+template <bool F32>
+struct Raw8 {
+    uint4 w[F32 ? 2 : 1];
+};
+template <bool F32>
+__device__ __forceinline__ Raw8<F32> fetch8(const void *base, long long at) {
+    Raw8<F32> r;
+    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + at * (F32 ? 4 : 2));
+    r.w[0] = __ldcs(p);
+    if constexpr (F32) r.w[1] = __ldcs(p + 1);
+    return r;
+}
+template <bool F32>
+__device__ __forceinline__ void widen8(const Raw8<F32> &r, float *x) {
+    const uint32_t u[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+    if constexpr (F32) {
+        const uint32_t v[4] = {r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = __uint_as_float(u[i]);
+            x[4 + i] = __uint_as_float(v[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(u[i] << 16);
+            x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void store8(void *base, long long at, const float *x) {
+    if constexpr (F32) {
+        float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(base) + at);
+        p[0] = make_float4(x[0], x[1], x[2], x[3]);
+        p[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = reinterpret_cast<const uint32_t &>(h);
+        }
+        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(base) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <bool F32>
+__device__ __forceinline__ float load1(const void *base, long long at) {
+    if constexpr (F32) return static_cast<const float *>(base)[at];
+    return __bfloat162float(static_cast<const __nv_bfloat16 *>(base)[at]);
+}
+template <bool F32>
+__device__ __forceinline__ void store1(void *base, long long at, float v) {
+    if constexpr (F32) static_cast<float *>(base)[at] = v;
+    else static_cast<__nv_bfloat16 *>(base)[at] = __float2bfloat16_rn(v);
+}
+// 8 floats of a weight, which stay in L1: loaded where they are used, so that they do not hold registers in between
+__device__ __forceinline__ void load8_again(const float *p, float *x) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(x[4 * i]), "=f"(x[4 * i + 1]), "=f"(x[4 * i + 2]), "=f"(x[4 * i + 3])
+                     : "l"(p + 4 * i));
+}
+
+// The values of a row that a thread of a group of `group` threads holds: P pieces of 8 neighbours (VEC), or 8 P values that lie
+// `group` apart, for rows that start on no 16-byte boundary.
+template <bool VEC, int P>
+struct Place {
+    int t, group, dim;
+    __device__ __forceinline__ int piece(int p) const { return (t + p * group) * 8; }
+    __device__ __forceinline__ int value(int i) const { return VEC ? piece(i >> 3) + (i & 7) : t + i * group; }
+    __device__ __forceinline__ bool has(int i) const { return (VEC ? piece(i >> 3) : value(i)) < dim; }
+};
+
+template <bool F32, bool VEC, int P>
+__device__ __forceinline__ void load_row(const Place<VEC, P> &l, const void *base, long long at, float (&v)[8 * P]) {
+    if constexpr (VEC) {
+        Raw8<F32> raw[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (l.piece(p) < l.dim) raw[p] = fetch8<F32>(base, at + l.piece(p));
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (l.piece(p) < l.dim) widen8<F32>(raw[p], v + 8 * p);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * p + i] = 0.f;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i) v[i] = l.has(i) ? load1<F32>(base, at + l.value(i)) : 0.f;
+    }
+}
+template <bool F32, bool VEC, int P>
+__device__ __forceinline__ void store_row(const Place<VEC, P> &l, void *base, long long at, const float (&v)[8 * P]) {
+    if constexpr (VEC) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (l.piece(p) < l.dim) store8<F32>(base, at + l.piece(p), v + 8 * p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i)
+            if (l.has(i)) store1<F32>(base, at + l.value(i), v[i]);
+    }
+}
+// f(index into the registers, weight of that value)
+template <bool VEC, int P, typename F>
+__device__ __forceinline__ void with_weight(const Place<VEC, P> &l, const float *w, F &&f) {
+    if constexpr (VEC) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (l.piece(p) < l.dim) {
+                float x[8];
+                load8_again(w + l.piece(p), x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f(8 * p + i, x[i]);
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i)
+            if (l.has(i)) f(i, __ldg(w + l.value(i)));
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+// sums over the group: a warp, or the CTA (every warp adds up the warps' sums in the same order).  `slot`: one of four places in
+// turn, so that one barrier a sum is enough
+template <bool WARP, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], float (*s)[32][2], int &slot) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+    if constexpr (!WARP) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[slot][warp][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? s[slot][lane][i] : 0.f);
+        slot = (slot + 1) & 3;
+    }
+}
+
+// mean and r of the row in v; v becomes x - mean
+template <bool WARP, bool VEC, int P>
+__device__ __forceinline__ float deviations(const RowNormParams &p, const Place<VEC, P> &l, float (&v)[8 * P], float (*s)[32][2], int &slot) {
+    if (!p.rms) {
+        float sum[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i) sum[0] += v[i];
+        group_sum<WARP>(sum, s, slot);
+        const float mean = sum[0] / (float)p.dim;           // (divided: equal values have no deviation)
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i) v[i] = l.has(i) ? v[i] - mean : 0.f;
+    }
+    float sq[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < 8 * P; ++i) sq[0] = fmaf(v[i], v[i], sq[0]);
+    group_sum<WARP>(sq, s, slot);
+    return rsqrtf(fmaf(sq[0], p.inv_dim, p.eps));
+}
+
+__device__ __forceinline__ long long actual_tokens(const RowNormParams &p) {
+    if (!p.count) return p.tokens;
+    const long long c = *p.count;
+    return c < 0 ? 0 : c > p.tokens ? p.tokens : c;
+}
+
+template <bool X32, bool Y32, bool WARP, bool VEC, int P>
+__global__ void __launch_bounds__(WARP ? 128 : 512) layer_norm_kernel(const RowNormParams p) {
+    __shared__ float s[4][32][2];
+    int slot = 0;
+    const Place<VEC, P> l = {WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x, WARP ? 32 : (int)blockDim.x, p.dim};
+    const long long token = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+    if (token >= actual_tokens(p)) return;                  // (the whole group)
+    const long long row = p.rows ? p.rows[token] : token;
+    if (row < 0 || row >= p.x_rows) return;
+    float v[8 * P];
+    load_row<X32>(l, p.x, row * p.x_stride, v);
+    const float r = deviations<WARP>(p, l, v, s, slot);
+    if (p.weight) with_weight(l, p.weight, [&](int i, float w) { v[i] = v[i] * r * w; });
+    else
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i) v[i] *= r;
+    if (p.bias) with_weight(l, p.bias, [&](int i, float b) { v[i] += b; });
+    store_row<Y32>(l, p.out, token * p.out_stride, v);
+}
+
+// Rows are dealt out to the groups of the grid in turn; a thread gathers its columns of both weight gradients over all of them.
+template <bool X32, bool Y32, bool WARP, bool VEC, int P>
+__global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(const RowNormParams p) {
+    constexpr int V = 8 * P;
+    __shared__ float s[4][32][2];
+    extern __shared__ float sums[];                         // WARP: [warps][dim]
+    int slot = 0;
+    const Place<VEC, P> l = {WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x, WARP ? 32 : (int)blockDim.x, p.dim};
+    const int groups_here = WARP ? blockDim.x >> 5 : 1, mine = WARP ? threadIdx.x >> 5 : 0;
+    float dw[V] = {}, db[V] = {};
+    for (long long row = (long long)blockIdx.x * groups_here + mine; row < p.tokens; row += (long long)gridDim.x * groups_here) {
+        float v[V], g[V];
+        load_row<X32>(l, p.x, row * p.x_stride, v);
+        load_row<Y32>(l, p.dy, row * p.dy_stride, g);
+        const float r = deviations<WARP>(p, l, v, s, slot);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            v[i] *= r;                                      // n
+            dw[i] = fmaf(g[i], v[i], dw[i]);
+            db[i] += g[i];
+        }
+        if (p.weight) with_weight(l, p.weight, [&](int i, float w) { g[i] *= w; });
+        float both[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            both[0] += g[i];
+            both[1] = fmaf(g[i], v[i], both[1]);
+        }
+        group_sum<WARP>(both, s, slot);
+        const float less = p.rms ? 0.f : both[0] * p.inv_dim, along = both[1] * p.inv_dim;
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = r * (g[i] - less - v[i] * along);
+        store_row<X32>(l, p.out, row * p.out_stride, g);
+    }
+    if (!p.partial) return;
+    float *const to = p.partial + (long long)blockIdx.x * 2 * p.dim;
+    if constexpr (!WARP) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (l.has(i)) {
+                to[l.value(i)] = dw[i];
+                to[p.dim + l.value(i)] = db[i];
+            }
+    } else {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (which) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (l.has(i)) sums[mine * p.dim + l.value(i)] = which ? db[i] : dw[i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < p.dim; c += blockDim.x) {
+                float total = 0.f;
+                for (int g = 0; g < groups_here; ++g) total += sums[g * p.dim + c];
+                to[which * p.dim + c] = total;
+            }
+        }
+    }
+}
+
+// Weight gradients from the CTAs' sums, 32 columns per CTA, always in the same order.
+__global__ void __launch_bounds__(1024) layer_norm_sum_kernel(const float *partial, int parts, int dim, float *dweight, float *dbias) {
+    __shared__ float s[32][33];
+    float *const out = blockIdx.y ? dbias : dweight;
+    if (!out) return;
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    float sum = 0.f;
+    if (col < dim)
+        for (int b = part; b < parts; b += 32) sum += partial[((long long)b * 2 + blockIdx.y) * dim + col];
+    s[part][lane] = sum;
+    __syncthreads();
+    if (part == 0 && col < dim) {
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) total += s[i][lane];
+        out[col] = total;
+    }
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <bool X32, bool Y32, bool VEC>
+void launch_forward(const RowNormParams &p, cudaStream_t stream) {
+    if (p.dim <= 1024) {
+        const unsigned grid = (unsigned)((p.tokens + 3) / 4);
+        if (p.dim <= 256) layer_norm_kernel<X32, Y32, true, VEC, 1><<<grid, 128, 0, stream>>>(p);
+        else if (p.dim <= 512) layer_norm_kernel<X32, Y32, true, VEC, 2><<<grid, 128, 0, stream>>>(p);
+        else layer_norm_kernel<X32, Y32, true, VEC, 4><<<grid, 128, 0, stream>>>(p);
+    } else {
+        const int threads = p.dim <= 4096 ? 128 : p.dim <= 8192 ? 256 : 512;
+        layer_norm_kernel<X32, Y32, false, VEC, 4><<<(unsigned)p.tokens, threads, 0, stream>>>(p);
+    }
+}
+
+template <bool X32, bool Y32, bool VEC>
+int launch_backward(const RowNormParams &p, int sms, cudaStream_t stream) {
+    if (p.dim <= 1024) {
+        const long long want = (p.tokens + 7) / 8, most = 2 * sms < kMaxPartials ? 2 * sms : kMaxPartials;
+        const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
+        const size_t smem = (size_t)8 * p.dim * sizeof(float);
+        if (p.dim <= 256) layer_norm_backward_kernel<X32, Y32, true, VEC, 1><<<grid, 256, smem, stream>>>(p);
+        else if (p.dim <= 512) layer_norm_backward_kernel<X32, Y32, true, VEC, 2><<<grid, 256, smem, stream>>>(p);
+        else layer_norm_backward_kernel<X32, Y32, true, VEC, 4><<<grid, 256, smem, stream>>>(p);
+        return (int)grid;
+    }
+    const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
+    const long long most = sms * (512 / threads) < kMaxPartials ? sms * (512 / threads) : kMaxPartials;
+    const unsigned grid = (unsigned)(p.tokens < 1 ? 1 : p.tokens < most ? p.tokens : most);
+    if (p.dim <= 8192) layer_norm_backward_kernel<X32, Y32, false, VEC, 2><<<grid, threads, 0, stream>>>(p);
+    else layer_norm_backward_kernel<X32, Y32, false, VEC, 4><<<grid, threads, 0, stream>>>(p);
+    return (int)grid;
+}
+
+template <typename F>
+void with_types(bool x32, bool y32, bool vec, F &&f) {
+    const auto types = [&](auto x, auto y) {
+        if (vec) f(x, y, std::true_type{});
+        else f(x, y, std::false_type{});
+    };
+    if (x32 && y32) types(std::true_type{}, std::true_type{});
+    else if (x32) types(std::true_type{}, std::false_type{});
+    else if (y32) types(std::false_type{}, std::true_type{});
+    else types(std::false_type{}, std::false_type{});
+}
+
+fi_status_t check_args(const fi_layer_norm_t *a, bool backward, const char *name) {
+    if (!a) {
+        set_error("%s: null argument", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if ((a->x_dtype != FI_F32 && a->x_dtype != FI_BF16) || (a->y_dtype != FI_F32 && a->y_dtype != FI_BF16)) {
+        set_error("%s: types must be FI_F32 or FI_BF16", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->dim < 1 || a->dim > kMaxDim || a->tokens < 0 || a->tokens > 2147483647ll || (a->rows && a->x_rows < 0)) {
+        set_error("%s: 1 <= dim <= %d, 0 <= tokens < 2^31 (got %lld rows of %d)", name, kMaxDim, (long long)a->tokens, a->dim);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->tokens > 0 && ((!a->x && !(a->rows && a->x_rows == 0)) || !a->out || (backward && !a->dy))) {
+        set_error("%s: null pointer", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (backward && (a->rows || a->tokens_dev)) {
+        set_error("%s: gradients of all rows only", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    if (backward && (a->dweight || a->dbias) && !a->workspace) {
+        set_error("%s: weight gradients need a workspace", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    const uintptr_t x_size = a->x_dtype == FI_F32 ? 4 : 2, y_size = a->y_dtype == FI_F32 ? 4 : 2;
+    const long long x_rows = a->rows ? a->x_rows : a->tokens;
+    const auto off = [](const void *p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; };
+    if (off(a->x, x_size) || off(a->out, backward ? x_size : y_size) || (backward && off(a->dy, y_size)) || off(a->weight, 4) || off(a->bias, 4) ||
+        off(a->workspace, 16) || (x_rows > 1 && a->x_stride < a->dim) || (a->tokens > 1 && (a->out_stride < a->dim || (backward && a->dy_stride < a->dim)))) {
+        set_error("%s: rows must not overlap; pointers must be aligned to their types", name);
+        return FI_ERR_INVALID_ARG;
+    }
+    return FI_OK;
+}
+
+RowNormParams row_norm_params(const fi_layer_norm_t *a, bool backward, bool *vec) {
+    RowNormParams p = {};
+    p.x = a->x;
+    p.dy = a->dy;
+    p.out = a->out;
+    p.weight = a->weight;
+    p.bias = a->bias;
+    p.rows = a->rows;
+    p.count = a->tokens_dev;
+    p.partial = backward && (a->dweight || a->dbias) ? static_cast<float *>(a->workspace) : nullptr;
+    p.x_stride = a->x_stride;
+    p.dy_stride = a->dy_stride;
+    p.out_stride = a->out_stride;
+    p.tokens = a->tokens;
+    p.x_rows = a->rows ? a->x_rows : a->tokens;
+    p.dim = a->dim;
+    p.rms = a->rms != 0;
+    p.eps = a->eps;
+    p.inv_dim = 1.f / (float)a->dim;
+    const auto unit = [](int dtype) { return dtype == FI_F32 ? 4 : 8; };
+    const int out_unit = unit(backward ? a->x_dtype : a->y_dtype);
+    *vec = a->dim % 8 == 0 && aligned16(a->x) && aligned16(a->out) && aligned16(a->weight) && aligned16(a->bias) &&
+           (p.x_rows <= 1 || a->x_stride % unit(a->x_dtype) == 0) && (a->tokens <= 1 || a->out_stride % out_unit == 0) &&
+           (!backward || (aligned16(a->dy) && (a->tokens <= 1 || a->dy_stride % unit(a->y_dtype) == 0)));
+    return p;
+}
+
+}  // namespace
+}  // namespace fi
+
+using namespace fi;
+
+extern "C" {
+
+int64_t fi_layer_norm_workspace(int32_t dim) { return dim < 1 || dim > kMaxDim ? 0 : (int64_t)kMaxPartials * 2 * dim * sizeof(float); }
+
+fi_status_t fi_layer_norm(const fi_layer_norm_t *a, void *cuda_stream) {
+    fi_status_t st = check_args(a, false, "fi_layer_norm");
+    if (st != FI_OK || a->tokens == 0) return st;
+    bool vec;
+    const RowNormParams p = row_norm_params(a, false, &vec);
+    with_types(a->x_dtype == FI_F32, a->y_dtype == FI_F32, vec, [&](auto x, auto y, auto v) {
+        launch_forward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, static_cast<cudaStream_t>(cuda_stream));
+    });
+    count_launch();
+    return check_launch("fi_layer_norm");
+}
+
+fi_status_t fi_layer_norm_backward(const fi_layer_norm_t *a, void *cuda_stream) {
+    fi_status_t st = check_args(a, true, "fi_layer_norm_backward");
+    if (st != FI_OK) return st;
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_fail(e, "fi_layer_norm_backward");
+    bool vec;
+    const RowNormParams p = row_norm_params(a, true, &vec);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    int parts = 0;
+    with_types(a->x_dtype == FI_F32, a->y_dtype == FI_F32, vec, [&](auto x, auto y, auto v) {
+        parts = launch_backward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, sms, stream);
+    });
+    count_launch();
+    if (p.partial) {
+        layer_norm_sum_kernel<<<dim3((a->dim + 31) / 32, 2), 1024, 0, stream>>>(p.partial, parts, a->dim, a->dweight, a->dbias);
+        count_launch();
+    }
+    return check_launch("fi_layer_norm_backward");
+}
+
+}  // extern "C"

@@ -592,7 +592,7 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
         set_error("%s: out_dtype must be FI_F32 or FI_BF16", name);
         return FI_ERR_INVALID_ARG;
     }
-    if (a->tokens == 0) return FI_OK;
+    if (a->tokens == 0 || (a->rows && a->out_rows == 0)) return FI_OK;
     if (!a->x || !a->weight || !a->out) {
         set_error("%s: null pointer", name);
         return FI_ERR_INVALID_ARG;
