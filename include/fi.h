@@ -584,6 +584,80 @@ fi_status_t fi_kv_set_wait_limit(fi_kv_t *kv, int64_t limit_cycles);
 fi_status_t fi_kv_poll_status(fi_kv_t *kv);
 
 /*
+ * Requests that branch: pages with several owners.
+ *
+ * A request may be forked into others that begin as it does (several continuations of one prompt).  Its full pages are shared; its last
+ * page, when it is not full, is still written to, so each copy gets one of its own.  shared[page] (device int32, [num_pages], zeros at
+ * first) counts the owners of a page beyond the first; a page that fi_pages_extend hands out or writes to has one owner, so that call
+ * need not know of it.  Where pages are shared, rows are given back by fi_pages_free, not by fi_pages_release.
+ *
+ * fi_pages_fork: row dst_rows[i], which must be empty, begins as row src_rows[i].  Tails get pages from the end of the free stack, in request
+ * order.  A request is refused when a row is outside [0, rows), both are the same, dst_rows[i] is not empty, the table is too short for it, or
+ * no page is left for its tail after the tails wanted before it.  A row may be a source several times, a destination once.
+ *   copies [batch_max x 3]: page to copy, page to fill, tokens to copy; (-1, -1, 0) where there is nothing to copy: for fi_kv_copy_pages,
+ *   in this stream before anything is stored for the new rows or read from them.  granted [batch_max]: 1, or 0 for the refused and those past
+ *   the batch count.  block_table and shared are written in place; lens_out / free_count_out as in fi_pages_extend.
+ * fi_pages_free: the listed rows give up their pages and their lengths become 0.  Pages without another owner go behind the free stack, in
+ * order of their numbers.  A row must not be listed twice.  num_pages <= 4194304.
+ * fi_pages_compact: the pages in use move to the low end of the pool: those at or above the number of pages in use, in order, to the free
+ * places below it, in order.  copies [max_copies x 3] as above (whole pages), max_copies >= num_pages / 2, moves [1] their number; entries
+ * past it are (-1, -1, 0).  Rewritten in place: block_table (entries of pages in use), shared, and the free stack, lowest page on top.  Every
+ * page must be in use or in the free stack.  workspace: fi_pages_compact_workspace(num_pages) bytes, contents free.
+ * fi_kv_copy_pages: copies what the listed tokens of pages hold, keys and values.  count [1] device int32, nullable: actual number of copies.
+ * Entries with a negative source are skipped; pages outside the pool are skipped and reported by fi_kv_poll_status.  No page that is filled may
+ * be listed again.
+ * All asynchronous.  Results do not depend on timing.  Calls of one fi_pages_t share its counters and must be ordered on one stream.
+ */
+typedef struct {
+    const int32_t *lens;        /* [rows] */
+    const int32_t *free_pages;  /* [num_pages] */
+    const int32_t *free_count;  /* [1] */
+    int32_t *block_table;       /* [rows x table_ld] */
+    int32_t *shared;            /* [num_pages] */
+    const int32_t *src_rows, *dst_rows; /* [batch_max] */
+    const int32_t *batch_count; /* [1] nullable */
+    int32_t *granted;           /* out [batch_max] */
+    int32_t *copies;            /* out [batch_max x 3] */
+    int32_t *lens_out;          /* out [rows]; may be lens */
+    int32_t *free_count_out;    /* out [1]; may be free_count */
+    int64_t table_ld;
+    int32_t rows, num_pages, batch_max;
+} fi_pages_fork_t;
+fi_status_t fi_pages_fork(fi_pages_t *pages, const fi_pages_fork_t *args, void *cuda_stream);
+
+typedef struct {
+    const int32_t *row_idx;     /* [batch_max] */
+    const int32_t *batch_count; /* [1] nullable */
+    const int32_t *lens;        /* [rows] */
+    const int32_t *block_table; /* [rows x table_ld] */
+    const int32_t *free_count;  /* [1] */
+    int32_t *free_pages;        /* [num_pages], written behind *free_count */
+    int32_t *shared;            /* [num_pages] */
+    int32_t *lens_out;          /* out [rows]; may be lens */
+    int32_t *free_count_out;    /* out [1]; may be free_count */
+    int64_t table_ld;
+    int32_t rows, num_pages, batch_max;
+} fi_pages_free_t;
+fi_status_t fi_pages_free(fi_pages_t *pages, const fi_pages_free_t *args, void *cuda_stream);
+
+typedef struct {
+    const int32_t *lens;        /* [rows] */
+    const int32_t *free_count;  /* [1] */
+    int32_t *free_pages;        /* [num_pages] */
+    int32_t *block_table;       /* [rows x table_ld] */
+    int32_t *shared;            /* [num_pages] */
+    int32_t *copies;            /* out [max_copies x 3] */
+    int32_t *moves;             /* out [1] */
+    void *workspace;
+    int64_t table_ld;
+    int32_t rows, num_pages, max_copies;
+} fi_pages_compact_t;
+fi_status_t fi_pages_compact(fi_pages_t *pages, const fi_pages_compact_t *args, void *cuda_stream);
+int64_t fi_pages_compact_workspace(int32_t num_pages);
+
+fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_copies, const int32_t *count, void *cuda_stream);
+
+/*
  * The products of a layer, for all requests or for those that were not frozen:
  *   y[i] = act(x[i] W^T + bias) + residual[rows[i]],  stored in row rows[i] of out
  *   x [tokens x in_dim] bfloat16; weight [out_dim x in_dim] bfloat16; bias [out_dim] float, nullable

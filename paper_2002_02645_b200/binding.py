@@ -34,6 +34,7 @@ EXPORTS = ["fi_cache_create", "fi_cache_destroy", "fi_cache_insert", "fi_cache_s
            "fi_head_norm_rope_backward", "fi_head_norm_rope_workspace", "fi_kv_create", "fi_kv_destroy", "fi_kv_append",
            "fi_kv_attend", "fi_kv_set_wait_limit", "fi_kv_poll_status", "fi_linear", "fi_linear_backward",
            "fi_linear_backward_workspace", "fi_linear_poll_status", "fi_layer_norm", "fi_layer_norm_backward", "fi_layer_norm_workspace",
+           "fi_pages_fork", "fi_pages_free", "fi_pages_compact", "fi_pages_compact_workspace", "fi_kv_copy_pages",
            "fi_launch_count", "fi_last_error", "fi_status_string"]
 
 
@@ -111,6 +112,22 @@ class fi_layer_norm_t(ctypes.Structure):
     _fields_ = _fields(ctypes.c_void_p, "x dy out weight bias rows tokens_dev dweight dbias workspace") \
         + _fields(ctypes.c_int64, "x_stride dy_stride out_stride tokens x_rows") \
         + _fields(ctypes.c_int32, "dim rms x_dtype y_dtype") + [("eps", ctypes.c_float)]
+
+
+class fi_pages_fork_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "lens free_pages free_count block_table shared src_rows dst_rows batch_count granted copies lens_out "
+                                        "free_count_out") \
+        + _fields(ctypes.c_int64, "table_ld") + _fields(ctypes.c_int32, "rows num_pages batch_max")
+
+
+class fi_pages_free_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "row_idx batch_count lens block_table free_count free_pages shared lens_out free_count_out") \
+        + _fields(ctypes.c_int64, "table_ld") + _fields(ctypes.c_int32, "rows num_pages batch_max")
+
+
+class fi_pages_compact_t(ctypes.Structure):
+    _fields_ = _fields(ctypes.c_void_p, "lens free_count free_pages block_table shared copies moves workspace") \
+        + _fields(ctypes.c_int64, "table_ld") + _fields(ctypes.c_int32, "rows num_pages max_copies")
 
 
 class FiError(RuntimeError):
@@ -198,6 +215,12 @@ def load_library(path: Optional[str] = None):
     lib.fi_layer_norm_backward.argtypes = [ctypes.c_char_p, vp]
     lib.fi_layer_norm_workspace.argtypes = [i32]
     lib.fi_layer_norm_workspace.restype = i64
+    lib.fi_pages_fork.argtypes = [vp, ctypes.c_char_p, vp]             # a packed fi_pages_fork_t
+    lib.fi_pages_free.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.fi_pages_compact.argtypes = [vp, ctypes.c_char_p, vp]
+    lib.fi_pages_compact_workspace.argtypes = [i32]
+    lib.fi_pages_compact_workspace.restype = i64
+    lib.fi_kv_copy_pages.argtypes = [vp, vp, i32, vp, vp]
     lib.fi_launch_count.argtypes = []
     lib.fi_launch_count.restype = i64
     lib.fi_last_error.argtypes = []
@@ -625,9 +648,10 @@ def _packer(kind) -> struct.Struct:
     return p
 
 
-_pack_extend, _pack_norm, _pack_append, _pack_attend, _pack_linear, _pack_linear_backward, _pack_layer_norm = (
+_pack_extend, _pack_norm, _pack_append, _pack_attend, _pack_linear, _pack_linear_backward, _pack_layer_norm, _pack_fork, _pack_free, \
+    _pack_compact = (
     _packer(k).pack for k in (fi_pages_extend_t, fi_head_norm_rope_t, fi_kv_append_t, fi_kv_attend_t, fi_linear_t, fi_linear_backward_t,
-                               fi_layer_norm_t))
+                               fi_layer_norm_t, fi_pages_fork_t, fi_pages_free_t, fi_pages_compact_t))
 
 
 def _at(t: Optional[torch.Tensor]) -> int:
@@ -754,6 +778,83 @@ class KvTables:
         if st:
             _check(st)
         return lens_out, count_out
+
+
+    # -- fi_pages_fork
+    def fork(self, src_rows: torch.Tensor, dst_rows: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+             block_table: torch.Tensor, shared: torch.Tensor, *, batch_count: Optional[torch.Tensor] = None,
+             out: Optional["ForkOut"] = None) -> "ForkOut":
+        """Rows dst_rows, which are empty, begin as rows src_rows do: full pages are shared (counted in `shared`, int32 [pages], zeros at
+        first), the tails' pages are to be copied: KvCache.copy_pages(out.copies).  block_table and shared are written in place."""
+        rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
+        batch, pages = src_rows.numel(), free_pages.numel()
+        _check_flat(src_rows, "src_rows", index)
+        _check_flat(dst_rows, "dst_rows", index, batch)
+        _check_flat(shared, "shared", index, pages)
+        _check_flat(batch_count, "batch_count", index, 1)
+        if out is None:
+            out = ForkOut(batch, rows, self.device)
+        else:
+            _check_flat(out.granted, "out.granted", index, batch)
+            _check_flat(out.copies, "out.copies", index, 3 * batch)
+            _check_flat(out.lens, "out.lens", index, rows)
+            _check_flat(out.free_count, "out.free_count", index, 1)
+        args = _pack_fork(lens.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), block_table.data_ptr(), shared.data_ptr(), src_rows.data_ptr(),
+                          dst_rows.data_ptr(), _at(batch_count), out.granted.data_ptr(), out.copies.data_ptr(), out.lens.data_ptr(),
+                          out.free_count.data_ptr(), block_table.stride(0), rows, pages, batch)
+        st = self._lib.fi_pages_fork(self._h, args, _raw_stream(index))
+        if st:
+            _check(st)
+        return out
+
+    # -- fi_pages_free
+    def free(self, row_idx: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor,
+             shared: torch.Tensor, *, batch_count: Optional[torch.Tensor] = None, out: Optional[Sequence[torch.Tensor]] = None):
+        """As release, where rows may share pages: those without another owner become free, in order of their numbers (free_pages and shared
+        are written in place); returns (lens, free_count) after it.  `out` may be (lens, free_count) themselves."""
+        rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
+        _check_flat(row_idx, "row_idx", index)
+        _check_flat(shared, "shared", index, free_pages.numel())
+        _check_flat(batch_count, "batch_count", index, 1)
+        if out is None:
+            out = torch.empty(rows + 1, dtype=torch.int32, device=self.device).split_with_sizes([rows, 1])
+        lens_out, count_out = out
+        _check_flat(lens_out, "out[0]", index, rows)
+        _check_flat(count_out, "out[1]", index, 1)
+        args = _pack_free(row_idx.data_ptr(), _at(batch_count), lens.data_ptr(), block_table.data_ptr(), free_count.data_ptr(), free_pages.data_ptr(),
+                          shared.data_ptr(), lens_out.data_ptr(), count_out.data_ptr(), block_table.stride(0), rows, free_pages.numel(), row_idx.numel())
+        st = self._lib.fi_pages_free(self._h, args, _raw_stream(index))
+        if st:
+            _check(st)
+        return lens_out, count_out
+
+    # -- fi_pages_compact
+    def compact(self, lens: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor, shared: torch.Tensor):
+        """Gives the pages in use the lowest numbers (block_table, free_pages and shared are rewritten in place) and returns (copies, moves) for
+        KvCache.copy_pages(copies, count=moves), which has to follow before the pools are read."""
+        rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
+        pages = free_pages.numel()
+        _check_flat(shared, "shared", index, pages)
+        most = pages // 2
+        words = torch.empty(3 * most + 1, dtype=torch.int32, device=self.device)
+        copies, moves = words[:3 * most].view(most, 3), words[3 * most:]
+        work = torch.empty(self._lib.fi_pages_compact_workspace(pages), dtype=torch.uint8, device=self.device)
+        args = _pack_compact(lens.data_ptr(), free_count.data_ptr(), free_pages.data_ptr(), block_table.data_ptr(), shared.data_ptr(), copies.data_ptr(),
+                             moves.data_ptr(), work.data_ptr(), block_table.stride(0), rows, pages, most)
+        st = self._lib.fi_pages_compact(self._h, args, _raw_stream(index))
+        if st:
+            _check(st)
+        return copies, moves
+
+
+class ForkOut:
+    """What KvTables.fork gives (torch owns the memory): granted [batch], copies [batch, 3] (page to copy, page to fill, tokens), lens [rows]
+    and free_count [1], int32."""
+
+    def __init__(self, batch: int, rows: int, device):
+        words = torch.empty(4 * batch + rows + 1, dtype=torch.int32, device=device)
+        self.granted, copies, self.lens, self.free_count = words.split_with_sizes([batch, 3 * batch, rows, 1])
+        self.copies = copies.view(batch, 3)
 
 
 def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count, q_res, k_res, dq_out=None,
@@ -1193,6 +1294,17 @@ class KvCache:
         if st:
             _check(st)
         return (ks, vs) if with_stored else None
+
+    # -- fi_kv_copy_pages
+    def copy_pages(self, copies: torch.Tensor, *, count: Optional[torch.Tensor] = None) -> None:
+        """Copies what pages hold, keys and values: copies [n, 3] (page to copy, page to fill, tokens) of KvTables.fork or compact."""
+        if copies.dim() != 2 or copies.size(1) != 3:
+            raise ValueError("copies must be int32 [n, 3]")
+        _check_flat(copies, "copies", self._index)
+        _check_flat(count, "count", self._index, 1)
+        st = self._lib.fi_kv_copy_pages(self._h, copies.data_ptr(), copies.size(0), _at(count), _raw_stream(self._index))
+        if st:
+            _check(st)
 
     # -- fi_kv_attend
     def attend(self, q: torch.Tensor, lens: torch.Tensor, block_table: torch.Tensor, *, cu_tokens: Optional[torch.Tensor] = None,

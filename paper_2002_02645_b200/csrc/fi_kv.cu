@@ -5,106 +5,10 @@
 
 #include <cuda_bf16.h>
 
-#include "fi_internal.cuh"
-
-struct fi_pages {
-    fi_pages_config_t cfg;
-    int sm_count;
-    uint32_t *ticket;   // [1] CTAs of the running call that are done; the last one puts it back to 0
-};
+#include "fi_pages.cuh"
 
 namespace fi {
 namespace {
-
-constexpr int kPageThreads = 1024;
-constexpr int kPageMaxBatch = 8192;
-constexpr int kRefused = -2147483647 - 1;
-constexpr int kPageItems = kPageMaxBatch / kPageThreads;   // requests per thread, at most
-
-// Exclusive sum over the block of one value per thread; *total receives the sum.  64 bits: lengths come from the device
-// unchecked, and their sum must not wrap.
-__device__ long long block_exclusive(long long v, long long *total) {
-    __shared__ long long warp_sum[kPageThreads / 32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    long long inc = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, inc, d);
-        if (lane >= d) inc += o;
-    }
-    if (lane == 31) warp_sum[warp] = inc;
-    __syncthreads();
-    // every warp adds up the warps' sums for itself: one barrier less than handing them back
-    long long w = lane < warps ? warp_sum[lane] : 0;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, w, d);
-        if (lane >= d) w += o;
-    }
-    const long long before = warp ? __shfl_sync(0xffffffffu, w, warp - 1) : 0;
-    *total = __shfl_sync(0xffffffffu, w, 31);
-    __syncthreads();   // the next call writes warp_sum again
-    return before + inc - v;
-}
-
-__device__ __forceinline__ int clamp_int(long long v) { return v > 2147483647ll ? 2147483647 : (int)v; }
-
-// last i in [0, n) with first[i] <= x, for non-decreasing first[] with first[0] <= x
-__device__ __forceinline__ int find_last(const int *first, int n, int x) {
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (first[mid] <= x) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
-// True in the last CTA of the grid to get here; everything the grid read before is then free to be overwritten.
-__device__ bool last_cta(uint32_t *ticket) {
-    if (gridDim.x == 1) {
-        __syncthreads();
-        return true;
-    }
-    __shared__ bool last;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        last = atomicAdd(ticket, 1u) == gridDim.x - 1;
-        if (last) *ticket = 0;
-        __threadfence();
-    }
-    __syncthreads();
-    return last;
-}
-
-// lens_out = lens, unless they are one array: each CTA copies its share before the last one enters the new lengths.  The loads
-// are issued at the start of the kernel and stored (put) when their values are there anyway.
-struct LensCopy {
-    int v[4];
-    int first, threads, rows;
-
-    __device__ __forceinline__ void get(const int32_t *lens, const int32_t *lens_out, int rows_) {
-        threads = gridDim.x * blockDim.x;
-        first = blockIdx.x * blockDim.x + threadIdx.x;
-        rows = lens_out == lens ? 0 : rows_;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (first + e * (long long)threads < rows) v[e] = lens[first + e * threads];
-    }
-
-    __device__ __forceinline__ void put(const int32_t *lens, int32_t *lens_out) const {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (first + e * (long long)threads < rows) lens_out[first + e * threads] = v[e];
-        for (long long r = first + 4ll * threads; r < rows; r += threads) lens_out[r] = lens[r];
-    }
-};
-
-__device__ __forceinline__ int actual_count(const int32_t *count_dev, int most) {
-    if (!count_dev) return most;
-    const int c = *count_dev;
-    return c < 0 ? 0 : c > most ? most : c;
-}
 
 // The step of the tables.  Every CTA forms both sums (tokens, then wanted pages) over all requests for itself: up to
 // 8,192 lengths from L2 cost less than a second launch, and one CTA is all that a decode step needs.  The tokens are
@@ -580,6 +484,7 @@ fi_status_t fi_pages_destroy(fi_pages_t *p) {
     DeviceGuard guard(p->cfg.device);
     cudaDeviceSynchronize();
     cudaFree(p->ticket);
+    cudaFree(p->segments);
     delete p;
     return FI_OK;
 }
@@ -609,6 +514,9 @@ fi_status_t fi_pages_create(const fi_pages_config_t *cfg, fi_pages_t **out) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_release_kernel<kPageItems>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 8);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&p->ticket), sizeof(uint32_t));
     if (e == cudaSuccess) e = cudaMemset(p->ticket, 0, sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void **>(&p->segments), kPageSegments * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMemset(p->segments, 0, kPageSegments * sizeof(int32_t));
+    if (e == cudaSuccess) e = prepare_pages_share();
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
         const fi_status_t st = cuda_fail(e, "fi_pages_create");
@@ -770,7 +678,7 @@ fi_status_t fi_kv_poll_status(fi_kv_t *kv) {
     }
     if (word) {
         set_error("fi_kv_poll_status:%s%s", word & 1 ? " a slot past the pool was skipped by fi_kv_append;" : "",
-                  word & 2 ? " a page number outside the pool was met by fi_kv_attend" : "");
+                  word & 2 ? " a page number outside the pool was met by fi_kv_attend or fi_kv_copy_pages" : "");
         return FI_ERR_INVALID_ARG;
     }
     return FI_OK;

@@ -1,0 +1,498 @@
+// Pages that requests share: forking a request, giving pages back by their owners, bringing used pages together, and copying what
+// pages hold.
+//
+// Only full pages are shared, and only by requests with the same beginning: a page that is still written to has one owner, so neither
+// the page tables' step nor the store has to look at owners.  shared[page] counts the owners beyond the first.
+#include "fi_pages.cuh"
+
+namespace fi {
+namespace {
+
+// last i in [0, n) with first[i] <= x, for non-decreasing first[] with first[0] <= x
+__device__ __forceinline__ int find_last64(const long long *first, int n, long long x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Every CTA forms the sums over all requests for itself (wanted tails, then full pages), the entries of the full pages are dealt out to
+// the grid, and the first CTA gives the tails their pages.  Lengths and the free count are committed by the last CTA to finish, so
+// they may be updated in place; counts of owners are added up by atomics on whole numbers.
+__global__ void __launch_bounds__(kPageThreads) pages_fork_kernel(const fi_pages_fork_t a, int page_shift, int max_blocks, uint32_t *ticket) {
+    extern __shared__ long long s_cu[];                       // first full page of each request, all laid end to end
+    int *const s_src = reinterpret_cast<int *>(s_cu + a.batch_max), *const s_dst = s_src + a.batch_max;
+    __shared__ int s_taken;
+    if (threadIdx.x == 0) s_taken = 0;
+    LensCopy copy;
+    copy.get(a.lens, a.lens_out, a.rows);
+    const int n = actual_count(a.batch_count, a.batch_max);
+    const int free_count = min(max(*a.free_count, 0), a.num_pages);
+    const int items = (a.batch_max + blockDim.x - 1) / blockDim.x, i0 = threadIdx.x * items;
+    const int place = (1 << page_shift) - 1;
+    int length[kPageItems], flags[kPageItems];                // flags: 1 possible, 2 needs a page for its tail, 4 granted
+    long long need = 0;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        flags[e] = length[e] = 0;
+        if (e < items && i < n) {
+            const int src = a.src_rows[i], dst = a.dst_rows[i];
+            if (src >= 0 && src < a.rows && dst >= 0 && dst < a.rows && src != dst && a.lens[dst] == 0) {
+                length[e] = a.lens[src];
+                if (length[e] >= 0 && ((long long)length[e] + place) >> page_shift <= max_blocks) flags[e] = length[e] & place ? 3 : 1;
+            }
+            s_src[i] = src;
+            s_dst[i] = dst;
+            need += flags[e] >> 1;
+        }
+    }
+    long long wanted;
+    long long before = block_exclusive(need, &wanted);
+    long long full = 0;
+    int taken = 0;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        if (e >= items || i >= a.batch_max) continue;
+        int page = -1, tail = -1;
+        if (i < n) {
+            if ((flags[e] & 1) && (!(flags[e] & 2) || before < free_count)) {
+                flags[e] |= 4;
+                full += length[e] >> page_shift;
+            }
+            if (flags[e] & 2) {
+                if (flags[e] & 4) {
+                    page = a.free_pages[free_count - 1 - (int)before];
+                    ++taken;
+                }
+                ++before;
+            }
+        }
+        if (blockIdx.x == 0) {
+            if (page >= 0) {
+                tail = a.block_table[(long long)s_src[i] * a.table_ld + (length[e] >> page_shift)];
+                a.block_table[(long long)s_dst[i] * a.table_ld + (length[e] >> page_shift)] = page;
+            }
+            a.granted[i] = flags[e] & 4 ? 1 : 0;
+            a.copies[3 * (long long)i] = tail;
+            a.copies[3 * (long long)i + 1] = page;
+            a.copies[3 * (long long)i + 2] = page >= 0 ? length[e] & place : 0;
+        }
+    }
+    long long pages;
+    long long cu = block_exclusive(full, &pages);
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        if (e < items && i < n) {
+            s_cu[i] = cu;
+            if (flags[e] & 4) cu += length[e] >> page_shift;
+        }
+    }
+    if (taken > 0) atomicAdd(&s_taken, taken);
+    copy.put(a.lens, a.lens_out);
+    __syncthreads();
+    for (long long p = (long long)blockIdx.x * blockDim.x + threadIdx.x; p < pages; p += (long long)gridDim.x * blockDim.x) {
+        const int i = find_last64(s_cu, n, p);                // (requests without full pages share their first with the next one)
+        const long long j = p - s_cu[i];
+        const int page = a.block_table[(long long)s_src[i] * a.table_ld + j];
+        a.block_table[(long long)s_dst[i] * a.table_ld + j] = page;
+        if (page >= 0 && page < a.num_pages) atomicAdd(a.shared + page, 1);
+    }
+    if (!last_cta(ticket)) return;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e)
+        if (e < items && i0 + e < n && (flags[e] & 4)) a.lens_out[s_dst[i0 + e]] = length[e];
+    if (threadIdx.x == 0) *a.free_count_out = free_count - s_taken;
+}
+
+// Every listed page loses an owner; one that had no other goes below 0 and is counted in its segment of 1,024 pages.  The last CTA then
+// takes the segments in order (a warp each), which puts the free pages in order of their numbers whatever the order of the atomics.
+__global__ void __launch_bounds__(kPageThreads) pages_free_kernel(const fi_pages_free_t a, int page_shift, int max_blocks, uint32_t *ticket,
+                                                                  int32_t *segments) {
+    extern __shared__ long long s_cu[];
+    int *const s_row = reinterpret_cast<int *>(s_cu + a.batch_max);
+    __shared__ int s_base[kPageSegments];
+    LensCopy copy;
+    copy.get(a.lens, a.lens_out, a.rows);
+    const int n = actual_count(a.batch_count, a.batch_max);
+    const int free_count = min(max(*a.free_count, 0), a.num_pages);
+    const int items = (a.batch_max + blockDim.x - 1) / blockDim.x, i0 = threadIdx.x * items;
+    int used[kPageItems];
+    long long sum = 0;
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e) {
+        const int i = i0 + e;
+        used[e] = 0;
+        if (e < items && i < n) {
+            const int row = a.row_idx[i];
+            const bool ok = row >= 0 && row < a.rows;
+            if (ok) used[e] = (int)min(((long long)max(a.lens[row], 0) + (1ll << page_shift) - 1) >> page_shift, (long long)max_blocks);
+            s_row[i] = ok ? row : -1;
+            sum += used[e];
+        }
+    }
+    long long pages;
+    long long cu = block_exclusive(sum, &pages);
+#pragma unroll
+    for (int e = 0; e < kPageItems; ++e)
+        if (e < items && i0 + e < n) {
+            s_cu[i0 + e] = cu;
+            cu += used[e];
+        }
+    copy.put(a.lens, a.lens_out);
+    __syncthreads();
+    for (long long p = (long long)blockIdx.x * blockDim.x + threadIdx.x; p < pages; p += (long long)gridDim.x * blockDim.x) {
+        const int i = find_last64(s_cu, n, p);
+        const int page = a.block_table[(long long)s_row[i] * a.table_ld + (p - s_cu[i])];
+        if (page >= 0 && page < a.num_pages && atomicSub(a.shared + page, 1) == 0) atomicAdd(segments + (page >> 10), 1);
+    }
+    if (!last_cta(ticket)) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int count = (a.num_pages + 1023) >> 10;
+    // each thread four neighbouring segments (kPageSegments / kPageThreads), whatever the number of threads
+    long long total = 0;
+    for (int s0 = 0; s0 < count; s0 += 4 * blockDim.x) {
+        int here[4];
+        long long mine = 0, all;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int s = s0 + 4 * threadIdx.x + e;
+            here[e] = s < count ? __ldcg(segments + s) : 0;
+            mine += here[e];
+        }
+        long long at = total + block_exclusive(mine, &all);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int s = s0 + 4 * threadIdx.x + e;
+            if (s < count) {
+                s_base[s] = here[e] ? (int)at : -1;
+                if (here[e]) segments[s] = 0;
+                at += here[e];
+            }
+        }
+        total += all;
+    }
+    __syncthreads();
+    for (int s = warp; s < count; s += warps) {
+        long long at = s_base[s];
+        if (at < 0) continue;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            int v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int page = s * 1024 + c * 256 + e * 32 + lane;
+                v[e] = page < a.num_pages ? __ldcg(a.shared + page) : 0;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int page = s * 1024 + c * 256 + e * 32 + lane;
+                const unsigned gone = __ballot_sync(0xffffffffu, v[e] < 0);
+                if (v[e] < 0) {
+                    const long long to = free_count + at + __popc(gone & ((1u << lane) - 1));
+                    if (to < a.num_pages) a.free_pages[to] = page;       // (more pages than there are: a stack that was not one)
+                    a.shared[page] = 0;
+                }
+                at += __popc(gone);
+            }
+        }
+    }
+    for (int i = threadIdx.x; i < n; i += blockDim.x)
+        if (s_row[i] >= 0) a.lens_out[s_row[i]] = 0;
+    if (threadIdx.x == 0) *a.free_count_out = (int)min(free_count + total, (long long)a.num_pages);
+}
+
+// Workspace of a compaction, in words: [0] used pages, then a bit for each free page, the places to fill, the pages to move, and the new
+// name of each page that moves.
+struct CompactSpace {
+    int32_t *used;
+    uint32_t *is_free;
+    int32_t *holes, *high, *name;
+    int words;
+};
+__host__ __device__ inline CompactSpace compact_space(void *workspace, int num_pages) {
+    CompactSpace c;
+    const int words = (num_pages + 31) / 32, half = num_pages / 2 + 1;
+    int32_t *const w = static_cast<int32_t *>(workspace);
+    c.used = w;
+    c.is_free = reinterpret_cast<uint32_t *>(w + 32);
+    c.holes = w + 32 + words;
+    c.high = c.holes + half;
+    c.name = c.high + half;
+    c.words = words;
+    return c;
+}
+
+constexpr int kCompactCtas = 8;        // one cluster: its barrier stands between the steps
+
+__device__ __forceinline__ void cluster_barrier() {
+    __threadfence();
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Used pages at or above the number of used pages, in order, get the free places below it, in order.  One cluster takes all steps: bits
+// of the free pages, their number, ranks, moves; then the free stack is rewritten, lowest number on top.
+__global__ void __cluster_dims__(kCompactCtas, 1, 1) __launch_bounds__(kPageThreads) pages_compact_kernel(const fi_pages_compact_t a, int page_size) {
+    const CompactSpace c = compact_space(a.workspace, a.num_pages);
+    const int threads = kCompactCtas * kPageThreads, tid = blockIdx.x * kPageThreads + threadIdx.x;
+    __shared__ long long s_counts;
+    const int free_count = min(max(*a.free_count, 0), a.num_pages);
+    for (int w = tid; w < c.words; w += threads) c.is_free[w] = 0;
+    cluster_barrier();
+    for (int i = tid; i < free_count; i += threads) {
+        const int page = a.free_pages[i];
+        if (page >= 0 && page < a.num_pages) atomicOr(c.is_free + (page >> 5), 1u << (page & 31));
+    }
+    cluster_barrier();
+    // each CTA a run of words, each thread a run of those
+    const int run = (c.words + threads - 1) / threads, first = min(tid * run, c.words), last = min(first + run, c.words);
+    const auto bits = [&](int w) { return __ldcg(c.is_free + w); };
+    const auto valid = [&](int w) { return w * 32 + 32 <= a.num_pages ? 0xffffffffu : (1u << (a.num_pages & 31)) - 1; };
+    long long mine = 0, all;
+    for (int w = first; w < last; ++w) mine += __popc(bits(w));
+    block_exclusive(mine, &all);
+    const auto from_all = [&](long long v) {                  // sum over the CTAs before this one in the low, over all in the high half
+        if (threadIdx.x == 0) s_counts = v;
+        cluster_barrier();
+        long long before = 0, total = 0;
+        uint32_t at = (uint32_t)__cvta_generic_to_shared(&s_counts);
+        for (int r = 0; r < kCompactCtas; ++r) {
+            uint32_t there;
+            long long x;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(r));
+            asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(x) : "r"(there) : "memory");
+            if (r < (int)blockIdx.x) before += x;
+            total += x;
+        }
+        cluster_barrier();                                     // (nobody writes or leaves before all have read)
+        return longlong2{before, total};
+    };
+    const int used = a.num_pages - (int)from_all(all).y;
+    // bits of word w that are places to fill, and pages to move
+    const auto low = [&](int w) { return w * 32 + 32 <= used ? 0xffffffffu : w * 32 >= used ? 0u : (1u << (used & 31)) - 1; };
+    mine = 0;
+    for (int w = first; w < last; ++w) {
+        const uint32_t f = bits(w);
+        mine += (long long)__popc(f & low(w)) | (long long)__popc(~f & ~low(w) & valid(w)) << 32;
+    }
+    const long long in_cta = block_exclusive(mine, &all);
+    const longlong2 sums = from_all(all);
+    long long at = sums.x + in_cta;
+    int hole = (int)(at & 0xffffffffll), high = (int)(at >> 32);
+    const int moves = min((int)(sums.y & 0xffffffffll), (int)(sums.y >> 32));
+    for (int w = first; w < last; ++w) {
+        const uint32_t f = bits(w);
+        for (uint32_t m = f & low(w); m; m &= m - 1) {
+            if (hole <= a.num_pages / 2) c.holes[hole] = w * 32 + __ffs(m) - 1;
+            ++hole;
+        }
+        for (uint32_t m = ~f & ~low(w) & valid(w); m; m &= m - 1) {
+            if (high <= a.num_pages / 2) c.high[high] = w * 32 + __ffs(m) - 1;
+            ++high;
+        }
+    }
+    if (tid == 0) {
+        *c.used = used;
+        *a.moves = moves;
+    }
+    cluster_barrier();
+    for (int k = tid; k < a.max_copies; k += threads) {
+        int src = -1, dst = -1;
+        if (k < moves) {
+            src = __ldcg(c.high + k);
+            dst = __ldcg(c.holes + k);
+            c.name[src] = dst;
+            a.shared[dst] = a.shared[src];
+            a.shared[src] = 0;
+        }
+        a.copies[3ll * k] = src;
+        a.copies[3ll * k + 1] = dst;
+        a.copies[3ll * k + 2] = k < moves ? page_size : 0;
+    }
+    for (int i = tid; i < free_count; i += threads) a.free_pages[i] = a.num_pages - 1 - i;
+}
+
+// The new names of the pages that moved, in the rows' entries.
+__global__ void __launch_bounds__(256) pages_rename_kernel(const fi_pages_compact_t a, int page_shift, int max_blocks) {
+    const CompactSpace c = compact_space(a.workspace, a.num_pages);
+    const int used = *c.used;
+    for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int blocks = (int)min(((long long)max(a.lens[row], 0) + (1ll << page_shift) - 1) >> page_shift, (long long)max_blocks);
+        int32_t *const entries = a.block_table + (long long)row * a.table_ld;
+        for (int j = threadIdx.x; j < blocks; j += 256) {
+            const int page = entries[j];
+            if (page >= used && page < a.num_pages && !(c.is_free[page >> 5] >> (page & 31) & 1)) entries[j] = c.name[page];
+        }
+    }
+}
+
+struct CopyPools {
+    unsigned char *codes[2];
+    uint32_t *meta[2];
+    long long ps, hs, ts, mps, mhs, mts;
+    int heads, page_size, num_pages, pieces;   // pieces of 16 bytes of a vector's codes
+    int32_t *status;
+};
+
+// A warp per page, head and kind (keys, values): its codes in pieces of 16 bytes, four on the way per lane, and its pairs.
+__global__ void __launch_bounds__(256) kv_copy_pages_kernel(const CopyPools p, const int32_t *copies, const int32_t *count_dev, int most) {
+    const int n = actual_count(count_dev, most), lane = threadIdx.x & 31;
+    const long long units = (long long)n * p.heads * 2, step = (long long)gridDim.x * 8;
+    for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += step) {
+        const long long i = u / (p.heads * 2);
+        const int rest = (int)(u - i * (p.heads * 2)), head = rest >> 1, kind = rest & 1;
+        const int src = copies[3 * i], dst = copies[3 * i + 1], tokens = min(copies[3 * i + 2], p.page_size);
+        if (src < 0 || tokens <= 0) continue;
+        if (src >= p.num_pages || dst < 0 || dst >= p.num_pages) {
+            if (lane == 0) atomicOr(p.status, 2);
+            continue;
+        }
+        const unsigned char *const from = p.codes[kind] + src * p.ps + head * p.hs;
+        unsigned char *const to = p.codes[kind] + dst * p.ps + head * p.hs;
+        const int pieces = tokens * p.pieces;
+        for (int q0 = lane; q0 < pieces; q0 += 128) {
+            uint4 v[4];
+            long long at[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int q = q0 + 32 * e, token = q / p.pieces;
+                at[e] = token * p.ts + (q - token * p.pieces) * 16ll;
+                if (q < pieces) v[e] = *reinterpret_cast<const uint4 *>(from + at[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (q0 + 32 * e < pieces) *reinterpret_cast<uint4 *>(to + at[e]) = v[e];
+        }
+        const uint32_t *const mf = p.meta[kind] + src * p.mps + head * p.mhs;
+        uint32_t *const mt = p.meta[kind] + dst * p.mps + head * p.mhs;
+        for (int t = lane; t < tokens; t += 32) mt[t * p.mts] = mf[t * p.mts];
+    }
+}
+
+int shift_of(int page_size) {
+    int s = 0;
+    while (1 << s < page_size) ++s;
+    return s;
+}
+
+}  // namespace
+
+cudaError_t prepare_pages_share() {
+    cudaError_t e = cudaFuncSetAttribute(pages_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 16);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_free_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 12);
+    return e;
+}
+
+}  // namespace fi
+
+using namespace fi;
+
+extern "C" {
+
+fi_status_t fi_pages_fork(fi_pages_t *p, const fi_pages_fork_t *a, void *cuda_stream) {
+    if (!p || !a) {
+        set_error("fi_pages_fork: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->batch_max < 0 || a->batch_max > p->cfg.max_batch || a->rows < 0 || a->num_pages < 0 || a->table_ld < p->cfg.max_blocks) {
+        set_error("fi_pages_fork: batch %d outside 0..%d, a negative size, or table_ld below max_blocks", a->batch_max, p->cfg.max_batch);
+        return FI_ERR_INVALID_ARG;
+    }
+    if ((a->rows > 0 && (!a->lens || !a->lens_out || !a->block_table)) || (a->num_pages > 0 && (!a->free_pages || !a->shared)) || !a->free_count ||
+        !a->free_count_out || (a->batch_max > 0 && (!a->src_rows || !a->dst_rows || !a->granted || !a->copies))) {
+        set_error("fi_pages_fork: null pointer (only batch_count may be)");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(p->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_fork");
+    long long grid = (long long)a->batch_max * p->cfg.max_blocks / 4096;       // an upper bound of the pages
+    grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
+    const int threads = a->batch_max <= 256 && a->rows <= 1024 && grid == 1 ? 256 : kPageThreads;
+    pages_fork_kernel<<<(int)grid, threads, (size_t)a->batch_max * 16, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(p->cfg.page_size),
+                                                                                                                p->cfg.max_blocks, p->ticket);
+    count_launch();
+    return check_launch("fi_pages_fork");
+}
+
+fi_status_t fi_pages_free(fi_pages_t *p, const fi_pages_free_t *a, void *cuda_stream) {
+    if (!p || !a) {
+        set_error("fi_pages_free: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->batch_max < 0 || a->batch_max > p->cfg.max_batch || a->rows < 0 || a->num_pages < 0 || a->num_pages > kPageSegments * 1024 ||
+        a->table_ld < p->cfg.max_blocks) {
+        set_error("fi_pages_free: batch %d outside 0..%d, a negative size, more than %d pages, or table_ld below max_blocks", a->batch_max,
+                  p->cfg.max_batch, kPageSegments * 1024);
+        return FI_ERR_INVALID_ARG;
+    }
+    if ((a->rows > 0 && (!a->lens || !a->lens_out || !a->block_table)) || (a->num_pages > 0 && (!a->free_pages || !a->shared)) || !a->free_count ||
+        !a->free_count_out || (a->batch_max > 0 && !a->row_idx)) {
+        set_error("fi_pages_free: null pointer (only batch_count may be)");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(p->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_free");
+    long long grid = (long long)a->batch_max * p->cfg.max_blocks / 4096;
+    grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
+    pages_free_kernel<<<(int)grid, kPageThreads, (size_t)a->batch_max * 12, static_cast<cudaStream_t>(cuda_stream)>>>(
+        *a, shift_of(p->cfg.page_size), p->cfg.max_blocks, p->ticket, p->segments);
+    count_launch();
+    return check_launch("fi_pages_free");
+}
+
+int64_t fi_pages_compact_workspace(int32_t num_pages) {
+    if (num_pages < 0) return 0;
+    return 4 * (32 + ((int64_t)num_pages + 31) / 32 + 2 * ((int64_t)num_pages / 2 + 1) + num_pages);
+}
+
+fi_status_t fi_pages_compact(fi_pages_t *p, const fi_pages_compact_t *a, void *cuda_stream) {
+    if (!p || !a) {
+        set_error("fi_pages_compact: null argument");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (a->rows < 0 || a->num_pages < 0 || a->max_copies < a->num_pages / 2 || a->table_ld < p->cfg.max_blocks) {
+        set_error("fi_pages_compact: a negative size, room for fewer copies than half the pages, or table_ld below max_blocks");
+        return FI_ERR_INVALID_ARG;
+    }
+    if ((a->rows > 0 && (!a->lens || !a->block_table)) || (a->num_pages > 0 && (!a->free_pages || !a->shared)) || !a->free_count || !a->moves ||
+        !a->workspace || (a->max_copies > 0 && !a->copies) || (reinterpret_cast<uintptr_t>(a->workspace) & 3)) {
+        set_error("fi_pages_compact: null pointer, or a workspace that is not on a 4-byte boundary");
+        return FI_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(p->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_compact");
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    pages_compact_kernel<<<kCompactCtas, kPageThreads, 0, stream>>>(*a, p->cfg.page_size);
+    count_launch();
+    if (a->rows > 0) {
+        const int grid = a->rows < 8 * p->sm_count ? a->rows : 8 * p->sm_count;
+        pages_rename_kernel<<<grid, 256, 0, stream>>>(*a, shift_of(p->cfg.page_size), p->cfg.max_blocks);
+        count_launch();
+    }
+    return check_launch("fi_pages_compact");
+}
+
+fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_copies, const int32_t *count, void *cuda_stream) {
+    if (!kv || max_copies < 0 || (max_copies > 0 && !copies)) {
+        set_error("fi_kv_copy_pages: null argument or a negative size");
+        return FI_ERR_INVALID_ARG;
+    }
+    if (max_copies == 0) return FI_OK;
+    DeviceGuard guard(kv->cfg.device);
+    if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_kv_copy_pages");
+    const fi_kv_config_t &c = kv->cfg;
+    const CopyPools p = {{static_cast<unsigned char *>(c.k_codes), static_cast<unsigned char *>(c.v_codes)},
+                         {static_cast<uint32_t *>(c.k_meta), static_cast<uint32_t *>(c.v_meta)},
+                         c.page_stride, c.head_stride, c.token_stride, c.meta_page_stride, c.meta_head_stride, c.meta_token_stride,
+                         c.kv_heads, c.page_size, c.num_pages, c.head_dim / 32, kv->status_dev};
+    const long long units = ((long long)max_copies * c.kv_heads * 2 + 7) / 8, most = 8ll * kv->sm_count;
+    kv_copy_pages_kernel<<<(unsigned)(units < most ? units : most), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, copies, count, max_copies);
+    count_launch();
+    return check_launch("fi_kv_copy_pages");
+}
+
+}  // extern "C"
