@@ -10,6 +10,7 @@
 #include <cuda_bf16.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "fi_internal.cuh"
 
@@ -33,6 +34,14 @@ __device__ int32_t g_linear_status;       // 1: a bounded wait ran out
 struct LinearCtl {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t done, never;
+    uint32_t tmem;
+    volatile int gave_up;
+};
+
+struct PairCtl {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t sums_full[2], sums_empty[2];
+    uint64_t never;
     uint32_t tmem;
     volatile int gave_up;
 };
@@ -174,13 +183,26 @@ constexpr float kGeluTanh = 0.044715f, kGeluTwice = 1.5957691216057308f;   // 2 
 
 __device__ __forceinline__ float logistic(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
-__device__ __forceinline__ float activate(float z, int act) {
+template <int N>
+__device__ __forceinline__ void activate(float (&z)[N], int act) {
     switch (act) {
-        case FI_ACT_RELU: return z < 0.f ? 0.f : z;                      // (NaN stays)
-        case FI_ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);     // (not 1 + erf, which loses the small values of z < 0)
-        case FI_ACT_GELU_TANH: return z * logistic(kGeluTwice * fmaf(kGeluTanh * z, z * z, z));
-        case FI_ACT_SILU: return z * logistic(z);
-        default: return z;
+        case FI_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = z[i] < 0.f ? 0.f : z[i];      // (NaN stays)
+            break;
+        case FI_ACT_GELU:                                                    // (not 1 + erf, which loses the small values of z < 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * erfcf(z[i] * -0.70710678f);
+            break;
+        case FI_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] *= logistic(kGeluTwice * fmaf(kGeluTanh * z[i], z[i] * z[i], z[i]));
+            break;
+        case FI_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) z[i] *= logistic(z[i]);
+            break;
+        default: break;
     }
 }
 
@@ -212,23 +234,52 @@ __device__ __forceinline__ int actual_rows(const LinearParams &p) {
     return c < 0 ? 0 : c > p.n ? p.n : c;
 }
 
-// What becomes of one sum: column m of row n of the product, `to` its row of out.
-template <bool F32>
-__device__ __forceinline__ void finish(const LinearParams &p, float v, float bias, int m, int n, long long to) {
-    const float z = v + bias;
-    if (p.preact) p.preact[(long long)n * p.ld_preact + m] = __float2bfloat16_rn(z);
-    float y = activate(z, p.act);
-    if (F32) {
-        if (p.residual) y += static_cast<const float *>(p.residual)[to * p.ld_res + m];
-        static_cast<float *>(p.out)[to * p.ld_out + m] = y;
-    } else {
-        if (p.residual) y += __bfloat162float(static_cast<const __nv_bfloat16 *>(p.residual)[to * p.ld_res + m]);
-        static_cast<__nv_bfloat16 *>(p.out)[to * p.ld_out + m] = __float2bfloat16_rn(y);
+constexpr int kNoRow = -1, kSkipRow = -2;   // no such row of the product; a row that is in no row of out
+
+// Row of out that row n of the product goes to, or one of these.
+__device__ __forceinline__ int row_of(const LinearParams &p, int n, int rows) {
+    if (n >= rows) return kNoRow;
+    if (!p.rows) return n;
+    const int to = p.rows[n];
+    return to >= 0 && to < p.out_rows ? to : kSkipRow;
+}
+
+// What becomes of N sums, column m and rows n0, n0 + step .. of the product; to[i]: their rows of out, negative: none.  (Every choice is
+// made once for all of them: with a choice per value the two warps of a scheduler wait for their own branches, 59 us, not 27, for 8,192
+// tokens 1,024 -> 1,024.  Loads before stores, so that they are on the way together.)
+template <bool F32, int N>
+__device__ __forceinline__ void finish(const LinearParams &p, float (&v)[N], float bias, int m, int n0, int step, const int (&to)[N]) {
+    using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+    T r[N];
+    const bool here = m < p.m;
+    if (p.residual) {
+        const T *const from = static_cast<const T *>(p.residual) + m;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (here && to[i] >= 0) r[i] = from[to[i] * p.ld_res];
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += bias;
+    if (p.preact) {
+        __nv_bfloat16 *const z = p.preact + (long long)n0 * p.ld_preact + m;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (here && to[i] != kNoRow) z[i * step * p.ld_preact] = __float2bfloat16_rn(v[i]);
+    }
+    activate(v, p.act);
+    if (p.residual) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += (float)r[i];
+    }
+    T *const out = static_cast<T *>(p.out) + m;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (here && to[i] >= 0) out[to[i] * p.ld_out] = (T)v[i];
 }
 
 // Few tiles: a CTA takes 128 output columns and up to 256 output rows, `split` CTAs of a cluster share its reduction and add up
 // their sums through distributed shared memory, in the order of their ranks.
+constexpr int kBatch = 8;              // values of a thread that go out together
 template <bool F32>
 __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                    const __grid_constant__ CUtensorMap map_b,
@@ -362,14 +413,20 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
         const int m = m0 + (tid & (kM - 1));
         const float bias = p.bias && m < p.m ? p.bias[m] : 0.f;
         const uint32_t mine = smem_at(part) + (tid & (kM - 1)) * 4;
-        for (int c = rank * 2 + (tid >> 7); c < cols && m < p.m; c += 2 * p.split) {
-            float v = 0.f;
-            if (p.split > 1)
-                for (int s = 0; s < p.split; ++s) v += cluster_load(map_to_rank(mine + c * (kM * 4), s));
-            else
-                v = part[c * kM + (tid & (kM - 1))];
-            const long long to = p.rows ? p.rows[n0 + c] : n0 + c;
-            if (to >= 0 && to < p.out_rows) finish<F32>(p, v, bias, m, n0 + c, to);
+        const int step = 2 * p.split;
+        for (int c0 = rank * 2 + (tid >> 7); c0 < cols; c0 += kBatch * step) {
+            float v[kBatch];
+            int to[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) to[i] = c0 + i * step < cols ? row_of(p, n0 + c0 + i * step, rows) : kNoRow;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) v[i] = 0.f;
+            for (int s = 0; s < p.split; ++s) {
+                const uint32_t from = p.split > 1 ? map_to_rank(mine, s) : mine;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) v[i] += cluster_load(from + min(c0 + i * step, cols - 1) * (kM * 4));
+            }
+            finish<F32>(p, v, bias, m, n0 + c0, step, to);
         }
     }
     if (p.split > 1) cluster_sync();                        // the others have read this CTA's sums
@@ -377,6 +434,262 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     if (warp == 0) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
+    }
+}
+
+// ---- pairs of CTAs: many tiles ----
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// lands in this CTA's shared memory, counts its bytes on a barrier of the first CTA
+__device__ __forceinline__ void load_box_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+}
+// D (256 x N, 128 rows in each CTA's TMEM) += A (128 rows of each CTA) x B (N / 2 rows of each)
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+        "}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// when the pair's products so far are over: the barrier at this place in both CTAs
+__device__ __forceinline__ void tc_commit_pair(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_at(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// tile t of the product: groups of 8 tiles along m are walked along n, so that the tiles that run at one time share their operands in L2
+__device__ __forceinline__ void tile_place(const LinearParams &p, int t, int n_tiles, int &m_tile, int &n_tile) {
+    constexpr int kGroup = 8;
+    const int group = t / (kGroup * n_tiles), first = group * kGroup, width = min(kGroup, p.m_tiles - first), in = t - first * n_tiles;
+    n_tile = in / width;
+    m_tile = first + in - n_tile * width;
+}
+
+// 16 sums of a thread (column m, rows n0 .. of the product) on their way out
+template <bool F32>
+__device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, float bias, int m, int n0, int rows) {
+    const int row = row_of(p, n0 + (threadIdx.x & 15), rows);
+    float v[16];
+    int to[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        v[i] = __uint_as_float(sums[i]);
+        to[i] = __shfl_sync(0xffffffffu, row, i);
+    }
+    finish<F32>(p, v, bias, m, n0, 1, to);
+}
+
+// One pair of CTAs per two SMs walks over tiles of 256 output columns (128 per CTA) and tile_n output rows; each CTA loads its half of
+// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the reduction) go out while the next is formed.
+template <bool F32>
+__global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                  const __grid_constant__ CUtensorMap map_b,
+                                                                  const __grid_constant__ LinearParams p) {
+    extern __shared__ unsigned char raw_smem[];
+    __shared__ PairCtl ctl_space;
+    PairCtl *const ctl = &ctl_space;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int rows = actual_rows(p), n_tiles = (rows + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
+    if (pair >= tiles) return;                              // (both CTAs)
+    unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
+    const int stage_bytes = kABytes + p.b_bytes, half_n = p.tile_n >> 1;
+    const int piece = F32 ? 8 : p.kb;                       // blocks of an accumulator
+    if (tid == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            bar_init(&ctl->full[s], 1);
+            bar_init(&ctl->empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&ctl->sums_full[i], 1);
+            bar_init(&ctl->sums_empty[i], 2 * kEpiThreads / 32);   // the warps of both CTAs
+        }
+        bar_init(&ctl->never, 1);
+        ctl->gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(p.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    cluster_sync();                                         // the other CTA's barriers are there before anything signals them
+    tc_after();
+    const uint32_t tmem = ctl->tmem;
+    if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
+    if (warp == 8) {
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0;
+            long long issued = 0;
+            bool ok = true;
+            for (int t = pair; t < tiles && ok; t += pairs) {
+                int mt, nt;
+                tile_place(p, t, n_tiles, mt, nt);
+                const int m0 = mt * 2 * kM + (int)rank * kM, n0 = nt * p.tile_n + (int)rank * half_n;
+                for (int kb = 0; kb < p.kb; ++kb, ++issued) {
+                    if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
+                    if (rank == 0) bar_expect(&ctl->full[stage], 2u * (uint32_t)stage_bytes);
+                    const uint32_t bar = map_to_rank(smem_at(&ctl->full[stage]), 0);
+                    if (p.a_mn) {
+                        load_box_pair(a, &map_a, bar, m0, kb * kKb);
+                        load_box_pair(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
+                    } else {
+                        load_box_pair(a, &map_a, bar, kb * kKb, m0);
+                    }
+                    if (p.b_mn)
+                        for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
+                    else
+                        load_box_pair(b, &map_b, bar, kb * kKb, n0);
+                    if (++stage == (uint32_t)p.stages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            if (!ok) {
+                // gave up: the copies that were started land first (the second CTA cannot see that, and gives them 10 ms)
+                if (rank == 0) {
+                    for (int back = (int)(issued < p.stages ? issued : p.stages); back > 0; --back) {
+                        if (stage == 0) {
+                            stage = p.stages;
+                            phase ^= 1;
+                        }
+                        bar_drain(&ctl->full[--stage], phase);
+                    }
+                } else {
+                    const long long t0 = clock64();
+                    while (clock64() - t0 < kDrainLimit / 10) {}
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = instruction(2 * kM, p.tile_n, p.a_mn, p.b_mn);
+            const uint32_t a_step = operand_step(p.a_mn), b_step = operand_step(p.b_mn);
+            uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+            bool ok = true;
+            for (int t = pair; t < tiles && ok; t += pairs) {
+                for (int kb = 0; kb < p.kb && ok;) {
+                    if (!bar_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_after();
+                    const uint32_t d = tmem + buf * p.tile_n;
+                    const int end = min(kb + piece, p.kb);
+                    for (int first = kb; kb < end; ++kb) {
+                        if (!bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_after();
+                        const uint32_t at = smem_at(smem + stage * stage_bytes);
+                        const uint64_t a = operand(at, p.a_mn), b = operand(at + kABytes, p.b_mn);
+#pragma unroll
+                        for (int i = 0; i < kKb / 16; ++i) mma_pair(d, a + i * a_step, b + i * b_step, idesc, ((kb - first) | i) != 0);
+                        tc_commit_pair(&ctl->empty[stage]);
+                        if (++stage == (uint32_t)p.stages) {
+                            stage = 0;
+                            phase ^= 1;
+                        }
+                    }
+                    if (ok) {
+                        tc_commit_pair(&ctl->sums_full[buf]);
+                        buf ^= 1;
+                        if (buf == 0) buf_phase ^= 1;
+                    }
+                }
+            }
+            if (!ok) {                                      // no product is on its way when TMEM is freed
+                tc_commit_pair(&ctl->never);
+                const long long t0 = clock64();
+                while (clock64() - t0 < kDrainLimit / 10) {}
+            }
+        }
+    } else {
+        // ---- sums on their way out: warp w reads TMEM lanes 32 (w mod 4) .., and every other 16 of the tile's rows ----
+        const int half = warp >> 2, my_m = (int)rank * kM + (warp & 3) * 32 + lane;
+        const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t buf = 0, buf_phase = 0;
+        bool ok = true;
+        for (int t = pair; t < tiles && ok; t += pairs) {
+            int mt, nt;
+            tile_place(p, t, n_tiles, mt, nt);
+            const int m = mt * 2 * kM + my_m, n0 = nt * p.tile_n, cols = min(p.tile_n, rows - n0);
+            const float bias = p.bias && m < p.m ? p.bias[m] : 0.f;
+            if constexpr (F32) {
+                uint32_t sum[kMaxN / 2];
+#pragma unroll
+                for (int i = 0; i < kMaxN / 2; ++i) sum[i] = 0;
+                for (int kb = 0; kb < p.kb && ok; kb += piece) {
+                    ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
+                    tc_after();
+                    const uint32_t at = lanes_at + buf * p.tile_n + half * 16;
+#pragma unroll
+                    for (int c = 0; c < kMaxN / 32; ++c)
+                        if (32 * c + half * 16 < cols) {
+                            uint32_t v[16];
+                            tmem_load(at + 32 * c, v);
+                            tmem_wait(v);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) sum[16 * c + i] = __float_as_uint(__uint_as_float(sum[16 * c + i]) + __uint_as_float(v[i]));
+                        }
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), 0));
+                    buf ^= 1;
+                    if (buf == 0) buf_phase ^= 1;
+                }
+#pragma unroll
+                for (int c = 0; c < kMaxN / 32; ++c)
+                    if (32 * c + half * 16 < cols) finish16<true>(p, sum + 16 * c, bias, m, n0 + 32 * c + half * 16, rows);
+            } else {
+                ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
+                tc_after();
+                const uint32_t at = lanes_at + buf * p.tile_n;
+                for (int c = half * 16; c < cols; c += 32) {
+                    uint32_t v[16];
+                    tmem_load(at + c, v);
+                    tmem_wait(v);
+                    finish16<false>(p, v, bias, m, n0 + c, rows);
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), 0));
+                buf ^= 1;
+                if (buf == 0) buf_phase ^= 1;
+            }
+        }
+    }
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    cluster_sync();                                         // neither leaves before the other's products and signals are over
+    if (warp == 0) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
     }
 }
 
@@ -453,6 +766,8 @@ fi_status_t device_facts(int *sms, const char *name) {
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
     if (e != cudaSuccess) return cuda_fail(e, name);
     g_facts[dev].sms.store(n, std::memory_order_release);
     *sms = n;
@@ -489,6 +804,39 @@ fi_status_t operand_map(CUtensorMap *map, const Matrix &x, int box_rows, const c
     return FI_OK;
 }
 
+// Which kernel, and its tiles.  Estimates in SM cycles: 16 x 256 x 256 products of a pair take 128 cycles (a CTA's 16 x 128 x 256 as
+// many), an SM gets about 56 bytes a cycle from L2, the device about 3,400 from memory.
+struct LinearPlan {
+    bool pair;
+    int tile_n, split;
+    double cycles;
+};
+
+LinearPlan plan_product(long long m, long long n, long long kb, bool b_mn, bool f32, int size, int sms) {
+    LinearPlan best = {false, 16, 1, 1e30};
+    const auto most = [](double a, double b) { return a > b ? a : b; };
+    const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
+    const double memory = ((double)m * kb * 128 + (double)n * kb * 128 + (double)m * n * size) / 3400.;
+    for (int tile = 32; tile <= kMaxN; tile += 32) {
+        if (b_mn && tile % 128) continue;
+        if (tile > 32 && tile - 32 >= n) break;
+        const double block = most(2. * tile, (128 + tile / 2) * 128 / 56.), rounds = (double)up(up(m, 2 * kM) * up(n, tile), sms / 2);
+        const double cycles = most(rounds * kb * block, memory) + 2500 + 20. * tile;
+        if (cycles < best.cycles) best = {true, tile, 1, cycles};
+    }
+    for (int tile = 16; tile <= kMaxN; tile += 16) {
+        if (tile > 16 && tile - 16 >= n) break;
+        for (int split = 1; split <= 8 && split <= kb; split *= 2) {
+            const long long blocks = up(kb, split);
+            if (f32 && up(blocks, 8) * tile > 512 && tile > 16) continue;      // pieces of 512 values have an accumulator each
+            const double block = most(2. * tile, (128 + tile) * 128 / 56.), rounds = (double)up(up(m, kM) * up(n, tile) * split, sms);
+            const double cycles = most(rounds * (blocks * block + 2500 + 20. * tile), memory + 2500 + 20. * tile) + (split > 1 ? 1000 : 0);
+            if (cycles < best.cycles) best = {false, tile, split, cycles};
+        }
+    }
+    return best;
+}
+
 // D[n][m] = sum over k of A(m, k) B(n, k); `p` holds what becomes of the sums
 fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, LinearParams p, int sms,
                            cudaStream_t stream, const char *name) {
@@ -497,49 +845,47 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     p.kb = (int)((k + kKb - 1) / kKb);
     p.a_mn = a_mn;
     p.b_mn = b_mn;
-    p.m_tiles = (int)((m + kM - 1) / kM);
-    // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
-    int widest = kMaxN;
-    if (f32) {
-        const int pieces = (p.kb + 7) / 8;
-        widest = pieces >= 32 ? 16 : 512 / pieces / 16 * 16;
-        if (widest > 128) widest = 128;
-    }
-    p.tile_n = n >= widest ? widest : (int)((n + 15) / 16 * 16);
+    const LinearPlan plan = plan_product(m, n, p.kb, b_mn, f32, f32 ? 4 : 2, sms);
+    p.tile_n = plan.tile_n;
+    p.split = plan.split;
+    const int wide = plan.pair ? 2 * kM : kM, mine = plan.pair ? p.tile_n / 2 : p.tile_n;    // output columns of a tile; rows of B that a CTA loads
+    p.m_tiles = (int)((m + wide - 1) / wide);
     const long long n_tiles = (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
-    p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= sms && p.kb >= 4 * p.split) p.split *= 2;
-    const int most = 512 / p.tile_n, blocks = (p.kb + p.split - 1) / p.split;
-    p.bufs = 1;
-    if (f32) p.bufs = (blocks + 7) / 8 < most ? (blocks + 7) / 8 : most;
+    p.bufs = plan.pair ? 2 : 1;
+    if (f32 && !plan.pair) {
+        // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
+        const int room = 512 / p.tile_n, pieces = ((p.kb + p.split - 1) / p.split + 7) / 8;
+        p.bufs = pieces < room ? pieces : room;
+    }
     p.tmem_cols = 32;
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
-    p.b_bytes = b_mn ? (p.tile_n + 63) / 64 * 8192 : p.tile_n * kKb * 2;
+    p.b_bytes = b_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
     const int stage = kABytes + p.b_bytes, room = kSmemMost - 1024 /* static */ - 1024 /* alignment */;
     p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
     int smem = p.stages * stage;
     if (smem < p.tile_n * kM * 4) smem = p.tile_n * kM * 4;
     smem += 1024;
-    if (tiles * p.split > 2147483647ll) {
+    if (tiles * p.split > 1073741823ll) {
         set_error("%s: too many tiles", name);
         return FI_ERR_INVALID_ARG;
     }
     CUtensorMap map_a, map_b;
     fi_status_t st = operand_map(&map_a, a, a_mn ? kKb : kM, name);
-    if (st == FI_OK) st = operand_map(&map_b, b, b_mn ? kKb : p.tile_n, name);
+    if (st == FI_OK) st = operand_map(&map_b, b, b_mn ? kKb : mine, name);
     if (st != FI_OK) return st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = p.split;
+    attr.val.clusterDim.x = plan.pair ? 2 : p.split;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * p.split));
+    cfg.gridDim = dim3((unsigned)(plan.pair ? 2 * (tiles < sms / 2 ? tiles : sms / 2) : tiles * p.split));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = f32 ? cudaLaunchKernelEx(&cfg, linear_split_kernel<true>, map_a, map_b, p) : cudaLaunchKernelEx(&cfg, linear_split_kernel<false>, map_a, map_b, p);
+    const auto kernel = plan.pair ? (f32 ? linear_pair_kernel<true> : linear_pair_kernel<false>) : (f32 ? linear_split_kernel<true> : linear_split_kernel<false>);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, p);
     if (e != cudaSuccess) return cuda_fail(e, name);
     count_launch();
     return check_launch(name);
