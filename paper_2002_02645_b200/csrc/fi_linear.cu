@@ -60,6 +60,7 @@ struct LinearParams {
     int bufs;                      // accumulators that a CTA's reduction is cut into
     int tmem_cols, stages, b_bytes;
     int act;
+    int wide;                      // rows of out, residual, preact and the bias lie on 16-byte boundaries
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -472,30 +473,107 @@ __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// tile t of the product: groups of 8 tiles along m are walked along n, so that the tiles that run at one time share their operands in L2
-__device__ __forceinline__ void tile_place(const LinearParams &p, int t, int n_tiles, int &m_tile, int &n_tile) {
+// tile t of the product: groups of 8 tiles of rows are walked along the columns, so that the tiles that run at one time share their
+// operands in L2
+__device__ __forceinline__ void tile_place(int t, int row_tiles, int col_tiles, int &row_tile, int &col_tile) {
     constexpr int kGroup = 8;
-    const int group = t / (kGroup * n_tiles), first = group * kGroup, width = min(kGroup, p.m_tiles - first), in = t - first * n_tiles;
-    n_tile = in / width;
-    m_tile = first + in - n_tile * width;
+    const int group = t / (kGroup * col_tiles), first = group * kGroup, width = min(kGroup, row_tiles - first), in = t - first * col_tiles;
+    col_tile = in / width;
+    row_tile = first + in - col_tile * width;
 }
 
-// 16 sums of a thread (column m, rows n0 .. of the product) on their way out
-template <bool F32>
-__device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, float bias, int m, int n0, int rows) {
-    const int row = row_of(p, n0 + (threadIdx.x & 15), rows);
-    float v[16];
-    int to[16];
+// 8 neighbouring values of a row of out, residual or preact
+__device__ __forceinline__ void put8(float *p, const float *v) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void put8(__nv_bfloat16 *p, const float *v) {
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        v[i] = __uint_as_float(sums[i]);
-        to[i] = __shfl_sync(0xffffffffu, row, i);
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = reinterpret_cast<const uint32_t &>(h);
     }
-    finish<F32>(p, v, bias, m, n0, 1, to);
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void get8(const float *p, float *v) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void get8(const __nv_bfloat16 *p, float *v) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
 }
 
-// One pair of CTAs per two SMs walks over tiles of 256 output columns (128 per CTA) and tile_n output rows; each CTA loads its half of
+// 16 sums of a thread (row n of the product, columns c .. ) on their way out to row `to`.  p.wide: rows of out, residual, preact and the
+// bias can be read and written 16 bytes at a time (the number of columns is a multiple of 8 anyway).
+template <bool F32>
+__device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, int c, int n, int to) {
+    using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+    float v[16], r[16];
+    const int here = n < 0 ? 0 : min(p.m - c, 16);          // 0, 8 or 16 columns, or less than none
+    const T *const from = static_cast<const T *>(p.residual) + to * p.ld_res + c;
+    T *const out = static_cast<T *>(p.out) + to * p.ld_out + c;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(sums[i]);
+    if (p.residual && to >= 0) {
+#pragma unroll
+        for (int g = 0; g < 16; g += 8)
+            if (g < here) {
+                if (p.wide) get8(from + g, r + g);
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) r[g + i] = (float)from[g + i];
+            }
+    }
+    if (p.bias) {
+        float b[8];
+#pragma unroll
+        for (int g = 0; g < 16; g += 8)
+            if (c + g < p.m) {
+                if (p.wide) get8(p.bias + c + g, b);
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) b[i] = p.bias[c + g + i];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[g + i] += b[i];
+            }
+    }
+    if (p.preact) {
+        __nv_bfloat16 *const z = p.preact + (long long)n * p.ld_preact + c;
+#pragma unroll
+        for (int g = 0; g < 16; g += 8)
+            if (g < here) {
+                if (p.wide) put8(z + g, v + g);
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[g + i] = __float2bfloat16_rn(v[g + i]);
+            }
+    }
+    activate(v, p.act);
+    if (to < 0) return;
+    if (p.residual) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += r[i];
+    }
+#pragma unroll
+    for (int g = 0; g < 16; g += 8)
+        if (g < here) {
+            if (p.wide) put8(out + g, v + g);
+            else
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[g + i] = (T)v[g + i];
+        }
+}
+
+// One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
 // both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the reduction) go out while the next is formed.
+// Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
 template <bool F32>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
@@ -506,7 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int rows = actual_rows(p), n_tiles = (rows + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
+    const int rows = actual_rows(p), row_tiles = (rows + 2 * kM - 1) / (2 * kM), col_tiles = p.m_tiles, tiles = row_tiles * col_tiles;
     if (pair >= tiles) return;                              // (both CTAs)
     unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
     const int stage_bytes = kABytes + p.b_bytes, half_n = p.tile_n >> 1;
@@ -541,9 +619,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             long long issued = 0;
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs) {
-                int mt, nt;
-                tile_place(p, t, n_tiles, mt, nt);
-                const int m0 = mt * 2 * kM + (int)rank * kM, n0 = nt * p.tile_n + (int)rank * half_n;
+                int rt, ct;
+                tile_place(t, row_tiles, col_tiles, rt, ct);
+                const int r0 = rt * 2 * kM + (int)rank * kM, c0 = ct * p.tile_n + (int)rank * half_n;
                 for (int kb = 0; kb < p.kb; ++kb, ++issued) {
                     if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) {
                         ok = false;
@@ -552,16 +630,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
                     if (rank == 0) bar_expect(&ctl->full[stage], 2u * (uint32_t)stage_bytes);
                     const uint32_t bar = map_to_rank(smem_at(&ctl->full[stage]), 0);
-                    if (p.a_mn) {
-                        load_box_pair(a, &map_a, bar, m0, kb * kKb);
-                        load_box_pair(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
+                    if (p.b_mn) {
+                        load_box_pair(a, &map_b, bar, r0, kb * kKb);
+                        load_box_pair(a + 8192, &map_b, bar, r0 + 64, kb * kKb);
                     } else {
-                        load_box_pair(a, &map_a, bar, kb * kKb, m0);
+                        load_box_pair(a, &map_b, bar, kb * kKb, r0);
                     }
-                    if (p.b_mn)
-                        for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
+                    if (p.a_mn)
+                        for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_a, bar, c0 + c, kb * kKb);
                     else
-                        load_box_pair(b, &map_b, bar, kb * kKb, n0);
+                        load_box_pair(b, &map_a, bar, kb * kKb, c0);
                     if (++stage == (uint32_t)p.stages) {
                         stage = 0;
                         phase ^= 1;
@@ -586,8 +664,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         }
     } else if (warp == 9) {
         if (lane == 0 && rank == 0) {
-            const uint32_t idesc = instruction(2 * kM, p.tile_n, p.a_mn, p.b_mn);
-            const uint32_t a_step = operand_step(p.a_mn), b_step = operand_step(p.b_mn);
+            const uint32_t idesc = instruction(2 * kM, p.tile_n, p.b_mn, p.a_mn);
+            const uint32_t a_step = operand_step(p.b_mn), b_step = operand_step(p.a_mn);
             uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs) {
@@ -606,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         }
                         tc_after();
                         const uint32_t at = smem_at(smem + stage * stage_bytes);
-                        const uint64_t a = operand(at, p.a_mn), b = operand(at + kABytes, p.b_mn);
+                        const uint64_t a = operand(at, p.b_mn), b = operand(at + kABytes, p.a_mn);
 #pragma unroll
                         for (int i = 0; i < kKb / 16; ++i) mma_pair(d, a + i * a_step, b + i * b_step, idesc, ((kb - first) | i) != 0);
                         tc_commit_pair(&ctl->empty[stage]);
@@ -629,16 +707,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             }
         }
     } else {
-        // ---- sums on their way out: warp w reads TMEM lanes 32 (w mod 4) .., and every other 16 of the tile's rows ----
-        const int half = warp >> 2, my_m = (int)rank * kM + (warp & 3) * 32 + lane;
-        const uint32_t lanes_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        // ---- sums on their way out: warp w reads TMEM lanes 32 (w mod 4) .., and half of the tile's columns ----
+        const int first = (warp >> 2) * half_n, my_row = (int)rank * kM + (warp & 3) * 32 + lane;
+        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + first;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = true;
         for (int t = pair; t < tiles && ok; t += pairs) {
-            int mt, nt;
-            tile_place(p, t, n_tiles, mt, nt);
-            const int m = mt * 2 * kM + my_m, n0 = nt * p.tile_n, cols = min(p.tile_n, rows - n0);
-            const float bias = p.bias && m < p.m ? p.bias[m] : 0.f;
+            int rt, ct;
+            tile_place(t, row_tiles, col_tiles, rt, ct);
+            const int row = rt * 2 * kM + my_row, n = row < rows ? row : -1, to = row_of(p, row, rows), c0 = ct * p.tile_n + first;
+            const int cols = min(half_n, p.m - c0);
             if constexpr (F32) {
                 uint32_t sum[kMaxN / 2];
 #pragma unroll
@@ -646,15 +724,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 for (int kb = 0; kb < p.kb && ok; kb += piece) {
                     ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                     tc_after();
-                    const uint32_t at = lanes_at + buf * p.tile_n + half * 16;
 #pragma unroll
-                    for (int c = 0; c < kMaxN / 32; ++c)
-                        if (32 * c + half * 16 < cols) {
+                    for (int c = 0; c < kMaxN / 2; c += 16)
+                        if (c < cols) {
                             uint32_t v[16];
-                            tmem_load(at + 32 * c, v);
+                            tmem_load(at + buf * p.tile_n + c, v);
                             tmem_wait(v);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) sum[16 * c + i] = __float_as_uint(__uint_as_float(sum[16 * c + i]) + __uint_as_float(v[i]));
+                            for (int i = 0; i < 16; ++i) sum[c + i] = __float_as_uint(__uint_as_float(sum[c + i]) + __uint_as_float(v[i]));
                         }
                     tc_before();
                     __syncwarp();
@@ -663,17 +740,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     if (buf == 0) buf_phase ^= 1;
                 }
 #pragma unroll
-                for (int c = 0; c < kMaxN / 32; ++c)
-                    if (32 * c + half * 16 < cols) finish16<true>(p, sum + 16 * c, bias, m, n0 + 32 * c + half * 16, rows);
+                for (int c = 0; c < kMaxN / 2; c += 16)
+                    if (c < cols) finish16<true>(p, sum + c, c0 + c, n, to);
             } else {
                 ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                 tc_after();
-                const uint32_t at = lanes_at + buf * p.tile_n;
-                for (int c = half * 16; c < cols; c += 32) {
+                for (int c = 0; c < cols; c += 16) {
                     uint32_t v[16];
-                    tmem_load(at + c, v);
+                    tmem_load(at + buf * p.tile_n + c, v);
                     tmem_wait(v);
-                    finish16<false>(p, v, bias, m, n0 + c, rows);
+                    finish16<false>(p, v, c0 + c, n, to);
                 }
                 tc_before();
                 __syncwarp();
@@ -812,15 +888,15 @@ struct LinearPlan {
     double cycles;
 };
 
-LinearPlan plan_product(long long m, long long n, long long kb, bool b_mn, bool f32, int size, int sms) {
+LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool f32, int size, int sms) {
     LinearPlan best = {false, 16, 1, 1e30};
     const auto most = [](double a, double b) { return a > b ? a : b; };
     const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
     const double memory = ((double)m * kb * 128 + (double)n * kb * 128 + (double)m * n * size) / 3400.;
     for (int tile = 32; tile <= kMaxN; tile += 32) {
-        if (b_mn && tile % 128) continue;
-        if (tile > 32 && tile - 32 >= n) break;
-        const double block = most(2. * tile, (128 + tile / 2) * 128 / 56.), rounds = (double)up(up(m, 2 * kM) * up(n, tile), sms / 2);
+        if (a_mn && tile % 128) continue;
+        if (tile > 32 && tile - 32 >= m) break;
+        const double block = most(2. * tile, (128 + tile / 2) * 128 / 56.), rounds = (double)up(up(n, 2 * kM) * up(m, tile), sms / 2);
         const double cycles = most(rounds * kb * block, memory) + 2500 + 20. * tile;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
     }
@@ -845,12 +921,14 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     p.kb = (int)((k + kKb - 1) / kKb);
     p.a_mn = a_mn;
     p.b_mn = b_mn;
-    const LinearPlan plan = plan_product(m, n, p.kb, b_mn, f32, f32 ? 4 : 2, sms);
+    const LinearPlan plan = plan_product(m, n, p.kb, a_mn, f32, f32 ? 4 : 2, sms);
     p.tile_n = plan.tile_n;
     p.split = plan.split;
-    const int wide = plan.pair ? 2 * kM : kM, mine = plan.pair ? p.tile_n / 2 : p.tile_n;    // output columns of a tile; rows of B that a CTA loads
-    p.m_tiles = (int)((m + wide - 1) / wide);
-    const long long n_tiles = (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
+    // tiles: of a pair 256 output rows and tile_n columns, of a CTA 128 columns and tile_n rows; the operand of the tile_n ones is the second
+    const bool second_mn = plan.pair ? a_mn : b_mn;
+    const int mine = plan.pair ? p.tile_n / 2 : p.tile_n;                                   // of them that a CTA loads
+    p.m_tiles = (int)(plan.pair ? (m + p.tile_n - 1) / p.tile_n : (m + kM - 1) / kM);
+    const long long n_tiles = plan.pair ? (n + 2 * kM - 1) / (2 * kM) : (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
     p.bufs = plan.pair ? 2 : 1;
     if (f32 && !plan.pair) {
         // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
@@ -859,7 +937,7 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     }
     p.tmem_cols = 32;
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
-    p.b_bytes = b_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
+    p.b_bytes = second_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
     const int stage = kABytes + p.b_bytes, room = kSmemMost - 1024 /* static */ - 1024 /* alignment */;
     p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
     int smem = p.stages * stage;
@@ -870,8 +948,8 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
         return FI_ERR_INVALID_ARG;
     }
     CUtensorMap map_a, map_b;
-    fi_status_t st = operand_map(&map_a, a, a_mn ? kKb : kM, name);
-    if (st == FI_OK) st = operand_map(&map_b, b, b_mn ? kKb : mine, name);
+    fi_status_t st = operand_map(&map_a, a, a_mn ? kKb : plan.pair ? mine : kM, name);
+    if (st == FI_OK) st = operand_map(&map_b, b, b_mn ? kKb : plan.pair ? kM : mine, name);
     if (st != FI_OK) return st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -972,6 +1050,9 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
     p.out_rows = out_rows;
     p.wait_limit = a->wait_limit > 0 && a->wait_limit < kWaitLimit ? a->wait_limit : kWaitLimit;
     p.act = a->activation;
+    const auto wide = [&](const void *at, int64_t ld, long long rows_of, int bytes) { return aligned16(at) && (rows_of <= 1 || ld * bytes % 16 == 0); };
+    p.wide = wide(a->out, a->out_stride, out_rows, size) && wide(a->residual, a->residual_stride, out_rows, size) &&
+             wide(a->preact, a->preact_stride, a->tokens, 2) && aligned16(a->bias);
     const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
     return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, p, sms, static_cast<cudaStream_t>(cuda_stream),
                           name);
@@ -1033,6 +1114,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     p.wait_limit = kWaitLimit;
     if (a->dx) {
         p.out = a->dx;
+        p.wide = aligned16(a->dx) && (a->tokens <= 1 || a->dx_stride % 8 == 0);
         p.ld_out = a->dx_stride;
         p.out_rows = a->tokens;
         const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride};
@@ -1041,6 +1123,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     }
     if (a->dweight) {
         p.out = a->dweight;
+        p.wide = aligned16(a->dweight) && a->dweight_stride % 8 == 0;
         p.ld_out = a->dweight_stride;
         p.out_rows = a->out_dim;
         const Matrix x = {a->x, a->tokens, a->in_dim, a->x_stride};
