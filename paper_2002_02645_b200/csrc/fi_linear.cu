@@ -22,9 +22,10 @@ constexpr int kKb = 64;                   // reduction values of a stage
 constexpr int kABytes = kM * kKb * 2;
 constexpr int kMaxN = 256;                // output rows of a tile, at most
 constexpr int kMaxStages = 12;
+constexpr int kPiece = 16;                // blocks of the reduction that are added up in one accumulator for float32 results
 constexpr int kEpiThreads = 256;          // warps 0..7: TMEM lanes 32 (w mod 4) ..; warp 8 loads, warp 9 issues the products
 constexpr int kThreads = kEpiThreads + 64;
-constexpr int kSmemMost = 227 * 1024;
+constexpr int kSmemMost = 227 * 1024, kStaticMost = 5 * 1024;
 constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
 constexpr long long kShortLimit = 1 << 20;       // limits below it are a test's
 constexpr long long kDrainLimit = 200000000ll;   // (about 0.1 s)
@@ -44,6 +45,7 @@ struct PairCtl {
     uint64_t never;
     uint32_t tmem;
     volatile int gave_up;
+    alignas(16) float bias[kEpiThreads / 32][kMaxN / 2];      // of the columns that a warp works on
 };
 
 struct LinearParams {
@@ -180,9 +182,34 @@ __device__ __forceinline__ float cluster_load(uint32_t addr) {
     return v;
 }
 
-constexpr float kGeluTanh = 0.044715f, kGeluTwice = 1.5957691216057308f;   // 2 sqrt(2 / pi)
+// Exponential and reciprocal of the special-function unit (2^-22 of the result); the power unit takes a few clocks off the whole kernel for
+// every instruction more in here.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float recip_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.4426950408889634f, kGeluTanh = 0.044715f, kGeluTwice = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 
-__device__ __forceinline__ float logistic(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+// 1 / (1 + 2^-x)
+__device__ __forceinline__ float logistic2(float x) { return recip_fast(1.f + exp2_fast(-x)); }
+
+// Phi(z) = erfc(-z / sqrt 2) / 2, from erfc(a) = t (a1 + t (a2 + ..)) exp(-a^2), t = 1 / (1 + p a), for a >= 0 (Abramowitz and Stegun, Handbook of
+// Mathematical Functions, 7.1.26: off by 1.5e-7 at most).  density: exp(-z^2 / 2)
+__device__ __forceinline__ float normal_cdf(float z, float &density) {
+    const float t = recip_fast(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
+    density = exp2_fast(z * z * (-0.5f * kLog2e));
+    float q = fmaf(t, 1.061405429f, -1.453152027f);
+    q = fmaf(t, q, 1.421413741f);
+    q = fmaf(t, q, -0.284496736f);
+    q = fmaf(t, q, 0.254829592f) * t * (0.5f * density);
+    return z >= 0.f ? 1.f - q : q;
+}
 
 template <int N>
 __device__ __forceinline__ void activate(float (&z)[N], int act) {
@@ -191,17 +218,20 @@ __device__ __forceinline__ void activate(float (&z)[N], int act) {
 #pragma unroll
             for (int i = 0; i < N; ++i) z[i] = z[i] < 0.f ? 0.f : z[i];      // (NaN stays)
             break;
-        case FI_ACT_GELU:                                                    // (not 1 + erf, which loses the small values of z < 0)
+        case FI_ACT_GELU:
 #pragma unroll
-            for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * erfcf(z[i] * -0.70710678f);
+            for (int i = 0; i < N; ++i) {
+                float density;
+                z[i] *= normal_cdf(z[i], density);
+            }
             break;
         case FI_ACT_GELU_TANH:
 #pragma unroll
-            for (int i = 0; i < N; ++i) z[i] *= logistic(kGeluTwice * fmaf(kGeluTanh * z[i], z[i] * z[i], z[i]));
+            for (int i = 0; i < N; ++i) z[i] *= logistic2(z[i] * fmaf(kGeluTwice * kGeluTanh * kLog2e, z[i] * z[i], kGeluTwice * kLog2e));
             break;
         case FI_ACT_SILU:
 #pragma unroll
-            for (int i = 0; i < N; ++i) z[i] *= logistic(z[i]);
+            for (int i = 0; i < N; ++i) z[i] *= logistic2(z[i] * kLog2e);
             break;
         default: break;
     }
@@ -213,16 +243,18 @@ __device__ __forceinline__ float slope(float z, int act) {
         case FI_ACT_RELU: return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
         case FI_ACT_GELU: {
             if (fabsf(z) > 20.f) return z > 0.f ? 1.f : 0.f;
-            return fmaf(z * 0.39894228f, __expf(-0.5f * z * z), 0.5f * erfcf(z * -0.70710678f));
+            float density;
+            const float whole = normal_cdf(z, density);
+            return fmaf(z * 0.39894228f, density, whole);
         }
         case FI_ACT_GELU_TANH: {
             if (fabsf(z) > 20.f) return z > 0.f ? 1.f : 0.f;
-            const float s = logistic(kGeluTwice * fmaf(kGeluTanh * z, z * z, z));
+            const float s = logistic2(z * fmaf(kGeluTwice * kGeluTanh * kLog2e, z * z, kGeluTwice * kLog2e));
             return fmaf(z * s * (1.f - s), kGeluTwice * fmaf(3.f * kGeluTanh * z, z, 1.f), s);
         }
         case FI_ACT_SILU: {
             if (fabsf(z) > 100.f) return z > 0.f ? 1.f : 0.f;
-            const float s = logistic(z);
+            const float s = logistic2(z * kLog2e);
             return s * fmaf(z, 1.f - s, 1.f);
         }
         default: return 1.f;
@@ -512,8 +544,9 @@ __device__ __forceinline__ void get8(const __nv_bfloat16 *p, float *v) {
 
 // 16 sums of a thread (row n of the product, columns c .. ) on their way out to row `to`.  p.wide: rows of out, residual, preact and the
 // bias can be read and written 16 bytes at a time (the number of columns is a multiple of 8 anyway).
+// `bias`: of these columns, in shared memory; nullptr: none.
 template <bool F32>
-__device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, int c, int n, int to) {
+__device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, int c, int n, int to, const float *bias, bool add) {
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     float v[16], r[16];
     const int here = n < 0 ? 0 : min(p.m - c, 16);          // 0, 8 or 16 columns, or less than none
@@ -521,7 +554,7 @@ __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *
     T *const out = static_cast<T *>(p.out) + to * p.ld_out + c;
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(sums[i]);
-    if (p.residual && to >= 0) {
+    if (add && to >= 0) {
 #pragma unroll
         for (int g = 0; g < 16; g += 8)
             if (g < here) {
@@ -531,18 +564,14 @@ __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *
                     for (int i = 0; i < 8; ++i) r[g + i] = (float)from[g + i];
             }
     }
-    if (p.bias) {
+    if (bias) {
         float b[8];
 #pragma unroll
-        for (int g = 0; g < 16; g += 8)
-            if (c + g < p.m) {
-                if (p.wide) get8(p.bias + c + g, b);
-                else
+        for (int g = 0; g < 16; g += 8) {
+            get8(bias + g, b);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) b[i] = p.bias[c + g + i];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[g + i] += b[i];
-            }
+            for (int i = 0; i < 8; ++i) v[g + i] += b[i];
+        }
     }
     if (p.preact) {
         __nv_bfloat16 *const z = p.preact + (long long)n * p.ld_preact + c;
@@ -557,7 +586,7 @@ __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *
     }
     activate(v, p.act);
     if (to < 0) return;
-    if (p.residual) {
+    if (add) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] += r[i];
     }
@@ -572,7 +601,7 @@ __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *
 }
 
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
-// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the reduction) go out while the next is formed.
+// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 1,024 values of the reduction) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
 template <bool F32>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
@@ -588,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     if (pair >= tiles) return;                              // (both CTAs)
     unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
     const int stage_bytes = kABytes + p.b_bytes, half_n = p.tile_n >> 1;
-    const int piece = F32 ? 8 : p.kb;                       // blocks of an accumulator
+    const int piece = F32 ? kPiece : p.kb;                  // blocks of an accumulator
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&ctl->full[s], 1);
@@ -717,10 +746,26 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             tile_place(t, row_tiles, col_tiles, rt, ct);
             const int row = rt * 2 * kM + my_row, n = row < rows ? row : -1, to = row_of(p, row, rows), c0 = ct * p.tile_n + first;
             const int cols = min(half_n, p.m - c0);
+            const float *bias = nullptr;
+            if (p.bias) {
+                __syncwarp();
+                for (int c = lane; c < cols; c += 32) ctl->bias[warp][c] = p.bias[c0 + c];
+                __syncwarp();
+                bias = ctl->bias[warp];
+            }
+            const char *const ahead = to >= 0 && p.residual ? static_cast<const char *>(p.residual) + (to * p.ld_res + c0) * (F32 ? 4 : 2) : nullptr;
             if constexpr (F32) {
+                // Without an activation the sum begins with the residual, whose way here is hidden behind the products then; only
+                // two accumulators of a tile can be ahead of the one that goes out.
                 uint32_t sum[kMaxN / 2];
+                const bool begin = ahead && p.act == FI_ACT_NONE && !p.preact && p.wide;
+                if (!begin && ahead)
+                    for (int c = 0; c < cols; c += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + c * 4));
 #pragma unroll
-                for (int i = 0; i < kMaxN / 2; ++i) sum[i] = 0;
+                for (int c = 0; c < kMaxN / 2; c += 4) {
+                    const uint4 r = begin && c < cols ? *reinterpret_cast<const uint4 *>(ahead + c * 4) : make_uint4(0, 0, 0, 0);
+                    sum[c] = r.x; sum[c + 1] = r.y; sum[c + 2] = r.z; sum[c + 3] = r.w;
+                }
                 for (int kb = 0; kb < p.kb && ok; kb += piece) {
                     ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                     tc_after();
@@ -741,15 +786,17 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 }
 #pragma unroll
                 for (int c = 0; c < kMaxN / 2; c += 16)
-                    if (c < cols) finish16<true>(p, sum + c, c0 + c, n, to);
+                    if (c < cols) finish16<true>(p, sum + c, c0 + c, n, to, bias ? bias + c : nullptr, ahead && !begin);
             } else {
+                if (ahead)
+                    for (int c = 0; c < cols; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + c * 2));
                 ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                 tc_after();
                 for (int c = 0; c < cols; c += 16) {
                     uint32_t v[16];
                     tmem_load(at + buf * p.tile_n + c, v);
                     tmem_wait(v);
-                    finish16<false>(p, v, c0 + c, n, to);
+                    finish16<false>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, ahead != nullptr);
                 }
                 tc_before();
                 __syncwarp();
@@ -840,10 +887,10 @@ fi_status_t device_facts(int *sms, const char *name) {
     if (*sms) return FI_OK;
     int n = 0;
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - 1024);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
     if (e != cudaSuccess) return cuda_fail(e, name);
     g_facts[dev].sms.store(n, std::memory_order_release);
     *sms = n;
@@ -904,7 +951,7 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
         if (tile > 16 && tile - 16 >= n) break;
         for (int split = 1; split <= 8 && split <= kb; split *= 2) {
             const long long blocks = up(kb, split);
-            if (f32 && up(blocks, 8) * tile > 512 && tile > 16) continue;      // pieces of 512 values have an accumulator each
+            if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 1,024 values have an accumulator each
             const double block = most(2. * tile, (128 + tile) * 128 / 56.), rounds = (double)up(up(m, kM) * up(n, tile) * split, sms);
             const double cycles = most(rounds * (blocks * block + 2500 + 20. * tile), memory + 2500 + 20. * tile) + (split > 1 ? 1000 : 0);
             if (cycles < best.cycles) best = {false, tile, split, cycles};
@@ -931,14 +978,14 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     const long long n_tiles = plan.pair ? (n + 2 * kM - 1) / (2 * kM) : (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
     p.bufs = plan.pair ? 2 : 1;
     if (f32 && !plan.pair) {
-        // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
-        const int room = 512 / p.tile_n, pieces = ((p.kb + p.split - 1) / p.split + 7) / 8;
+        // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 1,024 at a time
+        const int room = 512 / p.tile_n, pieces = ((p.kb + p.split - 1) / p.split + kPiece - 1) / kPiece;
         p.bufs = pieces < room ? pieces : room;
     }
     p.tmem_cols = 32;
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
     p.b_bytes = second_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
-    const int stage = kABytes + p.b_bytes, room = kSmemMost - 1024 /* static */ - 1024 /* alignment */;
+    const int stage = kABytes + p.b_bytes, room = kSmemMost - kStaticMost - 1024 /* alignment */;
     p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
     int smem = p.stages * stage;
     if (smem < p.tile_n * kM * 4) smem = p.tile_n * kM * 4;
