@@ -61,6 +61,7 @@ struct LinearParams {
     int split;                     // CTAs of a cluster that share a tile's reduction
     int bufs;                      // accumulators that a CTA's reduction is cut into
     int tmem_cols, stages, b_bytes;
+    int part_at;                   // place of a CTA's sums in shared memory
     int act;
     int wide;                      // rows of out, residual, preact and the bias lie on 16-byte boundaries
 };
@@ -175,13 +176,6 @@ __device__ __forceinline__ void tmem_wait(uint32_t *v) {
                  :
                  : "memory");
 }
-// result of a load that is not volatile to the compiler's order, from shared memory of a CTA of the cluster
-__device__ __forceinline__ float cluster_load(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 // Exponential and reciprocal of the special-function unit (2^-22 of the result); the power unit takes a few clocks off the whole kernel for
 // every instruction more in here.
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -310,8 +304,16 @@ __device__ __forceinline__ void finish(const LinearParams &p, float (&v)[N], flo
         if (here && to[i] >= 0) out[to[i] * p.ld_out] = (T)v[i];
 }
 
-// Few tiles: a CTA takes 128 output columns and up to 256 output rows, `split` CTAs of a cluster share its reduction and add up
-// their sums through distributed shared memory, in the order of their ranks.
+__device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
+// Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction.  Column sums of row c go
+// to CTA c mod split, which adds them up in the order of the ranks.  Bound by the latency from the launch to the last store, and by the
+// operands' way from memory: the loader sets up its barriers and has all stages on the way before the CTA has its TMEM.
 constexpr int kBatch = 8;              // values of a thread that go out together
 template <bool F32>
 __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
@@ -323,12 +325,33 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int tile = blockIdx.x / p.split, rank = blockIdx.x - tile * p.split;
     const int m0 = (tile % p.m_tiles) * kM, n0 = (tile / p.m_tiles) * p.tile_n;
-    const int rows = actual_rows(p);
-    if (n0 >= rows) return;                                 // (all CTAs of the cluster)
     unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
     const int kb0 = (int)((long long)p.kb * rank / p.split), kb1 = (int)((long long)p.kb * (rank + 1) / p.split);
     const int stage_bytes = kABytes + p.b_bytes;
-    if (tid == 0) {
+    uint32_t stage = 0, phase = 0;                          // of the loader
+    const auto load = [&](int kb) {
+        const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
+        uint64_t *const bar = &ctl->full[stage];
+        bar_expect(bar, (uint32_t)stage_bytes);
+        if (p.a_mn) {
+            load_box(a, &map_a, bar, m0, kb * kKb);
+            load_box(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
+        } else {
+            load_box(a, &map_a, bar, kb * kKb, m0);
+        }
+        if (p.b_mn)
+            for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
+        else
+            load_box(b, &map_b, bar, kb * kKb, n0);
+        if (++stage == (uint32_t)p.stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    };
+    const int early = min(kb1 - kb0, p.stages);             // blocks that need no free stage
+    if (tid == kEpiThreads) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&ctl->full[s], 1);
             bar_init(&ctl->empty[s], 1);
@@ -338,7 +361,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
         ctl->gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        for (int i = 0; i < early; ++i) load(kb0 + i);
     }
+    const int rows = actual_rows(p);
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(p.tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -347,35 +372,21 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     __syncthreads();
     tc_after();
     const uint32_t tmem = ctl->tmem;
+    const bool apart = p.split > 1 && p.part_at > 0;
+    if (apart) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const int cols = min(p.tile_n, rows - n0);              // rows of the output that there are; no more is done if there is none
     // so that a wait runs out for certain
     if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
     if (warp == 8) {
         if (lane == 0) {
-            int kb = kb0;
-            uint32_t stage = 0, phase = 0;
-            for (; kb < kb1; ++kb) {
-                if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) break;
-                const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
-                uint64_t *const bar = &ctl->full[stage];
-                bar_expect(bar, (uint32_t)stage_bytes);
-                if (p.a_mn) {
-                    load_box(a, &map_a, bar, m0, kb * kKb);
-                    load_box(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
-                } else {
-                    load_box(a, &map_a, bar, kb * kKb, m0);
+            int kb = kb0 + early;
+            if (cols > 0)
+                for (; kb < kb1; ++kb) {
+                    if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) break;
+                    load(kb);
                 }
-                if (p.b_mn)
-                    for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
-                else
-                    load_box(b, &map_b, bar, kb * kKb, n0);
-                if (++stage == (uint32_t)p.stages) {
-                    stage = 0;
-                    phase ^= 1;
-                }
-            }
-            if (kb < kb1) {                                 // gave up: the copies that were started land first
-                int back = min(kb - kb0, p.stages);
-                for (; back > 0; --back) {
+            if (kb < kb1 || cols <= 0 || ctl->gave_up) {    // stopped: the copies that were started land first
+                for (int back = min(kb - kb0, p.stages); back > 0; --back) {
                     if (stage == 0) {
                         stage = p.stages;
                         phase ^= 1;
@@ -385,11 +396,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             }
         }
     } else if (warp == 9) {
-        if (lane == 0) {
+        if (lane == 0 && cols > 0) {
             const uint32_t idesc = instruction(kM, p.tile_n, p.a_mn, p.b_mn);
             const uint32_t a_step = operand_step(p.a_mn), b_step = operand_step(p.b_mn);
             const int length = (kb1 - kb0 + p.bufs - 1) / p.bufs;
-            uint32_t stage = 0, phase = 0, d = tmem;
+            uint32_t d = tmem;
             int in_buf = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) break;
@@ -411,20 +422,22 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             tc_commit(&ctl->done);
             bar_drain(&ctl->done, 0);
         }
-    }
-    __syncwarp();
-    if (warp < 8) {
+    } else if (cols > 0) {
         bar_wait(&ctl->done, 0, ctl, p.wait_limit);
         tc_after();
     }
     __syncthreads();                                        // (the loader too has nothing on its way now)
-    // the CTA's sums into shared memory, [output row][128 columns]
-    float *const part = reinterpret_cast<float *>(smem);
-    const int cols = min(p.tile_n, rows - n0);
-    if (warp < 8) {
+    // sums of the CTA's reduction: [rank][row / split][128 columns] in the CTA that the row belongs to.  Few rows have a place of their own
+    // behind the stages, others that of the stages, which all CTAs of the cluster have to be done with.
+    float *const part = reinterpret_cast<float *>(smem + p.part_at);
+    const int slots = (p.tile_n + p.split - 1) / p.split;
+    if (apart) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (all of them have started, long ago)
+    else if (p.split > 1) cluster_sync();
+    if (warp < 8 && cols > 0) {
         const int used = (kb1 - kb0 + p.bufs - 1) / p.bufs;                       // blocks of a buffer
         const int bufs = (kb1 - kb0 + used - 1) / used;                           // buffers that hold something
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t to = smem_at(part) + ((rank * slots) * kM + (warp & 3) * 32 + lane) * 4;
         for (int c = (warp >> 2) * 16; c < cols; c += 32) {
             uint32_t v[16], w[16];
             tmem_load(at + c, v);
@@ -435,8 +448,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
             }
+            if (p.split == 1) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) part[(c + i) * kM + (warp & 3) * 32 + lane] = __uint_as_float(v[i]);
+                for (int i = 0; i < 16; ++i) part[(c + i) * kM + (warp & 3) * 32 + lane] = __uint_as_float(v[i]);
+            } else {
+                // (split is a power of two)
+                const int shift = __ffs(p.split) - 1;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (c + i < cols) cluster_store(map_to_rank(to + ((c + i) >> shift) * (kM * 4), (c + i) & (p.split - 1)), __uint_as_float(v[i]));
+            }
         }
         tc_before();
     }
@@ -445,29 +466,25 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     if (warp < 8) {
         const int m = m0 + (tid & (kM - 1));
         const float bias = p.bias && m < p.m ? p.bias[m] : 0.f;
-        const uint32_t mine = smem_at(part) + (tid & (kM - 1)) * 4;
+        const float *const mine = part + (tid & (kM - 1));
         const int step = 2 * p.split;
-        for (int c0 = rank * 2 + (tid >> 7); c0 < cols; c0 += kBatch * step) {
+        for (int c0 = (tid >> 7) * p.split + rank; c0 < cols; c0 += kBatch * step) {
             float v[kBatch];
             int to[kBatch];
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) to[i] = c0 + i * step < cols ? row_of(p, n0 + c0 + i * step, rows) : kNoRow;
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) v[i] = 0.f;
+            const int slot = c0 / p.split;
             for (int s = 0; s < p.split; ++s) {
-                const uint32_t from = p.split > 1 ? map_to_rank(mine, s) : mine;
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) v[i] += cluster_load(from + min(c0 + i * step, cols - 1) * (kM * 4));
+                for (int i = 0; i < kBatch; ++i) v[i] += mine[(s * slots + min(slot + 2 * i, slots - 1)) * kM];
             }
             finish<F32>(p, v, bias, m, n0 + c0, step, to);
         }
-    }
-    if (p.split > 1) cluster_sync();                        // the others have read this CTA's sums
-    else __syncthreads();
-    if (warp == 0) {
         tc_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
     }
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
 }
 
 // ---- pairs of CTAs: many tiles ----
@@ -986,9 +1003,13 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
     p.b_bytes = second_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
     const int stage = kABytes + p.b_bytes, room = kSmemMost - kStaticMost - 1024 /* alignment */;
-    p.stages = room / stage < kMaxStages ? room / stage : kMaxStages;
-    int smem = p.stages * stage;
-    if (smem < p.tile_n * kM * 4) smem = p.tile_n * kM * 4;
+    const int part = plan.pair ? 0 : p.split * ((p.tile_n + p.split - 1) / p.split) * kM * 4;
+    const bool apart = p.split > 1 && p.tile_n <= 64;
+    p.stages = (room - (apart ? part : 0)) / stage;
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    p.part_at = apart ? p.stages * stage : 0;
+    int smem = p.stages * stage + (apart ? part : 0);
+    if (smem < part) smem = part;
     smem += 1024;
     if (tiles * p.split > 1073741823ll) {
         set_error("%s: too many tiles", name);
