@@ -57,12 +57,10 @@ struct LinearParams {
     long long ld_res, ld_out, ld_preact, out_rows, wait_limit;
     int m, n, kb;                  // output columns, rows; blocks of 64 of the reduction
     int m_tiles, tile_n;
-    int a_mn, b_mn;                // operand with the reduction strided (its own index contiguous)
     int split;                     // CTAs of a cluster that share a tile's reduction
     int bufs;                      // accumulators that a CTA's reduction is cut into
     int tmem_cols, stages, b_bytes;
     int part_at;                   // place of a CTA's sums in shared memory
-    int act;
     int wide;                      // rows of out, residual, preact and the bias lie on 16-byte boundaries
 };
 
@@ -136,28 +134,67 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Operand in shared memory, 128-byte swizzle.  Reduction contiguous: rows of 128 bytes, groups of eight 1,024 bytes apart.  Else a
-// line of 128 bytes holds 64 rows at one k: 8 k's are 1,024 bytes, the next 64 rows 8,192 bytes further.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, int mn) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(mn ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
-           (uint64_t)2 << 61;
-}
-// between the k's of successive MMAs (16 of them), in units of 16 bytes
-__device__ __forceinline__ uint32_t operand_step(int mn) { return mn ? 2048 >> 4 : 32 >> 4; }
-// bf16 x bf16 -> fp32
-__device__ __forceinline__ uint32_t instruction(int m, int n, int a_mn, int b_mn) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
-           ((uint32_t)(m >> 4) << 24);
-}
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// One lane of the warp, always the same, for the instructions that are issued once; the loops around them are the whole warp's, so that their
+// operands stay in uniform registers (with the loops in one lane a block of the reduction took 650 cycles to issue, more than its products).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
     asm volatile(
         "{\n"
         ".reg .pred p;\n"
-        "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
-        "}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(yes));
+    return yes != 0;
+}
+
+// Operand in shared memory, 128-byte swizzle; low word of its descriptor.  Reduction contiguous: rows of 128 bytes, groups of eight 1,024 bytes
+// apart.  Else (MN) a line of 128 bytes holds 64 rows at one k: 8 k's are 1,024 bytes, the next 64 rows 8,192 bytes further.
+template <bool MN>
+__device__ __forceinline__ uint32_t operand(uint32_t addr) {
+    return (addr & 0x3ffffu) >> 4 | (uint32_t)(MN ? 8192 >> 4 : 1) << 16;    // (in a cluster an address has its CTA in the bits above)
+}
+constexpr uint32_t kOperandHigh = 1024 >> 4 | 1u << 14 | 2u << 29;
+// between the k's of successive MMAs (16 of them), in units of 16 bytes
+template <bool MN>
+constexpr uint32_t kOperandStep = MN ? 2048 >> 4 : 32 >> 4;
+
+// bf16 x bf16 -> fp32
+__device__ __forceinline__ uint32_t instruction(int m, int n, bool a_mn, bool b_mn) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(m >> 4) << 24);
+}
+// one block of the reduction, 4 MMAs of 16; PAIR: D (256 x N, 128 rows in each CTA's TMEM) from 128 rows of A and N / 2 of B in each CTA
+template <bool PAIR, bool A_MN, bool B_MN>
+__device__ __forceinline__ void mma_block(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+#pragma unroll
+    for (int i = 0; i < kKb / 16; ++i) {
+        const uint32_t a_low = a + i * kOperandStep<A_MN>, b_low = b + i * kOperandStep<B_MN>, more = i ? 1u : accumulate;
+        if (PAIR)
+            asm volatile(
+                "{\n"
+                ".reg .pred p;\n"
+                ".reg .b64 x, y;\n"
+                "setp.ne.b32 p, %4, 0;\n"
+                "mov.b64 x, {%1, %5};\n"
+                "mov.b64 y, {%2, %5};\n"
+                "tcgen05.mma.cta_group::2.kind::f16 [%0], x, y, %3, p;\n"
+                "}\n" ::"r"(d),
+                "r"(a_low), "r"(b_low), "r"(idesc), "r"(more), "r"(kOperandHigh)
+                : "memory");
+        else
+            asm volatile(
+                "{\n"
+                ".reg .pred p;\n"
+                ".reg .b64 x, y;\n"
+                "setp.ne.b32 p, %4, 0;\n"
+                "mov.b64 x, {%1, %5};\n"
+                "mov.b64 y, {%2, %5};\n"
+                "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n"
+                "}\n" ::"r"(d),
+                "r"(a_low), "r"(b_low), "r"(idesc), "r"(more), "r"(kOperandHigh)
+                : "memory");
+    }
 }
 // 16 columns of the thread's TMEM lane
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t *v) {
@@ -205,9 +242,9 @@ __device__ __forceinline__ float normal_cdf(float z, float &density) {
     return z >= 0.f ? 1.f - q : q;
 }
 
-template <int N>
-__device__ __forceinline__ void activate(float (&z)[N], int act) {
-    switch (act) {
+template <int ACT, int N>
+__device__ __forceinline__ void activate(float (&z)[N]) {
+    switch (ACT) {
         case FI_ACT_RELU:
 #pragma unroll
             for (int i = 0; i < N; ++i) z[i] = z[i] < 0.f ? 0.f : z[i];      // (NaN stays)
@@ -271,11 +308,10 @@ __device__ __forceinline__ int row_of(const LinearParams &p, int n, int rows) {
     return to >= 0 && to < p.out_rows ? to : kSkipRow;
 }
 
-// What becomes of N sums, column m and rows n0, n0 + step .. of the product; to[i]: their rows of out, negative: none.  (Every choice is
-// made once for all of them: with a choice per value the two warps of a scheduler wait for their own branches, 59 us, not 27, for 8,192
-// tokens 1,024 -> 1,024.  Loads before stores, so that they are on the way together.)
-template <bool F32, int N>
-__device__ __forceinline__ void finish(const LinearParams &p, float (&v)[N], float bias, int m, int n0, int step, const int (&to)[N]) {
+// What becomes of N sums, column m and rows n0, n0 + 1 .. of the product; to[i]: their rows of out, negative: none.  (Every choice is
+// made once for all of them, the activation when the kernel is compiled: what runs is short, and loads are on the way together.)
+template <bool F32, int ACT, int N>
+__device__ __forceinline__ void finish(const LinearParams &p, float (&v)[N], float bias, int m, int n0, const int (&to)[N]) {
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     T r[N];
     const bool here = m < p.m;
@@ -291,9 +327,9 @@ __device__ __forceinline__ void finish(const LinearParams &p, float (&v)[N], flo
         __nv_bfloat16 *const z = p.preact + (long long)n0 * p.ld_preact + m;
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (here && to[i] != kNoRow) z[i * step * p.ld_preact] = __float2bfloat16_rn(v[i]);
+            if (here && to[i] != kNoRow) z[i * p.ld_preact] = __float2bfloat16_rn(v[i]);
     }
-    activate(v, p.act);
+    activate<ACT>(v);
     if (p.residual) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += (float)r[i];
@@ -304,63 +340,71 @@ __device__ __forceinline__ void finish(const LinearParams &p, float (&v)[N], flo
         if (here && to[i] >= 0) out[to[i] * p.ld_out] = (T)v[i];
 }
 
-__device__ __forceinline__ void cluster_store(uint32_t addr, float v) {
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+__device__ __forceinline__ void cluster_store4(uint32_t addr, const uint32_t *v) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 
-// Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction.  Column sums of row c go
-// to CTA c mod split, which adds them up in the order of the ranks.  Bound by the latency from the launch to the last store, and by the
-// operands' way from memory: the loader sets up its barriers and has all stages on the way before the CTA has its TMEM.
-constexpr int kBatch = 8;              // values of a thread that go out together
-template <bool F32>
+// Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction.  Sums of four rows go
+// to CTA (row / 4) mod split, which adds them up in the order of the ranks.  Bound by the latency from the launch to the last store, and by
+// the operands' way from memory: the loader sets up its barriers and has all stages on the way before the CTA has its TMEM.
+template <bool F32, int ACT, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                    const __grid_constant__ CUtensorMap map_b,
                                                                    const __grid_constant__ LinearParams p) {
     extern __shared__ unsigned char raw_smem[];
     __shared__ LinearCtl ctl_space;
     LinearCtl *const ctl = &ctl_space;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int tile = blockIdx.x / p.split, rank = blockIdx.x - tile * p.split;
     const int m0 = (tile % p.m_tiles) * kM, n0 = (tile / p.m_tiles) * p.tile_n;
-    unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
+    const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u;
     const int kb0 = (int)((long long)p.kb * rank / p.split), kb1 = (int)((long long)p.kb * (rank + 1) / p.split);
-    const int stage_bytes = kABytes + p.b_bytes;
-    uint32_t stage = 0, phase = 0;                          // of the loader
-    const auto load = [&](int kb) {
-        const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
-        uint64_t *const bar = &ctl->full[stage];
-        bar_expect(bar, (uint32_t)stage_bytes);
-        if (p.a_mn) {
-            load_box(a, &map_a, bar, m0, kb * kKb);
-            load_box(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
-        } else {
-            load_box(a, &map_a, bar, kb * kKb, m0);
-        }
-        if (p.b_mn)
-            for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
-        else
-            load_box(b, &map_b, bar, kb * kKb, n0);
+    const uint32_t stage_bytes = kABytes + p.b_bytes;
+    uint32_t stage = 0, phase = 0;                          // of the loader, of the products
+    const auto next_stage = [&] {
         if (++stage == (uint32_t)p.stages) {
             stage = 0;
             phase ^= 1;
         }
     };
-    const int early = min(kb1 - kb0, p.stages);             // blocks that need no free stage
-    if (tid == kEpiThreads) {
-        prefetch_map(&map_a);
-        prefetch_map(&map_b);
-        for (int s = 0; s < p.stages; ++s) {
-            bar_init(&ctl->full[s], 1);
-            bar_init(&ctl->empty[s], 1);
+    const auto load = [&](int kb) {
+        if (elect_one()) {
+            const uint32_t a = smem + stage * stage_bytes, b = a + kABytes;
+            uint64_t *const bar = &ctl->full[stage];
+            bar_expect(bar, stage_bytes);
+            if (A_MN) {
+                load_box(a, &map_a, bar, m0, kb * kKb);
+                load_box(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
+            } else {
+                load_box(a, &map_a, bar, kb * kKb, m0);
+            }
+            if (B_MN)
+                for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
+            else
+                load_box(b, &map_b, bar, kb * kKb, n0);
         }
-        bar_init(&ctl->done, 1);
-        bar_init(&ctl->never, 1);
-        ctl->gave_up = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        next_stage();
+    };
+    const int early = min(kb1 - kb0, p.stages);             // blocks that need no free stage
+    if (warp == 8) {
+        if (elect_one()) {
+            prefetch_map(&map_a);
+            prefetch_map(&map_b);
+            for (int s = 0; s < p.stages; ++s) {
+                bar_init(&ctl->full[s], 1);
+                bar_init(&ctl->empty[s], 1);
+            }
+            bar_init(&ctl->done, 1);
+            bar_init(&ctl->never, 1);
+            ctl->gave_up = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
         for (int i = 0; i < early; ++i) load(kb0 + i);
     }
     const int rows = actual_rows(p);
@@ -378,48 +422,44 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     // so that a wait runs out for certain
     if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
     if (warp == 8) {
-        if (lane == 0) {
-            int kb = kb0 + early;
-            if (cols > 0)
-                for (; kb < kb1; ++kb) {
-                    if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) break;
-                    load(kb);
+        int kb = kb0 + early;
+        if (cols > 0)
+            for (; kb < kb1; ++kb) {
+                if (!__all_sync(0xffffffffu, bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit))) break;
+                load(kb);
+            }
+        if (kb < kb1 || cols <= 0 || __any_sync(0xffffffffu, ctl->gave_up)) {    // stopped: the copies that were started land first
+            for (int back = min(kb - kb0, p.stages); back > 0; --back) {
+                if (stage == 0) {
+                    stage = p.stages;
+                    phase ^= 1;
                 }
-            if (kb < kb1 || cols <= 0 || ctl->gave_up) {    // stopped: the copies that were started land first
-                for (int back = min(kb - kb0, p.stages); back > 0; --back) {
-                    if (stage == 0) {
-                        stage = p.stages;
-                        phase ^= 1;
-                    }
-                    bar_drain(&ctl->full[--stage], phase);
-                }
+                bar_drain(&ctl->full[--stage], phase);
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && cols > 0) {
-            const uint32_t idesc = instruction(kM, p.tile_n, p.a_mn, p.b_mn);
-            const uint32_t a_step = operand_step(p.a_mn), b_step = operand_step(p.b_mn);
+        if (cols > 0) {
+            const uint32_t idesc = instruction(kM, p.tile_n, A_MN, B_MN);
             const int length = (kb1 - kb0 + p.bufs - 1) / p.bufs;
             uint32_t d = tmem;
             int in_buf = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) break;
+                if (!__all_sync(0xffffffffu, bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit))) break;
                 tc_after();
-                const uint32_t at = smem_at(smem + stage * stage_bytes);
-                const uint64_t a = operand(at, p.a_mn), b = operand(at + kABytes, p.b_mn);
-#pragma unroll
-                for (int i = 0; i < kKb / 16; ++i) mma(d, a + i * a_step, b + i * b_step, idesc, (in_buf | i) != 0);
-                tc_commit(&ctl->empty[stage]);
+                if (elect_one()) {
+                    const uint32_t at = smem + stage * stage_bytes;
+                    mma_block<false, A_MN, B_MN>(d, operand<A_MN>(at), operand<B_MN>(at + kABytes), idesc, in_buf != 0);
+                    tc_commit(&ctl->empty[stage]);
+                }
+                __syncwarp();
                 if (++in_buf == length) {
                     in_buf = 0;
                     d += p.tile_n;
                 }
-                if (++stage == (uint32_t)p.stages) {
-                    stage = 0;
-                    phase ^= 1;
-                }
+                next_stage();
             }
-            tc_commit(&ctl->done);
+            if (elect_one()) tc_commit(&ctl->done);
+            __syncwarp();
             bar_drain(&ctl->done, 0);
         }
     } else if (cols > 0) {
@@ -427,36 +467,33 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
         tc_after();
     }
     __syncthreads();                                        // (the loader too has nothing on its way now)
-    // sums of the CTA's reduction: [rank][row / split][128 columns] in the CTA that the row belongs to.  Few rows have a place of their own
-    // behind the stages, others that of the stages, which all CTAs of the cluster have to be done with.
-    float *const part = reinterpret_cast<float *>(smem + p.part_at);
-    const int slots = (p.tile_n + p.split - 1) / p.split;
+    // Sums of the CTA's reduction: [rank][group of four rows / split][128 columns][4] in the CTA that the group belongs to.  Few rows have a place of
+    // their own behind the stages, others that of the stages, which all CTAs of the cluster have to be done with.
+    const uint32_t part = smem + p.part_at;
+    const int slots = (p.tile_n / 4 + p.split - 1) / p.split, shift = __ffs(p.split) - 1;       // (split is a power of two)
     if (apart) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // (all of them have started, long ago)
     else if (p.split > 1) cluster_sync();
     if (warp < 8 && cols > 0) {
         const int used = (kb1 - kb0 + p.bufs - 1) / p.bufs;                       // blocks of a buffer
         const int bufs = (kb1 - kb0 + used - 1) / used;                           // buffers that hold something
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t to = smem_at(part) + ((rank * slots) * kM + (warp & 3) * 32 + lane) * 4;
+        const uint32_t to = part + (rank * slots * kM + (warp & 3) * 32 + lane) * 16;
+#pragma unroll 1
         for (int c = (warp >> 2) * 16; c < cols; c += 32) {
             uint32_t v[16], w[16];
             tmem_load(at + c, v);
             tmem_wait(v);
+#pragma unroll 1
             for (int b = 1; b < bufs; ++b) {
                 tmem_load(at + b * p.tile_n + c, w);
                 tmem_wait(w);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
             }
-            if (p.split == 1) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) part[(c + i) * kM + (warp & 3) * 32 + lane] = __uint_as_float(v[i]);
-            } else {
-                // (split is a power of two)
-                const int shift = __ffs(p.split) - 1;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (c + i < cols) cluster_store(map_to_rank(to + ((c + i) >> shift) * (kM * 4), (c + i) & (p.split - 1)), __uint_as_float(v[i]));
+            for (int i = 0; i < 4; ++i) {
+                const int group = (c >> 2) + i;
+                if (group * 4 < cols) cluster_store4(map_to_rank(to + (group >> shift) * (kM * 16), group & (p.split - 1)), v + 4 * i);
             }
         }
         tc_before();
@@ -466,21 +503,23 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     if (warp < 8) {
         const int m = m0 + (tid & (kM - 1));
         const float bias = p.bias && m < p.m ? p.bias[m] : 0.f;
-        const float *const mine = part + (tid & (kM - 1));
-        const int step = 2 * p.split;
-        for (int c0 = (tid >> 7) * p.split + rank; c0 < cols; c0 += kBatch * step) {
-            float v[kBatch];
-            int to[kBatch];
+#pragma unroll 1
+        for (int slot = tid >> 7; (slot * p.split + rank) * 4 < cols; slot += 2) {
+            const int c = (slot * p.split + rank) * 4;
+            float v[4] = {};
+            int to[4];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) to[i] = c0 + i * step < cols ? row_of(p, n0 + c0 + i * step, rows) : kNoRow;
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) v[i] = 0.f;
-            const int slot = c0 / p.split;
+            for (int i = 0; i < 4; ++i) to[i] = row_of(p, n0 + c + i, rows < n0 + cols ? rows : n0 + cols);
+#pragma unroll 1
             for (int s = 0; s < p.split; ++s) {
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) v[i] += mine[(s * slots + min(slot + 2 * i, slots - 1)) * kM];
+                float4 x;
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+                             : "r"(part + ((s * slots + slot) * kM + (tid & (kM - 1))) * 16)
+                             : "memory");
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
             }
-            finish<F32>(p, v, bias, m, n0 + c0, step, to);
+            finish<F32, ACT>(p, v, bias, m, n0 + c, to);
         }
         tc_after();
     }
@@ -499,17 +538,6 @@ __device__ __forceinline__ void load_box_pair(uint32_t dst, const CUtensorMap *m
     asm volatile(
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
-        : "memory");
-}
-// D (256 x N, 128 rows in each CTA's TMEM) += A (128 rows of each CTA) x B (N / 2 rows of each)
-__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n"
-        ".reg .pred p;\n"
-        "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
-        "}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 // when the pair's products so far are over: the barrier at this place in both CTAs
@@ -562,7 +590,7 @@ __device__ __forceinline__ void get8(const __nv_bfloat16 *p, float *v) {
 // 16 sums of a thread (row n of the product, columns c .. ) on their way out to row `to`.  p.wide: rows of out, residual, preact and the
 // bias can be read and written 16 bytes at a time (the number of columns is a multiple of 8 anyway).
 // `bias`: of these columns, in shared memory; nullptr: none.
-template <bool F32>
+template <bool F32, int ACT>
 __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, int c, int n, int to, const float *bias, bool add) {
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     float v[16], r[16];
@@ -601,7 +629,7 @@ __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *
                     for (int i = 0; i < 8; ++i) z[g + i] = __float2bfloat16_rn(v[g + i]);
             }
     }
-    activate(v, p.act);
+    activate<ACT>(v);
     if (to < 0) return;
     if (add) {
 #pragma unroll
@@ -620,20 +648,20 @@ __device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
 // both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 1,024 values of the reduction) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
-template <bool F32>
+template <bool F32, int ACT, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
                                                                   const __grid_constant__ LinearParams p) {
     extern __shared__ unsigned char raw_smem[];
     __shared__ PairCtl ctl_space;
     PairCtl *const ctl = &ctl_space;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int rows = actual_rows(p), row_tiles = (rows + 2 * kM - 1) / (2 * kM), col_tiles = p.m_tiles, tiles = row_tiles * col_tiles;
     if (pair >= tiles) return;                              // (both CTAs)
-    unsigned char *const smem = raw_smem + ((1024 - (smem_at(raw_smem) & 1023)) & 1023);
-    const int stage_bytes = kABytes + p.b_bytes, half_n = p.tile_n >> 1;
+    const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u, stage_bytes = kABytes + p.b_bytes;
+    const int half_n = p.tile_n >> 1;
     const int piece = F32 ? kPiece : p.kb;                  // blocks of an accumulator
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
@@ -659,95 +687,93 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     tc_after();
     const uint32_t tmem = ctl->tmem;
     if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
+    uint32_t stage = 0, phase = 0;                          // of the loader, of the products
+    const auto next_stage = [&] {
+        if (++stage == (uint32_t)p.stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+    };
     if (warp == 8) {
-        if (lane == 0) {
-            uint32_t stage = 0, phase = 0;
-            long long issued = 0;
-            bool ok = true;
-            for (int t = pair; t < tiles && ok; t += pairs) {
-                int rt, ct;
-                tile_place(t, row_tiles, col_tiles, rt, ct);
-                const int r0 = rt * 2 * kM + (int)rank * kM, c0 = ct * p.tile_n + (int)rank * half_n;
-                for (int kb = 0; kb < p.kb; ++kb, ++issued) {
-                    if (!bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t a = smem_at(smem + stage * stage_bytes), b = a + kABytes;
-                    if (rank == 0) bar_expect(&ctl->full[stage], 2u * (uint32_t)stage_bytes);
+        int issued = 0;                                     // (up to the number of stages)
+        bool ok = true;
+        for (int t = pair; t < tiles && ok; t += pairs) {
+            int rt, ct;
+            tile_place(t, row_tiles, col_tiles, rt, ct);
+            const int r0 = rt * 2 * kM + (int)rank * kM, c0 = ct * p.tile_n + (int)rank * half_n;
+            for (int kb = 0; kb < p.kb; ++kb) {
+                ok = __all_sync(0xffffffffu, bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit));
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t a = smem + stage * stage_bytes, b = a + kABytes;
+                    if (rank == 0) bar_expect(&ctl->full[stage], 2u * stage_bytes);
                     const uint32_t bar = map_to_rank(smem_at(&ctl->full[stage]), 0);
-                    if (p.b_mn) {
+                    if (B_MN) {
                         load_box_pair(a, &map_b, bar, r0, kb * kKb);
                         load_box_pair(a + 8192, &map_b, bar, r0 + 64, kb * kKb);
                     } else {
                         load_box_pair(a, &map_b, bar, kb * kKb, r0);
                     }
-                    if (p.a_mn)
+                    if (A_MN)
                         for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_a, bar, c0 + c, kb * kKb);
                     else
                         load_box_pair(b, &map_a, bar, kb * kKb, c0);
-                    if (++stage == (uint32_t)p.stages) {
-                        stage = 0;
+                }
+                __syncwarp();
+                issued = min(issued + 1, p.stages);
+                next_stage();
+            }
+        }
+        if (!ok) {
+            // gave up: the copies that were started land first (the second CTA cannot see that, and gives them 10 ms)
+            if (rank == 0) {
+                for (; issued > 0; --issued) {
+                    if (stage == 0) {
+                        stage = p.stages;
                         phase ^= 1;
                     }
+                    bar_drain(&ctl->full[--stage], phase);
                 }
-            }
-            if (!ok) {
-                // gave up: the copies that were started land first (the second CTA cannot see that, and gives them 10 ms)
-                if (rank == 0) {
-                    for (int back = (int)(issued < p.stages ? issued : p.stages); back > 0; --back) {
-                        if (stage == 0) {
-                            stage = p.stages;
-                            phase ^= 1;
-                        }
-                        bar_drain(&ctl->full[--stage], phase);
-                    }
-                } else {
-                    const long long t0 = clock64();
-                    while (clock64() - t0 < kDrainLimit / 10) {}
-                }
+            } else {
+                const long long t0 = clock64();
+                while (clock64() - t0 < kDrainLimit / 10) {}
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && rank == 0) {
-            const uint32_t idesc = instruction(2 * kM, p.tile_n, p.b_mn, p.a_mn);
-            const uint32_t a_step = operand_step(p.b_mn), b_step = operand_step(p.a_mn);
-            uint32_t stage = 0, phase = 0, buf = 0, buf_phase = 0;
+        if (rank == 0) {
+            const uint32_t idesc = instruction(2 * kM, p.tile_n, B_MN, A_MN);
+            uint32_t buf = 0, buf_phase = 0;
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs) {
                 for (int kb = 0; kb < p.kb && ok;) {
-                    if (!bar_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit)) {
-                        ok = false;
-                        break;
-                    }
+                    ok = __all_sync(0xffffffffu, bar_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit));
+                    if (!ok) break;
                     tc_after();
                     const uint32_t d = tmem + buf * p.tile_n;
                     const int end = min(kb + piece, p.kb);
-                    for (int first = kb; kb < end; ++kb) {
-                        if (!bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) {
-                            ok = false;
-                            break;
-                        }
+                    for (uint32_t more = 0; kb < end; ++kb, more = 1) {
+                        ok = __all_sync(0xffffffffu, bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit));
+                        if (!ok) break;
                         tc_after();
-                        const uint32_t at = smem_at(smem + stage * stage_bytes);
-                        const uint64_t a = operand(at, p.b_mn), b = operand(at + kABytes, p.a_mn);
-#pragma unroll
-                        for (int i = 0; i < kKb / 16; ++i) mma_pair(d, a + i * a_step, b + i * b_step, idesc, ((kb - first) | i) != 0);
-                        tc_commit_pair(&ctl->empty[stage]);
-                        if (++stage == (uint32_t)p.stages) {
-                            stage = 0;
-                            phase ^= 1;
+                        if (elect_one()) {
+                            const uint32_t at = smem + stage * stage_bytes;
+                            mma_block<true, B_MN, A_MN>(d, operand<B_MN>(at), operand<A_MN>(at + kABytes), idesc, more);
+                            tc_commit_pair(&ctl->empty[stage]);
                         }
+                        __syncwarp();
+                        next_stage();
                     }
                     if (ok) {
-                        tc_commit_pair(&ctl->sums_full[buf]);
+                        if (elect_one()) tc_commit_pair(&ctl->sums_full[buf]);
+                        __syncwarp();
                         buf ^= 1;
                         if (buf == 0) buf_phase ^= 1;
                     }
                 }
             }
             if (!ok) {                                      // no product is on its way when TMEM is freed
-                tc_commit_pair(&ctl->never);
+                if (elect_one()) tc_commit_pair(&ctl->never);
+                __syncwarp();
                 const long long t0 = clock64();
                 while (clock64() - t0 < kDrainLimit / 10) {}
             }
@@ -775,7 +801,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 // Without an activation the sum begins with the residual, whose way here is hidden behind the products then; only
                 // two accumulators of a tile can be ahead of the one that goes out.
                 uint32_t sum[kMaxN / 2];
-                const bool begin = ahead && p.act == FI_ACT_NONE && !p.preact && p.wide;
+                const bool begin = ahead && ACT == FI_ACT_NONE && !p.preact && p.wide;
                 if (!begin && ahead)
                     for (int c = 0; c < cols; c += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + c * 4));
 #pragma unroll
@@ -803,7 +829,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 }
 #pragma unroll
                 for (int c = 0; c < kMaxN / 2; c += 16)
-                    if (c < cols) finish16<true>(p, sum + c, c0 + c, n, to, bias ? bias + c : nullptr, ahead && !begin);
+                    if (c < cols) finish16<true, ACT>(p, sum + c, c0 + c, n, to, bias ? bias + c : nullptr, ahead && !begin);
             } else {
                 if (ahead)
                     for (int c = 0; c < cols; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + c * 2));
@@ -813,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     uint32_t v[16];
                     tmem_load(at + buf * p.tile_n + c, v);
                     tmem_wait(v);
-                    finish16<false>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, ahead != nullptr);
+                    finish16<false, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, ahead != nullptr);
                 }
                 tc_before();
                 __syncwarp();
@@ -887,11 +913,31 @@ __global__ void __launch_bounds__(256) linear_bias_sum_kernel(const float *parti
 
 // ------------------------------------------------------------------------------------------------------------- host
 
+using LinearKernel = void (*)(CUtensorMap, CUtensorMap, LinearParams);
+
+// forward products in all their forms; gradients have none
+template <bool PAIR, bool F32, int ACT, bool A_MN, bool B_MN>
+constexpr LinearKernel kLinearKernel = PAIR ? &linear_pair_kernel<F32, ACT, A_MN, B_MN> : &linear_split_kernel<F32, ACT, A_MN, B_MN>;
+
+template <bool PAIR>
+LinearKernel linear_kernel(bool f32, int act, bool a_mn, bool b_mn) {
+    if (a_mn) return b_mn ? kLinearKernel<PAIR, false, FI_ACT_NONE, true, true> : kLinearKernel<PAIR, false, FI_ACT_NONE, true, false>;
+    switch (act) {
+        case FI_ACT_RELU: return f32 ? kLinearKernel<PAIR, true, FI_ACT_RELU, false, false> : kLinearKernel<PAIR, false, FI_ACT_RELU, false, false>;
+        case FI_ACT_GELU: return f32 ? kLinearKernel<PAIR, true, FI_ACT_GELU, false, false> : kLinearKernel<PAIR, false, FI_ACT_GELU, false, false>;
+        case FI_ACT_GELU_TANH:
+            return f32 ? kLinearKernel<PAIR, true, FI_ACT_GELU_TANH, false, false> : kLinearKernel<PAIR, false, FI_ACT_GELU_TANH, false, false>;
+        case FI_ACT_SILU: return f32 ? kLinearKernel<PAIR, true, FI_ACT_SILU, false, false> : kLinearKernel<PAIR, false, FI_ACT_SILU, false, false>;
+        default: return f32 ? kLinearKernel<PAIR, true, FI_ACT_NONE, false, false> : kLinearKernel<PAIR, false, FI_ACT_NONE, false, false>;
+    }
+}
+
 struct DeviceFacts {
     std::atomic<int> sms{0};
 };
 DeviceFacts g_facts[kMaxDevices];
 
+// SMs of the current device; its kernels are set up at the first call
 fi_status_t device_facts(int *sms, const char *name) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -904,10 +950,12 @@ fi_status_t device_facts(int *sms, const char *name) {
     if (*sms) return FI_OK;
     int n = 0;
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_split_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(linear_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+    for (int form = 0; form < 12; ++form) {                 // of a product: type and activation, or one of two gradients
+        const bool back = form >= 10, f32 = !back && form >= 5;
+        const LinearKernel both[2] = {linear_kernel<false>(f32, form % 5, back, form == 11), linear_kernel<true>(f32, form % 5, back, form == 11)};
+        for (int i = 0; i < 2 && e == cudaSuccess; ++i)
+            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(both[i]), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+    }
     if (e != cudaSuccess) return cuda_fail(e, name);
     g_facts[dev].sms.store(n, std::memory_order_release);
     *sms = n;
@@ -978,13 +1026,11 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
 }
 
 // D[n][m] = sum over k of A(m, k) B(n, k); `p` holds what becomes of the sums
-fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, LinearParams p, int sms,
-                           cudaStream_t stream, const char *name) {
+fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act, LinearParams p,
+                           int sms, cudaStream_t stream, const char *name) {
     p.m = (int)m;
     p.n = (int)n;
     p.kb = (int)((k + kKb - 1) / kKb);
-    p.a_mn = a_mn;
-    p.b_mn = b_mn;
     const LinearPlan plan = plan_product(m, n, p.kb, a_mn, f32, f32 ? 4 : 2, sms);
     p.tile_n = plan.tile_n;
     p.split = plan.split;
@@ -1003,7 +1049,7 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
     p.b_bytes = second_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
     const int stage = kABytes + p.b_bytes, room = kSmemMost - kStaticMost - 1024 /* alignment */;
-    const int part = plan.pair ? 0 : p.split * ((p.tile_n + p.split - 1) / p.split) * kM * 4;
+    const int part = plan.pair ? 0 : p.split * ((p.tile_n / 4 + p.split - 1) / p.split) * kM * 16;
     const bool apart = p.split > 1 && p.tile_n <= 64;
     p.stages = (room - (apart ? part : 0)) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
@@ -1030,7 +1076,7 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const auto kernel = plan.pair ? (f32 ? linear_pair_kernel<true> : linear_pair_kernel<false>) : (f32 ? linear_split_kernel<true> : linear_split_kernel<false>);
+    const LinearKernel kernel = plan.pair ? linear_kernel<true>(f32, act, a_mn, b_mn) : linear_kernel<false>(f32, act, a_mn, b_mn);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, p);
     if (e != cudaSuccess) return cuda_fail(e, name);
     count_launch();
@@ -1117,13 +1163,12 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
     p.ld_preact = a->preact_stride;
     p.out_rows = out_rows;
     p.wait_limit = a->wait_limit > 0 && a->wait_limit < kWaitLimit ? a->wait_limit : kWaitLimit;
-    p.act = a->activation;
     const auto wide = [&](const void *at, int64_t ld, long long rows_of, int bytes) { return aligned16(at) && (rows_of <= 1 || ld * bytes % 16 == 0); };
     p.wide = wide(a->out, a->out_stride, out_rows, size) && wide(a->residual, a->residual_stride, out_rows, size) &&
              wide(a->preact, a->preact_stride, a->tokens, 2) && aligned16(a->bias);
     const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
-    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, p, sms, static_cast<cudaStream_t>(cuda_stream),
-                          name);
+    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, a->activation, p, sms,
+                          static_cast<cudaStream_t>(cuda_stream), name);
 }
 
 int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation) {
@@ -1186,7 +1231,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         p.ld_out = a->dx_stride;
         p.out_rows = a->tokens;
         const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride};
-        st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, p, sms, stream, name);
+        st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, p, sms, stream, name);
         if (st != FI_OK) return st;
     }
     if (a->dweight) {
@@ -1195,7 +1240,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         p.ld_out = a->dweight_stride;
         p.out_rows = a->out_dim;
         const Matrix x = {a->x, a->tokens, a->in_dim, a->x_stride};
-        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, p, sms, stream, name);
+        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, p, sms, stream, name);
         if (st != FI_OK) return st;
     }
     if (a->dbias) {
