@@ -25,7 +25,7 @@ constexpr int kMaxStages = 12;
 constexpr int kPiece = 16;                // blocks of the reduction that are added up in one accumulator for float32 results
 constexpr int kEpiThreads = 256;          // warps 0..7: TMEM lanes 32 (w mod 4) ..; warp 8 loads, warp 9 issues the products
 constexpr int kThreads = kEpiThreads + 64;
-constexpr int kSmemMost = 227 * 1024, kStaticMost = 5 * 1024;
+constexpr int kSmemMost = 227 * 1024, kStaticMost = 22 * 1024;
 constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
 constexpr long long kShortLimit = 1 << 20;       // limits below it are a test's
 constexpr long long kDrainLimit = 200000000ll;   // (about 0.1 s)
@@ -46,6 +46,7 @@ struct PairCtl {
     uint32_t tmem;
     volatile int gave_up;
     alignas(16) float bias[kEpiThreads / 32][kMaxN / 2];      // of the columns that a warp works on
+    alignas(128) uint4 turn[kEpiThreads / 32][128];           // 64 bytes of its 32 rows
 };
 
 struct LinearParams {
@@ -559,90 +560,110 @@ __device__ __forceinline__ void tile_place(int t, int row_tiles, int col_tiles, 
     row_tile = first + in - col_tile * width;
 }
 
-// 8 neighbouring values of a row of out, residual or preact
-__device__ __forceinline__ void put8(float *p, const float *v) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+// 64 bytes of each of a warp's 32 rows on their way between registers (a thread has its row's) and memory, through 2 KB of shared memory: a
+// warp's access then covers 8 rows by 64 bytes, not 32 rows by 16 (float32 residual stream of 4,096 x 4,096 behind 4,096: 143 -> 114 us).
+__device__ __forceinline__ uint32_t turn_at(uint32_t base, int row, int piece) { return base + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
+__device__ __forceinline__ void shared_store4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void put8(__nv_bfloat16 *p, const float *v) {
-    uint32_t w[4];
+__device__ __forceinline__ uint4 shared_load4(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// columns c .. of row `to` (negative: none) of a matrix with `cols` columns
+template <typename T>
+__device__ __forceinline__ void rows_in(const T *from, long long ld, int to, int c, int cols, uint32_t base, uint32_t (&w)[16]) {
+    constexpr int kPieceCols = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31, col = c + (lane & 3) * kPieceCols;
+    uint4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int row = __shfl_sync(0xffffffffu, to, j * 8 + (lane >> 2));
+        v[j] = row >= 0 && col < cols ? *reinterpret_cast<const uint4 *>(from + row * ld + col) : make_uint4(0, 0, 0, 0);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) shared_store4(turn_at(base, j * 8 + (lane >> 2), lane & 3), v[j].x, v[j].y, v[j].z, v[j].w);
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        w[i] = reinterpret_cast<const uint32_t &>(h);
+        const uint4 x = shared_load4(turn_at(base, lane, i));
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
     }
-    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void get8(const float *p, float *v) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void get8(const __nv_bfloat16 *p, float *v) {
-    const uint4 a = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+template <typename T>
+__device__ __forceinline__ void rows_out(T *out, long long ld, int to, int c, int cols, uint32_t base, const uint32_t (&w)[16]) {
+    constexpr int kPieceCols = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31, col = c + (lane & 3) * kPieceCols;
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) shared_store4(turn_at(base, lane, i), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int row = __shfl_sync(0xffffffffu, to, j * 8 + (lane >> 2));
+        const uint4 v = shared_load4(turn_at(base, j * 8 + (lane >> 2), lane & 3));
+        if (row >= 0 && col < cols) *reinterpret_cast<uint4 *>(out + row * ld + col) = v;
     }
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return reinterpret_cast<const uint32_t &>(h);
 }
 
-// 16 sums of a thread (row n of the product, columns c .. ) on their way out to row `to`.  p.wide: rows of out, residual, preact and the
-// bias can be read and written 16 bytes at a time (the number of columns is a multiple of 8 anyway).
-// `bias`: of these columns, in shared memory; nullptr: none.
+// Sums of a thread (row n of the product, negative: none; 16 columns from c on, of bfloat16 results 32) on their way out to row `to`.
+// `bias`: of these columns, in shared memory; nullptr: none.  add: the residual is still to come.  p.wide: rows of out, residual and
+// preact can be read and written 16 bytes at a time (the number of columns is a multiple of 8 anyway).
 template <bool F32, int ACT>
-__device__ __forceinline__ void finish16(const LinearParams &p, const uint32_t *sums, int c, int n, int to, const float *bias, bool add) {
+__device__ __forceinline__ void finish_row(const LinearParams &p, float (&v)[F32 ? 16 : 32], int c, int n, int to, const float *bias, bool add,
+                                           uint32_t base) {
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
-    float v[16], r[16];
-    const int here = n < 0 ? 0 : min(p.m - c, 16);          // 0, 8 or 16 columns, or less than none
-    const T *const from = static_cast<const T *>(p.residual) + to * p.ld_res + c;
-    T *const out = static_cast<T *>(p.out) + to * p.ld_out + c;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(sums[i]);
-    if (add && to >= 0) {
-#pragma unroll
-        for (int g = 0; g < 16; g += 8)
-            if (g < here) {
-                if (p.wide) get8(from + g, r + g);
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) r[g + i] = (float)from[g + i];
-            }
-    }
+    constexpr int N = F32 ? 16 : 32;
+    uint32_t r[16];
+    if (add && p.wide) rows_in(static_cast<const T *>(p.residual), p.ld_res, to, c, p.m, base, r);
     if (bias) {
-        float b[8];
 #pragma unroll
-        for (int g = 0; g < 16; g += 8) {
-            get8(bias + g, b);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[g + i] += b[i];
+        for (int i = 0; i < N; i += 4) {
+            const float4 b = *reinterpret_cast<const float4 *>(bias + i);
+            v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
         }
     }
     if (p.preact) {
         __nv_bfloat16 *const z = p.preact + (long long)n * p.ld_preact + c;
+        uint32_t w[16];
+        if (!F32 && p.wide) {
 #pragma unroll
-        for (int g = 0; g < 16; g += 8)
-            if (g < here) {
-                if (p.wide) put8(z + g, v + g);
-                else
+            for (int i = 0; i < 16; ++i) w[i] = pack2(v[F32 ? 0 : 2 * i], v[F32 ? 0 : 2 * i + 1]);
+            rows_out(p.preact, p.ld_preact, n, c, p.m, base, w);
+        } else if (n >= 0) {
+#pragma unroll
+            for (int g = 0; g < N; g += 8)
+                if (c + g < p.m)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) z[g + i] = __float2bfloat16_rn(v[g + i]);
-            }
+        }
     }
     activate<ACT>(v);
-    if (to < 0) return;
-    if (add) {
+    if (p.wide) {
+        if (add) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += r[i];
-    }
-#pragma unroll
-    for (int g = 0; g < 16; g += 8)
-        if (g < here) {
-            if (p.wide) put8(out + g, v + g);
-            else
-#pragma unroll
-                for (int i = 0; i < 8; ++i) out[g + i] = (T)v[g + i];
+            for (int i = 0; i < N; ++i)
+                v[i] += F32 ? __uint_as_float(r[F32 ? i : 0]) : __uint_as_float(i & 1 ? r[F32 ? 0 : i / 2] & 0xffff0000u : r[F32 ? 0 : i / 2] << 16);
         }
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = F32 ? __float_as_uint(v[i]) : pack2(v[F32 ? 0 : 2 * i], v[F32 ? 0 : 2 * i + 1]);
+        rows_out(static_cast<T *>(p.out), p.ld_out, to, c, p.m, base, w);
+    } else if (to >= 0) {
+        const T *const from = static_cast<const T *>(p.residual) + to * p.ld_res + c;
+        T *const out = static_cast<T *>(p.out) + to * p.ld_out + c;
+#pragma unroll
+        for (int g = 0; g < N; g += 8)
+            if (c + g < p.m)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[g + i] = (T)(add ? v[g + i] + (float)from[g + i] : v[g + i]);
+    }
 }
 
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
@@ -796,21 +817,22 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 __syncwarp();
                 bias = ctl->bias[warp];
             }
-            const char *const ahead = to >= 0 && p.residual ? static_cast<const char *>(p.residual) + (to * p.ld_res + c0) * (F32 ? 4 : 2) : nullptr;
+            const uint32_t turn = smem_at(ctl->turn[warp]);
+            const bool add = p.residual != nullptr;
             if constexpr (F32) {
                 // Without an activation the sum begins with the residual, whose way here is hidden behind the products then; only
                 // two accumulators of a tile can be ahead of the one that goes out.
-                uint32_t sum[kMaxN / 2];
-                const bool begin = ahead && ACT == FI_ACT_NONE && !p.preact && p.wide;
-                if (!begin && ahead)
-                    for (int c = 0; c < cols; c += 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + c * 4));
+                float sum[kMaxN / 2];
+                const bool begin = add && ACT == FI_ACT_NONE && !p.preact && p.wide;
 #pragma unroll
-                for (int c = 0; c < kMaxN / 2; c += 4) {
-                    const uint4 r = begin && c < cols ? *reinterpret_cast<const uint4 *>(ahead + c * 4) : make_uint4(0, 0, 0, 0);
-                    sum[c] = r.x; sum[c + 1] = r.y; sum[c + 2] = r.z; sum[c + 3] = r.w;
+                for (int c = 0; c < kMaxN / 2; c += 16) {
+                    uint32_t r[16] = {};
+                    if (begin && c < cols) rows_in(static_cast<const float *>(p.residual), p.ld_res, to, c0 + c, p.m, turn, r);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[c + i] = __uint_as_float(r[i]);
                 }
                 for (int kb = 0; kb < p.kb && ok; kb += piece) {
-                    ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
+                    ok = __all_sync(0xffffffffu, bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit));
                     tc_after();
 #pragma unroll
                     for (int c = 0; c < kMaxN / 2; c += 16)
@@ -819,7 +841,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                             tmem_load(at + buf * p.tile_n + c, v);
                             tmem_wait(v);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) sum[c + i] = __float_as_uint(__uint_as_float(sum[c + i]) + __uint_as_float(v[i]));
+                            for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(v[i]);
                         }
                     tc_before();
                     __syncwarp();
@@ -829,17 +851,29 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                 }
 #pragma unroll
                 for (int c = 0; c < kMaxN / 2; c += 16)
-                    if (c < cols) finish16<true, ACT>(p, sum + c, c0 + c, n, to, bias ? bias + c : nullptr, ahead && !begin);
+                    if (c < cols) {
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = sum[c + i];
+                        finish_row<true, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add && !begin, turn);
+                    }
             } else {
-                if (ahead)
-                    for (int c = 0; c < cols; c += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(ahead + c * 2));
-                ok = bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
+                ok = __all_sync(0xffffffffu, bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit));
                 tc_after();
-                for (int c = 0; c < cols; c += 16) {
-                    uint32_t v[16];
-                    tmem_load(at + buf * p.tile_n + c, v);
-                    tmem_wait(v);
-                    finish16<false, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, ahead != nullptr);
+#pragma unroll 1
+                for (int c = 0; c < cols; c += 32) {
+                    uint32_t s0[16], s1[16];
+                    tmem_load(at + buf * p.tile_n + c, s0);
+                    tmem_load(at + buf * p.tile_n + c + 16, s1);
+                    tmem_wait(s0);
+                    tmem_wait(s1);
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        v[i] = __uint_as_float(s0[i]);
+                        v[16 + i] = __uint_as_float(s1[i]);
+                    }
+                    finish_row<false, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add, turn);
                 }
                 tc_before();
                 __syncwarp();
@@ -1005,9 +1039,8 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
     const auto most = [](double a, double b) { return a > b ? a : b; };
     const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
     const double memory = ((double)m * kb * 128 + (double)n * kb * 128 + (double)m * n * size) / 3400.;
-    for (int tile = 32; tile <= kMaxN; tile += 32) {
+    for (int tile = 64; tile <= kMaxN; tile += 64) {          // (a warp takes 32 columns of a half at a time)
         if (a_mn && tile % 128) continue;
-        if (tile > 32 && tile - 32 >= m) break;
         const double block = most(2. * tile, (128 + tile / 2) * 128 / 56.), rounds = (double)up(up(n, 2 * kM) * up(m, tile), sms / 2);
         const double cycles = most(rounds * kb * block, memory) + 2500 + 20. * tile;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
