@@ -18,8 +18,8 @@ namespace fi {
 namespace {
 
 constexpr int kM = 128;                   // output columns of a CTA (MMA rows)
-constexpr int kKb = 64;                   // reduction values of a stage
-constexpr int kABytes = kM * kKb * 2;
+constexpr int kKb = 64;                   // reduction values of a block: 128 bytes, a line of the swizzle
+constexpr int kABytes = kM * kKb * 2;     // of a block
 constexpr int kMaxN = 256;                // output rows of a tile, at most
 constexpr int kMaxStages = 12;
 constexpr int kPiece = 16;                // blocks of the reduction that are added up in one accumulator for float32 results
@@ -56,7 +56,7 @@ struct LinearParams {
     __nv_bfloat16 *preact;
     const int32_t *rows, *count;
     long long ld_res, ld_out, ld_preact, out_rows, wait_limit;
-    int m, n, kb;                  // output columns, rows; blocks of 64 of the reduction
+    int m, n, kb;                  // output columns, rows; steps of the reduction: one or two blocks of 64, a stage each
     int m_tiles, tile_n;
     int split;                     // CTAs of a cluster that share a tile's reduction
     int bufs;                      // accumulators that a CTA's reduction is cut into
@@ -105,6 +105,11 @@ __device__ __noinline__ bool bar_wait_long(uint64_t *bar, uint32_t parity, Ctl *
 template <typename Ctl>
 __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, Ctl *ctl, long long limit) {
     return bar_try(bar, parity) || bar_wait_long(bar, parity, ctl, limit);
+}
+// the same for a whole warp
+template <typename Ctl>
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl *ctl, long long limit) {
+    return __all_sync(0xffffffffu, bar_try(bar, parity)) || __all_sync(0xffffffffu, bar_wait_long(bar, parity, ctl, limit));
 }
 // for the end of a role that gave up: what it has started is over before the CTA leaves
 __device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity) {
@@ -351,7 +356,7 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
 // Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction.  Sums of four rows go
 // to CTA (row / 4) mod split, which adds them up in the order of the ranks.  Bound by the latency from the launch to the last store, and by
 // the operands' way from memory: the loader sets up its barriers and has all stages on the way before the CTA has its TMEM.
-template <bool F32, int ACT, bool A_MN, bool B_MN>
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
 __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                    const __grid_constant__ CUtensorMap map_b,
                                                                    const __grid_constant__ LinearParams p) {
@@ -363,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     const int m0 = (tile % p.m_tiles) * kM, n0 = (tile / p.m_tiles) * p.tile_n;
     const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u;
     const int kb0 = (int)((long long)p.kb * rank / p.split), kb1 = (int)((long long)p.kb * (rank + 1) / p.split);
-    const uint32_t stage_bytes = kABytes + p.b_bytes;
+    const uint32_t block_bytes = kABytes + p.b_bytes, stage_bytes = DEPTH * block_bytes;
     uint32_t stage = 0, phase = 0;                          // of the loader, of the products
     const auto next_stage = [&] {
         if (++stage == (uint32_t)p.stages) {
@@ -373,19 +378,23 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     };
     const auto load = [&](int kb) {
         if (elect_one()) {
-            const uint32_t a = smem + stage * stage_bytes, b = a + kABytes;
             uint64_t *const bar = &ctl->full[stage];
             bar_expect(bar, stage_bytes);
-            if (A_MN) {
-                load_box(a, &map_a, bar, m0, kb * kKb);
-                load_box(a + 8192, &map_a, bar, m0 + 64, kb * kKb);
-            } else {
-                load_box(a, &map_a, bar, kb * kKb, m0);
+#pragma unroll
+            for (int i = 0; i < DEPTH; ++i) {               // (a second block past the end is zeros)
+                const uint32_t a = smem + stage * stage_bytes + i * block_bytes, b = a + kABytes;
+                const int k = (kb * DEPTH + i) * kKb;
+                if (A_MN) {
+                    load_box(a, &map_a, bar, m0, k);
+                    load_box(a + 8192, &map_a, bar, m0 + 64, k);
+                } else {
+                    load_box(a, &map_a, bar, k, m0);
+                }
+                if (B_MN)
+                    for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, k);
+                else
+                    load_box(b, &map_b, bar, k, n0);
             }
-            if (B_MN)
-                for (int c = 0; c < p.tile_n; c += 64) load_box(b + c * 128, &map_b, bar, n0 + c, kb * kKb);
-            else
-                load_box(b, &map_b, bar, kb * kKb, n0);
         }
         __syncwarp();
         next_stage();
@@ -426,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
         int kb = kb0 + early;
         if (cols > 0)
             for (; kb < kb1; ++kb) {
-                if (!__all_sync(0xffffffffu, bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit))) break;
+                if (!warp_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) break;
                 load(kb);
             }
         if (kb < kb1 || cols <= 0 || __any_sync(0xffffffffu, ctl->gave_up)) {    // stopped: the copies that were started land first
@@ -445,11 +454,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             uint32_t d = tmem;
             int in_buf = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
-                if (!__all_sync(0xffffffffu, bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit))) break;
+                if (!warp_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) break;
                 tc_after();
                 if (elect_one()) {
-                    const uint32_t at = smem + stage * stage_bytes;
-                    mma_block<false, A_MN, B_MN>(d, operand<A_MN>(at), operand<B_MN>(at + kABytes), idesc, in_buf != 0);
+#pragma unroll
+                    for (int i = 0; i < DEPTH; ++i) {
+                        const uint32_t at = smem + stage * stage_bytes + i * block_bytes;
+                        mma_block<false, A_MN, B_MN>(d, operand<A_MN>(at), operand<B_MN>(at + kABytes), idesc, i || in_buf != 0);
+                    }
                     tc_commit(&ctl->empty[stage]);
                 }
                 __syncwarp();
@@ -669,7 +681,7 @@ __device__ __forceinline__ void finish_row(const LinearParams &p, float (&v)[F32
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
 // both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 1,024 values of the reduction) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
-template <bool F32, int ACT, bool A_MN, bool B_MN>
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
                                                                   const __grid_constant__ LinearParams p) {
@@ -681,9 +693,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int rows = actual_rows(p), row_tiles = (rows + 2 * kM - 1) / (2 * kM), col_tiles = p.m_tiles, tiles = row_tiles * col_tiles;
     if (pair >= tiles) return;                              // (both CTAs)
-    const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u, stage_bytes = kABytes + p.b_bytes;
+    const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u, block_bytes = kABytes + p.b_bytes, stage_bytes = DEPTH * block_bytes;
     const int half_n = p.tile_n >> 1;
-    const int piece = F32 ? kPiece : p.kb;                  // blocks of an accumulator
+    const int piece = F32 ? kPiece / DEPTH : p.kb;          // steps of an accumulator
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&ctl->full[s], 1);
@@ -723,22 +735,26 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             tile_place(t, row_tiles, col_tiles, rt, ct);
             const int r0 = rt * 2 * kM + (int)rank * kM, c0 = ct * p.tile_n + (int)rank * half_n;
             for (int kb = 0; kb < p.kb; ++kb) {
-                ok = __all_sync(0xffffffffu, bar_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit));
+                ok = warp_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit);
                 if (!ok) break;
                 if (elect_one()) {
-                    const uint32_t a = smem + stage * stage_bytes, b = a + kABytes;
                     if (rank == 0) bar_expect(&ctl->full[stage], 2u * stage_bytes);
                     const uint32_t bar = map_to_rank(smem_at(&ctl->full[stage]), 0);
-                    if (B_MN) {
-                        load_box_pair(a, &map_b, bar, r0, kb * kKb);
-                        load_box_pair(a + 8192, &map_b, bar, r0 + 64, kb * kKb);
-                    } else {
-                        load_box_pair(a, &map_b, bar, kb * kKb, r0);
+#pragma unroll
+                    for (int i = 0; i < DEPTH; ++i) {
+                        const uint32_t a = smem + stage * stage_bytes + i * block_bytes, b = a + kABytes;
+                        const int k = (kb * DEPTH + i) * kKb;
+                        if (B_MN) {
+                            load_box_pair(a, &map_b, bar, r0, k);
+                            load_box_pair(a + 8192, &map_b, bar, r0 + 64, k);
+                        } else {
+                            load_box_pair(a, &map_b, bar, k, r0);
+                        }
+                        if (A_MN)
+                            for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_a, bar, c0 + c, k);
+                        else
+                            load_box_pair(b, &map_a, bar, k, c0);
                     }
-                    if (A_MN)
-                        for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_a, bar, c0 + c, kb * kKb);
-                    else
-                        load_box_pair(b, &map_a, bar, kb * kKb, c0);
                 }
                 __syncwarp();
                 issued = min(issued + 1, p.stages);
@@ -767,18 +783,21 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs) {
                 for (int kb = 0; kb < p.kb && ok;) {
-                    ok = __all_sync(0xffffffffu, bar_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit));
+                    ok = warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit);
                     if (!ok) break;
                     tc_after();
                     const uint32_t d = tmem + buf * p.tile_n;
                     const int end = min(kb + piece, p.kb);
                     for (uint32_t more = 0; kb < end; ++kb, more = 1) {
-                        ok = __all_sync(0xffffffffu, bar_wait(&ctl->full[stage], phase, ctl, p.wait_limit));
+                        ok = warp_wait(&ctl->full[stage], phase, ctl, p.wait_limit);
                         if (!ok) break;
                         tc_after();
                         if (elect_one()) {
-                            const uint32_t at = smem + stage * stage_bytes;
-                            mma_block<true, B_MN, A_MN>(d, operand<B_MN>(at), operand<A_MN>(at + kABytes), idesc, more);
+#pragma unroll
+                            for (int i = 0; i < DEPTH; ++i) {
+                                const uint32_t at = smem + stage * stage_bytes + i * block_bytes;
+                                mma_block<true, B_MN, A_MN>(d, operand<B_MN>(at), operand<A_MN>(at + kABytes), idesc, i ? 1u : more);
+                            }
                             tc_commit_pair(&ctl->empty[stage]);
                         }
                         __syncwarp();
@@ -832,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     for (int i = 0; i < 16; ++i) sum[c + i] = __uint_as_float(r[i]);
                 }
                 for (int kb = 0; kb < p.kb && ok; kb += piece) {
-                    ok = __all_sync(0xffffffffu, bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit));
+                    ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                     tc_after();
 #pragma unroll
                     for (int c = 0; c < kMaxN / 2; c += 16)
@@ -858,7 +877,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         finish_row<true, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add && !begin, turn);
                     }
             } else {
-                ok = __all_sync(0xffffffffu, bar_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit));
+                ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                 tc_after();
 #pragma unroll 1
                 for (int c = 0; c < cols; c += 32) {
@@ -949,30 +968,38 @@ __global__ void __launch_bounds__(256) linear_bias_sum_kernel(const float *parti
 
 using LinearKernel = void (*)(CUtensorMap, CUtensorMap, LinearParams);
 
-// forward products in all their forms; gradients have none
-template <bool PAIR, bool F32, int ACT, bool A_MN, bool B_MN>
-constexpr LinearKernel kLinearKernel = PAIR ? &linear_pair_kernel<F32, ACT, A_MN, B_MN> : &linear_split_kernel<F32, ACT, A_MN, B_MN>;
+// forward products in all their forms; gradients have no activation and bfloat16 results
+template <bool PAIR, int DEPTH, bool F32, int ACT, bool A_MN, bool B_MN>
+constexpr LinearKernel kLinearKernel = PAIR ? &linear_pair_kernel<F32, ACT, A_MN, B_MN, DEPTH> : &linear_split_kernel<F32, ACT, A_MN, B_MN, DEPTH>;
 
-template <bool PAIR>
-LinearKernel linear_kernel(bool f32, int act, bool a_mn, bool b_mn) {
-    if (a_mn) return b_mn ? kLinearKernel<PAIR, false, FI_ACT_NONE, true, true> : kLinearKernel<PAIR, false, FI_ACT_NONE, true, false>;
+template <bool PAIR, int DEPTH, bool F32>
+LinearKernel forward_kernel(int act) {
     switch (act) {
-        case FI_ACT_RELU: return f32 ? kLinearKernel<PAIR, true, FI_ACT_RELU, false, false> : kLinearKernel<PAIR, false, FI_ACT_RELU, false, false>;
-        case FI_ACT_GELU: return f32 ? kLinearKernel<PAIR, true, FI_ACT_GELU, false, false> : kLinearKernel<PAIR, false, FI_ACT_GELU, false, false>;
-        case FI_ACT_GELU_TANH:
-            return f32 ? kLinearKernel<PAIR, true, FI_ACT_GELU_TANH, false, false> : kLinearKernel<PAIR, false, FI_ACT_GELU_TANH, false, false>;
-        case FI_ACT_SILU: return f32 ? kLinearKernel<PAIR, true, FI_ACT_SILU, false, false> : kLinearKernel<PAIR, false, FI_ACT_SILU, false, false>;
-        default: return f32 ? kLinearKernel<PAIR, true, FI_ACT_NONE, false, false> : kLinearKernel<PAIR, false, FI_ACT_NONE, false, false>;
+        case FI_ACT_RELU: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_RELU, false, false>;
+        case FI_ACT_GELU: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_GELU, false, false>;
+        case FI_ACT_GELU_TANH: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_GELU_TANH, false, false>;
+        case FI_ACT_SILU: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_SILU, false, false>;
+        default: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_NONE, false, false>;
     }
+}
+template <bool PAIR, int DEPTH>
+LinearKernel linear_kernel(bool f32, int act, bool a_mn, bool b_mn) {
+    if (a_mn) return b_mn ? kLinearKernel<PAIR, DEPTH, false, FI_ACT_NONE, true, true> : kLinearKernel<PAIR, DEPTH, false, FI_ACT_NONE, true, false>;
+    return f32 ? forward_kernel<PAIR, DEPTH, true>(act) : forward_kernel<PAIR, DEPTH, false>(act);
+}
+LinearKernel linear_kernel(bool pair, int depth, bool f32, int act, bool a_mn, bool b_mn) {
+    if (pair) return depth == 2 ? linear_kernel<true, 2>(f32, act, a_mn, b_mn) : linear_kernel<true, 1>(f32, act, a_mn, b_mn);
+    return depth == 2 ? linear_kernel<false, 2>(f32, act, a_mn, b_mn) : linear_kernel<false, 1>(f32, act, a_mn, b_mn);
 }
 
 struct DeviceFacts {
     std::atomic<int> sms{0};
+    int clusters[4];                                        // of 1, 2, 4, 8 CTAs that run at one time
 };
 DeviceFacts g_facts[kMaxDevices];
 
-// SMs of the current device; its kernels are set up at the first call
-fi_status_t device_facts(int *sms, const char *name) {
+// Facts of the current device; its kernels are set up at the first call
+fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e, name);
@@ -980,19 +1007,34 @@ fi_status_t device_facts(int *sms, const char *name) {
         set_error("%s: device ordinal %d", name, dev);
         return FI_ERR_UNSUPPORTED;
     }
-    *sms = g_facts[dev].sms.load(std::memory_order_acquire);
-    if (*sms) return FI_OK;
+    DeviceFacts &f = g_facts[dev];
+    *facts = &f;
+    if (f.sms.load(std::memory_order_acquire)) return FI_OK;
     int n = 0;
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     for (int form = 0; form < 12; ++form) {                 // of a product: type and activation, or one of two gradients
         const bool back = form >= 10, f32 = !back && form >= 5;
-        const LinearKernel both[2] = {linear_kernel<false>(f32, form % 5, back, form == 11), linear_kernel<true>(f32, form % 5, back, form == 11)};
-        for (int i = 0; i < 2 && e == cudaSuccess; ++i)
-            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(both[i]), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+        for (int i = 0; i < 4 && e == cudaSuccess; ++i)
+            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(linear_kernel(i & 1, 1 + (i >> 1), f32, form % 5, back, form == 11)),
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
+    }
+    f.clusters[0] = n;
+    for (int i = 1; i < 4 && e == cudaSuccess; ++i) {
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1u << i;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1u << i);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kSmemMost - kStaticMost;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&f.clusters[i], linear_kernel(i == 1, 1, false, FI_ACT_NONE, false, false), &cfg);
+        if (e == cudaSuccess && f.clusters[i] < 1) e = cudaErrorInvalidConfiguration;
     }
     if (e != cudaSuccess) return cuda_fail(e, name);
-    g_facts[dev].sms.store(n, std::memory_order_release);
-    *sms = n;
+    f.sms.store(n, std::memory_order_release);
     return FI_OK;
 }
 
@@ -1027,31 +1069,35 @@ fi_status_t operand_map(CUtensorMap *map, const Matrix &x, int box_rows, const c
 }
 
 // Which kernel, and its tiles.  Estimates in SM cycles: 16 x 256 x 256 products of a pair take 128 cycles (a CTA's 16 x 128 x 256 as
-// many), an SM gets about 56 bytes a cycle from L2, the device about 3,400 from memory.
+// many), an SM gets about 75 bytes a cycle from L2, the device about 3,400 from memory; the way out of a split tile goes
+// through another CTA.  (256 tokens 4,096 -> 4,096: pairs of 64 columns 20.5 us, 4 CTAs for 128 x 256 24.6; 128 tokens: 20.5 and, 4 CTAs for
+// 128 x 128, 18.4.)
 struct LinearPlan {
     bool pair;
     int tile_n, split;
     double cycles;
 };
 
-LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool f32, int size, int sms) {
+LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool f32, int size, const int *clusters) {
     LinearPlan best = {false, 16, 1, 1e30};
     const auto most = [](double a, double b) { return a > b ? a : b; };
     const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
     const double memory = ((double)m * kb * 128 + (double)n * kb * 128 + (double)m * n * size) / 3400.;
     for (int tile = 64; tile <= kMaxN; tile += 64) {          // (a warp takes 32 columns of a half at a time)
         if (a_mn && tile % 128) continue;
-        const double block = most(2. * tile, (128 + tile / 2) * 128 / 56.), rounds = (double)up(up(n, 2 * kM) * up(m, tile), sms / 2);
+        const double block = most(2. * tile, (128 + tile / 2) * 128 / 75.), rounds = (double)up(up(n, 2 * kM) * up(m, tile), clusters[1]);
         const double cycles = most(rounds * kb * block, memory) + 2500 + 20. * tile;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
     }
     for (int tile = 16; tile <= kMaxN; tile += 16) {
         if (tile > 16 && tile - 16 >= n) break;
-        for (int split = 1; split <= 8 && split <= kb; split *= 2) {
+        for (int i = 0; i < 4 && 1 << i <= kb; ++i) {
+            const int split = 1 << i;
             const long long blocks = up(kb, split);
             if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 1,024 values have an accumulator each
-            const double block = most(2. * tile, (128 + tile) * 128 / 56.), rounds = (double)up(up(m, kM) * up(n, tile) * split, sms);
-            const double cycles = most(rounds * (blocks * block + 2500 + 20. * tile), memory + 2500 + 20. * tile) + (split > 1 ? 1000 : 0);
+            const double block = most(2. * tile, (128 + tile) * 128 / 75.), rounds = (double)up(up(m, kM) * up(n, tile), clusters[i]);
+            const double end = split > 1 ? 4000 + 30. * tile : 2500 + 20. * tile;
+            const double cycles = most(rounds * (blocks * block + end), memory + end);
             if (cycles < best.cycles) best = {false, tile, split, cycles};
         }
     }
@@ -1060,13 +1106,17 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
 
 // D[n][m] = sum over k of A(m, k) B(n, k); `p` holds what becomes of the sums
 fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act, LinearParams p,
-                           int sms, cudaStream_t stream, const char *name) {
+                           const DeviceFacts &facts, cudaStream_t stream, const char *name) {
     p.m = (int)m;
     p.n = (int)n;
     p.kb = (int)((k + kKb - 1) / kKb);
-    const LinearPlan plan = plan_product(m, n, p.kb, a_mn, f32, f32 ? 4 : 2, sms);
+    const LinearPlan plan = plan_product(m, n, p.kb, a_mn, f32, f32 ? 4 : 2, facts.clusters);
+    // two blocks a stage where the products of one are over before the next is issued (430 cycles: 16 x 256 x 128 take 64)
+    const int depth = plan.tile_n <= 128 && p.kb > 1 ? 2 : 1, blocks = p.kb;
+    p.kb = (p.kb + depth - 1) / depth;
     p.tile_n = plan.tile_n;
     p.split = plan.split;
+    while (p.split > p.kb) p.split /= 2;
     // tiles: of a pair 256 output rows and tile_n columns, of a CTA 128 columns and tile_n rows; the operand of the tile_n ones is the second
     const bool second_mn = plan.pair ? a_mn : b_mn;
     const int mine = plan.pair ? p.tile_n / 2 : p.tile_n;                                   // of them that a CTA loads
@@ -1075,13 +1125,13 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     p.bufs = plan.pair ? 2 : 1;
     if (f32 && !plan.pair) {
         // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 1,024 at a time
-        const int room = 512 / p.tile_n, pieces = ((p.kb + p.split - 1) / p.split + kPiece - 1) / kPiece;
+        const int room = 512 / p.tile_n, pieces = ((blocks + p.split - 1) / p.split + depth + kPiece - 1) / kPiece;
         p.bufs = pieces < room ? pieces : room;
     }
     p.tmem_cols = 32;
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
     p.b_bytes = second_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
-    const int stage = kABytes + p.b_bytes, room = kSmemMost - kStaticMost - 1024 /* alignment */;
+    const int stage = depth * (kABytes + p.b_bytes), room = kSmemMost - kStaticMost - 1024 /* alignment */;
     const int part = plan.pair ? 0 : p.split * ((p.tile_n / 4 + p.split - 1) / p.split) * kM * 16;
     const bool apart = p.split > 1 && p.tile_n <= 64;
     p.stages = (room - (apart ? part : 0)) / stage;
@@ -1103,13 +1153,13 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     attr.val.clusterDim.x = plan.pair ? 2 : p.split;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(plan.pair ? 2 * (tiles < sms / 2 ? tiles : sms / 2) : tiles * p.split));
+    cfg.gridDim = dim3((unsigned)(plan.pair ? 2 * (tiles < facts.clusters[1] ? tiles : facts.clusters[1]) : tiles * p.split));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const LinearKernel kernel = plan.pair ? linear_kernel<true>(f32, act, a_mn, b_mn) : linear_kernel<false>(f32, act, a_mn, b_mn);
+    const LinearKernel kernel = linear_kernel(plan.pair, depth, f32, act, a_mn, b_mn);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, p);
     if (e != cudaSuccess) return cuda_fail(e, name);
     count_launch();
@@ -1181,8 +1231,8 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
         set_error("%s: rows of out, residual and preact must not overlap; pointers must be aligned to their types", name);
         return FI_ERR_INVALID_ARG;
     }
-    int sms = 0;
-    st = device_facts(&sms, name);
+    const DeviceFacts *facts = nullptr;
+    st = device_facts(&facts, name);
     if (st != FI_OK) return st;
     LinearParams p = {};
     p.bias = a->bias;
@@ -1200,7 +1250,7 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
     p.wide = wide(a->out, a->out_stride, out_rows, size) && wide(a->residual, a->residual_stride, out_rows, size) &&
              wide(a->preact, a->preact_stride, a->tokens, 2) && aligned16(a->bias);
     const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
-    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, a->activation, p, sms,
+    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, a->activation, p, *facts,
                           static_cast<cudaStream_t>(cuda_stream), name);
 }
 
@@ -1234,8 +1284,8 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         set_error("%s: rows of dx and dweight must not overlap; pointers must be aligned to their types", name);
         return FI_ERR_INVALID_ARG;
     }
-    int sms = 0;
-    st = device_facts(&sms, name);
+    const DeviceFacts *facts = nullptr;
+    st = device_facts(&facts, name);
     if (st != FI_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (a->tokens == 0) {                                   // sums over nothing
@@ -1264,7 +1314,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         p.ld_out = a->dx_stride;
         p.out_rows = a->tokens;
         const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride};
-        st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, p, sms, stream, name);
+        st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, p, *facts, stream, name);
         if (st != FI_OK) return st;
     }
     if (a->dweight) {
@@ -1273,7 +1323,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         p.ld_out = a->dweight_stride;
         p.out_rows = a->out_dim;
         const Matrix x = {a->x, a->tokens, a->in_dim, a->x_stride};
-        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, p, sms, stream, name);
+        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, p, *facts, stream, name);
         if (st != FI_OK) return st;
     }
     if (a->dbias) {
