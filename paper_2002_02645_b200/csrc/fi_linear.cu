@@ -21,6 +21,7 @@ constexpr int kM = 128;                   // output columns of a CTA (MMA rows)
 constexpr int kKb = 64;                   // reduction values of a block: 128 bytes, a line of the swizzle
 constexpr int kABytes = kM * kKb * 2;     // of a block
 constexpr int kMaxN = 256;                // output rows of a tile, at most
+constexpr int kMaxPairN32 = 192;          // of a pair's tile with float32 results, whose sums are in registers
 constexpr int kMaxStages = 12;
 constexpr int kPiece = 16;                // blocks of the reduction that are added up in one accumulator for float32 results
 constexpr int kEpiThreads = 256;          // warps 0..7: TMEM lanes 32 (w mod 4) ..; warp 8 loads, warp 9 issues the products
@@ -583,20 +584,23 @@ __device__ __forceinline__ uint4 shared_load4(uint32_t at) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
-// columns c .. of row `to` (negative: none) of a matrix with `cols` columns
+// columns c .. of row `to` (negative: none) of a matrix with `cols` columns: as the warp loads them, and turned to the threads' rows
 template <typename T>
-__device__ __forceinline__ void rows_in(const T *from, long long ld, int to, int c, int cols, uint32_t base, uint32_t (&w)[16]) {
+__device__ __forceinline__ void rows_load(const T *from, long long ld, int to, int c, int cols, uint32_t *w) {
     constexpr int kPieceCols = 16 / sizeof(T);
     const int lane = threadIdx.x & 31, col = c + (lane & 3) * kPieceCols;
-    uint4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int row = __shfl_sync(0xffffffffu, to, j * 8 + (lane >> 2));
-        v[j] = row >= 0 && col < cols ? *reinterpret_cast<const uint4 *>(from + row * ld + col) : make_uint4(0, 0, 0, 0);
+        const uint4 v = row >= 0 && col < cols ? *reinterpret_cast<const uint4 *>(from + row * ld + col) : make_uint4(0, 0, 0, 0);
+        w[4 * j] = v.x; w[4 * j + 1] = v.y; w[4 * j + 2] = v.z; w[4 * j + 3] = v.w;
     }
+}
+__device__ __forceinline__ void rows_turn(uint32_t base, uint32_t *w) {
+    const int lane = threadIdx.x & 31;
     __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) shared_store4(turn_at(base, j * 8 + (lane >> 2), lane & 3), v[j].x, v[j].y, v[j].z, v[j].w);
+    for (int j = 0; j < 4; ++j) shared_store4(turn_at(base, j * 8 + (lane >> 2), lane & 3), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -633,7 +637,10 @@ __device__ __forceinline__ void finish_row(const LinearParams &p, float (&v)[F32
     using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
     constexpr int N = F32 ? 16 : 32;
     uint32_t r[16];
-    if (add && p.wide) rows_in(static_cast<const T *>(p.residual), p.ld_res, to, c, p.m, base, r);
+    if (add && p.wide) {
+        rows_load(static_cast<const T *>(p.residual), p.ld_res, to, c, p.m, r);
+        rows_turn(base, r);
+    }
     if (bias) {
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
@@ -839,29 +846,21 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
             const uint32_t turn = smem_at(ctl->turn[warp]);
             const bool add = p.residual != nullptr;
             if constexpr (F32) {
-                // Without an activation the sum begins with the residual, whose way here is hidden behind the products then; only
-                // two accumulators of a tile can be ahead of the one that goes out.
-                float sum[kMaxN / 2];
-                const bool begin = add && ACT == FI_ACT_NONE && !p.preact && p.wide;
-#pragma unroll
-                for (int c = 0; c < kMaxN / 2; c += 16) {
-                    uint32_t r[16] = {};
-                    if (begin && c < cols) rows_in(static_cast<const float *>(p.residual), p.ld_res, to, c0 + c, p.m, turn, r);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[c + i] = __uint_as_float(r[i]);
-                }
+                float sum[kMaxPairN32 / 2] = {};
                 for (int kb = 0; kb < p.kb && ok; kb += piece) {
                     ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                     tc_after();
+                    // (a load from TMEM ahead of the sums)
+                    uint32_t v[2][16];
+                    tmem_load(at + buf * p.tile_n, v[0]);
 #pragma unroll
-                    for (int c = 0; c < kMaxN / 2; c += 16)
-                        if (c < cols) {
-                            uint32_t v[16];
-                            tmem_load(at + buf * p.tile_n + c, v);
-                            tmem_wait(v);
+                    for (int c = 0; c < kMaxPairN32 / 2; c += 16) {
+                        uint32_t (&now)[16] = v[c / 16 & 1], (&next)[16] = v[c / 16 + 1 & 1];
+                        tmem_wait(now);
+                        if (c + 16 < kMaxPairN32 / 2 && c + 16 < half_n) tmem_load(at + buf * p.tile_n + c + 16, next);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(v[i]);
-                        }
+                        for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(now[i]);
+                    }
                     tc_before();
                     __syncwarp();
                     if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), 0));
@@ -869,12 +868,12 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     if (buf == 0) buf_phase ^= 1;
                 }
 #pragma unroll
-                for (int c = 0; c < kMaxN / 2; c += 16)
+                for (int c = 0; c < kMaxPairN32 / 2; c += 16)
                     if (c < cols) {
                         float v[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) v[i] = sum[c + i];
-                        finish_row<true, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add && !begin, turn);
+                        finish_row<true, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add, turn);
                     }
             } else {
                 ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
@@ -1084,7 +1083,7 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
     const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
     const double memory = ((double)m * kb * 128 + (double)n * kb * 128 + (double)m * n * size) / 3400.;
     for (int tile = 64; tile <= kMaxN; tile += 64) {          // (a warp takes 32 columns of a half at a time)
-        if (a_mn && tile % 128) continue;
+        if ((a_mn && tile % 128) || (f32 && tile > kMaxPairN32)) continue;
         const double block = most(2. * tile, (128 + tile / 2) * 128 / 75.), rounds = (double)up(up(n, 2 * kM) * up(m, tile), clusters[1]);
         const double cycles = most(rounds * kb * block, memory) + 2500 + 20. * tile;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
