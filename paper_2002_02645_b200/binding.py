@@ -33,7 +33,7 @@ EXPORTS = ["fi_cache_create", "fi_cache_destroy", "fi_cache_insert", "fi_cache_s
            "fi_pages_create", "fi_pages_destroy", "fi_pages_extend", "fi_pages_release", "fi_head_norm_rope",
            "fi_head_norm_rope_backward", "fi_head_norm_rope_workspace", "fi_kv_create", "fi_kv_destroy", "fi_kv_append",
            "fi_kv_attend", "fi_kv_set_wait_limit", "fi_kv_poll_status", "fi_linear", "fi_linear_backward",
-           "fi_linear_backward_workspace", "fi_linear_poll_status", "fi_layer_norm", "fi_layer_norm_backward", "fi_layer_norm_workspace",
+           "fi_linear_backward_workspace", "fi_linear_poll_status", "fi_layer_norm", "fi_layer_norm_backward", "fi_layer_norm_workspace", "fi_layer_norm_poll_status",
            "fi_pages_fork", "fi_pages_free", "fi_pages_compact", "fi_pages_compact_workspace", "fi_kv_copy_pages",
            "fi_launch_count", "fi_last_error", "fi_status_string"]
 
@@ -214,6 +214,7 @@ def load_library(path: Optional[str] = None):
     lib.fi_layer_norm.argtypes = [ctypes.c_char_p, vp]                 # a packed fi_layer_norm_t
     lib.fi_layer_norm_backward.argtypes = [ctypes.c_char_p, vp]
     lib.fi_layer_norm_workspace.argtypes = [i32]
+    lib.fi_layer_norm_poll_status.argtypes = []
     lib.fi_layer_norm_workspace.restype = i64
     lib.fi_pages_fork.argtypes = [vp, ctypes.c_char_p, vp]             # a packed fi_pages_fork_t
     lib.fi_pages_free.argtypes = [vp, ctypes.c_char_p, vp]
@@ -1203,6 +1204,12 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
                             tokens, 0, dim, 1 if rms else 0, *kinds, eps)
     _on_device(index, lib.fi_layer_norm_backward, args)
     return dx, dw, db
+
+
+def layer_norm_poll_status(device: int = 0) -> None:
+    """fi_layer_norm_poll_status of a device: raises FI_ERR_TIMEOUT when a wait inside layer_norm_backward's kernel ran out there."""
+    with torch.cuda.device(device):
+        _check(load_library().fi_layer_norm_poll_status())
 
 
 class _LayerNorm(torch.autograd.Function):

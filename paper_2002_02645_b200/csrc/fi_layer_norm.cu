@@ -8,6 +8,7 @@
 // and r come again from x, which they read anyway.
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "fi_internal.cuh"
@@ -17,6 +18,8 @@ namespace {
 
 constexpr int kMaxDim = 16384;
 constexpr int kMaxPartials = 1024;     // CTAs of a backward pass, at most
+
+__device__ int32_t g_layer_norm_status;   // 1: a bounded wait ran out
 
 struct RowNormParams {
     const void *x, *dy;
@@ -283,8 +286,178 @@ __global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(c
     }
 }
 
-// Weight gradients from the CTAs' sums, 32 columns per CTA, always in the same order.
+// The same for long rows on 16-byte boundaries: rows come by bulk copies into a ring of stages in shared memory, several ahead of the ones
+// that are worked on, R rows a stage (of 4,096 values in bf16: 96 KB on their way per CTA, two CTAs per SM).  R rows together go
+// through the three sums over the CTA.  A stage is free again as soon as its values are in registers, which the first of these sums
+// shows, so the ring needs no barrier for that.
+constexpr int kMaxRing = 6;
+
+template <bool X32, bool Y32, int P, int R>
+__global__ void __launch_bounds__(P == 4 ? 512 : 256 * P, P == 4 ? 1 : 2 / P) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
+    constexpr int V = 8 * P;
+    __shared__ float s[4][32][2 * R];
+    __shared__ uint64_t full[kMaxRing];
+    extern __shared__ __align__(128) unsigned char ring[];
+    const Place<true, P> l = {(int)threadIdx.x, (int)blockDim.x, p.dim};
+    const int x_bytes = p.dim * (X32 ? 4 : 2), y_bytes = p.dim * (Y32 ? 4 : 2), row_bytes = x_bytes + y_bytes;
+    const long long steps = (p.tokens + R - 1) / R;
+    const auto address = [](const void *q) { return (uint32_t)__cvta_generic_to_shared(q); };
+    // rows step * R .. of both operands into a stage
+    const auto load = [&](long long step, int stage) {
+        const int rows = (int)min((long long)R, p.tokens - step * R);
+        const uint32_t bar = address(&full[stage]);
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(rows * row_bytes) : "memory");
+        for (int i = 0; i < rows; ++i) {
+            const long long row = step * R + i;
+            const uint32_t to = address(ring) + (stage * R + i) * row_bytes;
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+                         "l"(static_cast<const char *>(p.x) + row * p.x_stride * (X32 ? 4 : 2)), "r"(x_bytes), "r"(bar)
+                         : "memory");
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + x_bytes),
+                         "l"(static_cast<const char *>(p.dy) + row * p.dy_stride * (Y32 ? 4 : 2)), "r"(y_bytes), "r"(bar)
+                         : "memory");
+        }
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(address(&full[i])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        for (int i = 0; i < stages; ++i)
+            if (blockIdx.x + (long long)i * gridDim.x < steps) load(blockIdx.x + (long long)i * gridDim.x, i);
+    }
+    __syncthreads();
+    int slot = 0, stage = 0;
+    uint32_t phase = 0;
+    long long limit = 8000000000ll;                          // SM cycles (about 4 s); once it ran out, 0.01 s
+    float dw[V] = {}, db[V] = {};
+    // sums over the CTA of N values per row
+    const auto sums = [&](auto &v) {
+        constexpr int N = sizeof(v) / sizeof(float);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[slot][warp][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? s[slot][lane][i] : 0.f);
+        slot = (slot + 1) & 3;
+    };
+    for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
+        uint32_t there = 0;
+        for (long long t0 = clock64(); !there && clock64() - t0 < limit;)
+            asm volatile(
+                "{\n"
+                ".reg .pred q;\n"
+                "mbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2;\n"
+                "selp.u32 %0, 1, 0, q;\n"
+                "}\n"
+                : "=r"(there)
+                : "r"(address(&full[stage])), "r"(phase)
+                : "memory");
+        if (!there) {
+            limit = 20000000;
+            atomicOr(&g_layer_norm_status, 1);
+        }
+        const int rows = (int)min((long long)R, p.tokens - step * R);
+        float v[R][V], g[R][V], r[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                const bool here = i < rows && l.piece(q) < p.dim;
+                const unsigned char *const at = ring + (stage * R + i) * row_bytes;
+                Raw8<X32> rx = {};
+                Raw8<Y32> ry = {};
+                if (here) {
+                    const uint4 *const px = reinterpret_cast<const uint4 *>(at + l.piece(q) * (X32 ? 4 : 2));
+                    const uint4 *const py = reinterpret_cast<const uint4 *>(at + x_bytes + l.piece(q) * (Y32 ? 4 : 2));
+                    rx.w[0] = px[0];
+                    if constexpr (X32) rx.w[1] = px[1];
+                    ry.w[0] = py[0];
+                    if constexpr (Y32) ry.w[1] = py[1];
+                }
+                widen8<X32>(rx, v[i] + 8 * q);
+                widen8<Y32>(ry, g[i] + 8 * q);
+            }
+        float one[R] = {};
+        if (!p.rms) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) one[i] += v[i][e];
+            sums(one);
+        } else {
+            __syncthreads();
+        }
+        // everybody has the stage's values
+        if (threadIdx.x == 0 && step + (long long)stages * gridDim.x < steps) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            load(step + (long long)stages * gridDim.x, stage);
+        }
+        if (++stage == stages) {
+            stage = 0;
+            phase ^= 1;
+        }
+        float sq[R] = {};
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float mean = one[i] / (float)p.dim;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (!p.rms) v[i][e] = l.has(e) ? v[i][e] - mean : 0.f;
+                sq[i] = fmaf(v[i][e], v[i][e], sq[i]);
+            }
+        }
+        sums(sq);
+        float both[2 * R] = {};
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            r[i] = rsqrtf(fmaf(sq[i], p.inv_dim, p.eps));
+            if (i < rows)                                    // (a row that is not there has no values, but 0 / 0 for its n)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    v[i][e] *= r[i];                         // n
+                    dw[e] = fmaf(g[i][e], v[i][e], dw[e]);
+                    db[e] += g[i][e];
+                }
+        }
+        if (p.weight)
+            with_weight(l, p.weight, [&](int e, float w) {
+#pragma unroll
+                for (int i = 0; i < R; ++i) g[i][e] *= w;
+            });
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                both[2 * i] += g[i][e];
+                both[2 * i + 1] = fmaf(g[i][e], v[i][e], both[2 * i + 1]);
+            }
+        sums(both);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float less = p.rms ? 0.f : both[2 * i] * p.inv_dim, along = both[2 * i + 1] * p.inv_dim;
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[i][e] = r[i] * (g[i][e] - less - v[i][e] * along);
+            if (i < rows) store_row<X32>(l, p.out, (step * R + i) * p.out_stride, g[i]);
+        }
+    }
+    cudaTriggerProgrammaticLaunchCompletion();
+    if (!p.partial) return;
+    float *const to = p.partial + (long long)blockIdx.x * 2 * p.dim;
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+        if (l.piece(q) < p.dim) {
+            store8<true>(to, l.piece(q), dw + 8 * q);
+            store8<true>(to, p.dim + l.piece(q), db + 8 * q);
+        }
+}
+
+// Weight gradients from the CTAs' sums, 32 columns per CTA, always in the same order.  Launched while the CTAs that write them still run.
 __global__ void __launch_bounds__(1024) layer_norm_sum_kernel(const float *partial, int parts, int dim, float *dweight, float *dbias) {
+    cudaGridDependencySynchronize();
     __shared__ float s[32][33];
     float *const out = blockIdx.y ? dbias : dweight;
     if (!out) return;
@@ -326,6 +499,25 @@ int launch_backward(const RowNormParams &p, int sms, cudaStream_t stream) {
         if (p.dim <= 256) layer_norm_backward_kernel<X32, Y32, true, VEC, 1><<<grid, 256, smem, stream>>>(p);
         else if (p.dim <= 512) layer_norm_backward_kernel<X32, Y32, true, VEC, 2><<<grid, 256, smem, stream>>>(p);
         else layer_norm_backward_kernel<X32, Y32, true, VEC, 4><<<grid, 256, smem, stream>>>(p);
+        return (int)grid;
+    }
+    if constexpr (VEC) {
+        const int threads = p.dim <= 4096 ? 256 : 512, rows = p.dim <= 8192 ? 2 : 1, per_sm = p.dim <= 4096 ? 2 : 1;
+        const int stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2)), room = (per_sm == 2 ? 110 : 220) * 1024;
+        const int stages = room / stage < kMaxRing ? room / stage : kMaxRing;
+        const auto kernel = p.dim <= 2048   ? layer_norm_backward_ring_kernel<X32, Y32, 1, 2>
+                            : p.dim <= 8192 ? layer_norm_backward_ring_kernel<X32, Y32, 2, 2>
+                                            : layer_norm_backward_ring_kernel<X32, Y32, 4, 1>;
+        const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < kMaxPartials ? sms * per_sm : kMaxPartials;
+        const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
+        int device = 0;                                      // (set once for a device and kernel)
+        static std::atomic<unsigned long long> ready[3];
+        std::atomic<unsigned long long> &mine = ready[p.dim <= 2048 ? 0 : p.dim <= 8192 ? 1 : 2];
+        if (cudaGetDevice(&device) != cudaSuccess || !(mine.load(std::memory_order_acquire) >> (device & 63) & 1)) {
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+            mine.fetch_or(1ull << (device & 63), std::memory_order_release);
+        }
+        kernel<<<grid, threads, (size_t)stages * stage, stream>>>(p, stages);
         return (int)grid;
     }
     const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
@@ -448,10 +640,36 @@ fi_status_t fi_layer_norm_backward(const fi_layer_norm_t *a, void *cuda_stream) 
     });
     count_launch();
     if (p.partial) {
-        layer_norm_sum_kernel<<<dim3((a->dim + 31) / 32, 2), 1024, 0, stream>>>(p.partial, parts, a->dim, a->dweight, a->dbias);
+        cudaLaunchAttribute early;
+        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        early.val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((a->dim + 31) / 32, 2);
+        cfg.blockDim = dim3(1024);
+        cfg.stream = stream;
+        cfg.attrs = &early;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, layer_norm_sum_kernel, (const float *)p.partial, parts, (int)a->dim, a->dweight, a->dbias);
+        if (e != cudaSuccess) return cuda_fail(e, "fi_layer_norm_backward");
         count_launch();
     }
     return check_launch("fi_layer_norm_backward");
+}
+
+fi_status_t fi_layer_norm_poll_status(void) {
+    int32_t word = 0;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&word, g_layer_norm_status, sizeof word);
+    if (e == cudaSuccess && word) {
+        const int32_t zero = 0;
+        e = cudaMemcpyToSymbol(g_layer_norm_status, &zero, sizeof zero);
+    }
+    if (e != cudaSuccess) return cuda_fail(e, "fi_layer_norm_poll_status");
+    if (word) {
+        set_error("fi_layer_norm_backward: a wait inside a kernel ran out; its results are not valid");
+        return FI_ERR_TIMEOUT;
+    }
+    return FI_OK;
 }
 
 }  // extern "C"

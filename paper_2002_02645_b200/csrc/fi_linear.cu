@@ -1096,7 +1096,9 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
             if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 1,024 values have an accumulator each
             const double block = most(2. * tile, (128 + tile) * 128 / 75.), rounds = (double)up(up(m, kM) * up(n, tile), clusters[i]);
             const double end = split > 1 ? 4000 + 30. * tile : 2500 + 20. * tile;
-            const double cycles = most(rounds * (blocks * block + end), memory + end);
+            // columns' operand (weights) that L2 does not hold is read again for every tile of rows
+            const double again = (double)m * kb * 128 > 64e6 ? (up(n, tile) - 1) * ((double)m * kb * 128 / 3400.) : 0;
+            const double cycles = most(rounds * (blocks * block + end), memory + again + end);
             if (cycles < best.cycles) best = {false, tile, split, cycles};
         }
     }

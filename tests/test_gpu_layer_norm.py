@@ -93,6 +93,7 @@ def test_many_rows(tokens, dim, rms):
     x, w, b = rand(gen, tokens, dim).bfloat16(), 1 + 0.2 * rand(gen, dim), rand(gen, dim)
     within(fb.layer_norm(x, w, b, rms=rms), *forward(x, w, b, rms, 1e-5, torch.bfloat16))
     check_backward(x, w, rand(gen, tokens, dim).bfloat16(), rms, 1e-5, not rms)
+    fb.layer_norm_poll_status()
 
 
 @pytest.mark.parametrize("dim", [64, 1000, 4096])
