@@ -286,65 +286,95 @@ __global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(c
     }
 }
 
-// The same for long rows on 16-byte boundaries: rows come by bulk copies into a ring of stages in shared memory, several ahead of the ones
-// that are worked on, R rows a stage (of 4,096 values in bf16: 96 KB on their way per CTA, two CTAs per SM).  R rows together go
-// through the three sums over the CTA.  A stage is free again as soon as its values are in registers, which the first of these sums
-// shows, so the ring needs no barrier for that.
+// ---- long rows on 16-byte boundaries ----
+//
+// A CTA walks over the rows, R at a time.  A warp of its own brings them by bulk copies into a ring of stages in shared memory, several
+// ahead of the ones that are worked on (issued by a thread that works on them they hold up all the others: 100 us, not 50, for 16,384
+// rows of 4,096).  Weights stay in registers, of the gradients in shared memory: the ring leaves L1 too small for them.
+// Values are worked on in pairs.
 constexpr int kMaxRing = 6;
 
-template <bool X32, bool Y32, int P, int R>
-__global__ void __launch_bounds__(P == 4 ? 512 : 256 * P, P == 4 ? 1 : 2 / P) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
-    constexpr int V = 8 * P;
-    __shared__ float s[4][32][2 * R];
-    __shared__ uint64_t full[kMaxRing];
-    extern __shared__ __align__(128) unsigned char ring[];
-    const Place<true, P> l = {(int)threadIdx.x, (int)blockDim.x, p.dim};
-    const int x_bytes = p.dim * (X32 ? 4 : 2), y_bytes = p.dim * (Y32 ? 4 : 2), row_bytes = x_bytes + y_bytes;
-    const long long steps = (p.tokens + R - 1) / R;
-    const auto address = [](const void *q) { return (uint32_t)__cvta_generic_to_shared(q); };
-    // rows step * R .. of both operands into a stage
-    const auto load = [&](long long step, int stage) {
-        const int rows = (int)min((long long)R, p.tokens - step * R);
-        const uint32_t bar = address(&full[stage]);
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(rows * row_bytes) : "memory");
-        for (int i = 0; i < rows; ++i) {
-            const long long row = step * R + i;
-            const uint32_t to = address(ring) + (stage * R + i) * row_bytes;
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
-                         "l"(static_cast<const char *>(p.x) + row * p.x_stride * (X32 ? 4 : 2)), "r"(x_bytes), "r"(bar)
-                         : "memory");
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to + x_bytes),
-                         "l"(static_cast<const char *>(p.dy) + row * p.dy_stride * (Y32 ? 4 : 2)), "r"(y_bytes), "r"(bar)
-                         : "memory");
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t both(float a) { return pair(a, a); }
+__device__ __forceinline__ void unpair(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ float total(uint64_t p) {
+    float a, b;
+    unpair(p, a, b);
+    return a + b;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// 8 values as four pairs: from shared memory, from a weight in global memory (which stays in L1), and to global memory
+template <bool F32>
+__device__ __forceinline__ void pairs_in(const unsigned char *at, uint64_t *v) {
+    const uint4 a = *reinterpret_cast<const uint4 *>(at);
+    if constexpr (F32) {
+        const uint4 b = *reinterpret_cast<const uint4 *>(at + 16);
+        v[0] = pair(__uint_as_float(a.x), __uint_as_float(a.y));
+        v[1] = pair(__uint_as_float(a.z), __uint_as_float(a.w));
+        v[2] = pair(__uint_as_float(b.x), __uint_as_float(b.y));
+        v[3] = pair(__uint_as_float(b.z), __uint_as_float(b.w));
+    } else {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
+}
+__device__ __forceinline__ void pairs_weight(const float *p, uint64_t *v) {
+    float x[8];
+    load8_again(p, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
+}
+template <bool F32>
+__device__ __forceinline__ void pairs_out(void *base, long long at, const uint64_t *v) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpair(v[i], x[2 * i], x[2 * i + 1]);
+    store8<F32>(base, at, x);
+}
+
+struct RingBars {
+    uint64_t full[kMaxRing], empty[kMaxRing];
+};
+
+// The ring of a CTA, seen by one of its warps.  Waits have a limit in SM cycles (about 4 s); once one ran out, 0.01 s, and the status word
+// says that the results are not valid.
+struct Ring {
+    RingBars *bars;
+    uint32_t base, stage_bytes;
+    int stages;
+    int stage = 0;
+    uint32_t phase = 0;
+    long long limit = 8000000000ll;
+
+    static __device__ __forceinline__ uint32_t at(const uint64_t *bar) { return (uint32_t)__cvta_generic_to_shared(bar); }
+    __device__ __forceinline__ void set_up(int readers) const {
+        for (int i = 0; i < stages; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(at(bars->full + i)) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(at(bars->empty + i)), "r"(readers) : "memory");
         }
-    };
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < stages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(address(&full[i])) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        for (int i = 0; i < stages; ++i)
-            if (blockIdx.x + (long long)i * gridDim.x < steps) load(blockIdx.x + (long long)i * gridDim.x, i);
     }
-    __syncthreads();
-    int slot = 0, stage = 0;
-    uint32_t phase = 0;
-    long long limit = 8000000000ll;                          // SM cycles (about 4 s); once it ran out, 0.01 s
-    float dw[V] = {}, db[V] = {};
-    // sums over the CTA of N values per row
-    const auto sums = [&](auto &v) {
-        constexpr int N = sizeof(v) / sizeof(float);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) s[slot][warp][i] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? s[slot][lane][i] : 0.f);
-        slot = (slot + 1) & 3;
-    };
-    for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
+    __device__ __forceinline__ void wait(const uint64_t *bar, uint32_t parity) {
         uint32_t there = 0;
         for (long long t0 = clock64(); !there && clock64() - t0 < limit;)
             asm volatile(
@@ -354,94 +384,293 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 256 * P, P == 4 ? 1 : 2 / P) la
                 "selp.u32 %0, 1, 0, q;\n"
                 "}\n"
                 : "=r"(there)
-                : "r"(address(&full[stage])), "r"(phase)
+                : "r"(at(bar)), "r"(parity)
                 : "memory");
         if (!there) {
             limit = 20000000;
             atomicOr(&g_layer_norm_status, 1);
         }
-        const int rows = (int)min((long long)R, p.tokens - step * R);
-        float v[R][V], g[R][V], r[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int q = 0; q < P; ++q) {
-                const bool here = i < rows && l.piece(q) < p.dim;
-                const unsigned char *const at = ring + (stage * R + i) * row_bytes;
-                Raw8<X32> rx = {};
-                Raw8<Y32> ry = {};
-                if (here) {
-                    const uint4 *const px = reinterpret_cast<const uint4 *>(at + l.piece(q) * (X32 ? 4 : 2));
-                    const uint4 *const py = reinterpret_cast<const uint4 *>(at + x_bytes + l.piece(q) * (Y32 ? 4 : 2));
-                    rx.w[0] = px[0];
-                    if constexpr (X32) rx.w[1] = px[1];
-                    ry.w[0] = py[0];
-                    if constexpr (Y32) ry.w[1] = py[1];
-                }
-                widen8<X32>(rx, v[i] + 8 * q);
-                widen8<Y32>(ry, g[i] + 8 * q);
-            }
-        float one[R] = {};
-        if (!p.rms) {
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int e = 0; e < V; ++e) one[i] += v[i][e];
-            sums(one);
-        } else {
-            __syncthreads();
-        }
-        // everybody has the stage's values
-        if (threadIdx.x == 0 && step + (long long)stages * gridDim.x < steps) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            load(step + (long long)stages * gridDim.x, stage);
-        }
+    }
+    __device__ __forceinline__ void wait_full() { wait(bars->full + stage, phase); }
+    __device__ __forceinline__ void wait_empty() { wait(bars->empty + stage, phase ^ 1); }
+    __device__ __forceinline__ void next() {
         if (++stage == stages) {
             stage = 0;
             phase ^= 1;
         }
-        float sq[R] = {};
+    }
+    // the warp has the stage's values
+    __device__ __forceinline__ void release() {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(at(bars->empty + stage)) : "memory");
+        next();
+    }
+};
+__device__ __forceinline__ void ring_expect(uint32_t bar, int bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ring_copy(uint32_t to, const void *from, int bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Sums over the CTA of N values, always in the same order.  s: [4][N][16]; `slot`: one of four places in turn, so that one barrier is enough.
+// Of the working warps.
+template <int THREADS, int N>
+__device__ __forceinline__ void cta_sums(float (&v)[N], float *s, int &slot) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const float mean = one[i] / (float)p.dim;
+    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+    float *const here = s + slot * (N * 16);
+    if ((threadIdx.x & 31) == 0)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                if (!p.rms) v[i][e] = l.has(e) ? v[i][e] - mean : 0.f;
-                sq[i] = fmaf(v[i][e], v[i][e], sq[i]);
-            }
+        for (int i = 0; i < N; ++i) here[i * 16 + (threadIdx.x >> 5)] = v[i];
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; w += 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(here + i * 16 + w);
+            t += (x.x + x.y) + (x.z + x.w);
         }
-        sums(sq);
-        float both[2 * R] = {};
+        v[i] = t;
+    }
+    slot = (slot + 1) & 3;
+}
+
+// what a step reads, widened to pairs: row i of the stage, `skip` bytes behind its start
+template <bool F32, int P>
+__device__ __forceinline__ void stage_row(const Place<true, P> &l, const unsigned char *at, bool there, uint64_t (&v)[4 * P]) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            r[i] = rsqrtf(fmaf(sq[i], p.inv_dim, p.eps));
-            if (i < rows)                                    // (a row that is not there has no values, but 0 / 0 for its n)
+    for (int q = 0; q < P; ++q) {
+        if (there && l.piece(q) < l.dim) pairs_in<F32>(at + l.piece(q) * (F32 ? 4 : 2), v + 4 * q);
+        else
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[i][e] *= r[i];                         // n
-                    dw[e] = fmaf(g[i][e], v[i][e], dw[e]);
-                    db[e] += g[i][e];
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = 0;
+    }
+}
+
+// v becomes x - mean (0 where there is no value), from the sum of the row
+template <int P>
+__device__ __forceinline__ void less_mean(const Place<true, P> &l, uint64_t (&v)[4 * P], float sum) {
+    const uint64_t less = both(-(sum / (float)l.dim));
+#pragma unroll
+    for (int e = 0; e < 4 * P; ++e) v[e] = add2(v[e], less);
+    if (l.dim < l.group * 8 * P)                            // (not all threads have all pieces)
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = l.piece(q) < l.dim ? v[4 * q + e] : 0;
+}
+
+template <bool X32, bool Y32, bool RMS, int THREADS, int P, int R>
+__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_norm_ring_kernel(const RowNormParams p, int stages) {
+    __shared__ __align__(16) float s[4 * R * 16];
+    __shared__ RingBars bars;
+    extern __shared__ __align__(128) unsigned char ring[];
+    const Place<true, P> l = {(int)threadIdx.x, THREADS, p.dim};
+    const int row_bytes = p.dim * (X32 ? 4 : 2);
+    const long long tokens = actual_tokens(p), steps = (tokens + R - 1) / R;
+    const auto row_at = [&](long long token) {               // -1: none
+        if (token >= tokens) return -1ll;
+        const long long row = p.rows ? p.rows[token] : token;
+        return row >= 0 && row < p.x_rows ? row : -1ll;
+    };
+    Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages};
+    if (threadIdx.x == 0) r.set_up(THREADS / 32);
+    __syncthreads();
+    if (threadIdx.x >= THREADS) {
+        if (threadIdx.x == THREADS)
+            for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
+                long long row[R];
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    row[i] = row_at(step * R + i);
+                    n += row[i] >= 0;
                 }
-        }
-        if (p.weight)
-            with_weight(l, p.weight, [&](int e, float w) {
+                r.wait_empty();
+                const uint32_t bar = Ring::at(bars.full + r.stage), to = r.base + r.stage * r.stage_bytes;
+                ring_expect(bar, n * row_bytes);
 #pragma unroll
-                for (int i = 0; i < R; ++i) g[i][e] *= w;
-            });
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                both[2 * i] += g[i][e];
-                both[2 * i + 1] = fmaf(g[i][e], v[i][e], both[2 * i + 1]);
+                for (int i = 0; i < R; ++i)
+                    if (row[i] >= 0) ring_copy(to + i * row_bytes, static_cast<const char *>(p.x) + row[i] * p.x_stride * (X32 ? 4 : 2), row_bytes, bar);
+                r.next();
             }
-        sums(both);
+        return;
+    }
+    uint64_t w[4 * P], b[4 * P];
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w[4 * q + e] = both(1.f);
+            b[4 * q + e] = 0;
+        }
+        if (l.piece(q) < p.dim) {
+            if (p.weight) pairs_weight(p.weight + l.piece(q), w + 4 * q);
+            if (p.bias) pairs_weight(p.bias + l.piece(q), b + 4 * q);
+        }
+    }
+    int slot = 0;
+    for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
+        uint64_t v[R][4 * P];
+        bool there[R];
+        r.wait_full();
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const float less = p.rms ? 0.f : both[2 * i] * p.inv_dim, along = both[2 * i + 1] * p.inv_dim;
+            there[i] = row_at(step * R + i) >= 0;
+            stage_row<X32>(l, ring + (r.stage * R + i) * row_bytes, there[i], v[i]);
+        }
+        float sum[R];
 #pragma unroll
-            for (int e = 0; e < V; ++e) g[i][e] = r[i] * (g[i][e] - less - v[i][e] * along);
-            if (i < rows) store_row<X32>(l, p.out, (step * R + i) * p.out_stride, g[i]);
+        for (int i = 0; i < R; ++i) {
+            uint64_t t = 0;
+#pragma unroll
+            for (int e = 0; e < 4 * P; ++e) t = RMS ? fma2(v[i][e], v[i][e], t) : add2(t, v[i][e]);
+            sum[i] = total(t);
+        }
+        r.release();
+        cta_sums<THREADS>(sum, s, slot);
+        if (!RMS) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                less_mean(l, v[i], sum[i]);
+                uint64_t t = 0;
+#pragma unroll
+                for (int e = 0; e < 4 * P; ++e) t = fma2(v[i][e], v[i][e], t);
+                sum[i] = total(t);
+            }
+            cta_sums<THREADS>(sum, s, slot);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const uint64_t scale = both(rsqrtf(fmaf(sum[i], p.inv_dim, p.eps)));
+            if (there[i])
+#pragma unroll
+                for (int q = 0; q < P; ++q)
+                    if (l.piece(q) < p.dim) {
+                        uint64_t y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = fma2(mul2(v[i][4 * q + e], scale), w[4 * q + e], b[4 * q + e]);
+                        pairs_out<Y32>(p.out, (step * R + i) * p.out_stride + l.piece(q), y);
+                    }
+        }
+    }
+}
+
+// Gradients.  With d = x - mean and t = dy d the sums of a row are those of d^2, g = dy w and t w, all at once:
+//   along = mean(g n) = r mean(t w);  dw += r t;  dx = r g - r mean(g) - r along d r
+template <bool X32, bool Y32, bool RMS, int THREADS, int P, int R>
+__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
+    __shared__ __align__(16) float s1[4 * R * 16], s3[4 * 3 * R * 16];
+    __shared__ RingBars bars;
+    extern __shared__ __align__(128) unsigned char raw[];
+    float *const weight = reinterpret_cast<float *>(raw);    // [2][dim / 8][4]: halves of eight neighbours, apart for the banks' sake
+    unsigned char *const ring = raw + p.dim * 4;
+    const Place<true, P> l = {(int)threadIdx.x, THREADS, p.dim};
+    const int x_bytes = p.dim * (X32 ? 4 : 2), y_bytes = p.dim * (Y32 ? 4 : 2), row_bytes = x_bytes + y_bytes;
+    const long long steps = (p.tokens + R - 1) / R;
+    Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages};
+    if (threadIdx.x == 0) r.set_up(THREADS / 32);
+    for (int i = threadIdx.x; i < p.dim / 4; i += THREADS + 32)
+        *reinterpret_cast<float4 *>(weight + (i & 1) * (p.dim / 2) + (i >> 1) * 4) =
+            p.weight ? *reinterpret_cast<const float4 *>(p.weight + 4 * i) : make_float4(1.f, 1.f, 1.f, 1.f);
+    const auto weights = [&](int q, uint64_t (&w)[4]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float4 x = *reinterpret_cast<const float4 *>(weight + h * (p.dim / 2) + (l.t + q * THREADS) * 4);
+            w[2 * h] = pair(x.x, x.y);
+            w[2 * h + 1] = pair(x.z, x.w);
+        }
+    };
+    __syncthreads();
+    if (threadIdx.x >= THREADS) {
+        if (threadIdx.x == THREADS)
+            for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
+                const int rows = (int)min((long long)R, p.tokens - step * R);
+                r.wait_empty();
+                const uint32_t bar = Ring::at(bars.full + r.stage), to = r.base + r.stage * r.stage_bytes;
+                ring_expect(bar, rows * row_bytes);
+                for (int i = 0; i < rows; ++i) {
+                    const long long row = step * R + i;
+                    ring_copy(to + i * row_bytes, static_cast<const char *>(p.x) + row * p.x_stride * (X32 ? 4 : 2), x_bytes, bar);
+                    ring_copy(to + i * row_bytes + x_bytes, static_cast<const char *>(p.dy) + row * p.dy_stride * (Y32 ? 4 : 2), y_bytes, bar);
+                }
+                r.next();
+            }
+        return;
+    }
+    int slot = 0, slot3 = 0;
+    uint64_t dw[4 * P] = {}, db[4 * P] = {};
+    for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
+        r.wait_full();
+        const int rows = (int)min((long long)R, p.tokens - step * R);
+        uint64_t v[R][4 * P], g[R][4 * P];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const unsigned char *const at = ring + (r.stage * R + i) * row_bytes;
+            stage_row<X32>(l, at, i < rows, v[i]);
+            stage_row<Y32>(l, at + x_bytes, i < rows, g[i]);
+        }
+        r.release();
+        if (!RMS) {
+            float sum[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                uint64_t t = 0;
+#pragma unroll
+                for (int e = 0; e < 4 * P; ++e) t = add2(t, v[i][e]);
+                sum[i] = total(t);
+            }
+            cta_sums<THREADS>(sum, s1, slot);
+#pragma unroll
+            for (int i = 0; i < R; ++i) less_mean(l, v[i], sum[i]);
+        }
+        uint64_t sq[R] = {}, sg[R] = {}, st[R] = {};
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+            if (l.piece(q) < p.dim) {
+                uint64_t w[4];
+                weights(q, w);
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint64_t d = v[i][4 * q + e], dy = g[i][4 * q + e];
+                        db[4 * q + e] = add2(db[4 * q + e], dy);
+                        sq[i] = fma2(d, d, sq[i]);
+                        if (!RMS) sg[i] = fma2(dy, w[e], sg[i]);
+                        st[i] = fma2(mul2(dy, d), w[e], st[i]);
+                    }
+            }
+        float sums[3 * R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            sums[3 * i] = total(sq[i]);
+            sums[3 * i + 1] = total(sg[i]);
+            sums[3 * i + 2] = total(st[i]);
+        }
+        cta_sums<THREADS>(sums, s3, slot3);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (i >= rows) continue;                        // (a row that is not there: 1 / 0)
+            const float k = rsqrtf(fmaf(sums[3 * i], p.inv_dim, p.eps)), less = RMS ? 0.f : sums[3 * i + 1] * p.inv_dim;
+            const float along = sums[3 * i + 2] * p.inv_dim * k;
+            const uint64_t k2 = both(k), less2 = both(-less * k), along2 = both(-along * k * k);
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+                if (l.piece(q) < p.dim) {
+                    uint64_t w[4], out[4];
+                    weights(q, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint64_t d = v[i][4 * q + e], dy = g[i][4 * q + e];
+                        dw[4 * q + e] = fma2(mul2(dy, d), k2, dw[4 * q + e]);
+                        out[e] = fma2(d, along2, fma2(mul2(dy, w[e]), k2, less2));
+                    }
+                    pairs_out<X32>(p.out, (step * R + i) * p.out_stride + l.piece(q), out);
+                }
         }
     }
     cudaTriggerProgrammaticLaunchCompletion();
@@ -450,8 +679,8 @@ __global__ void __launch_bounds__(P == 4 ? 512 : 256 * P, P == 4 ? 1 : 2 / P) la
 #pragma unroll
     for (int q = 0; q < P; ++q)
         if (l.piece(q) < p.dim) {
-            store8<true>(to, l.piece(q), dw + 8 * q);
-            store8<true>(to, p.dim + l.piece(q), db + 8 * q);
+            pairs_out<true>(to, l.piece(q), dw + 4 * q);
+            pairs_out<true>(to, p.dim + l.piece(q), db + 4 * q);
         }
 }
 
@@ -477,8 +706,38 @@ __global__ void __launch_bounds__(1024) layer_norm_sum_kernel(const float *parti
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// once for a device and kernel
+template <typename Kernel>
+void ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
+    int device = 0;
+    if (cudaGetDevice(&device) == cudaSuccess && (done.load(std::memory_order_acquire) >> (device & 63) & 1)) return;
+    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    done.fetch_or(1ull << (device & 63), std::memory_order_release);
+}
+int ring_stages(int room, int stage) { return room / stage < kMaxRing ? room / stage : kMaxRing; }
+
 template <bool X32, bool Y32, bool VEC>
-void launch_forward(const RowNormParams &p, cudaStream_t stream) {
+void launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
+    if constexpr (VEC) {
+        // more rows than are worked on at one time: a few CTAs that stay, with the next rows on their way
+        if (p.dim > 1024 && p.tokens > 8ll * sms) {
+            static std::atomic<unsigned long long> done[4][2];
+            const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 256 : 512, rows = which == 3 ? 1 : 2;
+            const int per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * (X32 ? 4 : 2);
+            const auto kernel = p.rms ? (which == 0   ? layer_norm_ring_kernel<X32, Y32, true, 256, 1, 2>
+                                         : which == 1 ? layer_norm_ring_kernel<X32, Y32, true, 256, 2, 2>
+                                         : which == 2 ? layer_norm_ring_kernel<X32, Y32, true, 512, 2, 2>
+                                                      : layer_norm_ring_kernel<X32, Y32, true, 512, 4, 1>)
+                                      : (which == 0   ? layer_norm_ring_kernel<X32, Y32, false, 256, 1, 2>
+                                         : which == 1 ? layer_norm_ring_kernel<X32, Y32, false, 256, 2, 2>
+                                         : which == 2 ? layer_norm_ring_kernel<X32, Y32, false, 512, 2, 2>
+                                                      : layer_norm_ring_kernel<X32, Y32, false, 512, 4, 1>);
+            ring_ready(kernel, done[which][p.rms]);
+            const int stages = ring_stages((per_sm == 2 ? 110 : 216) * 1024, stage);
+            kernel<<<(unsigned)(sms * per_sm), threads + 32, (size_t)stages * stage, stream>>>(p, stages);
+            return;
+        }
+    }
     if (p.dim <= 1024) {
         const unsigned grid = (unsigned)((p.tokens + 3) / 4);
         if (p.dim <= 256) layer_norm_kernel<X32, Y32, true, VEC, 1><<<grid, 128, 0, stream>>>(p);
@@ -502,22 +761,23 @@ int launch_backward(const RowNormParams &p, int sms, cudaStream_t stream) {
         return (int)grid;
     }
     if constexpr (VEC) {
-        const int threads = p.dim <= 4096 ? 256 : 512, rows = p.dim <= 8192 ? 2 : 1, per_sm = p.dim <= 4096 ? 2 : 1;
-        const int stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2)), room = (per_sm == 2 ? 110 : 220) * 1024;
-        const int stages = room / stage < kMaxRing ? room / stage : kMaxRing;
-        const auto kernel = p.dim <= 2048   ? layer_norm_backward_ring_kernel<X32, Y32, 1, 2>
-                            : p.dim <= 8192 ? layer_norm_backward_ring_kernel<X32, Y32, 2, 2>
-                                            : layer_norm_backward_ring_kernel<X32, Y32, 4, 1>;
+        static std::atomic<unsigned long long> done[4][2];
+        const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 256 : 512;
+        // (two rows together as long as registers hold them)
+        const int rows = which == 0 ? 2 : 1, per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2));
+        const auto kernel = p.rms ? (which == 0   ? layer_norm_backward_ring_kernel<X32, Y32, true, 256, 1, 2>
+                                     : which == 1 ? layer_norm_backward_ring_kernel<X32, Y32, true, 256, 2, 1>
+                                     : which == 2 ? layer_norm_backward_ring_kernel<X32, Y32, true, 512, 2, 1>
+                                                  : layer_norm_backward_ring_kernel<X32, Y32, true, 512, 4, 1>)
+                                  : (which == 0   ? layer_norm_backward_ring_kernel<X32, Y32, false, 256, 1, 2>
+                                     : which == 1 ? layer_norm_backward_ring_kernel<X32, Y32, false, 256, 2, 1>
+                                     : which == 2 ? layer_norm_backward_ring_kernel<X32, Y32, false, 512, 2, 1>
+                                                  : layer_norm_backward_ring_kernel<X32, Y32, false, 512, 4, 1>);
+        const int stages = ring_stages((per_sm == 2 ? 108 : 216) * 1024 - p.dim * 4, stage);
         const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < kMaxPartials ? sms * per_sm : kMaxPartials;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
-        int device = 0;                                      // (set once for a device and kernel)
-        static std::atomic<unsigned long long> ready[3];
-        std::atomic<unsigned long long> &mine = ready[p.dim <= 2048 ? 0 : p.dim <= 8192 ? 1 : 2];
-        if (cudaGetDevice(&device) != cudaSuccess || !(mine.load(std::memory_order_acquire) >> (device & 63) & 1)) {
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
-            mine.fetch_or(1ull << (device & 63), std::memory_order_release);
-        }
-        kernel<<<grid, threads, (size_t)stages * stage, stream>>>(p, stages);
+        ring_ready(kernel, done[which][p.rms]);
+        kernel<<<grid, threads + 32, (size_t)stages * stage + p.dim * 4, stream>>>(p, stages);
         return (int)grid;
     }
     const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
@@ -615,10 +875,14 @@ int64_t fi_layer_norm_workspace(int32_t dim) { return dim < 1 || dim > kMaxDim ?
 fi_status_t fi_layer_norm(const fi_layer_norm_t *a, void *cuda_stream) {
     fi_status_t st = check_args(a, false, "fi_layer_norm");
     if (st != FI_OK || a->tokens == 0) return st;
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_fail(e, "fi_layer_norm");
     bool vec;
     const RowNormParams p = row_norm_params(a, false, &vec);
     with_types(a->x_dtype == FI_F32, a->y_dtype == FI_F32, vec, [&](auto x, auto y, auto v) {
-        launch_forward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, static_cast<cudaStream_t>(cuda_stream));
+        launch_forward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, sms, static_cast<cudaStream_t>(cuda_stream));
     });
     count_launch();
     return check_launch("fi_layer_norm");
