@@ -675,7 +675,7 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
  *   dz = dy act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over tokens of dz
  * dx, dweight bfloat16, dbias float; each nullable.  dz is rounded to bfloat16 for the products (2^-9 of each value), not for dbias;
  * without an activation it is dy and preact is not read.  dbias is summed in a fixed order.  `workspace`: fi_linear_backward_workspace
- * bytes of device memory on a 16-byte boundary, contents free, not shared by calls that overlap; may be null without activation and dbias.
+ * bytes of device memory on a 16-byte boundary, contents free, not shared by calls that overlap; may be null without an activation.
  *
  * fi_linear_poll_status: synchronises the current device; FI_ERR_TIMEOUT when a bounded wait inside a kernel of these calls ran out
  * there since the last poll (the word is cleared).

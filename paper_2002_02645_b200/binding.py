@@ -1095,7 +1095,7 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
         strides[3] = _check_rows(preact, "preact", index, torch.bfloat16, tokens, out_dim)
     dbias = torch.empty(out_dim, dtype=torch.float32, device=dy.device) if with_bias else None
     work = None
-    if kind or with_bias:
+    if kind:
         work = torch.empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind), dtype=torch.uint8, device=dy.device)
     args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
                                  *strides, tokens, in_dim, out_dim, kind)

@@ -752,7 +752,9 @@ void launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
 template <bool X32, bool Y32, bool VEC>
 int launch_backward(const RowNormParams &p, int sms, cudaStream_t stream) {
     if (p.dim <= 1024) {
-        const long long want = (p.tokens + 7) / 8, most = 2 * sms < kMaxPartials ? 2 * sms : kMaxPartials;
+        // no more CTAs than run at one time
+        const int per_sm = p.dim <= 256 ? 3 : p.dim <= 512 ? 2 : 1;
+        const long long want = (p.tokens + 7) / 8, most = per_sm * sms < kMaxPartials ? per_sm * sms : kMaxPartials;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
         const size_t smem = (size_t)8 * p.dim * sizeof(float);
         if (p.dim <= 256) layer_norm_backward_kernel<X32, Y32, true, VEC, 1><<<grid, 256, smem, stream>>>(p);

@@ -275,23 +275,32 @@ __device__ __forceinline__ void activate(float (&z)[N]) {
     }
 }
 
-// slope of the activation; where it has reached 0 or 1 it is taken as that, so that no product of infinities comes up
-__device__ __forceinline__ float slope(float z, int act) {
-    switch (act) {
+// z within -most .. most (NaN stays): past there every slope has reached 0 or 1, and no product of infinities comes up
+__device__ __forceinline__ float within(float z, float most) {
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(z), "f"(most));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(y), "f"(-most));
+    return y;
+}
+
+// slope of the activation
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+    switch (ACT) {
         case FI_ACT_RELU: return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
         case FI_ACT_GELU: {
-            if (fabsf(z) > 20.f) return z > 0.f ? 1.f : 0.f;
+            z = within(z, 20.f);
             float density;
             const float whole = normal_cdf(z, density);
             return fmaf(z * 0.39894228f, density, whole);
         }
         case FI_ACT_GELU_TANH: {
-            if (fabsf(z) > 20.f) return z > 0.f ? 1.f : 0.f;
-            const float s = logistic2(z * fmaf(kGeluTwice * kGeluTanh * kLog2e, z * z, kGeluTwice * kLog2e));
-            return fmaf(z * s * (1.f - s), kGeluTwice * fmaf(3.f * kGeluTanh * z, z, 1.f), s);
+            z = within(z, 20.f);
+            const float zz = z * z, s = logistic2(z * fmaf(kGeluTwice * kGeluTanh * kLog2e, zz, kGeluTwice * kLog2e));
+            return fmaf(z * fmaf(-s, s, s), fmaf(kGeluTwice * 3.f * kGeluTanh, zz, kGeluTwice), s);
         }
         case FI_ACT_SILU: {
-            if (fabsf(z) > 100.f) return z > 0.f ? 1.f : 0.f;
+            z = within(z, 100.f);
             const float s = logistic2(z * kLog2e);
             return s * fmaf(z, 1.f - s, 1.f);
         }
@@ -911,56 +920,69 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     }
 }
 
-// dz = dy act'(preact), and the CTA's sums of its columns (of dy itself without an activation: nothing is stored then).  A CTA takes 64
-// columns, eight per thread, and every gridDim.y-th group of 32 rows.
-constexpr int kSlopeThreads = 256, kSlopeCols = 64, kSlopeRows = kSlopeThreads * 8 / kSlopeCols;
+// dz = dy act'(preact), and dbias, the sums of its columns (of dy itself without an activation: nothing else is stored then).  A CTA takes 64
+// (where there are few, 16) columns, eight per thread, and its share of the rows, four of them on their way per thread; the CTAs of a cluster have the same
+// columns, whose sums the first one adds up in the order of their ranks.  Bound by the traffic.
+constexpr int kSlopeThreads = 256, kSlopeAhead = 4;
 
-__global__ void __launch_bounds__(kSlopeThreads) linear_slope_kernel(const __nv_bfloat16 *dy, long long ld_dy, const __nv_bfloat16 *z, long long ld_z,
-                                                                     __nv_bfloat16 *dz, float *partial, long long rows, int cols, int act) {
-    __shared__ float s[kSlopeRows][kSlopeCols + 1];
+template <int ACT, int kSlopeCols>
+__global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const __nv_bfloat16 *dy, long long ld_dy, const __nv_bfloat16 *z, long long ld_z,
+                                                                     __nv_bfloat16 *dz, float *dbias, long long rows, int cols) {
+    constexpr int kSlopeRows = kSlopeThreads * 8 / kSlopeCols;
+    __shared__ float s[kSlopeRows][kSlopeCols + 1], mine[kSlopeCols];
     const int part = threadIdx.x & (kSlopeCols / 8 - 1), group = threadIdx.x / (kSlopeCols / 8);
     const int c = blockIdx.x * kSlopeCols + part * 8;
     float sum[8] = {};
     if (c < cols)
-        for (long long r = (long long)blockIdx.y * kSlopeRows + group; r < rows; r += (long long)gridDim.y * kSlopeRows) {
-            const uint4 a = *reinterpret_cast<const uint4 *>(dy + r * ld_dy + c);
-            uint4 b = make_uint4(0, 0, 0, 0);
-            if (act != FI_ACT_NONE) b = *reinterpret_cast<const uint4 *>(z + r * ld_z + c);
-            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
-            uint32_t o[4];
+        for (long long r0 = (long long)blockIdx.y * kSlopeRows * kSlopeAhead + group; r0 < rows; r0 += (long long)gridDim.y * kSlopeRows * kSlopeAhead) {
+            uint4 a[kSlopeAhead], b[kSlopeAhead];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float lo = __uint_as_float(aw[i] << 16), hi = __uint_as_float(aw[i] & 0xffff0000u);
-                if (act != FI_ACT_NONE) {
-                    lo *= slope(__uint_as_float(bw[i] << 16), act);
-                    hi *= slope(__uint_as_float(bw[i] & 0xffff0000u), act);
+            for (int u = 0; u < kSlopeAhead; ++u) {
+                const long long r = r0 + u * kSlopeRows;
+                a[u] = b[u] = make_uint4(0, 0, 0, 0);
+                if (r < rows) {
+                    a[u] = __ldcs(reinterpret_cast<const uint4 *>(dy + r * ld_dy + c));
+                    if (ACT != FI_ACT_NONE) b[u] = __ldcs(reinterpret_cast<const uint4 *>(z + r * ld_z + c));
                 }
-                sum[2 * i] += lo;
-                sum[2 * i + 1] += hi;
-                const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                o[i] = reinterpret_cast<const uint32_t &>(h);
             }
-            if (act != FI_ACT_NONE) *reinterpret_cast<uint4 *>(dz + r * cols + c) = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+            for (int u = 0; u < kSlopeAhead; ++u) {
+                const long long r = r0 + u * kSlopeRows;
+                const uint32_t aw[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, bw[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+                uint32_t o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float lo = __uint_as_float(aw[i] << 16), hi = __uint_as_float(aw[i] & 0xffff0000u);
+                    lo *= slope<ACT>(__uint_as_float(bw[i] << 16));
+                    hi *= slope<ACT>(__uint_as_float(bw[i] & 0xffff0000u));
+                    sum[2 * i] += lo;
+                    sum[2 * i + 1] += hi;
+                    o[i] = pack2(lo, hi);
+                }
+                if (dz && r < rows) *reinterpret_cast<uint4 *>(dz + r * cols + c) = make_uint4(o[0], o[1], o[2], o[3]);
+            }
         }
-    if (!partial) return;
+    if (!dbias) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[group][part * 8 + i] = sum[i];
     __syncthreads();
-    if (threadIdx.x < kSlopeCols && blockIdx.x * kSlopeCols + threadIdx.x < (unsigned)cols) {
+    if (threadIdx.x < kSlopeCols) {
         float total = 0.f;
 #pragma unroll 8
         for (int g = 0; g < kSlopeRows; ++g) total += s[g][threadIdx.x];
-        partial[(long long)blockIdx.y * cols + blockIdx.x * kSlopeCols + threadIdx.x] = total;
+        mine[threadIdx.x] = total;
     }
-}
-
-// dbias from the CTAs' sums, always in the same order
-__global__ void __launch_bounds__(256) linear_bias_sum_kernel(const float *partial, int parts, int cols, float *dbias) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
-    float sum = 0.f;
-    for (int i = 0; i < parts; ++i) sum += partial[(long long)i * cols + c];
-    dbias[c] = sum;
+    cluster_sync();
+    if (blockIdx.y == 0 && threadIdx.x < kSlopeCols && blockIdx.x * kSlopeCols + threadIdx.x < (unsigned)cols) {
+        float total = 0.f;
+        for (unsigned i = 0; i < gridDim.y; ++i) {
+            float v;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(map_to_rank(smem_at(mine + threadIdx.x), i)) : "memory");
+            total += v;
+        }
+        dbias[blockIdx.x * kSlopeCols + threadIdx.x] = total;
+    }
+    cluster_sync();                                         // the first CTA has read the others' sums
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -1186,13 +1208,22 @@ bool tma_rows(const void *p, long long rows, long long dim, long long ld) {
     return aligned16(p) && (rows <= 1 || (ld % 8 == 0 && ld >= dim && ld < (1ll << 38)));
 }
 
-long long round256(long long v) { return (v + 255) / 256 * 256; }
+// CTAs of a cluster, which share the rows of `width` columns: up to eight, as many as run at one time (4,095 x 8,192 behind silu: 46 us with
+// 1,024 CTAs, 592 of which run together)
+int slope_parts(long long tokens, int out_dim, int width, int sms) {
+    const long long columns = (out_dim + width - 1) / width;
+    int parts = 1;
+    while (parts < 8 && tokens > (long long)parts * (kSlopeThreads * 8 / width) && columns * parts * 2 <= 4ll * sms) parts *= 2;
+    return parts;
+}
 
-int slope_parts(long long tokens, int out_dim) {
-    const long long columns = (out_dim + kSlopeCols - 1) / kSlopeCols, groups = (tokens + kSlopeRows - 1) / kSlopeRows;
-    long long parts = (8 * 148 + columns - 1) / columns;
-    if (parts > (groups + 3) / 4) parts = (groups + 3) / 4;
-    return parts < 1 ? 1 : parts > 256 ? 256 : (int)parts;
+template <int WIDTH>
+auto slope_kernel(int act) {
+    return act == FI_ACT_RELU        ? linear_slope_kernel<FI_ACT_RELU, WIDTH>
+           : act == FI_ACT_GELU      ? linear_slope_kernel<FI_ACT_GELU, WIDTH>
+           : act == FI_ACT_GELU_TANH ? linear_slope_kernel<FI_ACT_GELU_TANH, WIDTH>
+           : act == FI_ACT_SILU      ? linear_slope_kernel<FI_ACT_SILU, WIDTH>
+                                     : linear_slope_kernel<FI_ACT_NONE, WIDTH>;
 }
 
 }  // namespace
@@ -1257,7 +1288,7 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
 
 int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation) {
     if (tokens < 0 || tokens > 2147483647ll || out_dim < 8) return 0;
-    return round256((int64_t)slope_parts(tokens, out_dim) * out_dim * 4) + (activation != FI_ACT_NONE ? round256(tokens * out_dim * 2) : 0);
+    return activation != FI_ACT_NONE ? (tokens * out_dim * 2 + 255) / 256 * 256 : 0;
 }
 
 fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream) {
@@ -1270,7 +1301,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     if (st != FI_OK) return st;
     const bool slopes = a->activation != FI_ACT_NONE;
     if ((a->tokens > 0 && (!a->dy || (slopes && !a->preact) || (a->dx && !a->weight) || (a->dweight && !a->x))) ||
-        ((slopes || a->dbias) && !a->workspace)) {
+        (slopes && (a->dx || a->dweight) && a->tokens > 0 && !a->workspace)) {
         set_error("%s: null pointer", name);
         return FI_ERR_INVALID_ARG;
     }
@@ -1295,13 +1326,24 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, (size_t)a->out_dim * 4, stream);
         return e == cudaSuccess ? FI_OK : cuda_fail(e, name);
     }
-    const int parts = slope_parts(a->tokens, a->out_dim);
-    float *const partial = a->dbias ? static_cast<float *>(a->workspace) : nullptr;
-    __nv_bfloat16 *const dz = slopes ? reinterpret_cast<__nv_bfloat16 *>(static_cast<char *>(a->workspace) + round256((long long)parts * a->out_dim * 4)) : nullptr;
-    if ((slopes && (a->dx || a->dweight)) || a->dbias) {
-        linear_slope_kernel<<<dim3((a->out_dim + kSlopeCols - 1) / kSlopeCols, parts), kSlopeThreads, 0, stream>>>(
-            static_cast<const __nv_bfloat16 *>(a->dy), a->dy_stride, static_cast<const __nv_bfloat16 *>(a->preact), a->preact_stride, dz, partial, a->tokens,
-            a->out_dim, a->activation);
+    __nv_bfloat16 *const dz = slopes && (a->dx || a->dweight) ? static_cast<__nv_bfloat16 *>(a->workspace) : nullptr;
+    if (dz || a->dbias) {
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = attr.val.clusterDim.z = 1;
+        const int width = a->out_dim <= 64 * 16 && a->tokens >= 1024 ? 16 : 64;
+        attr.val.clusterDim.y = slope_parts(a->tokens, a->out_dim, width, facts->clusters[0]);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((a->out_dim + width - 1) / width, attr.val.clusterDim.y);
+        cfg.blockDim = dim3(kSlopeThreads);
+        cfg.stream = stream;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        const auto kernel = width == 16 ? slope_kernel<16>(a->activation) : slope_kernel<64>(a->activation);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<const __nv_bfloat16 *>(a->dy), (long long)a->dy_stride,
+                                                 static_cast<const __nv_bfloat16 *>(a->preact), (long long)a->preact_stride, dz, a->dbias,
+                                                 (long long)a->tokens, (int)a->out_dim);
+        if (e != cudaSuccess) return cuda_fail(e, name);
         count_launch();
         st = check_launch(name);
         if (st != FI_OK) return st;
@@ -1326,11 +1368,6 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         const Matrix x = {a->x, a->tokens, a->in_dim, a->x_stride};
         st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, p, *facts, stream, name);
         if (st != FI_OK) return st;
-    }
-    if (a->dbias) {
-        linear_bias_sum_kernel<<<(a->out_dim + 255) / 256, 256, 0, stream>>>(partial, parts, a->out_dim, a->dbias);
-        count_launch();
-        st = check_launch(name);
     }
     return st;
 }
