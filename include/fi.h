@@ -598,7 +598,7 @@ fi_status_t fi_kv_poll_status(fi_kv_t *kv);
  *   in this stream before anything is stored for the new rows or read from them.  granted [batch_max]: 1, or 0 for the refused and those past
  *   the batch count.  block_table and shared are written in place; lens_out / free_count_out as in fi_pages_extend.
  * fi_pages_free: the listed rows give up their pages and their lengths become 0.  Pages without another owner go behind the free stack, in
- * order of their numbers.  A row must not be listed twice.  num_pages <= 4194304.
+ * order of their numbers.  A row must not be listed twice.  num_pages <= 1048576.
  * fi_pages_compact: the pages in use move to the low end of the pool: those at or above the number of pages in use, in order, to the free
  * places below it, in order.  copies [max_copies x 3] as above (whole pages), max_copies >= num_pages / 2, moves [1] their number; entries
  * past it are (-1, -1, 0).  Rewritten in place: block_table (entries of pages in use), shared, and the free stack, lowest page on top.  Every

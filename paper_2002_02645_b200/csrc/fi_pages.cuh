@@ -7,12 +7,12 @@ struct fi_pages {
     fi_pages_config_t cfg;
     int sm_count;
     uint32_t *ticket;   // [1] CTAs of the running call that are done; the last one puts it back to 0
-    int32_t *segments;  // [kPageSegments] fi_pages_free: pages of each 1,024 that lost their last owner; 0 between calls
+    int32_t *segments;  // [kPageSegments] fi_pages_free: pages of each 256 that lost their last owner; 0 between calls
 };
 
 namespace fi {
 
-constexpr int kPageSegments = 4096;   // of 1,024 pages each
+constexpr int kPageSegments = 4096, kSegmentShift = 8;   // of 256 pages each
 
 cudaError_t prepare_pages_share();    // one-time set-up of the kernels of fi_pages_share.cu on the current device
 

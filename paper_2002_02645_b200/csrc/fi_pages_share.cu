@@ -8,6 +8,12 @@
 namespace fi {
 namespace {
 
+// see launch_early
+__device__ __forceinline__ void in_turn() {
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+}
+
 // last i in [0, n) with first[i] <= x, for non-decreasing first[] with first[0] <= x
 __device__ __forceinline__ int find_last64(const long long *first, int n, long long x) {
     int lo = 0, hi = n - 1;
@@ -25,6 +31,7 @@ __global__ void __launch_bounds__(kPageThreads) pages_fork_kernel(const fi_pages
     extern __shared__ long long s_cu[];                       // first full page of each request, all laid end to end
     int *const s_src = reinterpret_cast<int *>(s_cu + a.batch_max), *const s_dst = s_src + a.batch_max;
     __shared__ int s_taken;
+    in_turn();
     if (threadIdx.x == 0) s_taken = 0;
     LensCopy copy;
     copy.get(a.lens, a.lens_out, a.rows);
@@ -109,13 +116,14 @@ __global__ void __launch_bounds__(kPageThreads) pages_fork_kernel(const fi_pages
     if (threadIdx.x == 0) *a.free_count_out = free_count - s_taken;
 }
 
-// Every listed page loses an owner; one that had no other goes below 0 and is counted in its segment of 1,024 pages.  The last CTA then
+// Every listed page loses an owner; one that had no other goes below 0 and is counted in its segment of 256 pages.  The last CTA then
 // takes the segments in order (a warp each), which puts the free pages in order of their numbers whatever the order of the atomics.
 __global__ void __launch_bounds__(kPageThreads) pages_free_kernel(const fi_pages_free_t a, int page_shift, int max_blocks, uint32_t *ticket,
                                                                   int32_t *segments) {
     extern __shared__ long long s_cu[];
     int *const s_row = reinterpret_cast<int *>(s_cu + a.batch_max);
     __shared__ int s_base[kPageSegments];
+    in_turn();
     LensCopy copy;
     copy.get(a.lens, a.lens_out, a.rows);
     const int n = actual_count(a.batch_count, a.batch_max);
@@ -148,12 +156,12 @@ __global__ void __launch_bounds__(kPageThreads) pages_free_kernel(const fi_pages
     for (long long p = (long long)blockIdx.x * blockDim.x + threadIdx.x; p < pages; p += (long long)gridDim.x * blockDim.x) {
         const int i = find_last64(s_cu, n, p);
         const int page = a.block_table[(long long)s_row[i] * a.table_ld + (p - s_cu[i])];
-        if (page >= 0 && page < a.num_pages && atomicSub(a.shared + page, 1) == 0) atomicAdd(segments + (page >> 10), 1);
+        if (page >= 0 && page < a.num_pages && atomicSub(a.shared + page, 1) == 0) atomicAdd(segments + (page >> kSegmentShift), 1);
     }
     if (!last_cta(ticket)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int count = (a.num_pages + 1023) >> 10;
-    // each thread four neighbouring segments (kPageSegments / kPageThreads), whatever the number of threads
+    const int count = (a.num_pages + (1 << kSegmentShift) - 1) >> kSegmentShift;
+    // each thread four neighbouring segments at a time
     long long total = 0;
     for (int s0 = 0; s0 < count; s0 += 4 * blockDim.x) {
         int here[4];
@@ -180,25 +188,22 @@ __global__ void __launch_bounds__(kPageThreads) pages_free_kernel(const fi_pages
     for (int s = warp; s < count; s += warps) {
         long long at = s_base[s];
         if (at < 0) continue;
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-            int v[8];
+        int v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int page = s * 1024 + c * 256 + e * 32 + lane;
-                v[e] = page < a.num_pages ? __ldcg(a.shared + page) : 0;
-            }
+        for (int e = 0; e < 8; ++e) {
+            const int page = (s << kSegmentShift) + e * 32 + lane;
+            v[e] = page < a.num_pages ? __ldcg(a.shared + page) : 0;
+        }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int page = s * 1024 + c * 256 + e * 32 + lane;
-                const unsigned gone = __ballot_sync(0xffffffffu, v[e] < 0);
-                if (v[e] < 0) {
-                    const long long to = free_count + at + __popc(gone & ((1u << lane) - 1));
-                    if (to < a.num_pages) a.free_pages[to] = page;       // (more pages than there are: a stack that was not one)
-                    a.shared[page] = 0;
-                }
-                at += __popc(gone);
+        for (int e = 0; e < 8; ++e) {
+            const int page = (s << kSegmentShift) + e * 32 + lane;
+            const unsigned gone = __ballot_sync(0xffffffffu, v[e] < 0);
+            if (v[e] < 0) {
+                const long long to = free_count + at + __popc(gone & ((1u << lane) - 1));
+                if (to < a.num_pages) a.free_pages[to] = page;           // (more pages than there are: a stack that was not one)
+                a.shared[page] = 0;
             }
+            at += __popc(gone);
         }
     }
     for (int i = threadIdx.x; i < n; i += blockDim.x)
@@ -237,6 +242,7 @@ __device__ __forceinline__ void cluster_barrier() {
 // Used pages at or above the number of used pages, in order, get the free places below it, in order.  One cluster takes all steps: bits
 // of the free pages, their number, ranks, moves; then the free stack is rewritten, lowest number on top.
 __global__ void __cluster_dims__(kCompactCtas, 1, 1) __launch_bounds__(kPageThreads) pages_compact_kernel(const fi_pages_compact_t a, int page_size) {
+    in_turn();
     const CompactSpace c = compact_space(a.workspace, a.num_pages);
     const int threads = kCompactCtas * kPageThreads, tid = blockIdx.x * kPageThreads + threadIdx.x;
     __shared__ long long s_counts;
@@ -318,6 +324,7 @@ __global__ void __cluster_dims__(kCompactCtas, 1, 1) __launch_bounds__(kPageThre
 
 // The new names of the pages that moved, in the rows' entries.
 __global__ void __launch_bounds__(256) pages_rename_kernel(const fi_pages_compact_t a, int page_shift, int max_blocks) {
+    in_turn();
     const CompactSpace c = compact_space(a.workspace, a.num_pages);
     const int used = *c.used;
     for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -338,39 +345,71 @@ struct CopyPools {
     int32_t *status;
 };
 
-// A warp per page, head and kind (keys, values): its codes in pieces of 16 bytes, four on the way per lane, and its pairs.
+// A warp per page and head: codes of keys and values in pieces of 16 bytes, 4 + 4 on the way per lane, and their pairs beside them.
 __global__ void __launch_bounds__(256) kv_copy_pages_kernel(const CopyPools p, const int32_t *copies, const int32_t *count_dev, int most) {
+    in_turn();
     const int n = actual_count(count_dev, most), lane = threadIdx.x & 31;
-    const long long units = (long long)n * p.heads * 2, step = (long long)gridDim.x * 8;
+    const long long units = (long long)n * p.heads, step = (long long)gridDim.x * 8;
     for (long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += step) {
-        const long long i = u / (p.heads * 2);
-        const int rest = (int)(u - i * (p.heads * 2)), head = rest >> 1, kind = rest & 1;
+        const long long i = u / p.heads;
+        const int head = (int)(u - i * p.heads);
         const int src = copies[3 * i], dst = copies[3 * i + 1], tokens = min(copies[3 * i + 2], p.page_size);
         if (src < 0 || tokens <= 0) continue;
         if (src >= p.num_pages || dst < 0 || dst >= p.num_pages) {
             if (lane == 0) atomicOr(p.status, 2);
             continue;
         }
-        const unsigned char *const from = p.codes[kind] + src * p.ps + head * p.hs;
-        unsigned char *const to = p.codes[kind] + dst * p.ps + head * p.hs;
+        const long long from = src * p.ps + head * p.hs, to = dst * p.ps + head * p.hs;
+        const long long mfrom = src * p.mps + head * p.mhs, mto = dst * p.mps + head * p.mhs;
         const int pieces = tokens * p.pieces;
+        uint32_t m[2];
+        const bool first = lane < tokens;
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind)
+            if (first) m[kind] = p.meta[kind][mfrom + lane * p.mts];
         for (int q0 = lane; q0 < pieces; q0 += 128) {
-            uint4 v[4];
+            uint4 v[2][4];
             long long at[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int q = q0 + 32 * e, token = q / p.pieces;
                 at[e] = token * p.ts + (q - token * p.pieces) * 16ll;
-                if (q < pieces) v[e] = *reinterpret_cast<const uint4 *>(from + at[e]);
+                if (q < pieces) {
+                    v[0][e] = *reinterpret_cast<const uint4 *>(p.codes[0] + from + at[e]);
+                    v[1][e] = *reinterpret_cast<const uint4 *>(p.codes[1] + from + at[e]);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (q0 + 32 * e < pieces) *reinterpret_cast<uint4 *>(to + at[e]) = v[e];
+                if (q0 + 32 * e < pieces) {
+                    *reinterpret_cast<uint4 *>(p.codes[0] + to + at[e]) = v[0][e];
+                    *reinterpret_cast<uint4 *>(p.codes[1] + to + at[e]) = v[1][e];
+                }
         }
-        const uint32_t *const mf = p.meta[kind] + src * p.mps + head * p.mhs;
-        uint32_t *const mt = p.meta[kind] + dst * p.mps + head * p.mhs;
-        for (int t = lane; t < tokens; t += 32) mt[t * p.mts] = mf[t * p.mts];
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            if (first) p.meta[kind][mto + lane * p.mts] = m[kind];
+            for (int t = lane + 32; t < tokens; t += 32) p.meta[kind][mto + t * p.mts] = p.meta[kind][mfrom + t * p.mts];
+        }
     }
+}
+
+// A launch that may begin while the kernel before it in the stream still runs (a small kernel's launch takes as long as the kernel): every
+// kernel here waits for that one before it reads or writes anything, and lets the next one begin at once.
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), int grid, int threads, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
 
 int shift_of(int page_size) {
@@ -409,13 +448,13 @@ fi_status_t fi_pages_fork(fi_pages_t *p, const fi_pages_fork_t *a, void *cuda_st
     }
     DeviceGuard guard(p->cfg.device);
     if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_fork");
-    long long grid = (long long)a->batch_max * p->cfg.max_blocks / 4096;       // an upper bound of the pages
+    // an upper bound of the pages, a thread each where the sums over the requests are cheap (64 forks of 48 pages: 14.5 us in one CTA)
+    const int threads = a->batch_max <= 256 ? 256 : kPageThreads;
+    long long grid = (long long)a->batch_max * p->cfg.max_blocks / (a->batch_max <= 256 ? 512 : 4096);
     grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
-    const int threads = a->batch_max <= 256 && a->rows <= 1024 && grid == 1 ? 256 : kPageThreads;
-    pages_fork_kernel<<<(int)grid, threads, (size_t)a->batch_max * 16, static_cast<cudaStream_t>(cuda_stream)>>>(*a, shift_of(p->cfg.page_size),
-                                                                                                                p->cfg.max_blocks, p->ticket);
-    count_launch();
-    return check_launch("fi_pages_fork");
+    const cudaError_t e = launch_early(pages_fork_kernel, (int)grid, threads, (size_t)a->batch_max * 16, static_cast<cudaStream_t>(cuda_stream), *a,
+                                       shift_of(p->cfg.page_size), p->cfg.max_blocks, p->ticket);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_pages_fork");
 }
 
 fi_status_t fi_pages_free(fi_pages_t *p, const fi_pages_free_t *a, void *cuda_stream) {
@@ -423,10 +462,10 @@ fi_status_t fi_pages_free(fi_pages_t *p, const fi_pages_free_t *a, void *cuda_st
         set_error("fi_pages_free: null argument");
         return FI_ERR_INVALID_ARG;
     }
-    if (a->batch_max < 0 || a->batch_max > p->cfg.max_batch || a->rows < 0 || a->num_pages < 0 || a->num_pages > kPageSegments * 1024 ||
+    if (a->batch_max < 0 || a->batch_max > p->cfg.max_batch || a->rows < 0 || a->num_pages < 0 || a->num_pages > kPageSegments << kSegmentShift ||
         a->table_ld < p->cfg.max_blocks) {
         set_error("fi_pages_free: batch %d outside 0..%d, a negative size, more than %d pages, or table_ld below max_blocks", a->batch_max,
-                  p->cfg.max_batch, kPageSegments * 1024);
+                  p->cfg.max_batch, kPageSegments << kSegmentShift);
         return FI_ERR_INVALID_ARG;
     }
     if ((a->rows > 0 && (!a->lens || !a->lens_out || !a->block_table)) || (a->num_pages > 0 && (!a->free_pages || !a->shared)) || !a->free_count ||
@@ -436,12 +475,11 @@ fi_status_t fi_pages_free(fi_pages_t *p, const fi_pages_free_t *a, void *cuda_st
     }
     DeviceGuard guard(p->cfg.device);
     if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_free");
-    long long grid = (long long)a->batch_max * p->cfg.max_blocks / 4096;
+    long long grid = (long long)a->batch_max * p->cfg.max_blocks / 2048;
     grid = grid < 1 ? 1 : grid > p->sm_count ? p->sm_count : grid;
-    pages_free_kernel<<<(int)grid, kPageThreads, (size_t)a->batch_max * 12, static_cast<cudaStream_t>(cuda_stream)>>>(
-        *a, shift_of(p->cfg.page_size), p->cfg.max_blocks, p->ticket, p->segments);
-    count_launch();
-    return check_launch("fi_pages_free");
+    const cudaError_t e = launch_early(pages_free_kernel, (int)grid, kPageThreads, (size_t)a->batch_max * 12, static_cast<cudaStream_t>(cuda_stream), *a,
+                                       shift_of(p->cfg.page_size), p->cfg.max_blocks, p->ticket, p->segments);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_pages_free");
 }
 
 int64_t fi_pages_compact_workspace(int32_t num_pages) {
@@ -466,14 +504,11 @@ fi_status_t fi_pages_compact(fi_pages_t *p, const fi_pages_compact_t *a, void *c
     DeviceGuard guard(p->cfg.device);
     if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_compact");
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    pages_compact_kernel<<<kCompactCtas, kPageThreads, 0, stream>>>(*a, p->cfg.page_size);
-    count_launch();
-    if (a->rows > 0) {
-        const int grid = a->rows < 8 * p->sm_count ? a->rows : 8 * p->sm_count;
-        pages_rename_kernel<<<grid, 256, 0, stream>>>(*a, shift_of(p->cfg.page_size), p->cfg.max_blocks);
-        count_launch();
-    }
-    return check_launch("fi_pages_compact");
+    cudaError_t e = launch_early(pages_compact_kernel, kCompactCtas, kPageThreads, 0, stream, *a, p->cfg.page_size);
+    if (e == cudaSuccess && a->rows > 0)
+        e = launch_early(pages_rename_kernel, a->rows < 8 * p->sm_count ? a->rows : 8 * p->sm_count, 256, 0, stream, *a, shift_of(p->cfg.page_size),
+                         p->cfg.max_blocks);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_pages_compact");
 }
 
 fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_copies, const int32_t *count, void *cuda_stream) {
@@ -489,10 +524,10 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
                          {static_cast<uint32_t *>(c.k_meta), static_cast<uint32_t *>(c.v_meta)},
                          c.page_stride, c.head_stride, c.token_stride, c.meta_page_stride, c.meta_head_stride, c.meta_token_stride,
                          c.kv_heads, c.page_size, c.num_pages, c.head_dim / 32, kv->status_dev};
-    const long long units = ((long long)max_copies * c.kv_heads * 2 + 7) / 8, most = 8ll * kv->sm_count;
-    kv_copy_pages_kernel<<<(unsigned)(units < most ? units : most), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, copies, count, max_copies);
-    count_launch();
-    return check_launch("fi_kv_copy_pages");
+    const long long units = ((long long)max_copies * c.kv_heads + 7) / 8, most = 4ll * kv->sm_count;
+    const cudaError_t e = launch_early(kv_copy_pages_kernel, (int)(units < most ? units : most), 256, 0, static_cast<cudaStream_t>(cuda_stream), p, copies,
+                                       count, max_copies);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_kv_copy_pages");
 }
 
 }  // extern "C"
