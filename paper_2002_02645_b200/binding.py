@@ -818,7 +818,7 @@ class KvTables:
         _check_flat(shared, "shared", index, free_pages.numel())
         _check_flat(batch_count, "batch_count", index, 1)
         if out is None:
-            out = torch.empty(rows + 1, dtype=torch.int32, device=self.device).split_with_sizes([rows, 1])
+            out = lens.new_empty(rows + 1).split_with_sizes([rows, 1])
         lens_out, count_out = out
         _check_flat(lens_out, "out[0]", index, rows)
         _check_flat(count_out, "out[1]", index, 1)
@@ -836,10 +836,9 @@ class KvTables:
         rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
         pages = free_pages.numel()
         _check_flat(shared, "shared", index, pages)
-        most = pages // 2
-        words = torch.empty(3 * most + 1, dtype=torch.int32, device=self.device)
-        copies, moves = words[:3 * most].view(most, 3), words[3 * most:]
-        work = torch.empty(self._lib.fi_pages_compact_workspace(pages), dtype=torch.uint8, device=self.device)
+        most, space = pages // 2, self._lib.fi_pages_compact_workspace(pages) // 4
+        copies, moves, work = lens.new_empty(3 * most + 1 + space).split_with_sizes([3 * most, 1, space])
+        copies = copies.view(most, 3)
         args = _pack_compact(lens.data_ptr(), free_count.data_ptr(), free_pages.data_ptr(), block_table.data_ptr(), shared.data_ptr(), copies.data_ptr(),
                              moves.data_ptr(), work.data_ptr(), block_table.stride(0), rows, pages, most)
         st = self._lib.fi_pages_compact(self._h, args, _raw_stream(index))
@@ -989,10 +988,10 @@ def _on_device(index: int, call, *args) -> None:
         _check(st)
 
 
-def _check_rows(t: torch.Tensor, name: str, index: int, dtype, rows: Optional[int], dim: int) -> int:
+def _check_rows(t: torch.Tensor, name: str, index: int, dtype, rows: int, dim: int) -> int:
     """Stride between rows of a [rows, dim] tensor."""
-    if t.dtype is not dtype or t.get_device() != index or t.dim() != 2 or t.size(1) != dim or (rows is not None and t.size(0) != rows):
-        raise ValueError(f"{name} must be {dtype} [{'rows' if rows is None else rows}, {dim}] on cuda:{index}")
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (rows, dim):
+        raise ValueError(f"{name} must be {dtype} [{rows}, {dim}] on cuda:{index}")
     row, value = t.stride()
     if value != 1 and dim > 1:
         raise ValueError(f"{name}: the values of a row must lie side by side")
@@ -1008,40 +1007,41 @@ def _activation(name: str) -> int:
 
 def _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit=0):
     index = x.get_device()
-    if x.dtype is not torch.bfloat16 or x.dim() != 2 or index < 0:
-        raise ValueError("x must be a bfloat16 [tokens, in_dim] tensor on a GPU")
+    if x.dtype is not torch.bfloat16 or x.dim() != 2 or index < 0 or weight.dim() != 2:
+        raise ValueError("x must be bfloat16 [tokens, in_dim] on a GPU, weight [out_dim, in_dim]")
     tokens, in_dim = x.shape
-    x_stride = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
-    if weight.dim() != 2:
-        raise ValueError("weight must be [out_dim, in_dim]")
     out_dim = weight.size(0)
+    x_stride = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
     weight_stride = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
-    _check_flat(bias, "bias", index, out_dim, torch.float32)
-    _check_flat(rows, "rows", index, tokens)
-    _check_flat(count, "count", index, 1)
+    if bias is not None:
+        _check_flat(bias, "bias", index, out_dim, torch.float32)
+    if count is not None:
+        _check_flat(count, "count", index, 1)
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else residual.dtype if residual is not None else torch.bfloat16
-    if out_dtype not in _FI_DTYPE:
+    kind, act = _FI_DTYPE.get(out_dtype), FI_ACTIVATIONS.get(activation)
+    if kind is None:
         raise ValueError("out_dtype must be float32 or bfloat16")
-    out_rows, residual_stride = tokens, 0
+    if act is None:
+        raise ValueError(f"activation must be one of {', '.join(FI_ACTIVATIONS)}")
+    out_rows, residual_stride, preact_stride = tokens, 0, 0
     if rows is not None:
-        if out is None:
-            raise ValueError("rows are rows of `out`, which has to be given")
+        _check_flat(rows, "rows", index, tokens)
+        if out is None or out.dim() != 2:
+            raise ValueError("rows are rows of `out`, which has to be given as [rows, out_dim]")
         out_rows = out.size(0)
     if out is None:
-        out = torch.empty((tokens, out_dim), dtype=out_dtype, device=x.device)
+        out = x.new_empty((tokens, out_dim), dtype=out_dtype)
         out_stride = out_dim
     else:
         out_stride = _check_rows(out, "out", index, out_dtype, out_rows, out_dim)
     if residual is not None:
         residual_stride = _check_rows(residual, "residual", index, out_dtype, out_rows, out_dim)
-    preact_stride = 0
     if preact is not None:
         preact_stride = _check_rows(preact, "preact", index, torch.bfloat16, tokens, out_dim)
-    args = _pack_linear(x.data_ptr(), weight.data_ptr(), _at(bias), _at(residual), out.data_ptr(), _at(preact), _at(rows), _at(count), x_stride,
-                        weight_stride, residual_stride, out_stride, preact_stride, tokens, out_rows, wait_limit, in_dim, out_dim,
-                        _activation(activation), _FI_DTYPE[out_dtype])
-    _on_device(index, load_library().fi_linear, args)
+    _on_device(index, (_lib or load_library()).fi_linear, _pack_linear(
+        x.data_ptr(), weight.data_ptr(), _at(bias), _at(residual), out.data_ptr(), _at(preact), _at(rows), _at(count), x_stride, weight_stride,
+        residual_stride, out_stride, preact_stride, tokens, out_rows, wait_limit, in_dim, out_dim, act, kind))
     return out
 
 
@@ -1053,8 +1053,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     belongs to row rows[i] of residual and out (out may be residual); with `count` only that many tokens are real.  preact takes the sums
     before the activation.  Gradients flow to x, weight, bias and residual; not through rows, count, out or preact, which are refused
     where one is asked for."""
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
-                                    or residual is not None and residual.requires_grad):
+    if (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
+            or residual is not None and residual.requires_grad) and torch.is_grad_enabled():
         if out is not None or rows is not None or count is not None or preact is not None:
             raise ValueError("out, rows, count or preact is given, but a gradient is asked for")
         return _Linear.apply(x, weight, bias, residual, activation, out_dtype, wait_limit)
@@ -1078,14 +1078,14 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
     if weight is not None:
         strides[1] = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
         if dx is None:
-            dx = torch.empty((tokens, in_dim), dtype=torch.bfloat16, device=dy.device)
+            dx = dy.new_empty((tokens, in_dim))
         strides[4] = _check_rows(dx, "dx", index, torch.bfloat16, tokens, in_dim)
     elif dx is not None:
         raise ValueError("dx needs weight")
     if x is not None:
         strides[0] = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
         if dweight is None:
-            dweight = torch.empty((out_dim, in_dim), dtype=torch.bfloat16, device=dy.device)
+            dweight = dy.new_empty((out_dim, in_dim))
         strides[5] = _check_rows(dweight, "dweight", index, torch.bfloat16, out_dim, in_dim)
     elif dweight is not None:
         raise ValueError("dweight needs x")
@@ -1093,10 +1093,10 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
         if preact is None:
             raise ValueError("the gradient of an activation needs preact")
         strides[3] = _check_rows(preact, "preact", index, torch.bfloat16, tokens, out_dim)
-    dbias = torch.empty(out_dim, dtype=torch.float32, device=dy.device) if with_bias else None
+    dbias = dy.new_empty(out_dim, dtype=torch.float32) if with_bias else None
     work = None
     if kind:
-        work = torch.empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind), dtype=torch.uint8, device=dy.device)
+        work = dy.new_empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind), dtype=torch.uint8)
     args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
                                  *strides, tokens, in_dim, out_dim, kind)
     _on_device(index, lib.fi_linear_backward, args)
@@ -1143,10 +1143,10 @@ def _norm_types(x: torch.Tensor, y_dtype, weight, bias, index: int):
         raise ValueError("x must be a float32 or bfloat16 [rows, dim] tensor on a GPU")
     if y_dtype not in _FI_DTYPE:
         raise ValueError("the result must be float32 or bfloat16")
+    dim = x.size(1)
     for w, name in ((weight, "weight"), (bias, "bias")):
-        if w is not None and w.numel() != x.size(1):
-            raise ValueError(f"{name} must have {x.size(1)} values")
-        _check_flat(w, name, index, 0, torch.float32)
+        if w is not None and (w.dtype is not torch.float32 or w.get_device() != index or w.numel() != dim or not w.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 tensor of {dim} values on cuda:{index}")
     return _FI_DTYPE[x.dtype], _FI_DTYPE[y_dtype]
 
 
@@ -1157,17 +1157,20 @@ def _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out):
     kinds = _norm_types(x, out_dtype, weight, bias, index)
     x_rows, dim = x.shape
     x_stride = _check_rows(x, "x", index, x.dtype, x_rows, dim)
-    _check_flat(rows, "rows", index)
-    _check_flat(count, "count", index, 1)
-    tokens = x_rows if rows is None else rows.numel()
+    tokens = x_rows
+    if rows is not None:
+        _check_flat(rows, "rows", index)
+        tokens = rows.numel()
+    if count is not None:
+        _check_flat(count, "count", index, 1)
     if out is None:
-        out = torch.empty((tokens, dim), dtype=out_dtype, device=x.device)
+        out = x.new_empty((tokens, dim), dtype=out_dtype)
         out_stride = dim
     else:
         out_stride = _check_rows(out, "out", index, out_dtype, tokens, dim)
     args = _pack_layer_norm(x.data_ptr(), 0, out.data_ptr(), _at(weight), _at(bias), _at(rows), _at(count), 0, 0, 0, x_stride, 0, out_stride, tokens,
                             x_rows, dim, 1 if rms else 0, *kinds, eps)
-    _on_device(index, load_library().fi_layer_norm, args)
+    _on_device(index, (_lib or load_library()).fi_layer_norm, args)
     return out
 
 
@@ -1177,7 +1180,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     """fi_layer_norm: the rows of x [rows, dim] normed by mean and variance, or by root mean square.  With `rows`, token i of the result is
     row rows[i] of x; with `count` only that many tokens are real (the others are left as they are).  Gradients flow to x, weight and
     bias; not through rows, count or out, which are refused where one is asked for."""
-    if torch.is_grad_enabled() and (x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad):
+    if (x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad) and torch.is_grad_enabled():
         if out is not None or rows is not None or count is not None:
             raise ValueError("out, rows or count is given, but a gradient is asked for")
         return _LayerNorm.apply(x, weight, bias, eps, rms, out_dtype)
@@ -1193,13 +1196,13 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
     tokens, dim = x.shape
     x_stride, dy_stride = _check_rows(x, "x", index, x.dtype, tokens, dim), _check_rows(dy, "dy", index, dy.dtype, tokens, dim)
     if dx is None:
-        dx = torch.empty((tokens, dim), dtype=x.dtype, device=x.device)
+        dx = x.new_empty((tokens, dim))
     dx_stride = _check_rows(dx, "dx", index, x.dtype, tokens, dim)
-    dw = torch.empty(dim, dtype=torch.float32, device=x.device) if weight is not None else None
-    db = torch.empty(dim, dtype=torch.float32, device=x.device) if with_bias else None
+    dw = weight.new_empty(dim) if weight is not None else None
+    db = x.new_empty(dim, dtype=torch.float32) if with_bias else None
     work = None
     if dw is not None or db is not None:
-        work = torch.empty(lib.fi_layer_norm_workspace(dim), dtype=torch.uint8, device=x.device)
+        work = x.new_empty(lib.fi_layer_norm_workspace(dim), dtype=torch.uint8)
     args = _pack_layer_norm(x.data_ptr(), dy.data_ptr(), dx.data_ptr(), _at(weight), 0, 0, 0, _at(dw), _at(db), _at(work), x_stride, dy_stride, dx_stride,
                             tokens, 0, dim, 1 if rms else 0, *kinds, eps)
     _on_device(index, lib.fi_layer_norm_backward, args)
