@@ -63,6 +63,7 @@ struct LinearParams {
     int bufs;                      // accumulators that a CTA's reduction is cut into
     int tmem_cols, stages, b_bytes;
     int part_at;                   // place of a CTA's sums in shared memory
+    int early;                     // two products in one launch: see TileWalk
     int wide;                      // rows of out, residual, preact and the bias lie on 16-byte boundaries
 };
 
@@ -694,24 +695,50 @@ __device__ __forceinline__ void finish_row(const LinearParams &p, float (&v)[F32
     }
 }
 
+// The tiles of a pair, one after another: every pairs-th one.  Of two products the second follows on the first: the pairs from `late` on,
+// which have a tile less of the first, take `early` tiles of the second in its time, then all share the rest.  (Gradients of 4,095 tokens,
+// 2,048 -> 8,192: 128 tiles of 128 steps and 256 of 64 on 74 pairs take 448 steps, one after the other in two launches 512.)
+template <int JOBS>
+struct TileWalk {
+    int pair, pairs, tiles[2];
+    int late = 0, early = 0, job = 0, k = 0, t = 0;
+    __device__ __forceinline__ bool next() {
+        if (JOBS == 1 || job == 0) {
+            t = pair + k++ * pairs;
+            if (t < tiles[0]) return true;
+            if (JOBS == 1) return false;
+            job = 1;
+            k = 0;
+        }
+        const int lead = pairs - late, mine = pair >= late ? early : 0;
+        t = k < mine ? k * lead + pair - late : early * lead + (k - mine) * pairs + pair;
+        ++k;
+        return t < tiles[1];
+    }
+};
+
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
 // both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 1,024 values of the reduction) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
-template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
-__global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
-                                                                  const __grid_constant__ CUtensorMap map_b,
-                                                                  const __grid_constant__ LinearParams p) {
+// JOBS = 2: a second product behind the first, whose rows' operand lies the other way round (the two gradients).
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, int JOBS>
+__device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUtensorMap *maps_b, const LinearParams *jobs) {
+    const LinearParams &p = jobs[0];                        // (tiles and stages are those of both)
     extern __shared__ unsigned char raw_smem[];
     __shared__ PairCtl ctl_space;
     PairCtl *const ctl = &ctl_space;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int rows = actual_rows(p), row_tiles = (rows + 2 * kM - 1) / (2 * kM), col_tiles = p.m_tiles, tiles = row_tiles * col_tiles;
-    if (pair >= tiles) return;                              // (both CTAs)
+    const int rows0 = actual_rows(p);
+    const auto rows_of = [&](int job) { return JOBS == 2 && job ? jobs[1].n : rows0; };
+    const auto row_tiles_of = [&](int job) { return (rows_of(job) + 2 * kM - 1) / (2 * kM); };
+    TileWalk<JOBS> walk = {pair, pairs, {row_tiles_of(0) * p.m_tiles, JOBS == 2 ? row_tiles_of(1) * jobs[JOBS - 1].m_tiles : 0}};
+    walk.late = walk.tiles[0] % pairs;
+    walk.early = p.early;
+    if (pair >= walk.tiles[0] + walk.tiles[1]) return;      // (both CTAs)
     const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u, block_bytes = kABytes + p.b_bytes, stage_bytes = DEPTH * block_bytes;
     const int half_n = p.tile_n >> 1;
-    const int piece = F32 ? kPiece / DEPTH : p.kb;          // steps of an accumulator
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&ctl->full[s], 1);
@@ -746,11 +773,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
     if (warp == 8) {
         int issued = 0;                                     // (up to the number of stages)
         bool ok = true;
-        for (int t = pair; t < tiles && ok; t += pairs) {
+        for (TileWalk<JOBS> w = walk; ok && w.next();) {
+            const LinearParams &q = jobs[w.job];
+            const CUtensorMap *const map_a = maps_a + w.job, *const map_b = maps_b + w.job;
+            const bool b_mn = B_MN != (w.job != 0);
             int rt, ct;
-            tile_place(t, row_tiles, col_tiles, rt, ct);
+            tile_place(w.t, row_tiles_of(w.job), q.m_tiles, rt, ct);
             const int r0 = rt * 2 * kM + (int)rank * kM, c0 = ct * p.tile_n + (int)rank * half_n;
-            for (int kb = 0; kb < p.kb; ++kb) {
+            for (int kb = 0; kb < q.kb; ++kb) {
                 ok = warp_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit);
                 if (!ok) break;
                 if (elect_one()) {
@@ -760,16 +790,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                     for (int i = 0; i < DEPTH; ++i) {
                         const uint32_t a = smem + stage * stage_bytes + i * block_bytes, b = a + kABytes;
                         const int k = (kb * DEPTH + i) * kKb;
-                        if (B_MN) {
-                            load_box_pair(a, &map_b, bar, r0, k);
-                            load_box_pair(a + 8192, &map_b, bar, r0 + 64, k);
+                        if (b_mn) {
+                            load_box_pair(a, map_b, bar, r0, k);
+                            load_box_pair(a + 8192, map_b, bar, r0 + 64, k);
                         } else {
-                            load_box_pair(a, &map_b, bar, k, r0);
+                            load_box_pair(a, map_b, bar, k, r0);
                         }
                         if (A_MN)
-                            for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, &map_a, bar, c0 + c, k);
+                            for (int c = 0; c < half_n; c += 64) load_box_pair(b + c * 128, map_a, bar, c0 + c, k);
                         else
-                            load_box_pair(b, &map_a, bar, k, c0);
+                            load_box_pair(b, map_a, bar, k, c0);
                     }
                 }
                 __syncwarp();
@@ -794,16 +824,17 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         }
     } else if (warp == 9) {
         if (rank == 0) {
-            const uint32_t idesc = instruction(2 * kM, p.tile_n, B_MN, A_MN);
             uint32_t buf = 0, buf_phase = 0;
             bool ok = true;
-            for (int t = pair; t < tiles && ok; t += pairs) {
-                for (int kb = 0; kb < p.kb && ok;) {
+            for (TileWalk<JOBS> w = walk; ok && w.next();) {
+                const int steps = jobs[w.job].kb, piece = F32 ? kPiece / DEPTH : steps;     // steps of an accumulator
+                const uint32_t idesc = instruction(2 * kM, p.tile_n, B_MN != (w.job != 0), A_MN);
+                for (int kb = 0; kb < steps && ok;) {
                     ok = warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit);
                     if (!ok) break;
                     tc_after();
                     const uint32_t d = tmem + buf * p.tile_n;
-                    const int end = min(kb + piece, p.kb);
+                    const int end = min(kb + piece, steps);
                     for (uint32_t more = 0; kb < end; ++kb, more = 1) {
                         ok = warp_wait(&ctl->full[stage], phase, ctl, p.wait_limit);
                         if (!ok) break;
@@ -812,7 +843,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
 #pragma unroll
                             for (int i = 0; i < DEPTH; ++i) {
                                 const uint32_t at = smem + stage * stage_bytes + i * block_bytes;
-                                mma_block<true, B_MN, A_MN>(d, operand<B_MN>(at), operand<A_MN>(at + kABytes), idesc, i ? 1u : more);
+                                if (JOBS == 2 && w.job) mma_block<true, !B_MN, A_MN>(d, operand<!B_MN>(at), operand<A_MN>(at + kABytes), idesc, i ? 1u : more);
+                                else mma_block<true, B_MN, A_MN>(d, operand<B_MN>(at), operand<A_MN>(at + kABytes), idesc, i ? 1u : more);
                             }
                             tc_commit_pair(&ctl->empty[stage]);
                         }
@@ -840,23 +872,25 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + first;
         uint32_t buf = 0, buf_phase = 0;
         bool ok = true;
-        for (int t = pair; t < tiles && ok; t += pairs) {
+        for (TileWalk<JOBS> w = walk; ok && w.next();) {
+            const LinearParams &q = jobs[w.job];
+            const int rows = rows_of(w.job);
             int rt, ct;
-            tile_place(t, row_tiles, col_tiles, rt, ct);
-            const int row = rt * 2 * kM + my_row, n = row < rows ? row : -1, to = row_of(p, row, rows), c0 = ct * p.tile_n + first;
-            const int cols = min(half_n, p.m - c0);
+            tile_place(w.t, row_tiles_of(w.job), q.m_tiles, rt, ct);
+            const int row = rt * 2 * kM + my_row, n = row < rows ? row : -1, to = row_of(q, row, rows), c0 = ct * p.tile_n + first;
+            const int cols = min(half_n, q.m - c0);
             const float *bias = nullptr;
-            if (p.bias) {
+            if (q.bias) {
                 __syncwarp();
-                for (int c = lane; c < cols; c += 32) ctl->bias[warp][c] = p.bias[c0 + c];
+                for (int c = lane; c < cols; c += 32) ctl->bias[warp][c] = q.bias[c0 + c];
                 __syncwarp();
                 bias = ctl->bias[warp];
             }
             const uint32_t turn = smem_at(ctl->turn[warp]);
-            const bool add = p.residual != nullptr;
+            const bool add = q.residual != nullptr;
             if constexpr (F32) {
                 float sum[kMaxPairN32 / 2] = {};
-                for (int kb = 0; kb < p.kb && ok; kb += piece) {
+                for (int kb = 0; kb < q.kb && ok; kb += kPiece / DEPTH) {
                     ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                     tc_after();
                     // (a load from TMEM ahead of the sums)
@@ -882,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         float v[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) v[i] = sum[c + i];
-                        finish_row<true, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add, turn);
+                        finish_row<true, ACT>(q, v, c0 + c, n, to, bias ? bias + c : nullptr, add, turn);
                     }
             } else {
                 ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
@@ -900,7 +934,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
                         v[i] = __uint_as_float(s0[i]);
                         v[16 + i] = __uint_as_float(s1[i]);
                     }
-                    finish_row<false, ACT>(p, v, c0 + c, n, to, bias ? bias + c : nullptr, add, turn);
+                    finish_row<false, ACT>(q, v, c0 + c, n, to, bias ? bias + c : nullptr, add, turn);
                 }
                 tc_before();
                 __syncwarp();
@@ -918,6 +952,23 @@ __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_c
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
     }
+}
+
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
+__global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
+                                                                  const __grid_constant__ CUtensorMap map_b,
+                                                                  const __grid_constant__ LinearParams p) {
+    linear_pair<F32, ACT, A_MN, B_MN, DEPTH, 1>(&map_a, &map_b, &p);
+}
+
+// Both gradients, the one with the longer reduction first (ROWS_MN: that of the weights).
+struct LinearTwo {
+    CUtensorMap a[2], b[2];
+    LinearParams p[2];
+};
+template <bool ROWS_MN, int DEPTH>
+__global__ void __launch_bounds__(kThreads, 1) linear_two_kernel(const __grid_constant__ LinearTwo two) {
+    linear_pair<false, FI_ACT_NONE, true, ROWS_MN, DEPTH, 2>(two.a, two.b, two.p);
 }
 
 // dz = dy act'(preact), and dbias, the sums of its columns (of dy itself without an activation: nothing else is stored then).  A CTA takes 64
@@ -1013,6 +1064,12 @@ LinearKernel linear_kernel(bool pair, int depth, bool f32, int act, bool a_mn, b
     return depth == 2 ? linear_kernel<false, 2>(f32, act, a_mn, b_mn) : linear_kernel<false, 1>(f32, act, a_mn, b_mn);
 }
 
+using TwoKernel = void (*)(LinearTwo);
+TwoKernel two_kernel(bool rows_mn, int depth) {
+    if (rows_mn) return depth == 2 ? linear_two_kernel<true, 2> : linear_two_kernel<true, 1>;
+    return depth == 2 ? linear_two_kernel<false, 2> : linear_two_kernel<false, 1>;
+}
+
 struct DeviceFacts {
     std::atomic<int> sms{0};
     int clusters[4];                                        // of 1, 2, 4, 8 CTAs that run at one time
@@ -1039,6 +1096,9 @@ fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
             e = cudaFuncSetAttribute(reinterpret_cast<const void *>(linear_kernel(i & 1, 1 + (i >> 1), f32, form % 5, back, form == 11)),
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
     }
+    for (int i = 0; i < 4 && e == cudaSuccess; ++i)
+        e = cudaFuncSetAttribute(reinterpret_cast<const void *>(two_kernel(i & 1, 1 + (i >> 1))), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kSmemMost - kStaticMost);
     f.clusters[0] = n;
     for (int i = 1; i < 4 && e == cudaSuccess; ++i) {
         cudaLaunchAttribute attr;
@@ -1127,9 +1187,19 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
     return best;
 }
 
-// D[n][m] = sum over k of A(m, k) B(n, k); `p` holds what becomes of the sums
-fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act, LinearParams p,
-                           const DeviceFacts &facts, cudaStream_t stream, const char *name) {
+// A product that is ready to be launched
+struct Product {
+    CUtensorMap map_a, map_b;
+    LinearParams p;
+    LinearPlan plan;
+    long long tiles;
+    int depth, smem;
+};
+
+// D[n][m] = sum over k of A(m, k) B(n, k); x.p holds what becomes of the sums
+fi_status_t plan_launch(Product &x, const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32,
+                        const DeviceFacts &facts, const char *name) {
+    LinearParams &p = x.p;
     p.m = (int)m;
     p.n = (int)n;
     p.kb = (int)((k + kKb - 1) / kKb);
@@ -1167,23 +1237,63 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
         set_error("%s: too many tiles", name);
         return FI_ERR_INVALID_ARG;
     }
-    CUtensorMap map_a, map_b;
-    fi_status_t st = operand_map(&map_a, a, a_mn ? kKb : plan.pair ? mine : kM, name);
-    if (st == FI_OK) st = operand_map(&map_b, b, b_mn ? kKb : plan.pair ? kM : mine, name);
+    fi_status_t st = operand_map(&x.map_a, a, a_mn ? kKb : plan.pair ? mine : kM, name);
+    if (st == FI_OK) st = operand_map(&x.map_b, b, b_mn ? kKb : plan.pair ? kM : mine, name);
+    x.plan = plan;
+    x.tiles = tiles;
+    x.depth = depth;
+    x.smem = smem;
+    return st;
+}
+
+fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act,
+                           const LinearParams &what, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
+    Product x;
+    x.p = what;
+    const fi_status_t st = plan_launch(x, a, a_mn, b, b_mn, m, n, k, f32, facts, name);
     if (st != FI_OK) return st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = plan.pair ? 2 : p.split;
+    attr.val.clusterDim.x = x.plan.pair ? 2 : x.p.split;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(plan.pair ? 2 * (tiles < facts.clusters[1] ? tiles : facts.clusters[1]) : tiles * p.split));
+    cfg.gridDim = dim3((unsigned)(x.plan.pair ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * x.p.split));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = x.smem;
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    const LinearKernel kernel = linear_kernel(plan.pair, depth, f32, act, a_mn, b_mn);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, p);
+    const LinearKernel kernel = linear_kernel(x.plan.pair, x.depth, f32, act, a_mn, b_mn);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, x.map_a, x.map_b, x.p);
+    if (e != cudaSuccess) return cuda_fail(e, name);
+    count_launch();
+    return check_launch(name);
+}
+
+// Two products of pairs in one launch, the one with the longer reduction first; their tiles and stages are the same.
+fi_status_t launch_two(const Product &x, const Product &y, bool rows_mn, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
+    LinearTwo two;
+    two.a[0] = x.map_a;
+    two.a[1] = y.map_a;
+    two.b[0] = x.map_b;
+    two.b[1] = y.map_b;
+    two.p[0] = x.p;
+    two.p[1] = y.p;
+    two.p[0].early = (x.p.kb + y.p.kb / 2) / y.p.kb;
+    const long long tiles = x.tiles + y.tiles;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < facts.clusters[1] ? tiles : facts.clusters[1])));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = x.smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const auto kernel = two_kernel(rows_mn, x.depth);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, two);
     if (e != cudaSuccess) return cuda_fail(e, name);
     count_launch();
     return check_launch(name);
@@ -1349,26 +1459,30 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         if (st != FI_OK) return st;
     }
     const Matrix g = slopes ? Matrix{dz, a->tokens, a->out_dim, a->out_dim} : Matrix{a->dy, a->tokens, a->out_dim, a->dy_stride};
-    LinearParams p = {};
-    p.wait_limit = kWaitLimit;
-    if (a->dx) {
-        p.out = a->dx;
-        p.wide = aligned16(a->dx) && (a->tokens <= 1 || a->dx_stride % 8 == 0);
-        p.ld_out = a->dx_stride;
-        p.out_rows = a->tokens;
-        const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride};
-        st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, p, *facts, stream, name);
+    const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
+    LinearParams dx = {}, dw = {};
+    dx.wait_limit = dw.wait_limit = kWaitLimit;
+    dx.out = a->dx;
+    dx.wide = aligned16(a->dx) && (a->tokens <= 1 || a->dx_stride % 8 == 0);
+    dx.ld_out = a->dx_stride;
+    dx.out_rows = a->tokens;
+    dw.out = a->dweight;
+    dw.wide = aligned16(a->dweight) && a->dweight_stride % 8 == 0;
+    dw.ld_out = a->dweight_stride;
+    dw.out_rows = a->out_dim;
+    if (a->dx && a->dweight) {
+        Product px, pw;
+        px.p = dx;
+        pw.p = dw;
+        st = plan_launch(px, w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, *facts, name);
+        if (st == FI_OK) st = plan_launch(pw, x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, *facts, name);
         if (st != FI_OK) return st;
+        if (px.plan.pair && pw.plan.pair && px.plan.tile_n == pw.plan.tile_n && px.depth == pw.depth)
+            return px.p.kb >= pw.p.kb ? launch_two(px, pw, false, *facts, stream, name) : launch_two(pw, px, true, *facts, stream, name);
     }
-    if (a->dweight) {
-        p.out = a->dweight;
-        p.wide = aligned16(a->dweight) && a->dweight_stride % 8 == 0;
-        p.ld_out = a->dweight_stride;
-        p.out_rows = a->out_dim;
-        const Matrix x = {a->x, a->tokens, a->in_dim, a->x_stride};
-        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, p, *facts, stream, name);
-        if (st != FI_OK) return st;
-    }
+    if (a->dx) st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, dx, *facts, stream, name);
+    if (st == FI_OK && a->dweight)
+        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, dw, *facts, stream, name);
     return st;
 }
 
