@@ -233,6 +233,13 @@ __device__ __forceinline__ float recip_fast(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Kernels here are launched while the one before them in the stream still runs, and set themselves up meanwhile; nothing that it may write is
+// read, and nothing that it may read is written, before this.  The next one may begin at once.
+__device__ __forceinline__ void in_turn() {
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+}
+
 constexpr float kLog2e = 1.4426950408889634f, kGeluTanh = 0.044715f, kGeluTwice = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 
 // 1 / (1 + 2^-x)
@@ -426,9 +433,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         __syncwarp();
+        in_turn();
         for (int i = 0; i < early; ++i) load(kb0 + i);
     }
-    const int rows = actual_rows(p);
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(p.tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -437,6 +444,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     __syncthreads();
     tc_after();
     const uint32_t tmem = ctl->tmem;
+    if (warp != 8) in_turn();
+    const int rows = actual_rows(p);
     const bool apart = p.split > 1 && p.part_at > 0;
     if (apart) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const int cols = min(p.tile_n, rows - n0);              // rows of the output that there are; no more is done if there is none
@@ -730,13 +739,6 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int rows0 = actual_rows(p);
-    const auto rows_of = [&](int job) { return JOBS == 2 && job ? jobs[1].n : rows0; };
-    const auto row_tiles_of = [&](int job) { return (rows_of(job) + 2 * kM - 1) / (2 * kM); };
-    TileWalk<JOBS> walk = {pair, pairs, {row_tiles_of(0) * p.m_tiles, JOBS == 2 ? row_tiles_of(1) * jobs[JOBS - 1].m_tiles : 0}};
-    walk.late = walk.tiles[0] % pairs;
-    walk.early = p.early;
-    if (pair >= walk.tiles[0] + walk.tiles[1]) return;      // (both CTAs)
     const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u, block_bytes = kABytes + p.b_bytes, stage_bytes = DEPTH * block_bytes;
     const int half_n = p.tile_n >> 1;
     if (tid == 0) {
@@ -762,6 +764,13 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
     cluster_sync();                                         // the other CTA's barriers are there before anything signals them
     tc_after();
     const uint32_t tmem = ctl->tmem;
+    in_turn();
+    const int rows0 = actual_rows(p);
+    const auto rows_of = [&](int job) { return JOBS == 2 && job ? jobs[1].n : rows0; };
+    const auto row_tiles_of = [&](int job) { return (rows_of(job) + 2 * kM - 1) / (2 * kM); };
+    TileWalk<JOBS> walk = {pair, pairs, {row_tiles_of(0) * p.m_tiles, JOBS == 2 ? row_tiles_of(1) * jobs[JOBS - 1].m_tiles : 0}};
+    walk.late = walk.tiles[0] % pairs;
+    walk.early = p.early;
     if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
     uint32_t stage = 0, phase = 0;                          // of the loader, of the products
     const auto next_stage = [&] {
@@ -984,6 +993,7 @@ __global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const __
     const int part = threadIdx.x & (kSlopeCols / 8 - 1), group = threadIdx.x / (kSlopeCols / 8);
     const int c = blockIdx.x * kSlopeCols + part * 8;
     float sum[8] = {};
+    in_turn();
     if (c < cols)
         for (long long r0 = (long long)blockIdx.y * kSlopeRows * kSlopeAhead + group; r0 < rows; r0 += (long long)gridDim.y * kSlopeRows * kSlopeAhead) {
             uint4 a[kSlopeAhead], b[kSlopeAhead];
@@ -1039,6 +1049,29 @@ __global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const __
 // ------------------------------------------------------------------------------------------------------------- host
 
 using LinearKernel = void (*)(CUtensorMap, CUtensorMap, LinearParams);
+
+// see in_turn
+template <typename... Params, typename... Args>
+fi_status_t launch_early(const char *name, void (*kernel)(Params...), dim3 grid, int threads, int smem, dim3 cluster, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster.x;
+    attr[0].val.clusterDim.y = cluster.y;
+    attr[0].val.clusterDim.z = cluster.z;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+    if (e != cudaSuccess) return cuda_fail(e, name);
+    count_launch();
+    return check_launch(name);
+}
 
 // forward products in all their forms; gradients have no activation and bfloat16 results
 template <bool PAIR, int DEPTH, bool F32, int ACT, bool A_MN, bool B_MN>
@@ -1252,22 +1285,10 @@ fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_m
     x.p = what;
     const fi_status_t st = plan_launch(x, a, a_mn, b, b_mn, m, n, k, f32, facts, name);
     if (st != FI_OK) return st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = x.plan.pair ? 2 : x.p.split;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(x.plan.pair ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * x.p.split));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = x.smem;
-    cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const LinearKernel kernel = linear_kernel(x.plan.pair, x.depth, f32, act, a_mn, b_mn);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, x.map_a, x.map_b, x.p);
-    if (e != cudaSuccess) return cuda_fail(e, name);
-    count_launch();
-    return check_launch(name);
+    const bool pair = x.plan.pair;
+    const long long ctas = pair ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * x.p.split;
+    return launch_early(name, linear_kernel(pair, x.depth, f32, act, a_mn, b_mn), dim3((unsigned)ctas), kThreads, x.smem, dim3(pair ? 2 : x.p.split), stream,
+                        x.map_a, x.map_b, x.p);
 }
 
 // Two products of pairs in one launch, the one with the longer reduction first; their tiles and stages are the same.
@@ -1281,22 +1302,8 @@ fi_status_t launch_two(const Product &x, const Product &y, bool rows_mn, const D
     two.p[1] = y.p;
     two.p[0].early = (x.p.kb + y.p.kb / 2) / y.p.kb;
     const long long tiles = x.tiles + y.tiles;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < facts.clusters[1] ? tiles : facts.clusters[1])));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = x.smem;
-    cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const auto kernel = two_kernel(rows_mn, x.depth);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, two);
-    if (e != cudaSuccess) return cuda_fail(e, name);
-    count_launch();
-    return check_launch(name);
+    return launch_early(name, two_kernel(rows_mn, x.depth), dim3((unsigned)(2 * (tiles < facts.clusters[1] ? tiles : facts.clusters[1]))), kThreads, x.smem,
+                        dim3(2), stream, two);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -1438,24 +1445,11 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     }
     __nv_bfloat16 *const dz = slopes && (a->dx || a->dweight) ? static_cast<__nv_bfloat16 *>(a->workspace) : nullptr;
     if (dz || a->dbias) {
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = attr.val.clusterDim.z = 1;
-        const int width = a->out_dim <= 64 * 16 && a->tokens >= 1024 ? 16 : 64;
-        attr.val.clusterDim.y = slope_parts(a->tokens, a->out_dim, width, facts->clusters[0]);
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((a->out_dim + width - 1) / width, attr.val.clusterDim.y);
-        cfg.blockDim = dim3(kSlopeThreads);
-        cfg.stream = stream;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        const auto kernel = width == 16 ? slope_kernel<16>(a->activation) : slope_kernel<64>(a->activation);
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<const __nv_bfloat16 *>(a->dy), (long long)a->dy_stride,
-                                                 static_cast<const __nv_bfloat16 *>(a->preact), (long long)a->preact_stride, dz, a->dbias,
-                                                 (long long)a->tokens, (int)a->out_dim);
-        if (e != cudaSuccess) return cuda_fail(e, name);
-        count_launch();
-        st = check_launch(name);
+        const int width = a->out_dim <= 64 * 16 && a->tokens >= 1024 ? 16 : 64, parts = slope_parts(a->tokens, a->out_dim, width, facts->clusters[0]);
+        st = launch_early(name, width == 16 ? slope_kernel<16>(a->activation) : slope_kernel<64>(a->activation),
+                          dim3((a->out_dim + width - 1) / width, parts), kSlopeThreads, 0, dim3(1, parts), stream, static_cast<const __nv_bfloat16 *>(a->dy),
+                          (long long)a->dy_stride, static_cast<const __nv_bfloat16 *>(a->preact), (long long)a->preact_stride, dz, a->dbias,
+                          (long long)a->tokens, (int)a->out_dim);
         if (st != FI_OK) return st;
     }
     const Matrix g = slopes ? Matrix{dz, a->tokens, a->out_dim, a->out_dim} : Matrix{a->dy, a->tokens, a->out_dim, a->dy_stride};
