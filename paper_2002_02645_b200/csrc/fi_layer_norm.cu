@@ -206,9 +206,17 @@ __device__ __forceinline__ long long actual_tokens(const RowNormParams &p) {
     return c < 0 ? 0 : c > p.tokens ? p.tokens : c;
 }
 
+// Kernels here are launched while the one before them in the stream still runs; nothing that it may write is read, and nothing that it may
+// read is written, before this.  The next one may begin at once.
+__device__ __forceinline__ void in_turn() {
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+}
+
 template <bool X32, bool Y32, bool WARP, bool VEC, int P>
 __global__ void __launch_bounds__(WARP ? 128 : 512) layer_norm_kernel(const RowNormParams p) {
     __shared__ float s[4][32][2];
+    in_turn();
     int slot = 0;
     const Place<VEC, P> l = {WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x, WARP ? 32 : (int)blockDim.x, p.dim};
     const long long token = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
@@ -232,6 +240,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(c
     constexpr int V = 8 * P;
     __shared__ float s[4][32][2];
     extern __shared__ float sums[];                         // WARP: [warps][dim]
+    in_turn();
     int slot = 0;
     const Place<VEC, P> l = {WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x, WARP ? 32 : (int)blockDim.x, p.dim};
     const int groups_here = WARP ? blockDim.x >> 5 : 1, mine = WARP ? threadIdx.x >> 5 : 0;
@@ -470,7 +479,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
     extern __shared__ __align__(128) unsigned char ring[];
     const Place<true, P> l = {(int)threadIdx.x, THREADS, p.dim};
     const int row_bytes = p.dim * (X32 ? 4 : 2);
-    const long long tokens = actual_tokens(p), steps = (tokens + R - 1) / R;
+    long long tokens = 0;
     const auto row_at = [&](long long token) {               // -1: none
         if (token >= tokens) return -1ll;
         const long long row = p.rows ? p.rows[token] : token;
@@ -478,6 +487,9 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
     };
     Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages};
     if (threadIdx.x == 0) r.set_up(THREADS / 32);
+    in_turn();
+    tokens = actual_tokens(p);
+    const long long steps = (tokens + R - 1) / R;
     __syncthreads();
     if (threadIdx.x >= THREADS) {
         if (threadIdx.x == THREADS)
@@ -573,6 +585,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
     const long long steps = (p.tokens + R - 1) / R;
     Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages};
     if (threadIdx.x == 0) r.set_up(THREADS / 32);
+    in_turn();
     for (int i = threadIdx.x; i < p.dim / 4; i += THREADS + 32)
         *reinterpret_cast<float4 *>(weight + (i & 1) * (p.dim / 2) + (i >> 1) * 4) =
             p.weight ? *reinterpret_cast<const float4 *>(p.weight + 4 * i) : make_float4(1.f, 1.f, 1.f, 1.f);
@@ -673,7 +686,6 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
                 }
         }
     }
-    cudaTriggerProgrammaticLaunchCompletion();
     if (!p.partial) return;
     float *const to = p.partial + (long long)blockIdx.x * 2 * p.dim;
 #pragma unroll
@@ -686,7 +698,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
 
 // Weight gradients from the CTAs' sums, 32 columns per CTA, always in the same order.  Launched while the CTAs that write them still run.
 __global__ void __launch_bounds__(1024) layer_norm_sum_kernel(const float *partial, int parts, int dim, float *dweight, float *dbias) {
-    cudaGridDependencySynchronize();
+    in_turn();
     __shared__ float s[32][33];
     float *const out = blockIdx.y ? dbias : dweight;
     if (!out) return;
@@ -706,6 +718,23 @@ __global__ void __launch_bounds__(1024) layer_norm_sum_kernel(const float *parti
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// see in_turn
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
 // once for a device and kernel
 template <typename Kernel>
 void ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
@@ -717,7 +746,7 @@ void ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
 int ring_stages(int room, int stage) { return room / stage < kMaxRing ? room / stage : kMaxRing; }
 
 template <bool X32, bool Y32, bool VEC>
-void launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
+cudaError_t launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
     if constexpr (VEC) {
         // more rows than are worked on at one time: a few CTAs that stay, with the next rows on their way
         if (p.dim > 1024 && p.tokens > 8ll * sms) {
@@ -734,33 +763,32 @@ void launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
                                                       : layer_norm_ring_kernel<X32, Y32, false, 512, 4, 1>);
             ring_ready(kernel, done[which][p.rms]);
             const int stages = ring_stages((per_sm == 2 ? 110 : 216) * 1024, stage);
-            kernel<<<(unsigned)(sms * per_sm), threads + 32, (size_t)stages * stage, stream>>>(p, stages);
-            return;
+            return launch_early(kernel, dim3((unsigned)(sms * per_sm)), threads + 32, (size_t)stages * stage, stream, p, stages);
         }
     }
     if (p.dim <= 1024) {
-        const unsigned grid = (unsigned)((p.tokens + 3) / 4);
-        if (p.dim <= 256) layer_norm_kernel<X32, Y32, true, VEC, 1><<<grid, 128, 0, stream>>>(p);
-        else if (p.dim <= 512) layer_norm_kernel<X32, Y32, true, VEC, 2><<<grid, 128, 0, stream>>>(p);
-        else layer_norm_kernel<X32, Y32, true, VEC, 4><<<grid, 128, 0, stream>>>(p);
-    } else {
-        const int threads = p.dim <= 4096 ? 128 : p.dim <= 8192 ? 256 : 512;
-        layer_norm_kernel<X32, Y32, false, VEC, 4><<<(unsigned)p.tokens, threads, 0, stream>>>(p);
+        const auto kernel = p.dim <= 256   ? layer_norm_kernel<X32, Y32, true, VEC, 1>
+                            : p.dim <= 512 ? layer_norm_kernel<X32, Y32, true, VEC, 2>
+                                           : layer_norm_kernel<X32, Y32, true, VEC, 4>;
+        return launch_early(kernel, dim3((unsigned)((p.tokens + 3) / 4)), 128, 0, stream, p);
     }
+    const int threads = p.dim <= 4096 ? 128 : p.dim <= 8192 ? 256 : 512;
+    return launch_early(layer_norm_kernel<X32, Y32, false, VEC, 4>, dim3((unsigned)p.tokens), threads, 0, stream, p);
 }
 
 template <bool X32, bool Y32, bool VEC>
-int launch_backward(const RowNormParams &p, int sms, cudaStream_t stream) {
+cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStream_t stream) {
     if (p.dim <= 1024) {
         // no more CTAs than run at one time
         const int per_sm = p.dim <= 256 ? 3 : p.dim <= 512 ? 2 : 1;
         const long long want = (p.tokens + 7) / 8, most = per_sm * sms < kMaxPartials ? per_sm * sms : kMaxPartials;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
         const size_t smem = (size_t)8 * p.dim * sizeof(float);
-        if (p.dim <= 256) layer_norm_backward_kernel<X32, Y32, true, VEC, 1><<<grid, 256, smem, stream>>>(p);
-        else if (p.dim <= 512) layer_norm_backward_kernel<X32, Y32, true, VEC, 2><<<grid, 256, smem, stream>>>(p);
-        else layer_norm_backward_kernel<X32, Y32, true, VEC, 4><<<grid, 256, smem, stream>>>(p);
-        return (int)grid;
+        const auto kernel = p.dim <= 256   ? layer_norm_backward_kernel<X32, Y32, true, VEC, 1>
+                            : p.dim <= 512 ? layer_norm_backward_kernel<X32, Y32, true, VEC, 2>
+                                           : layer_norm_backward_kernel<X32, Y32, true, VEC, 4>;
+        *parts = (int)grid;
+        return launch_early(kernel, dim3(grid), 256, smem, stream, p);
     }
     if constexpr (VEC) {
         static std::atomic<unsigned long long> done[4][2];
@@ -779,15 +807,15 @@ int launch_backward(const RowNormParams &p, int sms, cudaStream_t stream) {
         const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < kMaxPartials ? sms * per_sm : kMaxPartials;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
         ring_ready(kernel, done[which][p.rms]);
-        kernel<<<grid, threads + 32, (size_t)stages * stage + p.dim * 4, stream>>>(p, stages);
-        return (int)grid;
+        *parts = (int)grid;
+        return launch_early(kernel, dim3(grid), threads + 32, (size_t)stages * stage + p.dim * 4, stream, p, stages);
     }
     const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
     const long long most = sms * (512 / threads) < kMaxPartials ? sms * (512 / threads) : kMaxPartials;
     const unsigned grid = (unsigned)(p.tokens < 1 ? 1 : p.tokens < most ? p.tokens : most);
-    if (p.dim <= 8192) layer_norm_backward_kernel<X32, Y32, false, VEC, 2><<<grid, threads, 0, stream>>>(p);
-    else layer_norm_backward_kernel<X32, Y32, false, VEC, 4><<<grid, threads, 0, stream>>>(p);
-    return (int)grid;
+    *parts = (int)grid;
+    return launch_early(p.dim <= 8192 ? layer_norm_backward_kernel<X32, Y32, false, VEC, 2> : layer_norm_backward_kernel<X32, Y32, false, VEC, 4>, dim3(grid),
+                        threads, 0, stream, p);
 }
 
 template <typename F>
@@ -884,10 +912,9 @@ fi_status_t fi_layer_norm(const fi_layer_norm_t *a, void *cuda_stream) {
     bool vec;
     const RowNormParams p = row_norm_params(a, false, &vec);
     with_types(a->x_dtype == FI_F32, a->y_dtype == FI_F32, vec, [&](auto x, auto y, auto v) {
-        launch_forward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, sms, static_cast<cudaStream_t>(cuda_stream));
+        e = launch_forward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, sms, static_cast<cudaStream_t>(cuda_stream));
     });
-    count_launch();
-    return check_launch("fi_layer_norm");
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_layer_norm");
 }
 
 fi_status_t fi_layer_norm_backward(const fi_layer_norm_t *a, void *cuda_stream) {
@@ -902,24 +929,11 @@ fi_status_t fi_layer_norm_backward(const fi_layer_norm_t *a, void *cuda_stream) 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     int parts = 0;
     with_types(a->x_dtype == FI_F32, a->y_dtype == FI_F32, vec, [&](auto x, auto y, auto v) {
-        parts = launch_backward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, sms, stream);
+        e = launch_backward<decltype(x)::value, decltype(y)::value, decltype(v)::value>(p, sms, &parts, stream);
     });
-    count_launch();
-    if (p.partial) {
-        cudaLaunchAttribute early;
-        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        early.val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((a->dim + 31) / 32, 2);
-        cfg.blockDim = dim3(1024);
-        cfg.stream = stream;
-        cfg.attrs = &early;
-        cfg.numAttrs = 1;
-        e = cudaLaunchKernelEx(&cfg, layer_norm_sum_kernel, (const float *)p.partial, parts, (int)a->dim, a->dweight, a->dbias);
-        if (e != cudaSuccess) return cuda_fail(e, "fi_layer_norm_backward");
-        count_launch();
-    }
-    return check_launch("fi_layer_norm_backward");
+    if (e == cudaSuccess && p.partial)
+        e = launch_early(layer_norm_sum_kernel, dim3((a->dim + 31) / 32, 2), 1024, 0, stream, p.partial, parts, a->dim, a->dweight, a->dbias);
+    return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_layer_norm_backward");
 }
 
 fi_status_t fi_layer_norm_poll_status(void) {
