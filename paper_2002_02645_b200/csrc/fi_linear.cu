@@ -23,7 +23,7 @@ constexpr int kABytes = kM * kKb * 2;     // of a block
 constexpr int kMaxN = 256;                // output rows of a tile, at most
 constexpr int kMaxPairN32 = 192;          // of a pair's tile with float32 results, whose sums are in registers
 constexpr int kMaxStages = 12;
-constexpr int kPiece = 16;                // blocks of the reduction that are added up in one accumulator for float32 results
+constexpr int kPiece = 8;                 // blocks of the reduction that are added up in one accumulator for float32 results
 constexpr int kEpiThreads = 256;          // warps 0..7: TMEM lanes 32 (w mod 4) ..; warp 8 loads, warp 9 issues the products
 constexpr int kThreads = kEpiThreads + 64;
 constexpr int kSmemMost = 227 * 1024, kStaticMost = 22 * 1024;
@@ -727,7 +727,7 @@ struct TileWalk {
 };
 
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
-// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 1,024 values of the reduction) go out while the next is formed.
+// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the reduction) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
 // JOBS = 2: a second product behind the first, whose rows' operand lies the other way round (the two gradients).
 template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, int JOBS>
@@ -1208,7 +1208,7 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
         for (int i = 0; i < 4 && 1 << i <= kb; ++i) {
             const int split = 1 << i;
             const long long blocks = up(kb, split);
-            if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 1,024 values have an accumulator each
+            if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 512 values have an accumulator each
             const double block = most(2. * tile, (128 + tile) * 128 / 75.), rounds = (double)up(up(m, kM) * up(n, tile), clusters[i]);
             const double end = split > 1 ? 4000 + 30. * tile : 2500 + 20. * tile;
             // columns' operand (weights) that L2 does not hold is read again for every tile of rows
@@ -1250,7 +1250,7 @@ fi_status_t plan_launch(Product &x, const Matrix &a, bool a_mn, const Matrix &b,
     const long long n_tiles = plan.pair ? (n + 2 * kM - 1) / (2 * kM) : (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
     p.bufs = plan.pair ? 2 : 1;
     if (f32 && !plan.pair) {
-        // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 1,024 at a time
+        // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
         const int room = 512 / p.tile_n, pieces = ((blocks + p.split - 1) / p.split + depth + kPiece - 1) / kPiece;
         p.bufs = pieces < room ? pieces : room;
     }

@@ -100,8 +100,8 @@ def test_bias_activation_residual_preact(tokens, dtype, act):
 
 
 def test_float32_sums_do_not_drift():
-    """Long float32 sums of one sign, where cutting adds up: pieces of 1,024 values, at most 32 of them added up, so off by
-    (1024 / 16 + 32 + 32) 2^-23 of the sum, not by K / 16 of them."""
+    """Long float32 sums of one sign, where cutting adds up: pieces of 512 values (a few more where few CTAs share a sum), so off by
+    (2 * 512 / 16 + 64) 2^-23 of the sum, not by K / 16 of them."""
     gen = torch.Generator(device=DEV).manual_seed(3)
     for tokens, n_in, n_out in [(1, 16384, 512), (40, 16384, 4096), (300, 16384, 2048), (2000, 16384, 1024), (5000, 8192, 512)]:
         x, w = (t.abs().bfloat16() for t in operands(gen, tokens, n_in, n_out))
