@@ -447,12 +447,13 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float *s, int &slot) {
     slot = (slot + 1) & 3;
 }
 
+// FULL: every thread has all its pieces, as with rows of 2,048 or 4,096 values.
 // what a step reads, widened to pairs: row i of the stage, `skip` bytes behind its start
-template <bool F32, int P>
+template <bool F32, bool FULL, int P>
 __device__ __forceinline__ void stage_row(const Place<true, P> &l, const unsigned char *at, bool there, uint64_t (&v)[4 * P]) {
 #pragma unroll
     for (int q = 0; q < P; ++q) {
-        if (there && l.piece(q) < l.dim) pairs_in<F32>(at + l.piece(q) * (F32 ? 4 : 2), v + 4 * q);
+        if (there && (FULL || l.piece(q) < l.dim)) pairs_in<F32>(at + l.piece(q) * (F32 ? 4 : 2), v + 4 * q);
         else
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[4 * q + e] = 0;
@@ -460,19 +461,19 @@ __device__ __forceinline__ void stage_row(const Place<true, P> &l, const unsigne
 }
 
 // v becomes x - mean (0 where there is no value), from the sum of the row
-template <int P>
+template <bool FULL, int P>
 __device__ __forceinline__ void less_mean(const Place<true, P> &l, uint64_t (&v)[4 * P], float sum) {
     const uint64_t less = both(-(sum / (float)l.dim));
 #pragma unroll
     for (int e = 0; e < 4 * P; ++e) v[e] = add2(v[e], less);
-    if (l.dim < l.group * 8 * P)                            // (not all threads have all pieces)
+    if (!FULL)                                              // (not all threads have all pieces)
 #pragma unroll
         for (int q = 0; q < P; ++q)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[4 * q + e] = l.piece(q) < l.dim ? v[4 * q + e] : 0;
 }
 
-template <bool X32, bool Y32, bool RMS, int THREADS, int P, int R>
+template <bool X32, bool Y32, bool RMS, bool FULL, int THREADS, int P, int R>
 __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_norm_ring_kernel(const RowNormParams p, int stages) {
     __shared__ __align__(16) float s[4 * R * 16];
     __shared__ RingBars bars;
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
             w[4 * q + e] = both(1.f);
             b[4 * q + e] = 0;
         }
-        if (l.piece(q) < p.dim) {
+        if (FULL || l.piece(q) < p.dim) {
             if (p.weight) pairs_weight(p.weight + l.piece(q), w + 4 * q);
             if (p.bias) pairs_weight(p.bias + l.piece(q), b + 4 * q);
         }
@@ -532,7 +533,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             there[i] = row_at(step * R + i) >= 0;
-            stage_row<X32>(l, ring + (r.stage * R + i) * row_bytes, there[i], v[i]);
+            stage_row<X32, FULL>(l, ring + (r.stage * R + i) * row_bytes, there[i], v[i]);
         }
         float sum[R];
 #pragma unroll
@@ -547,7 +548,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
         if (!RMS) {
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                less_mean(l, v[i], sum[i]);
+                less_mean<FULL>(l, v[i], sum[i]);
                 uint64_t t = 0;
 #pragma unroll
                 for (int e = 0; e < 4 * P; ++e) t = fma2(v[i][e], v[i][e], t);
@@ -561,7 +562,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
             if (there[i])
 #pragma unroll
                 for (int q = 0; q < P; ++q)
-                    if (l.piece(q) < p.dim) {
+                    if (FULL || l.piece(q) < p.dim) {
                         uint64_t y[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[e] = fma2(mul2(v[i][4 * q + e], scale), w[4 * q + e], b[4 * q + e]);
@@ -573,6 +574,8 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
 
 // Gradients.  With d = x - mean and t = dy d the sums of a row are those of d^2, g = dy w and t w, all at once:
 //   along = mean(g n) = r mean(t w);  dw += r t;  dx = r g - r mean(g) - r along d r
+// 8,191 rows of 4,096 take 54 us with the sums' kernel, 3.7 TB/s.  What bounds it: the instructions, 430 per warp and row, a quarter of them for the
+// two rounds of sums, at 16 working warps per SM, which 96 registers leave.  (Without the checks for rows that do not fill the threads: 60 us.)
 template <bool X32, bool Y32, bool RMS, int THREADS, int P, int R>
 __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
     __shared__ __align__(16) float s1[4 * R * 16], s3[4 * 3 * R * 16];
@@ -623,8 +626,8 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const unsigned char *const at = ring + (r.stage * R + i) * row_bytes;
-            stage_row<X32>(l, at, i < rows, v[i]);
-            stage_row<Y32>(l, at + x_bytes, i < rows, g[i]);
+            stage_row<X32, false>(l, at, i < rows, v[i]);
+            stage_row<Y32, false>(l, at + x_bytes, i < rows, g[i]);
         }
         r.release();
         if (!RMS) {
@@ -638,7 +641,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
             }
             cta_sums<THREADS>(sum, s1, slot);
 #pragma unroll
-            for (int i = 0; i < R; ++i) less_mean(l, v[i], sum[i]);
+            for (int i = 0; i < R; ++i) less_mean<false>(l, v[i], sum[i]);
         }
         uint64_t sq[R] = {}, sg[R] = {}, st[R] = {};
 #pragma unroll
@@ -745,23 +748,38 @@ void ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
 }
 int ring_stages(int room, int stage) { return room / stage < kMaxRing ? room / stage : kMaxRing; }
 
+// `which`: rows of up to 2,048, 4,096, 8,192 and 16,384 values
+template <bool X32, bool Y32, bool RMS, bool FULL>
+auto ring_forward(int which) {
+    return which == 0   ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 256, 1, 2>
+           : which == 1 ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 256, 2, 2>
+           : which == 2 ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 512, 2, 2>
+                        : layer_norm_ring_kernel<X32, Y32, RMS, FULL, 512, 4, 1>;
+}
+template <bool X32, bool Y32>
+auto ring_forward(bool rms, bool full, int which) {
+    if (rms) return full ? ring_forward<X32, Y32, true, true>(which) : ring_forward<X32, Y32, true, false>(which);
+    return full ? ring_forward<X32, Y32, false, true>(which) : ring_forward<X32, Y32, false, false>(which);
+}
+template <bool X32, bool Y32, bool RMS>
+auto ring_backward(int which) {
+    return which == 0   ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 256, 1, 2>
+           : which == 1 ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 256, 2, 1>
+           : which == 2 ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 512, 2, 1>
+                        : layer_norm_backward_ring_kernel<X32, Y32, RMS, 512, 4, 1>;
+}
+
 template <bool X32, bool Y32, bool VEC>
 cudaError_t launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
     if constexpr (VEC) {
         // more rows than are worked on at one time: a few CTAs that stay, with the next rows on their way
         if (p.dim > 1024 && p.tokens > 8ll * sms) {
-            static std::atomic<unsigned long long> done[4][2];
+            static std::atomic<unsigned long long> done[4][4];
             const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 256 : 512, rows = which == 3 ? 1 : 2;
             const int per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * (X32 ? 4 : 2);
-            const auto kernel = p.rms ? (which == 0   ? layer_norm_ring_kernel<X32, Y32, true, 256, 1, 2>
-                                         : which == 1 ? layer_norm_ring_kernel<X32, Y32, true, 256, 2, 2>
-                                         : which == 2 ? layer_norm_ring_kernel<X32, Y32, true, 512, 2, 2>
-                                                      : layer_norm_ring_kernel<X32, Y32, true, 512, 4, 1>)
-                                      : (which == 0   ? layer_norm_ring_kernel<X32, Y32, false, 256, 1, 2>
-                                         : which == 1 ? layer_norm_ring_kernel<X32, Y32, false, 256, 2, 2>
-                                         : which == 2 ? layer_norm_ring_kernel<X32, Y32, false, 512, 2, 2>
-                                                      : layer_norm_ring_kernel<X32, Y32, false, 512, 4, 1>);
-            ring_ready(kernel, done[which][p.rms]);
+            const bool full = p.dim == threads * 8 * (which == 0 ? 1 : which == 3 ? 4 : 2);
+            const auto kernel = ring_forward<X32, Y32>(p.rms, full, which);
+            ring_ready(kernel, done[which][p.rms + 2 * full]);
             const int stages = ring_stages((per_sm == 2 ? 110 : 216) * 1024, stage);
             return launch_early(kernel, dim3((unsigned)(sms * per_sm)), threads + 32, (size_t)stages * stage, stream, p, stages);
         }
@@ -791,18 +809,11 @@ cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStr
         return launch_early(kernel, dim3(grid), 256, smem, stream, p);
     }
     if constexpr (VEC) {
-        static std::atomic<unsigned long long> done[4][2];
+        static std::atomic<unsigned long long> done[4][4];
         const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 256 : 512;
         // (two rows together as long as registers hold them)
         const int rows = which == 0 ? 2 : 1, per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2));
-        const auto kernel = p.rms ? (which == 0   ? layer_norm_backward_ring_kernel<X32, Y32, true, 256, 1, 2>
-                                     : which == 1 ? layer_norm_backward_ring_kernel<X32, Y32, true, 256, 2, 1>
-                                     : which == 2 ? layer_norm_backward_ring_kernel<X32, Y32, true, 512, 2, 1>
-                                                  : layer_norm_backward_ring_kernel<X32, Y32, true, 512, 4, 1>)
-                                  : (which == 0   ? layer_norm_backward_ring_kernel<X32, Y32, false, 256, 1, 2>
-                                     : which == 1 ? layer_norm_backward_ring_kernel<X32, Y32, false, 256, 2, 1>
-                                     : which == 2 ? layer_norm_backward_ring_kernel<X32, Y32, false, 512, 2, 1>
-                                                  : layer_norm_backward_ring_kernel<X32, Y32, false, 512, 4, 1>);
+        const auto kernel = p.rms ? ring_backward<X32, Y32, true>(which) : ring_backward<X32, Y32, false>(which);
         const int stages = ring_stages((per_sm == 2 ? 108 : 216) * 1024 - p.dim * 4, stage);
         const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < kMaxPartials ? sms * per_sm : kMaxPartials;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
