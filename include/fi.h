@@ -668,12 +668,12 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
  *   preact [tokens x out_dim] bfloat16, nullable: x W^T + bias before the activation, which the gradients need.
  * Products on the tensor cores, sums in fp32; one rounding at the end.  A float32 out is summed up in pieces of about 512 values outside
  * of the tensor cores, which cut what they add (an error of some 2^-24 of the sum for 16 values).
- * in_dim and out_dim multiples of 8; rows of x and weight start on 16-byte boundaries; strides in elements.  Asynchronous, on the
- * current device; no workspace, so calls may overlap.  x and weight must not be written by the call's own results.
+ * in_dim and out_dim multiples of 8, they and tokens at most 2^30; rows of x and weight start on 16-byte boundaries; strides in elements.
+ * Asynchronous, on the current device; no workspace, so calls may overlap.  x and weight must not be written by the call's own results.
  *
  * fi_linear_backward: gradients for dy [tokens x out_dim] bfloat16 (of the result without its residual, whose gradient is dy itself):
  *   dz = dy act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over tokens of dz
- * dx, dweight bfloat16, dbias float; each nullable.  dz is rounded to bfloat16 for the products (2^-9 of each value), not for dbias;
+ * dx, dweight bfloat16, dbias float; each nullable.  dz is rounded to bfloat16 for the products (2^-8 of each value at most), not for dbias;
  * without an activation it is dy and preact is not read.  dbias is summed in a fixed order.  `workspace`: fi_linear_backward_workspace
  * bytes of device memory on a 16-byte boundary, contents free, not shared by calls that overlap; may be null without an activation.
  *

@@ -1013,8 +1013,8 @@ def _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dt
     out_dim = weight.size(0)
     x_stride = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
     weight_stride = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
-    if bias is not None:
-        _check_flat(bias, "bias", index, out_dim, torch.float32)
+    if bias is not None and (bias.dtype is not torch.float32 or bias.get_device() != index or bias.numel() != out_dim or not bias.is_contiguous()):
+        raise ValueError(f"bias must be a contiguous float32 tensor of {out_dim} values on cuda:{index}")
     if count is not None:
         _check_flat(count, "count", index, 1)
     if out_dtype is None:
@@ -1112,7 +1112,8 @@ def linear_poll_status(device: int = 0) -> None:
 def _as_rows(t: torch.Tensor) -> torch.Tensor:
     """t, or a copy that the kernels read: bfloat16 values of a row side by side, rows on 16-byte boundaries."""
     t = t.to(torch.bfloat16)
-    return t if t.stride(1) == 1 and t.stride(0) % 8 == 0 and t.stride(0) >= t.size(1) and t.data_ptr() % 16 == 0 else t.contiguous()
+    return t if t.stride(1) == 1 and t.stride(0) % 8 == 0 and t.stride(0) >= t.size(1) and t.data_ptr() % 16 == 0 \
+        else t.clone(memory_format=torch.contiguous_format)
 
 
 class _Linear(torch.autograd.Function):
@@ -1123,7 +1124,7 @@ class _Linear(torch.autograd.Function):
             preact = torch.empty((x.size(0), weight.size(0)), dtype=torch.bfloat16, device=x.device)
         y = _linear_call(x, weight, bias, activation, residual, None, None, None, out_dtype, preact, wait_limit)
         ctx.save_for_backward(x, weight, preact)
-        ctx.activation, ctx.with_bias = activation, bias is not None
+        ctx.activation, ctx.bias = activation, None if bias is None else bias.shape
         return y
 
     @staticmethod
@@ -1135,7 +1136,7 @@ class _Linear(torch.autograd.Function):
         if need[0] or need[1] or need[2]:
             dx, dw, db = linear_backward(x if need[1] else None, weight if need[0] else None, _as_rows(dy), preact=preact,
                                          activation=ctx.activation, with_bias=need[2])
-        return dx, dw, db, dy if need[3] else None, None, None, None
+        return dx, dw, None if db is None else db.view(ctx.bias), dy if need[3] else None, None, None, None
 
 
 def _norm_types(x: torch.Tensor, y_dtype, weight, bias, index: int):

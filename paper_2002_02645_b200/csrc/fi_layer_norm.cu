@@ -17,7 +17,8 @@ namespace fi {
 namespace {
 
 constexpr int kMaxDim = 16384;
-constexpr int kMaxPartials = 1024;     // CTAs of a backward pass, at most
+// CTAs of a backward pass, at most: so many sums of both weight gradients are in the workspace
+constexpr int max_partials(int dim) { return dim <= 2048 ? 640 : dim <= 4096 ? 320 : 160; }
 
 __device__ int32_t g_layer_norm_status;   // 1: a bounded wait ran out
 
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(c
 // ---- long rows on 16-byte boundaries ----
 //
 // A CTA walks over the rows, R at a time.  A warp of its own brings them by bulk copies into a ring of stages in shared memory, several
-// ahead of the ones that are worked on (issued by a thread that works on them they hold up all the others: 100 us, not 50, for 16,384
+// ahead of the ones that are worked on (issued by a thread that works on them they hold up all the others: 100 us, not 59, for 16,384
 // rows of 4,096).  Weights stay in registers, of the gradients in shared memory: the ring leaves L1 too small for them.
 // Values are worked on in pairs.
 constexpr int kMaxRing = 6;
@@ -799,7 +800,7 @@ cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStr
     if (p.dim <= 1024) {
         // no more CTAs than run at one time
         const int per_sm = p.dim <= 256 ? 3 : p.dim <= 512 ? 2 : 1;
-        const long long want = (p.tokens + 7) / 8, most = per_sm * sms < kMaxPartials ? per_sm * sms : kMaxPartials;
+        const long long want = (p.tokens + 7) / 8, most = per_sm * sms < max_partials(p.dim) ? per_sm * sms : max_partials(p.dim);
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
         const size_t smem = (size_t)8 * p.dim * sizeof(float);
         const auto kernel = p.dim <= 256   ? layer_norm_backward_kernel<X32, Y32, true, VEC, 1>
@@ -815,14 +816,14 @@ cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStr
         const int rows = which == 0 ? 2 : 1, per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2));
         const auto kernel = p.rms ? ring_backward<X32, Y32, true>(which) : ring_backward<X32, Y32, false>(which);
         const int stages = ring_stages((per_sm == 2 ? 108 : 216) * 1024 - p.dim * 4, stage);
-        const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < kMaxPartials ? sms * per_sm : kMaxPartials;
+        const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < max_partials(p.dim) ? sms * per_sm : max_partials(p.dim);
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
         ring_ready(kernel, done[which][p.rms]);
         *parts = (int)grid;
         return launch_early(kernel, dim3(grid), threads + 32, (size_t)stages * stage + p.dim * 4, stream, p, stages);
     }
     const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
-    const long long most = sms * (512 / threads) < kMaxPartials ? sms * (512 / threads) : kMaxPartials;
+    const long long most = sms * (512 / threads) < max_partials(p.dim) ? sms * (512 / threads) : max_partials(p.dim);
     const unsigned grid = (unsigned)(p.tokens < 1 ? 1 : p.tokens < most ? p.tokens : most);
     *parts = (int)grid;
     return launch_early(p.dim <= 8192 ? layer_norm_backward_kernel<X32, Y32, false, VEC, 2> : layer_norm_backward_kernel<X32, Y32, false, VEC, 4>, dim3(grid),
@@ -911,7 +912,7 @@ using namespace fi;
 
 extern "C" {
 
-int64_t fi_layer_norm_workspace(int32_t dim) { return dim < 1 || dim > kMaxDim ? 0 : (int64_t)kMaxPartials * 2 * dim * sizeof(float); }
+int64_t fi_layer_norm_workspace(int32_t dim) { return dim < 1 || dim > kMaxDim ? 0 : (int64_t)max_partials(dim) * 2 * dim * sizeof(float); }
 
 fi_status_t fi_layer_norm(const fi_layer_norm_t *a, void *cuda_stream) {
     fi_status_t st = check_args(a, false, "fi_layer_norm");

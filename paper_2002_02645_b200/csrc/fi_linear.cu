@@ -221,8 +221,8 @@ __device__ __forceinline__ void tmem_wait(uint32_t *v) {
                  :
                  : "memory");
 }
-// Exponential and reciprocal of the special-function unit (2^-22 of the result); the power unit takes a few clocks off the whole kernel for
-// every instruction more in here.
+// Exponential and reciprocal of the special-function unit (2^-22 of the result).  At full power the clock falls with every instruction that is
+// executed beside the products, so the activation is kept short (8,191 x 4,096 -> 16,384 and back with the library's erfcf: 909 us, so: 799).
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -371,9 +371,11 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 
-// Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction.  Sums of four rows go
-// to CTA (row / 4) mod split, which adds them up in the order of the ranks.  Bound by the latency from the launch to the last store, and by
-// the operands' way from memory: the loader sets up its barriers and has all stages on the way before the CTA has its TMEM.
+// Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction, so that the SMs have
+// work where the tiles alone are fewer than they are.  Sums of four rows go to CTA (row / 4) mod split, which adds them up in the order of
+// the ranks.  Bound by the latency from the launch to the last store (one token 2,048 -> 2,560: 8.8 us from one call to the next), and by the
+// operands' way from memory (48 tokens 4,096 -> 16,384: 28 us for 134 MB of weights, 4.8 TB/s): the loader sets up its barriers and has all
+// stages on the way before the CTA has its TMEM.
 template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
 __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                    const __grid_constant__ CUtensorMap map_b,
@@ -593,7 +595,7 @@ __device__ __forceinline__ void tile_place(int t, int row_tiles, int col_tiles, 
 }
 
 // 64 bytes of each of a warp's 32 rows on their way between registers (a thread has its row's) and memory, through 2 KB of shared memory: a
-// warp's access then covers 8 rows by 64 bytes, not 32 rows by 16 (float32 residual stream of 4,096 x 4,096 behind 4,096: 143 -> 114 us).
+// warp's access then covers 8 rows by 64 bytes, not 32 rows by 16 (8,192 x 8,192 -> 8,192 added to a float32 stream: 1,133 -> 899 us).
 __device__ __forceinline__ uint32_t turn_at(uint32_t base, int row, int piece) { return base + row * 64 + ((piece ^ (row >> 1 & 3)) << 4); }
 __device__ __forceinline__ void shared_store4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -729,6 +731,8 @@ struct TileWalk {
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
 // both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the reduction) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
+// Bound by the tensor cores and, in long runs, by the power that they draw: 4,096^3 takes 94 us, 1,460 TFLOP/s (tensor pipe 91 % active);
+// with float32 results, whose sums are added up outside of it, 104 us; 8,191 x 4,096 -> 16,384 651 to 665 us, 1,680 TFLOP/s.
 // JOBS = 2: a second product behind the first, whose rows' operand lies the other way round (the two gradients).
 template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, int JOBS>
 __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUtensorMap *maps_b, const LinearParams *jobs) {
@@ -1306,11 +1310,14 @@ fi_status_t launch_two(const Product &x, const Product &y, bool rows_mn, const D
                         dim3(2), stream, two);
 }
 
+constexpr long long kMostRows = 1 << 30;                    // (rows are indexed with int32, tiles may overshoot)
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 fi_status_t check_sizes(long long tokens, int in_dim, int out_dim, int act, const char *name) {
-    if (tokens < 0 || tokens > 2147483647ll || in_dim < 8 || in_dim % 8 || out_dim < 8 || out_dim % 8) {
-        set_error("%s: in_dim and out_dim must be multiples of 8, 0 <= tokens < 2^31 (got %lld tokens, %d -> %d)", name, tokens, in_dim, out_dim);
+    if (tokens < 0 || tokens > kMostRows || in_dim < 8 || in_dim % 8 || in_dim > kMostRows || out_dim < 8 || out_dim % 8 || out_dim > kMostRows) {
+        set_error("%s: in_dim and out_dim must be multiples of 8, and they and tokens at most 2^30 (got %lld tokens, %d -> %d)", name, tokens, in_dim,
+                  out_dim);
         return FI_ERR_INVALID_ARG;
     }
     if (act < FI_ACT_NONE || act > FI_ACT_SILU) {
@@ -1325,8 +1332,8 @@ bool tma_rows(const void *p, long long rows, long long dim, long long ld) {
     return aligned16(p) && (rows <= 1 || (ld % 8 == 0 && ld >= dim && ld < (1ll << 38)));
 }
 
-// CTAs of a cluster, which share the rows of `width` columns: up to eight, as many as run at one time (4,095 x 8,192 behind silu: 46 us with
-// 1,024 CTAs, 592 of which run together)
+// CTAs of a cluster, which share the rows of `width` columns: up to eight, as many as run at one time (4,095 x 8,192 behind silu: 41 us,
+// 4.9 TB/s; 46 with 1,024 CTAs, 592 of which run together)
 int slope_parts(long long tokens, int out_dim, int width, int sms) {
     const long long columns = (out_dim + width - 1) / width;
     int parts = 1;
@@ -1404,7 +1411,7 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
 }
 
 int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation) {
-    if (tokens < 0 || tokens > 2147483647ll || out_dim < 8) return 0;
+    if (tokens < 0 || tokens > kMostRows || out_dim < 8) return 0;
     return activation != FI_ACT_NONE ? (tokens * out_dim * 2 + 255) / 256 * 256 : 0;
 }
 

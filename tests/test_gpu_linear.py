@@ -218,6 +218,21 @@ def test_backward_large(tokens, n_in, n_out):
     check_backward(x, w, rand(gen, tokens, n_out).bfloat16(), rand(gen, tokens, n_out).bfloat16(), "gelu_tanh", True)
 
 
+@pytest.mark.parametrize("tokens,n_in,n_out", [(5000, 512, 6144), (7001, 1544, 520), (4104, 1024, 4096), (2056, 2048, 2056)])
+def test_both_gradients_whichever_sums_are_longer(tokens, n_in, n_out):
+    """Sizes at which both products are large: over the tokens (dweight) longer than over the outputs (dx), shorter, and alike."""
+    gen = torch.Generator(device=DEV).manual_seed(tokens)
+    x, w = operands(gen, tokens, n_in, n_out)
+    dy = rand(gen, tokens, n_out).bfloat16()
+    check_backward(x, w, dy, None, "none", False)
+    dx, dw, _ = fb.linear_backward(x, w, dy)
+    # each alone: two such results are twice their bound apart at most
+    for got, want, steps, left, right in ((fb.linear_backward(None, w, dy)[0], dx, n_out, dy, w), (fb.linear_backward(x, None, dy)[1], dw, tokens, dy.t(), x)):
+        size = want.double().abs()
+        within(got, want.double(), 1.01 * (2.0 ** -7 * size + 2 * (steps / 16 + 4) * 2.0 ** -23 * (left.double().abs() @ right.double().abs())) + 1e-37)
+    fb.linear_poll_status()
+
+
 def test_backward_of_extreme_preactivations():
     """Slopes that have reached 0 or 1 are that; nothing becomes NaN but what is NaN."""
     z = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 30.0, -30.0, 150.0, -150.0, 1e30, -1e30, math.inf, -math.inf, 5.0, -5.0, 19.0, -19.0], device=DEV)
@@ -285,6 +300,13 @@ def test_autograd(act):
     ones = torch.ones(77, 264, dtype=torch.bfloat16, device=DEV)
     fb.linear(x, w, bias, activation=act, preact=z)
     assert torch.equal(only.grad, fb.linear_backward(x, None, ones, preact=z, activation=act)[1])
+    # a bias of another shape; a gradient that starts off a 16-byte boundary
+    wide = bias[None].clone().requires_grad_(True)
+    y = fb.linear(x, only, wide, activation=act)
+    off = torch.empty(77 * 264 + 4, dtype=torch.bfloat16, device=DEV)[4:].view(77, 264).copy_(dy)
+    g = torch.autograd.grad(y, (only, wide), off)
+    want = fb.linear_backward(x, None, dy.bfloat16(), preact=z, activation=act, with_bias=True)
+    assert torch.equal(g[0], want[1]) and g[1].shape == wide.shape and torch.equal(g[1][0], want[2])
     for kw in (dict(out=torch.empty(77, 264, device=DEV)), dict(preact=z), dict(count=torch.ones(1, dtype=torch.int32, device=DEV))):
         with pytest.raises(ValueError, match="gradient"):
             fb.linear(x, only, **kw)
@@ -373,7 +395,8 @@ def test_refusals():
     unsound = [lambda: fb.linear(flat[4:260].view(4, 64), w), lambda: fb.linear(x[:, :60], w[:, :60]), lambda: fb.linear(x, w[:12]),
                lambda: fb.linear(torch.as_strided(flat, (4, 64), (60, 1)), w), lambda: fb.linear(torch.as_strided(flat, (4, 64), (32, 1)), w),
                lambda: fb.linear(x, w, out=torch.as_strided(torch.zeros(99, device=DEV), (4, 16), (8, 1))),
-               lambda: fb.linear_backward(flat[4:260].view(4, 64), w, dy), lambda: fb.linear(x, w, wait_limit=-1)]
+               lambda: fb.linear_backward(flat[4:260].view(4, 64), w, dy), lambda: fb.linear(x, w, wait_limit=-1),
+               lambda: fb.linear(x, w, residual=torch.zeros(1, 16, device=DEV).expand(4, 16), out_dtype=torch.float32)]
     for call in unsound:
         with pytest.raises(fb.FiError, match="INVALID"):
             call()

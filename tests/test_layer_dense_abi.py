@@ -62,7 +62,8 @@ def test_refusals_need_no_device():
         return lib.fi_linear(bytes(a), None)
 
     assert linear(tokens=0) == fb.FI_OK and linear(rows=1 << 23, out_rows=0) == fb.FI_OK      # nothing to do
-    for bad in (dict(in_dim=60), dict(in_dim=0), dict(out_dim=36), dict(tokens=-1), dict(tokens=1 << 31), dict(activation=5), dict(activation=-1),
+    for bad in (dict(in_dim=60), dict(in_dim=0), dict(out_dim=36), dict(tokens=-1), dict(tokens=1 << 31), dict(tokens=(1 << 30) + 1),
+                dict(in_dim=(1 << 30) + 8, x_stride=1 << 31, weight_stride=1 << 31), dict(out_dim=(1 << 30) + 8, out_stride=1 << 31), dict(activation=5), dict(activation=-1),
                 dict(out_dtype=2), dict(x=None), dict(weight=None), dict(out=None), dict(x=8), dict(x_stride=60), dict(x_stride=56),
                 dict(weight_stride=32), dict(out_stride=31), dict(out=(1 << 22) + 1), dict(residual=1 << 23, residual_stride=8), dict(bias=2),
                 dict(preact=1 << 23, preact_stride=8), dict(wait_limit=-1), dict(rows=1 << 23, out_rows=-1)):
@@ -82,4 +83,6 @@ def test_refusals_need_no_device():
         assert norm(True, **bad) == fb.FI_ERR_INVALID_ARG, bad
     assert lib.fi_layer_norm_workspace(0) == 0 and lib.fi_layer_norm_workspace(16385) == 0 and lib.fi_layer_norm_workspace(100) > 0
     assert lib.fi_linear_backward_workspace(10, 64, 0) == 0 and lib.fi_linear_backward_workspace(10, 64, 4) >= 1280
+    for dim, ctas in ((8, 444), (1024, 444), (2048, 592), (4096, 296), (16384, 148)):     # sums of as many CTAs as run at one time
+        assert 2 * 4 * dim * ctas <= lib.fi_layer_norm_workspace(dim) <= 21 << 20
     assert lib.fi_pages_compact_workspace(-1) == 0 and lib.fi_pages_compact_workspace(1000) >= 4 * 2000
