@@ -602,7 +602,7 @@ fi_status_t fi_kv_poll_status(fi_kv_t *kv);
  * fi_pages_compact: the pages in use move to the low end of the pool: those at or above the number of pages in use, in order, to the free
  * places below it, in order.  copies [max_copies x 3] as above (whole pages), max_copies >= num_pages / 2, moves [1] their number; entries
  * past it are (-1, -1, 0).  Rewritten in place: block_table (entries of pages in use), shared, and the free stack, lowest page on top.  Every
- * page must be in use or in the free stack.  workspace: fi_pages_compact_workspace(num_pages) bytes, contents free.
+ * page must be in use or in the free stack.  workspace: fi_pages_compact_workspace(num_pages) bytes, contents free.  num_pages <= 1048576.
  * fi_kv_copy_pages: copies what the listed tokens of pages hold, keys and values.  count [1] device int32, nullable: actual number of copies.
  * Entries with a negative source are skipped; pages outside the pool are skipped and reported by fi_kv_poll_status.  No page that is filled may
  * be listed again.

@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kPageThreads) pages_fork_kernel(const fi_pages
 
 // Every listed page loses an owner; one that had no other goes below 0 and is counted in its segment of 256 pages.  The last CTA then
 // takes the segments in order (a warp each), which puts the free pages in order of their numbers whatever the order of the atomics.  Bound by
-// the chain of its steps, most of it two sums over a CTA and the way to the last one: 13 us for 93 requests of up to 128 pages.
+// the chain of its steps, most of it two sums over a CTA and the way to the last one: 12 us for 93 requests of up to 128 pages.
 __global__ void __launch_bounds__(kPageThreads) pages_free_kernel(const fi_pages_free_t a, int page_shift, int max_blocks, uint32_t *ticket,
                                                                   int32_t *segments) {
     extern __shared__ long long s_cu[];
@@ -212,131 +212,92 @@ __global__ void __launch_bounds__(kPageThreads) pages_free_kernel(const fi_pages
     if (threadIdx.x == 0) *a.free_count_out = (int)min(free_count + total, (long long)a.num_pages);
 }
 
-// Workspace of a compaction, in words: [0] used pages, then a bit for each free page, the places to fill, the pages to move, and the new
-// name of each page that moves.
-struct CompactSpace {
-    int32_t *used;
-    uint32_t *is_free;
-    int32_t *holes, *high, *name;
-    int words;
-};
-__host__ __device__ inline CompactSpace compact_space(void *workspace, int num_pages) {
-    CompactSpace c;
-    const int words = (num_pages + 31) / 32, half = num_pages / 2 + 1;
-    int32_t *const w = static_cast<int32_t *>(workspace);
-    c.used = w;
-    c.is_free = reinterpret_cast<uint32_t *>(w + 32);
-    c.holes = w + 32 + words;
-    c.high = c.holes + half;
-    c.name = c.high + half;
-    c.words = words;
-    return c;
-}
+// Workspace of a compaction, in words: [0] used pages, from [32] on the new name of each page at or above that number, -1 where it keeps it.
+constexpr int kNamesAt = 32;
+constexpr int kCompactMost = 64, kCompactPages = 2048;     // CTAs of a compaction, and pages for each of them (beyond 131,072 pages: more)
 
-constexpr int kCompactCtas = 8;        // one cluster: its barrier stands between the steps
-
-__device__ __forceinline__ void cluster_barrier() {
-    __threadfence();
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// Used pages at or above the number of used pages, in order, get the free places below it, in order.  One cluster takes all steps: bits
-// of the free pages, their number, ranks, moves; then the free stack is rewritten, lowest number on top.  Bound by six barriers of the cluster
-// one after another and what is read between them: 15 us for 5,224 pages.
-__global__ void __cluster_dims__(kCompactCtas, 1, 1) __launch_bounds__(kPageThreads) pages_compact_kernel(const fi_pages_compact_t a, int page_size) {
+// Used pages at or above the number of used pages, in order, get the free places below it, in order.  Every CTA has a bit for each page in
+// its shared memory and counts all of them for itself, so that nothing is waited for between CTAs; each then takes its share of the moves.
+// Bound by the chain of loads, two sums over the CTA and stores: 9.5 us for 5,224 pages (a cluster that shared bits in global memory between
+// six barriers: 15.9).  The free stack is read here by all, and rewritten by the kernel behind this one.
+__global__ void __launch_bounds__(kPageThreads) pages_compact_kernel(const fi_pages_compact_t a, int page_size, int share) {
+    extern __shared__ uint32_t s_free[];                     // a bit for each free page; then the pages to fill and to move of this CTA's share
     in_turn();
-    const CompactSpace c = compact_space(a.workspace, a.num_pages);
-    const int threads = kCompactCtas * kPageThreads, tid = blockIdx.x * kPageThreads + threadIdx.x;
-    __shared__ long long s_counts;
+    const int words = (a.num_pages + 31) / 32, tid = threadIdx.x;
+    int32_t *const s_hole = reinterpret_cast<int32_t *>(s_free + words), *const s_high = s_hole + share;
+    int32_t *const name = static_cast<int32_t *>(a.workspace) + kNamesAt;
     const int free_count = min(max(*a.free_count, 0), a.num_pages);
-    for (int w = tid; w < c.words; w += threads) c.is_free[w] = 0;
-    cluster_barrier();
-    for (int i = tid; i < free_count; i += threads) {
-        const int page = a.free_pages[i];
-        if (page >= 0 && page < a.num_pages) atomicOr(c.is_free + (page >> 5), 1u << (page & 31));
+    for (int w = tid; w < words; w += kPageThreads) s_free[w] = 0;
+    __syncthreads();
+    for (int i0 = tid; i0 < a.num_pages; i0 += 4 * kPageThreads) {
+        int page[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) page[e] = i0 + e * kPageThreads < a.num_pages ? a.free_pages[i0 + e * kPageThreads] : -1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i0 + e * kPageThreads < free_count && page[e] >= 0 && page[e] < a.num_pages) atomicOr(s_free + (page[e] >> 5), 1u << (page[e] & 31));
     }
-    cluster_barrier();
-    // each CTA a run of words, each thread a run of those
-    const int run = (c.words + threads - 1) / threads, first = min(tid * run, c.words), last = min(first + run, c.words);
-    const auto bits = [&](int w) { return __ldcg(c.is_free + w); };
-    const auto valid = [&](int w) { return w * 32 + 32 <= a.num_pages ? 0xffffffffu : (1u << (a.num_pages & 31)) - 1; };
+    __syncthreads();
+    // each thread a run of words
+    const int run = (words + kPageThreads - 1) / kPageThreads, first = min(tid * run, words), last = min(first + run, words);
     long long mine = 0, all;
-    for (int w = first; w < last; ++w) mine += __popc(bits(w));
+    for (int w = first; w < last; ++w) mine += __popc(s_free[w]);
     block_exclusive(mine, &all);
-    const auto from_all = [&](long long v) {                  // sum over the CTAs before this one in the low, over all in the high half
-        if (threadIdx.x == 0) s_counts = v;
-        cluster_barrier();
-        long long before = 0, total = 0;
-        uint32_t at = (uint32_t)__cvta_generic_to_shared(&s_counts);
-        for (int r = 0; r < kCompactCtas; ++r) {
-            uint32_t there;
-            long long x;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(r));
-            asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(x) : "r"(there) : "memory");
-            if (r < (int)blockIdx.x) before += x;
-            total += x;
-        }
-        cluster_barrier();                                     // (nobody writes or leaves before all have read)
-        return longlong2{before, total};
-    };
-    const int used = a.num_pages - (int)from_all(all).y;
-    // bits of word w that are places to fill, and pages to move
+    const int used = a.num_pages - (int)all;
+    // bits of word w that are below `used`, and that are pages
     const auto low = [&](int w) { return w * 32 + 32 <= used ? 0xffffffffu : w * 32 >= used ? 0u : (1u << (used & 31)) - 1; };
+    const auto valid = [&](int w) { return w * 32 + 32 <= a.num_pages ? 0xffffffffu : (1u << (a.num_pages & 31)) - 1; };
+    // places to fill in the low, pages to move in the high half
     mine = 0;
-    for (int w = first; w < last; ++w) {
-        const uint32_t f = bits(w);
-        mine += (long long)__popc(f & low(w)) | (long long)__popc(~f & ~low(w) & valid(w)) << 32;
-    }
-    const long long in_cta = block_exclusive(mine, &all);
-    const longlong2 sums = from_all(all);
-    long long at = sums.x + in_cta;
+    for (int w = first; w < last; ++w)
+        mine += (long long)__popc(s_free[w] & low(w)) | (long long)__popc(~s_free[w] & ~low(w) & valid(w)) << 32;
+    const long long at = block_exclusive(mine, &all);
     int hole = (int)(at & 0xffffffffll), high = (int)(at >> 32);
-    const int moves = min((int)(sums.y & 0xffffffffll), (int)(sums.y >> 32));
+    const int moves = min((int)(all & 0xffffffffll), (int)(all >> 32)), k0 = blockIdx.x * share, k1 = min(k0 + share, moves);
     for (int w = first; w < last; ++w) {
-        const uint32_t f = bits(w);
-        for (uint32_t m = f & low(w); m; m &= m - 1) {
-            if (hole <= a.num_pages / 2) c.holes[hole] = w * 32 + __ffs(m) - 1;
-            ++hole;
-        }
-        for (uint32_t m = ~f & ~low(w) & valid(w); m; m &= m - 1) {
-            if (high <= a.num_pages / 2) c.high[high] = w * 32 + __ffs(m) - 1;
-            ++high;
-        }
+        const uint32_t f = s_free[w];
+        for (uint32_t m = f & low(w); m; m &= m - 1, ++hole)
+            if (hole >= k0 && hole < k1) s_hole[hole - k0] = w * 32 + __ffs(m) - 1;
+        for (uint32_t m = ~f & ~low(w) & valid(w); m; m &= m - 1, ++high)
+            if (high >= k0 && high < k1) s_high[high - k0] = w * 32 + __ffs(m) - 1;
+            else if (high >= moves && blockIdx.x == 0) name[w * 32 + __ffs(m) - 1] = -1;       // (a stack that was not one)
+        if (w % gridDim.x == blockIdx.x)
+            for (uint32_t m = f & ~low(w); m; m &= m - 1) name[w * 32 + __ffs(m) - 1] = -1;
     }
-    if (tid == 0) {
-        *c.used = used;
+    if (blockIdx.x == 0 && tid == 0) {
+        *static_cast<int32_t *>(a.workspace) = used;
         *a.moves = moves;
     }
-    cluster_barrier();
-    for (int k = tid; k < a.max_copies; k += threads) {
-        int src = -1, dst = -1;
-        if (k < moves) {
-            src = __ldcg(c.high + k);
-            dst = __ldcg(c.holes + k);
-            c.name[src] = dst;
-            a.shared[dst] = a.shared[src];
-            a.shared[src] = 0;
-        }
+    __syncthreads();
+    for (int k = k0 + tid; k < k1; k += kPageThreads) {
+        const int src = s_high[k - k0], dst = s_hole[k - k0];
+        name[src] = dst;
+        a.shared[dst] = a.shared[src];
+        a.shared[src] = 0;
         a.copies[3ll * k] = src;
         a.copies[3ll * k + 1] = dst;
-        a.copies[3ll * k + 2] = k < moves ? page_size : 0;
+        a.copies[3ll * k + 2] = page_size;
     }
-    for (int i = tid; i < free_count; i += threads) a.free_pages[i] = a.num_pages - 1 - i;
+    for (long long k = moves + (long long)blockIdx.x * kPageThreads + tid; k < a.max_copies; k += (long long)gridDim.x * kPageThreads) {
+        a.copies[3 * k] = a.copies[3 * k + 1] = -1;
+        a.copies[3 * k + 2] = 0;
+    }
 }
 
-// The new names of the pages that moved, in the rows' entries.
+// The new names of the pages that moved, in the rows' entries; and the free stack, lowest number on top.
 __global__ void __launch_bounds__(256) pages_rename_kernel(const fi_pages_compact_t a, int page_shift, int max_blocks) {
     in_turn();
-    const CompactSpace c = compact_space(a.workspace, a.num_pages);
-    const int used = *c.used;
+    const int used = *static_cast<const int32_t *>(a.workspace), free_count = min(max(*a.free_count, 0), a.num_pages);
+    const int32_t *const name = static_cast<const int32_t *>(a.workspace) + kNamesAt;
     for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int blocks = (int)min(((long long)max(a.lens[row], 0) + (1ll << page_shift) - 1) >> page_shift, (long long)max_blocks);
         int32_t *const entries = a.block_table + (long long)row * a.table_ld;
         for (int j = threadIdx.x; j < blocks; j += 256) {
-            const int page = entries[j];
-            if (page >= used && page < a.num_pages && !(c.is_free[page >> 5] >> (page & 31) & 1)) entries[j] = c.name[page];
+            const int page = entries[j], to = page >= used && page < a.num_pages ? name[page] : -1;
+            if (to >= 0) entries[j] = to;
         }
     }
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < free_count; i += gridDim.x * 256) a.free_pages[i] = a.num_pages - 1 - i;
 }
 
 struct CopyPools {
@@ -347,9 +308,10 @@ struct CopyPools {
     int32_t *status;
 };
 
-// A warp per page and head: codes of keys and values in pieces of 16 bytes, 4 + 4 on the way per lane, and their pairs beside them.  Bound
-// by the traffic, twice what the tokens take.
-__global__ void __launch_bounds__(256) kv_copy_pages_kernel(const CopyPools p, const int32_t *copies, const int32_t *count_dev, int most) {
+// A warp per page and head: codes of keys and values in pieces of 16 bytes, 2 + 2 on the way per lane, and their pairs beside them.  Bound
+// by the traffic, twice what the tokens take, and by two round trips (1,300 pages of 16 tokens and 8 heads of 128: 9.7 us, 22 MB; with 4 + 4
+// pieces, of which such a page has 2 + 2, in 80 registers 13.1).
+__global__ void __launch_bounds__(256, 4) kv_copy_pages_kernel(const CopyPools p, const int32_t *copies, const int32_t *count_dev, int most) {
     in_turn();
     const int n = actual_count(count_dev, most), lane = threadIdx.x & 31;
     const long long units = (long long)n * p.heads, step = (long long)gridDim.x * 8;
@@ -370,11 +332,11 @@ __global__ void __launch_bounds__(256) kv_copy_pages_kernel(const CopyPools p, c
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind)
             if (first) m[kind] = p.meta[kind][mfrom + lane * p.mts];
-        for (int q0 = lane; q0 < pieces; q0 += 128) {
-            uint4 v[2][4];
-            long long at[4];
+        for (int q0 = lane; q0 < pieces; q0 += 64) {
+            uint4 v[2][2];
+            long long at[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < 2; ++e) {
                 const int q = q0 + 32 * e, token = q / p.pieces;
                 at[e] = token * p.ts + (q - token * p.pieces) * 16ll;
                 if (q < pieces) {
@@ -383,7 +345,7 @@ __global__ void __launch_bounds__(256) kv_copy_pages_kernel(const CopyPools p, c
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < 2; ++e)
                 if (q0 + 32 * e < pieces) {
                     *reinterpret_cast<uint4 *>(p.codes[0] + to + at[e]) = v[0][e];
                     *reinterpret_cast<uint4 *>(p.codes[1] + to + at[e]) = v[1][e];
@@ -426,6 +388,7 @@ int shift_of(int page_size) {
 cudaError_t prepare_pages_share() {
     cudaError_t e = cudaFuncSetAttribute(pages_fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 16);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_free_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPageMaxBatch * 12);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(pages_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
     return e;
 }
 
@@ -488,7 +451,7 @@ fi_status_t fi_pages_free(fi_pages_t *p, const fi_pages_free_t *a, void *cuda_st
 
 int64_t fi_pages_compact_workspace(int32_t num_pages) {
     if (num_pages < 0) return 0;
-    return 4 * (32 + ((int64_t)num_pages + 31) / 32 + 2 * ((int64_t)num_pages / 2 + 1) + num_pages);
+    return 4 * (kNamesAt + (int64_t)num_pages);
 }
 
 fi_status_t fi_pages_compact(fi_pages_t *p, const fi_pages_compact_t *a, void *cuda_stream) {
@@ -496,8 +459,10 @@ fi_status_t fi_pages_compact(fi_pages_t *p, const fi_pages_compact_t *a, void *c
         set_error("fi_pages_compact: null argument");
         return FI_ERR_INVALID_ARG;
     }
-    if (a->rows < 0 || a->num_pages < 0 || a->max_copies < a->num_pages / 2 || a->table_ld < p->cfg.max_blocks) {
-        set_error("fi_pages_compact: a negative size, room for fewer copies than half the pages, or table_ld below max_blocks");
+    if (a->rows < 0 || a->num_pages < 0 || a->num_pages > kPageSegments << kSegmentShift || a->max_copies < a->num_pages / 2 ||
+        a->table_ld < p->cfg.max_blocks) {
+        set_error("fi_pages_compact: a negative size, more than %d pages, room for fewer copies than half of them, or table_ld below max_blocks",
+                  kPageSegments << kSegmentShift);
         return FI_ERR_INVALID_ARG;
     }
     if ((a->rows > 0 && (!a->lens || !a->block_table)) || (a->num_pages > 0 && (!a->free_pages || !a->shared)) || !a->free_count || !a->moves ||
@@ -508,10 +473,14 @@ fi_status_t fi_pages_compact(fi_pages_t *p, const fi_pages_compact_t *a, void *c
     DeviceGuard guard(p->cfg.device);
     if (!guard.ok) return cuda_fail(cudaErrorInvalidDevice, "fi_pages_compact");
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t e = launch_early(pages_compact_kernel, kCompactCtas, kPageThreads, 0, stream, *a, p->cfg.page_size);
-    if (e == cudaSuccess && a->rows > 0)
-        e = launch_early(pages_rename_kernel, a->rows < 8 * p->sm_count ? a->rows : 8 * p->sm_count, 256, 0, stream, *a, shift_of(p->cfg.page_size),
-                         p->cfg.max_blocks);
+    int ctas = (a->num_pages + kCompactPages - 1) / kCompactPages;
+    ctas = ctas < 1 ? 1 : ctas > kCompactMost ? kCompactMost : ctas;
+    const int share = (a->num_pages / 2 + ctas - 1) / ctas;
+    cudaError_t e = launch_early(pages_compact_kernel, ctas, kPageThreads, ((size_t)(a->num_pages + 31) / 32 + 2 * (size_t)share) * 4, stream, *a,
+                                 p->cfg.page_size, share);
+    if (e == cudaSuccess)
+        e = launch_early(pages_rename_kernel, a->rows < 1 ? 1 : a->rows < 8 * p->sm_count ? a->rows : 8 * p->sm_count, 256, 0, stream, *a,
+                         shift_of(p->cfg.page_size), p->cfg.max_blocks);
     return e == cudaSuccess ? FI_OK : cuda_fail(e, "fi_pages_compact");
 }
 

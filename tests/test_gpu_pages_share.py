@@ -245,6 +245,23 @@ def test_compact_of_nothing_and_everything():
     d.compact()
 
 
+@pytest.mark.parametrize("pages", [4095, 4097, 70001, 200000])
+@pytest.mark.parametrize("share", [0.02, 0.5, 0.97])
+def test_compact_of_large_pools(pages, share):
+    """Pools for many CTAs, a few or nearly all of their pages free, in any order."""
+    rng = random.Random(pages)
+    m = Model(rows=20, blocks=60, pages=pages, page=16)
+    m.free = rng.sample(range(pages), int(share * pages))
+    left = sorted(set(range(pages)) - set(m.free))
+    for r in range(20):
+        m.lens[r] = rng.randint(0, 960)
+        m.table[r] = [rng.choice(left) for _ in range(60)]
+    m.shared = [0 if p % 3 else p % 7 for p in range(pages)]
+    for p in m.free:
+        m.shared[p] = 0
+    Device(m).compact()
+
+
 def pools(gen, pages, heads, page, dim):
     codes = lambda: torch.randint(0, 256, (pages, heads, page, dim // 2), generator=gen, device=DEV, dtype=torch.uint8)
     meta = lambda: torch.randn(pages, heads, page, 2, generator=gen, device=DEV).bfloat16()
@@ -370,7 +387,8 @@ def test_refusals():
     for call in bad:
         with pytest.raises(ValueError):
             call()
-    five = ints([0, 1, 2, 3, 0])
-    for call in (lambda: d.h.fork(five, five, *state, d.shared), lambda: d.h.free(five, *state, d.shared)):
+    five, many = ints([0, 1, 2, 3, 0]), torch.zeros(1048577, dtype=torch.int32, device=DEV)
+    for call in (lambda: d.h.fork(five, five, *state, d.shared), lambda: d.h.free(five, *state, d.shared),
+                 lambda: d.h.free(rows, d.lens, many, d.count, d.table, many.clone()), lambda: d.h.compact(d.lens, many, d.count, d.table, many.clone())):
         with pytest.raises(fb.FiError, match="INVALID"):
             call()
