@@ -1186,42 +1186,79 @@ fi_status_t operand_map(CUtensorMap *map, const Matrix &x, int box_rows, const c
     return FI_OK;
 }
 
-// Which kernel, and its tiles.  Estimates in SM cycles: 16 x 256 x 256 products of a pair take 128 cycles (a CTA's 16 x 128 x 256 as
-// many), an SM gets about 75 bytes a cycle from L2, the device about 3,400 from memory; the way out of a split tile goes
-// through another CTA.  (256 tokens 4,096 -> 4,096: pairs of 64 columns 20.5 us, 4 CTAs for 128 x 256 24.6; 128 tokens: 20.5 and, 4 CTAs for
-// 128 x 128, 18.4.)
+// Which kernel, and its tiles: the one with the least estimated cycles.  The tensor cores take 16 x 256 x 256 products of a pair in 128 cycles (a
+// CTA's 16 x 128 x 256 in as many), an SM gets 80 bytes a cycle from L2 where pairs ask for them and 55 where single CTAs do, all together
+// 8,600, and the device 5,000 from memory and what L2 still has; a tile's way out is hidden behind the next one of a pair, but for a fifth
+// of it.  These figures and the ways out are fitted to the times of 212 products in all their forms (1 to 8,192 tokens, 80 to 8,192 values,
+// both types): what is taken is 0.9 % slower than the best form of each in the mean, 15 % at most.  (Both sides, us: 777 x 512 -> 2,048:
+// pairs of 128 columns 6.3, CTAs with 96 tokens 8.8; 32 x 4,096 -> 4,096: clusters of 4 9.5, single CTAs 11.3; 4,000 x 768 <- 768: pairs
+// 9.3, CTAs 14.2; 200 x 8,192 -> 2,048 in float32: clusters of 4 18.4, pairs 25.3.)
 struct LinearPlan {
     bool pair;
     int tile_n, split;
     double cycles;
 };
 
+double most(double a, double b) { return a > b ? a : b; }
+long long up(long long a, long long b) { return (a + b - 1) / b; }
+
+// what a product of m columns, n rows and kb blocks has to move, in cycles: from memory, and from L2 in tiles
+double memory_cycles(double m, double n, double kb, int size) { return ((m + n) * kb * (kKb * 2) + m * n * size) / 5000.; }
+double tile_traffic(double m, double n, double kb, double m_tiles, double n_tiles) { return (m_tiles * n + n_tiles * m) * kb * (kKb * 2) / 8600.; }
+
+struct PairCost {
+    double tiles, each, least, end;                         // a tile's cycles; what the traffic takes at least; the last way out
+};
+PairCost pair_cost(long long m, long long n, long long kb, int tile, bool f32, int size) {
+    const double m_tiles = (double)up(m, tile), n_tiles = (double)up(n, 2 * kM), end = 2500 + (f32 ? 20. : 12.) * tile;
+    const double each = most(kb * most(2. * tile, (128 + tile / 2) * 128 / 80.), 0.8 * end);
+    return {m_tiles * n_tiles, each, most(memory_cycles((double)m, (double)n, (double)kb, size), tile_traffic((double)m, (double)n, (double)kb, m_tiles, n_tiles)), end};
+}
+
 LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool f32, int size, const int *clusters) {
     LinearPlan best = {false, 16, 1, 1e30};
-    const auto most = [](double a, double b) { return a > b ? a : b; };
-    const auto up = [](long long a, long long b) { return (a + b - 1) / b; };
-    const double memory = ((double)m * kb * 128 + (double)n * kb * 128 + (double)m * n * size) / 3400.;
     for (int tile = 64; tile <= kMaxN; tile += 64) {          // (a warp takes 32 columns of a half at a time)
         if ((a_mn && tile % 128) || (f32 && tile > kMaxPairN32)) continue;
-        const double block = most(2. * tile, (128 + tile / 2) * 128 / 75.), rounds = (double)up(up(n, 2 * kM) * up(m, tile), clusters[1]);
-        const double cycles = most(rounds * kb * block, memory) + 2500 + 20. * tile;
+        const PairCost c = pair_cost(m, n, kb, tile, f32, size);
+        const double cycles = most((double)up((long long)c.tiles, clusters[1]) * c.each, c.least) + c.end;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
     }
+    const double memory = memory_cycles((double)m, (double)n, (double)kb, size), weights = (double)m * kb * (kKb * 2);
     for (int tile = 16; tile <= kMaxN; tile += 16) {
         if (tile > 16 && tile - 16 >= n) break;
+        const double m_tiles = (double)up(m, kM), n_tiles = (double)up(n, tile), block = most(2. * tile, (128 + tile) * 128 / 55.);
+        // columns' operand (weights) that L2 does not hold is read again for every tile of rows
+        const double again = weights > 64e6 ? (n_tiles - 1) * weights / 3400. : 0;
+        const double least = most(memory + again, tile_traffic((double)m, (double)n, (double)kb, m_tiles, n_tiles));
         for (int i = 0; i < 4 && 1 << i <= kb; ++i) {
-            const int split = 1 << i;
-            const long long blocks = up(kb, split);
+            const long long blocks = up(kb, 1 << i);
             if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 512 values have an accumulator each
-            const double block = most(2. * tile, (128 + tile) * 128 / 75.), rounds = (double)up(up(m, kM) * up(n, tile), clusters[i]);
-            const double end = split > 1 ? 4000 + 30. * tile : 2500 + 20. * tile;
-            // columns' operand (weights) that L2 does not hold is read again for every tile of rows
-            const double again = (double)m * kb * 128 > 64e6 ? (up(n, tile) - 1) * ((double)m * kb * 128 / 3400.) : 0;
-            const double cycles = most(rounds * (blocks * block + end), memory + again + end);
-            if (cycles < best.cycles) best = {false, tile, split, cycles};
+            const double rounds = (double)up(up(m, kM) * up(n, tile), clusters[i]), end = i ? 2800 + 40. * tile : 6000 + 20. * tile;
+            const double cycles = most(rounds * (blocks * block + end) - end, least) + end;
+            if (cycles < best.cycles) best = {false, tile, 1 << i, cycles};
         }
     }
     return best;
+}
+
+// two blocks a stage where the products of one are over before the next is issued (430 cycles: 16 x 256 x 128 take 64)
+int stage_blocks(const LinearPlan &plan, long long kb) { return plan.tile_n <= 128 && kb > 1 ? 2 : 1; }
+
+// Both gradients (m columns each) as two launches, or in one by pairs with tiles of one size, which share the SMs without a gap between them.
+// (777 tokens, 1,000 -> 1,400: 13.1 us together, one after the other 20.1 as pairs and 22.)
+void plan_two(long long m, long long n0, long long kb0, long long n1, long long kb1, const int *clusters, LinearPlan &x, LinearPlan &y) {
+    x = plan_product(m, n0, kb0, true, false, 2, clusters);
+    y = plan_product(m, n1, kb1, true, false, 2, clusters);
+    double least = x.cycles + y.cycles;
+    for (int tile = 128; tile <= kMaxN; tile += 128) {
+        const PairCost a = pair_cost(m, n0, kb0, tile, false, 2), b = pair_cost(m, n1, kb1, tile, false, 2);
+        const double work = most((a.tiles * a.each + b.tiles * b.each) / clusters[1], most(a.each, b.each)), cycles = most(work, a.least + b.least) + a.end;
+        const LinearPlan plan = {true, tile, 1, cycles};
+        if (cycles < least && stage_blocks(plan, kb0) == stage_blocks(plan, kb1)) {
+            least = cycles;
+            x = y = plan;
+        }
+    }
 }
 
 // A product that is ready to be launched
@@ -1234,15 +1271,13 @@ struct Product {
 };
 
 // D[n][m] = sum over k of A(m, k) B(n, k); x.p holds what becomes of the sums
-fi_status_t plan_launch(Product &x, const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32,
-                        const DeviceFacts &facts, const char *name) {
+fi_status_t plan_launch(Product &x, const LinearPlan &plan, const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k,
+                        bool f32, const char *name) {
     LinearParams &p = x.p;
     p.m = (int)m;
     p.n = (int)n;
-    p.kb = (int)((k + kKb - 1) / kKb);
-    const LinearPlan plan = plan_product(m, n, p.kb, a_mn, f32, f32 ? 4 : 2, facts.clusters);
-    // two blocks a stage where the products of one are over before the next is issued (430 cycles: 16 x 256 x 128 take 64)
-    const int depth = plan.tile_n <= 128 && p.kb > 1 ? 2 : 1, blocks = p.kb;
+    p.kb = (int)up(k, kKb);
+    const int depth = stage_blocks(plan, p.kb), blocks = p.kb;
     p.kb = (p.kb + depth - 1) / depth;
     p.tile_n = plan.tile_n;
     p.split = plan.split;
@@ -1283,16 +1318,20 @@ fi_status_t plan_launch(Product &x, const Matrix &a, bool a_mn, const Matrix &b,
     return st;
 }
 
-fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act,
-                           const LinearParams &what, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
-    Product x;
-    x.p = what;
-    const fi_status_t st = plan_launch(x, a, a_mn, b, b_mn, m, n, k, f32, facts, name);
-    if (st != FI_OK) return st;
+fi_status_t launch_planned(const Product &x, bool a_mn, bool b_mn, bool f32, int act, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
     const bool pair = x.plan.pair;
     const long long ctas = pair ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * x.p.split;
     return launch_early(name, linear_kernel(pair, x.depth, f32, act, a_mn, b_mn), dim3((unsigned)ctas), kThreads, x.smem, dim3(pair ? 2 : x.p.split), stream,
                         x.map_a, x.map_b, x.p);
+}
+
+fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act,
+                           const LinearParams &what, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
+    Product x;
+    x.p = what;
+    const LinearPlan plan = plan_product(m, n, up(k, kKb), a_mn, f32, f32 ? 4 : 2, facts.clusters);
+    const fi_status_t st = plan_launch(x, plan, a, a_mn, b, b_mn, m, n, k, f32, name);
+    return st == FI_OK ? launch_planned(x, a_mn, b_mn, f32, act, facts, stream, name) : st;
 }
 
 // Two products of pairs in one launch, the one with the longer reduction first; their tiles and stages are the same.
@@ -1475,11 +1514,15 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         Product px, pw;
         px.p = dx;
         pw.p = dw;
-        st = plan_launch(px, w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, *facts, name);
-        if (st == FI_OK) st = plan_launch(pw, x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, *facts, name);
+        LinearPlan plan_x, plan_w;
+        plan_two(a->in_dim, a->tokens, up(a->out_dim, kKb), a->out_dim, up(a->tokens, kKb), facts->clusters, plan_x, plan_w);
+        st = plan_launch(px, plan_x, w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, name);
+        if (st == FI_OK) st = plan_launch(pw, plan_w, x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, name);
         if (st != FI_OK) return st;
-        if (px.plan.pair && pw.plan.pair && px.plan.tile_n == pw.plan.tile_n && px.depth == pw.depth)
+        if (plan_x.pair && plan_w.pair && plan_x.tile_n == plan_w.tile_n && px.depth == pw.depth)
             return px.p.kb >= pw.p.kb ? launch_two(px, pw, false, *facts, stream, name) : launch_two(pw, px, true, *facts, stream, name);
+        st = launch_planned(px, true, false, false, FI_ACT_NONE, *facts, stream, name);
+        return st == FI_OK ? launch_planned(pw, true, true, false, FI_ACT_NONE, *facts, stream, name) : st;
     }
     if (a->dx) st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, dx, *facts, stream, name);
     if (st == FI_OK && a->dweight)
