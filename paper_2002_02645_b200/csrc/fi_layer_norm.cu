@@ -3,7 +3,7 @@
 //   n = (x - mean) r, r = 1 / sqrt(mean((x - mean)^2) + eps);  y = n w + b        (rms: mean taken as 0)
 //   backward:  g = dy w;  dx = r (g - mean(g) - n mean(g n));  dw = sum dy n, db = sum dy        (rms: without mean(g))
 //
-// A row is held in registers by a warp (up to 1,024 values) or a CTA, so that it is read once, its deviations are squared after the
+// A row is held in registers by a warp or a part of one (up to 1,024 values) or by a CTA, so that it is read once, its deviations are squared after the
 // mean is known, and it is written once: the bound is the traffic.  Nothing of the forward pass is kept for the gradients; mean
 // and r come again from x, which they read anyway.
 #include <cuda_bf16.h>
@@ -159,18 +159,20 @@ __device__ __forceinline__ void with_weight(const Place<VEC, P> &l, const float 
     }
 }
 
+// sums over neighbouring lanes, a power of two of them
+template <int LANES = 32>
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
-// sums over the group: a warp, or the CTA (every warp adds up the warps' sums in the same order).  `slot`: one of four places in
+// sums over the group: LANES of a warp, or (0) the CTA (every warp adds up the warps' sums in the same order).  `slot`: one of four places in
 // turn, so that one barrier a sum is enough
-template <bool WARP, int N>
+template <int LANES, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float (*s)[32][2], int &slot) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-    if constexpr (!WARP) {
+    for (int i = 0; i < N; ++i) v[i] = warp_sum<LANES ? LANES : 32>(v[i]);
+    if constexpr (!LANES) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
         if (lane == 0)
 #pragma unroll
@@ -183,13 +185,13 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float (*s)[32][2], int 
 }
 
 // mean and r of the row in v; v becomes x - mean
-template <bool WARP, bool VEC, int P>
+template <int LANES, bool VEC, int P>
 __device__ __forceinline__ float deviations(const RowNormParams &p, const Place<VEC, P> &l, float (&v)[8 * P], float (*s)[32][2], int &slot) {
     if (!p.rms) {
         float sum[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < 8 * P; ++i) sum[0] += v[i];
-        group_sum<WARP>(sum, s, slot);
+        group_sum<LANES>(sum, s, slot);
         const float mean = sum[0] / (float)p.dim;           // (divided: equal values have no deviation)
 #pragma unroll
         for (int i = 0; i < 8 * P; ++i) v[i] = l.has(i) ? v[i] - mean : 0.f;
@@ -197,7 +199,7 @@ __device__ __forceinline__ float deviations(const RowNormParams &p, const Place<
     float sq[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < 8 * P; ++i) sq[0] = fmaf(v[i], v[i], sq[0]);
-    group_sum<WARP>(sq, s, slot);
+    group_sum<LANES>(sq, s, slot);
     return rsqrtf(fmaf(sq[0], p.inv_dim, p.eps));
 }
 
@@ -214,19 +216,23 @@ __device__ __forceinline__ void in_turn() {
     cudaTriggerProgrammaticLaunchCompletion();
 }
 
-template <bool X32, bool Y32, bool WARP, bool VEC, int P>
-__global__ void __launch_bounds__(WARP ? 128 : 512) layer_norm_kernel(const RowNormParams p) {
+// A row per group of LANES lanes (few enough that a short row leaves none of them idle: 262,144 rows of 64 values in bfloat16 take 20 us, with a
+// warp each 70), or (0) of the CTA's threads.  Groups without a row take part in the sums.
+template <bool X32, bool Y32, int LANES, bool VEC, int P>
+__global__ void __launch_bounds__(LANES ? 128 : 512) layer_norm_kernel(const RowNormParams p) {
     __shared__ float s[4][32][2];
     in_turn();
     int slot = 0;
-    const Place<VEC, P> l = {WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x, WARP ? 32 : (int)blockDim.x, p.dim};
-    const long long token = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-    if (token >= actual_tokens(p)) return;                  // (the whole group)
-    const long long row = p.rows ? p.rows[token] : token;
-    if (row < 0 || row >= p.x_rows) return;
-    float v[8 * P];
-    load_row<X32>(l, p.x, row * p.x_stride, v);
-    const float r = deviations<WARP>(p, l, v, s, slot);
+    const Place<VEC, P> l = {LANES ? (int)threadIdx.x & (LANES - 1) : (int)threadIdx.x, LANES ? LANES : (int)blockDim.x, p.dim};
+    const long long token = LANES ? (long long)blockIdx.x * (128 / (LANES ? LANES : 1)) + threadIdx.x / (LANES ? LANES : 1) : blockIdx.x;
+    long long row = -1;
+    if (token < actual_tokens(p)) row = p.rows ? p.rows[token] : token;
+    const bool there = row >= 0 && row < p.x_rows;
+    if ((LANES == 0 || LANES == 32) && !there) return;
+    float v[8 * P] = {};
+    if (there) load_row<X32>(l, p.x, row * p.x_stride, v);
+    const float r = deviations<LANES>(p, l, v, s, slot);
+    if (!there) return;
     if (p.weight) with_weight(l, p.weight, [&](int i, float w) { v[i] = v[i] * r * w; });
     else
 #pragma unroll
@@ -236,21 +242,27 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) layer_norm_kernel(const RowN
 }
 
 // Rows are dealt out to the groups of the grid in turn; a thread gathers its columns of both weight gradients over all of them.
-template <bool X32, bool Y32, bool WARP, bool VEC, int P>
-__global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(const RowNormParams p) {
+template <bool X32, bool Y32, int LANES, bool VEC, int P>
+__global__ void __launch_bounds__(LANES ? 256 : 512) layer_norm_backward_kernel(const RowNormParams p) {
     constexpr int V = 8 * P;
     __shared__ float s[4][32][2];
-    extern __shared__ float sums[];                         // WARP: [warps][dim]
+    extern __shared__ float sums[];                         // LANES: [groups][dim]
     in_turn();
     int slot = 0;
-    const Place<VEC, P> l = {WARP ? (int)(threadIdx.x & 31) : (int)threadIdx.x, WARP ? 32 : (int)blockDim.x, p.dim};
-    const int groups_here = WARP ? blockDim.x >> 5 : 1, mine = WARP ? threadIdx.x >> 5 : 0;
+    const Place<VEC, P> l = {LANES ? (int)threadIdx.x & (LANES - 1) : (int)threadIdx.x, LANES ? LANES : (int)blockDim.x, p.dim};
+    const int groups_here = LANES ? 256 / (LANES ? LANES : 1) : 1, mine = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
+    const int warp_first = LANES ? (threadIdx.x >> 5) * (32 / (LANES ? LANES : 32)) : 0;
     float dw[V] = {}, db[V] = {};
-    for (long long row = (long long)blockIdx.x * groups_here + mine; row < p.tokens; row += (long long)gridDim.x * groups_here) {
-        float v[V], g[V];
-        load_row<X32>(l, p.x, row * p.x_stride, v);
-        load_row<Y32>(l, p.dy, row * p.dy_stride, g);
-        const float r = deviations<WARP>(p, l, v, s, slot);
+    for (long long row0 = (long long)blockIdx.x * groups_here; row0 + warp_first < p.tokens; row0 += (long long)gridDim.x * groups_here) {
+        const long long row = row0 + mine;
+        const bool there = LANES == 0 || LANES == 32 || row < p.tokens;
+        float v[V] = {}, g[V] = {};
+        if (there) {
+            load_row<X32>(l, p.x, row * p.x_stride, v);
+            load_row<Y32>(l, p.dy, row * p.dy_stride, g);
+        }
+        float r = deviations<LANES>(p, l, v, s, slot);
+        if (!there) r = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             v[i] *= r;                                      // n
@@ -264,15 +276,15 @@ __global__ void __launch_bounds__(WARP ? 256 : 512) layer_norm_backward_kernel(c
             both[0] += g[i];
             both[1] = fmaf(g[i], v[i], both[1]);
         }
-        group_sum<WARP>(both, s, slot);
+        group_sum<LANES>(both, s, slot);
         const float less = p.rms ? 0.f : both[0] * p.inv_dim, along = both[1] * p.inv_dim;
 #pragma unroll
         for (int i = 0; i < V; ++i) g[i] = r * (g[i] - less - v[i] * along);
-        store_row<X32>(l, p.out, row * p.out_stride, g);
+        if (there) store_row<X32>(l, p.out, row * p.out_stride, g);
     }
     if (!p.partial) return;
     float *const to = p.partial + (long long)blockIdx.x * 2 * p.dim;
-    if constexpr (!WARP) {
+    if constexpr (!LANES) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (l.has(i)) {
@@ -475,7 +487,7 @@ __device__ __forceinline__ void less_mean(const Place<true, P> &l, uint64_t (&v)
 }
 
 template <bool X32, bool Y32, bool RMS, bool FULL, int THREADS, int P, int R>
-__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_norm_ring_kernel(const RowNormParams p, int stages) {
+__global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_ring_kernel(const RowNormParams p, int stages) {
     __shared__ __align__(16) float s[4 * R * 16];
     __shared__ RingBars bars;
     extern __shared__ __align__(128) unsigned char ring[];
@@ -578,7 +590,7 @@ __global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_no
 // 8,191 rows of 4,096 take 54 us with the sums' kernel, 3.7 TB/s.  What bounds it: the instructions, 430 per warp and row, a quarter of them for the
 // two rounds of sums, at 16 working warps per SM, which 96 registers leave.  (Without the checks for rows that do not fill the threads: 60 us.)
 template <bool X32, bool Y32, bool RMS, int THREADS, int P, int R>
-__global__ void __launch_bounds__(THREADS + 32, THREADS == 256 ? 2 : 1) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
+__global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
     __shared__ __align__(16) float s1[4 * R * 16], s3[4 * 3 * R * 16];
     __shared__ RingBars bars;
     extern __shared__ __align__(128) unsigned char raw[];
@@ -749,10 +761,11 @@ void ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
 }
 int ring_stages(int room, int stage) { return room / stage < kMaxRing ? room / stage : kMaxRing; }
 
-// `which`: rows of up to 2,048, 4,096, 8,192 and 16,384 values
+// `which`: rows of up to (-1, gradients only: 1,024) 2,048, 4,096, 8,192 and 16,384 values.  512 working threads an SM; a row's warps have all
+// pieces of the row or nearly: four CTAs of 128 threads for 2,048 values take 48 us for 32,768 rows, two of 256 threads 70.
 template <bool X32, bool Y32, bool RMS, bool FULL>
 auto ring_forward(int which) {
-    return which == 0   ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 256, 1, 2>
+    return which == 0   ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 128, 2, 2>
            : which == 1 ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 256, 2, 2>
            : which == 2 ? layer_norm_ring_kernel<X32, Y32, RMS, FULL, 512, 2, 2>
                         : layer_norm_ring_kernel<X32, Y32, RMS, FULL, 512, 4, 1>;
@@ -764,11 +777,17 @@ auto ring_forward(bool rms, bool full, int which) {
 }
 template <bool X32, bool Y32, bool RMS>
 auto ring_backward(int which) {
-    return which == 0   ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 256, 1, 2>
+    return which < 0    ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 128, 1, 2>
+           : which == 0 ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 128, 2, 1>
            : which == 1 ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 256, 2, 1>
            : which == 2 ? layer_norm_backward_ring_kernel<X32, Y32, RMS, 512, 2, 1>
                         : layer_norm_backward_ring_kernel<X32, Y32, RMS, 512, 4, 1>;
 }
+
+// lanes that have a row's values, 8 each (up to 256 values), 16 or 32
+int lanes_of(int dim) { return dim <= 32 ? 4 : dim <= 64 ? 8 : dim <= 128 ? 16 : 32; }
+// threads that have them, 8 `pieces` each
+int threads_of(int dim, int pieces) { return (dim + pieces * 256 - 1) / (pieces * 256) * 32; }
 
 template <bool X32, bool Y32, bool VEC>
 cudaError_t launch_forward(const RowNormParams &p, int sms, cudaStream_t stream) {
@@ -776,58 +795,78 @@ cudaError_t launch_forward(const RowNormParams &p, int sms, cudaStream_t stream)
         // more rows than are worked on at one time: a few CTAs that stay, with the next rows on their way
         if (p.dim > 1024 && p.tokens > 8ll * sms) {
             static std::atomic<unsigned long long> done[4][4];
-            const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 256 : 512, rows = which == 3 ? 1 : 2;
-            const int per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * (X32 ? 4 : 2);
-            const bool full = p.dim == threads * 8 * (which == 0 ? 1 : which == 3 ? 4 : 2);
+            const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 128 << which : 512, rows = which == 3 ? 1 : 2;
+            const int per_sm = 512 / threads, stage = rows * p.dim * (X32 ? 4 : 2);
+            const bool full = p.dim == threads * 8 * (which == 3 ? 4 : 2);
             const auto kernel = ring_forward<X32, Y32>(p.rms, full, which);
             ring_ready(kernel, done[which][p.rms + 2 * full]);
-            const int stages = ring_stages((per_sm == 2 ? 110 : 216) * 1024, stage);
+            const int stages = ring_stages((220 / per_sm - 1) * 1024, stage);
             return launch_early(kernel, dim3((unsigned)(sms * per_sm)), threads + 32, (size_t)stages * stage, stream, p, stages);
         }
     }
     if (p.dim <= 1024) {
-        const auto kernel = p.dim <= 256   ? layer_norm_kernel<X32, Y32, true, VEC, 1>
-                            : p.dim <= 512 ? layer_norm_kernel<X32, Y32, true, VEC, 2>
-                                           : layer_norm_kernel<X32, Y32, true, VEC, 4>;
-        return launch_early(kernel, dim3((unsigned)((p.tokens + 3) / 4)), 128, 0, stream, p);
+        const int lanes = lanes_of(p.dim);
+        const auto kernel = lanes == 4      ? layer_norm_kernel<X32, Y32, 4, VEC, 1>
+                            : lanes == 8    ? layer_norm_kernel<X32, Y32, 8, VEC, 1>
+                            : lanes == 16   ? layer_norm_kernel<X32, Y32, 16, VEC, 1>
+                            : p.dim <= 256  ? layer_norm_kernel<X32, Y32, 32, VEC, 1>
+                            : p.dim <= 512  ? layer_norm_kernel<X32, Y32, 32, VEC, 2>
+                                            : layer_norm_kernel<X32, Y32, 32, VEC, 4>;
+        const int rows = 128 / lanes;
+        return launch_early(kernel, dim3((unsigned)((p.tokens + rows - 1) / rows)), 128, 0, stream, p);
     }
-    const int threads = p.dim <= 4096 ? 128 : p.dim <= 8192 ? 256 : 512;
-    return launch_early(layer_norm_kernel<X32, Y32, false, VEC, 4>, dim3((unsigned)p.tokens), threads, 0, stream, p);
+    if constexpr (!VEC) {
+        const int pieces = p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 4;
+        return launch_early(pieces == 1   ? layer_norm_kernel<X32, Y32, 0, VEC, 1>
+                            : pieces == 2 ? layer_norm_kernel<X32, Y32, 0, VEC, 2>
+                                          : layer_norm_kernel<X32, Y32, 0, VEC, 4>,
+                            dim3((unsigned)p.tokens), threads_of(p.dim, pieces), 0, stream, p);
+    } else {
+        const int threads = p.dim <= 4096 ? 128 : p.dim <= 8192 ? 256 : 512;
+        return launch_early(layer_norm_kernel<X32, Y32, 0, VEC, 4>, dim3((unsigned)p.tokens), threads, 0, stream, p);
+    }
 }
 
 template <bool X32, bool Y32, bool VEC>
 cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStream_t stream) {
-    if (p.dim <= 1024) {
+    // Short rows: a warp's or a part of one's.  From 513 values on the ring is faster where rows lie on 16-byte boundaries (65,536 of 1,024: 103 us,
+    // with a warp each, whose 64 sums a lane leave room for 8 warps an SM, 115).
+    if (p.dim <= (VEC ? 512 : 1024)) {
         // no more CTAs than run at one time
-        const int per_sm = p.dim <= 256 ? 3 : p.dim <= 512 ? 2 : 1;
-        const long long want = (p.tokens + 7) / 8, most = per_sm * sms < max_partials(p.dim) ? per_sm * sms : max_partials(p.dim);
+        const int lanes = lanes_of(p.dim), rows = 256 / lanes, per_sm = p.dim <= 256 ? 3 : p.dim <= 512 ? 2 : 1;
+        const long long want = (p.tokens + rows - 1) / rows, most = per_sm * sms < max_partials(p.dim) ? per_sm * sms : max_partials(p.dim);
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
-        const size_t smem = (size_t)8 * p.dim * sizeof(float);
-        const auto kernel = p.dim <= 256   ? layer_norm_backward_kernel<X32, Y32, true, VEC, 1>
-                            : p.dim <= 512 ? layer_norm_backward_kernel<X32, Y32, true, VEC, 2>
-                                           : layer_norm_backward_kernel<X32, Y32, true, VEC, 4>;
+        const size_t smem = (size_t)rows * p.dim * sizeof(float);
+        const auto kernel = lanes == 4      ? layer_norm_backward_kernel<X32, Y32, 4, VEC, 1>
+                            : lanes == 8    ? layer_norm_backward_kernel<X32, Y32, 8, VEC, 1>
+                            : lanes == 16   ? layer_norm_backward_kernel<X32, Y32, 16, VEC, 1>
+                            : p.dim <= 256  ? layer_norm_backward_kernel<X32, Y32, 32, VEC, 1>
+                            : p.dim <= 512  ? layer_norm_backward_kernel<X32, Y32, 32, VEC, 2>
+                                            : layer_norm_backward_kernel<X32, Y32, 32, VEC, VEC ? 2 : 4>;
         *parts = (int)grid;
         return launch_early(kernel, dim3(grid), 256, smem, stream, p);
     }
     if constexpr (VEC) {
-        static std::atomic<unsigned long long> done[4][4];
-        const int which = p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 2 ? 256 : 512;
-        // (two rows together as long as registers hold them)
-        const int rows = which == 0 ? 2 : 1, per_sm = which < 2 ? 2 : 1, stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2));
+        static std::atomic<unsigned long long> done[5][2];
+        const int which = p.dim <= 1024 ? -1 : p.dim <= 2048 ? 0 : p.dim <= 4096 ? 1 : p.dim <= 8192 ? 2 : 3, threads = which < 0 ? 128 : which < 2 ? 128 << which : 512;
+        const int per_sm = 512 / threads, rows = which < 0 ? 2 : 1, stage = rows * p.dim * ((X32 ? 4 : 2) + (Y32 ? 4 : 2));
         const auto kernel = p.rms ? ring_backward<X32, Y32, true>(which) : ring_backward<X32, Y32, false>(which);
-        const int stages = ring_stages((per_sm == 2 ? 108 : 216) * 1024 - p.dim * 4, stage);
-        const long long want = (p.tokens + rows - 1) / rows, most = sms * per_sm < max_partials(p.dim) ? sms * per_sm : max_partials(p.dim);
+        const int stages = ring_stages((220 / per_sm - 2) * 1024 - p.dim * 4, stage);
+        const long long most = sms * per_sm < max_partials(p.dim) ? sms * per_sm : max_partials(p.dim);
+        const long long want = (p.tokens + rows - 1) / rows;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
-        ring_ready(kernel, done[which][p.rms]);
+        ring_ready(kernel, done[which + 1][p.rms]);
         *parts = (int)grid;
         return launch_early(kernel, dim3(grid), threads + 32, (size_t)stages * stage + p.dim * 4, stream, p, stages);
     }
-    const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
-    const long long most = sms * (512 / threads) < max_partials(p.dim) ? sms * (512 / threads) : max_partials(p.dim);
-    const unsigned grid = (unsigned)(p.tokens < 1 ? 1 : p.tokens < most ? p.tokens : most);
-    *parts = (int)grid;
-    return launch_early(p.dim <= 8192 ? layer_norm_backward_kernel<X32, Y32, false, VEC, 2> : layer_norm_backward_kernel<X32, Y32, false, VEC, 4>, dim3(grid),
-                        threads, 0, stream, p);
+    if constexpr (!VEC) {
+        const int threads = p.dim <= 2048 ? 128 : p.dim <= 4096 ? 256 : 512;
+        const long long most = sms * (512 / threads) < max_partials(p.dim) ? sms * (512 / threads) : max_partials(p.dim);
+        const unsigned grid = (unsigned)(p.tokens < 1 ? 1 : p.tokens < most ? p.tokens : most);
+        *parts = (int)grid;
+        return launch_early(p.dim <= 8192 ? layer_norm_backward_kernel<X32, Y32, 0, VEC, 2> : layer_norm_backward_kernel<X32, Y32, 0, VEC, 4>, dim3(grid),
+                            threads, 0, stream, p);
+    }
 }
 
 template <typename F>

@@ -149,6 +149,40 @@ def test_rows_and_count(tokens, alive, dim):
         assert (y == 7).all() if n < 0 else not (y[rows[:1].long()] == 7).all()
 
 
+@pytest.mark.parametrize("dim", [5, 8, 24, 32, 40, 64, 100, 128, 136])
+@pytest.mark.parametrize("tokens", [1, 3, 17, 5001])
+def test_short_rows_side_by_side(tokens, dim):
+    """Rows that share a warp: one of NaN, one outside of x and the places past the last row leave the others as they are, also without eps."""
+    gen = torch.Generator(device=DEV).manual_seed(dim)
+    x, w, b, dy = rand(gen, tokens, dim), 1 + 0.2 * rand(gen, dim), rand(gen, dim), rand(gen, tokens, dim)
+    for rms in (False, True):
+        check_backward(x, w, dy, rms, 0.0, True)
+        want, bound = forward(x, w, b, rms, 0.0, torch.float32)
+        rows = torch.arange(tokens, device=DEV).int()
+        bad = torch.arange(tokens, device=DEV) % 3 == 1
+        rows[bad] = tokens
+        y = fb.layer_norm(x, w, b, eps=0.0, rms=rms, rows=rows, out=torch.full((tokens, dim), 7.0, device=DEV))
+        within(y[~bad], want[~bad], bound[~bad])
+        assert (y[bad] == 7).all()
+        z = x.clone()
+        z[bad] = math.nan
+        y = fb.layer_norm(z, w, b, eps=0.0, rms=rms)
+        within(y[~bad], want[~bad], bound[~bad])
+        assert y[bad].isnan().all()
+        dx = fb.layer_norm_backward(z, w, dy, eps=0.0, rms=rms)[0]
+        assert dx[bad].isnan().all() and torch.equal(dx[~bad], fb.layer_norm_backward(x, w, dy, eps=0.0, rms=rms)[0][~bad])
+
+
+@pytest.mark.parametrize("tokens,dim", [(9000, 1024), (1, 520), (4001, 776), (7000, 2048), (4999, 1032), (3000, 1500), (1500, 4100)])
+def test_more_rows_than_run_at_one_time(tokens, dim):
+    gen = torch.Generator(device=DEV).manual_seed(dim)
+    for types, rms in ((TYPES[0], False), (TYPES[-1], True)):
+        x, w, b = rand(gen, tokens, dim).to(types[0]), 1 + 0.2 * rand(gen, dim), rand(gen, dim)
+        within(fb.layer_norm(x, w, b, rms=rms, out_dtype=types[1]), *forward(x, w, b, rms, 1e-5, types[1]))
+        check_backward(x, w, rand(gen, tokens, dim).to(types[1]), rms, 1e-5, True)
+    fb.layer_norm_poll_status()
+
+
 def test_strides_alignment_and_in_place():
     gen = torch.Generator(device=DEV).manual_seed(4)
     wide, wb = rand(gen, 40, 1300), rand(gen, 2101)
