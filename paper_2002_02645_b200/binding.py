@@ -818,10 +818,11 @@ class KvTables:
         _check_flat(shared, "shared", index, free_pages.numel())
         _check_flat(batch_count, "batch_count", index, 1)
         if out is None:
-            out = lens.new_empty(rows + 1).split_with_sizes([rows, 1])
-        lens_out, count_out = out
-        _check_flat(lens_out, "out[0]", index, rows)
-        _check_flat(count_out, "out[1]", index, 1)
+            out = lens_out, count_out = lens.new_empty(rows + 1).split_with_sizes([rows, 1])
+        else:
+            lens_out, count_out = out
+            _check_flat(lens_out, "out[0]", index, rows)
+            _check_flat(count_out, "out[1]", index, 1)
         args = _pack_free(row_idx.data_ptr(), _at(batch_count), lens.data_ptr(), block_table.data_ptr(), free_count.data_ptr(), free_pages.data_ptr(),
                           shared.data_ptr(), lens_out.data_ptr(), count_out.data_ptr(), block_table.stride(0), rows, free_pages.numel(), row_idx.numel())
         st = self._lib.fi_pages_free(self._h, args, _raw_stream(index))
@@ -836,11 +837,12 @@ class KvTables:
         rows, index = self._check_state(lens, free_pages, free_count, block_table), self._index
         pages = free_pages.numel()
         _check_flat(shared, "shared", index, pages)
-        most, space = pages // 2, self._lib.fi_pages_compact_workspace(pages) // 4
-        copies, moves, work = lens.new_empty(3 * most + 1 + space).split_with_sizes([3 * most, 1, space])
-        copies = copies.view(most, 3)
-        args = _pack_compact(lens.data_ptr(), free_count.data_ptr(), free_pages.data_ptr(), block_table.data_ptr(), shared.data_ptr(), copies.data_ptr(),
-                             moves.data_ptr(), work.data_ptr(), block_table.stride(0), rows, pages, most)
+        most = pages // 2
+        words = lens.new_empty(3 * most + 1 + self._lib.fi_pages_compact_workspace(pages) // 4)      # copies, moves, workspace
+        at = words.data_ptr()
+        copies, moves = words.as_strided((most, 3), (3, 1)), words.as_strided((1,), (1,), 3 * most)
+        args = _pack_compact(lens.data_ptr(), free_count.data_ptr(), free_pages.data_ptr(), block_table.data_ptr(), shared.data_ptr(), at,
+                             at + 12 * most, at + 12 * most + 4, block_table.stride(0), rows, pages, most)
         st = self._lib.fi_pages_compact(self._h, args, _raw_stream(index))
         if st:
             _check(st)
@@ -1078,15 +1080,17 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
     if weight is not None:
         strides[1] = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
         if dx is None:
-            dx = dy.new_empty((tokens, in_dim))
-        strides[4] = _check_rows(dx, "dx", index, torch.bfloat16, tokens, in_dim)
+            dx, strides[4] = dy.new_empty((tokens, in_dim)), in_dim
+        else:
+            strides[4] = _check_rows(dx, "dx", index, torch.bfloat16, tokens, in_dim)
     elif dx is not None:
         raise ValueError("dx needs weight")
     if x is not None:
         strides[0] = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
         if dweight is None:
-            dweight = dy.new_empty((out_dim, in_dim))
-        strides[5] = _check_rows(dweight, "dweight", index, torch.bfloat16, out_dim, in_dim)
+            dweight, strides[5] = dy.new_empty((out_dim, in_dim)), in_dim
+        else:
+            strides[5] = _check_rows(dweight, "dweight", index, torch.bfloat16, out_dim, in_dim)
     elif dweight is not None:
         raise ValueError("dweight needs x")
     if kind:
@@ -1188,6 +1192,9 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out)
 
 
+_layer_norm_work = {}      # values of fi_layer_norm_workspace by dim
+
+
 def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: torch.Tensor, *, eps: float = 1e-5, rms: bool = False,
                         with_bias: bool = False, dx: Optional[torch.Tensor] = None):
     """fi_layer_norm_backward: (dx, dweight, dbias) from the forward pass's x and weight and the gradient of its result.  Without a weight
@@ -1197,13 +1204,21 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
     tokens, dim = x.shape
     x_stride, dy_stride = _check_rows(x, "x", index, x.dtype, tokens, dim), _check_rows(dy, "dy", index, dy.dtype, tokens, dim)
     if dx is None:
-        dx = x.new_empty((tokens, dim))
-    dx_stride = _check_rows(dx, "dx", index, x.dtype, tokens, dim)
-    dw = weight.new_empty(dim) if weight is not None else None
-    db = x.new_empty(dim, dtype=torch.float32) if with_bias else None
-    work = None
-    if dw is not None or db is not None:
-        work = x.new_empty(lib.fi_layer_norm_workspace(dim), dtype=torch.uint8)
+        dx, dx_stride = x.new_empty((tokens, dim)), dim
+    else:
+        dx_stride = _check_rows(dx, "dx", index, x.dtype, tokens, dim)
+    dw = db = work = None
+    if weight is not None or with_bias:
+        work = _layer_norm_work.get(dim)
+        if work is None:
+            work = _layer_norm_work[dim] = lib.fi_layer_norm_workspace(dim) // 4
+        if weight is not None:
+            dw = weight.new_empty(dim)
+            work = weight.new_empty(work)
+        else:
+            work = x.new_empty(work, dtype=torch.float32)
+        if with_bias:
+            db = work.new_empty(dim)
     args = _pack_layer_norm(x.data_ptr(), dy.data_ptr(), dx.data_ptr(), _at(weight), 0, 0, 0, _at(dw), _at(db), _at(work), x_stride, dy_stride, dx_stride,
                             tokens, 0, dim, 1 if rms else 0, *kinds, eps)
     _on_device(index, lib.fi_layer_norm_backward, args)
