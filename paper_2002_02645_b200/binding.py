@@ -1013,7 +1013,9 @@ def _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dt
         raise ValueError("x must be bfloat16 [tokens, in_dim] on a GPU, weight [out_dim, in_dim]")
     tokens, in_dim = x.shape
     out_dim = weight.size(0)
-    x_stride = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
+    x_stride, side_by_side = x.stride()
+    if side_by_side != 1 and in_dim > 1:
+        raise ValueError("x: the values of a row must lie side by side")
     weight_stride = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
     if bias is not None and (bias.dtype is not torch.float32 or bias.get_device() != index or bias.numel() != out_dim or not bias.is_contiguous()):
         raise ValueError(f"bias must be a contiguous float32 tensor of {out_dim} values on cuda:{index}")
@@ -1161,7 +1163,9 @@ def _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out):
         out_dtype = x.dtype if out is None else out.dtype
     kinds = _norm_types(x, out_dtype, weight, bias, index)
     x_rows, dim = x.shape
-    x_stride = _check_rows(x, "x", index, x.dtype, x_rows, dim)
+    x_stride, side_by_side = x.stride()
+    if side_by_side != 1 and dim > 1:
+        raise ValueError("x: the values of a row must lie side by side")
     tokens = x_rows
     if rows is not None:
         _check_flat(rows, "rows", index)

@@ -1201,6 +1201,12 @@ struct LinearPlan {
 
 double most(double a, double b) { return a > b ? a : b; }
 long long up(long long a, long long b) { return (a + b - 1) / b; }
+// the same of whole numbers below 2^53, without the long division of whole numbers (a plan has some hundred of them)
+double times(double a, double b) {
+    const double q = a / b;
+    const long long i = (long long)q;
+    return (double)(i + ((double)i * b < a));
+}
 
 // what a product of m columns, n rows and kb blocks has to move, in cycles: from memory, and from L2 in tiles
 double memory_cycles(double m, double n, double kb, int size) { return ((m + n) * kb * (kKb * 2) + m * n * size) / 5000.; }
@@ -1210,7 +1216,7 @@ struct PairCost {
     double tiles, each, least, end;                         // a tile's cycles; what the traffic takes at least; the last way out
 };
 PairCost pair_cost(long long m, long long n, long long kb, int tile, bool f32, int size) {
-    const double m_tiles = (double)up(m, tile), n_tiles = (double)up(n, 2 * kM), end = 2500 + (f32 ? 20. : 12.) * tile;
+    const double m_tiles = times((double)m, tile), n_tiles = (double)up(n, 2 * kM), end = 2500 + (f32 ? 20. : 12.) * tile;
     const double each = most(kb * most(2. * tile, (128 + tile / 2) * 128 / 80.), 0.8 * end);
     return {m_tiles * n_tiles, each, most(memory_cycles((double)m, (double)n, (double)kb, size), tile_traffic((double)m, (double)n, (double)kb, m_tiles, n_tiles)), end};
 }
@@ -1220,21 +1226,21 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
     for (int tile = 64; tile <= kMaxN; tile += 64) {          // (a warp takes 32 columns of a half at a time)
         if ((a_mn && tile % 128) || (f32 && tile > kMaxPairN32)) continue;
         const PairCost c = pair_cost(m, n, kb, tile, f32, size);
-        const double cycles = most((double)up((long long)c.tiles, clusters[1]) * c.each, c.least) + c.end;
+        const double cycles = most(times(c.tiles, clusters[1]) * c.each, c.least) + c.end;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
     }
-    const double memory = memory_cycles((double)m, (double)n, (double)kb, size), weights = (double)m * kb * (kKb * 2);
+    const double memory = memory_cycles((double)m, (double)n, (double)kb, size), weights = (double)m * kb * (kKb * 2), m_tiles = (double)up(m, kM);
     for (int tile = 16; tile <= kMaxN; tile += 16) {
         if (tile > 16 && tile - 16 >= n) break;
-        const double m_tiles = (double)up(m, kM), n_tiles = (double)up(n, tile), block = most(2. * tile, (128 + tile) * 128 / 55.);
+        const double n_tiles = times((double)n, tile), block = most(2. * tile, (128 + tile) * 128 / 55.);
         // columns' operand (weights) that L2 does not hold is read again for every tile of rows
         const double again = weights > 64e6 ? (n_tiles - 1) * weights / 3400. : 0;
         const double least = most(memory + again, tile_traffic((double)m, (double)n, (double)kb, m_tiles, n_tiles));
         for (int i = 0; i < 4 && 1 << i <= kb; ++i) {
-            const long long blocks = up(kb, 1 << i);
-            if (f32 && up(blocks, kPiece) * tile > 512 && tile > 16) continue; // pieces of 512 values have an accumulator each
-            const double rounds = (double)up(up(m, kM) * up(n, tile), clusters[i]), end = i ? 2800 + 40. * tile : 6000 + 20. * tile;
-            const double cycles = most(rounds * (blocks * block + end) - end, least) + end;
+            const long long blocks = (kb + (1 << i) - 1) >> i;
+            if (f32 && (blocks + kPiece - 1) / kPiece * tile > 512 && tile > 16) continue;   // pieces of 512 values have an accumulator each
+            const double rounds = times(m_tiles * n_tiles, clusters[i]), end = i ? 2800 + 40. * tile : 6000 + 20. * tile;
+            const double cycles = most(rounds * ((double)blocks * block + end) - end, least) + end;
             if (cycles < best.cycles) best = {false, tile, 1 << i, cycles};
         }
     }
