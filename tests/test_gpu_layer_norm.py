@@ -278,6 +278,27 @@ def test_streams_and_capture():
     assert all(torch.equal(a, c) for a, c in zip(fb.layer_norm_backward(x[:77], w, dy[:77], with_bias=True), r2))
 
 
+def test_offsets_past_32_bits():
+    """140,000 rows of 16,384 values, and their last ones in other forms."""
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    tokens, dim = 140000, 16384
+    x = torch.zeros(tokens, dim, dtype=torch.bfloat16, device=DEV)
+    last = torch.arange(tokens - 40, tokens, device=DEV)
+    x[last] = rand(gen, 40, dim).bfloat16()
+    w, b, dy = 1 + 0.2 * rand(gen, dim), rand(gen, dim), torch.zeros_like(x)
+    dy[last] = rand(gen, 40, dim).bfloat16()
+    want = forward(x[last], w, b, False, 1e-5, torch.bfloat16)
+    within(fb.layer_norm(x, w, b)[last], *want)
+    within(fb.layer_norm(x, w, b, rows=last.int()), *want)
+    dx, dw, _ = fb.layer_norm_backward(x, w, dy)
+    alone = fb.layer_norm_backward(x[last].clone(), w, dy[last].clone())
+    assert torch.equal(dx[last], alone[0])
+    n, off, _, _ = parts(x[last], False, 1e-5)
+    d = dy[last].double()
+    within(dw, (d * n).sum(0), (d.abs() * off).sum(0) + 90 * U * (d * n).abs().sum(0) + 1e-38)
+    fb.layer_norm_poll_status()
+
+
 def test_refusals():
     x, w = torch.zeros(4, 64, device=DEV), torch.zeros(64, device=DEV)
     ints = torch.zeros(4, dtype=torch.int32, device=DEV)

@@ -375,6 +375,34 @@ def test_a_wait_that_runs_out_is_reported():
         assert torch.equal(fb.linear(x, w), want)
 
 
+def test_offsets_past_32_bits():
+    """140,000 rows of 16,384 values: more than 2^31 of them in the result, the residual and the gradients' inputs."""
+    gen = torch.Generator(device=DEV).manual_seed(15)
+    tokens, n_in, n_out = 140000, 16, 16384
+    x, w = operands(gen, tokens, n_in, n_out)
+    bias, stream = rand(gen, n_out), torch.zeros(tokens, n_out, dtype=torch.bfloat16, device=DEV)
+    stream[:, ::5] = 2
+    last = torch.arange(tokens - 70, tokens, device=DEV)
+    preact = torch.empty(tokens, n_out, dtype=torch.bfloat16, device=DEV)
+    r = stream[last].clone()
+    assert fb.linear(x, w, bias, activation="silu", residual=stream, out=stream, preact=preact) is stream
+    within(stream[last], *expected(x[last], w, bias, "silu", r, torch.bfloat16))
+    within(preact[last], *expected(x[last], w, bias, "none", None, torch.bfloat16))
+    # few tokens whose rows are the last ones
+    r = stream[last].clone()
+    fb.linear(x[:70], w, bias, residual=stream, out=stream, rows=last.int())
+    within(stream[last], *expected(x[:70], w, bias, "none", r, torch.bfloat16))
+    # gradients: dx of the last rows; dweight of rows that only the last tokens have
+    dx = fb.linear_backward(None, w, stream, preact=preact, activation="relu")[0]
+    g = torch.where(preact[last].double() > 0, stream[last].double(), 0)
+    within(dx[last], g @ w.double(), (1 + 2.0 ** -8) * ((n_out / 16 + 4) * 2.0 ** -23 + 2.0 ** -8) * (g.abs() @ w.double().abs()) + 2.0 ** -8 * (g @ w.double()).abs())
+    stream[:tokens - 70] = 0
+    dw = fb.linear_backward(x, None, stream)[1]
+    a, b = stream[last].double().t(), x[last].double()
+    within(dw, a @ b, (1 + 2.0 ** -8) * (tokens / 16 + 4) * 2.0 ** -23 * (a.abs() @ b.abs()) + 2.0 ** -8 * (a @ b).abs() + 1e-37)
+    fb.linear_poll_status()
+
+
 def test_refusals():
     x, w = torch.zeros(4, 64, device=DEV).bfloat16(), torch.zeros(16, 64, device=DEV).bfloat16()
     flat = torch.zeros(4 * 64 + 8, device=DEV).bfloat16()
