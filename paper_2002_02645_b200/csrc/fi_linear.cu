@@ -575,10 +575,10 @@ __device__ __forceinline__ void load_box_pair(uint32_t dst, const CUtensorMap *m
         "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
         : "memory");
 }
-// when the pair's products so far are over: the barrier at this place in both CTAs
-__device__ __forceinline__ void tc_commit_pair(uint64_t *bar) {
+// when the pair's products so far are over: the barrier at this place in both CTAs, `first` and the next of the cluster
+__device__ __forceinline__ void tc_commit_pair(uint64_t *bar, uint32_t first) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_at(bar)),
-                 "h"((uint16_t)3)
+                 "h"((uint16_t)(3u << first))
                  : "memory");
 }
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
@@ -734,17 +734,21 @@ struct TileWalk {
 // Bound by the tensor cores and, in long runs, by the power that they draw: 4,096^3 takes 94 us, 1,460 TFLOP/s (tensor pipe 91 % active);
 // with float32 results, whose sums are added up outside of it, 104 us; 8,191 x 4,096 -> 16,384 651 to 665 us, 1,680 TFLOP/s.
 // JOBS = 2: a second product behind the first, whose rows' operand lies the other way round (the two gradients).
-template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, int JOBS>
+// SPLIT = 2: two pairs, a cluster of 4, have a tile together, each half of its reduction; sums of half of the columns go to the other pair, and
+// a cluster has no second tile.  (Tiles twice as wide bring half of the rows' operand through L2 for as many SMs.)
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, int JOBS, int SPLIT>
 __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUtensorMap *maps_b, const LinearParams *jobs) {
     const LinearParams &p = jobs[0];                        // (tiles and stages are those of both)
     extern __shared__ unsigned char raw_smem[];
     __shared__ PairCtl ctl_space;
     PairCtl *const ctl = &ctl_space;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
-    const uint32_t rank = cluster_rank();
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t cluster = cluster_rank(), rank = cluster & 1, first_cta = cluster & ~1u, part = cluster >> 1;
+    const int pair = blockIdx.x / (2 * SPLIT), pairs = gridDim.x / (2 * SPLIT);
     const uint32_t smem = (smem_at(raw_smem) + 1023) & ~1023u, block_bytes = kABytes + p.b_bytes, stage_bytes = DEPTH * block_bytes;
     const int half_n = p.tile_n >> 1;
+    const auto step0 = [&](const LinearParams &q) { return SPLIT == 1 ? 0 : (int)(part * (uint32_t)q.kb) / SPLIT; };
+    const auto step1 = [&](const LinearParams &q) { return SPLIT == 1 ? q.kb : (int)((part + 1) * (uint32_t)q.kb) / SPLIT; };
     if (tid == 0) {
         for (int s = 0; s < p.stages; ++s) {
             bar_init(&ctl->full[s], 1);
@@ -793,12 +797,12 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
             int rt, ct;
             tile_place(w.t, row_tiles_of(w.job), q.m_tiles, rt, ct);
             const int r0 = rt * 2 * kM + (int)rank * kM, c0 = ct * p.tile_n + (int)rank * half_n;
-            for (int kb = 0; kb < q.kb; ++kb) {
+            for (int kb = step0(q); kb < step1(q); ++kb) {
                 ok = warp_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit);
                 if (!ok) break;
                 if (elect_one()) {
                     if (rank == 0) bar_expect(&ctl->full[stage], 2u * stage_bytes);
-                    const uint32_t bar = map_to_rank(smem_at(&ctl->full[stage]), 0);
+                    const uint32_t bar = map_to_rank(smem_at(&ctl->full[stage]), first_cta);
 #pragma unroll
                     for (int i = 0; i < DEPTH; ++i) {
                         const uint32_t a = smem + stage * stage_bytes + i * block_bytes, b = a + kABytes;
@@ -840,9 +844,9 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
             uint32_t buf = 0, buf_phase = 0;
             bool ok = true;
             for (TileWalk<JOBS> w = walk; ok && w.next();) {
-                const int steps = jobs[w.job].kb, piece = F32 ? kPiece / DEPTH : steps;     // steps of an accumulator
+                const int steps = step1(jobs[w.job]), piece = F32 ? kPiece / DEPTH : steps;     // steps of an accumulator
                 const uint32_t idesc = instruction(2 * kM, p.tile_n, B_MN != (w.job != 0), A_MN);
-                for (int kb = 0; kb < steps && ok;) {
+                for (int kb = step0(jobs[w.job]); kb < steps && ok;) {
                     ok = warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit);
                     if (!ok) break;
                     tc_after();
@@ -859,13 +863,13 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
                                 if (JOBS == 2 && w.job) mma_block<true, !B_MN, A_MN>(d, operand<!B_MN>(at), operand<A_MN>(at + kABytes), idesc, i ? 1u : more);
                                 else mma_block<true, B_MN, A_MN>(d, operand<B_MN>(at), operand<A_MN>(at + kABytes), idesc, i ? 1u : more);
                             }
-                            tc_commit_pair(&ctl->empty[stage]);
+                            tc_commit_pair(&ctl->empty[stage], first_cta);
                         }
                         __syncwarp();
                         next_stage();
                     }
                     if (ok) {
-                        if (elect_one()) tc_commit_pair(&ctl->sums_full[buf]);
+                        if (elect_one()) tc_commit_pair(&ctl->sums_full[buf], first_cta);
                         __syncwarp();
                         buf ^= 1;
                         if (buf == 0) buf_phase ^= 1;
@@ -873,13 +877,13 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
                 }
             }
             if (!ok) {                                      // no product is on its way when TMEM is freed
-                if (elect_one()) tc_commit_pair(&ctl->never);
+                if (elect_one()) tc_commit_pair(&ctl->never, first_cta);
                 __syncwarp();
                 const long long t0 = clock64();
                 while (clock64() - t0 < kDrainLimit / 10) {}
             }
         }
-    } else {
+    } else if constexpr (SPLIT == 1) {
         // ---- sums on their way out: warp w reads TMEM lanes 32 (w mod 4) .., and half of the tile's columns ----
         const int first = (warp >> 2) * half_n, my_row = (int)rank * kM + (warp & 3) * 32 + lane;
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + first;
@@ -919,7 +923,7 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
                     }
                     tc_before();
                     __syncwarp();
-                    if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), 0));
+                    if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), first_cta));
                     buf ^= 1;
                     if (buf == 0) buf_phase ^= 1;
                 }
@@ -951,9 +955,117 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
                 }
                 tc_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), 0));
+                if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), first_cta));
                 buf ^= 1;
                 if (buf == 0) buf_phase ^= 1;
+            }
+        }
+    }
+    if constexpr (SPLIT == 2) {
+        // As above, but of the columns that a warp has, it sends half to its like in the other pair, to where the stages were, and adds what
+        // comes from there to the other half.
+        float sum[F32 ? kMaxPairN32 / 2 : 1] = {};
+        const int first = (warp >> 2) * half_n, my_row = (int)rank * kM + (warp & 3) * 32 + lane, mine = half_n / 2, keep = (int)part * mine;
+        const int send = mine - keep;
+        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + first;
+        const bool tile = walk.next();
+        if (warp < 8 && tile) {
+            if constexpr (F32) {
+                uint32_t buf = 0, buf_phase = 0;
+                for (int kb = step0(p); kb < step1(p); kb += kPiece / DEPTH) {
+                    if (!warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit)) break;
+                    tc_after();
+                    uint32_t v[2][16];
+                    tmem_load(at + buf * p.tile_n, v[0]);
+#pragma unroll
+                    for (int c = 0; c < kMaxPairN32 / 2; c += 16) {
+                        uint32_t (&now)[16] = v[c / 16 & 1], (&next)[16] = v[c / 16 + 1 & 1];
+                        tmem_wait(now);
+                        if (c + 16 < kMaxPairN32 / 2 && c + 16 < half_n) tmem_load(at + buf * p.tile_n + c + 16, next);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(now[i]);
+                    }
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[buf]), first_cta));
+                    buf ^= 1;
+                    if (buf == 0) buf_phase ^= 1;
+                }
+            } else {
+                warp_wait(&ctl->sums_full[0], 0, ctl, p.wait_limit);
+                tc_after();
+            }
+        }
+        __syncwarp();
+        cluster_sync();                                     // no product reads the stages any more, in either pair
+        const uint32_t box = smem + (uint32_t)(warp * mine * 32 + lane * 4) * 4;            // [8 warps][mine / 4][32 rows][4]
+        if (warp < 8 && tile) {
+            const uint32_t there = map_to_rank(box, cluster ^ 2);
+            if constexpr (F32) {
+#pragma unroll
+                for (int c = 0; c < kMaxPairN32 / 2; c += 16)
+                    if (c >= send && c < send + mine)
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) cluster_store4(there + (uint32_t)(c + i - send) * 128, reinterpret_cast<const uint32_t *>(sum + c + i));
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < mine; c += 16) {
+                    uint32_t v[16];
+                    tmem_load(at + send + c, v);
+                    tmem_wait(v);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) cluster_store4(there + (uint32_t)(c + i) * 128, v + i);
+                }
+            }
+        }
+        __syncwarp();
+        cluster_sync();
+        if (warp < 8 && tile) {
+            int rt, ct;
+            tile_place(walk.t, row_tiles_of(0), p.m_tiles, rt, ct);
+            const int row = rt * 2 * kM + my_row, n = row < rows0 ? row : -1, to = row_of(p, row, rows0), c0 = ct * p.tile_n + first + keep;
+            const int cols = min(mine, p.m - c0);
+            if (p.bias) {
+                for (int c = lane; c < cols; c += 32) ctl->bias[warp][c] = p.bias[c0 + c];
+                __syncwarp();
+            }
+            const uint32_t turn = smem_at(ctl->turn[warp]);
+            const bool add = p.residual != nullptr;
+            const auto from_other = [&](int c) {
+                const uint4 x = shared_load4(box + (uint32_t)c * 128);
+                return make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+            };
+            if constexpr (F32) {
+#pragma unroll
+                for (int c = 0; c < kMaxPairN32 / 2; c += 16)
+                    if (c >= keep && c < keep + cols) {
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            const float4 x = from_other(c + i - keep);
+                            v[i] = sum[c + i] + x.x; v[i + 1] = sum[c + i + 1] + x.y; v[i + 2] = sum[c + i + 2] + x.z; v[i + 3] = sum[c + i + 3] + x.w;
+                        }
+                        finish_row<true, ACT>(p, v, c0 + c - keep, n, to, p.bias ? ctl->bias[warp] + c - keep : nullptr, add, turn);
+                    }
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < cols; c += 32) {
+                    uint32_t s0[16], s1[16];
+                    tmem_load(at + keep + c, s0);
+                    tmem_load(at + keep + c + 16, s1);
+                    tmem_wait(s0);
+                    tmem_wait(s1);
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const float4 x = from_other(c + i), y = from_other(c + 16 + i);
+                        v[i] = __uint_as_float(s0[i]) + x.x; v[i + 1] = __uint_as_float(s0[i + 1]) + x.y;
+                        v[i + 2] = __uint_as_float(s0[i + 2]) + x.z; v[i + 3] = __uint_as_float(s0[i + 3]) + x.w;
+                        v[16 + i] = __uint_as_float(s1[i]) + y.x; v[17 + i] = __uint_as_float(s1[i + 1]) + y.y;
+                        v[18 + i] = __uint_as_float(s1[i + 2]) + y.z; v[19 + i] = __uint_as_float(s1[i + 3]) + y.w;
+                    }
+                    finish_row<false, ACT>(p, v, c0 + c, n, to, p.bias ? ctl->bias[warp] + c : nullptr, add, turn);
+                }
             }
         }
     }
@@ -967,11 +1079,11 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
     }
 }
 
-template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, int SPLIT>
 __global__ void __launch_bounds__(kThreads, 1) linear_pair_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
                                                                   const __grid_constant__ LinearParams p) {
-    linear_pair<F32, ACT, A_MN, B_MN, DEPTH, 1>(&map_a, &map_b, &p);
+    linear_pair<F32, ACT, A_MN, B_MN, DEPTH, 1, SPLIT>(&map_a, &map_b, &p);
 }
 
 // Both gradients, the one with the longer reduction first (ROWS_MN: that of the weights).
@@ -981,7 +1093,7 @@ struct LinearTwo {
 };
 template <bool ROWS_MN, int DEPTH>
 __global__ void __launch_bounds__(kThreads, 1) linear_two_kernel(const __grid_constant__ LinearTwo two) {
-    linear_pair<false, FI_ACT_NONE, true, ROWS_MN, DEPTH, 2>(two.a, two.b, two.p);
+    linear_pair<false, FI_ACT_NONE, true, ROWS_MN, DEPTH, 2, 1>(two.a, two.b, two.p);
 }
 
 // dz = dy act'(preact), and dbias, the sums of its columns (of dy itself without an activation: nothing else is stored then).  A CTA takes 64
@@ -1077,28 +1189,32 @@ fi_status_t launch_early(const char *name, void (*kernel)(Params...), dim3 grid,
     return check_launch(name);
 }
 
-// forward products in all their forms; gradients have no activation and bfloat16 results
-template <bool PAIR, int DEPTH, bool F32, int ACT, bool A_MN, bool B_MN>
-constexpr LinearKernel kLinearKernel = PAIR ? &linear_pair_kernel<F32, ACT, A_MN, B_MN, DEPTH> : &linear_split_kernel<F32, ACT, A_MN, B_MN, DEPTH>;
+// forward products in all their forms; gradients have no activation and bfloat16 results.  PAIRS: that have a tile together, 0: single CTAs
+template <int PAIRS, int DEPTH, bool F32, int ACT, bool A_MN, bool B_MN>
+constexpr LinearKernel linear_kernel_of() {
+    if constexpr (PAIRS == 0) return &linear_split_kernel<F32, ACT, A_MN, B_MN, DEPTH>;
+    else return &linear_pair_kernel<F32, ACT, A_MN, B_MN, DEPTH, PAIRS>;
+}
 
-template <bool PAIR, int DEPTH, bool F32>
+template <int PAIRS, int DEPTH, bool F32>
 LinearKernel forward_kernel(int act) {
     switch (act) {
-        case FI_ACT_RELU: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_RELU, false, false>;
-        case FI_ACT_GELU: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_GELU, false, false>;
-        case FI_ACT_GELU_TANH: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_GELU_TANH, false, false>;
-        case FI_ACT_SILU: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_SILU, false, false>;
-        default: return kLinearKernel<PAIR, DEPTH, F32, FI_ACT_NONE, false, false>;
+        case FI_ACT_RELU: return linear_kernel_of<PAIRS, DEPTH, F32, FI_ACT_RELU, false, false>();
+        case FI_ACT_GELU: return linear_kernel_of<PAIRS, DEPTH, F32, FI_ACT_GELU, false, false>();
+        case FI_ACT_GELU_TANH: return linear_kernel_of<PAIRS, DEPTH, F32, FI_ACT_GELU_TANH, false, false>();
+        case FI_ACT_SILU: return linear_kernel_of<PAIRS, DEPTH, F32, FI_ACT_SILU, false, false>();
+        default: return linear_kernel_of<PAIRS, DEPTH, F32, FI_ACT_NONE, false, false>();
     }
 }
-template <bool PAIR, int DEPTH>
+template <int PAIRS, int DEPTH>
 LinearKernel linear_kernel(bool f32, int act, bool a_mn, bool b_mn) {
-    if (a_mn) return b_mn ? kLinearKernel<PAIR, DEPTH, false, FI_ACT_NONE, true, true> : kLinearKernel<PAIR, DEPTH, false, FI_ACT_NONE, true, false>;
-    return f32 ? forward_kernel<PAIR, DEPTH, true>(act) : forward_kernel<PAIR, DEPTH, false>(act);
+    if (a_mn) return b_mn ? linear_kernel_of<PAIRS, DEPTH, false, FI_ACT_NONE, true, true>() : linear_kernel_of<PAIRS, DEPTH, false, FI_ACT_NONE, true, false>();
+    return f32 ? forward_kernel<PAIRS, DEPTH, true>(act) : forward_kernel<PAIRS, DEPTH, false>(act);
 }
-LinearKernel linear_kernel(bool pair, int depth, bool f32, int act, bool a_mn, bool b_mn) {
-    if (pair) return depth == 2 ? linear_kernel<true, 2>(f32, act, a_mn, b_mn) : linear_kernel<true, 1>(f32, act, a_mn, b_mn);
-    return depth == 2 ? linear_kernel<false, 2>(f32, act, a_mn, b_mn) : linear_kernel<false, 1>(f32, act, a_mn, b_mn);
+LinearKernel linear_kernel(int pairs, int depth, bool f32, int act, bool a_mn, bool b_mn) {
+    if (pairs == 2) return depth == 2 ? linear_kernel<2, 2>(f32, act, a_mn, b_mn) : linear_kernel<2, 1>(f32, act, a_mn, b_mn);
+    if (pairs == 1) return depth == 2 ? linear_kernel<1, 2>(f32, act, a_mn, b_mn) : linear_kernel<1, 1>(f32, act, a_mn, b_mn);
+    return depth == 2 ? linear_kernel<0, 2>(f32, act, a_mn, b_mn) : linear_kernel<0, 1>(f32, act, a_mn, b_mn);
 }
 
 using TwoKernel = void (*)(LinearTwo);
@@ -1129,8 +1245,8 @@ fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     for (int form = 0; form < 12; ++form) {                 // of a product: type and activation, or one of two gradients
         const bool back = form >= 10, f32 = !back && form >= 5;
-        for (int i = 0; i < 4 && e == cudaSuccess; ++i)
-            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(linear_kernel(i & 1, 1 + (i >> 1), f32, form % 5, back, form == 11)),
+        for (int i = 0; i < 6 && e == cudaSuccess; ++i)
+            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(linear_kernel(i >> 1, 1 + (i & 1), f32, form % 5, back, form == 11)),
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
     }
     for (int i = 0; i < 4 && e == cudaSuccess; ++i)
@@ -1190,9 +1306,10 @@ fi_status_t operand_map(CUtensorMap *map, const Matrix &x, int box_rows, const c
 // CTA's 16 x 128 x 256 in as many), an SM gets 80 bytes a cycle from L2 where pairs ask for them and 55 where single CTAs do, all together
 // 8,600, and the device 5,000 from memory and what L2 still has; a tile's way out is hidden behind the next one of a pair, but for a fifth
 // of it.  These figures and the ways out are fitted to the times of 212 products in all their forms (1 to 8,192 tokens, 80 to 8,192 values,
-// both types): what is taken is 0.9 % slower than the best form of each in the mean, 15 % at most.  (Both sides, us: 777 x 512 -> 2,048:
+// both types): what is taken is 0.9 % slower than the best form of each in the mean, 16 % at most.  (Both sides, us: 777 x 512 -> 2,048:
 // pairs of 128 columns 6.3, CTAs with 96 tokens 8.8; 32 x 4,096 -> 4,096: clusters of 4 9.5, single CTAs 11.3; 4,000 x 768 <- 768: pairs
-// 9.3, CTAs 14.2; 200 x 8,192 -> 2,048 in float32: clusters of 4 18.4, pairs 25.3.)
+// 9.3, CTAs 14.2; 200 x 8,192 -> 2,048 in float32: clusters of 4 18.4, pairs 25.3; two pairs a tile against the best of the others:
+// 256 x 4,096 -> 4,096 in float32 16.4 and 17.9, 1,000 x 8,192 -> 1,024 19.1 and 21.8, 256 x 14,336 -> 4,096 31.5 and 35.5.)
 struct LinearPlan {
     bool pair;
     int tile_n, split;
@@ -1228,6 +1345,10 @@ LinearPlan plan_product(long long m, long long n, long long kb, bool a_mn, bool 
         const PairCost c = pair_cost(m, n, kb, tile, f32, size);
         const double cycles = most(times(c.tiles, clusters[1]) * c.each, c.least) + c.end;
         if (cycles < best.cycles) best = {true, tile, 1, cycles};
+        // two pairs a tile; what a warp has of the columns is halved, 16 (in bfloat16 32) of them go out together
+        if (kb < 16 || tile % (f32 ? 64 : 128)) continue;
+        const double split = most(times(c.tiles, clusters[2]) * (0.5 * c.each + c.end), c.least) + c.end + 3000;
+        if (split < best.cycles) best = {true, tile, 2, split};
     }
     const double memory = memory_cycles((double)m, (double)n, (double)kb, size), weights = (double)m * kb * (kKb * 2), m_tiles = (double)up(m, kM);
     for (int tile = 16; tile <= kMaxN; tile += 16) {
@@ -1304,14 +1425,14 @@ fi_status_t plan_launch(Product &x, const LinearPlan &plan, const Matrix &a, boo
     p.b_bytes = second_mn ? (mine + 63) / 64 * 8192 : mine * kKb * 2;
     const int stage = depth * (kABytes + p.b_bytes), room = kSmemMost - kStaticMost - 1024 /* alignment */;
     const int part = plan.pair ? 0 : p.split * ((p.tile_n / 4 + p.split - 1) / p.split) * kM * 16;
-    const bool apart = p.split > 1 && p.tile_n <= 64;
+    const bool apart = !plan.pair && p.split > 1 && p.tile_n <= 64;
     p.stages = (room - (apart ? part : 0)) / stage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     p.part_at = apart ? p.stages * stage : 0;
     int smem = p.stages * stage + (apart ? part : 0);
     if (smem < part) smem = part;
     smem += 1024;
-    if (tiles * p.split > 1073741823ll) {
+    if (tiles * p.split * 2 > 1073741823ll) {
         set_error("%s: too many tiles", name);
         return FI_ERR_INVALID_ARG;
     }
@@ -1325,10 +1446,10 @@ fi_status_t plan_launch(Product &x, const LinearPlan &plan, const Matrix &a, boo
 }
 
 fi_status_t launch_planned(const Product &x, bool a_mn, bool b_mn, bool f32, int act, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
-    const bool pair = x.plan.pair;
-    const long long ctas = pair ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * x.p.split;
-    return launch_early(name, linear_kernel(pair, x.depth, f32, act, a_mn, b_mn), dim3((unsigned)ctas), kThreads, x.smem, dim3(pair ? 2 : x.p.split), stream,
-                        x.map_a, x.map_b, x.p);
+    const int pairs = x.plan.pair ? x.p.split : 0, cluster = pairs ? 2 * pairs : x.p.split;
+    const long long ctas = pairs == 1 ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * cluster;
+    return launch_early(name, linear_kernel(pairs, x.depth, f32, act, a_mn, b_mn), dim3((unsigned)ctas), kThreads, x.smem, dim3(cluster), stream, x.map_a,
+                        x.map_b, x.p);
 }
 
 fi_status_t launch_product(const Matrix &a, bool a_mn, const Matrix &b, bool b_mn, long long m, long long n, long long k, bool f32, int act,
@@ -1525,7 +1646,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         st = plan_launch(px, plan_x, w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, name);
         if (st == FI_OK) st = plan_launch(pw, plan_w, x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, name);
         if (st != FI_OK) return st;
-        if (plan_x.pair && plan_w.pair && plan_x.tile_n == plan_w.tile_n && px.depth == pw.depth)
+        if (plan_x.pair && plan_w.pair && plan_x.split == 1 && plan_w.split == 1 && plan_x.tile_n == plan_w.tile_n && px.depth == pw.depth)
             return px.p.kb >= pw.p.kb ? launch_two(px, pw, false, *facts, stream, name) : launch_two(pw, px, true, *facts, stream, name);
         st = launch_planned(px, true, false, false, FI_ACT_NONE, *facts, stream, name);
         return st == FI_OK ? launch_planned(pw, true, true, false, FI_ACT_NONE, *facts, stream, name) : st;

@@ -233,6 +233,40 @@ def test_both_gradients_whichever_sums_are_longer(tokens, n_in, n_out):
     fb.linear_poll_status()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tokens,n_in,n_out,act", [(256, 4096, 4096, "none"), (251, 4104, 4040, "gelu"), (1000, 8192, 1024, "silu"), (256, 14336, 1032, "relu"),
+                                                   (220, 4096, 6144, "none"), (777, 1400, 1000, "gelu_tanh"), (150, 2048, 2056, "none")])
+def test_long_sums_of_a_few_hundred_tokens(tokens, n_in, n_out, act, dtype):
+    """Sizes whose sums are shared, with all that an epilogue does, for listed rows of a stream, and their gradients."""
+    gen = torch.Generator(device=DEV).manual_seed(n_in)
+    x, w = operands(gen, tokens, n_in, n_out)
+    bias, r = rand(gen, n_out), rand(gen, tokens + 30, n_out).to(dtype)
+    preact = torch.full((tokens, n_out), 7.0, device=DEV, dtype=torch.bfloat16)
+    y = fb.linear(x, w, bias, activation=act, residual=r[:tokens], preact=preact)
+    within(y, *expected(x, w, bias, act, r[:tokens], dtype))
+    within(preact, *expected(x, w, bias, "none", None, torch.bfloat16))
+    assert torch.equal(y, fb.linear(x, w, bias, activation=act, residual=r[:tokens]))
+    rows, alive = torch.randperm(tokens + 30, generator=gen, device=DEV)[:tokens].int(), tokens - 19
+    x[alive:] = math.nan
+    stream = r.clone()
+    fb.linear(x, w, bias, activation=act, residual=stream, out=stream, rows=rows, count=torch.tensor([alive], dtype=torch.int32, device=DEV))
+    at = rows[:alive].long()
+    within(stream[at], *expected(x[:alive], w, bias, act, r[at], dtype))
+    left = torch.ones(tokens + 30, dtype=torch.bool, device=DEV)
+    left[at] = False
+    assert torch.equal(stream[left], r[left])
+    fb.linear_poll_status()
+    if dtype is torch.bfloat16:
+        dy, x = rand(gen, tokens, n_out).bfloat16(), rand(gen, tokens, n_in).bfloat16()
+        check_backward(x, w, dy, preact, act, True)
+        dx = fb.linear_backward(None, w, dy)[0]
+        want, size = dy.double() @ w.double(), dy.double().abs() @ w.double().abs()
+        within(dx, want, (1 + 2.0 ** -8) * (n_out / 16 + 4) * 2.0 ** -23 * size + 2.0 ** -8 * want.abs() + 1e-37)
+        fb.linear(x, w, wait_limit=1000)                       # (and a wait that runs out is reported)
+        with pytest.raises(fb.FiError, match="TIMEOUT"):
+            fb.linear_poll_status()
+
+
 def test_backward_of_extreme_preactivations():
     """Slopes that have reached 0 or 1 are that; nothing becomes NaN but what is NaN."""
     z = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 30.0, -30.0, 150.0, -150.0, 1e30, -1e30, math.inf, -math.inf, 5.0, -5.0, 19.0, -19.0], device=DEV)
