@@ -59,7 +59,7 @@ struct LinearParams {
     long long ld_res, ld_out, ld_preact, out_rows, wait_limit;
     int m, n, kb;                  // output columns, rows; steps of the reduction: one or two blocks of 64, a stage each
     int m_tiles, tile_n;
-    int split;                     // CTAs of a cluster that share a tile's reduction
+    int split;                     // CTAs, or pairs of them, of a cluster that share a tile's reduction
     int bufs;                      // accumulators that a CTA's reduction is cut into
     int tmem_cols, stages, b_bytes;
     int part_at;                   // place of a CTA's sums in shared memory
