@@ -666,8 +666,9 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
  *   outside [0, out_rows) is not stored; null: token i is row i.  Rows that are not listed are left untouched.
  *   tokens_dev [1] device int32, nullable: actual number of tokens (<= tokens); later ones are left out.
  *   preact [tokens x out_dim] bfloat16, nullable: x W^T + bias before the activation, which the gradients need.
- * Products on the tensor cores, sums in fp32; one rounding at the end.  A float32 out is summed up in pieces of about 512 values outside
- * of the tensor cores, which cut what they add (an error of some 2^-24 of the sum for 16 values).
+ * Products on the tensor cores, sums in fp32; one rounding at the end.  The tensor cores cut what they add (some 2^-24 of the sum for 16
+ * values, always towards zero), so a float32 out is summed up in pieces of about 512 values outside of them, a bfloat16 out (and dx and
+ * dweight below) in pieces of 16,384 (off by 2^-15 of the sum, before it is rounded to 2^-8), however long the sums are.
  * in_dim and out_dim multiples of 8, they and tokens at most 2^30; rows of x and weight start on 16-byte boundaries; strides in elements.
  * Asynchronous, on the current device; no workspace, so calls may overlap.  x and weight must not be written by the call's own results.
  *

@@ -6,7 +6,7 @@
 //   dx         D = dx  [tokens][in]    A = W  (m contiguous)   B = dz (k contiguous)      k over out
 //   dW         D = dW  [out][in]       A = x  (m contiguous)   B = dz (n contiguous)      k over tokens
 // Operands come by TMA in blocks of 64 along k, 128-byte swizzle, as they lie in memory: the tensor cores take either order.
-// Sums are fp32 in TMEM.
+// Sums are fp32 in TMEM, long ones in pieces.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -23,7 +23,12 @@ constexpr int kABytes = kM * kKb * 2;     // of a block
 constexpr int kMaxN = 256;                // output rows of a tile, at most
 constexpr int kMaxPairN32 = 192;          // of a pair's tile with float32 results, whose sums are in registers
 constexpr int kMaxStages = 12;
-constexpr int kPiece = 8;                 // blocks of the reduction that are added up in one accumulator for float32 results
+// Blocks of the reduction that are added up in one accumulator.  The tensor cores cut what they add: a running sum of one sign loses 2^-24
+// of itself with every 16 values, 2^-23 at most.  So float32 results are taken out of them every 512 values, bfloat16 results, which are
+// rounded to 2^-8, every 16,384 (2^-15 of the sum, 2^-13 at most; left there for 2^20 values: 2^-9, and results are a step off).
+constexpr int kPiece = 8, kHalfPiece = 256;
+template <bool F32>
+constexpr int kPieceOf = F32 ? kPiece : kHalfPiece;
 constexpr int kEpiThreads = 256;          // warps 0..7: TMEM lanes 32 (w mod 4) ..; warp 8 loads, warp 9 issues the products
 constexpr int kThreads = kEpiThreads + 64;
 constexpr int kSmemMost = 227 * 1024, kStaticMost = 22 * 1024;
@@ -36,6 +41,7 @@ __device__ int32_t g_linear_status;       // 1: a bounded wait ran out
 struct LinearCtl {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t done, never;
+    uint64_t sums_full[2], sums_empty[2];
     uint32_t tmem;
     volatile int gave_up;
 };
@@ -61,6 +67,7 @@ struct LinearParams {
     int m_tiles, tile_n;
     int split;                     // CTAs, or pairs of them, of a cluster that share a tile's reduction
     int bufs;                      // accumulators that a CTA's reduction is cut into
+    int piece;                     // single CTAs: steps of an accumulator where there are more pieces than those, else 0
     int tmem_cols, stages, b_bytes;
     int part_at;                   // place of a CTA's sums in shared memory
     int early;                     // two products in one launch: see TileWalk
@@ -73,6 +80,9 @@ __device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
 }
 __device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t *bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_at(bar)) : "memory");
 }
 __device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
     uint32_t ok;
@@ -220,6 +230,35 @@ __device__ __forceinline__ void tmem_wait(uint32_t *v) {
                    "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
                  :
                  : "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(v[0]), "r"(v[1]), "r"(v[2]),
+        "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+        "r"(addr)
+        : "memory");
+}
+// the accumulators take turns
+__device__ __forceinline__ void next_buffer(uint32_t &buf, uint32_t &phase) {
+    buf ^= 1;
+    if (buf == 0) phase ^= 1;
+}
+// Long sums: the piece at `to` takes up the sum so far, at `from`, which is free then.  Columns from `first` on, 16 at a time.
+__device__ __forceinline__ void join_pieces(uint32_t from, uint32_t to, int first, int cols, int step) {
+#pragma unroll 1
+    for (int c = first; c < cols; c += step) {
+        uint32_t v[16], w[16];
+        tmem_load(from + c, v);
+        tmem_load(to + c, w);
+        tmem_wait(v);
+        tmem_wait(w);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(w[i]));
+        tmem_store(to + c, v);
+    }
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+    tc_before();
+    __syncwarp();
 }
 // Exponential and reciprocal of the special-function unit (2^-22 of the result).  At full power the clock falls with every instruction that is
 // executed beside the products, so the activation is kept short (8,191 x 4,096 -> 16,384 and back with the library's erfcf: 909 us, so: 799).
@@ -430,6 +469,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             }
             bar_init(&ctl->done, 1);
             bar_init(&ctl->never, 1);
+            for (int i = 0; i < 2; ++i) {
+                bar_init(&ctl->sums_full[i], 1);
+                bar_init(&ctl->sums_empty[i], kEpiThreads / 32);
+            }
             ctl->gave_up = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -453,6 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     const int cols = min(p.tile_n, rows - n0);              // rows of the output that there are; no more is done if there is none
     // so that a wait runs out for certain
     if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
+    uint32_t last_buf = 0, last_phase = 0;                  // with p.piece: the accumulator that holds the sum in the end
     if (warp == 8) {
         int kb = kb0 + early;
         if (cols > 0)
@@ -472,10 +516,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     } else if (warp == 9) {
         if (cols > 0) {
             const uint32_t idesc = instruction(kM, p.tile_n, A_MN, B_MN);
-            const int length = (kb1 - kb0 + p.bufs - 1) / p.bufs;
-            uint32_t d = tmem;
+            const int length = p.piece ? p.piece : (kb1 - kb0 + p.bufs - 1) / p.bufs;
+            uint32_t d = tmem, buf = 0, buf_phase = 0;      // (buf: with p.piece only)
             int in_buf = 0;
             for (int kb = kb0; kb < kb1; ++kb) {
+                if (p.piece && in_buf == 0) {
+                    if (!warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit)) break;
+                    tc_after();
+                    d = tmem + buf * p.tile_n;
+                }
                 if (!warp_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) break;
                 tc_after();
                 if (elect_one()) {
@@ -490,6 +539,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
                 if (++in_buf == length) {
                     in_buf = 0;
                     d += p.tile_n;
+                    if (p.piece) {
+                        if (elect_one()) tc_commit(&ctl->sums_full[buf]);
+                        __syncwarp();
+                        next_buffer(buf, buf_phase);
+                    }
                 }
                 next_stage();
             }
@@ -498,6 +552,19 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             bar_drain(&ctl->done, 0);
         }
     } else if (cols > 0) {
+        if (p.piece) {
+            for (int kb = kb0 + p.piece; kb < kb1; kb += p.piece) {
+                // (the last piece, which may be shorter, is over when all are)
+                const uint32_t old = last_buf;
+                next_buffer(last_buf, last_phase);
+                const bool end = kb + p.piece >= kb1;
+                if (!warp_wait(end ? &ctl->done : &ctl->sums_full[last_buf], end ? 0 : last_phase, ctl, p.wait_limit)) break;
+                tc_after();
+                const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+                join_pieces(at + old * p.tile_n, at + last_buf * p.tile_n, (warp >> 2) * 16, cols, 32);
+                if (lane == 0) bar_arrive(&ctl->sums_empty[old]);
+            }
+        }
         bar_wait(&ctl->done, 0, ctl, p.wait_limit);
         tc_after();
     }
@@ -510,8 +577,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     else if (p.split > 1) cluster_sync();
     if (warp < 8 && cols > 0) {
         const int used = (kb1 - kb0 + p.bufs - 1) / p.bufs;                       // blocks of a buffer
-        const int bufs = (kb1 - kb0 + used - 1) / used;                           // buffers that hold something
-        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const int bufs = p.piece ? 1 : (kb1 - kb0 + used - 1) / used;             // buffers that hold something
+        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + last_buf * p.tile_n;
         const uint32_t to = part + (rank * slots * kM + (warp & 3) * 32 + lane) * 16;
 #pragma unroll 1
         for (int c = (warp >> 2) * 16; c < cols; c += 32) {
@@ -729,7 +796,8 @@ struct TileWalk {
 };
 
 // One pair of CTAs per two SMs walks over tiles of 256 output rows (128 per CTA) and tile_n output columns; each CTA loads its half of
-// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the reduction) go out while the next is formed.
+// both operands.  Two accumulators in TMEM: the sums of one tile (F32: of 512 values of the
+// reduction, else a piece of 16,384) go out while the next is formed.
 // Here the MMA's rows are rows of the output, so that a thread has neighbouring values of one row: 16 bytes a store, the row looked up once.
 // Bound by the tensor cores and, in long runs, by the power that they draw: 4,096^3 takes 94 us, 1,460 TFLOP/s (tensor pipe 91 % active);
 // with float32 results, whose sums are added up outside of it, 104 us; 8,191 x 4,096 -> 16,384 651 to 665 us, 1,680 TFLOP/s.
@@ -844,7 +912,7 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
             uint32_t buf = 0, buf_phase = 0;
             bool ok = true;
             for (TileWalk<JOBS> w = walk; ok && w.next();) {
-                const int steps = step1(jobs[w.job]), piece = F32 ? kPiece / DEPTH : steps;     // steps of an accumulator
+                const int steps = step1(jobs[w.job]), piece = kPieceOf<F32> / DEPTH;             // steps of an accumulator
                 const uint32_t idesc = instruction(2 * kM, p.tile_n, B_MN != (w.job != 0), A_MN);
                 for (int kb = step0(jobs[w.job]); kb < steps && ok;) {
                     ok = warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit);
@@ -938,6 +1006,14 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
             } else {
                 ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
                 tc_after();
+                for (int kb = kHalfPiece / DEPTH; kb < q.kb && ok; kb += kHalfPiece / DEPTH) {
+                    const uint32_t old = buf;
+                    next_buffer(buf, buf_phase);
+                    ok = warp_wait(&ctl->sums_full[buf], buf_phase, ctl, p.wait_limit);
+                    tc_after();
+                    join_pieces(at + old * p.tile_n, at + buf * p.tile_n, 0, cols, 16);
+                    if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[old]), first_cta));
+                }
 #pragma unroll 1
                 for (int c = 0; c < cols; c += 32) {
                     uint32_t s0[16], s1[16];
@@ -969,6 +1045,7 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
         const int send = mine - keep;
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + first;
         const bool tile = walk.next();
+        uint32_t last_buf = 0;                              // accumulator that holds a bfloat16 result's sum in the end
         if (warp < 8 && tile) {
             if constexpr (F32) {
                 uint32_t buf = 0, buf_phase = 0;
@@ -992,8 +1069,17 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
                     if (buf == 0) buf_phase ^= 1;
                 }
             } else {
-                warp_wait(&ctl->sums_full[0], 0, ctl, p.wait_limit);
+                bool ok = warp_wait(&ctl->sums_full[0], 0, ctl, p.wait_limit);
                 tc_after();
+                uint32_t buf_phase = 0;
+                for (int kb = step0(p) + kHalfPiece / DEPTH; kb < step1(p) && ok; kb += kHalfPiece / DEPTH) {
+                    const uint32_t old = last_buf;
+                    next_buffer(last_buf, buf_phase);
+                    ok = warp_wait(&ctl->sums_full[last_buf], buf_phase, ctl, p.wait_limit);
+                    tc_after();
+                    join_pieces(at + old * p.tile_n, at + last_buf * p.tile_n, 0, half_n, 16);
+                    if (lane == 0) bar_arrive_cluster(map_to_rank(smem_at(&ctl->sums_empty[old]), first_cta));
+                }
             }
         }
         __syncwarp();
@@ -1011,7 +1097,7 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
 #pragma unroll 1
                 for (int c = 0; c < mine; c += 16) {
                     uint32_t v[16];
-                    tmem_load(at + send + c, v);
+                    tmem_load(at + last_buf * p.tile_n + send + c, v);
                     tmem_wait(v);
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) cluster_store4(there + (uint32_t)(c + i) * 128, v + i);
@@ -1051,8 +1137,8 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
 #pragma unroll 1
                 for (int c = 0; c < cols; c += 32) {
                     uint32_t s0[16], s1[16];
-                    tmem_load(at + keep + c, s0);
-                    tmem_load(at + keep + c + 16, s1);
+                    tmem_load(at + last_buf * p.tile_n + keep + c, s0);
+                    tmem_load(at + last_buf * p.tile_n + keep + c + 16, s1);
                     tmem_wait(s0);
                     tmem_wait(s1);
                     float v[32];
@@ -1414,11 +1500,14 @@ fi_status_t plan_launch(Product &x, const LinearPlan &plan, const Matrix &a, boo
     const int mine = plan.pair ? p.tile_n / 2 : p.tile_n;                                   // of them that a CTA loads
     p.m_tiles = (int)(plan.pair ? (m + p.tile_n - 1) / p.tile_n : (m + kM - 1) / kM);
     const long long n_tiles = plan.pair ? (n + 2 * kM - 1) / (2 * kM) : (n + p.tile_n - 1) / p.tile_n, tiles = p.m_tiles * n_tiles;
-    p.bufs = plan.pair ? 2 : 1;
-    if (f32 && !plan.pair) {
-        // fp32 results: the tensor cores cut what they add, so that sums drift by 2^-24 of themselves for 16 values; 512 at a time
-        const int room = 512 / p.tile_n, pieces = ((blocks + p.split - 1) / p.split + depth + kPiece - 1) / kPiece;
-        p.bufs = pieces < room ? pieces : room;
+    p.bufs = 2;
+    p.piece = 0;
+    if (!plan.pair) {
+        const int room = 512 / p.tile_n, pieces = f32 ? ((blocks + p.split - 1) / p.split + depth + kPiece - 1) / kPiece
+                                                      : (int)up(up(p.kb, p.split), kHalfPiece / depth);
+        // (in float32 a few blocks more a piece where their number is at the limit)
+        if (pieces > room + (f32 ? 1 : 0)) p.piece = (f32 ? kPiece : kHalfPiece) / depth;
+        else p.bufs = pieces < room ? pieces : room;
     }
     p.tmem_cols = 32;
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
