@@ -38,10 +38,12 @@ constexpr long long kDrainLimit = 200000000ll;   // (about 0.1 s)
 
 __device__ int32_t g_linear_status;       // 1: a bounded wait ran out
 
+constexpr int kRing = 4;                  // accumulators of a single CTA's long sum, at most
+
 struct LinearCtl {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t done, never;
-    uint64_t sums_full[2], sums_empty[2];
+    uint64_t sums_full[kRing], sums_empty[kRing];
     uint32_t tmem;
     volatile int gave_up;
 };
@@ -67,7 +69,7 @@ struct LinearParams {
     int m_tiles, tile_n;
     int split;                     // CTAs, or pairs of them, of a cluster that share a tile's reduction
     int bufs;                      // accumulators that a CTA's reduction is cut into
-    int piece;                     // single CTAs: steps of an accumulator where there are more pieces than those, else 0
+    int piece;                     // single CTAs: steps of an accumulator where there are more pieces than fit, which then take turns; else 0
     int tmem_cols, stages, b_bytes;
     int part_at;                   // place of a CTA's sums in shared memory
     int early;                     // two products in one launch: see TileWalk
@@ -239,9 +241,11 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t *v) {
         : "memory");
 }
 // the accumulators take turns
-__device__ __forceinline__ void next_buffer(uint32_t &buf, uint32_t &phase) {
-    buf ^= 1;
-    if (buf == 0) phase ^= 1;
+__device__ __forceinline__ void next_buffer(uint32_t &buf, uint32_t &phase, uint32_t bufs = 2) {
+    if (++buf == bufs) {
+        buf = 0;
+        phase ^= 1;
+    }
 }
 // Long sums: the piece at `to` takes up the sum so far, at `from`, which is free then.  Columns from `first` on, 16 at a time.
 __device__ __forceinline__ void join_pieces(uint32_t from, uint32_t to, int first, int cols, int step) {
@@ -414,8 +418,9 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
 // work where the tiles alone are fewer than they are.  Sums of four rows go to CTA (row / 4) mod split, which adds them up in the order of
 // the ranks.  Bound by the latency from the launch to the last store (one token 2,048 -> 2,560: 8.8 us from one call to the next), and by the
 // operands' way from memory (48 tokens 4,096 -> 16,384: 28 us for 134 MB of weights, 4.8 TB/s): the loader sets up its barriers and has all
-// stages on the way before the CTA has its TMEM.
-template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH>
+// stages on the way before the CTA has its TMEM.  LONG: more pieces of the reduction than accumulators, which take turns: a
+// kernel of its own, as its tests cost the other one up to 2 % (16 tokens 8,192 -> 8,192 in float32 24.5 -> 24.9 us).
+template <bool F32, int ACT, bool A_MN, bool B_MN, int DEPTH, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                    const __grid_constant__ CUtensorMap map_b,
                                                                    const __grid_constant__ LinearParams p) {
@@ -469,10 +474,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             }
             bar_init(&ctl->done, 1);
             bar_init(&ctl->never, 1);
-            for (int i = 0; i < 2; ++i) {
-                bar_init(&ctl->sums_full[i], 1);
-                bar_init(&ctl->sums_empty[i], kEpiThreads / 32);
-            }
             ctl->gave_up = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -480,6 +481,17 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
         __syncwarp();
         in_turn();
         for (int i = 0; i < early; ++i) load(kb0 + i);
+    }
+    if (LONG && warp == 9) {
+        if (elect_one()) {
+            for (int i = 0; i < p.bufs; ++i) {
+                bar_init(&ctl->sums_full[i], 1);
+                bar_init(&ctl->sums_empty[i], kEpiThreads / 32);
+            }
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_at(&ctl->tmem)), "r"(p.tmem_cols) : "memory");
@@ -496,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     const int cols = min(p.tile_n, rows - n0);              // rows of the output that there are; no more is done if there is none
     // so that a wait runs out for certain
     if (p.wait_limit < kShortLimit && tid == 0) bar_wait(&ctl->never, 0, ctl, p.wait_limit);
-    uint32_t last_buf = 0, last_phase = 0;                  // with p.piece: the accumulator that holds the sum in the end
+    uint32_t last_buf = 0, last_phase = 0;                  // LONG: the accumulator that holds the sum in the end
     if (warp == 8) {
         int kb = kb0 + early;
         if (cols > 0)
@@ -516,55 +528,52 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     } else if (warp == 9) {
         if (cols > 0) {
             const uint32_t idesc = instruction(kM, p.tile_n, A_MN, B_MN);
-            const int length = p.piece ? p.piece : (kb1 - kb0 + p.bufs - 1) / p.bufs;
-            uint32_t d = tmem, buf = 0, buf_phase = 0;      // (buf: with p.piece only)
-            int in_buf = 0;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (p.piece && in_buf == 0) {
-                    if (!warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit)) break;
+            const int length = LONG ? p.piece : (kb1 - kb0 + p.bufs - 1) / p.bufs;
+            uint32_t buf = 0, buf_phase = 0;
+            bool ok = true;
+            for (int kb = kb0; kb < kb1 && ok;) {
+                if (LONG) {
+                    ok = warp_wait(&ctl->sums_empty[buf], buf_phase ^ 1, ctl, p.wait_limit);
+                    if (!ok) break;
                     tc_after();
-                    d = tmem + buf * p.tile_n;
                 }
-                if (!warp_wait(&ctl->full[stage], phase, ctl, p.wait_limit)) break;
-                tc_after();
-                if (elect_one()) {
+                const uint32_t d = tmem + buf * p.tile_n;
+                const int end = min(kb + length, kb1);
+                for (uint32_t more = 0; kb < end; ++kb, more = 1) {
+                    ok = warp_wait(&ctl->full[stage], phase, ctl, p.wait_limit);
+                    if (!ok) break;
+                    tc_after();
+                    if (elect_one()) {
 #pragma unroll
-                    for (int i = 0; i < DEPTH; ++i) {
-                        const uint32_t at = smem + stage * stage_bytes + i * block_bytes;
-                        mma_block<false, A_MN, B_MN>(d, operand<A_MN>(at), operand<B_MN>(at + kABytes), idesc, i || in_buf != 0);
+                        for (int i = 0; i < DEPTH; ++i) {
+                            const uint32_t at = smem + stage * stage_bytes + i * block_bytes;
+                            mma_block<false, A_MN, B_MN>(d, operand<A_MN>(at), operand<B_MN>(at + kABytes), idesc, i ? 1u : more);
+                        }
+                        tc_commit(&ctl->empty[stage]);
                     }
-                    tc_commit(&ctl->empty[stage]);
+                    __syncwarp();
+                    next_stage();
                 }
-                __syncwarp();
-                if (++in_buf == length) {
-                    in_buf = 0;
-                    d += p.tile_n;
-                    if (p.piece) {
-                        if (elect_one()) tc_commit(&ctl->sums_full[buf]);
-                        __syncwarp();
-                        next_buffer(buf, buf_phase);
-                    }
+                if (LONG) {
+                    if (elect_one()) tc_commit(&ctl->sums_full[buf]);
+                    __syncwarp();
                 }
-                next_stage();
+                next_buffer(buf, buf_phase, p.bufs);
             }
             if (elect_one()) tc_commit(&ctl->done);
             __syncwarp();
             bar_drain(&ctl->done, 0);
         }
     } else if (cols > 0) {
-        if (p.piece) {
+        if (LONG)
             for (int kb = kb0 + p.piece; kb < kb1; kb += p.piece) {
-                // (the last piece, which may be shorter, is over when all are)
-                const uint32_t old = last_buf;
-                next_buffer(last_buf, last_phase);
-                const bool end = kb + p.piece >= kb1;
-                if (!warp_wait(end ? &ctl->done : &ctl->sums_full[last_buf], end ? 0 : last_phase, ctl, p.wait_limit)) break;
+                const uint32_t old = last_buf, at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+                next_buffer(last_buf, last_phase, p.bufs);
+                if (!warp_wait(&ctl->sums_full[last_buf], last_phase, ctl, p.wait_limit)) break;
                 tc_after();
-                const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
                 join_pieces(at + old * p.tile_n, at + last_buf * p.tile_n, (warp >> 2) * 16, cols, 32);
                 if (lane == 0) bar_arrive(&ctl->sums_empty[old]);
             }
-        }
         bar_wait(&ctl->done, 0, ctl, p.wait_limit);
         tc_after();
     }
@@ -577,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
     else if (p.split > 1) cluster_sync();
     if (warp < 8 && cols > 0) {
         const int used = (kb1 - kb0 + p.bufs - 1) / p.bufs;                       // blocks of a buffer
-        const int bufs = p.piece ? 1 : (kb1 - kb0 + used - 1) / used;             // buffers that hold something
+        const int bufs = LONG ? 1 : (kb1 - kb0 + used - 1) / used;             // buffers that hold something
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + last_buf * p.tile_n;
         const uint32_t to = part + (rank * slots * kM + (warp & 3) * 32 + lane) * 16;
 #pragma unroll 1
@@ -1275,10 +1284,11 @@ fi_status_t launch_early(const char *name, void (*kernel)(Params...), dim3 grid,
     return check_launch(name);
 }
 
-// forward products in all their forms; gradients have no activation and bfloat16 results.  PAIRS: that have a tile together, 0: single CTAs
+// forward products in all their forms; gradients have no activation and bfloat16 results.  PAIRS: that have a tile together, 0: single CTAs,
+// -1: single CTAs with long sums
 template <int PAIRS, int DEPTH, bool F32, int ACT, bool A_MN, bool B_MN>
 constexpr LinearKernel linear_kernel_of() {
-    if constexpr (PAIRS == 0) return &linear_split_kernel<F32, ACT, A_MN, B_MN, DEPTH>;
+    if constexpr (PAIRS <= 0) return &linear_split_kernel<F32, ACT, A_MN, B_MN, DEPTH, PAIRS < 0>;
     else return &linear_pair_kernel<F32, ACT, A_MN, B_MN, DEPTH, PAIRS>;
 }
 
@@ -1300,7 +1310,8 @@ LinearKernel linear_kernel(bool f32, int act, bool a_mn, bool b_mn) {
 LinearKernel linear_kernel(int pairs, int depth, bool f32, int act, bool a_mn, bool b_mn) {
     if (pairs == 2) return depth == 2 ? linear_kernel<2, 2>(f32, act, a_mn, b_mn) : linear_kernel<2, 1>(f32, act, a_mn, b_mn);
     if (pairs == 1) return depth == 2 ? linear_kernel<1, 2>(f32, act, a_mn, b_mn) : linear_kernel<1, 1>(f32, act, a_mn, b_mn);
-    return depth == 2 ? linear_kernel<0, 2>(f32, act, a_mn, b_mn) : linear_kernel<0, 1>(f32, act, a_mn, b_mn);
+    if (pairs == 0) return depth == 2 ? linear_kernel<0, 2>(f32, act, a_mn, b_mn) : linear_kernel<0, 1>(f32, act, a_mn, b_mn);
+    return depth == 2 ? linear_kernel<-1, 2>(f32, act, a_mn, b_mn) : linear_kernel<-1, 1>(f32, act, a_mn, b_mn);
 }
 
 using TwoKernel = void (*)(LinearTwo);
@@ -1331,8 +1342,8 @@ fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     for (int form = 0; form < 12; ++form) {                 // of a product: type and activation, or one of two gradients
         const bool back = form >= 10, f32 = !back && form >= 5;
-        for (int i = 0; i < 6 && e == cudaSuccess; ++i)
-            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(linear_kernel(i >> 1, 1 + (i & 1), f32, form % 5, back, form == 11)),
+        for (int i = 0; i < 8 && e == cudaSuccess; ++i)
+            e = cudaFuncSetAttribute(reinterpret_cast<const void *>(linear_kernel((i >> 1) - 1, 1 + (i & 1), f32, form % 5, back, form == 11)),
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - kStaticMost);
     }
     for (int i = 0; i < 4 && e == cudaSuccess; ++i)
@@ -1506,8 +1517,12 @@ fi_status_t plan_launch(Product &x, const LinearPlan &plan, const Matrix &a, boo
         const int room = 512 / p.tile_n, pieces = f32 ? ((blocks + p.split - 1) / p.split + depth + kPiece - 1) / kPiece
                                                       : (int)up(up(p.kb, p.split), kHalfPiece / depth);
         // (in float32 a few blocks more a piece where their number is at the limit)
-        if (pieces > room + (f32 ? 1 : 0)) p.piece = (f32 ? kPiece : kHalfPiece) / depth;
-        else p.bufs = pieces < room ? pieces : room;
+        if (pieces > room + (f32 ? 1 : 0)) {
+            p.piece = (f32 ? kPiece : kHalfPiece) / depth;
+            p.bufs = room < kRing ? room : kRing;
+        } else {
+            p.bufs = pieces < room ? pieces : room;
+        }
     }
     p.tmem_cols = 32;
     while (p.tmem_cols < p.bufs * p.tile_n) p.tmem_cols *= 2;
@@ -1535,7 +1550,7 @@ fi_status_t plan_launch(Product &x, const LinearPlan &plan, const Matrix &a, boo
 }
 
 fi_status_t launch_planned(const Product &x, bool a_mn, bool b_mn, bool f32, int act, const DeviceFacts &facts, cudaStream_t stream, const char *name) {
-    const int pairs = x.plan.pair ? x.p.split : 0, cluster = pairs ? 2 * pairs : x.p.split;
+    const int pairs = x.plan.pair ? x.p.split : x.p.piece ? -1 : 0, cluster = pairs > 0 ? 2 * pairs : x.p.split;
     const long long ctas = pairs == 1 ? 2 * (x.tiles < facts.clusters[1] ? x.tiles : facts.clusters[1]) : x.tiles * cluster;
     return launch_early(name, linear_kernel(pairs, x.depth, f32, act, a_mn, b_mn), dim3((unsigned)ctas), kThreads, x.smem, dim3(cluster), stream, x.map_a,
                         x.map_b, x.p);
