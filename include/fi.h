@@ -669,6 +669,8 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
  * Products on the tensor cores, sums in fp32; one rounding at the end.  The tensor cores cut what they add (some 2^-24 of the sum for 16
  * values, always towards zero), so a float32 out is summed up in pieces of about 512 values outside of them, a bfloat16 out (and dx and
  * dweight below) in pieces of 16,384 (off by 2^-15 of the sum, before it is rounded to 2^-8), however long the sums are.
+ * Activations in fp32, relative to the value itself: some 2^-20, and what an exponent's rounding does far out in the left tail (1.1 z^2 2^-24 for
+ * FI_ACT_GELU, |z| 2^-23 for FI_ACT_SILU, |z|^3 2^-22 for FI_ACT_GELU_TANH); values below 2^-120 may be 0.
  * in_dim and out_dim multiples of 8, they and tokens at most 2^30; rows of x and weight start on 16-byte boundaries; strides in elements.
  * Asynchronous, on the current device; no workspace, so calls may overlap.  x and weight must not be written by the call's own results.
  *

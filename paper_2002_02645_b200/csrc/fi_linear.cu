@@ -288,16 +288,38 @@ constexpr float kLog2e = 1.4426950408889634f, kGeluTanh = 0.044715f, kGeluTwice 
 // 1 / (1 + 2^-x)
 __device__ __forceinline__ float logistic2(float x) { return recip_fast(1.f + exp2_fast(-x)); }
 
-// Phi(z) = erfc(-z / sqrt 2) / 2, from erfc(a) = t (a1 + t (a2 + ..)) exp(-a^2), t = 1 / (1 + p a), for a >= 0 (Abramowitz and Stegun, Handbook of
-// Mathematical Functions, 7.1.26: off by 1.5e-7 at most).  density: exp(-z^2 / 2)
-__device__ __forceinline__ float normal_cdf(float z, float &density) {
-    const float t = recip_fast(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.f));
-    density = exp2_fast(z * z * (-0.5f * kLog2e));
-    float q = fmaf(t, 1.061405429f, -1.453152027f);
-    q = fmaf(t, q, 1.421413741f);
-    q = fmaf(t, q, -0.284496736f);
-    q = fmaf(t, q, 0.254829592f) * t * (0.5f * density);
-    return z >= 0.f ? 1.f - q : q;
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, float c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(pair_of(c, c)));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Phi(z) = erfc(-z / sqrt 2) / 2, from erfc(a) = exp(-a^2) t P(t), t = 1 / (1 + 0.43 a), for a >= 0.  P is the polynomial of seventh degree whose
+// largest error relative to erfc is least (8.5e-8, by Remez' exchange; half of it here), so that the left tail is right to a few 2^-24 of
+// itself and to what the exponent's rounding does: 1.1 z^2 2^-24.  density: exp(-z^2 / 2).  Two values at a time: the polynomial of one at a time
+// makes the slopes' kernel slower, 45.3 instead of 42.9 us for 4,095 x 8,192.
+__device__ __forceinline__ void normal_cdf(float z0, float z1, float (&cdf)[2], float (&density)[2]) {
+    constexpr float c[8] = {0.12125748710f, 0.12218486825f, 0.10249370120f, 0.12336100105f, -0.042744353075f, 0.19172071880f, -0.15510789720f, 0.03683451189f};
+    const uint64_t t = pair_of(recip_fast(fmaf(fabsf(z0), 0.43f * 0.70710678f, 1.f)), recip_fast(fmaf(fabsf(z1), 0.43f * 0.70710678f, 1.f)));
+    density[0] = exp2_fast(z0 * z0 * (-0.5f * kLog2e));
+    density[1] = exp2_fast(z1 * z1 * (-0.5f * kLog2e));
+    uint64_t q = pair_of(c[7], c[7]);
+#pragma unroll
+    for (int i = 6; i >= 0; --i) q = fma2(t, q, c[i]);
+    q = mul2(mul2(q, t), pair_of(density[0], density[1]));
+    float q0, q1;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(q0), "=f"(q1) : "l"(q));
+    cdf[0] = z0 >= 0.f ? 1.f - q0 : q0;
+    cdf[1] = z1 >= 0.f ? 1.f - q1 : q1;
 }
 
 template <int ACT, int N>
@@ -309,9 +331,11 @@ __device__ __forceinline__ void activate(float (&z)[N]) {
             break;
         case FI_ACT_GELU:
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float density;
-                z[i] *= normal_cdf(z[i], density);
+            for (int i = 0; i < N; i += 2) {
+                float cdf[2], density[2];
+                normal_cdf(z[i], z[i + 1], cdf, density);
+                z[i] *= cdf[0];
+                z[i + 1] *= cdf[1];
             }
             break;
         case FI_ACT_GELU_TANH:
@@ -334,17 +358,11 @@ __device__ __forceinline__ float within(float z, float most) {
     return y;
 }
 
-// slope of the activation
+// slopes of the activation, of two values
 template <int ACT>
 __device__ __forceinline__ float slope(float z) {
     switch (ACT) {
         case FI_ACT_RELU: return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
-        case FI_ACT_GELU: {
-            z = within(z, 20.f);
-            float density;
-            const float whole = normal_cdf(z, density);
-            return fmaf(z * 0.39894228f, density, whole);
-        }
         case FI_ACT_GELU_TANH: {
             z = within(z, 20.f);
             const float zz = z * z, s = logistic2(z * fmaf(kGeluTwice * kGeluTanh * kLog2e, zz, kGeluTwice * kLog2e));
@@ -356,6 +374,20 @@ __device__ __forceinline__ float slope(float z) {
             return s * fmaf(z, 1.f - s, 1.f);
         }
         default: return 1.f;
+    }
+}
+template <int ACT>
+__device__ __forceinline__ void slopes(float &z0, float &z1) {
+    if (ACT == FI_ACT_GELU) {
+        z0 = within(z0, 20.f);
+        z1 = within(z1, 20.f);
+        float cdf[2], density[2];
+        normal_cdf(z0, z1, cdf, density);
+        z0 = fmaf(z0 * 0.39894228f, density[0], cdf[0]);
+        z1 = fmaf(z1 * 0.39894228f, density[1], cdf[1]);
+    } else {
+        z0 = slope<ACT>(z0);
+        z1 = slope<ACT>(z1);
     }
 }
 
@@ -1225,8 +1257,10 @@ __global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const __
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float lo = __uint_as_float(aw[i] << 16), hi = __uint_as_float(aw[i] & 0xffff0000u);
-                    lo *= slope<ACT>(__uint_as_float(bw[i] << 16));
-                    hi *= slope<ACT>(__uint_as_float(bw[i] & 0xffff0000u));
+                    float lo_slope = __uint_as_float(bw[i] << 16), hi_slope = __uint_as_float(bw[i] & 0xffff0000u);
+                    slopes<ACT>(lo_slope, hi_slope);
+                    lo *= lo_slope;
+                    hi *= hi_slope;
                     sum[2 * i] += lo;
                     sum[2 * i + 1] += hi;
                     o[i] = pack2(lo, hi);
