@@ -674,11 +674,13 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
  * in_dim and out_dim multiples of 8, they and tokens at most 2^30; rows of x and weight start on 16-byte boundaries; strides in elements.
  * Asynchronous, on the current device; no workspace, so calls may overlap.  x and weight must not be written by the call's own results.
  *
- * fi_linear_backward: gradients for dy [tokens x out_dim] bfloat16 (of the result without its residual, whose gradient is dy itself):
+ * fi_linear_backward: gradients for dy [tokens x out_dim], bfloat16 (of the result without its residual, whose gradient is dy itself):
  *   dz = dy act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over tokens of dz
  * dx, dweight bfloat16, dbias float; each nullable.  dz is rounded to bfloat16 for the products (2^-8 of each value at most), not for dbias;
- * without an activation it is dy and preact is not read.  dbias is summed in a fixed order.  `workspace`: fi_linear_backward_workspace
- * bytes of device memory on a 16-byte boundary, contents free, not shared by calls that overlap; may be null without an activation.
+ * without an activation it is dy and preact is not read.  dbias is summed in a fixed order.  With dy_f32 dy is float32, as the gradient of
+ * a float32 result is (rows on 16-byte boundaries): only dz is rounded, dbias is the sum of what dy holds.  `workspace`:
+ * fi_linear_backward_workspace bytes of device memory (with dy_f32 that of an activation, whichever) on a 16-byte boundary, contents free, not
+ * shared by calls that overlap; may be null without an activation and dy_f32.
  *
  * fi_linear_poll_status: synchronises the current device; FI_ERR_TIMEOUT when a bounded wait inside a kernel of these calls ran out
  * there since the last poll (the word is cleared).
@@ -714,6 +716,7 @@ typedef struct {
     int64_t tokens;
     int32_t in_dim, out_dim;
     int32_t activation;
+    int32_t dy_f32;             /* dy is float32, not bfloat16 */
 } fi_linear_backward_t;
 fi_status_t fi_linear_backward(const fi_linear_backward_t *args, void *cuda_stream);
 int64_t fi_linear_backward_workspace(int64_t tokens, int32_t out_dim, int32_t activation);

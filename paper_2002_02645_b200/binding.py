@@ -105,7 +105,7 @@ class fi_linear_t(ctypes.Structure):
 class fi_linear_backward_t(ctypes.Structure):
     _fields_ = _fields(ctypes.c_void_p, "x weight dy preact dx dweight dbias workspace") \
         + _fields(ctypes.c_int64, "x_stride weight_stride dy_stride preact_stride dx_stride dweight_stride tokens") \
-        + _fields(ctypes.c_int32, "in_dim out_dim activation")
+        + _fields(ctypes.c_int32, "in_dim out_dim activation dy_f32")
 
 
 class fi_layer_norm_t(ctypes.Structure):
@@ -1052,37 +1052,41 @@ def _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dt
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *, activation: str = "none",
            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
            count: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None, preact: Optional[torch.Tensor] = None,
-           wait_limit: int = 0) -> torch.Tensor:
+           grad_dtype: torch.dtype = torch.bfloat16, wait_limit: int = 0) -> torch.Tensor:
     """fi_linear: act(x weight^T + bias) + residual, of x [tokens, in_dim] and weight [out_dim, in_dim] in bfloat16.  With `rows`, token i
     belongs to row rows[i] of residual and out (out may be residual); with `count` only that many tokens are real.  preact takes the sums
     before the activation.  Gradients flow to x, weight, bias and residual; not through rows, count, out or preact, which are refused
-    where one is asked for."""
+    where one is asked for.  grad_dtype is the type in which the gradient of a float32 result is taken: bfloat16 rounds each of its values
+    (2^-8) before the gradients of x, weight and bias are formed; float32 takes them as they are, and only what the products read is rounded."""
+    if grad_dtype is not torch.bfloat16 and grad_dtype is not torch.float32:
+        raise ValueError("grad_dtype must be bfloat16 or float32")
     if (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
             or residual is not None and residual.requires_grad) and torch.is_grad_enabled():
         if out is not None or rows is not None or count is not None or preact is not None:
             raise ValueError("out, rows, count or preact is given, but a gradient is asked for")
-        return _Linear.apply(x, weight, bias, residual, activation, out_dtype, wait_limit)
+        return _Linear.apply(x, weight, bias, residual, activation, out_dtype, grad_dtype, wait_limit)
     return _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
 
 
 def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], dy: torch.Tensor, *, preact: Optional[torch.Tensor] = None,
                     activation: str = "none", with_bias: bool = False, dx: Optional[torch.Tensor] = None,
-                    dweight: Optional[torch.Tensor] = None):
-    """fi_linear_backward: (dx, dweight, dbias) for dy, the bfloat16 gradient of the result.  Without weight there is no dx, without x no
-    dweight, and dbias only with with_bias."""
+                    dweight: Optional[torch.Tensor] = None, dy_dtype: torch.dtype = torch.bfloat16):
+    """fi_linear_backward: (dx, dweight, dbias) for dy, the gradient of the result, of type dy_dtype (bfloat16 or float32).  Without weight
+    there is no dx, without x no dweight, and dbias only with with_bias."""
     lib, kind, index = load_library(), _activation(activation), dy.get_device()
-    if dy.dtype is not torch.bfloat16 or dy.dim() != 2 or index < 0:
-        raise ValueError("dy must be a bfloat16 [tokens, out_dim] tensor on a GPU")
+    if dy.dtype is not dy_dtype or dy_dtype not in _FI_DTYPE or dy.dim() != 2 or index < 0:
+        raise ValueError("dy must be a [tokens, out_dim] tensor of dy_dtype, bfloat16 or float32, on a GPU")
     tokens, out_dim = dy.shape
+    wide = dy_dtype is torch.float32
     if x is None and weight is None:
         in_dim = 8                                         # nothing but dbias
     else:
         in_dim = (x if x is not None else weight).shape[-1]
-    strides = [0, 0, _check_rows(dy, "dy", index, torch.bfloat16, tokens, out_dim), 0, 0, 0]
+    strides = [0, 0, _check_rows(dy, "dy", index, dy_dtype, tokens, out_dim), 0, 0, 0]
     if weight is not None:
         strides[1] = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
         if dx is None:
-            dx, strides[4] = dy.new_empty((tokens, in_dim)), in_dim
+            dx, strides[4] = dy.new_empty((tokens, in_dim), dtype=torch.bfloat16), in_dim
         else:
             strides[4] = _check_rows(dx, "dx", index, torch.bfloat16, tokens, in_dim)
     elif dx is not None:
@@ -1090,7 +1094,7 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
     if x is not None:
         strides[0] = _check_rows(x, "x", index, torch.bfloat16, tokens, in_dim)
         if dweight is None:
-            dweight, strides[5] = dy.new_empty((out_dim, in_dim)), in_dim
+            dweight, strides[5] = dy.new_empty((out_dim, in_dim), dtype=torch.bfloat16), in_dim
         else:
             strides[5] = _check_rows(dweight, "dweight", index, torch.bfloat16, out_dim, in_dim)
     elif dweight is not None:
@@ -1101,10 +1105,10 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
         strides[3] = _check_rows(preact, "preact", index, torch.bfloat16, tokens, out_dim)
     dbias = dy.new_empty(out_dim, dtype=torch.float32) if with_bias else None
     work = None
-    if kind:
-        work = dy.new_empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind), dtype=torch.uint8)
+    if kind or wide:
+        work = dy.new_empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind or 1), dtype=torch.uint8)
     args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
-                                 *strides, tokens, in_dim, out_dim, kind)
+                                 *strides, tokens, in_dim, out_dim, kind, 1 if wide else 0)
     _on_device(index, lib.fi_linear_backward, args)
     return dx, dweight, dbias
 
@@ -1115,22 +1119,23 @@ def linear_poll_status(device: int = 0) -> None:
         _check(load_library().fi_linear_poll_status())
 
 
-def _as_rows(t: torch.Tensor) -> torch.Tensor:
-    """t, or a copy that the kernels read: bfloat16 values of a row side by side, rows on 16-byte boundaries."""
-    t = t.to(torch.bfloat16)
+def _as_rows(t: torch.Tensor, dtype: torch.dtype) -> torch.Tensor:
+    """t, or a copy that the kernels read: values of a row side by side, rows on 16-byte boundaries."""
+    t = t.to(dtype)
     return t if t.stride(1) == 1 and t.stride(0) % 8 == 0 and t.stride(0) >= t.size(1) and t.data_ptr() % 16 == 0 \
         else t.clone(memory_format=torch.contiguous_format)
 
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, activation, out_dtype, wait_limit):
+    def forward(ctx, x, weight, bias, residual, activation, out_dtype, grad_dtype, wait_limit):
         preact = None
         if _activation(activation):
             preact = torch.empty((x.size(0), weight.size(0)), dtype=torch.bfloat16, device=x.device)
         y = _linear_call(x, weight, bias, activation, residual, None, None, None, out_dtype, preact, wait_limit)
         ctx.save_for_backward(x, weight, preact)
         ctx.activation, ctx.bias = activation, None if bias is None else bias.shape
+        ctx.dy_dtype = torch.bfloat16 if y.dtype is torch.bfloat16 else grad_dtype
         return y
 
     @staticmethod
@@ -1140,9 +1145,9 @@ class _Linear(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx = dw = db = None
         if need[0] or need[1] or need[2]:
-            dx, dw, db = linear_backward(x if need[1] else None, weight if need[0] else None, _as_rows(dy), preact=preact,
-                                         activation=ctx.activation, with_bias=need[2])
-        return dx, dw, None if db is None else db.view(ctx.bias), dy if need[3] else None, None, None, None
+            dx, dw, db = linear_backward(x if need[1] else None, weight if need[0] else None, _as_rows(dy, ctx.dy_dtype), preact=preact,
+                                         activation=ctx.activation, with_bias=need[2], dy_dtype=ctx.dy_dtype)
+        return dx, dw, None if db is None else db.view(ctx.bias), dy if need[3] else None, None, None, None, None
 
 
 def _norm_types(x: torch.Tensor, y_dtype, weight, bias, index: int):

@@ -1226,12 +1226,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_two_kernel(const __grid_co
 // dz = dy act'(preact), and dbias, the sums of its columns (of dy itself without an activation: nothing else is stored then).  A CTA takes 64
 // (where there are few, 16) columns, eight per thread, and its share of the rows, four of them on their way per thread; the CTAs of a cluster have the same
 // columns, whose sums the first one adds up in the order of their ranks.  Bound by the traffic.
-constexpr int kSlopeThreads = 256, kSlopeAhead = 4;
+// dz is rounded to bfloat16 (2^-8 of it), the type of the tensor cores' other operand; its sums are not.  DY32: dy is float32.
+constexpr int kSlopeThreads = 256;
 
-template <int ACT, int kSlopeCols>
-__global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const __nv_bfloat16 *dy, long long ld_dy, const __nv_bfloat16 *z, long long ld_z,
+template <int ACT, int kSlopeCols, bool DY32>
+__global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const void *dy, long long ld_dy, const __nv_bfloat16 *z, long long ld_z,
                                                                      __nv_bfloat16 *dz, float *dbias, long long rows, int cols) {
-    constexpr int kSlopeRows = kSlopeThreads * 8 / kSlopeCols;
+    constexpr int kSlopeRows = kSlopeThreads * 8 / kSlopeCols, kSlopeAhead = DY32 ? 2 : 4;      // (64 registers a thread)
     __shared__ float s[kSlopeRows][kSlopeCols + 1], mine[kSlopeCols];
     const int part = threadIdx.x & (kSlopeCols / 8 - 1), group = threadIdx.x / (kSlopeCols / 8);
     const int c = blockIdx.x * kSlopeCols + part * 8;
@@ -1239,24 +1240,27 @@ __global__ void __launch_bounds__(kSlopeThreads, 4) linear_slope_kernel(const __
     in_turn();
     if (c < cols)
         for (long long r0 = (long long)blockIdx.y * kSlopeRows * kSlopeAhead + group; r0 < rows; r0 += (long long)gridDim.y * kSlopeRows * kSlopeAhead) {
-            uint4 a[kSlopeAhead], b[kSlopeAhead];
+            uint4 a[kSlopeAhead][DY32 ? 2 : 1], b[kSlopeAhead];
 #pragma unroll
             for (int u = 0; u < kSlopeAhead; ++u) {
                 const long long r = r0 + u * kSlopeRows;
-                a[u] = b[u] = make_uint4(0, 0, 0, 0);
+                a[u][0] = a[u][DY32 ? 1 : 0] = b[u] = make_uint4(0, 0, 0, 0);
                 if (r < rows) {
-                    a[u] = __ldcs(reinterpret_cast<const uint4 *>(dy + r * ld_dy + c));
+                    const uint4 *const from = reinterpret_cast<const uint4 *>(static_cast<const char *>(dy) + (r * ld_dy + c) * (DY32 ? 4 : 2));
+                    a[u][0] = __ldcs(from);
+                    if (DY32) a[u][DY32 ? 1 : 0] = __ldcs(from + 1);
                     if (ACT != FI_ACT_NONE) b[u] = __ldcs(reinterpret_cast<const uint4 *>(z + r * ld_z + c));
                 }
             }
 #pragma unroll
             for (int u = 0; u < kSlopeAhead; ++u) {
                 const long long r = r0 + u * kSlopeRows;
-                const uint32_t aw[4] = {a[u].x, a[u].y, a[u].z, a[u].w}, bw[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
+                const uint4 &more = a[u][DY32 ? 1 : 0];
+                const uint32_t aw[8] = {a[u][0].x, a[u][0].y, a[u][0].z, a[u][0].w, more.x, more.y, more.z, more.w}, bw[4] = {b[u].x, b[u].y, b[u].z, b[u].w};
                 uint32_t o[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float lo = __uint_as_float(aw[i] << 16), hi = __uint_as_float(aw[i] & 0xffff0000u);
+                    float lo = __uint_as_float(DY32 ? aw[2 * i] : aw[i] << 16), hi = __uint_as_float(DY32 ? aw[2 * i + 1] : aw[i] & 0xffff0000u);
                     float lo_slope = __uint_as_float(bw[i] << 16), hi_slope = __uint_as_float(bw[i] & 0xffff0000u);
                     slopes<ACT>(lo_slope, hi_slope);
                     lo *= lo_slope;
@@ -1645,13 +1649,17 @@ int slope_parts(long long tokens, int out_dim, int width, int sms) {
     return parts;
 }
 
-template <int WIDTH>
+template <int WIDTH, bool DY32>
 auto slope_kernel(int act) {
-    return act == FI_ACT_RELU        ? linear_slope_kernel<FI_ACT_RELU, WIDTH>
-           : act == FI_ACT_GELU      ? linear_slope_kernel<FI_ACT_GELU, WIDTH>
-           : act == FI_ACT_GELU_TANH ? linear_slope_kernel<FI_ACT_GELU_TANH, WIDTH>
-           : act == FI_ACT_SILU      ? linear_slope_kernel<FI_ACT_SILU, WIDTH>
-                                     : linear_slope_kernel<FI_ACT_NONE, WIDTH>;
+    return act == FI_ACT_RELU        ? linear_slope_kernel<FI_ACT_RELU, WIDTH, DY32>
+           : act == FI_ACT_GELU      ? linear_slope_kernel<FI_ACT_GELU, WIDTH, DY32>
+           : act == FI_ACT_GELU_TANH ? linear_slope_kernel<FI_ACT_GELU_TANH, WIDTH, DY32>
+           : act == FI_ACT_SILU      ? linear_slope_kernel<FI_ACT_SILU, WIDTH, DY32>
+                                     : linear_slope_kernel<FI_ACT_NONE, WIDTH, DY32>;
+}
+template <int WIDTH>
+auto slope_kernel(int act, bool dy32) {
+    return dy32 ? slope_kernel<WIDTH, true>(act) : slope_kernel<WIDTH, false>(act);
 }
 
 }  // namespace
@@ -1727,13 +1735,15 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     }
     fi_status_t st = check_sizes(a->tokens, a->in_dim, a->out_dim, a->activation, name);
     if (st != FI_OK) return st;
-    const bool slopes = a->activation != FI_ACT_NONE;
+    const bool slopes = a->activation != FI_ACT_NONE, dy32 = a->dy_f32 != 0, apart = slopes || dy32;      // apart: dz is not dy
     if ((a->tokens > 0 && (!a->dy || (slopes && !a->preact) || (a->dx && !a->weight) || (a->dweight && !a->x))) ||
-        (slopes && (a->dx || a->dweight) && a->tokens > 0 && !a->workspace)) {
+        (apart && (a->dx || a->dweight) && a->tokens > 0 && !a->workspace)) {
         set_error("%s: null pointer", name);
         return FI_ERR_INVALID_ARG;
     }
-    if (!tma_rows(a->dy, a->tokens, a->out_dim, a->dy_stride) || (slopes && !tma_rows(a->preact, a->tokens, a->out_dim, a->preact_stride)) ||
+    const bool dy_rows = dy32 ? aligned16(a->dy) && (a->tokens <= 1 || (a->dy_stride % 4 == 0 && a->dy_stride >= a->out_dim))
+                              : tma_rows(a->dy, a->tokens, a->out_dim, a->dy_stride);
+    if (!dy_rows || (slopes && !tma_rows(a->preact, a->tokens, a->out_dim, a->preact_stride)) ||
         (a->dx && !tma_rows(a->weight, a->out_dim, a->in_dim, a->weight_stride)) ||
         (a->dweight && !tma_rows(a->x, a->tokens, a->in_dim, a->x_stride)) || !aligned16(a->workspace)) {
         set_error("%s: rows of x, weight, dy and preact must start on 16-byte boundaries and not overlap", name);
@@ -1754,16 +1764,15 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         if (e == cudaSuccess && a->dbias) e = cudaMemsetAsync(a->dbias, 0, (size_t)a->out_dim * 4, stream);
         return e == cudaSuccess ? FI_OK : cuda_fail(e, name);
     }
-    __nv_bfloat16 *const dz = slopes && (a->dx || a->dweight) ? static_cast<__nv_bfloat16 *>(a->workspace) : nullptr;
+    __nv_bfloat16 *const dz = apart && (a->dx || a->dweight) ? static_cast<__nv_bfloat16 *>(a->workspace) : nullptr;
     if (dz || a->dbias) {
         const int width = a->out_dim <= 64 * 16 && a->tokens >= 1024 ? 16 : 64, parts = slope_parts(a->tokens, a->out_dim, width, facts->clusters[0]);
-        st = launch_early(name, width == 16 ? slope_kernel<16>(a->activation) : slope_kernel<64>(a->activation),
-                          dim3((a->out_dim + width - 1) / width, parts), kSlopeThreads, 0, dim3(1, parts), stream, static_cast<const __nv_bfloat16 *>(a->dy),
-                          (long long)a->dy_stride, static_cast<const __nv_bfloat16 *>(a->preact), (long long)a->preact_stride, dz, a->dbias,
+        st = launch_early(name, width == 16 ? slope_kernel<16>(a->activation, dy32) : slope_kernel<64>(a->activation, dy32),
+                          dim3((a->out_dim + width - 1) / width, parts), kSlopeThreads, 0, dim3(1, parts), stream, a->dy, (long long)a->dy_stride, static_cast<const __nv_bfloat16 *>(a->preact), (long long)a->preact_stride, dz, a->dbias,
                           (long long)a->tokens, (int)a->out_dim);
         if (st != FI_OK) return st;
     }
-    const Matrix g = slopes ? Matrix{dz, a->tokens, a->out_dim, a->out_dim} : Matrix{a->dy, a->tokens, a->out_dim, a->dy_stride};
+    const Matrix g = apart ? Matrix{dz, a->tokens, a->out_dim, a->out_dim} : Matrix{a->dy, a->tokens, a->out_dim, a->dy_stride};
     const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
     LinearParams dx = {}, dw = {};
     dx.wait_limit = dw.wait_limit = kWaitLimit;
