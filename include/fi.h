@@ -749,6 +749,7 @@ typedef struct {
     int64_t x_stride, dy_stride, out_stride;
     int64_t tokens;
     int64_t x_rows;             /* read with `rows` only */
+    int64_t wait_limit;         /* SM cycles a wait inside the kernel may take; 0: 8e9 (about 4 s), also the most.  For tests */
     int32_t dim;
     int32_t rms;
     int32_t x_dtype, y_dtype;   /* fi_dtype_t */

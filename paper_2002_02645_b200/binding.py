@@ -110,7 +110,7 @@ class fi_linear_backward_t(ctypes.Structure):
 
 class fi_layer_norm_t(ctypes.Structure):
     _fields_ = _fields(ctypes.c_void_p, "x dy out weight bias rows tokens_dev dweight dbias workspace") \
-        + _fields(ctypes.c_int64, "x_stride dy_stride out_stride tokens x_rows") \
+        + _fields(ctypes.c_int64, "x_stride dy_stride out_stride tokens x_rows wait_limit") \
         + _fields(ctypes.c_int32, "dim rms x_dtype y_dtype") + [("eps", ctypes.c_float)]
 
 
@@ -1162,7 +1162,7 @@ def _norm_types(x: torch.Tensor, y_dtype, weight, bias, index: int):
     return _FI_DTYPE[x.dtype], _FI_DTYPE[y_dtype]
 
 
-def _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out):
+def _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit=0):
     index = x.get_device()
     if out_dtype is None:
         out_dtype = x.dtype if out is None else out.dtype
@@ -1183,29 +1183,29 @@ def _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out):
     else:
         out_stride = _check_rows(out, "out", index, out_dtype, tokens, dim)
     args = _pack_layer_norm(x.data_ptr(), 0, out.data_ptr(), _at(weight), _at(bias), _at(rows), _at(count), 0, 0, 0, x_stride, 0, out_stride, tokens,
-                            x_rows, dim, 1 if rms else 0, *kinds, eps)
+                            x_rows, wait_limit, dim, 1 if rms else 0, *kinds, eps)
     _on_device(index, (_lib or load_library()).fi_layer_norm, args)
     return out
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, eps: float = 1e-5, rms: bool = False,
                out_dtype: Optional[torch.dtype] = None, rows: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
-               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+               out: Optional[torch.Tensor] = None, wait_limit: int = 0) -> torch.Tensor:
     """fi_layer_norm: the rows of x [rows, dim] normed by mean and variance, or by root mean square.  With `rows`, token i of the result is
     row rows[i] of x; with `count` only that many tokens are real (the others are left as they are).  Gradients flow to x, weight and
     bias; not through rows, count or out, which are refused where one is asked for."""
     if (x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad) and torch.is_grad_enabled():
         if out is not None or rows is not None or count is not None:
             raise ValueError("out, rows or count is given, but a gradient is asked for")
-        return _LayerNorm.apply(x, weight, bias, eps, rms, out_dtype)
-    return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out)
+        return _LayerNorm.apply(x, weight, bias, eps, rms, out_dtype, wait_limit)
+    return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit)
 
 
 _layer_norm_work = {}      # values of fi_layer_norm_workspace by dim
 
 
 def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: torch.Tensor, *, eps: float = 1e-5, rms: bool = False,
-                        with_bias: bool = False, dx: Optional[torch.Tensor] = None):
+                        with_bias: bool = False, dx: Optional[torch.Tensor] = None, wait_limit: int = 0):
     """fi_layer_norm_backward: (dx, dweight, dbias) from the forward pass's x and weight and the gradient of its result.  Without a weight
     there is no dweight, and dbias only with with_bias.  dx may be dy."""
     lib, index = load_library(), x.get_device()
@@ -1229,7 +1229,7 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
         if with_bias:
             db = work.new_empty(dim)
     args = _pack_layer_norm(x.data_ptr(), dy.data_ptr(), dx.data_ptr(), _at(weight), 0, 0, 0, _at(dw), _at(db), _at(work), x_stride, dy_stride, dx_stride,
-                            tokens, 0, dim, 1 if rms else 0, *kinds, eps)
+                            tokens, 0, wait_limit, dim, 1 if rms else 0, *kinds, eps)
     _on_device(index, lib.fi_layer_norm_backward, args)
     return dx, dw, db
 
@@ -1242,10 +1242,10 @@ def layer_norm_poll_status(device: int = 0) -> None:
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps, rms, out_dtype):
+    def forward(ctx, x, weight, bias, eps, rms, out_dtype, wait_limit):
         ctx.save_for_backward(x, weight)
         ctx.eps, ctx.rms, ctx.bias = eps, rms, None if bias is None else bias.shape
-        return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, None, None, None)
+        return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, None, None, None, wait_limit)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -1254,7 +1254,7 @@ class _LayerNorm(torch.autograd.Function):
         if dy.stride(1) != 1 or dy.stride(0) < dy.size(1):
             dy = dy.contiguous()
         dx, dw, db = layer_norm_backward(x, weight, dy, eps=ctx.eps, rms=ctx.rms, with_bias=ctx.needs_input_grad[2])
-        return dx, None if dw is None else dw.view_as(weight), None if db is None else db.view(ctx.bias), None, None, None
+        return dx, None if dw is None else dw.view_as(weight), None if db is None else db.view(ctx.bias), None, None, None, None
 
 
 class KvCache:

@@ -28,7 +28,7 @@ struct RowNormParams {
     const float *weight, *bias;
     const int32_t *rows, *count;
     float *partial;                    // backward: [CTAs][2][dim]; nullable
-    long long x_stride, dy_stride, out_stride, tokens, x_rows;
+    long long x_stride, dy_stride, out_stride, tokens, x_rows, wait_limit;
     int dim, rms;
     float eps, inv_dim;
 };
@@ -310,8 +310,9 @@ __global__ void __launch_bounds__(LANES ? 256 : 512) layer_norm_backward_kernel(
 
 // ---- long rows on 16-byte boundaries ----
 //
-// A CTA walks over the rows, R at a time.  A warp of its own brings them by bulk copies into a ring of stages in shared memory, several
-// ahead of the ones that are worked on (issued by a thread that works on them they hold up all the others: 100 us, not 59, for 16,384
+// A CTA walks over the rows, R at a time.  A warp of its own brings them by bulk copies into a ring of stages in shared memory, as many
+// ahead of the ones that are worked on as there is room for: up to 5 of 2,048 values, of 16,384 values in bfloat16 1 (gradients) to 5, of more
+// than 11,160 float32 values with a float32 gradient none (issued by a thread that works on them they hold up all the others: 100 us, not 59, for 16,384
 // rows of 4,096).  Weights stay in registers, of the gradients in shared memory: the ring leaves L1 too small for them.
 // Values are worked on in pairs.
 constexpr int kMaxRing = 6;
@@ -373,19 +374,25 @@ __device__ __forceinline__ void pairs_out(void *base, long long at, const uint64
     store8<F32>(base, at, x);
 }
 
+constexpr long long kWaitLimit = 8000000000ll;   // SM cycles (about 4 s)
+constexpr long long kShortLimit = 1 << 20;       // limits below it are a test's
+constexpr long long kDrainLimit = 200000000ll;   // (about 0.1 s)
+
 struct RingBars {
-    uint64_t full[kMaxRing], empty[kMaxRing];
+    uint64_t full[kMaxRing], empty[kMaxRing], never;
+    volatile int gave_up;
 };
 
-// The ring of a CTA, seen by one of its warps.  Waits have a limit in SM cycles (about 4 s); once one ran out, 0.01 s, and the status word
-// says that the results are not valid.
+// The ring of a CTA, seen by one of its warps.  Waits have a limit in SM cycles; once one ran out, no row is asked for any more, every later
+// wait of the CTA gives up at once, the kernel runs to its end with whatever is in its buffers, and the status word says that the results are
+// not valid.
 struct Ring {
     RingBars *bars;
     uint32_t base, stage_bytes;
     int stages;
+    long long limit;
     int stage = 0;
     uint32_t phase = 0;
-    long long limit = 8000000000ll;
 
     static __device__ __forceinline__ uint32_t at(const uint64_t *bar) { return (uint32_t)__cvta_generic_to_shared(bar); }
     __device__ __forceinline__ void set_up(int readers) const {
@@ -393,28 +400,59 @@ struct Ring {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(at(bars->full + i)) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(at(bars->empty + i)), "r"(readers) : "memory");
         }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(at(&bars->never)) : "memory");
+        bars->gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    __device__ __forceinline__ void wait(const uint64_t *bar, uint32_t parity) {
-        uint32_t there = 0;
-        for (long long t0 = clock64(); !there && clock64() - t0 < limit;)
-            asm volatile(
-                "{\n"
-                ".reg .pred q;\n"
-                "mbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2;\n"
-                "selp.u32 %0, 1, 0, q;\n"
-                "}\n"
-                : "=r"(there)
-                : "r"(at(bar)), "r"(parity)
-                : "memory");
-        if (!there) {
-            limit = 20000000;
-            atomicOr(&g_layer_norm_status, 1);
+    static __device__ __forceinline__ bool there(const uint64_t *bar, uint32_t parity) {
+        uint32_t yes;
+        asm volatile(
+            "{\n"
+            ".reg .pred q;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2;\n"
+            "selp.u32 %0, 1, 0, q;\n"
+            "}\n"
+            : "=r"(yes)
+            : "r"(at(bar)), "r"(parity)
+            : "memory");
+        return yes != 0;
+    }
+    __device__ __forceinline__ bool wait(const uint64_t *bar, uint32_t parity) const {
+        if (there(bar, parity)) return true;
+        for (const long long t0 = clock64(); !there(bar, parity);) {
+            if (bars->gave_up) return false;
+            if (clock64() - t0 > limit) {
+                bars->gave_up = 1;
+                atomicOr(&g_layer_norm_status, 1);
+                return false;
+            }
+        }
+        return true;
+    }
+    __device__ __forceinline__ void wait_full() const { wait(bars->full + stage, phase); }
+    // false: nothing is to be asked for any more
+    __device__ __forceinline__ bool wait_empty() const { return wait(bars->empty + stage, phase ^ 1) && !bars->gave_up; }
+    // so that a wait runs out for certain
+    __device__ __forceinline__ void short_limit() const {
+        if (limit < kShortLimit && threadIdx.x == 0) wait(&bars->never, 0);
+    }
+    // The end of the warp that asks for rows: all that it has started lands before it leaves, so that none of it comes down where another
+    // CTA is by then.  `issued`: stages in use since the ring began, up to all of them
+    __device__ __forceinline__ void drain(int issued) {
+        for (; issued > 0; --issued) {
+            if (stage == 0) {
+                stage = stages;
+                phase ^= 1;
+            }
+            --stage;
+            for (const long long t0 = clock64(); !there(bars->full + stage, phase);)
+                if (clock64() - t0 > (bars->gave_up ? kDrainLimit : kWaitLimit)) {
+                    atomicOr(&g_layer_norm_status, 1);
+                    return;
+                }
         }
     }
-    __device__ __forceinline__ void wait_full() { wait(bars->full + stage, phase); }
-    __device__ __forceinline__ void wait_empty() { wait(bars->empty + stage, phase ^ 1); }
     __device__ __forceinline__ void next() {
         if (++stage == stages) {
             stage = 0;
@@ -499,14 +537,15 @@ __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_ring_k
         const long long row = p.rows ? p.rows[token] : token;
         return row >= 0 && row < p.x_rows ? row : -1ll;
     };
-    Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages};
+    Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages, p.wait_limit};
     if (threadIdx.x == 0) r.set_up(THREADS / 32);
     in_turn();
     tokens = actual_tokens(p);
     const long long steps = (tokens + R - 1) / R;
     __syncthreads();
     if (threadIdx.x >= THREADS) {
-        if (threadIdx.x == THREADS)
+        if (threadIdx.x == THREADS) {
+            int issued = 0;
             for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
                 long long row[R];
                 int n = 0;
@@ -515,16 +554,20 @@ __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_ring_k
                     row[i] = row_at(step * R + i);
                     n += row[i] >= 0;
                 }
-                r.wait_empty();
+                if (!r.wait_empty()) break;
                 const uint32_t bar = Ring::at(bars.full + r.stage), to = r.base + r.stage * r.stage_bytes;
                 ring_expect(bar, n * row_bytes);
 #pragma unroll
                 for (int i = 0; i < R; ++i)
                     if (row[i] >= 0) ring_copy(to + i * row_bytes, static_cast<const char *>(p.x) + row[i] * p.x_stride * (X32 ? 4 : 2), row_bytes, bar);
                 r.next();
+                issued = min(issued + 1, stages);
             }
+            r.drain(issued);
+        }
         return;
     }
+    r.short_limit();
     uint64_t w[4 * P], b[4 * P];
 #pragma unroll
     for (int q = 0; q < P; ++q) {
@@ -599,7 +642,7 @@ __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_backwa
     const Place<true, P> l = {(int)threadIdx.x, THREADS, p.dim};
     const int x_bytes = p.dim * (X32 ? 4 : 2), y_bytes = p.dim * (Y32 ? 4 : 2), row_bytes = x_bytes + y_bytes;
     const long long steps = (p.tokens + R - 1) / R;
-    Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages};
+    Ring r = {&bars, (uint32_t)__cvta_generic_to_shared(ring), (uint32_t)(R * row_bytes), stages, p.wait_limit};
     if (threadIdx.x == 0) r.set_up(THREADS / 32);
     in_turn();
     for (int i = threadIdx.x; i < p.dim / 4; i += THREADS + 32)
@@ -615,10 +658,11 @@ __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_backwa
     };
     __syncthreads();
     if (threadIdx.x >= THREADS) {
-        if (threadIdx.x == THREADS)
+        if (threadIdx.x == THREADS) {
+            int issued = 0;
             for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
                 const int rows = (int)min((long long)R, p.tokens - step * R);
-                r.wait_empty();
+                if (!r.wait_empty()) break;
                 const uint32_t bar = Ring::at(bars.full + r.stage), to = r.base + r.stage * r.stage_bytes;
                 ring_expect(bar, rows * row_bytes);
                 for (int i = 0; i < rows; ++i) {
@@ -627,9 +671,13 @@ __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_backwa
                     ring_copy(to + i * row_bytes + x_bytes, static_cast<const char *>(p.dy) + row * p.dy_stride * (Y32 ? 4 : 2), y_bytes, bar);
                 }
                 r.next();
+                issued = min(issued + 1, stages);
             }
+            r.drain(issued);
+        }
         return;
     }
+    r.short_limit();
     int slot = 0, slot3 = 0;
     uint64_t dw[4 * P] = {}, db[4 * P] = {};
     for (long long step = blockIdx.x; step < steps; step += gridDim.x) {
@@ -910,7 +958,7 @@ fi_status_t check_args(const fi_layer_norm_t *a, bool backward, const char *name
     const long long x_rows = a->rows ? a->x_rows : a->tokens;
     const auto off = [](const void *p, uintptr_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; };
     if (off(a->x, x_size) || off(a->out, backward ? x_size : y_size) || (backward && off(a->dy, y_size)) || off(a->weight, 4) || off(a->bias, 4) ||
-        off(a->workspace, 16) || (x_rows > 1 && a->x_stride < a->dim) || (a->tokens > 1 && (a->out_stride < a->dim || (backward && a->dy_stride < a->dim)))) {
+        off(a->workspace, 16) || a->wait_limit < 0 || (x_rows > 1 && a->x_stride < a->dim) || (a->tokens > 1 && (a->out_stride < a->dim || (backward && a->dy_stride < a->dim)))) {
         set_error("%s: rows must not overlap; pointers must be aligned to their types", name);
         return FI_ERR_INVALID_ARG;
     }
@@ -932,6 +980,7 @@ RowNormParams row_norm_params(const fi_layer_norm_t *a, bool backward, bool *vec
     p.out_stride = a->out_stride;
     p.tokens = a->tokens;
     p.x_rows = a->rows ? a->x_rows : a->tokens;
+    p.wait_limit = a->wait_limit > 0 && a->wait_limit < kWaitLimit ? a->wait_limit : kWaitLimit;
     p.dim = a->dim;
     p.rms = a->rms != 0;
     p.eps = a->eps;
