@@ -221,6 +221,7 @@ def main():
         h, state = model.step(h)
         h = 0.7 * (h + torch.randn_like(h))
     fb.linear_poll_status()
+    fb.layer_norm_poll_status()
     for i, layer in enumerate(model.layers):
         layer.kv.poll_status()
         print(f"block {i}: keys per request {layer.out.lens.tolist()}, pages with several owners {int((layer.shared > 0).sum())}")

@@ -758,7 +758,8 @@ typedef struct {
 fi_status_t fi_layer_norm(const fi_layer_norm_t *args, void *cuda_stream);
 fi_status_t fi_layer_norm_backward(const fi_layer_norm_t *args, void *cuda_stream);
 int64_t fi_layer_norm_workspace(int32_t dim);
-/* Synchronises the current device; FI_ERR_TIMEOUT when a bounded wait inside fi_layer_norm_backward ran out there since the last poll. */
+/* Synchronises the current device; FI_ERR_TIMEOUT when a bounded wait inside a kernel of fi_layer_norm or fi_layer_norm_backward ran out
+ * there since the last poll (the word is cleared). */
 fi_status_t fi_layer_norm_poll_status(void);
 
 /* Number of kernels this library has launched in the calling process (all caches). */

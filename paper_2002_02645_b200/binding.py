@@ -1114,7 +1114,7 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
 
 
 def linear_poll_status(device: int = 0) -> None:
-    """fi_linear_poll_status of a device: raises FI_ERR_TIMEOUT when a wait inside a product's kernel ran out there."""
+    """fi_linear_poll_status of a device: raises FI_ERR_TIMEOUT when a wait inside a kernel of linear or linear_backward ran out there."""
     with torch.cuda.device(device):
         _check(load_library().fi_linear_poll_status())
 
@@ -1235,7 +1235,8 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
 
 
 def layer_norm_poll_status(device: int = 0) -> None:
-    """fi_layer_norm_poll_status of a device: raises FI_ERR_TIMEOUT when a wait inside layer_norm_backward's kernel ran out there."""
+    """fi_layer_norm_poll_status of a device: raises FI_ERR_TIMEOUT when a wait inside a kernel of layer_norm or layer_norm_backward ran out
+    there."""
     with torch.cuda.device(device):
         _check(load_library().fi_layer_norm_poll_status())
 

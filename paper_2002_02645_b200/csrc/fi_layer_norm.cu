@@ -1046,7 +1046,7 @@ fi_status_t fi_layer_norm_poll_status(void) {
     }
     if (e != cudaSuccess) return cuda_fail(e, "fi_layer_norm_poll_status");
     if (word) {
-        set_error("fi_layer_norm_backward: a wait inside a kernel ran out; its results are not valid");
+        set_error("fi_layer_norm, fi_layer_norm_backward: a wait inside a kernel ran out; its results are not valid");
         return FI_ERR_TIMEOUT;
     }
     return FI_OK;

@@ -1814,7 +1814,7 @@ fi_status_t fi_linear_poll_status(void) {
     }
     if (e != cudaSuccess) return cuda_fail(e, "fi_linear_poll_status");
     if (word) {
-        set_error("fi_linear: a wait inside a kernel ran out; its results are not valid");
+        set_error("fi_linear, fi_linear_backward: a wait inside a kernel ran out; its results are not valid");
         return FI_ERR_TIMEOUT;
     }
     return FI_OK;

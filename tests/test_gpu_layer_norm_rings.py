@@ -95,3 +95,12 @@ def test_in_place_while_later_rows_are_on_their_way(tokens, dim, dtype):
         got = fb.layer_norm_backward(x, w, into, rms=rms, with_bias=True, dx=into)
         assert got[0] is into and all(torch.equal(s, t) for s, t in zip(ref, got))
     fb.layer_norm_poll_status()
+
+
+def test_the_report_names_both_directions():
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x = rand(gen, 1500, 2048)
+    for call in (lambda: fb.layer_norm(x, wait_limit=1000), lambda: fb.layer_norm_backward(x, None, x, wait_limit=1000)):
+        call()
+        with pytest.raises(fb.FiError, match=r"fi_layer_norm, fi_layer_norm_backward: a wait"):
+            fb.layer_norm_poll_status()
