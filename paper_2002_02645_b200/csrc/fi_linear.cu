@@ -125,11 +125,12 @@ template <typename Ctl>
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Ctl *ctl, long long limit) {
     return __all_sync(0xffffffffu, bar_try(bar, parity)) || __all_sync(0xffffffffu, bar_wait_long(bar, parity, ctl, limit));
 }
-// for the end of a role that gave up: what it has started is over before the CTA leaves
-__device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity) {
+// for the end of a role, whichever one has given up: what it has started is over before the CTA leaves
+template <typename Ctl>
+__device__ __forceinline__ void bar_drain(uint64_t *bar, uint32_t parity, Ctl *ctl) {
     const long long t0 = clock64();
     while (!bar_try(bar, parity))
-        if (clock64() - t0 > kDrainLimit) {
+        if (clock64() - t0 > (ctl->gave_up ? kDrainLimit : kWaitLimit)) {
             atomicOr(&g_linear_status, 1);
             return;
         }
@@ -548,14 +549,12 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
                 if (!warp_wait(&ctl->empty[stage], phase ^ 1, ctl, p.wait_limit)) break;
                 load(kb);
             }
-        if (kb < kb1 || cols <= 0 || __any_sync(0xffffffffu, ctl->gave_up)) {    // stopped: the copies that were started land first
-            for (int back = min(kb - kb0, p.stages); back > 0; --back) {
-                if (stage == 0) {
-                    stage = p.stages;
-                    phase ^= 1;
-                }
-                bar_drain(&ctl->full[--stage], phase);
+        for (int back = min(kb - kb0, p.stages); back > 0; --back) {             // (at once where the products have been through)
+            if (stage == 0) {
+                stage = p.stages;
+                phase ^= 1;
             }
+            bar_drain(&ctl->full[--stage], phase, ctl);
         }
     } else if (warp == 9) {
         if (cols > 0) {
@@ -594,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_split_kernel(const __grid_
             }
             if (elect_one()) tc_commit(&ctl->done);
             __syncwarp();
-            bar_drain(&ctl->done, 0);
+            bar_drain(&ctl->done, 0, ctl);
         }
     } else if (cols > 0) {
         if (LONG)
@@ -933,20 +932,20 @@ __device__ __forceinline__ void linear_pair(const CUtensorMap *maps_a, const CUt
                 next_stage();
             }
         }
-        if (!ok) {
-            // gave up: the copies that were started land first (the second CTA cannot see that, and gives them 10 ms)
-            if (rank == 0) {
-                for (; issued > 0; --issued) {
-                    if (stage == 0) {
-                        stage = p.stages;
-                        phase ^= 1;
-                    }
-                    bar_drain(&ctl->full[--stage], phase);
+        // The copies of both CTAs that were started land first, which the first CTA's barriers count.  After a wait that ran out one CTA may have
+        // started copies that the other has no part in: 10 ms for those.
+        if (rank == 0) {
+            for (; issued > 0; --issued) {
+                if (stage == 0) {
+                    stage = p.stages;
+                    phase ^= 1;
                 }
-            } else {
-                const long long t0 = clock64();
-                while (clock64() - t0 < kDrainLimit / 10) {}
+                bar_drain(&ctl->full[--stage], phase, ctl);
             }
+        }
+        if (!ok || ctl->gave_up) {
+            const long long t0 = clock64();
+            while (clock64() - t0 < kDrainLimit / 10) {}
         }
     } else if (warp == 9) {
         if (rank == 0) {
