@@ -714,6 +714,7 @@ typedef struct {
     void *workspace;
     int64_t x_stride, weight_stride, dy_stride, preact_stride, dx_stride, dweight_stride;
     int64_t tokens;
+    int64_t wait_limit;         /* as in fi_linear_t */
     int32_t in_dim, out_dim;
     int32_t activation;
     int32_t dy_f32;             /* dy is float32, not bfloat16 */

@@ -104,7 +104,7 @@ class fi_linear_t(ctypes.Structure):
 
 class fi_linear_backward_t(ctypes.Structure):
     _fields_ = _fields(ctypes.c_void_p, "x weight dy preact dx dweight dbias workspace") \
-        + _fields(ctypes.c_int64, "x_stride weight_stride dy_stride preact_stride dx_stride dweight_stride tokens") \
+        + _fields(ctypes.c_int64, "x_stride weight_stride dy_stride preact_stride dx_stride dweight_stride tokens wait_limit") \
         + _fields(ctypes.c_int32, "in_dim out_dim activation dy_f32")
 
 
@@ -1070,7 +1070,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
 
 def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], dy: torch.Tensor, *, preact: Optional[torch.Tensor] = None,
                     activation: str = "none", with_bias: bool = False, dx: Optional[torch.Tensor] = None,
-                    dweight: Optional[torch.Tensor] = None, dy_dtype: torch.dtype = torch.bfloat16):
+                    dweight: Optional[torch.Tensor] = None, dy_dtype: torch.dtype = torch.bfloat16, wait_limit: int = 0):
     """fi_linear_backward: (dx, dweight, dbias) for dy, the gradient of the result, of type dy_dtype (bfloat16 or float32).  Without weight
     there is no dx, without x no dweight, and dbias only with with_bias."""
     lib, kind, index = load_library(), _activation(activation), dy.get_device()
@@ -1108,7 +1108,7 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
     if kind or wide:
         work = dy.new_empty(lib.fi_linear_backward_workspace(tokens, out_dim, kind or 1), dtype=torch.uint8)
     args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
-                                 *strides, tokens, in_dim, out_dim, kind, 1 if wide else 0)
+                                 *strides, tokens, wait_limit, in_dim, out_dim, kind, 1 if wide else 0)
     _on_device(index, lib.fi_linear_backward, args)
     return dx, dweight, dbias
 

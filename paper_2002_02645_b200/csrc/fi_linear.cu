@@ -1619,6 +1619,8 @@ fi_status_t launch_two(const Product &x, const Product &y, bool rows_mn, const D
 
 constexpr long long kMostRows = 1 << 30;                    // (rows are indexed with int32, tiles may overshoot)
 
+long long wait_limit_of(long long given) { return given > 0 && given < kWaitLimit ? given : kWaitLimit; }
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 fi_status_t check_sizes(long long tokens, int in_dim, int out_dim, int act, const char *name) {
@@ -1712,7 +1714,7 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
     p.ld_out = a->out_stride;
     p.ld_preact = a->preact_stride;
     p.out_rows = out_rows;
-    p.wait_limit = a->wait_limit > 0 && a->wait_limit < kWaitLimit ? a->wait_limit : kWaitLimit;
+    p.wait_limit = wait_limit_of(a->wait_limit);
     const auto wide = [&](const void *at, int64_t ld, long long rows_of, int bytes) { return aligned16(at) && (rows_of <= 1 || ld * bytes % 16 == 0); };
     p.wide = wide(a->out, a->out_stride, out_rows, size) && wide(a->residual, a->residual_stride, out_rows, size) &&
              wide(a->preact, a->preact_stride, a->tokens, 2) && aligned16(a->bias);
@@ -1749,7 +1751,8 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         return FI_ERR_INVALID_ARG;
     }
     if ((a->dx && a->tokens > 1 && a->dx_stride < a->in_dim) || (a->dweight && a->dweight_stride < a->in_dim) ||
-        (reinterpret_cast<uintptr_t>(a->dx) & 1) || (reinterpret_cast<uintptr_t>(a->dweight) & 1) || (reinterpret_cast<uintptr_t>(a->dbias) & 3)) {
+        (reinterpret_cast<uintptr_t>(a->dx) & 1) || (reinterpret_cast<uintptr_t>(a->dweight) & 1) || (reinterpret_cast<uintptr_t>(a->dbias) & 3) ||
+        a->wait_limit < 0) {
         set_error("%s: rows of dx and dweight must not overlap; pointers must be aligned to their types", name);
         return FI_ERR_INVALID_ARG;
     }
@@ -1774,7 +1777,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     const Matrix g = apart ? Matrix{dz, a->tokens, a->out_dim, a->out_dim} : Matrix{a->dy, a->tokens, a->out_dim, a->dy_stride};
     const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
     LinearParams dx = {}, dw = {};
-    dx.wait_limit = dw.wait_limit = kWaitLimit;
+    dx.wait_limit = dw.wait_limit = wait_limit_of(a->wait_limit);
     dx.out = a->dx;
     dx.wide = aligned16(a->dx) && (a->tokens <= 1 || a->dx_stride % 8 == 0);
     dx.ld_out = a->dx_stride;
