@@ -80,21 +80,32 @@ __device__ __forceinline__ void store8(void *base, long long at, const float *x)
         *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(base) + at) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
+// The value, or 0; asked for in program order, so that those of a row are on their way together (65,536 rows of 1,500 values: 182 us, in the
+// order that the compiler finds 247)
 template <bool F32>
-__device__ __forceinline__ float load1(const void *base, long long at) {
-    if constexpr (F32) return static_cast<const float *>(base)[at];
-    return __bfloat162float(static_cast<const __nv_bfloat16 *>(base)[at]);
+__device__ __forceinline__ float load1_if(const void *base, long long at, bool there) {
+    const char *const from = static_cast<const char *>(base) + at * (F32 ? 4 : 2);
+    if constexpr (F32) {
+        float v;
+        asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\nmov.b32 %0, 0;\n@q ld.global.f32 %0, [%1];\n}" : "=f"(v) : "l"(from), "r"((int)there));
+        return v;
+    } else {
+        unsigned short v;
+        asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\nmov.b16 %0, 0;\n@q ld.global.u16 %0, [%1];\n}" : "=h"(v) : "l"(from), "r"((int)there));
+        return __uint_as_float((uint32_t)v << 16);
+    }
 }
 template <bool F32>
 __device__ __forceinline__ void store1(void *base, long long at, float v) {
     if constexpr (F32) static_cast<float *>(base)[at] = v;
     else static_cast<__nv_bfloat16 *>(base)[at] = __float2bfloat16_rn(v);
 }
-// 8 floats of a weight, which stay in L1: loaded where they are used, so that they do not hold registers in between
+// 8 floats of a weight, which stay in L1: loaded where they are used, so that they do not hold registers in between.  (Plain loads: the kernel
+// before this one, which may still run when this one starts, may be what writes them.)
 __device__ __forceinline__ void load8_again(const float *p, float *x) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-        asm volatile("ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];"
+        asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];"
                      : "=f"(x[4 * i]), "=f"(x[4 * i + 1]), "=f"(x[4 * i + 2]), "=f"(x[4 * i + 3])
                      : "l"(p + 4 * i));
 }
@@ -125,7 +136,7 @@ __device__ __forceinline__ void load_row(const Place<VEC, P> &l, const void *bas
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 8 * P; ++i) v[i] = l.has(i) ? load1<F32>(base, at + l.value(i)) : 0.f;
+        for (int i = 0; i < 8 * P; ++i) v[i] = load1_if<F32>(base, at + l.value(i), l.has(i));
     }
 }
 template <bool F32, bool VEC, int P>
@@ -140,8 +151,10 @@ __device__ __forceinline__ void store_row(const Place<VEC, P> &l, void *base, lo
             if (l.has(i)) store1<F32>(base, at + l.value(i), v[i]);
     }
 }
-// f(index into the registers, weight of that value)
-template <bool VEC, int P, typename F>
+// f(index into the registers, weight of that value).  TOGETHER: without 16-byte boundaries all weights are asked for before the first is used.  So
+// for gradients (100,000 rows of 300 values in float32: 83 us, one at a time 98) and for 32 values a thread (5,000 rows of 15,001: 210 and 298), else
+// not (100,000 rows of 300: 54 and 49).
+template <bool TOGETHER = false, bool VEC, int P, typename F>
 __device__ __forceinline__ void with_weight(const Place<VEC, P> &l, const float *w, F &&f) {
     if constexpr (VEC) {
 #pragma unroll
@@ -152,10 +165,16 @@ __device__ __forceinline__ void with_weight(const Place<VEC, P> &l, const float 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f(8 * p + i, x[i]);
             }
+    } else if constexpr (TOGETHER) {
+        float x[8 * P];
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i) x[i] = load1_if<true>(w, l.value(i), l.has(i));
+#pragma unroll
+        for (int i = 0; i < 8 * P; ++i) f(i, x[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8 * P; ++i)
-            if (l.has(i)) f(i, __ldg(w + l.value(i)));
+            if (l.has(i)) f(i, w[l.value(i)]);
     }
 }
 
@@ -233,11 +252,12 @@ __global__ void __launch_bounds__(LANES ? 128 : 512) layer_norm_kernel(const Row
     if (there) load_row<X32>(l, p.x, row * p.x_stride, v);
     const float r = deviations<LANES>(p, l, v, s, slot);
     if (!there) return;
-    if (p.weight) with_weight(l, p.weight, [&](int i, float w) { v[i] = v[i] * r * w; });
+    constexpr bool kTogether = LANES == 0 && P == 4;
+    if (p.weight) with_weight<kTogether>(l, p.weight, [&](int i, float w) { v[i] = v[i] * r * w; });
     else
 #pragma unroll
         for (int i = 0; i < 8 * P; ++i) v[i] *= r;
-    if (p.bias) with_weight(l, p.bias, [&](int i, float b) { v[i] += b; });
+    if (p.bias) with_weight<kTogether>(l, p.bias, [&](int i, float b) { v[i] += b; });
     store_row<Y32>(l, p.out, token * p.out_stride, v);
 }
 
@@ -253,6 +273,12 @@ __global__ void __launch_bounds__(LANES ? 256 : 512) layer_norm_backward_kernel(
     const int groups_here = LANES ? 256 / (LANES ? LANES : 1) : 1, mine = LANES ? threadIdx.x / (LANES ? LANES : 1) : 0;
     const int warp_first = LANES ? (threadIdx.x >> 5) * (32 / (LANES ? LANES : 32)) : 0;
     float dw[V] = {}, db[V] = {};
+    // Rows off 16-byte boundaries: a warp's long ones keep their weights, 32 a lane (65,536 rows of 1,023 values: 165 us, loaded again for each row 183)
+    constexpr bool kKept = !VEC && LANES && P == 4;
+    float kept[kKept ? V : 1];
+    if constexpr (kKept)
+#pragma unroll
+        for (int i = 0; i < V; ++i) kept[i] = p.weight ? load1_if<true>(p.weight, l.value(i), l.has(i)) : 1.f;
     for (long long row0 = (long long)blockIdx.x * groups_here; row0 + warp_first < p.tokens; row0 += (long long)gridDim.x * groups_here) {
         const long long row = row0 + mine;
         const bool there = LANES == 0 || LANES == 32 || row < p.tokens;
@@ -269,7 +295,12 @@ __global__ void __launch_bounds__(LANES ? 256 : 512) layer_norm_backward_kernel(
             dw[i] = fmaf(g[i], v[i], dw[i]);
             db[i] += g[i];
         }
-        if (p.weight) with_weight(l, p.weight, [&](int i, float w) { g[i] *= w; });
+        if constexpr (kKept) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] *= kept[i];
+        } else if (p.weight) {
+            with_weight<true>(l, p.weight, [&](int i, float w) { g[i] *= w; });
+        }
         float both[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < V; ++i) {
