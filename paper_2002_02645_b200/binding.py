@@ -12,6 +12,7 @@ import struct
 from typing import List, Optional, Sequence
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 
 from . import build as _build
 
@@ -859,6 +860,13 @@ class ForkOut:
         self.copies = copies.view(batch, 3)
 
 
+def _no_tangents(*tensors: Optional[torch.Tensor]) -> None:
+    """Refuses dual tensors of forward-mode differentiation, whose tangents the kernels would drop."""
+    for t in tensors:
+        if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError("forward-mode differentiation is not supported: a tensor has a tangent")
+
+
 def _norm_rope_call(fn, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count, q_res, k_res, dq_out=None,
                     dk_out=None, dq_weight=None, dk_weight=None, workspace=None):
     """Checks and packs the arguments of both directions; makes the results (q_res, k_res) that are not given."""
@@ -917,7 +925,10 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optiona
                    eps: float = 1e-6, interleaved: bool = False, count: Optional[torch.Tensor] = None,
                    q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """fi_head_norm_rope: (q, k) normed head by head and turned to their positions.  q_out / k_out may be q / k.  Gradients flow to
-    q, k and the weights; results that are given have none, so they are refused where one is asked for."""
+    q, k and the weights; results that are given have none, so they are refused where one is asked for.  Tensors with a forward-mode tangent
+    are refused."""
+    if _forward_ad._current_level >= 0:                     # (a dual level is entered)
+        _no_tangents(q, k, q_weight, k_weight, rope)
     if (q.requires_grad or k is not None and k.requires_grad or q_weight is not None and q_weight.requires_grad
             or k_weight is not None and k_weight.requires_grad) and torch.is_grad_enabled():
         if q_out is not None or k_out is not None:
@@ -1057,7 +1068,10 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     belongs to row rows[i] of residual and out (out may be residual); with `count` only that many tokens are real.  preact takes the sums
     before the activation.  Gradients flow to x, weight, bias and residual; not through rows, count, out or preact, which are refused
     where one is asked for.  grad_dtype is the type in which the gradient of a float32 result is taken: bfloat16 rounds each of its values
-    (2^-8) before the gradients of x, weight and bias are formed; float32 takes them as they are, and only what the products read is rounded."""
+    (2^-8) before the gradients of x, weight and bias are formed; float32 takes them as they are, and only what the products read is rounded.  Tensors
+    with a forward-mode tangent are refused."""
+    if _forward_ad._current_level >= 0:                     # (a dual level is entered)
+        _no_tangents(x, weight, bias, residual)
     if grad_dtype is not torch.bfloat16 and grad_dtype is not torch.float32:
         raise ValueError("grad_dtype must be bfloat16 or float32")
     if (x.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad
@@ -1193,7 +1207,9 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                out: Optional[torch.Tensor] = None, wait_limit: int = 0) -> torch.Tensor:
     """fi_layer_norm: the rows of x [rows, dim] normed by mean and variance, or by root mean square.  With `rows`, token i of the result is
     row rows[i] of x; with `count` only that many tokens are real (the others are left as they are).  Gradients flow to x, weight and
-    bias; not through rows, count or out, which are refused where one is asked for."""
+    bias; not through rows, count or out, which are refused where one is asked for.  Tensors with a forward-mode tangent are refused."""
+    if _forward_ad._current_level >= 0:                     # (a dual level is entered)
+        _no_tangents(x, weight, bias)
     if (x.requires_grad or weight is not None and weight.requires_grad or bias is not None and bias.requires_grad) and torch.is_grad_enabled():
         if out is not None or rows is not None or count is not None:
             raise ValueError("out, rows or count is given, but a gradient is asked for")
