@@ -665,7 +665,8 @@ fi_status_t fi_kv_copy_pages(fi_kv_t *kv, const int32_t *copies, int32_t max_cop
  *   rows [tokens] device int32, nullable: row of residual and out of each token (miss_idx of a cascade step), no row twice; a row
  *   outside [0, out_rows) is not stored; null: token i is row i.  Rows that are not listed are left untouched.
  *   tokens_dev [1] device int32, nullable: actual number of tokens (<= tokens); later ones are left out.
- *   preact [tokens x out_dim] bfloat16, nullable: x W^T + bias before the activation, which the gradients need.
+ *   preact [tokens x out_dim] bfloat16, nullable: x W^T + bias before the activation, which the gradients need; written for every actual token,
+ *   whatever its row.
  * Products on the tensor cores, sums in fp32; one rounding at the end.  The tensor cores cut what they add (some 2^-24 of the sum for 16
  * values, always towards zero), so a float32 out is summed up in pieces of about 512 values outside of them, a bfloat16 out (and dx and
  * dweight below) in pieces of 16,384 (off by 2^-15 of the sum, before it is rounded to 2^-8), however long the sums are.

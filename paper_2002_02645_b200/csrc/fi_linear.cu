@@ -1682,8 +1682,9 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
         set_error("%s: out_dtype must be FI_F32 or FI_BF16", name);
         return FI_ERR_INVALID_ARG;
     }
-    if (a->tokens == 0 || (a->rows && a->out_rows == 0)) return FI_OK;
-    if (!a->x || !a->weight || !a->out) {
+    const bool nowhere = a->rows && a->out_rows == 0;       // (preact is written all the same)
+    if (a->tokens == 0 || (nowhere && !a->preact)) return FI_OK;
+    if (!a->x || !a->weight || (!a->out && !nowhere)) {
         set_error("%s: null pointer", name);
         return FI_ERR_INVALID_ARG;
     }

@@ -39,3 +39,21 @@ def test_norm_by_weights_that_the_kernel_before_wrote(rows, dim):
         assert s.any()
         torch.cuda.synchronize()
         assert torch.equal(kept[0], fb.layer_norm(x, s, b)) and all(torch.equal(p, q) for p, q in zip(kept[1:], fb.layer_norm_backward(x, s, dy)))
+
+
+@pytest.mark.parametrize("tokens", [3, 700])
+def test_preact_of_a_stream_without_rows(tokens):
+    """preact is written for every real token, whatever its row: with out of no rows as with rows outside of it."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x, w, bias = rand(gen, tokens, 64).bfloat16(), rand(gen, 128, 64).bfloat16(), rand(gen, 128)
+    want = torch.empty(tokens, 128, dtype=torch.bfloat16, device=DEV)
+    fb.linear(x, w, bias, activation="silu", preact=want)
+    rows = torch.zeros(tokens, dtype=torch.int32, device=DEV)
+    count = torch.tensor([tokens - 1], dtype=torch.int32, device=DEV)
+    for out in (torch.empty(0, 128, device=DEV), torch.full((1, 128), 5.0, device=DEV)):
+        got = torch.full_like(want, 7.0)
+        where = rows if out.size(0) == 0 else rows + 1
+        fb.linear(x, w, bias, activation="silu", rows=where, out=out, residual=out, preact=got, count=count)
+        assert torch.equal(got[:-1], want[:-1]) and (got[-1] == 7).all() and (out == 5).all()
+        fb.linear(x, w, bias, rows=where, out=out)
+    fb.linear_poll_status()
