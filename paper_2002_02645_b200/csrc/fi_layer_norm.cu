@@ -832,11 +832,14 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size
 
 // once for a device and kernel
 template <typename Kernel>
-void ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
+cudaError_t ring_ready(Kernel kernel, std::atomic<unsigned long long> &done) {
     int device = 0;
-    if (cudaGetDevice(&device) == cudaSuccess && (done.load(std::memory_order_acquire) >> (device & 63) & 1)) return;
-    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
-    done.fetch_or(1ull << (device & 63), std::memory_order_release);
+    cudaError_t e = cudaGetDevice(&device);
+    const unsigned long long bit = device >= 0 && device < 64 ? 1ull << device : 0;
+    if (e != cudaSuccess || (done.load(std::memory_order_acquire) & bit)) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
 }
 int ring_stages(int room, int stage) { return room / stage < kMaxRing ? room / stage : kMaxRing; }
 
@@ -878,7 +881,8 @@ cudaError_t launch_forward(const RowNormParams &p, int sms, cudaStream_t stream)
             const int per_sm = 512 / threads, stage = rows * p.dim * (X32 ? 4 : 2);
             const bool full = p.dim == threads * 8 * (which == 3 ? 4 : 2);
             const auto kernel = ring_forward<X32, Y32>(p.rms, full, which);
-            ring_ready(kernel, done[which][p.rms + 2 * full]);
+            const cudaError_t e = ring_ready(kernel, done[which][p.rms + 2 * full]);
+            if (e != cudaSuccess) return e;
             const int stages = ring_stages((220 / per_sm - 1) * 1024, stage);
             return launch_early(kernel, dim3((unsigned)(sms * per_sm)), threads + 32, (size_t)stages * stage, stream, p, stages);
         }
@@ -934,8 +938,9 @@ cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStr
         const long long most = sms * per_sm < max_partials(p.dim) ? sms * per_sm : max_partials(p.dim);
         const long long want = (p.tokens + rows - 1) / rows;
         const unsigned grid = (unsigned)(want < 1 ? 1 : want < most ? want : most);
-        ring_ready(kernel, done[which + 1][p.rms]);
         *parts = (int)grid;
+        const cudaError_t e = ring_ready(kernel, done[which + 1][p.rms]);
+        if (e != cudaSuccess) return e;
         return launch_early(kernel, dim3(grid), threads + 32, (size_t)stages * stage + p.dim * 4, stream, p, stages);
     }
     if constexpr (!VEC) {

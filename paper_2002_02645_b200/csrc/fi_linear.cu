@@ -1358,13 +1358,12 @@ TwoKernel two_kernel(bool rows_mn, int depth) {
 }
 
 struct DeviceFacts {
-    std::atomic<int> sms{0};
     int clusters[4];                                        // of 1, 2, 4, 8 CTAs that run at one time
 };
-DeviceFacts g_facts[kMaxDevices];
+std::atomic<unsigned long long> g_facts[kMaxDevices];       // 16 bits each, published in one piece; 0: not known yet
 
 // Facts of the current device; its kernels are set up at the first call
-fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
+fi_status_t device_facts(DeviceFacts &f, const char *name) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return cuda_fail(e, name);
@@ -1372,9 +1371,10 @@ fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
         set_error("%s: device ordinal %d", name, dev);
         return FI_ERR_UNSUPPORTED;
     }
-    DeviceFacts &f = g_facts[dev];
-    *facts = &f;
-    if (f.sms.load(std::memory_order_acquire)) return FI_OK;
+    if (const unsigned long long known = g_facts[dev].load(std::memory_order_acquire)) {
+        for (int i = 0; i < 4; ++i) f.clusters[i] = (int)(known >> (16 * i) & 0xffff);
+        return FI_OK;
+    }
     int n = 0;
     e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     for (int form = 0; form < 12; ++form) {                 // of a product: type and activation, or one of two gradients
@@ -1402,7 +1402,9 @@ fi_status_t device_facts(const DeviceFacts **facts, const char *name) {
         if (e == cudaSuccess && f.clusters[i] < 1) e = cudaErrorInvalidConfiguration;
     }
     if (e != cudaSuccess) return cuda_fail(e, name);
-    f.sms.store(n, std::memory_order_release);
+    unsigned long long known = 0;
+    for (int i = 0; i < 4; ++i) known |= (unsigned long long)f.clusters[i] << (16 * i);
+    g_facts[dev].store(known, std::memory_order_release);   // (threads that come here together find the same)
     return FI_OK;
 }
 
@@ -1701,8 +1703,8 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
         set_error("%s: rows of out, residual and preact must not overlap; pointers must be aligned to their types", name);
         return FI_ERR_INVALID_ARG;
     }
-    const DeviceFacts *facts = nullptr;
-    st = device_facts(&facts, name);
+    DeviceFacts facts;
+    st = device_facts(facts, name);
     if (st != FI_OK) return st;
     LinearParams p = {};
     p.bias = a->bias;
@@ -1720,7 +1722,7 @@ fi_status_t fi_linear(const fi_linear_t *a, void *cuda_stream) {
     p.wide = wide(a->out, a->out_stride, out_rows, size) && wide(a->residual, a->residual_stride, out_rows, size) &&
              wide(a->preact, a->preact_stride, a->tokens, 2) && aligned16(a->bias);
     const Matrix w = {a->weight, a->out_dim, a->in_dim, a->weight_stride}, x = {a->x, a->tokens, a->in_dim, a->x_stride};
-    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, a->activation, p, *facts,
+    return launch_product(w, false, x, false, a->out_dim, a->tokens, a->in_dim, a->out_dtype == FI_F32, a->activation, p, facts,
                           static_cast<cudaStream_t>(cuda_stream), name);
 }
 
@@ -1757,8 +1759,8 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         set_error("%s: rows of dx and dweight must not overlap; pointers must be aligned to their types", name);
         return FI_ERR_INVALID_ARG;
     }
-    const DeviceFacts *facts = nullptr;
-    st = device_facts(&facts, name);
+    DeviceFacts facts;
+    st = device_facts(facts, name);
     if (st != FI_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (a->tokens == 0) {                                   // sums over nothing
@@ -1769,7 +1771,7 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
     }
     __nv_bfloat16 *const dz = apart && (a->dx || a->dweight) ? static_cast<__nv_bfloat16 *>(a->workspace) : nullptr;
     if (dz || a->dbias) {
-        const int width = a->out_dim <= 64 * 16 && a->tokens >= 1024 ? 16 : 64, parts = slope_parts(a->tokens, a->out_dim, width, facts->clusters[0]);
+        const int width = a->out_dim <= 64 * 16 && a->tokens >= 1024 ? 16 : 64, parts = slope_parts(a->tokens, a->out_dim, width, facts.clusters[0]);
         st = launch_early(name, width == 16 ? slope_kernel<16>(a->activation, dy32) : slope_kernel<64>(a->activation, dy32),
                           dim3((a->out_dim + width - 1) / width, parts), kSlopeThreads, 0, dim3(1, parts), stream, a->dy, (long long)a->dy_stride, static_cast<const __nv_bfloat16 *>(a->preact), (long long)a->preact_stride, dz, a->dbias,
                           (long long)a->tokens, (int)a->out_dim);
@@ -1792,18 +1794,18 @@ fi_status_t fi_linear_backward(const fi_linear_backward_t *a, void *cuda_stream)
         px.p = dx;
         pw.p = dw;
         LinearPlan plan_x, plan_w;
-        plan_two(a->in_dim, a->tokens, up(a->out_dim, kKb), a->out_dim, up(a->tokens, kKb), facts->clusters, plan_x, plan_w);
+        plan_two(a->in_dim, a->tokens, up(a->out_dim, kKb), a->out_dim, up(a->tokens, kKb), facts.clusters, plan_x, plan_w);
         st = plan_launch(px, plan_x, w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, name);
         if (st == FI_OK) st = plan_launch(pw, plan_w, x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, name);
         if (st != FI_OK) return st;
         if (plan_x.pair && plan_w.pair && plan_x.split == 1 && plan_w.split == 1 && plan_x.tile_n == plan_w.tile_n && px.depth == pw.depth)
-            return px.p.kb >= pw.p.kb ? launch_two(px, pw, false, *facts, stream, name) : launch_two(pw, px, true, *facts, stream, name);
-        st = launch_planned(px, true, false, false, FI_ACT_NONE, *facts, stream, name);
-        return st == FI_OK ? launch_planned(pw, true, true, false, FI_ACT_NONE, *facts, stream, name) : st;
+            return px.p.kb >= pw.p.kb ? launch_two(px, pw, false, facts, stream, name) : launch_two(pw, px, true, facts, stream, name);
+        st = launch_planned(px, true, false, false, FI_ACT_NONE, facts, stream, name);
+        return st == FI_OK ? launch_planned(pw, true, true, false, FI_ACT_NONE, facts, stream, name) : st;
     }
-    if (a->dx) st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, dx, *facts, stream, name);
+    if (a->dx) st = launch_product(w, true, g, false, a->in_dim, a->tokens, a->out_dim, false, FI_ACT_NONE, dx, facts, stream, name);
     if (st == FI_OK && a->dweight)
-        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, dw, *facts, stream, name);
+        st = launch_product(x, true, g, true, a->in_dim, a->out_dim, a->tokens, false, FI_ACT_NONE, dw, facts, stream, name);
     return st;
 }
 

@@ -1,4 +1,8 @@
 """Edges of the layer's products and norm that go with what surrounds them: autograd's bookkeeping, empty streams, kernels launched early."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -57,3 +61,33 @@ def test_preact_of_a_stream_without_rows(tokens):
         assert torch.equal(got[:-1], want[:-1]) and (got[-1] == 7).all() and (out == 5).all()
         fb.linear(x, w, bias, rows=where, out=out)
     fb.linear_poll_status()
+
+
+def test_first_calls_of_many_threads_at_once():
+    """In a process of its own: facts of the device and set-up of the kernels are found by whoever comes first."""
+    code = '''
+import threading, torch
+from paper_2002_02645_b200 import binding as fb
+fb.load_library()
+gen = torch.Generator(device="cuda").manual_seed(0)
+rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+jobs = [(rand(t, k).bfloat16(), rand(n, k).bfloat16(), rand(3000, d)) for t, k, n, d in ((1, 2048, 256, 2048), (300, 1024, 1024, 4104), (50, 4096, 512, 9000), (2000, 512, 768, 1500))]
+torch.cuda.synchronize()
+start, got = threading.Barrier(16), [None] * 16
+def work(i):
+    x, w, rows = jobs[i % 4]
+    start.wait()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got[i] = (fb.linear(x, w), *fb.linear_backward(x, w, x @ w.t())[:2], fb.layer_norm(rows), fb.layer_norm_backward(rows, None, rows)[0])
+        torch.cuda.current_stream().synchronize()
+threads = [threading.Thread(target=work, args=(i,)) for i in range(16)]
+[t.start() for t in threads]; [t.join() for t in threads]
+for i in range(16):
+    x, w, rows = jobs[i % 4]
+    want = (fb.linear(x, w), *fb.linear_backward(x, w, x @ w.t())[:2], fb.layer_norm(rows), fb.layer_norm_backward(rows, None, rows)[0])
+    assert all(torch.equal(s, t) for s, t in zip(got[i], want)), i
+print("right")
+'''
+    done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), stdout=subprocess.PIPE,
+                          stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert done.returncode == 0 and "right" in done.stdout, done.stdout
