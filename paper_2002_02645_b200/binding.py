@@ -860,6 +860,19 @@ class ForkOut:
         self.copies = copies.view(batch, 3)
 
 
+def _written(*tensors: Optional[torch.Tensor]) -> None:
+    """Tells autograd that a call has written to tensors that were there before it: gradients that still need what they held are refused then."""
+    for t in tensors:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
+def _no_gradient(name: str, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name}: results are written there, but a gradient is asked for")
+
+
 def _no_tangents(*tensors: Optional[torch.Tensor]) -> None:
     """Refuses dual tensors of forward-mode differentiation, whose tangents the kernels would drop."""
     for t in tensors:
@@ -934,8 +947,11 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optiona
         if q_out is not None or k_out is not None:
             raise ValueError("q_out and k_out are given, but a gradient is asked for")
         return _HeadNormRope.apply(q, k, q_weight, k_weight, rope, positions, eps, interleaved, count)
-    return _norm_rope_call(load_library().fi_head_norm_rope, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
-                           q_out, k_out)
+    _no_gradient("q_out, k_out", q_out, k_out)
+    res = _norm_rope_call(load_library().fi_head_norm_rope, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
+                          q_out, k_out)
+    _written(q_out, k_out)
+    return res
 
 
 def head_norm_rope_backward(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
@@ -1079,7 +1095,12 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
         if out is not None or rows is not None or count is not None or preact is not None:
             raise ValueError("out, rows, count or preact is given, but a gradient is asked for")
         return _Linear.apply(x, weight, bias, residual, activation, out_dtype, grad_dtype, wait_limit)
-    return _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
+    if out is None and preact is None:
+        return _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
+    _no_gradient("out, preact", out, preact)
+    y = _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
+    _written(out, preact)
+    return y
 
 
 def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], dy: torch.Tensor, *, preact: Optional[torch.Tensor] = None,
@@ -1096,6 +1117,9 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
         in_dim = 8                                         # nothing but dbias
     else:
         in_dim = (x if x is not None else weight).shape[-1]
+    given = [t for t in (dx, dweight) if t is not None]
+    if given:
+        _no_gradient("dx, dweight", *given)
     strides = [0, 0, _check_rows(dy, "dy", index, dy_dtype, tokens, out_dim), 0, 0, 0]
     if weight is not None:
         strides[1] = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
@@ -1124,6 +1148,8 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
     args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
                                  *strides, tokens, wait_limit, in_dim, out_dim, kind, 1 if wide else 0)
     _on_device(index, lib.fi_linear_backward, args)
+    if given:
+        _written(*given)
     return dx, dweight, dbias
 
 
@@ -1214,7 +1240,12 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         if out is not None or rows is not None or count is not None:
             raise ValueError("out, rows or count is given, but a gradient is asked for")
         return _LayerNorm.apply(x, weight, bias, eps, rms, out_dtype, wait_limit)
-    return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit)
+    if out is None:
+        return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit)
+    _no_gradient("out", out)
+    _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit)
+    _written(out)
+    return out
 
 
 _layer_norm_work = {}      # values of fi_layer_norm_workspace by dim
@@ -1228,9 +1259,11 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
     kinds = _norm_types(x, dy.dtype, weight, None, index)
     tokens, dim = x.shape
     x_stride, dy_stride = _check_rows(x, "x", index, x.dtype, tokens, dim), _check_rows(dy, "dy", index, dy.dtype, tokens, dim)
+    given = dx
     if dx is None:
         dx, dx_stride = x.new_empty((tokens, dim)), dim
     else:
+        _no_gradient("dx", dx)
         dx_stride = _check_rows(dx, "dx", index, x.dtype, tokens, dim)
     dw = db = work = None
     if weight is not None or with_bias:
@@ -1247,6 +1280,8 @@ def layer_norm_backward(x: torch.Tensor, weight: Optional[torch.Tensor], dy: tor
     args = _pack_layer_norm(x.data_ptr(), dy.data_ptr(), dx.data_ptr(), _at(weight), 0, 0, 0, _at(dw), _at(db), _at(work), x_stride, dy_stride, dx_stride,
                             tokens, 0, wait_limit, dim, 1 if rms else 0, *kinds, eps)
     _on_device(index, lib.fi_layer_norm_backward, args)
+    if given is not None:
+        _written(given)
     return dx, dw, db
 
 

@@ -91,3 +91,28 @@ print("right")
     done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), stdout=subprocess.PIPE,
                           stderr=subprocess.STDOUT, text=True, timeout=300)
     assert done.returncode == 0 and "right" in done.stdout, done.stdout
+
+
+def test_results_written_in_place_count_as_changes():
+    """What a gradient still needs cannot be overwritten unnoticed, and a tensor that asks for a gradient is no place for a result."""
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x, a = rand(gen, 64, 64).bfloat16(), rand(gen, 64, 32).bfloat16()
+    w, b = rand(gen, 64, 64).bfloat16(), rand(gen, 64, 32).bfloat16()
+    heads = lambda t: t.view(64, 1, 64)
+    writes = [lambda t: fb.linear(a, b, out=t), lambda t: fb.linear(a, b, preact=t), lambda t: fb.layer_norm(w, out=t),
+              lambda t: fb.linear_backward(None, w, x.clone(), dx=t), lambda t: fb.linear_backward(w, None, w, dweight=t),
+              lambda t: fb.layer_norm_backward(w, None, w, dx=t), lambda t: fb.head_norm_rope(heads(w), None, None, None, None, None, q_out=heads(t))]
+    for write in writes:
+        saved, leaf = x.clone(), w.clone().requires_grad_(True)
+        y = fb.linear(saved, leaf)
+        write(saved)
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.sum().backward()
+        asked = x.clone().requires_grad_(True)
+        with pytest.raises(ValueError, match="gradient"):
+            write(asked)
+        with torch.no_grad():
+            write(asked)
+    with torch.inference_mode():
+        for write in writes:
+            write(torch.empty(64, 64, device=DEV, dtype=torch.bfloat16))
