@@ -924,8 +924,8 @@ cudaError_t launch_backward(const RowNormParams &p, int sms, int *parts, cudaStr
                             : lanes == 8    ? layer_norm_backward_kernel<X32, Y32, 8, VEC, 1>
                             : lanes == 16   ? layer_norm_backward_kernel<X32, Y32, 16, VEC, 1>
                             : p.dim <= 256  ? layer_norm_backward_kernel<X32, Y32, 32, VEC, 1>
-                            : p.dim <= 512  ? layer_norm_backward_kernel<X32, Y32, 32, VEC, 2>
-                                            : layer_norm_backward_kernel<X32, Y32, 32, VEC, VEC ? 2 : 4>;
+                            : VEC || p.dim <= 512 ? layer_norm_backward_kernel<X32, Y32, 32, VEC, 2>
+                                                  : layer_norm_backward_kernel<X32, Y32, 32, false, 4>;
         *parts = (int)grid;
         return launch_early(kernel, dim3(grid), 256, smem, stream, p);
     }
