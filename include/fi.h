@@ -731,8 +731,8 @@ fi_status_t fi_linear_poll_status(void);
  *   rows [tokens] device int32, nullable: row of x of each token (miss_idx of a cascade step); null: token i is row i.  A token whose row
  *   is outside [0, x_rows) is left out.  tokens_dev as in fi_linear; rows of out that are left out are untouched.
  * 1 <= dim <= 16384, strides between rows in elements, any alignment (16-byte boundaries and dim a multiple of 8 are faster).  out may
- * be x itself when types and rows are the same.  Arithmetic in fp32 (a row whose squares float32 does not hold has no finite norm),
- * rounded once.  Asynchronous, on the current device.
+ * be x itself when types and rows are the same.  Arithmetic in fp32 (a row whose squares float32 does not hold, above some
+ * 1e19, comes out as its bias: 1 / sqrt(infinity) is 0), rounded once.  Asynchronous, on the current device.
  *
  * fi_layer_norm_backward: gradients for dy [tokens x dim] (y_dtype), from the same x (nothing of the forward is kept):
  *   g = dy * weight;  out = dx = (g - mean(g) - n * mean(g * n)) / sqrt(...), with rms without mean(g);  dweight = sum of dy * n, dbias = sum of dy

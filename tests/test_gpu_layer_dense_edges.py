@@ -1,4 +1,5 @@
 """Edges of the layer's products and norm that go with what surrounds them: autograd's bookkeeping, empty streams, kernels launched early."""
+import math
 import os
 import subprocess
 import sys
@@ -116,3 +117,14 @@ def test_results_written_in_place_count_as_changes():
     with torch.inference_mode():
         for write in writes:
             write(torch.empty(64, 64, device=DEV, dtype=torch.bfloat16))
+
+
+def test_squares_that_float32_does_not_hold():
+    """1 / sqrt(infinity) is 0: such a row comes out as the bias, in short and in long rows."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for dim in (64, 1000, 4096):
+        x, w, b = rand(gen, 1300, dim), rand(gen, dim), rand(gen, dim)
+        x[3] = 1e25 * rand(gen, dim)
+        y = fb.layer_norm(x, w, b)
+        assert torch.equal(y[3], b) and not torch.equal(y[4], b) and not y.isnan().any()
+        assert math.isfinite(fb.layer_norm_backward(x, w, torch.ones_like(x))[0][3].abs().max().item())
