@@ -860,11 +860,8 @@ class ForkOut:
         self.copies = copies.view(batch, 3)
 
 
-def _written(*tensors: Optional[torch.Tensor]) -> None:
-    """Tells autograd that a call has written to tensors that were there before it: gradients that still need what they held are refused then."""
-    for t in tensors:
-        if t is not None:
-            torch.autograd.graph.increment_version(t)
+# Tells autograd that a call has written to a tensor that was there before it: gradients that still need what it held are refused then
+_written = torch.autograd.graph.increment_version
 
 
 def _no_gradient(name: str, *tensors: Optional[torch.Tensor]) -> None:
@@ -950,7 +947,9 @@ def head_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], q_weight: Optiona
     _no_gradient("q_out, k_out", q_out, k_out)
     res = _norm_rope_call(load_library().fi_head_norm_rope, q, k, q_weight, k_weight, rope, positions, eps, interleaved, count,
                           q_out, k_out)
-    _written(q_out, k_out)
+    for t in (q_out, k_out):
+        if t is not None:
+            _written(t)
     return res
 
 
@@ -1099,7 +1098,10 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
         return _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
     _no_gradient("out, preact", out, preact)
     y = _linear_call(x, weight, bias, activation, residual, out, rows, count, out_dtype, preact, wait_limit)
-    _written(out, preact)
+    if out is not None:
+        _written(out)
+    if preact is not None:
+        _written(preact)
     return y
 
 
@@ -1117,9 +1119,9 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
         in_dim = 8                                         # nothing but dbias
     else:
         in_dim = (x if x is not None else weight).shape[-1]
-    given = [t for t in (dx, dweight) if t is not None]
-    if given:
-        _no_gradient("dx, dweight", *given)
+    dx_given, dweight_given = dx, dweight
+    if dx is not None or dweight is not None:
+        _no_gradient("dx, dweight", dx, dweight)
     strides = [0, 0, _check_rows(dy, "dy", index, dy_dtype, tokens, out_dim), 0, 0, 0]
     if weight is not None:
         strides[1] = _check_rows(weight, "weight", index, torch.bfloat16, out_dim, in_dim)
@@ -1148,8 +1150,10 @@ def linear_backward(x: Optional[torch.Tensor], weight: Optional[torch.Tensor], d
     args = _pack_linear_backward(_at(x), _at(weight), dy.data_ptr(), _at(preact) if kind else 0, _at(dx), _at(dweight), _at(dbias), _at(work),
                                  *strides, tokens, wait_limit, in_dim, out_dim, kind, 1 if wide else 0)
     _on_device(index, lib.fi_linear_backward, args)
-    if given:
-        _written(*given)
+    if dx_given is not None:
+        _written(dx_given)
+    if dweight_given is not None:
+        _written(dweight_given)
     return dx, dweight, dbias
 
 
@@ -1242,7 +1246,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
         return _LayerNorm.apply(x, weight, bias, eps, rms, out_dtype, wait_limit)
     if out is None:
         return _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit)
-    _no_gradient("out", out)
+    if out.requires_grad:
+        _no_gradient("out", out)
     _layer_norm_call(x, weight, bias, eps, rms, out_dtype, rows, count, out, wait_limit)
     _written(out)
     return out
