@@ -661,8 +661,10 @@ __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_ring_k
 
 // Gradients.  With d = x - mean and t = dy d the sums of a row are those of d^2, g = dy w and t w, all at once:
 //   along = mean(g n) = r mean(t w);  dw += r t;  dx = r g - r mean(g) - r along d r
-// 8,191 rows of 4,096 take 54 us with the sums' kernel, 3.7 TB/s.  What bounds it: the instructions, 430 per warp and row, a quarter of them for the
-// two rounds of sums, at 16 working warps per SM, which 96 registers leave.  (Without the checks for rows that do not fill the threads: 60 us.)
+// 8,191 rows of 4,096 take 53 us with the sums' kernel, 3.8 TB/s.  What bounds it: latency.  Issue slots are 53 % full; a warp waits for shared memory and
+// shuffles most of the time between two of its 430 instructions a row, in two rounds of sums one after the other, at 16 working warps per SM, which
+// 96 registers leave.  (Without the checks for rows that do not fill the threads: 60 us.)  Rows of more than 8,192 values, 32 of each array a
+// thread, spill 464 to 480 bytes.
 template <bool X32, bool Y32, bool RMS, int THREADS, int P, int R>
 __global__ void __launch_bounds__(THREADS + 32, 512 / THREADS) layer_norm_backward_ring_kernel(const RowNormParams p, int stages) {
     __shared__ __align__(16) float s1[4 * R * 16], s3[4 * 3 * R * 16];

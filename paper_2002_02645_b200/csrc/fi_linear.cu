@@ -449,7 +449,7 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
 
 // Few tiles: a CTA takes 128 output columns and up to 256 output rows; `split` CTAs of a cluster share its reduction, so that the SMs have
 // work where the tiles alone are fewer than they are.  Sums of four rows go to CTA (row / 4) mod split, which adds them up in the order of
-// the ranks.  Bound by the latency from the launch to the last store (one token 2,048 -> 2,560: 8.8 us from one call to the next), and by the
+// the ranks.  Bound by the latency from the start to the last store (one token 2,048 -> 2,560: 5.2 us; its call takes the host 8.2), and by the
 // operands' way from memory (48 tokens 4,096 -> 16,384: 28 us for 134 MB of weights, 4.8 TB/s): the loader sets up its barriers and has all
 // stages on the way before the CTA has its TMEM.  LONG: more pieces of the reduction than accumulators, which take turns: a
 // kernel of its own, as its tests cost the other one up to 2 % (16 tokens 8,192 -> 8,192 in float32 24.5 -> 24.9 us).
